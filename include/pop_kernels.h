@@ -188,6 +188,81 @@ int pop_k_decode_attention_static(const void* q, int64_t ldq, const void* k_pool
                                   void* out, int64_t ldo, int32_t batch, int32_t n_q, int32_t n_kv,
                                   int32_t head_dim, int32_t kv_len, int32_t window, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------
+ * 8-bit paged cache: half the bytes of pop_kv_cache_t. One layer consists of
+ *   k_codes, v_codes: uint8 [num_pages][n_kv][page_size][hd], OCP E4M3 codes (16-byte aligned);
+ *   k_scales, v_scales: uint8 [num_pages][n_kv][page_size / 16], one E8M0 scale (a power of two, stored as its
+ *     exponent + 127) for each block of 16 positions and kv head:  value = code * 2^(scale - 127);
+ *   block_table, page_size, num_pages, max_pages_per_seq as in pop_kv_cache_t (page_size 16, 32, 64 or a multiple of
+ *     128; a page serves K and V alike). Positions of one page and head are contiguous.
+ * The scale of a block is the smallest power of two s >= 2^-64 with max |value| <= 448 s (NaN does not count; infinities
+ * make it 2^120), a code is value / s rounded to nearest even, saturating at 448 (NaN stays NaN). hd is 64, 128 or 256.
+ * Device-side checks in every call: a block-table entry outside [0, num_pages), a length above the stated maximum, a
+ * rotation row outside the table are never turned into addresses; the status word is raised to POP_E_INVALID and what
+ * depends on them is not written or reads as zeros. The codes behind a sequence's last position are left as they are.
+ *
+ * pop_k_quant_cache_e4m3: the bf16 cache that a prefill left, for `layers` consecutive layers (src_layer_stride elements,
+ *   code_layer_stride and scale_layer_stride bytes apart), positions 0 .. n-1 of every sequence, n = seq_lens[b] (device
+ *   int32 [batch], each <= max_len) or max_len for all if seq_lens is NULL. The two caches have tables of their own. */
+int pop_k_quant_cache_e4m3(const void* k_pool, const void* v_pool, int64_t src_layer_stride, const int32_t* src_table,
+                           int32_t src_page_size, int32_t src_num_pages, int32_t src_max_pages_per_seq, void* k_codes,
+                           void* v_codes, void* k_scales, void* v_scales, int64_t code_layer_stride,
+                           int64_t scale_layer_stride, const int32_t* block_table, int32_t page_size,
+                           int32_t num_pages, int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_len,
+                           int32_t layers, int32_t batch, int32_t n_kv, int32_t head_dim, void* stream);
+
+/* pop_k_rope_cache for the 8-bit cache (paper Eq. 2-3; Eq. 14 with n_q = 0), with a position per sequence and rotations
+ * over several axes. in: projections [q heads | k heads | v heads] * hd, fp32 or (in_bf16) bf16, row stride ld_in (a
+ * multiple of 4; 16-byte aligned). Sequence b owns the packed rows cu_rows[b] .. cu_rows[b + 1] - 1 (device int32
+ * [batch + 1], at most max_rows each), or rows b * max_rows .. if cu_rows is NULL; its first row goes to cache position
+ * start[b] (device int32 [batch]) or pos0 for all if start is NULL. Per row: optional per-head RMSNorm of q and k
+ * (q_gain / k_gain fp32 [hd] or NULL; eps), rotation of q and k, q to q_out (bf16, row stride ldq, a multiple of 4), k and
+ * v to the cache.
+ *   Rotation: pair (j, j + hd/2) turns by rope_table[p][j] = (cos, sin), float2 [table_rows][hd/2]. p is the cache position
+ * if positions is NULL, else positions[axis * ld_pos + row] (device int32 [n_axes][ld_pos], row = packed row) with axis =
+ * pair_axis[j] (device uint8 [hd/2], values < n_axes; NULL: axis 0): time, height and width of image and video tokens,
+ * in sections or interleaved as the model has it.
+ *   Scales: a block whose 16 positions all come from this call, or whose earlier positions are all new, gets the scale of its
+ * rows. A block that holds earlier positions (start not a multiple of 16) keeps the larger of its scale and the one the new
+ * rows need, and its codes are brought to it. Positions at or behind `start` count as empty, whatever is there: a sequence
+ * may be cut back and appended to again. Two sequences of one call may share pages only in front of both starts' blocks. */
+int pop_k_rope_cache_e4m3(const void* in, int32_t in_bf16, int64_t ld_in, const int32_t* cu_rows, int32_t max_rows,
+                          const int32_t* start, int32_t pos0, int32_t batch, void* q_out, int64_t ldq, void* k_codes,
+                          void* v_codes, void* k_scales, void* v_scales, const int32_t* block_table, int32_t page_size,
+                          int32_t num_pages, int32_t max_pages_per_seq, const float* q_gain, const float* k_gain,
+                          float eps, const void* rope_table, int32_t table_rows, const int32_t* positions,
+                          int64_t ld_pos, const void* pair_axis, int32_t n_axes, int32_t n_q, int32_t n_kv,
+                          int32_t head_dim, void* stream);
+
+/* Workspace of the two calls below: device memory, 16-byte aligned, contents irrelevant before and after. This size
+ * covers every call; a smaller one is refused with POP_E_NOSPACE where the call needs more, NULL is taken where it needs
+ * none. Calls that may overlap on the GPU (other streams, concurrently replayed graphs) need one each. */
+#define POP_E4M3_WORKSPACE_BYTES (64 * 1024 * 1024)
+
+/* pop_k_decode_attention over the 8-bit cache, with a length per sequence: one query per sequence at position
+ * len - 1, len = seq_lens[b] (device int32 [batch], each <= kv_len) or kv_len for all if seq_lens is NULL, over the last
+ * `window` positions (0: all). q bf16 [batch][ldq], out bf16 [batch][ldo] (strides multiples of 8, 16-byte aligned), any
+ * n_q that is a multiple of n_kv. A sequence of length 0 gets a row of zeros. batch <= 16384. Work is split evenly over the
+ * GPU whatever the lengths are; results do not depend on scheduling. */
+int pop_k_decode_attention_e4m3(const void* q, int64_t ldq, const void* k_codes, const void* v_codes,
+                                const void* k_scales, const void* v_scales, const int32_t* block_table,
+                                int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq,
+                                const int32_t* seq_lens, int32_t kv_len, void* workspace, size_t workspace_bytes,
+                                void* out, int64_t ldo, int32_t batch, int32_t n_q, int32_t n_kv, int32_t head_dim,
+                                int32_t window, void* stream);
+
+/* pop_k_attention over the 8-bit cache: the last rows of each sequence are its queries (a whole prompt, a chunk of it,
+ * a few drafted tokens). Sequence b has n = cu_rows[b + 1] - cu_rows[b] packed rows (device int32 [batch + 1], each n <=
+ * max_rows), or max_rows rows each if cu_rows is NULL, and len cached positions (seq_lens / kv_len as above) which include
+ * the rows' own: row i sits at position len - n + i and sees positions j <= its own, and j > its own - window if window > 0.
+ * A row that sees nothing (a length below its sequence's rows) becomes zeros. Rows of no sequence are left as they are.
+ * NaN codes inside a sequence may reach rows that do not see them. */
+int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int32_t max_rows, const void* k_codes,
+                         const void* v_codes, const void* k_scales, const void* v_scales, const int32_t* block_table,
+                         int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, const int32_t* seq_lens,
+                         int32_t kv_len, void* workspace, size_t workspace_bytes, void* out, int64_t ldo,
+                         int32_t batch, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t window, void* stream);
+
 /* Synchronise the stream, then read and clear the library's device status word. */
 int pop_k_status(void* stream);
 

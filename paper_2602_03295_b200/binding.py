@@ -20,6 +20,7 @@ POP_E_NOSPACE = -2
 POP_E_CUDA = -3
 POP_E_DEVICE_TIMEOUT = -4
 POP_E_MISSING = -5
+POP_E4M3_WORKSPACE_BYTES = 64 << 20     # workspace that covers every attention call over the 8-bit cache
 
 
 class PopError(RuntimeError):
@@ -102,6 +103,14 @@ SIGNATURES = {
     "pop_k_decode_attention_qkv": (C.c_int, [_P, _I64, _P, _P, C.c_float, _P, _P, _P, _P, _I32, _I32, _I32, _P, _P, _P,
                                              _I64] + [_I32] * 6 + [_P]),
     "pop_k_decode_attention_static": (C.c_int, [_P, _I64, _P, _P, _P, _I32, _I32, _P, _I64] + [_I32] * 6 + [_P]),
+    "pop_k_quant_cache_e4m3": (C.c_int, [_P, _P, _I64, _P, _I32, _I32, _I32, _P, _P, _P, _P, _I64, _I64, _P, _I32, _I32,
+                                         _I32, _P] + [_I32] * 5 + [_P]),
+    "pop_k_rope_cache_e4m3": (C.c_int, [_P, _I32, _I64, _P, _I32, _P, _I32, _I32, _P, _I64, _P, _P, _P, _P, _P, _I32, _I32,
+                                        _I32, _P, _P, _F, _P, _I32, _P, _I64, _P] + [_I32] * 4 + [_P]),
+    "pop_k_decode_attention_e4m3": (C.c_int, [_P, _I64, _P, _P, _P, _P, _P, _I32, _I32, _I32, _P, _I32, _P, C.c_size_t,
+                                              _P, _I64] + [_I32] * 5 + [_P]),
+    "pop_k_attention_e4m3": (C.c_int, [_P, _I64, _P, _I32, _P, _P, _P, _P, _P, _I32, _I32, _I32, _P, _I32, _P, C.c_size_t,
+                                       _P, _I64] + [_I32] * 5 + [_P]),
     "pop_k_profile": (None, [_I32]),
     "pop_k_profile_summary": (C.c_int, [_I32, C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(_I64)]),
     "pop_k_status": (C.c_int, [_P]),
@@ -365,6 +374,138 @@ class PopLibrary:
         self.check(code, "pop_k_decode_attention_static")
         return out
 
+    # -------------------------------------------------------------- 8-bit paged cache
+    # One layer of it: k8 / v8 uint8 codes [pages, n_kv, page_size, hd], ks / vs uint8 E8M0 scales
+    # [pages, n_kv, page_size / 16], block_table int32 [batch, max_pages] (KVCacheE4M3 holds them for all layers).
+    @staticmethod
+    def _cache8(k8, v8, ks, vs, block_table, n_kv, hd, *others):
+        """Checks what the C call cannot see, that all tensors (`others` too) are on the current CUDA device among it;
+        returns (page_size, num_pages, max_pages)."""
+        at = k8.get_device()
+        if at < 0 or at != torch.cuda.current_device() or \
+                any(t is not None and t.get_device() != at for t in (v8, ks, vs, block_table) + others):
+            raise PopError(POP_E_INVALID, "8-bit cache: all tensors have to be on the current CUDA device")
+        pages, heads, page, d = k8.shape
+        if heads != n_kv or d != hd or v8.shape != k8.shape or ks.shape != (pages, n_kv, page // 16) or ks.shape != vs.shape:
+            raise PopError(POP_E_INVALID, "8-bit cache: shapes of codes and scales do not belong together")
+        if not (k8.dtype == v8.dtype == ks.dtype == vs.dtype == torch.uint8) or block_table.dtype != torch.int32:
+            raise PopError(POP_E_INVALID, "8-bit cache: uint8 codes and scales and an int32 block table are wanted")
+        if not (k8.is_contiguous() and v8.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()
+                and block_table.is_contiguous()):
+            raise PopError(POP_E_INVALID, "8-bit cache: one layer's tensors and the block table have to be contiguous")
+        return page, pages, block_table.shape[1]
+
+    @staticmethod
+    def _ints(t, n, what, like):
+        """Pointer of an optional int32 device vector of n entries."""
+        if t is None:
+            return None
+        if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.device != like.device:
+            raise PopError(POP_E_INVALID, f"{what}: contiguous int32 [{n}] on {like.device} is wanted")
+        return t.data_ptr()
+
+    def quant_cache_e4m3(self, k_pool, v_pool, src_table, k8, v8, ks, vs, block_table, max_len, seq_lens=None, stream=None):
+        """pop_k_quant_cache_e4m3: pools bf16 [layers, pages, page_size, n_kv, hd] -> codes uint8 [layers, pages, n_kv,
+        page_size, hd] and scales uint8 [layers, pages, n_kv, page_size / 16]; seq_lens int32 [batch] or None (max_len)."""
+        layers, src_pages, src_page, n_kv, hd = k_pool.shape
+        if k8.dim() != 5 or not (k8.shape[0] == v8.shape[0] == ks.shape[0] == vs.shape[0] == layers) or \
+                k_pool.dtype != torch.bfloat16 or v_pool.dtype != torch.bfloat16 or v_pool.shape != k_pool.shape:
+            raise PopError(POP_E_INVALID, "quant_cache_e4m3: pools, codes and scales of the same layers are wanted")
+        page, pages, max_pages = self._cache8(k8[0], v8[0], ks[0], vs[0], block_table, n_kv, hd, k_pool, v_pool, src_table)
+        batch = block_table.shape[0]
+        if src_table.shape[0] != batch or src_table.dtype != torch.int32 or not src_table.is_contiguous() or \
+                not (k_pool[0].is_contiguous() and v_pool[0].is_contiguous()) or \
+                k_pool.stride(0) != v_pool.stride(0) or k8.stride(0) != v8.stride(0) or ks.stride(0) != vs.stride(0):
+            raise PopError(POP_E_INVALID, "quant_cache_e4m3: layers contiguous and alike for K and V, tables of one batch")
+        code = self.dll.pop_k_quant_cache_e4m3(
+            k_pool.data_ptr(), v_pool.data_ptr(), k_pool.stride(0), src_table.data_ptr(), src_page, src_pages,
+            src_table.shape[1], k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), k8.stride(0), ks.stride(0),
+            block_table.data_ptr(), page, pages, max_pages, self._ints(seq_lens, batch, "seq_lens", k8), max_len, layers,
+            batch, n_kv, hd, _stream_ptr(stream))
+        self.check(code, "pop_k_quant_cache_e4m3")
+
+    def rope_cache_e4m3(self, x, q_out, k8, v8, ks, vs, block_table, rope_table, n_q, n_kv, hd, max_rows, start=None,
+                        pos0=0, cu_rows=None, q_gain=None, k_gain=None, eps=0.0, positions=None, pair_axis=None,
+                        stream=None):
+        """pop_k_rope_cache_e4m3: x fp32 or bf16 [rows, (n_q + 2 n_kv) hd]; q_out bf16 [rows, n_q hd] (None if n_q is 0);
+        rope_table fp32 [positions, hd / 2, 2]; start int32 [batch] or pos0 for all; cu_rows int32 [batch + 1] or max_rows rows
+        each; positions int32 [axes, rows] with pair_axis uint8 [hd / 2] for rotations over several axes."""
+        page, pages, max_pages = self._cache8(k8, v8, ks, vs, block_table, n_kv, hd, x, q_out, rope_table, q_gain, k_gain,
+                                              positions, pair_axis)
+        batch, rows = block_table.shape[0], x.shape[0]
+        if x.dtype not in (torch.float32, torch.bfloat16) or x.shape[1] != (n_q + 2 * n_kv) * hd or x.stride(1) != 1 or \
+                (cu_rows is None and rows != batch * max_rows):
+            raise PopError(POP_E_INVALID, "rope_cache_e4m3: x is fp32 or bf16 [rows, (n_q + 2 n_kv) hd], rows as stated")
+        if n_q and (q_out.dtype != torch.bfloat16 or q_out.shape != (rows, n_q * hd) or q_out.stride(1) != 1):
+            raise PopError(POP_E_INVALID, "rope_cache_e4m3: q_out is bf16 [rows, n_q hd]")
+        if rope_table.dtype != torch.float32 or rope_table.numel() % hd or not rope_table.is_contiguous():
+            raise PopError(POP_E_INVALID, "rope_cache_e4m3: rope_table is fp32 [positions, hd / 2, 2]")
+        axes, ld_pos = 0, 0
+        if positions is not None:
+            axes, ld_pos = positions.shape[0], positions.stride(0)
+            if positions.dtype != torch.int32 or positions.shape[1] != rows or positions.stride(1) != 1:
+                raise PopError(POP_E_INVALID, "rope_cache_e4m3: positions is int32 [axes, rows]")
+        if pair_axis is not None and (pair_axis.dtype != torch.uint8 or pair_axis.numel() != hd // 2
+                                      or not pair_axis.is_contiguous()):
+            raise PopError(POP_E_INVALID, "rope_cache_e4m3: pair_axis is uint8 [hd / 2]")
+        for g in (q_gain, k_gain):
+            if g is not None and (g.dtype != torch.float32 or g.numel() != hd or not g.is_contiguous()):
+                raise PopError(POP_E_INVALID, "rope_cache_e4m3: gains are fp32 [hd]")
+        if rows == 0:
+            return q_out
+        code = self.dll.pop_k_rope_cache_e4m3(
+            x.data_ptr(), 1 if x.dtype == torch.bfloat16 else 0, x.stride(0), self._ints(cu_rows, batch + 1, "cu_rows", x),
+            max_rows, self._ints(start, batch, "start", x), pos0, batch, _ptr(q_out) if n_q else None,
+            q_out.stride(0) if n_q else 0, k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(),
+            block_table.data_ptr(), page, pages, max_pages, _ptr(q_gain), _ptr(k_gain), eps, rope_table.data_ptr(),
+            rope_table.numel() // hd, _ptr(positions), ld_pos, _ptr(pair_axis), axes, n_q, n_kv, hd, _stream_ptr(stream))
+        self.check(code, "pop_k_rope_cache_e4m3")
+        return q_out
+
+    def _attn8_args(self, q, k8, v8, ks, vs, block_table, out, n_q, n_kv, hd, workspace):
+        page, pages, max_pages = self._cache8(k8, v8, ks, vs, block_table, n_kv, hd, q, out, workspace)
+        if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or q.shape != out.shape or q.shape[1] != n_q * hd or \
+                q.stride(1) != 1 or out.stride(1) != 1:
+            raise PopError(POP_E_INVALID, "q and out are bf16 [rows, n_q hd]")
+        if workspace is None:
+            workspace = torch.empty(POP_E4M3_WORKSPACE_BYTES, dtype=torch.uint8, device=q.device)
+        elif not workspace.is_contiguous():
+            raise PopError(POP_E_INVALID, "workspace has to be contiguous")
+        return page, pages, max_pages, workspace, workspace.numel() * workspace.element_size()
+
+    def decode_attention_e4m3(self, q, k8, v8, ks, vs, block_table, out, n_q, n_kv, hd, kv_len, seq_lens=None, window=0,
+                              workspace=None, stream=None):
+        """pop_k_decode_attention_e4m3: q, out bf16 [batch, n_q hd]; seq_lens int32 [batch] (each <= kv_len) or kv_len for
+        all. `workspace` (POP_E4M3_WORKSPACE_BYTES of any dtype) is allocated if not given."""
+        page, pages, max_pages, ws, nbytes = self._attn8_args(q, k8, v8, ks, vs, block_table, out, n_q, n_kv, hd, workspace)
+        batch = q.shape[0]
+        if block_table.shape[0] != batch:
+            raise PopError(POP_E_INVALID, "decode_attention_e4m3: one query row and one block-table row per sequence")
+        code = self.dll.pop_k_decode_attention_e4m3(
+            q.data_ptr(), q.stride(0), k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), block_table.data_ptr(),
+            page, pages, max_pages, self._ints(seq_lens, batch, "seq_lens", q), kv_len, ws.data_ptr(), nbytes,
+            out.data_ptr(), out.stride(0), batch, n_q, n_kv, hd, window, _stream_ptr(stream))
+        self.check(code, "pop_k_decode_attention_e4m3")
+        return out
+
+    def attention_e4m3(self, q, k8, v8, ks, vs, block_table, out, n_q, n_kv, hd, max_rows, kv_len, cu_rows=None,
+                       seq_lens=None, window=0, workspace=None, stream=None):
+        """pop_k_attention_e4m3: q, out bf16 [rows, n_q hd], the last rows of each sequence (cu_rows int32 [batch + 1], or
+        max_rows rows each); seq_lens int32 [batch] cached positions, the rows' own included, or kv_len for all."""
+        page, pages, max_pages, ws, nbytes = self._attn8_args(q, k8, v8, ks, vs, block_table, out, n_q, n_kv, hd, workspace)
+        batch = block_table.shape[0]
+        if cu_rows is None and q.shape[0] != batch * max_rows:
+            raise PopError(POP_E_INVALID, "attention_e4m3: max_rows rows of every sequence, or cu_rows, are wanted")
+        if q.shape[0] == 0:
+            return out
+        code = self.dll.pop_k_attention_e4m3(
+            q.data_ptr(), q.stride(0), self._ints(cu_rows, batch + 1, "cu_rows", q), max_rows, k8.data_ptr(), v8.data_ptr(),
+            ks.data_ptr(), vs.data_ptr(), block_table.data_ptr(), page, pages, max_pages,
+            self._ints(seq_lens, batch, "seq_lens", q), kv_len, ws.data_ptr(), nbytes, out.data_ptr(), out.stride(0),
+            batch, n_q, n_kv, hd, window, _stream_ptr(stream))
+        self.check(code, "pop_k_attention_e4m3")
+        return out
+
 
 _LIB: Optional[PopLibrary] = None
 
@@ -419,6 +560,50 @@ class KVCache:
         pages = self.block_table[:, pos // self.page_size].long()          # [batch, n]
         slots = (pos % self.page_size)[None, :].expand_as(pages)
         return self.k[layer][pages, slots], self.v[layer][pages, slots]
+
+
+class KVCacheE4M3:
+    """Caller-owned 8-bit paged KV cache: E4M3 codes uint8 [n_layers, num_pages, n_kv, page_size, hd], one E8M0 scale per
+    block of 16 positions and kv head, uint8 [n_layers, num_pages, n_kv, page_size / 16], and an int32 block table
+    [batch, max_pages_per_seq] (identity paging unless `block_table` is given)."""
+
+    def __init__(self, cfg, batch: int, seq_len: int, page_size: int = 128, device="cuda",
+                 block_table: Optional[torch.Tensor] = None, num_pages: Optional[int] = None):
+        pps = (seq_len + page_size - 1) // page_size
+        self.page_size = page_size
+        self.num_pages = num_pages or batch * pps
+        shape = (cfg.n_layers, self.num_pages, cfg.n_kv_heads, page_size, cfg.head_dim)
+        self.k, self.v = (torch.zeros(shape, dtype=torch.uint8, device=device) for _ in range(2))
+        self.k_scale, self.v_scale = (torch.full(shape[:3] + (page_size // 16,), 63, dtype=torch.uint8, device=device)
+                                      for _ in range(2))
+        if block_table is None:
+            block_table = torch.arange(batch * pps, dtype=torch.int32).reshape(batch, pps)
+        self.block_table = block_table.to(device=device, dtype=torch.int32).contiguous()
+        self.batch, self.seq_len = batch, seq_len
+
+    def layer(self, layer: int):
+        """(codes K, codes V, scales K, scales V, block table) of 0-based `layer`, as the library's calls take them."""
+        return self.k[layer], self.v[layer], self.k_scale[layer], self.v_scale[layer], self.block_table
+
+    def fill_from(self, cache: KVCache, max_len: Optional[int] = None, seq_lens=None, library: Optional[PopLibrary] = None,
+                  stream=None):
+        """pop_k_quant_cache_e4m3: all layers of a bf16 cache, positions 0 .. n-1 (max_len, or seq_lens int32 [batch])."""
+        (library or lib()).quant_cache_e4m3(cache.k, cache.v, cache.block_table, self.k, self.v, self.k_scale, self.v_scale,
+                                            self.block_table, max_len or min(cache.seq_len, self.seq_len),
+                                            seq_lens=seq_lens, stream=stream)
+
+    def gather(self, layer: int, seq_len: Optional[int] = None):
+        """(K, V) of 0-based `layer` as dense bf16 [batch, seq_len, n_kv, hd]: code times scale is exact in bf16 (a
+        host-side view for checks)."""
+        n = seq_len or self.seq_len
+        pos = torch.arange(n, device=self.k.device)
+        pages = self.block_table[:, pos // self.page_size].long()          # [batch, n]
+        slots = (pos % self.page_size)[None, :].expand_as(pages)
+        out = []
+        for codes, scales in ((self.k, self.k_scale), (self.v, self.v_scale)):
+            e = (scales[layer][pages, :, slots // 16].int() << 23).view(torch.float32)
+            out.append((codes[layer][pages, :, slots].view(torch.float8_e4m3fn).float() * e[..., None]).bfloat16())
+        return tuple(out)
 
 
 class PopModel:

@@ -1,5 +1,5 @@
 // C-ABI wrappers for the kernel-level entry points declared in pop_kernels.h.
-#include "common.cuh"
+#include "cache8.cuh"
 #include "../../include/pop_kernels.h"
 
 using namespace pop;
@@ -199,6 +199,81 @@ const char* pop_strerror(int status) {
     case POP_E_MISSING: return "a required tensor is missing";
   }
   return "unknown status";
+}
+
+static Cache8 cache8(const void* k, const void* v, const void* ks, const void* vs, const int32_t* table,
+                     int32_t page_size, int32_t num_pages, int32_t max_pages) {
+  Cache8 c;
+  c.k = static_cast<uint8_t*>(const_cast<void*>(k)); c.v = static_cast<uint8_t*>(const_cast<void*>(v));
+  c.ks = static_cast<uint8_t*>(const_cast<void*>(ks)); c.vs = static_cast<uint8_t*>(const_cast<void*>(vs));
+  c.table = table; c.page_size = page_size; c.num_pages = num_pages; c.max_pages = max_pages;
+  return c;
+}
+
+int pop_k_quant_cache_e4m3(const void* k_pool, const void* v_pool, int64_t src_layer_stride, const int32_t* src_table,
+                           int32_t src_page_size, int32_t src_num_pages, int32_t src_max_pages_per_seq, void* k_codes,
+                           void* v_codes, void* k_scales, void* v_scales, int64_t code_layer_stride,
+                           int64_t scale_layer_stride, const int32_t* block_table, int32_t page_size,
+                           int32_t num_pages, int32_t max_pages_per_seq, const int32_t* seq_lens, int32_t max_len,
+                           int32_t layers, int32_t batch, int32_t n_kv, int32_t head_dim, void* stream) {
+  Quant8Args a{};
+  a.k = static_cast<const bf16*>(k_pool); a.v = static_cast<const bf16*>(v_pool); a.layer_stride = src_layer_stride;
+  a.table = src_table; a.page_size = src_page_size; a.num_pages = src_num_pages; a.max_pages = src_max_pages_per_seq;
+  a.dst = cache8(k_codes, v_codes, k_scales, v_scales, block_table, page_size, num_pages, max_pages_per_seq);
+  a.code_layer_stride = code_layer_stride; a.scale_layer_stride = scale_layer_stride;
+  a.seq_lens = seq_lens; a.max_len = max_len;
+  a.layers = layers; a.batch = batch; a.n_kv = n_kv; a.head_dim = head_dim;
+  return launch_quant_cache8(a, static_cast<cudaStream_t>(stream));
+}
+
+int pop_k_rope_cache_e4m3(const void* in, int32_t in_bf16, int64_t ld_in, const int32_t* cu_rows, int32_t max_rows,
+                          const int32_t* start, int32_t pos0, int32_t batch, void* q_out, int64_t ldq, void* k_codes,
+                          void* v_codes, void* k_scales, void* v_scales, const int32_t* block_table, int32_t page_size,
+                          int32_t num_pages, int32_t max_pages_per_seq, const float* q_gain, const float* k_gain,
+                          float eps, const void* rope_table, int32_t table_rows, const int32_t* positions,
+                          int64_t ld_pos, const void* pair_axis, int32_t n_axes, int32_t n_q, int32_t n_kv,
+                          int32_t head_dim, void* stream) {
+  Append8Args a{};
+  a.in = in; a.in_bf16 = in_bf16 != 0; a.ld_in = ld_in;
+  a.cu = cu_rows; a.rows = max_rows; a.start = start; a.pos0 = pos0; a.batch = batch;
+  a.q_out = static_cast<bf16*>(q_out); a.ldq = ldq;
+  a.dst = cache8(k_codes, v_codes, k_scales, v_scales, block_table, page_size, num_pages, max_pages_per_seq);
+  a.q_gain = q_gain; a.k_gain = k_gain; a.eps = eps;
+  a.table = static_cast<const float2*>(rope_table); a.table_rows = table_rows;
+  a.positions = positions; a.ld_pos = ld_pos; a.pair_axis = static_cast<const uint8_t*>(pair_axis); a.n_axes = n_axes;
+  a.n_q = n_q; a.n_kv = n_kv; a.head_dim = head_dim;
+  return launch_append8(a, static_cast<cudaStream_t>(stream));
+}
+
+int pop_k_decode_attention_e4m3(const void* q, int64_t ldq, const void* k_codes, const void* v_codes,
+                                const void* k_scales, const void* v_scales, const int32_t* block_table,
+                                int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq,
+                                const int32_t* seq_lens, int32_t kv_len, void* workspace, size_t workspace_bytes,
+                                void* out, int64_t ldo, int32_t batch, int32_t n_q, int32_t n_kv, int32_t head_dim,
+                                int32_t window, void* stream) {
+  Attn8Args a{};
+  a.q = static_cast<const bf16*>(q); a.ldq = ldq;
+  a.c = cache8(k_codes, v_codes, k_scales, v_scales, block_table, page_size, num_pages, max_pages_per_seq);
+  a.rows = 1; a.seq_lens = seq_lens; a.kv_len = kv_len;
+  a.out = static_cast<bf16*>(out); a.ldo = ldo;
+  a.batch = batch; a.n_q = n_q; a.n_kv = n_kv; a.head_dim = head_dim; a.window = window;
+  a.workspace = workspace; a.workspace_bytes = workspace ? workspace_bytes : 0;
+  return launch_decode_attention8(a, static_cast<cudaStream_t>(stream));
+}
+
+int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int32_t max_rows, const void* k_codes,
+                         const void* v_codes, const void* k_scales, const void* v_scales, const int32_t* block_table,
+                         int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, const int32_t* seq_lens,
+                         int32_t kv_len, void* workspace, size_t workspace_bytes, void* out, int64_t ldo,
+                         int32_t batch, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t window, void* stream) {
+  Attn8Args a{};
+  a.q = static_cast<const bf16*>(q); a.ldq = ldq;
+  a.c = cache8(k_codes, v_codes, k_scales, v_scales, block_table, page_size, num_pages, max_pages_per_seq);
+  a.cu = cu_rows; a.rows = max_rows; a.seq_lens = seq_lens; a.kv_len = kv_len;
+  a.out = static_cast<bf16*>(out); a.ldo = ldo;
+  a.batch = batch; a.n_q = n_q; a.n_kv = n_kv; a.head_dim = head_dim; a.window = window;
+  a.workspace = workspace; a.workspace_bytes = workspace ? workspace_bytes : 0;
+  return launch_attention8(a, static_cast<cudaStream_t>(stream));
 }
 
 int pop_k_status(void* stream) { return read_and_clear_status(static_cast<cudaStream_t>(stream)); }

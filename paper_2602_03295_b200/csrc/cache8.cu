@@ -1,0 +1,375 @@
+// Filling the 8-bit paged cache: conversion of a bf16 paged cache, and the append of a step's rows with per-head
+// RMSNorm and rotation (paper Eq. 2-3, Eq. 14) on the way.
+#include "cache8.cuh"
+
+namespace pop {
+
+int device_sms() {
+  static int sms = 0;
+  if (sms == 0) {
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1)
+      n = 148;
+    sms = n;
+  }
+  return sms;
+}
+
+namespace {
+
+constexpr uint32_t FULL = 0xffffffffu;
+
+__device__ __forceinline__ float warp_amax(float v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(FULL, v, o));
+  return v;
+}
+__device__ __forceinline__ void unpack_bf16x2(uint32_t w, float& a, float& b) {
+  a = __uint_as_float(w << 16);
+  b = __uint_as_float(w & 0xffff0000u);
+}
+
+// page of a position's block, or -1 (status word raised) for an entry or position that is no place in the pool
+__device__ __forceinline__ int page_of(const int32_t* table, int b, int max_pages, int num_pages, int page_index,
+                                       int* status, int lane) {
+  if (page_index < max_pages) {
+    const int page = table[(int64_t)b * max_pages + page_index];
+    if ((unsigned)page < (unsigned)num_pages) return page;
+  }
+  if (lane == 0) atomicMin(status, (int)POP_E_INVALID);
+  return -1;
+}
+
+// ------------------------------------------------------------------------------ bf16 cache -> 8-bit cache
+// One warp per (layer, K or V, sequence, block of 16 positions, kv head): hd / 8 lanes take one row, 16 bytes each;
+// all loads of the block go out before the maximum. 6 bytes move per pair of values, nothing else happens.
+struct Quant8Dev {
+  Quant8Args a;
+  int* status;
+};
+
+template <int HD>
+__global__ void __launch_bounds__(256) quant_cache8_kernel(const __grid_constant__ Quant8Dev p) {
+  constexpr int LPR = HD / 8, RPW = 32 / LPR, NP = C8_BLOCK / RPW;
+  const Quant8Args& a = p.a;
+  chain_trigger();
+  chain_wait();
+  const int lane = threadIdx.x & 31, sub = lane / LPR, col = (lane % LPR) * 8;
+  const int64_t item = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int h = (int)(item % a.n_kv), blk = (int)(item / a.n_kv), b = blockIdx.y;
+  const int layer = blockIdx.z >> 1;
+  const bool is_v = blockIdx.z & 1;
+  int n = a.seq_lens ? a.seq_lens[b] : a.max_len;
+  if (n > a.max_len) {
+    n = a.max_len;
+    if (lane == 0) atomicMin(p.status, (int)POP_E_INVALID);
+  }
+  const int pos = blk * C8_BLOCK;
+  if (pos >= n) return;
+  const int src_page = page_of(a.table, b, a.max_pages, a.num_pages, pos / a.page_size, p.status, lane);
+  const int dst_page = page_of(a.dst.table, b, a.dst.max_pages, a.dst.num_pages, pos / a.dst.page_size, p.status, lane);
+  if (src_page < 0 || dst_page < 0) return;
+  const bf16* src = (is_v ? a.v : a.k) + (int64_t)layer * a.layer_stride +
+                    (((int64_t)src_page * a.page_size + pos % a.page_size) * a.n_kv + h) * HD + col;
+  const int live = n - pos;            // rows of the block (from its first on) that hold something
+  uint4 raw[NP];
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int r = i * RPW + sub;
+    raw[i] = r < live ? *reinterpret_cast<const uint4*>(src + (int64_t)r * a.n_kv * HD) : make_uint4(0, 0, 0, 0);
+  }
+  float am = 0.f;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float x, y;
+      unpack_bf16x2(w[j], x, y);
+      am = fmaxf(am, fmaxf(fabsf(x), fabsf(y)));
+    }
+  }
+  const int e = c8_scale_exp(warp_amax(am));
+  const float inv = c8_pow2(127 - e);
+  const int slot = pos % a.dst.page_size;
+  const int64_t tile = (int64_t)dst_page * a.n_kv + h;
+  uint8_t* dst = (is_v ? a.dst.v : a.dst.k) + (int64_t)layer * a.code_layer_stride +
+                 (tile * a.dst.page_size + slot) * HD + col;
+  if (lane == 0)
+    ((is_v ? a.dst.vs : a.dst.ks) + (int64_t)layer * a.scale_layer_stride)[tile * (a.dst.page_size / C8_BLOCK) +
+                                                                          slot / C8_BLOCK] = (uint8_t)e;
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int r = i * RPW + sub;
+    if (r >= live) continue;
+    float f[8];
+    unpack_bf16x2(raw[i].x, f[0], f[1]);
+    unpack_bf16x2(raw[i].y, f[2], f[3]);
+    unpack_bf16x2(raw[i].z, f[4], f[5]);
+    unpack_bf16x2(raw[i].w, f[6], f[7]);
+    uint2 o;
+    o.x = c8_codes4(f[0] * inv, f[1] * inv, f[2] * inv, f[3] * inv);
+    o.y = c8_codes4(f[4] * inv, f[5] * inv, f[6] * inv, f[7] * inv);
+    *reinterpret_cast<uint2*>(dst + (int64_t)r * HD) = o;
+  }
+}
+
+// ------------------------------------------------------------------------------ norm + rotation + append
+// One warp per (sequence, block of 16 cache positions that the new rows touch, head). hd / 8 lanes take one row, each
+// four rotation pairs (j, j + hd/2): two 16-byte loads of fp32 (8-byte of bf16). A k or v head's rows all stay in
+// registers until the block's maximum is known; the eight warps of a CTA are eight heads of the same rows, so the
+// rotary rows come from L1 after the first.
+struct Append8Dev {
+  Append8Args a;
+  int* status;
+};
+
+template <int HD, bool IN_BF16>
+__global__ void __launch_bounds__(256) append8_kernel(const __grid_constant__ Append8Dev p) {
+  constexpr int LPR = HD / 8, RPW = 32 / LPR, NP = C8_BLOCK / RPW, HALF = HD / 2;
+  const Append8Args& a = p.a;
+  chain_trigger();
+  chain_wait();
+  const int lane = threadIdx.x & 31, sub = lane / LPR, j0 = (lane % LPR) * 4;
+  const int heads = a.n_q + 2 * a.n_kv;
+  const int head_groups = (heads + 7) / 8;
+  const int h = (int)(blockIdx.x % head_groups) * 8 + (threadIdx.x >> 5);
+  const int b = blockIdx.y;
+  if (h >= heads) return;
+  const int row0 = a.cu ? a.cu[b] : b * a.rows;
+  const int start = a.start ? a.start[b] : a.pos0;
+  int n = a.cu ? a.cu[b + 1] - row0 : a.rows;
+  const bool over = n > a.rows || start < 0 || start > 0x7ffffff0 - a.rows;
+  if (over && lane == 0) atomicMin(p.status, (int)POP_E_INVALID);
+  if (over || n <= 0) return;
+  const int first = start / C8_BLOCK * C8_BLOCK + (int)(blockIdx.x / head_groups) * C8_BLOCK;   // of this block
+  if (first >= start + n) return;
+  const int lo = max(start - first, 0), hi = min(start + n - first, C8_BLOCK);    // live slots of the block
+  const bool is_q = h < a.n_q, is_v = h >= a.n_q + a.n_kv;
+  const int64_t r_base = (int64_t)row0 + first - start;                           // packed row of slot 0
+
+  float x[NP][8];               // [.. 0..3] elements j0 + i, [.. 4..7] their partners j0 + i + hd/2
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int s = i * RPW + sub;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[i][u] = 0.f;
+    if (s < lo || s >= hi) continue;
+    const int64_t off = (r_base + s) * a.ld_in + (int64_t)h * HD + j0;
+    if constexpr (IN_BF16) {
+      const uint2 l = *reinterpret_cast<const uint2*>(static_cast<const bf16*>(a.in) + off);
+      const uint2 m = *reinterpret_cast<const uint2*>(static_cast<const bf16*>(a.in) + off + HALF);
+      unpack_bf16x2(l.x, x[i][0], x[i][1]);
+      unpack_bf16x2(l.y, x[i][2], x[i][3]);
+      unpack_bf16x2(m.x, x[i][4], x[i][5]);
+      unpack_bf16x2(m.y, x[i][6], x[i][7]);
+    } else {
+      const float4 l = *reinterpret_cast<const float4*>(static_cast<const float*>(a.in) + off);
+      const float4 m = *reinterpret_cast<const float4*>(static_cast<const float*>(a.in) + off + HALF);
+      x[i][0] = l.x; x[i][1] = l.y; x[i][2] = l.z; x[i][3] = l.w;
+      x[i][4] = m.x; x[i][5] = m.y; x[i][6] = m.z; x[i][7] = m.w;
+    }
+  }
+  float am = 0.f;
+  if (!is_v) {
+    const float* gain = is_q ? a.q_gain : a.k_gain;
+    float g[8];
+    if (gain != nullptr) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        g[u] = gain[j0 + u];
+        g[u + 4] = gain[j0 + u + HALF];
+      }
+    }
+    int axis[4] = {0, 0, 0, 0};
+    if (a.pair_axis != nullptr) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        axis[u] = a.pair_axis[j0 + u];
+        if (axis[u] >= a.n_axes) {           // never turned into an address
+          atomicMin(p.status, (int)POP_E_INVALID);
+          axis[u] = 0;
+        }
+      }
+    }
+    const bool one_axis = axis[0] == axis[1] && axis[1] == axis[2] && axis[2] == axis[3];
+    auto angle_row = [&](int ax, int64_t r, int pos) {
+      int t = a.positions ? a.positions[(int64_t)ax * a.ld_pos + r] : pos;
+      if ((unsigned)t >= (unsigned)a.table_rows) {      // never turned into an address
+        atomicMin(p.status, (int)POP_E_INVALID);
+        t = 0;
+      }
+      return a.table + (int64_t)t * HALF + j0;
+    };
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int s = i * RPW + sub;
+      const bool live = s >= lo && s < hi;
+      if (gain != nullptr) {
+        float ss = 0.f;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) ss = fmaf(x[i][u], x[i][u], ss);
+#pragma unroll
+        for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(FULL, ss, o);
+        const float rstd = rsqrtf(ss / (float)HD + a.eps);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[i][u] = x[i][u] * rstd * g[u];
+      }
+      if (live) {
+        float2 cs[4];
+        if (one_axis) {
+          const float4* t = reinterpret_cast<const float4*>(angle_row(axis[0], r_base + s, first + s));
+          const float4 t0 = t[0], t1 = t[1];
+          cs[0] = make_float2(t0.x, t0.y); cs[1] = make_float2(t0.z, t0.w);
+          cs[2] = make_float2(t1.x, t1.y); cs[3] = make_float2(t1.z, t1.w);
+        } else {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) cs[u] = angle_row(axis[u], r_base + s, first + s)[u];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const float c = x[i][u] * cs[u].x - x[i][u + 4] * cs[u].y;
+          const float d = x[i][u + 4] * cs[u].x + x[i][u] * cs[u].y;
+          x[i][u] = c;
+          x[i][u + 4] = d;
+        }
+      }
+      if (is_q && live) {
+        bf16* dst = a.q_out + (r_base + s) * a.ldq + (int64_t)h * HD + j0;
+        __nv_bfloat162 w0 = __floats2bfloat162_rn(x[i][0], x[i][1]), w1 = __floats2bfloat162_rn(x[i][2], x[i][3]);
+        __nv_bfloat162 w2 = __floats2bfloat162_rn(x[i][4], x[i][5]), w3 = __floats2bfloat162_rn(x[i][6], x[i][7]);
+        uint2 o;
+        o.x = *reinterpret_cast<uint32_t*>(&w0); o.y = *reinterpret_cast<uint32_t*>(&w1);
+        *reinterpret_cast<uint2*>(dst) = o;
+        o.x = *reinterpret_cast<uint32_t*>(&w2); o.y = *reinterpret_cast<uint32_t*>(&w3);
+        *reinterpret_cast<uint2*>(dst + HALF) = o;
+      }
+    }
+    if (is_q) return;
+  }
+#pragma unroll
+  for (int i = 0; i < NP; ++i)
+#pragma unroll
+    for (int u = 0; u < 8; ++u) am = fmaxf(am, fabsf(x[i][u]));      // dead slots are zeros
+  const int page = page_of(a.dst.table, b, a.dst.max_pages, a.dst.num_pages, first / a.dst.page_size, p.status, lane);
+  if (page < 0) return;
+  const int slot = first % a.dst.page_size;
+  const int64_t tile = (int64_t)page * a.n_kv + (h - a.n_q - (is_v ? a.n_kv : 0));
+  uint8_t* dst = (is_v ? a.dst.v : a.dst.k) + (tile * a.dst.page_size + slot) * HD + j0;
+  uint8_t* scale = (is_v ? a.dst.vs : a.dst.ks) + tile * (a.dst.page_size / C8_BLOCK) + slot / C8_BLOCK;
+  int e = c8_scale_exp(warp_amax(am));
+  if (lo > 0) {                 // the block holds earlier positions: their scale stays unless the new rows need a larger
+    const int was = *scale;
+    if (e > was) {              // bring their codes to it: exponents shift, small codes round again
+      const float f = c8_pow2(was - e);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        const int s = i * RPW + sub;
+        if (s >= lo) continue;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD + half * HALF);
+          const uint32_t l = c8_half2_lo(*w), m = c8_half2_hi(*w);
+          const float2 v0 = __half22float2(*reinterpret_cast<const __half2*>(&l));
+          const float2 v1 = __half22float2(*reinterpret_cast<const __half2*>(&m));
+          *w = c8_codes4(v0.x * f, v0.y * f, v1.x * f, v1.y * f);
+        }
+      }
+    } else {
+      e = was;
+    }
+  }
+  __syncwarp();                 // every lane has read the old scale
+  if (lane == 0) *scale = (uint8_t)e;
+  const float inv = c8_pow2(127 - e);
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    const int s = i * RPW + sub;
+    if (s < lo || s >= hi) continue;
+    *reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD) =
+        c8_codes4(x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv);
+    *reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD + HALF) =
+        c8_codes4(x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv);
+  }
+}
+
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+}  // namespace
+
+int launch_quant_cache8(const Quant8Args& a, cudaStream_t s) {
+  if (!a.k || !a.v || !a.table || !c8_cache_ok(a.dst)) return POP_E_INVALID;
+  if (a.layers < 1 || a.layers > 32767 || a.batch < 1 || a.batch > 65535 || a.n_kv < 1 || a.n_kv > 1024 ||
+      a.max_len < 0 || !page_size_ok(a.page_size) || a.num_pages < 1 || a.max_pages < 1)
+    return POP_E_INVALID;
+  if (a.head_dim != 64 && a.head_dim != 128 && a.head_dim != 256) return POP_E_INVALID;
+  if (!aligned(a.k, 16) || !aligned(a.v, 16) || a.layer_stride % 8 || a.code_layer_stride % 16) return POP_E_INVALID;
+  if ((int64_t)a.max_len > (int64_t)a.max_pages * a.page_size ||
+      (int64_t)a.max_len > (int64_t)a.dst.max_pages * a.dst.page_size)
+    return POP_E_NOSPACE;
+  if (a.max_len == 0) return POP_OK;
+  Quant8Dev p;
+  p.a = a;
+  p.status = status_word();
+  if (!p.status) return POP_E_CUDA;
+  const int64_t items = (((int64_t)a.max_len + C8_BLOCK - 1) / C8_BLOCK) * a.n_kv;
+  if ((items + 7) / 8 > 0x7fffffff) return POP_E_INVALID;
+  const dim3 grid((unsigned)((items + 7) / 8), a.batch, a.layers * 2);
+  ProfScope prof(PROF_ELEMENTWISE, (double)a.layers * a.batch * a.max_len * a.n_kv * a.head_dim * 6.0, s);
+  cudaError_t rc;
+  switch (a.head_dim) {
+    case 64: rc = launch_chained(quant_cache8_kernel<64>, grid, dim3(256), 0, s, p); break;
+    case 128: rc = launch_chained(quant_cache8_kernel<128>, grid, dim3(256), 0, s, p); break;
+    default: rc = launch_chained(quant_cache8_kernel<256>, grid, dim3(256), 0, s, p); break;
+  }
+  if (rc != cudaSuccess) return POP_E_CUDA;
+  count_launch();
+  return POP_OK;
+}
+
+int launch_append8(const Append8Args& a, cudaStream_t s) {
+  if (!a.in || !a.table || !c8_cache_ok(a.dst) || (a.n_q > 0 && !a.q_out)) return POP_E_INVALID;
+  if (a.batch < 1 || a.batch > 65535 || a.rows < 0 || a.n_q < 0 || a.n_kv < 1 || a.n_q > 4096 || a.n_kv > 1024 ||
+      a.pos0 < 0 || a.table_rows < 1)
+    return POP_E_INVALID;
+  if (a.head_dim != 64 && a.head_dim != 128 && a.head_dim != 256) return POP_E_INVALID;
+  if (a.positions != nullptr && a.n_axes < 1) return POP_E_INVALID;
+  if (a.pair_axis != nullptr && (a.positions == nullptr || a.n_axes > 255)) return POP_E_INVALID;
+  if (!aligned(a.in, 16) || !aligned(a.table, 16) || a.ld_in % 4 || (a.n_q > 0 && (!aligned(a.q_out, 8) || a.ldq % 4)))
+    return POP_E_INVALID;
+  if ((int64_t)a.batch * a.rows > 0x7fffffff) return POP_E_INVALID;
+  if (a.start == nullptr && (int64_t)a.pos0 + a.rows > (int64_t)a.dst.max_pages * a.dst.page_size) return POP_E_NOSPACE;
+  if (a.rows == 0) return POP_OK;
+  Append8Dev p;
+  p.a = a;
+  p.status = status_word();
+  if (!p.status) return POP_E_CUDA;
+  const int heads = a.n_q + 2 * a.n_kv;
+  // rows that start anywhere in a block touch at most this many blocks
+  const int64_t blocks = ((int64_t)a.rows + 2 * C8_BLOCK - 2) / C8_BLOCK;
+  const int64_t gx = blocks * ceil_div(heads, 8);
+  if (gx > 0x7fffffff) return POP_E_INVALID;
+  const dim3 grid((unsigned)gx, a.batch);
+  ProfScope prof(PROF_ELEMENTWISE,
+                 (double)a.batch * a.rows * a.head_dim * (heads * (a.in_bf16 ? 2.0 : 4.0) + a.n_q * 2.0 + a.n_kv * 2.0), s);
+  cudaError_t rc;
+  if (a.in_bf16) {
+    switch (a.head_dim) {
+      case 64: rc = launch_chained(append8_kernel<64, true>, grid, dim3(256), 0, s, p); break;
+      case 128: rc = launch_chained(append8_kernel<128, true>, grid, dim3(256), 0, s, p); break;
+      default: rc = launch_chained(append8_kernel<256, true>, grid, dim3(256), 0, s, p); break;
+    }
+  } else {
+    switch (a.head_dim) {
+      case 64: rc = launch_chained(append8_kernel<64, false>, grid, dim3(256), 0, s, p); break;
+      case 128: rc = launch_chained(append8_kernel<128, false>, grid, dim3(256), 0, s, p); break;
+      default: rc = launch_chained(append8_kernel<256, false>, grid, dim3(256), 0, s, p); break;
+    }
+  }
+  if (rc != cudaSuccess) return POP_E_CUDA;
+  count_launch();
+  return POP_OK;
+}
+
+}  // namespace pop

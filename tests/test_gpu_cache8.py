@@ -1,0 +1,594 @@
+"""The 8-bit paged cache on the GPU against plain 64-bit arithmetic (tests/cache8_ref.py): conversion, append with norm
+and rotation, single-query and prompt attention, and all of them together.
+
+Conversion is exact. Stored codes of the append are held to the interval that fp32 arithmetic allows: rounding is monotone,
+so a code must lie between the codes of the exact value minus and plus the bound of the fp32 error. Attention outputs are
+held elementwise to the bound that `cache8_ref.attend` derives."""
+import math
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+from tests import cache8_ref as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BLOCK = 16
+
+
+@pytest.fixture(scope="module")
+def L():
+    import paper_2602_03295_b200 as pk
+    return pk.lib()
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def random_cache(seed, layers, batch, length, n_kv, hd, page, spare=2):
+    """(k8, v8, ks, vs, table) on the CPU: every byte random, no NaN codes, shuffled pages."""
+    g = gen(seed)
+    each = max(1, -(-length // page))
+    pages = batch * each + spare
+    codes = [torch.randint(0, 256, (layers, pages, n_kv, page, hd), generator=g, dtype=torch.uint8) for _ in range(2)]
+    for c in codes:
+        c[(c & 127) == 127] = 9
+    scales = [torch.randint(115, 124, (layers, pages, n_kv, page // BLOCK), generator=g, dtype=torch.uint8) for _ in range(2)]
+    table = torch.randperm(pages, generator=g)[:batch * each].view(batch, each).int()
+    return codes[0], codes[1], scales[0], scales[1], table
+
+
+def poison_behind(cache, lens, layer=0):
+    """NaN codes and scales of 255 behind every sequence's end and in unused pages."""
+    k8, v8, ks, vs, table = cache
+    page = k8.shape[3]
+    live = torch.zeros(k8.shape[1], page, dtype=torch.bool)
+    for b, n in enumerate(lens):
+        pos = torch.arange(n)
+        live[table[b].long()[pos // page], pos % page] = True
+    for c in (k8, v8):
+        c[layer][(~live)[:, None, :].expand(-1, c.shape[2], -1)] = 0x7f
+    dead_blocks = ~live.view(live.shape[0], -1, BLOCK).any(-1)
+    for s in (ks, vs):
+        s[layer][dead_blocks[:, None, :].expand(-1, s.shape[2], -1)] = 255
+
+
+# ---------------------------------------------------------------------------------------------- conversion
+QUANT = [  # layers, lens, n_kv, hd, source page, page
+    (2, [1, 15, 16, 17, 0, 250], 2, 64, 16, 32), (1, [300], 3, 128, 128, 16), (3, [33, 129], 1, 256, 32, 128),
+    (1, [500, 128, 129], 8, 128, 64, 256), (1, [0], 1, 64, 16, 16), (2, [257], 5, 64, 384, 64),
+]
+
+
+@pytest.mark.parametrize("layers,lens,n_kv,hd,src_page,page", QUANT)
+def test_conversion_is_exact(L, layers, lens, n_kv, hd, src_page, page):
+    g, batch, top = gen(1), len(lens), max(max(lens), 1)
+    each = -(-top // src_page)
+    pages = batch * each + 2
+    shape = (layers, pages, src_page, n_kv, hd)
+    k = (torch.randn(shape, generator=g) * torch.exp(torch.randn(shape[:3] + (n_kv, 1), generator=g) * 3)).bfloat16()
+    v = (torch.randn(shape, generator=g) * 1e-3).bfloat16()
+    src = torch.randperm(pages, generator=g)[:batch * each].view(batch, each).int()
+    k8, v8, ks, vs, table = random_cache(2, layers, batch, top, n_kv, hd, page)
+    if lens[0] > 16:           # a block of zeros, one below the smallest scale, infinities and NaN
+        k[:, src[0, 0].long(), :16] = 0
+        v[:, src[0, 0].long(), :16] = 1e-25
+        at = (src[0, 16 // src_page].long(), 16 % src_page)
+        v[0, at[0], at[1], 0, :3] = torch.tensor([math.inf, math.nan, -math.inf]).bfloat16()
+    dev = [t.to(DEV) for t in (k, v, src, k8, v8, ks, vs, table)]
+    L.quant_cache_e4m3(*dev, top, seq_lens=torch.tensor(lens, dtype=torch.int32, device=DEV))
+    assert L.status() == 0
+    for x, codes, scales, got_c, got_s in ((k, k8, ks, dev[3], dev[5]), (v, v8, vs, dev[4], dev[6])):
+        want_c, want_s = ref.code_values(codes), scales.clone()
+        for b, n in enumerate(lens):
+            for p0 in range(0, n, BLOCK):
+                pos = torch.arange(p0, min(n, p0 + BLOCK))
+                for l in range(layers):
+                    y = x[l, src[b].long()[pos // src_page], pos % src_page].double()          # [rows, n_kv, hd]
+                    for h in range(n_kv):
+                        e = ref.scale_exp(float(y[:, h].abs().nan_to_num(0.0, posinf=math.inf).max()))
+                        pg = table[b].long()[p0 // page]
+                        want_s[l, pg, h, p0 % page // BLOCK] = e
+                        c = ref.round_e4m3((y[:, h] / 2.0 ** (e - 127)).nan_to_num(nan=0.0, posinf=1e9, neginf=-1e9))
+                        c[y[:, h].isnan()] = math.nan
+                        want_c[l, pg, h, pos % page] = c
+        assert torch.equal(got_s.cpu(), want_s)
+        assert torch.equal(ref.code_values(got_c.cpu()).nan_to_num(1e9), want_c.nan_to_num(1e9))
+
+
+def test_cache_object_round_trip(L):
+    from paper_2602_03295_b200.binding import KVCache, KVCacheE4M3
+    cfg = SimpleNamespace(n_layers=3, n_kv_heads=2, head_dim=128)
+    a = KVCache(cfg, 2, 200, 64)
+    a.k.copy_(torch.randn(a.k.shape, generator=gen(3)))
+    a.v.copy_(torch.randn(a.v.shape, generator=gen(4)))
+    c = KVCacheE4M3(cfg, 2, 200, 128)
+    c.fill_from(a)
+    for l in range(3):
+        for got, want in zip(c.gather(l), a.gather(l)):
+            d = (got.double() - want.double()).abs()
+            # half a step of E4M3, or half of its smallest code in the block's scale (at most 2^-9 / 2 of amax / 224)
+            assert (d <= 2.0 ** -4 * want.double().abs() + 2.0 ** -10 * want.double().abs().max() / 224).all()
+
+
+# ---------------------------------------------------------------------------------------------- append
+APPEND = [  # starts, rows of each, n_q, n_kv, hd, page, bf16 input, norm, axes
+    ([0], [1], 4, 2, 64, 16, False, False, 1), ([7, 16, 31, 0], [1, 1, 1, 1], 8, 2, 128, 32, True, True, 1),
+    ([5, 40], [70, 0], 3, 1, 128, 64, False, True, 3), ([0], [45], 2, 2, 256, 128, True, False, 3),
+    ([100, 3, 15], [1, 30, 2], 0, 3, 64, 16, False, False, 1), ([130], [17], 5, 1, 256, 384, False, True, 1),
+    ([12], [200], 12, 3, 64, 16, True, True, 3),
+]
+
+
+def append_inputs(case, seed=5, scale=1.0):
+    starts, rows, n_q, n_kv, hd, page, bf, norm, axes = case
+    g = gen(seed)
+    top = max(s + r for s, r in zip(starts, rows))
+    total = sum(rows)
+    x = torch.randn(total, (n_q + 2 * n_kv) * hd, generator=g) * scale
+    x = x.bfloat16() if bf else x
+    gains = [0.5 + torch.rand(hd, generator=g) if norm else None for _ in range(2)]
+    ang = torch.arange(top + 50)[:, None].double() * 1e4 ** (-torch.arange(0, hd, 2).double() / hd)
+    table = torch.stack([ang.cos(), ang.sin()], -1).float()
+    positions = torch.randint(0, top + 50, (axes, total), generator=g, dtype=torch.int32) if axes > 1 else None
+    pair_axis = (torch.arange(hd // 2) * 5 % 7 % axes).to(torch.uint8) if axes > 1 else None
+    cu = torch.tensor([sum(rows[:i]) for i in range(len(rows) + 1)], dtype=torch.int32)
+    return SimpleNamespace(x=x, gains=gains, rope=table, positions=positions, pair_axis=pair_axis, cu=cu, top=top,
+                           starts=torch.tensor(starts, dtype=torch.int32), eps=1e-5)
+
+
+def check_append(case, a, cache, got_q, got):
+    """`cache`: the CPU cache before the call; `got`: its four tensors after it."""
+    starts, rows, n_q, n_kv, hd, page, bf, norm, axes = case
+    k8, v8, ks, vs, table = cache
+    r = 0
+    left = [t[0].clone() for t in (k8, v8, ks, vs)]          # what must not change is compared at the end
+    touched = [torch.zeros_like(t, dtype=torch.bool) for t in left]
+    for b, (s0, n) in enumerate(zip(starts, rows)):
+        vals = {"k": [], "v": []}
+        for i in range(n):
+            x = a.x[r].double().view(-1, hd)
+            if a.positions is None:
+                cs = a.rope[s0 + i]
+            else:
+                cs = a.rope[a.positions[a.pair_axis.long(), r].long(), torch.arange(hd // 2)]
+            for part, gain, is_q in ((x[:n_q], a.gains[0], True), (x[n_q:n_q + n_kv], a.gains[1], False)):
+                y, err = ref.rotate(part, gain, a.eps, cs), ref.rotate_error(part, gain, a.eps, cs)
+                if is_q and n_q:
+                    d = (got_q[r].double().view(n_q, hd) - y).abs()
+                    assert (d <= 2.0 ** -8 * (y.abs() + err) + err).all()
+                elif not is_q:
+                    vals["k"].append((y, err))
+            vals["v"].append((x[n_q + n_kv:], torch.zeros_like(x[n_q + n_kv:])))
+            r += 1
+        for first in range(s0 // BLOCK * BLOCK, s0 + n if n else 0, BLOCK):
+            pg, slot = int(table[b, first // page]), first % page
+            lo, hi = max(s0 - first, 0), min(s0 + n - first, BLOCK)
+            for h in range(n_kv):
+                for which, ci, si in (("k", 0, 2), ("v", 1, 3)):
+                    y = torch.stack([vals[which][first + j - s0][0][h] for j in range(lo, hi)])
+                    err = torch.stack([vals[which][first + j - s0][1][h] for j in range(lo, hi)])
+                    e = int(got[si][pg, h, slot // BLOCK])
+                    low, high = (ref.scale_exp(max(0.0, float((y.abs() + sg * err).max()))) for sg in (-1, 1))
+                    old = int(left[si][pg, h, slot // BLOCK]) if lo else 0
+                    assert max(low, old) <= e <= max(high, old)
+                    sc = 2.0 ** (e - 127)
+                    code = ref.code_values(got[ci][pg, h, slot + lo:slot + hi])
+                    assert (code >= ref.round_e4m3((y - err) / sc)).all() and (code <= ref.round_e4m3((y + err) / sc)).all()
+                    if lo:
+                        before = ref.code_values(left[ci][pg, h, slot:slot + lo]) * 2.0 ** (old - e)
+                        assert torch.equal(ref.code_values(got[ci][pg, h, slot:slot + lo]), ref.round_e4m3(before))
+                    touched[ci][pg, h, slot:slot + hi] = True
+                    touched[si][pg, h, slot // BLOCK] = True
+    for t, m, g in zip(left, touched, got):
+        assert torch.equal(t[~m], g[~m])
+
+
+def run_append(L, case, a, cache, strided=False, **over):
+    starts, rows, n_q, n_kv, hd, page, bf, norm, axes = case
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]]
+    up = lambda t: None if t is None else t.to(DEV)  # noqa: E731
+    pad = 8 if strided else 0
+    x = torch.full((a.x.shape[0], a.x.shape[1] + pad), math.nan, dtype=a.x.dtype, device=DEV)
+    x[:, :a.x.shape[1]] = a.x.to(DEV)
+    q = torch.full((a.x.shape[0], n_q * hd + pad), 7.0, dtype=torch.bfloat16, device=DEV) if n_q else None
+    L.rope_cache_e4m3(x[:, :a.x.shape[1]], q[:, :n_q * hd] if n_q else None, *dev, up(cache[4]), up(a.rope), n_q, n_kv, hd,
+                      max(rows), **{**dict(start=up(a.starts), cu_rows=up(a.cu), q_gain=up(a.gains[0]),
+                                           k_gain=up(a.gains[1]), eps=a.eps, positions=up(a.positions),
+                                           pair_axis=up(a.pair_axis)), **over})
+    assert L.status() == 0
+    if n_q and strided:
+        assert (q[:, n_q * hd:] == 7.0).all()
+    return (q[:, :n_q * hd].cpu() if n_q else None), [t.cpu() for t in dev]
+
+
+@pytest.mark.parametrize("case", APPEND, ids=str)
+@pytest.mark.parametrize("strided", [False, True])
+def test_append(L, case, strided):
+    a = append_inputs(case)
+    cache = random_cache(6, 1, len(case[0]), a.top + 20, case[3], case[4], case[5])
+    check_append(case, a, cache, *run_append(L, case, a, cache, strided))
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-4, 3e4, 1e30])
+def test_append_with_scales_far_from_one(L, scale):
+    """Blocks whose scale has to grow by many powers of two (earlier codes vanish), or not at all."""
+    case = ([5, 20], [2, 9], 1, 2, 64, 32, False, False, 1)
+    a = append_inputs(case, 8, scale)
+    cache = random_cache(9, 1, 2, 64, 2, 64, 32)
+    check_append(case, a, cache, *run_append(L, case, a, cache))
+
+
+def test_append_uniform_form_and_zero_rows(L):
+    """cu_rows and start left out: max_rows rows of every sequence from pos0 on. And a call without rows does nothing."""
+    case = ([21, 21], [4, 4], 2, 1, 128, 16, False, True, 1)
+    a = append_inputs(case)
+    cache = random_cache(10, 1, 2, 48, 1, 128, 16)
+    check_append(case, a, cache, *run_append(L, case, a, cache, start=None, pos0=21, cu_rows=None))
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]]
+    L.rope_cache_e4m3(torch.empty(0, 4 * 128, device=DEV), torch.empty(0, 256, dtype=torch.bfloat16, device=DEV), *dev,
+                      cache[4].to(DEV), a.rope.to(DEV), 2, 1, 128, 0)
+    assert all(torch.equal(x.cpu(), y[0]) for x, y in zip(dev, cache[:4]))
+
+
+def test_appended_block_is_the_block_of_one_call(L):
+    """Appending a block's rows one by one leaves the scale of one call, and values within the two roundings of it."""
+    case = ([0], [48], 1, 2, 128, 16, False, False, 1)
+    a = append_inputs(case, 11)
+    a.x *= torch.exp(torch.linspace(-2, 2, 48))[:, None]          # growing: every scale grows inside its block
+    cache = random_cache(12, 1, 1, 48, 2, 128, 16)
+    _, once = run_append(L, case, a, cache)
+    cur = cache
+    for i in range(48):
+        one = SimpleNamespace(**{**vars(a), "x": a.x[i:i + 1], "starts": torch.tensor([i], dtype=torch.int32),
+                                 "cu": torch.tensor([0, 1], dtype=torch.int32)})
+        _, got = run_append(L, ([i], [1]) + case[2:], one, cur)
+        cur = [t[None] for t in got] + [cache[4]]
+    assert torch.equal(cur[2][0], once[2]) and torch.equal(cur[3][0], once[3])
+    for c in (0, 1):
+        x, y = (ref.read(t[c], t[2 + c], cache[4][0], 48) for t in ([t[0] for t in cur[:4]], once))
+        assert ((x - y).abs() <= 2.0 ** -10 * torch.exp2(torch.tensor(3.0)) * y.abs().amax() / 224 + 1e-12).all()
+
+
+def test_append_raises_the_status_for_bad_places(L):
+    from paper_2602_03295_b200 import POP_E_INVALID
+    case = ([0, 0], [3, 3], 1, 1, 64, 16, False, False, 3)
+    for what in ("page", "rotation", "axis", "rows", "start"):
+        a = append_inputs(case, 13)
+        cache = list(random_cache(14, 1, 2, 16, 1, 64, 16))
+        up = lambda t: t.to(DEV)  # noqa: E731
+        over = {}
+        if what == "page":
+            cache[4][1, 0] = 1000
+        elif what == "rotation":
+            a.positions[2, 1] = a.rope.shape[0]
+        elif what == "axis":
+            a.pair_axis[3] = 3
+        elif what == "rows":
+            a.cu = torch.tensor([0, 5, 6], dtype=torch.int32)
+        else:
+            a.starts[0] = -16
+        dev = [t[0].to(DEV).contiguous() for t in cache[:4]]
+        q = torch.empty(6, 64, dtype=torch.bfloat16, device=DEV)
+        L.rope_cache_e4m3(up(a.x), q, *dev, up(cache[4]), up(a.rope), 1, 1, 64, 3, start=up(a.starts), cu_rows=up(a.cu),
+                          positions=up(a.positions), pair_axis=up(a.pair_axis), **over)
+        assert L.status() == POP_E_INVALID and L.status() == 0
+        if what == "page":          # the sequence with a good table is stored, nothing else changes
+            pg = int(cache[4][0, 0])
+            keep = torch.ones(cache[0].shape[1], dtype=torch.bool)
+            keep[pg] = False
+            assert torch.equal(dev[0].cpu()[keep], cache[0][0][keep])
+            assert not torch.equal(dev[0].cpu()[pg], cache[0][0][pg])
+
+
+# ---------------------------------------------------------------------------------------------- attention
+def check_attention(q, got, cache, rows, lens, n_q, n_kv, hd, window, pick=None, shift=7):
+    k8, v8, ks, vs, table = cache
+    r0 = 0
+    for b, (n, ln) in enumerate(zip(rows, lens)):
+        ln = max(ln, 0)
+        k, v = (ref.read(c[0], s[0], table[b], ln).repeat_interleave(n_q // n_kv, 1) for c, s in ((k8, ks), (v8, vs)))
+        ev = ref.read_exponents(vs[0], table[b], vs.shape[3] * BLOCK, ln).repeat_interleave(n_q // n_kv, 1)
+        for i in (range(n) if pick is None else sorted({0, 1, n // 3, n // 2, n - 2, n - 1} & set(range(n)))):
+            at, pos = ln - n + i, torch.arange(ln)
+            seen = pos <= at
+            if window:
+                seen &= pos > at - window
+            want, tol = ref.attend(q[r0 + i].double().view(n_q, hd), k, v, seen, ev, shift)
+            d = (got[r0 + i].double().view(n_q, hd) - want).abs()
+            assert (d <= tol).all(), (b, i, (d / tol.clamp_min(1e-30)).max())
+        r0 += n
+
+
+def queries(seed, rows, n_q, hd, std=1.5, pad=0):
+    q = torch.randn(rows, n_q * hd + pad, generator=gen(seed)) * std
+    return q.bfloat16()
+
+
+DECODE = [  # lens, n_q, n_kv, hd, page, window
+    ([1], 1, 1, 64, 16, 0), ([0, 1, 15, 16, 17, 511, 512, 513], 4, 2, 128, 16, 0), ([2000, 3, 0, 77], 8, 1, 64, 32, 0),
+    ([5000], 32, 8, 128, 128, 0), ([900, 1300, 31], 6, 2, 256, 64, 0), ([700], 16, 1, 128, 384, 0), ([600, 601], 20, 2, 64, 64, 0),
+    ([3000, 100, 5], 8, 2, 128, 64, 1), ([3000, 100, 5], 10, 2, 128, 64, 100), ([1000, 1024, 1025], 4, 2, 256, 128, 1024),
+    ([3000, 40], 3, 3, 64, 16, 999), ([8192 + 5], 5, 1, 128, 256, 0), ([1] * 40 + [600] + [0] * 300 + [33] * 20, 4, 2, 64, 16, 0),
+    ([0, 0], 2, 1, 128, 16, 0),
+]
+
+
+@pytest.mark.parametrize("lens,n_q,n_kv,hd,page,window", DECODE, ids=lambda v: str(v)[:40])
+def test_decode_attention(L, lens, n_q, n_kv, hd, page, window):
+    cache = random_cache(20, 1, len(lens), max(max(lens), 1), n_kv, hd, page)
+    poison_behind(cache, lens)
+    q = queries(21, len(lens), n_q, hd)
+    out = torch.full(q.shape, math.nan, dtype=torch.bfloat16, device=DEV)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    L.decode_attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, max(lens), window=window,
+                            seq_lens=torch.tensor(lens, dtype=torch.int32, device=DEV))
+    assert L.status() == 0
+    check_attention(q, out.cpu(), cache, [1] * len(lens), lens, n_q, n_kv, hd, window)
+
+
+@pytest.mark.parametrize("length,hd,page", [(1, 128, 16), (16, 64, 16), (333, 128, 32), (640, 256, 128), (1500, 64, 64)])
+def test_decode_attention_with_equal_lengths_and_strides(L, length, hd, page):
+    n_q, n_kv, batch = 6, 2, 3
+    cache = random_cache(22, 1, batch, length, n_kv, hd, page)
+    q = queries(23, batch, n_q, hd, pad=24)
+    out = torch.full((batch, n_q * hd + 8), 5.0, dtype=torch.bfloat16, device=DEV)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    L.decode_attention_e4m3(q.to(DEV)[:, :n_q * hd], *dev, out[:, :n_q * hd], n_q, n_kv, hd, length)
+    assert L.status() == 0 and (out[:, n_q * hd:] == 5.0).all()
+    check_attention(q[:, :n_q * hd], out[:, :n_q * hd].cpu(), cache, [1] * batch, [length] * batch, n_q, n_kv, hd, 0)
+
+
+PROMPT = [  # rows, lens, n_q, n_kv, hd, page, window
+    ([1], [1], 1, 1, 64, 16, 0), ([5, 0, 1], [5, 30, 40], 4, 2, 128, 16, 0), ([130], [130], 2, 2, 128, 128, 0),
+    ([200, 64], [200, 64], 8, 2, 64, 64, 0), ([33, 7], [300, 1000], 8, 1, 128, 32, 0), ([70], [700], 6, 2, 256, 64, 0),
+    ([16, 16, 3], [2000, 16, 900], 5, 1, 128, 256, 0), ([300], [300], 3, 1, 64, 16, 50), ([260], [500], 4, 2, 128, 384, 64),
+    ([150, 20], [600, 700], 2, 1, 256, 128, 100), ([9, 4], [5, 2], 4, 2, 128, 16, 0), ([40], [4000], 7, 1, 64, 128, 0),
+    ([5] * 12, [900 - 60 * i for i in range(12)], 16, 4, 128, 32, 0), ([129], [129], 1, 1, 256, 16, 1),
+    ([600], [600], 32, 8, 128, 128, 0), ([3], [3000], 4, 2, 128, 128, 1), ([12], [2500], 8, 4, 256, 64, 0),
+    ([4], [0], 2, 1, 64, 16, 0), ([2], [70], 130, 1, 64, 16, 0),
+]
+
+
+@pytest.mark.parametrize("rows,lens,n_q,n_kv,hd,page,window", PROMPT, ids=lambda v: str(v)[:40])
+def test_prompt_attention(L, rows, lens, n_q, n_kv, hd, page, window):
+    cache = random_cache(30, 1, len(lens), max(max(lens), 1), n_kv, hd, page)
+    poison_behind(cache, lens)
+    total = sum(rows)
+    q = queries(31, total + 3, n_q, hd, pad=8)
+    out = torch.full((total + 3, n_q * hd + 16), 5.0, dtype=torch.bfloat16, device=DEV)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    cu = torch.tensor([sum(rows[:i]) for i in range(len(rows) + 1)], dtype=torch.int32, device=DEV)
+    L.attention_e4m3(q.to(DEV)[:, :n_q * hd], *dev, out[:, :n_q * hd], n_q, n_kv, hd, max(rows), max(lens), cu_rows=cu,
+                     seq_lens=torch.tensor(lens, dtype=torch.int32, device=DEV), window=window)
+    assert L.status() == 0
+    assert (out[:, n_q * hd:] == 5.0).all() and (out[total:] == 5.0).all()       # rows of no sequence stay
+    check_attention(q[:, :n_q * hd], out[:, :n_q * hd].cpu(), cache, rows, lens, n_q, n_kv, hd, window,
+                    pick=None if total * max(lens) < 40000 else 1)
+
+
+@pytest.mark.parametrize("hd,rows,length", [(64, 100, 100), (128, 40, 555), (256, 17, 90)])
+def test_prompt_attention_with_equal_lengths(L, hd, rows, length):
+    n_q, n_kv, batch = 4, 2, 2
+    cache = random_cache(32, 1, batch, length, n_kv, hd, 64)
+    q = queries(33, batch * rows, n_q, hd)
+    out = torch.empty_like(q, device=DEV)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    L.attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, rows, length)
+    assert L.status() == 0
+    check_attention(q, out.cpu(), cache, [rows] * batch, [length] * batch, n_q, n_kv, hd, 0, pick=1)
+
+
+@pytest.mark.parametrize("op", ["decode", "prompt"])
+@pytest.mark.parametrize("hd", [64, 128, 256])
+def test_blocks_of_very_unequal_scales(L, hd, op):
+    """V scales from 2^-50 to 2^50 and K scales that make single keys dominate: the weights that meet the tensor cores carry
+    the V scale, so a key with small values and all of the probability must not vanish beside one with large values and none."""
+    n, n_q, n_kv, page = 700, 4, 2, 64
+    cache = random_cache(40, 1, 1, n, n_kv, hd, page)
+    g = gen(41)
+    cache[3][:] = torch.randint(77, 178, cache[3].shape, generator=g, dtype=torch.uint8)
+    cache[2][:] = torch.randint(100, 124, cache[2].shape, generator=g, dtype=torch.uint8)
+    rows = 1 if op == "decode" else 20
+    q = queries(42, rows, n_q, hd, std=1e-3)
+    out = torch.empty_like(q, device=DEV)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    if op == "decode":
+        L.decode_attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, n)
+    else:
+        L.attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, rows, n)
+    check_attention(q, out.cpu(), cache, [rows], [n], n_q, n_kv, hd, 0)
+    # one key has all of the weight and the smallest values, its neighbours enormous values and no weight
+    k8, v8, ks, vs, table = random_cache(43, 1, 1, n, n_kv, hd, page)
+    ks[:], vs[:] = 100, 160
+    pos = 355
+    pg, slot = int(table[0, pos // page]), pos % page
+    ks[0, pg, :, slot // BLOCK], vs[0, pg, :, slot // BLOCK] = 127, 70
+    k8[0, pg, :, slot // BLOCK * BLOCK:slot // BLOCK * BLOCK + BLOCK] = 0
+    k8[0, pg, :, slot] = 0x7e                                    # 448 in every dimension
+    q = torch.full((rows, n_q * hd), 0.05).bfloat16()
+    dev = [t[0].to(DEV).contiguous() for t in (k8, v8, ks, vs)] + [table.to(DEV)]
+    if op == "decode":
+        L.decode_attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, n)
+    else:
+        L.attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, rows, n)
+    check_attention(q, out.cpu(), (k8, v8, ks, vs, table), [rows], [n], n_q, n_kv, hd, 0)
+
+
+def test_attention_with_tiny_and_zero_queries(L):
+    n, n_q, n_kv, hd, page = 300, 4, 2, 128, 32
+    cache = random_cache(44, 1, 3, n, n_kv, hd, page)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    q = queries(45, 3, n_q, hd)
+    q[0] = 0
+    q[1] *= 1e-30
+    q[2, :hd] = 0
+    out = torch.empty_like(q, device=DEV)
+    L.decode_attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, n)
+    check_attention(q, out.cpu(), cache, [1] * 3, [n] * 3, n_q, n_kv, hd, 0)
+    L.attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, 1, n)
+    check_attention(q, out.cpu(), cache, [1] * 3, [n] * 3, n_q, n_kv, hd, 0)
+
+
+@pytest.mark.parametrize("op", ["decode", "prompt"])
+def test_attention_raises_the_status_for_bad_places(L, op):
+    from paper_2602_03295_b200 import POP_E_INVALID
+    n_q, n_kv, hd, page = 2, 1, 64, 16
+    for what in ("page", "length"):
+        cache = random_cache(46, 1, 2, 600, n_kv, hd, page)
+        lens = torch.tensor([600, 600], dtype=torch.int32, device=DEV)
+        if what == "page":
+            cache[4][1, 3] = -5
+        else:
+            lens[1] = 601
+        dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+        q = queries(47, 2, n_q, hd).to(DEV)
+        out = torch.zeros_like(q)
+        if op == "decode":
+            L.decode_attention_e4m3(q, *dev, out, n_q, n_kv, hd, 600, seq_lens=lens)
+        else:
+            L.attention_e4m3(q, *dev, out, n_q, n_kv, hd, 1, 600, seq_lens=lens)
+        assert L.status() == POP_E_INVALID and L.status() == 0
+
+
+# ---------------------------------------------------------------------------------------------- together
+@pytest.mark.parametrize("hd,n_q,n_kv,page,window", [(128, 8, 2, 32, 0), (64, 3, 1, 16, 40), (256, 4, 2, 128, 0)])
+def test_prompt_chunk_drafts_and_decode_over_one_cache(L, hd, n_q, n_kv, page, window):
+    """A bf16 prompt cache is converted, a chunk and a few drafts are appended and attended to, drafts are cut back, single
+    tokens follow; every attention result is checked against the values that the cache holds at that moment."""
+    from paper_2602_03295_b200.binding import KVCache, KVCacheE4M3
+    cfg = SimpleNamespace(n_layers=2, n_kv_heads=n_kv, head_dim=hd)
+    lens, batch = [37, 100], 2
+    a = KVCache(cfg, batch, 100, page)
+    a.k.copy_(torch.randn(a.k.shape, generator=gen(50)))
+    a.v.copy_(torch.randn(a.v.shape, generator=gen(51)))
+    c = KVCacheE4M3(cfg, batch, 400, page, block_table=torch.randperm(batch * -(-400 // page), generator=gen(52)).view(batch, -1))
+    c.fill_from(a, 100, torch.tensor(lens, dtype=torch.int32, device=DEV))
+    ang = torch.arange(400)[:, None].double() * 1e4 ** (-torch.arange(0, hd, 2).double() / hd)
+    rope = torch.stack([ang.cos(), ang.sin()], -1).float().to(DEV)
+    gain = (0.5 + torch.rand(hd, generator=gen(53))).to(DEV)
+    ws = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+    up = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+
+    def step(seed, rows, layer, single):
+        cu = [0, rows[0], sum(rows)]
+        x = torch.randn(sum(rows), (n_q + 2 * n_kv) * hd, generator=gen(seed)).to(DEV)
+        q = torch.empty(sum(rows), n_q * hd, dtype=torch.bfloat16, device=DEV)
+        L.rope_cache_e4m3(x, q, *c.layer(layer), rope, n_q, n_kv, hd, max(rows), start=up(lens), cu_rows=up(cu),
+                          q_gain=gain, k_gain=gain, eps=1e-6)
+        now = [n + r for n, r in zip(lens, rows)]
+        out = torch.empty_like(q)
+        if single:
+            L.decode_attention_e4m3(q, *c.layer(layer), out, n_q, n_kv, hd, max(now), seq_lens=up(now), window=window, workspace=ws)
+        else:
+            L.attention_e4m3(q, *c.layer(layer), out, n_q, n_kv, hd, max(rows), max(now), cu_rows=up(cu), seq_lens=up(now),
+                             window=window, workspace=ws)
+        assert L.status() == 0
+        cpu = tuple(t[layer:layer + 1].cpu() for t in (c.k, c.v, c.k_scale, c.v_scale)) + (c.block_table.cpu(),)
+        check_attention(q.cpu(), out.cpu(), cpu, rows, now, n_q, n_kv, hd, window)
+        return now
+
+    for layer in range(2):
+        lens[:] = [37, 100]
+        lens[:] = step(60 + layer, [50, 21], layer, False)
+        drafted = step(62 + layer, [5, 5], layer, False)
+        lens[:] = [drafted[0] - 3, drafted[1] - 5]               # drafts that were not taken
+        for i in range(3):
+            lens[:] = step(64 + layer + 10 * i, [1, 1], layer, True)
+
+
+def test_captured_graphs_and_other_streams(L):
+    """Append and both attentions captured into two graphs with a workspace each, replayed on new inputs and on two streams
+    at once, equal the eager calls bit for bit."""
+    n_q, n_kv, hd, page, batch, length = 8, 2, 128, 64, 3, 900
+    cache = random_cache(70, 1, batch, length, n_kv, hd, page)
+    ang = torch.arange(length)[:, None].double() * 1e4 ** (-torch.arange(0, hd, 2).double() / hd)
+    rope = torch.stack([ang.cos(), ang.sin()], -1).float().to(DEV)
+    lens = torch.tensor([900, 17, 640], dtype=torch.int32, device=DEV)
+    start = lens - 1
+
+    def make(seed):
+        s = SimpleNamespace()
+        s.dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+        s.x = torch.randn(batch, (n_q + 2 * n_kv) * hd, generator=gen(seed)).to(DEV)
+        s.q = torch.empty(batch, n_q * hd, dtype=torch.bfloat16, device=DEV)
+        s.o1, s.o2 = torch.empty_like(s.q), torch.empty_like(s.q)
+        s.ws = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+        return s
+
+    def chain(s):
+        L.rope_cache_e4m3(s.x, s.q, *s.dev, rope, n_q, n_kv, hd, 1, start=start)
+        L.decode_attention_e4m3(s.q, *s.dev, s.o1, n_q, n_kv, hd, length, seq_lens=lens, workspace=s.ws)
+        L.attention_e4m3(s.q, *s.dev, s.o2, n_q, n_kv, hd, 1, length, seq_lens=lens, workspace=s.ws)
+
+    states, graphs = [make(71), make(72)], []
+    chain(make(73))
+    torch.cuda.synchronize()
+    side = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in states:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            chain(s)
+        graphs.append(g)
+    for seed in (74, 76):
+        for i, (s, g, st) in enumerate(zip(states, graphs, side)):
+            s.x.copy_(torch.randn(s.x.shape, generator=gen(seed + i)))
+        torch.cuda.synchronize()
+        for g, st in zip(graphs, side):
+            with torch.cuda.stream(st):
+                g.replay()
+        torch.cuda.synchronize()
+        assert L.status() == 0
+        for i, s in enumerate(states):
+            e = make(seed + i)
+            for t, u in zip(e.dev, s.dev):
+                t.copy_(u)                     # the replayed append is repeated on its own result: same scales, same codes
+            chain(e)
+            torch.cuda.synchronize()
+            assert torch.equal(e.o1, s.o1) and torch.equal(e.o2, s.o2) and torch.equal(e.q, s.q)
+            assert all(torch.equal(t, u) for t, u in zip(e.dev, s.dev))
+
+
+def test_results_do_not_depend_on_scheduling(L):
+    n_q, n_kv, hd, page = 8, 2, 64, 16
+    lens = [5000, 1, 300, 2222, 0, 48]
+    cache = random_cache(80, 1, len(lens), 5000, n_kv, hd, page)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    q = queries(81, len(lens), n_q, hd).to(DEV)
+    ln = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    outs = []
+    for _ in range(5):
+        out = torch.full_like(q, 3.0)
+        L.decode_attention_e4m3(q, *dev, out, n_q, n_kv, hd, 5000, seq_lens=ln,
+                                workspace=torch.full((64 << 18,), math.nan, device=DEV))
+        outs.append(out)
+    assert all(torch.equal(o, outs[0]) for o in outs) and (outs[0][4] == 0).all()
+
+
+def test_offsets_behind_32_bits(L):
+    """A pool of more than 2^32 code bytes: its last pages are addressed as well as its first."""
+    n_kv, hd, page, pages = 8, 256, 256, 8300                    # 8300 * 524288 bytes = 4.35 GB
+    k8 = torch.zeros(pages, n_kv, page, hd, dtype=torch.uint8, device=DEV)
+    v8 = torch.zeros_like(k8)
+    ks = torch.full((pages, n_kv, page // BLOCK), 120, dtype=torch.uint8, device=DEV)
+    vs = ks.clone()
+    small = random_cache(90, 1, 1, 3 * page, n_kv, hd, page)
+    ids = torch.tensor([[pages - 1, 3, pages - 40]], dtype=torch.int32)
+    for t, u in zip((k8, v8, ks, vs), small[:4]):
+        t[ids[0].long().to(DEV)] = u[0][small[4][0].long()].to(DEV)
+    n = 2 * page + 100
+    case = ([n], [1], 8, n_kv, hd, page, False, False, 1)
+    a = append_inputs(case, 91)
+    q = torch.empty(1, 8 * hd, dtype=torch.bfloat16, device=DEV)
+    out = torch.empty_like(q)
+    L.rope_cache_e4m3(a.x.to(DEV), q, k8, v8, ks, vs, ids.to(DEV), a.rope.to(DEV), 8, n_kv, hd, 1, pos0=n)
+    L.decode_attention_e4m3(q, k8, v8, ks, vs, ids.to(DEV), out, 8, n_kv, hd, n + 1)
+    assert L.status() == 0
+    local = tuple(t[ids[0].long().to(DEV)].cpu()[None] for t in (k8, v8, ks, vs)) + (torch.tensor([[0, 1, 2]], dtype=torch.int32),)
+    before = tuple(u[:, small[4][0].long()] for u in small[:4]) + (local[4],)
+    check_append(case, a, before, q.cpu(), [t[0] for t in local[:4]])
+    check_attention(q.cpu(), out.cpu(), local, [1], [n + 1], 8, n_kv, hd, 0)
+    L.attention_e4m3(q, k8, v8, ks, vs, ids.to(DEV), out, 8, n_kv, hd, 1, n + 1)
+    check_attention(q.cpu(), out.cpu(), local, [1], [n + 1], 8, n_kv, hd, 0)
