@@ -377,31 +377,37 @@ class PopLibrary:
     # -------------------------------------------------------------- 8-bit paged cache
     # One layer of it: k8 / v8 uint8 codes [pages, n_kv, page_size, hd], ks / vs uint8 E8M0 scales
     # [pages, n_kv, page_size / 16], block_table int32 [batch, max_pages] (KVCacheE4M3 holds them for all layers).
+    # The checks are of what the C calls cannot see; they run on every call, so they are kept to plain attribute reads.
     @staticmethod
-    def _cache8(k8, v8, ks, vs, block_table, n_kv, hd, *others):
-        """Checks what the C call cannot see, that all tensors (`others` too) are on the current CUDA device among it;
-        returns (page_size, num_pages, max_pages)."""
+    def _cache8(k8, v8, ks, vs, block_table, n_kv, hd, others):
+        """Checks one layer of the cache, and that all tensors (`others` too) are on the current CUDA device; returns
+        (page_size, num_pages, max_pages, batch, current stream)."""
         at = k8.get_device()
-        if at < 0 or at != torch.cuda.current_device() or \
-                any(t is not None and t.get_device() != at for t in (v8, ks, vs, block_table) + others):
-            raise PopError(POP_E_INVALID, "8-bit cache: all tensors have to be on the current CUDA device")
-        pages, heads, page, d = k8.shape
-        if heads != n_kv or d != hd or v8.shape != k8.shape or ks.shape != (pages, n_kv, page // 16) or ks.shape != vs.shape:
+        if at < 0 or at != torch._C._cuda_getDevice():
+            raise PopError(POP_E_INVALID, "8-bit cache: tensors on the current CUDA device are wanted")
+        for t in (v8, ks, vs, block_table) + others:
+            if t is not None and t.get_device() != at:
+                raise PopError(POP_E_INVALID, "8-bit cache: all tensors have to be on the current CUDA device")
+        shape, u8 = k8.shape, torch.uint8
+        pages, heads, page, d = shape
+        scales = ks.shape
+        if heads != n_kv or d != hd or v8.shape != shape or scales != (pages, n_kv, page // 16) or scales != vs.shape:
             raise PopError(POP_E_INVALID, "8-bit cache: shapes of codes and scales do not belong together")
-        if not (k8.dtype == v8.dtype == ks.dtype == vs.dtype == torch.uint8) or block_table.dtype != torch.int32:
+        if k8.dtype != u8 or v8.dtype != u8 or ks.dtype != u8 or vs.dtype != u8 or block_table.dtype != torch.int32:
             raise PopError(POP_E_INVALID, "8-bit cache: uint8 codes and scales and an int32 block table are wanted")
         if not (k8.is_contiguous() and v8.is_contiguous() and ks.is_contiguous() and vs.is_contiguous()
                 and block_table.is_contiguous()):
             raise PopError(POP_E_INVALID, "8-bit cache: one layer's tensors and the block table have to be contiguous")
-        return page, pages, block_table.shape[1]
+        batch, max_pages = block_table.shape
+        return page, pages, max_pages, batch, torch._C._cuda_getCurrentRawStream(at)
 
     @staticmethod
-    def _ints(t, n, what, like):
+    def _ints(t, n, what):
         """Pointer of an optional int32 device vector of n entries."""
         if t is None:
             return None
-        if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous() or t.device != like.device:
-            raise PopError(POP_E_INVALID, f"{what}: contiguous int32 [{n}] on {like.device} is wanted")
+        if t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous():
+            raise PopError(POP_E_INVALID, f"{what}: contiguous int32 [{n}] is wanted")
         return t.data_ptr()
 
     def quant_cache_e4m3(self, k_pool, v_pool, src_table, k8, v8, ks, vs, block_table, max_len, seq_lens=None, stream=None):
@@ -411,8 +417,8 @@ class PopLibrary:
         if k8.dim() != 5 or not (k8.shape[0] == v8.shape[0] == ks.shape[0] == vs.shape[0] == layers) or \
                 k_pool.dtype != torch.bfloat16 or v_pool.dtype != torch.bfloat16 or v_pool.shape != k_pool.shape:
             raise PopError(POP_E_INVALID, "quant_cache_e4m3: pools, codes and scales of the same layers are wanted")
-        page, pages, max_pages = self._cache8(k8[0], v8[0], ks[0], vs[0], block_table, n_kv, hd, k_pool, v_pool, src_table)
-        batch = block_table.shape[0]
+        page, pages, max_pages, batch, here = self._cache8(k8[0], v8[0], ks[0], vs[0], block_table, n_kv, hd,
+                                                           (k_pool, v_pool, src_table, seq_lens))
         if src_table.shape[0] != batch or src_table.dtype != torch.int32 or not src_table.is_contiguous() or \
                 not (k_pool[0].is_contiguous() and v_pool[0].is_contiguous()) or \
                 k_pool.stride(0) != v_pool.stride(0) or k8.stride(0) != v8.stride(0) or ks.stride(0) != vs.stride(0):
@@ -420,9 +426,10 @@ class PopLibrary:
         code = self.dll.pop_k_quant_cache_e4m3(
             k_pool.data_ptr(), v_pool.data_ptr(), k_pool.stride(0), src_table.data_ptr(), src_page, src_pages,
             src_table.shape[1], k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), k8.stride(0), ks.stride(0),
-            block_table.data_ptr(), page, pages, max_pages, self._ints(seq_lens, batch, "seq_lens", k8), max_len, layers,
-            batch, n_kv, hd, _stream_ptr(stream))
-        self.check(code, "pop_k_quant_cache_e4m3")
+            block_table.data_ptr(), page, pages, max_pages, self._ints(seq_lens, batch, "seq_lens"), max_len, layers,
+            batch, n_kv, hd, here if stream is None else stream.cuda_stream)
+        if code:
+            self.check(code, "pop_k_quant_cache_e4m3")
 
     def rope_cache_e4m3(self, x, q_out, k8, v8, ks, vs, block_table, rope_table, n_q, n_kv, hd, max_rows, start=None,
                         pos0=0, cu_rows=None, q_gain=None, k_gain=None, eps=0.0, positions=None, pair_axis=None,
@@ -430,15 +437,22 @@ class PopLibrary:
         """pop_k_rope_cache_e4m3: x fp32 or bf16 [rows, (n_q + 2 n_kv) hd]; q_out bf16 [rows, n_q hd] (None if n_q is 0);
         rope_table fp32 [positions, hd / 2, 2]; start int32 [batch] or pos0 for all; cu_rows int32 [batch + 1] or max_rows rows
         each; positions int32 [axes, rows] with pair_axis uint8 [hd / 2] for rotations over several axes."""
-        page, pages, max_pages = self._cache8(k8, v8, ks, vs, block_table, n_kv, hd, x, q_out, rope_table, q_gain, k_gain,
-                                              positions, pair_axis)
-        batch, rows = block_table.shape[0], x.shape[0]
-        if x.dtype not in (torch.float32, torch.bfloat16) or x.shape[1] != (n_q + 2 * n_kv) * hd or x.stride(1) != 1 or \
+        page, pages, max_pages, batch, here = self._cache8(
+            k8, v8, ks, vs, block_table, n_kv, hd, (x, q_out, rope_table, q_gain, k_gain, positions, pair_axis, start, cu_rows))
+        rows, width = x.shape
+        bf16 = x.dtype == torch.bfloat16
+        ld_in, inner = x.stride()
+        if not (bf16 or x.dtype == torch.float32) or width != (n_q + 2 * n_kv) * hd or inner != 1 or \
                 (cu_rows is None and rows != batch * max_rows):
             raise PopError(POP_E_INVALID, "rope_cache_e4m3: x is fp32 or bf16 [rows, (n_q + 2 n_kv) hd], rows as stated")
-        if n_q and (q_out.dtype != torch.bfloat16 or q_out.shape != (rows, n_q * hd) or q_out.stride(1) != 1):
-            raise PopError(POP_E_INVALID, "rope_cache_e4m3: q_out is bf16 [rows, n_q hd]")
-        if rope_table.dtype != torch.float32 or rope_table.numel() % hd or not rope_table.is_contiguous():
+        q_ptr, ldq = None, 0
+        if n_q:
+            ldq, inner = q_out.stride()
+            q_ptr = q_out.data_ptr()
+            if q_out.dtype != torch.bfloat16 or q_out.shape != (rows, n_q * hd) or inner != 1:
+                raise PopError(POP_E_INVALID, "rope_cache_e4m3: q_out is bf16 [rows, n_q hd]")
+        table_rows = rope_table.numel() // hd
+        if rope_table.dtype != torch.float32 or table_rows * hd != rope_table.numel() or not rope_table.is_contiguous():
             raise PopError(POP_E_INVALID, "rope_cache_e4m3: rope_table is fp32 [positions, hd / 2, 2]")
         axes, ld_pos = 0, 0
         if positions is not None:
@@ -454,56 +468,64 @@ class PopLibrary:
         if rows == 0:
             return q_out
         code = self.dll.pop_k_rope_cache_e4m3(
-            x.data_ptr(), 1 if x.dtype == torch.bfloat16 else 0, x.stride(0), self._ints(cu_rows, batch + 1, "cu_rows", x),
-            max_rows, self._ints(start, batch, "start", x), pos0, batch, _ptr(q_out) if n_q else None,
-            q_out.stride(0) if n_q else 0, k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(),
-            block_table.data_ptr(), page, pages, max_pages, _ptr(q_gain), _ptr(k_gain), eps, rope_table.data_ptr(),
-            rope_table.numel() // hd, _ptr(positions), ld_pos, _ptr(pair_axis), axes, n_q, n_kv, hd, _stream_ptr(stream))
-        self.check(code, "pop_k_rope_cache_e4m3")
+            x.data_ptr(), 1 if bf16 else 0, ld_in, self._ints(cu_rows, batch + 1, "cu_rows"), max_rows,
+            self._ints(start, batch, "start"), pos0, batch, q_ptr, ldq, k8.data_ptr(), v8.data_ptr(), ks.data_ptr(),
+            vs.data_ptr(), block_table.data_ptr(), page, pages, max_pages, _ptr(q_gain), _ptr(k_gain), eps,
+            rope_table.data_ptr(), table_rows, _ptr(positions), ld_pos, _ptr(pair_axis), axes, n_q, n_kv, hd,
+            here if stream is None else stream.cuda_stream)
+        if code:
+            self.check(code, "pop_k_rope_cache_e4m3")
         return q_out
 
-    def _attn8_args(self, q, k8, v8, ks, vs, block_table, out, n_q, n_kv, hd, workspace):
-        page, pages, max_pages = self._cache8(k8, v8, ks, vs, block_table, n_kv, hd, q, out, workspace)
-        if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or q.shape != out.shape or q.shape[1] != n_q * hd or \
-                q.stride(1) != 1 or out.stride(1) != 1:
+    @staticmethod
+    def _attn8_rows(q, out, width, workspace):
+        """Checks queries and outputs; returns (rows, strides of both, workspace, its bytes)."""
+        rows, w = q.shape
+        ldq, q_inner = q.stride()
+        ldo, o_inner = out.stride()
+        if q.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or q.shape != out.shape or w != width or \
+                q_inner != 1 or o_inner != 1:
             raise PopError(POP_E_INVALID, "q and out are bf16 [rows, n_q hd]")
         if workspace is None:
             workspace = torch.empty(POP_E4M3_WORKSPACE_BYTES, dtype=torch.uint8, device=q.device)
         elif not workspace.is_contiguous():
             raise PopError(POP_E_INVALID, "workspace has to be contiguous")
-        return page, pages, max_pages, workspace, workspace.numel() * workspace.element_size()
+        return rows, ldq, ldo, workspace, workspace.numel() * workspace.element_size()
 
     def decode_attention_e4m3(self, q, k8, v8, ks, vs, block_table, out, n_q, n_kv, hd, kv_len, seq_lens=None, window=0,
                               workspace=None, stream=None):
         """pop_k_decode_attention_e4m3: q, out bf16 [batch, n_q hd]; seq_lens int32 [batch] (each <= kv_len) or kv_len for
         all. `workspace` (POP_E4M3_WORKSPACE_BYTES of any dtype) is allocated if not given."""
-        page, pages, max_pages, ws, nbytes = self._attn8_args(q, k8, v8, ks, vs, block_table, out, n_q, n_kv, hd, workspace)
-        batch = q.shape[0]
-        if block_table.shape[0] != batch:
+        page, pages, max_pages, batch, here = self._cache8(k8, v8, ks, vs, block_table, n_kv, hd, (q, out, workspace, seq_lens))
+        rows, ldq, ldo, ws, nbytes = self._attn8_rows(q, out, n_q * hd, workspace)
+        if rows != batch:
             raise PopError(POP_E_INVALID, "decode_attention_e4m3: one query row and one block-table row per sequence")
         code = self.dll.pop_k_decode_attention_e4m3(
-            q.data_ptr(), q.stride(0), k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), block_table.data_ptr(),
-            page, pages, max_pages, self._ints(seq_lens, batch, "seq_lens", q), kv_len, ws.data_ptr(), nbytes,
-            out.data_ptr(), out.stride(0), batch, n_q, n_kv, hd, window, _stream_ptr(stream))
-        self.check(code, "pop_k_decode_attention_e4m3")
+            q.data_ptr(), ldq, k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), block_table.data_ptr(), page,
+            pages, max_pages, self._ints(seq_lens, batch, "seq_lens"), kv_len, ws.data_ptr(), nbytes, out.data_ptr(), ldo,
+            batch, n_q, n_kv, hd, window, here if stream is None else stream.cuda_stream)
+        if code:
+            self.check(code, "pop_k_decode_attention_e4m3")
         return out
 
     def attention_e4m3(self, q, k8, v8, ks, vs, block_table, out, n_q, n_kv, hd, max_rows, kv_len, cu_rows=None,
                        seq_lens=None, window=0, workspace=None, stream=None):
         """pop_k_attention_e4m3: q, out bf16 [rows, n_q hd], the last rows of each sequence (cu_rows int32 [batch + 1], or
         max_rows rows each); seq_lens int32 [batch] cached positions, the rows' own included, or kv_len for all."""
-        page, pages, max_pages, ws, nbytes = self._attn8_args(q, k8, v8, ks, vs, block_table, out, n_q, n_kv, hd, workspace)
-        batch = block_table.shape[0]
-        if cu_rows is None and q.shape[0] != batch * max_rows:
+        page, pages, max_pages, batch, here = self._cache8(k8, v8, ks, vs, block_table, n_kv, hd,
+                                                           (q, out, workspace, seq_lens, cu_rows))
+        rows, ldq, ldo, ws, nbytes = self._attn8_rows(q, out, n_q * hd, workspace)
+        if cu_rows is None and rows != batch * max_rows:
             raise PopError(POP_E_INVALID, "attention_e4m3: max_rows rows of every sequence, or cu_rows, are wanted")
-        if q.shape[0] == 0:
+        if rows == 0:
             return out
         code = self.dll.pop_k_attention_e4m3(
-            q.data_ptr(), q.stride(0), self._ints(cu_rows, batch + 1, "cu_rows", q), max_rows, k8.data_ptr(), v8.data_ptr(),
+            q.data_ptr(), ldq, self._ints(cu_rows, batch + 1, "cu_rows"), max_rows, k8.data_ptr(), v8.data_ptr(),
             ks.data_ptr(), vs.data_ptr(), block_table.data_ptr(), page, pages, max_pages,
-            self._ints(seq_lens, batch, "seq_lens", q), kv_len, ws.data_ptr(), nbytes, out.data_ptr(), out.stride(0),
-            batch, n_q, n_kv, hd, window, _stream_ptr(stream))
-        self.check(code, "pop_k_attention_e4m3")
+            self._ints(seq_lens, batch, "seq_lens"), kv_len, ws.data_ptr(), nbytes, out.data_ptr(), ldo, batch, n_q, n_kv,
+            hd, window, here if stream is None else stream.cuda_stream)
+        if code:
+            self.check(code, "pop_k_attention_e4m3")
         return out
 
 

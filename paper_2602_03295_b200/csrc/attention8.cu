@@ -9,14 +9,18 @@
 // row's largest element) and the weights as f16. Scores, statistics, sums and the accumulator are fp32.
 //
 // A CTA owns NQT tiles of 128 rows of one kv head; a row is a (position, query head) pair of that kv head, so that the
-// keys are read and converted once for all heads that share them, however few the positions are. Keys are walked 64
-// at a time. Warp roles:
-//   NQT softmax warpgroups, one row per thread: place Q in shared memory, then read S = Q K^T from one of two TMEM
-//       buffers, write the weights over it, rescale the TMEM accumulator when the maximum grew by more than 2^8;
-//   4 converter warps: 16 codes per load straight from the paged cache, a tile ahead of its use, to f16 in the
-//       128-byte-swizzled operand layout (K-major for K, MN-major for V: the same bytes); positions past the end become
-//       zeros, the blocks' scales go to a small ring beside them;
-//   1 MMA warp: scores two key tiles ahead of the softmax, then O += P V with P from TMEM.
+// keys are read once for all heads that share them, however few the positions are. K codes are E4M3 operands as they
+// lie in the cache (tcgen05 kind::f8f6f4): after a power-of-two scale per row an element of q is the sum of two codes (exactly
+// for bf16 elements down to 2^-9 of the row's largest, within 2^-17 of that below), two instruction sets at twice the f16
+// rate accumulate both. V has to become f16 (exact) because the weights are f16. Warp roles:
+//   NQT softmax warpgroups, one row per thread: place both codes of Q in shared memory, then read S = Q K^T from TMEM 64
+//       keys at a time, write the weights over it, rescale the TMEM accumulator when the maximum grew by more than 2^8;
+//   a converter warpgroup: 64 keys of V at a time from the staged codes to f16 in the 128-byte-swizzled operand layout;
+//       positions past the end become zeros;
+//   a TMA warp: codes of K (128 keys) and V (64 keys) from the paged pools, a row being one position of one head;
+//   an MMA warp: scores of 128 keys with one set of instructions, O += P V per 64 keys with P from TMEM. Two score
+//       buffers: one for each of two tiles, or two for one tile, so that the tensor pipe works while the softmax does;
+//   a scale warp: the scales of 32 blocks at a time, converted, in a small ring.
 // With fewer CTAs than SMs (few rows) the keys are split over several CTAs, which leave unnormalised rows in the
 // workspace for a second, chained launch to merge.
 #include "cache8.cuh"
@@ -27,40 +31,45 @@ namespace {
 
 constexpr int kSmemLimit = 227 * 1024;
 constexpr float W_SHIFT = 7.f;        // weights are stored times 2^7; the lazy maximum lets them reach 2^15
-constexpr int SC_RING = 16;           // key tiles whose scales are held: more than the ring of operand tiles can be ahead
 
 template <int HD, int NQT>
 struct A8 {
-  static constexpr int BKV = 64;
-  static constexpr int KV_TILE_BYTES = BKV * HD * 2;
-  static constexpr int KV_SUB_BYTES = BKV * 128;     // one 64-wide slice of head_dim
-  static constexpr int Q_TILE_BYTES = 128 * HD * 2;
-  static constexpr int RING_BYTES = kSmemLimit - 4 * 1024 - NQT * Q_TILE_BYTES;   // alignment slack, scales, barriers
-  static constexpr int STAGES = RING_BYTES / KV_TILE_BYTES < 8 ? RING_BYTES / KV_TILE_BYTES : 8;
+  static constexpr int BKV = 64, PKV = 128;
+  static constexpr int INNER = HD < 128 ? HD : 128;            // bytes of a code row in one swizzled slice
+  static constexpr int SLICES = HD / INNER;
+  static constexpr int Q_PART = 128 * HD;                      // one code per element; two parts per tile
+  static constexpr int K_STAGE = PKV * HD;
+  static constexpr int VR_STAGE = BKV * HD;                    // V codes
+  static constexpr int VF_STAGE = BKV * HD * 2;                // V as f16
+  static constexpr int VF_SUB = BKV * 128;                     // one 64-wide slice of it
+  static constexpr int NK = HD == 256 ? 2 : 3;
+  static constexpr int NVR = HD == 256 ? 2 : 4;
+  static constexpr int NVF = HD == 256 ? 2 : 4;
+  static constexpr int NB = NQT == 1 ? 2 : 1;                  // score buffers per tile
   static constexpr int SM_WARPS = NQT * 4;
-  static constexpr int THREADS = (SM_WARPS + 4 + 1) * 32;
-  static constexpr int LOADS = BKV * HD / (16 * 128);          // 16-byte loads of a tile per converter thread
-  static constexpr int S_COL = 0;                    // S_t[b] at (t * 2 + b) * 64
-  static constexpr int O_COL = NQT * 2 * BKV;        // O_t at O_COL + t * HD
-  static constexpr int COLS_USED = O_COL + NQT * HD;
-  static constexpr uint32_t TMEM_COLS = COLS_USED <= 128 ? 128 : (COLS_USED <= 256 ? 256 : 512);
-  static_assert(COLS_USED <= 512, "TMEM budget");
-  static_assert(STAGES >= 4, "ring too shallow");
+  static constexpr int THREADS = (SM_WARPS + 8) * 32;
+  static constexpr int LOADS = BKV * HD / (16 * 128);          // 16-byte pieces of a V stage per converter thread
+  static constexpr int O_COL = 256;                            // S at (t + buffer) * 128, O_t at O_COL + t * HD
+  static constexpr uint32_t TMEM_COLS = 512;
+  static_assert(O_COL + NQT * HD <= 512, "TMEM budget");
 };
 
 template <int HD, int NQT>
 struct __align__(1024) A8Smem {
   using C = A8<HD, NQT>;
-  uint8_t q[NQT][C::Q_TILE_BYTES];
-  uint8_t kv[C::STAGES][C::KV_TILE_BYTES];
-  float4 sc[SC_RING][4];        // per block of 16 keys: 2^ek, ev, 2^-ev
+  uint8_t q[NQT][2][C::Q_PART];
+  uint8_t k[C::NK][C::K_STAGE];
+  uint8_t vr[C::NVR][C::VR_STAGE];
+  uint8_t vf[C::NVF][C::VF_STAGE];
+  float4 sc[2][32];             // per block of 16 keys: 2^ek, ev, 2^-ev; two groups of 32 blocks
   uint64_t q_full;
-  uint64_t kv_full[C::STAGES];
-  uint64_t kv_empty[C::STAGES];
-  uint64_t sc_full[SC_RING];
-  uint64_t s_full[NQT][2];      // S_t[b] = Q_t K^T complete, b = key tile & 1, phase = key tile >> 1
-  uint64_t p_ready[NQT][2];     // P_t[b] written over S_t[b] (one arrival per softmax warp)
-  uint64_t pv_done[NQT][2];     // O_t += P_t[b] V complete
+  uint64_t k_full[C::NK], k_empty[C::NK];
+  uint64_t vr_full[C::NVR], vr_empty[C::NVR];
+  uint64_t vf_full[C::NVF], vf_empty[C::NVF];
+  uint64_t sc_full[2], sc_empty[2];
+  uint64_t s_full[2];           // scores of a pair of key tiles complete; index: tile or buffer
+  uint64_t p_ready[2][2];       // P of half h written over its scores (one arrival per softmax warp)
+  uint64_t pv_done[2][2];       // O += P V of half h complete
   uint32_t tmem_base;
   uint32_t raised;
   volatile uint32_t abort;
@@ -69,7 +78,8 @@ struct __align__(1024) A8Smem {
 struct A8Dev {
   const bf16* q; int64_t ldq;
   Cache8 c;
-  int ps_log2;                  // log2 of the page size, or -1
+  int box;                      // rows of one copy: min(page size, 64)
+  int pool_rows;                // rows of the pool: pages * n_kv * page size
   const int32_t* cu; int rows;
   const int32_t* seq_lens; int kv_len;
   bf16* out; int64_t ldo;
@@ -144,11 +154,30 @@ __host__ __device__ constexpr uint32_t umma_idesc_f16(int m, int n, int b_mn_maj
     atomicMin((status), (int)POP_E_DEVICE_TIMEOUT);   \
   } while (0)
 
+// Shared-memory matrix descriptor of a K-major tile of codes: rows of 128 bytes with 128-byte swizzle, or (hd 64) rows of
+// 64 bytes with 64-byte swizzle (layout 4); groups of 8 rows follow each other
+template <int INNER>
+__device__ __forceinline__ uint64_t code_desc(uint32_t saddr) {
+  uint64_t d = umma_smem_desc(saddr, 16, INNER * 8);
+  if (INNER == 64) d = (d & ~(uint64_t(7) << 61)) | (uint64_t(4) << 61);
+  return d;
+}
+// where 16-byte piece c of a code row lies in its slice
+template <int INNER>
+__device__ __forceinline__ int code_at(int row, int c) {
+  return INNER == 128 ? row * 128 + ((c ^ (row & 7)) << 4) : row * 64 + ((c ^ ((row >> 1) & 3)) << 4);
+}
+template <int N>
+__device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
 template <int HD, int NQT>
 __global__ void __launch_bounds__(A8<HD, NQT>::THREADS, 1)
-attn8_kernel(const __grid_constant__ A8Dev p, int* __restrict__ status) {
+attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+             const __grid_constant__ A8Dev p, int* __restrict__ status) {
   using C = A8<HD, NQT>;
-  constexpr int BKV = C::BKV, STAGES = C::STAGES;
+  constexpr int BKV = C::BKV, PKV = C::PKV, INNER = C::INNER, SLICES = C::SLICES, NB = C::NB;
   extern __shared__ uint8_t smem_raw[];
   A8Smem<HD, NQT>& s =
       *reinterpret_cast<A8Smem<HD, NQT>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -160,8 +189,9 @@ attn8_kernel(const __grid_constant__ A8Dev p, int* __restrict__ status) {
   const Job x = job_of<NQT>(p, blockIdx.x, blockIdx.y, blockIdx.z / p.splits, status);
   if (x.q0 < 0) return;                                  // past the rows of this sequence
   const int t_lo = (int)((int64_t)x.n_tiles * split / p.splits);
-  const int n_tiles = (int)((int64_t)x.n_tiles * (split + 1) / p.splits) - t_lo;
-  const int j_lo = x.j_lo + t_lo;
+  const int n_tiles = (int)((int64_t)x.n_tiles * (split + 1) / p.splits) - t_lo;      // 64 keys each
+  const int n_pairs = (n_tiles + 1) >> 1;
+  const int key0 = (x.j_lo + t_lo) * BKV;                // first key of tile 0
   float* part = p.splits > 1 ? p.partial + (((int64_t)(blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x) *
                                             (NQT * 128)) * (HD + 4)
                              : nullptr;
@@ -184,21 +214,20 @@ attn8_kernel(const __grid_constant__ A8Dev p, int* __restrict__ status) {
   }
   if (threadIdx.x == 0) {
     mbar_init(&s.q_full, C::SM_WARPS);
-    for (int i = 0; i < STAGES; ++i) {
-      mbar_init(&s.kv_full[i], 4);
-      mbar_init(&s.kv_empty[i], 1);
+    for (int i = 0; i < C::NK; ++i) { mbar_init(&s.k_full[i], 1); mbar_init(&s.k_empty[i], 1); }
+    for (int i = 0; i < C::NVR; ++i) { mbar_init(&s.vr_full[i], 1); mbar_init(&s.vr_empty[i], 4); }
+    for (int i = 0; i < C::NVF; ++i) { mbar_init(&s.vf_full[i], 4); mbar_init(&s.vf_empty[i], 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(&s.sc_full[i], 1); mbar_init(&s.sc_empty[i], C::SM_WARPS); }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(&s.s_full[t], 1);
+      for (int i = 0; i < 2; ++i) { mbar_init(&s.p_ready[t][i], 4); mbar_init(&s.pv_done[t][i], 1); }
     }
-    for (int i = 0; i < SC_RING; ++i) mbar_init(&s.sc_full[i], 1);
-    for (int t = 0; t < NQT; ++t)
-      for (int i = 0; i < 2; ++i) {
-        mbar_init(&s.s_full[t][i], 1);
-        mbar_init(&s.p_ready[t][i], 4);
-        mbar_init(&s.pv_done[t][i], 1);
-      }
     s.abort = 0;
     fence_barrier_init();
+    prefetch_tmap(&tmK);
+    prefetch_tmap(&tmV);
   }
-  if (warp == C::SM_WARPS + 4) {
+  if (warp == C::SM_WARPS + 5) {
     tmem_alloc(&s.tmem_base, C::TMEM_COLS);
     tmem_relinquish();
   }
@@ -206,85 +235,190 @@ attn8_kernel(const __grid_constant__ A8Dev p, int* __restrict__ status) {
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = s.tmem_base;
+  const int32_t* bt = p.c.table + (int64_t)x.b * p.c.max_pages;
+  const int ps = p.c.page_size;
+  // pool row (page * n_kv + head) * page_size + slot of a position, or -1 for a table entry that is no page of the pool
+  auto pool_row = [&](int pos) {
+    const int pi = pos / ps, page = bt[pi];
+    if ((unsigned)page >= (unsigned)p.c.num_pages) {
+      atomicMin(status, (int)POP_E_INVALID);
+      return -1;
+    }
+    return (page * p.n_kv + x.kvh) * ps + (pos - pi * ps);
+  };
 
-  if (warp >= C::SM_WARPS && warp < C::SM_WARPS + 4) {
-    // ------------------------------------------------------------------ converters
+  if (warp >= C::SM_WARPS + 4) {
+    if constexpr (NQT == 2) regs_dec<56>();
+    const int role = warp - C::SM_WARPS - 4;
+    if (role == 0) {
+      // ---------------------------------------------------------------- TMA
+      // Lane l holds the pool row of copy l of a pair (128 keys), fetched a pair ahead. A copy that starts past the end is
+      // left out; one of a bad page goes past the pool's end and is filled with zeros.
+      const int boxes = PKV / p.box, half_boxes = boxes >> 1;
+      auto row_of = [&](int J) {
+        const int pos = key0 + J * PKV + lane * p.box;
+        if (lane >= boxes || J >= n_pairs || pos >= x.len) return -2;
+        const int r = pool_row(pos);
+        return r < 0 ? p.pool_rows : r;
+      };
+      auto copy = [&](const CUtensorMap* tm, uint64_t* bar, uint8_t* dst, int row, int first, int count) {
+        const int live = __popc(__ballot_sync(0xffffffffu, row != -2) & (((1u << count) - 1u) << first));
+        if (lane == 0) mbar_expect_tx(bar, live * p.box * HD);
+        for (int i = 0; i < count; ++i) {
+          const int r = __shfl_sync(0xffffffffu, row, first + i);
+          if (r != -2 && lane == 0)
+            for (int c = 0; c < SLICES; ++c)
+              tma_load_2d(dst + c * (count * p.box * INNER) + i * p.box * INNER, tm, bar, c * INNER, r);
+        }
+      };
+      int row = row_of(0);
+      bool ok = true;
+      for (int J = 0; J < n_pairs && ok && !s.abort; ++J) {
+        const int next = row_of(J + 1);
+        const int ks = J % C::NK;
+        ok = mbar_wait_relaxed(&s.k_empty[ks], ((J / C::NK) & 1) ^ 1);
+        __syncwarp();
+        if (!ok) break;
+        copy(&tmK, &s.k_full[ks], s.k[ks], row, 0, boxes);
+        for (int h = 0; h < 2 && ok; ++h) {
+          const int jj = 2 * J + h, vs = jj % C::NVR;
+          if (jj >= n_tiles) break;
+          ok = mbar_wait_relaxed(&s.vr_empty[vs], ((jj / C::NVR) & 1) ^ 1);
+          __syncwarp();
+          if (ok) copy(&tmV, &s.vr_full[vs], s.vr[vs], row, h * half_boxes, half_boxes);
+        }
+        row = next;
+      }
+      if (!ok) A8_ABORT(s, status);
+    } else if (role == 1) {
+      // ---------------------------------------------------------------- MMA (whole warp, elected lane)
+      const uint32_t leader = elect_one();
+      constexpr uint32_t idesc_s = umma_idesc_e4m3(128, PKV);
+      constexpr uint32_t idesc_o = umma_idesc_f16(128, HD, 1);
+      const uint64_t q_desc = code_desc<INNER>(smem_u32(s.q[0][0]));
+      const uint64_t k_desc = code_desc<INNER>(smem_u32(s.k[0]));
+      const uint64_t v_desc = umma_smem_desc(smem_u32(s.vf[0]), C::VF_SUB, 1024);    // MN-major
+      auto issue_s = [&](int t, int J) {                   // 128 keys, both codes of q
+        const int sb = NQT == 1 ? (J & 1) : t;
+        const uint64_t kd = k_desc + uint64_t((J % C::NK) * (C::K_STAGE >> 4));
+        const uint32_t d = tmem_base + sb * 128;
+#pragma unroll
+        for (int part_i = 0; part_i < 2; ++part_i) {
+          const uint64_t qd = q_desc + uint64_t((t * 2 + part_i) * (C::Q_PART >> 4));
+#pragma unroll
+          for (int kk = 0; kk < HD / 32; ++kk) {
+            const int sl = kk / (INNER / 32), in = kk % (INNER / 32);
+            umma_e4m3_ss_w(leader, d, qd + uint64_t((sl * 128 * INNER + in * 32) >> 4),
+                           kd + uint64_t((sl * PKV * INNER + in * 32) >> 4), idesc_s, (part_i | kk) ? 1u : 0u);
+          }
+        }
+        umma_commit_w(leader, &s.s_full[sb]);
+      };
+      auto issue_pv = [&](int t, int jj) {                 // 64 keys: A = P in TMEM (8 packed columns per 16 keys), B = V
+        const int sb = NQT == 1 ? ((jj >> 1) & 1) : t, h = jj & 1;
+        const uint32_t pa = tmem_base + sb * 128 + h * BKV;
+        const uint64_t vd = v_desc + uint64_t((jj % C::NVF) * (C::VF_STAGE >> 4));
+        const uint32_t d = tmem_base + C::O_COL + t * HD;
+#pragma unroll
+        for (int kk = 0; kk < BKV / 16; ++kk)
+          umma_bf16_ts_w(leader, d, pa + kk * 8, vd + uint64_t((kk * 2048) >> 4), idesc_o, (jj > 0 || kk > 0) ? 1u : 0u);
+        umma_commit_w(leader, &s.pv_done[sb][h]);
+      };
+      bool ok = mbar_wait_relaxed(&s.q_full, 0);
+      // scores of the first pair (of two pairs where one tile has both buffers)
+      for (int J = 0; J < NB && J < n_pairs && ok; ++J) {
+        ok = mbar_wait_relaxed(&s.k_full[J % C::NK], (J / C::NK) & 1);
+        if (!ok) break;
+        tc_fence_after();
+        for (int t = 0; t < NQT; ++t) issue_s(t, J);
+        umma_commit_w(leader, &s.k_empty[J % C::NK]);
+      }
+      for (int J = 0; J < n_pairs && ok && !s.abort; ++J) {
+        const int Jn = J + NB;                             // the pair whose scores go where this one's are
+        const bool more = Jn < n_pairs;
+        bool k_ready = false;
+        for (int h = 0; h < 2 && ok; ++h) {
+          const int jj = 2 * J + h;
+          if (jj >= n_tiles) break;
+          const bool last_half = h == 1 || jj + 1 >= n_tiles;
+          ok = mbar_wait_relaxed(&s.vf_full[jj % C::NVF], (jj / C::NVF) & 1);
+          for (int t = 0; t < NQT && ok; ++t) {
+            const int sb = NQT == 1 ? (J & 1) : t;
+            ok = mbar_wait_relaxed(&s.p_ready[sb][h], (J / NB) & 1);
+            if (!ok) break;
+            tc_fence_after();
+            issue_pv(t, jj);
+            if (last_half && more) {
+              // both halves of the buffer are consumed: the pipe runs its instructions in order
+              if (!k_ready) {
+                ok = mbar_wait_relaxed(&s.k_full[Jn % C::NK], (Jn / C::NK) & 1);
+                if (!ok) break;
+                tc_fence_after();
+                k_ready = true;
+              }
+              issue_s(t, Jn);
+            }
+          }
+          if (ok) umma_commit_w(leader, &s.vf_empty[jj % C::NVF]);
+        }
+        if (ok && more) umma_commit_w(leader, &s.k_empty[Jn % C::NK]);
+      }
+      if (!ok) A8_ABORT(s, status);
+    } else if (role == 2) {
+      // ---------------------------------------------------------------- scales: 32 blocks (8 tiles) at a time, one per lane
+      auto fetch = [&](int grp, int& ke, int& ve) {
+        ke = ve = 127;
+        const int pos = key0 + (grp * 32 + lane) * C8_BLOCK;
+        if (pos < x.len && grp * 8 + (lane >> 2) < n_tiles) {
+          const int r = pool_row(pos);
+          if (r >= 0) {
+            ke = p.c.ks[r / C8_BLOCK];
+            ve = p.c.vs[r / C8_BLOCK];
+          }
+        }
+      };
+      const int groups = (n_tiles + 7) >> 3;
+      int ke, ve;
+      fetch(0, ke, ve);
+      bool ok = true;
+      for (int grp = 0; grp < groups && !s.abort; ++grp) {
+        ok = mbar_wait_relaxed(&s.sc_empty[grp & 1], ((grp >> 1) & 1) ^ 1);
+        if (!ok) break;
+        s.sc[grp & 1][lane] = make_float4(c8_pow2(ke - 127), (float)(ve - 127), c8_pow2(127 - ve), 0.f);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.sc_full[grp & 1]);
+        if (grp + 1 < groups) fetch(grp + 1, ke, ve);
+      }
+      if (!ok) A8_ABORT(s, status);
+    }
+  } else if (warp >= C::SM_WARPS) {
+    // ------------------------------------------------------------------ converters: V codes -> f16, 64 keys at a time
+    if constexpr (NQT == 2) regs_dec<56>();
     const int tid = threadIdx.x - C::SM_WARPS * 32;
     constexpr int CPR = HD / 16;                         // 16-code pieces per row
-    const int32_t* bt = p.c.table + (int64_t)x.b * p.c.max_pages;
-    const int ps = p.c.page_size;
-    // pool row (page * n_kv + head) * page_size + slot of a position below len, or -1
-    auto pool_row = [&](int pos) -> int64_t {
-      const int pi = p.ps_log2 >= 0 ? pos >> p.ps_log2 : pos / ps;
-      const int page = bt[pi];
-      if ((unsigned)page >= (unsigned)p.c.num_pages) {   // never turned into an address: reads as zeros
-        atomicMin(status, (int)POP_E_INVALID);
-        return -1;
-      }
-      return ((int64_t)page * p.n_kv + x.kvh) * ps + (pos - pi * ps);
-    };
-    auto load_tile = [&](const uint8_t* pool, int j, uint4 (&r)[C::LOADS]) {
-      const int kv0 = (j_lo + j) * BKV;
+    bool ok = true;
+    for (int jj = 0; jj < n_tiles && !s.abort; ++jj) {
+      const int vs = jj % C::NVR, vd = jj % C::NVF, kv0 = key0 + jj * BKV;
+      ok = mbar_wait_relaxed(&s.vr_full[vs], (jj / C::NVR) & 1) &&
+           mbar_wait_relaxed(&s.vf_empty[vd], ((jj / C::NVF) & 1) ^ 1);
+      if (!ok) break;
+      uint4 cur[C::LOADS];
 #pragma unroll
       for (int i = 0; i < C::LOADS; ++i) {
-        const int ci = i * 128 + tid, pos = kv0 + ci / CPR;
-        r[i] = make_uint4(0, 0, 0, 0);
-        if (pos < x.len) {
-          const int64_t row = pool_row(pos);
-          if (row >= 0) r[i] = *reinterpret_cast<const uint4*>(pool + row * HD + (ci % CPR) * 16);
-        }
+        const int ci = i * 128 + tid, row = ci / CPR, c = ci % CPR;
+        cur[i] = *reinterpret_cast<const uint4*>(s.vr[vs] + (c / (INNER / 16)) * (BKV * INNER) +
+                                                 code_at<INNER>(row, c % (INNER / 16)));
+        if (kv0 + row >= x.len) cur[i] = make_uint4(0, 0, 0, 0);
       }
-    };
-    int ke = 127, ve = 127;                              // threads 0..3: scales of the tile's four blocks
-    auto load_scales = [&](int j) {
-      ke = ve = 127;
-      const int pos = (j_lo + j) * BKV + tid * C8_BLOCK;
-      if (tid < 4 && pos < x.len) {
-        const int64_t row = pool_row(pos);
-        if (row >= 0) {
-          ke = p.c.ks[row / C8_BLOCK];
-          ve = p.c.vs[row / C8_BLOCK];
-        }
-      }
-    };
-    // ring order = the order the MMA warp consumes: K_0, K_1, then V_j, K_{j+2} for j = 0, 1, ...
-    const int total = 2 * n_tiles;
-    auto entry = [&](int r, bool& is_v, int& j) {
-      if (r < 2 && r < n_tiles) { is_v = false; j = r; return; }
-      // behind K_0, K_1: V_0 K_2 V_1 K_3 ... and the last two V without a K between
-      const int k = r - (n_tiles < 2 ? n_tiles : 2);
-      const int pairs = n_tiles > 2 ? n_tiles - 2 : 0;
-      if (k < 2 * pairs) { is_v = !(k & 1); j = is_v ? k >> 1 : (k >> 1) + 2; }
-      else { is_v = true; j = pairs + (k - 2 * pairs); }
-    };
-    uint4 cur[C::LOADS], nxt[C::LOADS];
-    bool is_v;
-    int j;
-    entry(0, is_v, j);
-    load_tile(p.c.k, j, cur);
-    load_scales(j);
-    bool ok = true;
-    for (int r = 0; r < total && !s.abort; ++r) {
-      const int ke_c = ke, ve_c = ve, j_c = j;
-      const bool v_c = is_v;
-      if (r + 1 < total) {
-        entry(r + 1, is_v, j);
-        load_tile(is_v ? p.c.v : p.c.k, j, nxt);
-        if (!is_v) load_scales(j);
-      }
-      const int stage = r % STAGES;
-      if (!mbar_wait_relaxed(&s.kv_empty[stage], ((r / STAGES) & 1) ^ 1)) { ok = false; break; }
-      if (!v_c && tid < 4) s.sc[j_c % SC_RING][tid] = make_float4(c8_pow2(ke_c - 127), (float)(ve_c - 127), c8_pow2(127 - ve_c), 0.f);
-      uint8_t* dst = s.kv[stage];
 #pragma unroll
       for (int i = 0; i < C::LOADS; ++i) {
         const int ci = i * 128 + tid, row = ci / CPR, c16 = ci % CPR;
         uint4 lo, hi;
         lo.x = c8_half2_lo(cur[i].x); lo.y = c8_half2_hi(cur[i].x); lo.z = c8_half2_lo(cur[i].y); lo.w = c8_half2_hi(cur[i].y);
         hi.x = c8_half2_lo(cur[i].z); hi.y = c8_half2_hi(cur[i].z); hi.z = c8_half2_lo(cur[i].w); hi.w = c8_half2_hi(cur[i].w);
-        // two 16-byte chunks of the row's 128-byte slice; the halves of a warp that write the same chunk of two
-        // slices take the two in opposite order (no bank conflict)
-        uint8_t* base = dst + (c16 >> 2) * C::KV_SUB_BYTES + row * 128;
+        // two 16-byte chunks of the row's 128-byte slice; the threads of a warp that write the same chunk of two slices
+        // take the two in opposite order (no bank conflict)
+        uint8_t* base = s.vf[vd] + (c16 >> 2) * C::VF_SUB + row * 128;
         const int ch = (c16 & 3) * 2, sw = row & 7, flip = (c16 >> 2) & 1;
         *reinterpret_cast<uint4*>(base + (((ch + flip) ^ sw) << 4)) = flip ? hi : lo;
         *reinterpret_cast<uint4*>(base + (((ch + (flip ^ 1)) ^ sw) << 4)) = flip ? lo : hi;
@@ -292,101 +426,27 @@ attn8_kernel(const __grid_constant__ A8Dev p, int* __restrict__ status) {
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(&s.kv_full[stage]);
-        if (!v_c && tid == 0) mbar_arrive(&s.sc_full[j_c % SC_RING]);
-      }
-#pragma unroll
-      for (int i = 0; i < C::LOADS; ++i) cur[i] = nxt[i];
-    }
-    if (!ok) A8_ABORT(s, status);
-  } else if (warp == C::SM_WARPS + 4) {
-    // ------------------------------------------------------------------ MMA issuer (whole warp, elected lane)
-    const uint32_t leader = elect_one();
-    constexpr uint32_t idesc_s = umma_idesc_f16(128, BKV, 0);
-    constexpr uint32_t idesc_o = umma_idesc_f16(128, HD, 1);
-    uint64_t q_desc[NQT];
-    for (int t = 0; t < NQT; ++t) q_desc[t] = umma_smem_desc(smem_u32(s.q[t]), 16, 1024);
-    const uint64_t k_desc0 = umma_smem_desc(smem_u32(s.kv[0]), 16, 1024);                 // K-major
-    const uint64_t v_desc0 = umma_smem_desc(smem_u32(s.kv[0]), C::KV_SUB_BYTES, 1024);    // MN-major
-    auto issue_s = [&](int t, int j, int stage) {
-      const uint64_t qd = q_desc[t];
-      const uint64_t kd = k_desc0 + uint64_t(stage * (C::KV_TILE_BYTES >> 4));
-      const uint32_t d = tmem_base + C::S_COL + (t * 2 + (j & 1)) * BKV;
-#pragma unroll
-      for (int kk = 0; kk < HD / 16; ++kk) {
-        const uint64_t ad = qd + uint64_t(((kk >> 2) * 16384 + (kk & 3) * 32) >> 4);
-        const uint64_t bd = kd + uint64_t(((kk >> 2) * C::KV_SUB_BYTES + (kk & 3) * 32) >> 4);
-        umma_bf16_ss_w(leader, d, ad, bd, idesc_s, kk > 0 ? 1u : 0u);
-      }
-      umma_commit_w(leader, &s.s_full[t][j & 1]);
-    };
-    auto issue_pv = [&](int t, int j, int stage) {
-      // A operand = P_t in TMEM: 16 keys are 8 packed 32-bit columns; B = V tile, MN-major
-      const uint32_t pa = tmem_base + C::S_COL + (t * 2 + (j & 1)) * BKV;
-      const uint64_t vd = v_desc0 + uint64_t(stage * (C::KV_TILE_BYTES >> 4));
-      const uint32_t d = tmem_base + C::O_COL + t * HD;
-#pragma unroll
-      for (int kk = 0; kk < BKV / 16; ++kk)
-        umma_bf16_ts_w(leader, d, pa + kk * 8, vd + uint64_t((kk * 2048) >> 4), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
-      umma_commit_w(leader, &s.pv_done[t][j & 1]);
-    };
-    int ring = 0;
-    auto wait_tile = [&](int& stage) {      // next ring entry, in the converters' order
-      stage = ring % STAGES;
-      const uint32_t phase = (ring / STAGES) & 1;
-      ++ring;
-      return mbar_wait_relaxed(&s.kv_full[stage], phase);
-    };
-    bool ok = mbar_wait_relaxed(&s.q_full, 0);
-    for (int j = 0; j < 2 && j < n_tiles && ok; ++j) {
-      int sk;
-      ok = wait_tile(sk);
-      if (!ok) break;
-      tc_fence_after();
-      for (int t = 0; t < NQT; ++t) issue_s(t, j, sk);
-      umma_commit_w(leader, &s.kv_empty[sk]);
-    }
-    for (int jj = 0; jj < n_tiles && ok && !s.abort; ++jj) {
-      int sv, sk = 0;
-      ok = wait_tile(sv);
-      const bool more = jj + 2 < n_tiles;
-      for (int t = 0; t < NQT && ok; ++t) {
-        ok = mbar_wait_relaxed(&s.p_ready[t][jj & 1], (jj >> 1) & 1);
-        if (!ok) break;
-        tc_fence_after();
-        issue_pv(t, jj, sv);
-        if (more) {
-          // the scores of key tile jj+2 go into the buffer P_t(jj) occupies: the tensor pipe runs its instructions
-          // in order, so the product above has read P before this overwrites it
-          if (t == 0) {
-            ok = wait_tile(sk);
-            if (!ok) break;
-            tc_fence_after();
-          }
-          issue_s(t, jj + 2, sk);
-        }
-      }
-      if (ok) {
-        umma_commit_w(leader, &s.kv_empty[sv]);
-        if (more) umma_commit_w(leader, &s.kv_empty[sk]);
+        mbar_arrive(&s.vf_full[vd]);
+        mbar_arrive(&s.vr_empty[vs]);
       }
     }
     if (!ok) A8_ABORT(s, status);
   } else {
     // ------------------------------------------------------------------ softmax warpgroups
+    if constexpr (NQT == 2) regs_inc<200>();
     const int t = warp >> 2;
     const int quarter = warp & 3;
     const int row = quarter * 32 + lane;                  // row in the tile == TMEM lane
     const int i_row = x.q0 + t * x.per + row / x.heads;   // row of the sequence
     const bool used = row < x.per * x.heads && i_row < x.n;
     const int pos = used ? x.len - x.n + i_row : -1;      // its position; unused rows see nothing
-    // positions of this tile's rows: keys up to `pos_min` need no causal mask, keys below `edge` a window mask
+    // positions of this tile's rows: keys up to pos_min need no causal mask, keys from pos_max - window on no window mask
     const int pos_min = x.pos0 + t * x.per;
     const int pos_max = pos_min + x.per - 1;
     const uint32_t lane_addr = uint32_t(quarter * 32) << 16;
-    const uint32_t s_addr = tmem_base + lane_addr + C::S_COL + t * 2 * BKV;
     const uint32_t o_addr = tmem_base + lane_addr + C::O_COL + t * HD;
-    // this thread's query row, scaled so that its largest element is in [2^12, 2^13)
+    // this thread's query row, scaled so that its largest element is in [2^7, 2^8), as the nearest codes and the nearest
+    // codes of what is left
     float c_row;
     {
       const uint4* src = reinterpret_cast<const uint4*>(p.q + ((int64_t)x.row0 + (used ? i_row : 0)) * p.ldq +
@@ -401,18 +461,29 @@ attn8_kernel(const __grid_constant__ A8Dev p, int* __restrict__ status) {
           am = max3(am, fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xffff0000u)));
       }
       const int eb = max((int)(__float_as_uint(am) >> 23), 20);
-      const float mul = c8_pow2(139 - eb);
-      c_row = c8_pow2(eb - 139) * p.scale_log2;
-#pragma unroll 4
-      for (int c = 0; c < HD / 8; ++c) {
-        const uint4 v = used ? src[c] : make_uint4(0, 0, 0, 0);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-        uint32_t o[4];
+      const float mul = c8_pow2(134 - eb);
+      c_row = c8_pow2(eb - 134) * p.scale_log2;
+#pragma unroll 2
+      for (int c = 0; c < HD / 16; ++c) {
+        uint32_t hi[4], lo[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          o[k] = pack_h2(__uint_as_float(w[k] << 16) * mul, __uint_as_float(w[k] & 0xffff0000u) * mul);
-        *reinterpret_cast<uint4*>(s.q[t] + (c >> 3) * 16384 + row * 128 + (((c & 7) ^ (row & 7)) << 4)) =
-            make_uint4(o[0], o[1], o[2], o[3]);
+        for (int u = 0; u < 2; ++u) {
+          const uint4 v = used ? src[2 * c + u] : make_uint4(0, 0, 0, 0);
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float e0 = __uint_as_float(w[2 * k] << 16) * mul, e1 = __uint_as_float(w[2 * k] & 0xffff0000u) * mul;
+            const float e2 = __uint_as_float(w[2 * k + 1] << 16) * mul, e3 = __uint_as_float(w[2 * k + 1] & 0xffff0000u) * mul;
+            const uint32_t h4 = c8_codes4(e0, e1, e2, e3), f0 = c8_half2_lo(h4), f1 = c8_half2_hi(h4);
+            const float2 r0 = __half22float2(*reinterpret_cast<const __half2*>(&f0));
+            const float2 r1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
+            hi[2 * u + k] = h4;
+            lo[2 * u + k] = c8_codes4(e0 - r0.x, e1 - r0.y, e2 - r1.x, e3 - r1.y);
+          }
+        }
+        const int at = (c / (INNER / 16)) * (128 * INNER) + code_at<INNER>(row, c % (INNER / 16));
+        *reinterpret_cast<uint4*>(s.q[t][0] + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(s.q[t][1] + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
       }
       fence_proxy_async_smem();
       __syncwarp();
@@ -421,22 +492,25 @@ attn8_kernel(const __grid_constant__ A8Dev p, int* __restrict__ status) {
     float m_run = -INFINITY;      // running (possibly stale) maximum of the exponent, ev included
     float l_run = 0.f;
     bool ok = true;
-    auto wait_pv = [&](int j) { return mbar_wait(&s.pv_done[t][j & 1], (j >> 1) & 1); };
+    auto buf_of = [&](int jj) { return NQT == 1 ? ((jj >> 1) & 1) : t; };
+    auto wait_pv = [&](int jj) { return mbar_wait(&s.pv_done[buf_of(jj)][jj & 1], ((jj >> 1) / NB) & 1); };
 
     for (int jj = 0; jj < n_tiles && !s.abort; ++jj) {
-      const int kv0 = (j_lo + jj) * BKV;
-      const uint32_t sp_addr = s_addr + (jj & 1) * BKV;
-      if (!mbar_wait(&s.sc_full[jj % SC_RING], (jj / SC_RING) & 1)) { ok = false; break; }
+      const int kv0 = key0 + jj * BKV, J = jj >> 1, h = jj & 1, sb = buf_of(jj), grp = jj >> 3;
+      const uint32_t sp_addr = tmem_base + lane_addr + sb * 128 + h * BKV;
+      if ((jj & 7) == 0 && !mbar_wait(&s.sc_full[grp & 1], (grp >> 1) & 1)) { ok = false; break; }
       float kf[4], lv[4], iv[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float4 f = s.sc[jj % SC_RING][k];
+        const float4 f = s.sc[grp & 1][(jj & 7) * 4 + k];
         kf[k] = fmaxf(f.x * c_row, 1e-37f);              // stays positive: a masked score times it stays -inf
         lv[k] = f.y;
         iv[k] = f.z;
       }
-      if (!mbar_wait(&s.s_full[t][jj & 1], (jj >> 1) & 1)) { ok = false; break; }
-      tc_fence_after();
+      if (h == 0) {
+        if (!mbar_wait(&s.s_full[sb], (J / NB) & 1)) { ok = false; break; }
+        tc_fence_after();
+      }
       float sv[BKV];
 #pragma unroll
       for (int c = 0; c < BKV / 32; ++c)
@@ -522,7 +596,10 @@ attn8_kernel(const __grid_constant__ A8Dev p, int* __restrict__ status) {
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(&s.p_ready[t][jj & 1]);
+      if (lane == 0) {
+        mbar_arrive(&s.p_ready[sb][h]);
+        if ((jj & 7) == 7) mbar_arrive(&s.sc_empty[grp & 1]);
+      }
     }
     if (ok && !s.abort) {
       if (!wait_pv(n_tiles - 1)) {
@@ -568,7 +645,11 @@ attn8_kernel(const __grid_constant__ A8Dev p, int* __restrict__ status) {
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == C::SM_WARPS + 4) {
+  if (s.abort && threadIdx.x == 0) {
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // let in-flight bulk copies land
+  }
+  __syncthreads();
+  if (warp == C::SM_WARPS + 5) {
     tc_fence_after();
     tmem_dealloc(tmem_base, C::TMEM_COLS);
   }
@@ -638,9 +719,13 @@ int launch_t(const Attn8Args& a, A8Dev& p, cudaStream_t s) {
   }
   int* status = status_word();
   if (!status) return POP_E_CUDA;
+  CUtensorMap tk, tv;
+  if (make_tmap_u8_rows(&tk, a.c.k, HD, p.pool_rows, C::INNER, p.box) != POP_OK ||
+      make_tmap_u8_rows(&tv, a.c.v, HD, p.pool_rows, C::INNER, p.box) != POP_OK)
+    return POP_E_CUDA;
   ProfScope prof(PROF_ATTENTION, 4.0 * HD * a.n_q * a.batch * (double)a.rows * (span - (a.window > 0 ? 0.0 : 0.5 * a.rows)), s);
   if (launch_chained(attn8_kernel<HD, NQT>, dim3(a.n_kv * p.hg, (unsigned)q_tiles, (unsigned)(a.batch * splits)),
-                     dim3(C::THREADS), smem, s, p, status) != cudaSuccess)
+                     dim3(C::THREADS), smem, s, tk, tv, p, status) != cudaSuccess)
     return POP_E_CUDA;
   count_launch();
   if (splits > 1) {
@@ -664,14 +749,15 @@ int launch_attention8(const Attn8Args& a, cudaStream_t s) {
     return POP_E_INVALID;
   if (reinterpret_cast<uintptr_t>(a.workspace) % 16 || (int64_t)a.batch * a.rows > 0x7fffffff) return POP_E_INVALID;
   if (!a.seq_lens && a.rows > a.kv_len) return POP_E_INVALID;
+  // rows of the pool are 32-bit coordinates
+  if (a.c.num_pages * (int64_t)a.n_kv > 0x7ffffff0 / a.c.page_size) return POP_E_INVALID;
   if ((int64_t)a.kv_len > (int64_t)a.c.max_pages * a.c.page_size) return POP_E_NOSPACE;
   if (a.rows == 0) return POP_OK;
   A8Dev p{};
   p.q = a.q; p.ldq = a.ldq;
   p.c = a.c;
-  p.ps_log2 = -1;
-  for (int i = 4; i < 31; ++i)
-    if (a.c.page_size == 1 << i) p.ps_log2 = i;
+  p.box = a.c.page_size < 64 ? a.c.page_size : 64;
+  p.pool_rows = (int)(a.c.num_pages * (int64_t)a.n_kv * a.c.page_size);
   p.cu = a.cu; p.rows = a.rows;
   p.seq_lens = a.seq_lens; p.kv_len = a.kv_len;
   p.out = a.out; p.ldo = a.ldo;

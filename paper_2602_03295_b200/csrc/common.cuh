@@ -95,6 +95,10 @@ int make_tmap_bf16_3d(CUtensorMap* out, const void* base, uint64_t dim0, uint64_
 // 3-D byte tensor (FP8 operands), 128-byte swizzle, box = [1][box1][128]
 int make_tmap_u8_3d(CUtensorMap* out, const void* base, uint64_t dim0, uint64_t dim1, uint64_t dim2,
                     uint64_t stride1_bytes, uint64_t stride2_bytes, uint32_t box1);
+// 2-D byte tensor [rows][row_bytes], rows contiguous, box = [box_rows][inner], inner 128 or 64 bytes with the swizzle of
+// that width: the codes of the 8-bit cache, one row per position and head
+int make_tmap_u8_rows(CUtensorMap* out, const void* base, uint64_t row_bytes, uint64_t rows, uint32_t inner,
+                      uint32_t box_rows);
 int make_tmap_f32_3d(CUtensorMap* out, const void* base, uint64_t dim0, uint64_t dim1, uint64_t dim2,
                      uint64_t stride1_elems, uint64_t stride2_elems, uint32_t box1);
 // rank-`rank` (3..5) bf16 tensor, dims/strides/box given innermost first (strides in elements, for

@@ -6,6 +6,7 @@ import torch
 
 BLOCK = 16
 F32 = 2.0 ** -24             # half a step of fp32, relative
+DECODE_SHIFT = 14            # the single-query kernel's weights are stored times 2^14, the prompt kernel's times 2^7
 
 
 def round_e4m3(y):
@@ -88,7 +89,12 @@ def attend(q, k, v, seen, ev, shift):
     Weights below f16's smallest normal value are off by up to 2^-25 absolutely. What is stored for key j is
     w_j = A p_j 2^ev_j, A such that the largest is 2^shift or more: A >= 2^shift / max_j p_j 2^ev_j. The result is
     sum_j w_j c_j / A with c_j the codes' values, so 2^-25 in every w_j costs at most 2^-25 sum_j |c_j| / A
-    <= 2^(-25 - shift) max_j (p_j 2^ev_j) sum_j |c_j|."""
+    <= 2^(-25 - shift) max_j (p_j 2^ev_j) sum_j |c_j|.
+
+    The kernels hold an element of q as the sum of two E4M3 codes after a power-of-two scale that brings the
+    head's largest element to 2^7 or more. The first code leaves at most 2^-4 of the element, four bits of a bf16 element's
+    eight, which the second holds unless it is below the smallest normal code: then it is off by at most half a step of
+    2^-9, 2^-17 of the head's largest. That is an absolute error of the score of 2^-17 max |q| sum |k| / sqrt(hd)."""
     hd = q.shape[-1]
     if not bool(seen.any()):
         return torch.zeros_like(q), torch.zeros_like(q)
@@ -97,7 +103,8 @@ def attend(q, k, v, seen, ev, shift):
     p = torch.softmax(s, 0)
     out = torch.einsum("nh,nhd->hd", p, v)
     size = torch.einsum("hd,nhd->nh", q.abs(), k.abs()).amax(0) / math.sqrt(hd)              # [heads]
-    rel = 2.0 ** -11 + 2.0 ** -20 + 2 * (hd + 4) * F32 * size + 2 * (k.shape[0] / 16 + 64) * F32
+    split = 2.0 ** -17 * q.abs().amax(1) * k.abs().sum(2).amax(0) / math.sqrt(hd)
+    rel = 2.0 ** -11 + 2.0 ** -20 + 2 * ((hd + 4) * F32 * size + split) + 2 * (k.shape[0] / 16 + 64) * F32
     mean_abs = torch.einsum("nh,nhd->hd", p, v.abs())
     codes = (v.abs() / torch.exp2(ev)[..., None]).sum(0)                                      # [heads, hd]
     small = 2.0 ** (-25 - shift) * (p * torch.exp2(ev)).amax(0)[:, None] * codes

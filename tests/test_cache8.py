@@ -71,7 +71,7 @@ REFUSED = {
                        dict(positions=A), dict(pair_axis=A), dict(positions=A, pair_axis=A, n_axes=300), dict(n_q=-1),
                        dict(batch=70000), dict(batch=60000, max_rows=60000)],
     "decode": CACHE + [dict(q=None), dict(out=None), dict(q=A + 8), dict(out=A + 2), dict(ldq=65), dict(ldo=68),
-                       dict(n_q=3, n_kv=2), dict(n_q=0), dict(kv_len=-1), dict(window=-1), dict(batch=16385),
+                       dict(n_q=3, n_kv=2), dict(n_q=0), dict(kv_len=-1), dict(window=-1), dict(batch=8193),
                        dict(workspace=A + 4)],
     "prompt": CACHE + [dict(q=None), dict(out=None), dict(q=A + 8), dict(out=A + 2), dict(ldq=65), dict(ldo=68),
                        dict(n_q=3, n_kv=2), dict(n_q=0), dict(kv_len=-1), dict(window=-1), dict(max_rows=-1),

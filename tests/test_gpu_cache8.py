@@ -284,7 +284,7 @@ def test_append_raises_the_status_for_bad_places(L):
 
 
 # ---------------------------------------------------------------------------------------------- attention
-def check_attention(q, got, cache, rows, lens, n_q, n_kv, hd, window, pick=None, shift=7):
+def check_attention(q, got, cache, rows, lens, n_q, n_kv, hd, window, pick=None, decode=False):
     k8, v8, ks, vs, table = cache
     r0 = 0
     for b, (n, ln) in enumerate(zip(rows, lens)):
@@ -296,7 +296,7 @@ def check_attention(q, got, cache, rows, lens, n_q, n_kv, hd, window, pick=None,
             seen = pos <= at
             if window:
                 seen &= pos > at - window
-            want, tol = ref.attend(q[r0 + i].double().view(n_q, hd), k, v, seen, ev, shift)
+            want, tol = ref.attend(q[r0 + i].double().view(n_q, hd), k, v, seen, ev, ref.DECODE_SHIFT if decode else 7)
             d = (got[r0 + i].double().view(n_q, hd) - want).abs()
             assert (d <= tol).all(), (b, i, (d / tol.clamp_min(1e-30)).max())
         r0 += n
@@ -326,7 +326,7 @@ def test_decode_attention(L, lens, n_q, n_kv, hd, page, window):
     L.decode_attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, max(lens), window=window,
                             seq_lens=torch.tensor(lens, dtype=torch.int32, device=DEV))
     assert L.status() == 0
-    check_attention(q, out.cpu(), cache, [1] * len(lens), lens, n_q, n_kv, hd, window)
+    check_attention(q, out.cpu(), cache, [1] * len(lens), lens, n_q, n_kv, hd, window, decode=True)
 
 
 @pytest.mark.parametrize("length,hd,page", [(1, 128, 16), (16, 64, 16), (333, 128, 32), (640, 256, 128), (1500, 64, 64)])
@@ -338,7 +338,7 @@ def test_decode_attention_with_equal_lengths_and_strides(L, length, hd, page):
     dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
     L.decode_attention_e4m3(q.to(DEV)[:, :n_q * hd], *dev, out[:, :n_q * hd], n_q, n_kv, hd, length)
     assert L.status() == 0 and (out[:, n_q * hd:] == 5.0).all()
-    check_attention(q[:, :n_q * hd], out[:, :n_q * hd].cpu(), cache, [1] * batch, [length] * batch, n_q, n_kv, hd, 0)
+    check_attention(q[:, :n_q * hd], out[:, :n_q * hd].cpu(), cache, [1] * batch, [length] * batch, n_q, n_kv, hd, 0, decode=True)
 
 
 PROMPT = [  # rows, lens, n_q, n_kv, hd, page, window
@@ -399,7 +399,7 @@ def test_blocks_of_very_unequal_scales(L, hd, op):
         L.decode_attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, n)
     else:
         L.attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, rows, n)
-    check_attention(q, out.cpu(), cache, [rows], [n], n_q, n_kv, hd, 0)
+    check_attention(q, out.cpu(), cache, [rows], [n], n_q, n_kv, hd, 0, decode=op == "decode")
     # one key has all of the weight and the smallest values, its neighbours enormous values and no weight
     k8, v8, ks, vs, table = random_cache(43, 1, 1, n, n_kv, hd, page)
     ks[:], vs[:] = 100, 160
@@ -414,7 +414,7 @@ def test_blocks_of_very_unequal_scales(L, hd, op):
         L.decode_attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, n)
     else:
         L.attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, rows, n)
-    check_attention(q, out.cpu(), (k8, v8, ks, vs, table), [rows], [n], n_q, n_kv, hd, 0)
+    check_attention(q, out.cpu(), (k8, v8, ks, vs, table), [rows], [n], n_q, n_kv, hd, 0, decode=op == "decode")
 
 
 def test_attention_with_tiny_and_zero_queries(L):
@@ -427,7 +427,7 @@ def test_attention_with_tiny_and_zero_queries(L):
     q[2, :hd] = 0
     out = torch.empty_like(q, device=DEV)
     L.decode_attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, n)
-    check_attention(q, out.cpu(), cache, [1] * 3, [n] * 3, n_q, n_kv, hd, 0)
+    check_attention(q, out.cpu(), cache, [1] * 3, [n] * 3, n_q, n_kv, hd, 0, decode=True)
     L.attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, 1, n)
     check_attention(q, out.cpu(), cache, [1] * 3, [n] * 3, n_q, n_kv, hd, 0)
 
@@ -487,7 +487,7 @@ def test_prompt_chunk_drafts_and_decode_over_one_cache(L, hd, n_q, n_kv, page, w
                              window=window, workspace=ws)
         assert L.status() == 0
         cpu = tuple(t[layer:layer + 1].cpu() for t in (c.k, c.v, c.k_scale, c.v_scale)) + (c.block_table.cpu(),)
-        check_attention(q.cpu(), out.cpu(), cpu, rows, now, n_q, n_kv, hd, window)
+        check_attention(q.cpu(), out.cpu(), cpu, rows, now, n_q, n_kv, hd, window, decode=single)
         return now
 
     for layer in range(2):
@@ -589,6 +589,6 @@ def test_offsets_behind_32_bits(L):
     local = tuple(t[ids[0].long().to(DEV)].cpu()[None] for t in (k8, v8, ks, vs)) + (torch.tensor([[0, 1, 2]], dtype=torch.int32),)
     before = tuple(u[:, small[4][0].long()] for u in small[:4]) + (local[4],)
     check_append(case, a, before, q.cpu(), [t[0] for t in local[:4]])
-    check_attention(q.cpu(), out.cpu(), local, [1], [n + 1], 8, n_kv, hd, 0)
+    check_attention(q.cpu(), out.cpu(), local, [1], [n + 1], 8, n_kv, hd, 0, decode=True)
     L.attention_e4m3(q, k8, v8, ks, vs, ids.to(DEV), out, 8, n_kv, hd, 1, n + 1)
     check_attention(q.cpu(), out.cpu(), local, [1], [n + 1], 8, n_kv, hd, 0)
