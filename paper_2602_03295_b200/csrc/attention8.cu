@@ -62,7 +62,7 @@ struct __align__(1024) A8Smem {
   uint8_t vr[C::NVR][C::VR_STAGE];
   uint8_t vf[C::NVF][C::VF_STAGE];
   float4 sc[2][32];             // per block of 16 keys: 2^ek, ev, 2^-ev; two groups of 32 blocks
-  uint64_t q_full;
+  float crow[NQT * 128];        // factor of each row's scores
   uint64_t k_full[C::NK], k_empty[C::NK];
   uint64_t vr_full[C::NVR], vr_empty[C::NVR];
   uint64_t vf_full[C::NVF], vf_empty[C::NVF];
@@ -85,6 +85,8 @@ struct A8Dev {
   bf16* out; int64_t ldo;
   int n_q, n_kv, G, hg;         // query heads per kv head; head groups of at most 128 per kv head
   int window;
+  int per;                      // positions per tile (one head group)
+  uint32_t inv;                 // 2^16 / G, rounded up
   int q_tiles;                  // CTAs along the rows of the longest sequence
   int splits;
   float* partial;               // [CTA][NQT * 128][hd + 4]: m, l, two unused, accumulator
@@ -94,7 +96,8 @@ struct A8Dev {
 // The rows and keys of one CTA (without the split)
 struct Job {
   int b, kvh, h0, heads, per;   // heads of this group; positions per tile
-  int row0, n, q0;              // first packed row of the sequence, its rows, first row of the CTA
+  uint32_t inv;                 // 2^16 / heads, rounded up: r / heads = r * inv >> 16 for r < 256
+  int row0, n, q0;              // first packed row of the sequence, its rows, first row of the CTA (< 0: none)
   int len, pos0;                // cached positions; position of row q0
   int j_lo, n_tiles;            // 64-key tiles that its rows see
 };
@@ -102,28 +105,41 @@ template <int NQT>
 __device__ __forceinline__ Job job_of(const A8Dev& p, int bx, int by, int b, int* status) {
   Job x;
   x.b = b;
-  x.kvh = bx / p.hg;
-  const int grp = bx - x.kvh * p.hg;
-  x.h0 = x.kvh * p.G + grp * 128;
-  x.heads = min(128, p.G - grp * 128);
-  x.per = 128 / x.heads;
-  x.row0 = p.cu ? p.cu[b] : b * p.rows;
-  x.n = p.cu ? p.cu[b + 1] - x.row0 : p.rows;
+  // the lengths' loads first: all of them are in flight together
+  const int c0 = p.cu ? p.cu[b] : b * p.rows, c1 = p.cu ? p.cu[b + 1] : c0 + p.rows;
   x.len = p.seq_lens ? p.seq_lens[b] : p.kv_len;
+  if (p.hg == 1) {
+    x.kvh = bx;
+    x.h0 = bx * p.G;
+    x.heads = p.G;
+    x.per = p.per;
+    x.inv = p.inv;
+  } else {
+    x.kvh = bx / p.hg;
+    const int grp = bx - x.kvh * p.hg;
+    x.h0 = x.kvh * p.G + grp * 128;
+    x.heads = min(128, p.G - grp * 128);
+    x.per = 128 / x.heads;
+    x.inv = (65536 + x.heads - 1) / x.heads;
+  }
+  x.row0 = c0;
+  x.n = c1 - c0;
   if (x.len > p.kv_len || x.n > p.rows) {       // more than the caller said: nothing past it is touched
     atomicMin(status, (int)POP_E_INVALID);
     x.n = min(x.n, p.rows);
     x.len = min(x.len, p.kv_len);
   }
   x.len = max(x.len, 0);
-  const int tile = (int)(((int64_t)x.n + (int64_t)NQT * x.per - 1) / (NQT * x.per)) - 1 - by;   // latest rows first
-  x.q0 = tile * NQT * x.per;
+  // latest rows first
+  const int step = NQT * x.per, tile = (x.n > 0 ? (x.n - 1) / step : -1) - by;
+  x.q0 = tile * step;
   x.pos0 = x.len - x.n + x.q0;
-  const int last = min(x.pos0 + NQT * x.per - 1, x.len - 1);
+  const int last = min(x.pos0 + step - 1, x.len - 1);
   x.j_lo = p.window > 0 ? max(0, x.pos0 - p.window + 1) / 64 : 0;
   x.n_tiles = last < 0 || tile < 0 ? 0 : last / 64 - x.j_lo + 1;
   return x;
 }
+__device__ __forceinline__ int row_pos(const Job& x, int r) { return (int)(r * x.inv >> 16); }     // r / heads
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
@@ -184,36 +200,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
   chain_trigger();
   const int warp = threadIdx.x >> 5;
   const int lane = threadIdx.x & 31;
-  chain_wait();
-  const int split = blockIdx.z % p.splits;
-  const Job x = job_of<NQT>(p, blockIdx.x, blockIdx.y, blockIdx.z / p.splits, status);
-  if (x.q0 < 0) return;                                  // past the rows of this sequence
-  const int t_lo = (int)((int64_t)x.n_tiles * split / p.splits);
-  const int n_tiles = (int)((int64_t)x.n_tiles * (split + 1) / p.splits) - t_lo;      // 64 keys each
-  const int n_pairs = (n_tiles + 1) >> 1;
-  const int key0 = (x.j_lo + t_lo) * BKV;                // first key of tile 0
-  float* part = p.splits > 1 ? p.partial + (((int64_t)(blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x) *
-                                            (NQT * 128)) * (HD + 4)
-                             : nullptr;
-
-  if (status_raised(status, &s.raised)) return;
-  if (n_tiles <= 0) {                                    // rows that see nothing (here): zeros, or an empty piece
-    for (int r = threadIdx.x; r < NQT * 128; r += blockDim.x) {
-      if (part != nullptr) {
-        part[(int64_t)r * (HD + 4)] = -INFINITY;
-        part[(int64_t)r * (HD + 4) + 1] = 0.f;
-        continue;
-      }
-      const int in_tile = r & 127, i = x.q0 + (r >> 7) * x.per + in_tile / x.heads;
-      if (in_tile >= x.per * x.heads || i >= x.n) continue;
-      uint4* dst = reinterpret_cast<uint4*>(p.out + ((int64_t)x.row0 + i) * p.ldo +
-                                            (int64_t)(x.h0 + in_tile % x.heads) * HD);
-      for (int c = 0; c < HD / 8; ++c) dst[c] = make_uint4(0, 0, 0, 0);
-    }
-    return;
-  }
-  if (threadIdx.x == 0) {
-    mbar_init(&s.q_full, C::SM_WARPS);
+  if (threadIdx.x == (C::SM_WARPS + 4) * 32) {           // the TMA warp's first lane: it uses them before the others do
     for (int i = 0; i < C::NK; ++i) { mbar_init(&s.k_full[i], 1); mbar_init(&s.k_empty[i], 1); }
     for (int i = 0; i < C::NVR; ++i) { mbar_init(&s.vr_full[i], 1); mbar_init(&s.vr_empty[i], 4); }
     for (int i = 0; i < C::NVF; ++i) { mbar_init(&s.vf_full[i], 4); mbar_init(&s.vf_empty[i], 1); }
@@ -227,14 +214,42 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     prefetch_tmap(&tmK);
     prefetch_tmap(&tmV);
   }
-  if (warp == C::SM_WARPS + 5) {
-    tmem_alloc(&s.tmem_base, C::TMEM_COLS);
-    tmem_relinquish();
+  chain_wait();
+  // the status word is on its way while the lengths are (read by the TMA warp alone)
+  int raised = 0;
+  if (warp == C::SM_WARPS + 4) raised = *reinterpret_cast<const volatile int*>(status);
+  int split = 0, b = blockIdx.z;
+  if (p.splits > 1) {
+    b = blockIdx.z / p.splits;
+    split = blockIdx.z - b * p.splits;
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem_base = s.tmem_base;
+  const Job x = job_of<NQT>(p, blockIdx.x, blockIdx.y, b, status);
+  if (x.q0 < 0) return;                                  // past the rows of this sequence
+  int t_lo = 0, n_tiles = x.n_tiles;                     // 64 keys each
+  float* part = nullptr;
+  if (p.splits > 1) {
+    t_lo = (int)((int64_t)x.n_tiles * split / p.splits);
+    n_tiles = (int)((int64_t)x.n_tiles * (split + 1) / p.splits) - t_lo;
+    part = p.partial + (((int64_t)(blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x) * (NQT * 128)) * (HD + 4);
+  }
+  const int n_pairs = (n_tiles + 1) >> 1;
+  const int key0 = (x.j_lo + t_lo) * BKV;                // first key of tile 0
+
+  if (n_tiles <= 0) {                                    // rows that see nothing (here): zeros, or an empty piece
+    for (int r = threadIdx.x; r < NQT * 128; r += blockDim.x) {
+      if (part != nullptr) {
+        part[(int64_t)r * (HD + 4)] = -INFINITY;
+        part[(int64_t)r * (HD + 4) + 1] = 0.f;
+        continue;
+      }
+      const int in_tile = r & 127, ip = row_pos(x, in_tile), i = x.q0 + (r >> 7) * x.per + ip;
+      if (in_tile >= x.per * x.heads || i >= x.n) continue;
+      uint4* dst = reinterpret_cast<uint4*>(p.out + ((int64_t)x.row0 + i) * p.ldo +
+                                            (int64_t)(x.h0 + in_tile - ip * x.heads) * HD);
+      for (int c = 0; c < HD / 8; ++c) dst[c] = make_uint4(0, 0, 0, 0);
+    }
+    return;
+  }
   const int32_t* bt = p.c.table + (int64_t)x.b * p.c.max_pages;
   const int ps = p.c.page_size;
   // pool row (page * n_kv + head) * page_size + slot of a position, or -1 for a table entry that is no page of the pool
@@ -247,47 +262,124 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     return (page * p.n_kv + x.kvh) * ps + (pos - pi * ps);
   };
 
+
+  // TMA: lane l holds the pool row of copy l of a pair (128 keys), fetched a pair ahead. A copy that starts past the end
+  // is left out; one of a bad page goes past the pool's end and is filled with zeros.
+  const int boxes = PKV / p.box, half_boxes = boxes >> 1;
+  auto row_of = [&](int J) {
+    const int pos = key0 + J * PKV + lane * p.box;
+    if (lane >= boxes || J >= n_pairs || pos >= x.len) return -2;
+    const int r = pool_row(pos);
+    return r < 0 ? p.pool_rows : r;
+  };
+  auto copy = [&](const CUtensorMap* tm, uint64_t* bar, uint8_t* dst, int row, int first, int count) {
+    const int live = __popc(__ballot_sync(0xffffffffu, row != -2) & (((1u << count) - 1u) << first));
+    if (lane == 0) mbar_expect_tx(bar, live * p.box * HD);
+    for (int i = 0; i < count; ++i) {
+      const int r = __shfl_sync(0xffffffffu, row, first + i);
+      if (r != -2 && lane == 0)
+        for (int c = 0; c < SLICES; ++c)
+          tma_load_2d(dst + c * (count * p.box * INNER) + i * p.box * INNER, tm, bar, c * INNER, r);
+    }
+  };
+  auto load_pair = [&](int J, int row) {
+    const int ks = J % C::NK;
+    if (!mbar_wait_relaxed(&s.k_empty[ks], ((J / C::NK) & 1) ^ 1)) return false;
+    __syncwarp();
+    copy(&tmK, &s.k_full[ks], s.k[ks], row, 0, boxes);
+    for (int h = 0; h < 2; ++h) {
+      const int jj = 2 * J + h, vs = jj % C::NVR;
+      if (jj >= n_tiles) break;
+      if (!mbar_wait_relaxed(&s.vr_empty[vs], ((jj / C::NVR) & 1) ^ 1)) return false;
+      __syncwarp();
+      copy(&tmV, &s.vr_full[vs], s.vr[vs], row, h * half_boxes, half_boxes);
+    }
+    return true;
+  };
+
+  // Start: the TMA warp asks for the first pair, the MMA warp for TMEM, the others place the query rows in shared memory:
+  // each row scaled so that its largest element is in [2^7, 2^8), as the nearest codes and the nearest codes of what is
+  // left. hd / 8 lanes take a row, 16 bytes each, several rows at once.
+  int tma_row = -2;
+  if (warp == C::SM_WARPS + 4) {
+    raised = __shfl_sync(0xffffffffu, raised, 0);
+    if (lane == 0) s.raised = raised != 0 ? 1u : 0u;
+    if (raised == 0) {
+      tma_row = row_of(0);
+      load_pair(0, tma_row);                               // the ring is empty: nothing is waited for
+      tma_row = row_of(1);
+    }
+  } else if (warp == C::SM_WARPS + 5) {
+    tmem_alloc(&s.tmem_base, C::TMEM_COLS);
+    tmem_relinquish();
+  } else if (warp < C::SM_WARPS + 4) {
+    constexpr int LPR = HD / 8, RPI = 32 / LPR, WARPS = C::SM_WARPS + 4;      // lanes per row, rows per load
+    constexpr int GROUPS = NQT * 128 / RPI;
+    static_assert(NQT * 128 * HD * 2 <= sizeof(s.vf), "the rows pass through the memory of V's stages");
+    const int c = lane % LPR;
+    // asynchronous copies and small loops instead of registers and unrolled code: this runs once per CTA, from a cold
+    // instruction cache (unrolled it took 9900 cycles, most of them fetching instructions)
+    uint8_t* raw = s.vf[0] + lane * 16;
+#pragma unroll 1
+    for (int g = warp; g < GROUPS; g += WARPS) {
+      const int r = g * RPI + lane / LPR, tr = r & 127, ip = row_pos(x, tr), iq = x.q0 + (r >> 7) * x.per + ip;
+      const bool live = tr < x.per * x.heads && iq < x.n;
+      const bf16* src = p.q;
+      if (live) src += ((int64_t)x.row0 + iq) * p.ldq + (int64_t)(x.h0 + tr - ip * x.heads) * HD + c * 8;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(raw + g * 512)), "l"(src),
+                   "r"(live ? 16 : 0) : "memory");
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+#pragma unroll 2
+    for (int g = warp; g < GROUPS; g += WARPS) {
+      const int r = g * RPI + lane / LPR;
+      const uint4 v = *reinterpret_cast<const uint4*>(raw + g * 512);       // this thread's own copy
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      float am = 0.f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        am = max3(am, fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xffff0000u)));
+#pragma unroll
+      for (int o = LPR / 2; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(0xffffffffu, am, o));
+      const int eb = max((int)(__float_as_uint(am) >> 23), 20);
+      const float mul = c8_pow2(134 - eb);
+      if (c == 0) s.crow[r] = c8_pow2(eb - 134) * p.scale_log2;
+      uint32_t hi[2], lo[2];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const float e0 = __uint_as_float(w[2 * k] << 16) * mul, e1 = __uint_as_float(w[2 * k] & 0xffff0000u) * mul;
+        const float e2 = __uint_as_float(w[2 * k + 1] << 16) * mul, e3 = __uint_as_float(w[2 * k + 1] & 0xffff0000u) * mul;
+        const uint32_t h4 = c8_codes4(e0, e1, e2, e3), f0 = c8_half2_lo(h4), f1 = c8_half2_hi(h4);
+        const float2 r0 = __half22float2(*reinterpret_cast<const __half2*>(&f0));
+        const float2 r1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
+        hi[k] = h4;
+        lo[k] = c8_codes4(e0 - r0.x, e1 - r0.y, e2 - r1.x, e3 - r1.y);
+      }
+      const int c16 = c >> 1;
+      const int at = (c16 / (INNER / 16)) * (128 * INNER) + code_at<INNER>(r & 127, c16 % (INNER / 16)) + (c & 1) * 8;
+      *reinterpret_cast<uint2*>(s.q[r >> 7][0] + at) = make_uint2(hi[0], hi[1]);
+      *reinterpret_cast<uint2*>(s.q[r >> 7][1] + at) = make_uint2(lo[0], lo[1]);
+    }
+    fence_proxy_async_smem();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = s.tmem_base;
+  if (*reinterpret_cast<volatile uint32_t*>(&s.raised)) {      // an earlier kernel gave up: do nothing
+    if (warp == C::SM_WARPS + 5) tmem_dealloc(tmem_base, C::TMEM_COLS);
+    return;
+  }
   if (warp >= C::SM_WARPS + 4) {
-    if constexpr (NQT == 2) regs_dec<56>();
+    if constexpr (NQT == 2) regs_dec<88>();
     const int role = warp - C::SM_WARPS - 4;
     if (role == 0) {
       // ---------------------------------------------------------------- TMA
-      // Lane l holds the pool row of copy l of a pair (128 keys), fetched a pair ahead. A copy that starts past the end is
-      // left out; one of a bad page goes past the pool's end and is filled with zeros.
-      const int boxes = PKV / p.box, half_boxes = boxes >> 1;
-      auto row_of = [&](int J) {
-        const int pos = key0 + J * PKV + lane * p.box;
-        if (lane >= boxes || J >= n_pairs || pos >= x.len) return -2;
-        const int r = pool_row(pos);
-        return r < 0 ? p.pool_rows : r;
-      };
-      auto copy = [&](const CUtensorMap* tm, uint64_t* bar, uint8_t* dst, int row, int first, int count) {
-        const int live = __popc(__ballot_sync(0xffffffffu, row != -2) & (((1u << count) - 1u) << first));
-        if (lane == 0) mbar_expect_tx(bar, live * p.box * HD);
-        for (int i = 0; i < count; ++i) {
-          const int r = __shfl_sync(0xffffffffu, row, first + i);
-          if (r != -2 && lane == 0)
-            for (int c = 0; c < SLICES; ++c)
-              tma_load_2d(dst + c * (count * p.box * INNER) + i * p.box * INNER, tm, bar, c * INNER, r);
-        }
-      };
-      int row = row_of(0);
       bool ok = true;
-      for (int J = 0; J < n_pairs && ok && !s.abort; ++J) {
+      for (int J = 1; J < n_pairs && ok && !s.abort; ++J) {
         const int next = row_of(J + 1);
-        const int ks = J % C::NK;
-        ok = mbar_wait_relaxed(&s.k_empty[ks], ((J / C::NK) & 1) ^ 1);
-        __syncwarp();
-        if (!ok) break;
-        copy(&tmK, &s.k_full[ks], s.k[ks], row, 0, boxes);
-        for (int h = 0; h < 2 && ok; ++h) {
-          const int jj = 2 * J + h, vs = jj % C::NVR;
-          if (jj >= n_tiles) break;
-          ok = mbar_wait_relaxed(&s.vr_empty[vs], ((jj / C::NVR) & 1) ^ 1);
-          __syncwarp();
-          if (ok) copy(&tmV, &s.vr_full[vs], s.vr[vs], row, h * half_boxes, half_boxes);
-        }
-        row = next;
+        ok = load_pair(J, tma_row);
+        tma_row = next;
       }
       if (!ok) A8_ABORT(s, status);
     } else if (role == 1) {
@@ -324,7 +416,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
           umma_bf16_ts_w(leader, d, pa + kk * 8, vd + uint64_t((kk * 2048) >> 4), idesc_o, (jj > 0 || kk > 0) ? 1u : 0u);
         umma_commit_w(leader, &s.pv_done[sb][h]);
       };
-      bool ok = mbar_wait_relaxed(&s.q_full, 0);
+      bool ok = true;
       // scores of the first pair (of two pairs where one tile has both buffers)
       for (int J = 0; J < NB && J < n_pairs && ok; ++J) {
         ok = mbar_wait_relaxed(&s.k_full[J % C::NK], (J / C::NK) & 1);
@@ -393,7 +485,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     }
   } else if (warp >= C::SM_WARPS) {
     // ------------------------------------------------------------------ converters: V codes -> f16, 64 keys at a time
-    if constexpr (NQT == 2) regs_dec<56>();
+    if constexpr (NQT == 2) regs_dec<72>();
     const int tid = threadIdx.x - C::SM_WARPS * 32;
     constexpr int CPR = HD / 16;                         // 16-code pieces per row
     bool ok = true;
@@ -433,11 +525,11 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     if (!ok) A8_ABORT(s, status);
   } else {
     // ------------------------------------------------------------------ softmax warpgroups
-    if constexpr (NQT == 2) regs_inc<200>();
+    if constexpr (NQT == 2) regs_inc<176>();
     const int t = warp >> 2;
     const int quarter = warp & 3;
     const int row = quarter * 32 + lane;                  // row in the tile == TMEM lane
-    const int i_row = x.q0 + t * x.per + row / x.heads;   // row of the sequence
+    const int ip_row = row_pos(x, row), i_row = x.q0 + t * x.per + ip_row;   // row of the sequence
     const bool used = row < x.per * x.heads && i_row < x.n;
     const int pos = used ? x.len - x.n + i_row : -1;      // its position; unused rows see nothing
     // positions of this tile's rows: keys up to pos_min need no causal mask, keys from pos_max - window on no window mask
@@ -445,57 +537,14 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     const int pos_max = pos_min + x.per - 1;
     const uint32_t lane_addr = uint32_t(quarter * 32) << 16;
     const uint32_t o_addr = tmem_base + lane_addr + C::O_COL + t * HD;
-    // this thread's query row, scaled so that its largest element is in [2^7, 2^8), as the nearest codes and the nearest
-    // codes of what is left
-    float c_row;
-    {
-      const uint4* src = reinterpret_cast<const uint4*>(p.q + ((int64_t)x.row0 + (used ? i_row : 0)) * p.ldq +
-                                                        (int64_t)(x.h0 + (used ? row % x.heads : 0)) * HD);
-      float am = 0.f;
-#pragma unroll 4
-      for (int c = 0; c < HD / 8; ++c) {
-        const uint4 v = used ? src[c] : make_uint4(0, 0, 0, 0);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          am = max3(am, fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xffff0000u)));
-      }
-      const int eb = max((int)(__float_as_uint(am) >> 23), 20);
-      const float mul = c8_pow2(134 - eb);
-      c_row = c8_pow2(eb - 134) * p.scale_log2;
-#pragma unroll 2
-      for (int c = 0; c < HD / 16; ++c) {
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const uint4 v = used ? src[2 * c + u] : make_uint4(0, 0, 0, 0);
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float e0 = __uint_as_float(w[2 * k] << 16) * mul, e1 = __uint_as_float(w[2 * k] & 0xffff0000u) * mul;
-            const float e2 = __uint_as_float(w[2 * k + 1] << 16) * mul, e3 = __uint_as_float(w[2 * k + 1] & 0xffff0000u) * mul;
-            const uint32_t h4 = c8_codes4(e0, e1, e2, e3), f0 = c8_half2_lo(h4), f1 = c8_half2_hi(h4);
-            const float2 r0 = __half22float2(*reinterpret_cast<const __half2*>(&f0));
-            const float2 r1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
-            hi[2 * u + k] = h4;
-            lo[2 * u + k] = c8_codes4(e0 - r0.x, e1 - r0.y, e2 - r1.x, e3 - r1.y);
-          }
-        }
-        const int at = (c / (INNER / 16)) * (128 * INNER) + code_at<INNER>(row, c % (INNER / 16));
-        *reinterpret_cast<uint4*>(s.q[t][0] + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        *reinterpret_cast<uint4*>(s.q[t][1] + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-      }
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&s.q_full);
-    }
+    const float c_row = s.crow[t * 128 + row];
     float m_run = -INFINITY;      // running (possibly stale) maximum of the exponent, ev included
     float l_run = 0.f;
     bool ok = true;
     auto buf_of = [&](int jj) { return NQT == 1 ? ((jj >> 1) & 1) : t; };
     auto wait_pv = [&](int jj) { return mbar_wait(&s.pv_done[buf_of(jj)][jj & 1], ((jj >> 1) / NB) & 1); };
 
-    for (int jj = 0; jj < n_tiles && !s.abort; ++jj) {
+    for (int jj = 0; jj < n_tiles; ++jj) {
       const int kv0 = key0 + jj * BKV, J = jj >> 1, h = jj & 1, sb = buf_of(jj), grp = jj >> 3;
       const uint32_t sp_addr = tmem_base + lane_addr + sb * 128 + h * BKV;
       if ((jj & 7) == 0 && !mbar_wait(&s.sc_full[grp & 1], (grp >> 1) & 1)) { ok = false; break; }
@@ -608,7 +657,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         tc_fence_after();
         const bool none = l_run == 0.f;                          // a row that sees nothing is a row of zeros
         const float inv = none ? 0.f : 1.0f / l_run;
-        bf16* out = p.out + ((int64_t)x.row0 + i_row) * p.ldo + (int64_t)(x.h0 + row % x.heads) * HD;
+        bf16* out = p.out + ((int64_t)x.row0 + i_row) * p.ldo + (int64_t)(x.h0 + row - ip_row * x.heads) * HD;
         float* pr = part != nullptr ? part + (int64_t)(t * 128 + row) * (HD + 4) : nullptr;
         if (pr != nullptr) *reinterpret_cast<float4*>(pr) = make_float4(m_run, l_run, 0.f, 0.f);
 #pragma unroll 1
@@ -664,7 +713,7 @@ __global__ void __launch_bounds__(256) attn8_merge_kernel(const __grid_constant_
   const int by = blockIdx.y / groups, r = (blockIdx.y % groups) * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const Job x = job_of<NQT>(p, blockIdx.x, by, blockIdx.z, status);
   if (x.q0 < 0) return;
-  const int in_tile = r & 127, i = x.q0 + (r >> 7) * x.per + in_tile / x.heads;
+  const int in_tile = r & 127, ip = row_pos(x, in_tile), i = x.q0 + (r >> 7) * x.per + ip;
   if (in_tile >= x.per * x.heads || i >= x.n) return;
   constexpr int PER = HD / 32;
   float m = -INFINITY, l = 0.f, o[PER];
@@ -686,7 +735,7 @@ __global__ void __launch_bounds__(256) attn8_merge_kernel(const __grid_constant_
     m = n;
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;      // l 0: no piece was read, the sums are zeros
-  bf16* dst = p.out + ((int64_t)x.row0 + i) * p.ldo + (int64_t)(x.h0 + in_tile % x.heads) * HD + lane * 2;
+  bf16* dst = p.out + ((int64_t)x.row0 + i) * p.ldo + (int64_t)(x.h0 + in_tile - ip * x.heads) * HD + lane * 2;
 #pragma unroll
   for (int k = 0; k < PER; k += 2)
     *reinterpret_cast<__nv_bfloat162*>(dst + k * 32) = __floats2bfloat162_rn(o[k] * inv, o[k + 1] * inv);
@@ -697,7 +746,7 @@ int launch_t(const Attn8Args& a, A8Dev& p, cudaStream_t s) {
   using C = A8<HD, NQT>;
   const size_t smem = sizeof(A8Smem<HD, NQT>) + 1024;
   static_assert(sizeof(A8Smem<HD, NQT>) + 1024 <= kSmemLimit, "shared memory budget");
-  const int per = 128 / (p.G < 128 ? p.G : 128);
+  const int per = p.per;
   const int64_t q_tiles = ((int64_t)a.rows + NQT * per - 1) / (NQT * per);
   if (q_tiles > 65535) return POP_E_INVALID;
   p.q_tiles = (int)q_tiles;
@@ -762,6 +811,8 @@ int launch_attention8(const Attn8Args& a, cudaStream_t s) {
   p.seq_lens = a.seq_lens; p.kv_len = a.kv_len;
   p.out = a.out; p.ldo = a.ldo;
   p.n_q = a.n_q; p.n_kv = a.n_kv; p.G = a.n_q / a.n_kv; p.hg = (p.G + 127) / 128;
+  p.per = 128 / (p.G < 128 ? p.G : 128);
+  p.inv = (65536 + p.G - 1) / p.G;
   p.window = a.window;
   p.partial = static_cast<float*>(a.workspace);
   p.scale_log2 = 1.4426950408889634f / sqrtf((float)a.head_dim);
