@@ -30,6 +30,7 @@ namespace pop {
 namespace {
 
 constexpr int kSmemLimit = 227 * 1024;
+constexpr int FEW_COLUMNS = 32;       // up to this many (row, head) pairs of a kv head go to decode8.cu
 constexpr float W_SHIFT = 7.f;        // weights are stored times 2^7; the lazy maximum lets them reach 2^15
 
 template <int HD, int NQT>
@@ -802,6 +803,8 @@ int launch_attention8(const Attn8Args& a, cudaStream_t s) {
   if (a.c.num_pages * (int64_t)a.n_kv > 0x7ffffff0 / a.c.page_size) return POP_E_INVALID;
   if ((int64_t)a.kv_len > (int64_t)a.c.max_pages * a.c.page_size) return POP_E_NOSPACE;
   if (a.rows == 0) return POP_OK;
+  // few (row, head) columns per kv head: the kernel that streams the cache
+  if ((int64_t)a.rows * (a.n_q / a.n_kv) <= FEW_COLUMNS && a.batch <= 4096) return launch_few8(a, s);
   A8Dev p{};
   p.q = a.q; p.ldq = a.ldq;
   p.c = a.c;

@@ -90,6 +90,7 @@ struct Attn8Args {
 };
 int launch_decode_attention8(const Attn8Args& a, cudaStream_t s);
 int launch_attention8(const Attn8Args& a, cudaStream_t s);
+int launch_few8(const Attn8Args& a, cudaStream_t s);           // few rows; arguments checked by the two above
 int device_sms();                                              // SMs of the device that was current at the first call
 
 }  // namespace pop

@@ -83,6 +83,26 @@ inline cudaError_t launch_chained_cluster(void (*kernel)(P...), dim3 grid, dim3 
   cfg.numAttrs = chained_launch_enabled() ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
 }
+// The same with thread-block clusters of (cluster_x, 1, 1) CTAs.
+template <typename... P, typename... A>
+inline cudaError_t launch_chained_cluster_x(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
+                                            unsigned cluster_x, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster_x;
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = chained_launch_enabled() ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
 #endif
 
 // Tensor-map encoding through the driver entry point (no link-time dependency on libcuda).

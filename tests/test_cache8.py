@@ -71,7 +71,7 @@ REFUSED = {
                        dict(positions=A), dict(pair_axis=A), dict(positions=A, pair_axis=A, n_axes=300), dict(n_q=-1),
                        dict(batch=70000), dict(batch=60000, max_rows=60000)],
     "decode": CACHE + [dict(q=None), dict(out=None), dict(q=A + 8), dict(out=A + 2), dict(ldq=65), dict(ldo=68),
-                       dict(n_q=3, n_kv=2), dict(n_q=0), dict(kv_len=-1), dict(window=-1), dict(batch=8193),
+                       dict(n_q=3, n_kv=2), dict(n_q=0), dict(kv_len=-1), dict(window=-1), dict(batch=4097),
                        dict(workspace=A + 4)],
     "prompt": CACHE + [dict(q=None), dict(out=None), dict(q=A + 8), dict(out=A + 2), dict(ldq=65), dict(ldo=68),
                        dict(n_q=3, n_kv=2), dict(n_q=0), dict(kv_len=-1), dict(window=-1), dict(max_rows=-1),
@@ -80,8 +80,11 @@ REFUSED = {
 NOSPACE = {
     "quant": [dict(max_len=65), dict(max_len=65, max_pages=5)],
     "append": [dict(pos0=64), dict(pos0=60, max_rows=5)],
-    "decode": [dict(kv_len=6401), dict(kv_len=6400, workspace_bytes=1000), dict(kv_len=6400, workspace=None)],
-    "prompt": [dict(kv_len=6401), dict(kv_len=6400, workspace_bytes=1000), dict(kv_len=6400, workspace=None)],
+    "decode": [dict(kv_len=6401), dict(kv_len=64000, max_pages=4000, workspace_bytes=1000),
+               dict(kv_len=64000, max_pages=4000, workspace=None)],
+    "prompt": [dict(kv_len=6401), dict(kv_len=64000, max_pages=4000, workspace_bytes=1000),
+               dict(kv_len=64000, max_pages=4000, workspace=None), dict(kv_len=6400, max_rows=64, workspace_bytes=1000),
+               dict(kv_len=6400, max_rows=64, workspace=None)],
 }
 CALLS = {"quant": ("pop_k_quant_cache_e4m3", QUANT), "append": ("pop_k_rope_cache_e4m3", APPEND),
          "decode": ("pop_k_decode_attention_e4m3", DECODE), "prompt": ("pop_k_attention_e4m3", PROMPT)}
