@@ -22,8 +22,8 @@
 //   - few items (a small batch): a thread-block cluster of 1, 2, 4 or 8 CTAs per item, its blocks dealt to the warps in
 //     equal stretches, the pieces merged in shared memory and over the cluster's. One launch.
 //   - else all items form one line of blocks and every warp of a full GPU takes an equal stretch of it, whatever the
-//     lengths are. An item that a warp has whole is finished by it; pieces of one CTA are merged in shared memory, items
-//     that cross CTAs through the workspace by a second, chained launch.
+//     lengths are. An item that a warp has whole is finished by it; the pieces of the others go through the workspace to a
+//     second, chained launch (a CTA that lies inside one item merges its eight in shared memory first).
 #include "cache8.cuh"
 #include "ptx.cuh"
 
@@ -44,17 +44,18 @@ struct D8 {
   static constexpr int VW = HD / 32;           // words of a value row per lane
   static constexpr int CH = HD / 16;           // 16-byte pieces of a row
   static constexpr int TILE = C8_BLOCK * HD;   // bytes of a block's keys; its values behind them
-  static constexpr int PER_SM = CG > 1 ? 1 : (HD == 64 ? 3 : (HD == 128 ? 2 : 1));
-  static constexpr int NST = CG > 1 ? 3 : (HD == 64 ? 3 : 2);   // blocks in flight per warp: 96 KB and more per SM
+  // Blocks of one turn of the loop (their MMAs, exponentials and shuffles overlap, one maximum for all of them), and turns
+  // in flight per warp: 192 KB per SM, two thirds of it always under way
+  static constexpr int BPI = HD == 256 ? 1 : 2;
+  static constexpr int NST = 3;
+  static constexpr int STAGE = BPI * 2 * TILE;
+  static constexpr int PER_SM = HD == 64 ? 2 : 1;
   static constexpr int HS = HD + 4;            // floats per column of a piece in shared memory: rows 4 banks apart
   static constexpr int SLOT = NC * HS + 2 * NC;         // m, l, then the sums
   static constexpr int PSLOT = NC * HD + 2 * NC;        // floats of a piece in the workspace
-  // a warp's memory: ring, the piece it begins with (the one it ends with goes over the idle ring), queries if CG > 1
-  static constexpr int RING = NST * 2 * TILE;
-  static constexpr int QB = CG > 1 ? CG * KC * 2 * 512 : 0;
-  static constexpr int WARP_BYTES = RING + SLOT * 4 + QB;
-  static constexpr int SMEM = WARPS * WARP_BYTES + SLOT * 4;    // and the CTA's merged piece, for its cluster
-  static_assert(SLOT * 4 <= RING, "the last piece goes over the ring");
+  static constexpr int RING = NST * STAGE;              // of a warp; a piece for the CTA's merge goes over the idle ring
+  static constexpr int SMEM = WARPS * RING + SLOT * 4;  // and the CTA's merged piece, for its cluster
+  static_assert(SLOT * 4 <= RING, "a piece goes over the ring");
 };
 
 // Where 16-byte piece ch of row r of a block lies in its stage: permuted so that the eight lanes that read together (two
@@ -79,7 +80,7 @@ struct Dec8Dev {
   int batch, n_q, n_kv, G;
   int chunks;                        // column groups of a sequence with `rows` rows
   int cluster;                       // CTAs per item; 0: the line
-  float* partial;                    // [CTAs][2][PSLOT]
+  float* partial;                    // [warps][2][PSLOT]: the piece a warp begins with, and the one it ends with
   int* status;
   float scale_log2;
 };
@@ -148,23 +149,32 @@ __device__ __forceinline__ Seq seq_of(const Dec8Dev& p, int b) {
   return s;
 }
 
-// prefix[b] = blocks of all items of the sequences before b, for b <= batch. By all threads.
+// Blocks of all items of the sequences before b. Up to 32 sequences: lane b of every warp knows its own, no shared memory;
+// more: prefix[b] in shared memory, by all threads.
+struct Prefix { int mine, total; const int* all; };
 template <int NC>
-__device__ __forceinline__ void scan_blocks(const Dec8Dev& p, int* prefix, int* warp_sums) {
-  const int per = (p.batch + blockDim.x - 1) / blockDim.x;
-  const int b0 = min(p.batch, (int)threadIdx.x * per), b1 = min(p.batch, b0 + per);
+__device__ __forceinline__ Prefix scan_blocks(const Dec8Dev& p, int* prefix, int* warp_sums) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   auto units = [&](int b) {
     const Seq s = seq_of<NC>(p, b);
     return s.n * s.chunks * p.n_kv;
   };
+  Prefix x{0, 0, prefix};
+  const bool small = p.batch <= 32;
+  const int per = small ? 1 : (p.batch + blockDim.x - 1) / blockDim.x;
+  const int b0 = min(p.batch, (small ? lane : (int)threadIdx.x) * per), b1 = min(p.batch, b0 + per);
   int sum = 0;
   for (int b = b0; b < b1; ++b) sum += units(b);
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   int incl = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     const int t = __shfl_up_sync(FULL, incl, o);
     if (lane >= o) incl += t;
+  }
+  if (small) {
+    x.mine = incl - sum;
+    x.total = __shfl_sync(FULL, incl, 31);
+    return x;
   }
   if (lane == 31) warp_sums[warp] = incl;
   __syncthreads();
@@ -172,10 +182,12 @@ __device__ __forceinline__ void scan_blocks(const Dec8Dev& p, int* prefix, int* 
   for (int w = 0; w < warp; ++w) run += warp_sums[w];
   for (int b = b0; b < b1; ++b) {
     prefix[b] = run;
-    run += b + 1 == b1 && per == 1 ? sum : units(b);
+    run += per == 1 ? sum : units(b);
   }
   if (b1 == p.batch && b0 < p.batch) prefix[p.batch] = run;
   __syncthreads();
+  x.total = prefix[p.batch];
+  return x;
 }
 // The line of all blocks, cut into W stretches that differ by at most one block (everything below 2^31: the host checks)
 struct Line {
@@ -194,17 +206,25 @@ struct Line {
 // Where unit u (< total) of the line lies: sequence, item of the sequence (kv head, column group), block of the item
 struct Place { int b, kvh, chunk, blk; Seq s; };
 template <int NC>
-__device__ __forceinline__ Place locate(const Dec8Dev& p, const int* prefix, int u) {
+__device__ __forceinline__ Place locate(const Dec8Dev& p, const Prefix& pre, int u) {      // by whole warps
   Place x;
-  int lo = 0, hi = p.batch - 1;                 // the last b with prefix[b] <= u: it is not empty
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (prefix[mid] <= u) lo = mid;
-    else hi = mid - 1;
+  int before;                                   // of the last b with prefix[b] <= u: it is not empty
+  if (p.batch <= 32) {
+    const int lane = threadIdx.x & 31;
+    x.b = 31 - __clz(__ballot_sync(FULL, lane < p.batch && pre.mine <= u));
+    before = __shfl_sync(FULL, pre.mine, x.b);
+  } else {
+    int lo = 0, hi = p.batch - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (pre.all[mid] <= u) lo = mid;
+      else hi = mid - 1;
+    }
+    x.b = lo;
+    before = pre.all[lo];
   }
-  x.b = lo;
-  x.s = seq_of<NC>(p, lo);
-  const int off = u - prefix[lo], item = off / x.s.n;
+  x.s = seq_of<NC>(p, x.b);
+  const int off = u - before, item = off / x.s.n;
   x.blk = off - item * x.s.n;
   x.kvh = item / x.s.chunks;
   x.chunk = item - x.kvh * x.s.chunks;
@@ -214,17 +234,13 @@ __device__ __forceinline__ Place locate(const Dec8Dev& p, const int* prefix, int
 template <int HD, int CG>
 __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(const __grid_constant__ Dec8Dev p) {
   using C = D8<HD, CG>;
-  constexpr int NC = C::NC, NT = C::NT, KC = C::KC, VW = C::VW, CH = C::CH, HS = C::HS, NST = C::NST;
-  extern __shared__ __align__(128) uint8_t smem[];            // WARP_BYTES of every warp, SLOT floats, the prefix sums
+  constexpr int NC = C::NC, NT = C::NT, KC = C::KC, VW = C::VW, CH = C::CH, HS = C::HS, NST = C::NST, BPI = C::BPI;
+  extern __shared__ __align__(128) uint8_t smem[];            // RING bytes of every warp, SLOT floats, the prefix sums
   __shared__ int warp_sums[WARPS];
-  __shared__ int hdr_item[2 * WARPS], hdr_flags[2 * WARPS], hdr_b[2 * WARPS];   // flags: 1 the item's first block, 2 its last
-  float* const xchg = reinterpret_cast<float*>(smem + WARPS * C::WARP_BYTES);
+  float* const xchg = reinterpret_cast<float*>(smem + WARPS * C::RING);
   int* const prefix = reinterpret_cast<int*>(xchg + C::SLOT);
-  auto slot_of = [&](int i) {        // slot 2 w: the piece that warp w began with, 2 w + 1: the one it ended with
-    return reinterpret_cast<float*>(smem + (i >> 1) * C::WARP_BYTES + ((i & 1) ? 0 : C::RING));
-  };
+  auto slot_of = [&](int w) { return reinterpret_cast<float*>(smem + w * C::RING); };     // the piece of warp w
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  if (threadIdx.x < 2 * WARPS) hdr_item[threadIdx.x] = -1;
   chain_wait();
   chain_trigger();                   // after the wait: the merge reads the lengths before its own
 
@@ -232,6 +248,8 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
   Place x;
   int left;                          // blocks of the stretch that are still to do
   int u = 0;                         // line form: the unit that x is at
+  bool inside = false;               // line form: the CTA's stretch lies inside one item
+  Prefix pre{};
   if (p.cluster) {
     const int item = blockIdx.x / p.cluster, rank = blockIdx.x - item * p.cluster;
     const int per_seq = p.n_kv * p.chunks;
@@ -243,14 +261,17 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
     const int w = rank * WARPS + warp, W = p.cluster * WARPS;
     x.blk = (int)((int64_t)x.s.n * w / W);
     left = x.chunk < x.s.chunks ? (int)((int64_t)x.s.n * (w + 1) / W) - x.blk : 0;
-    __syncthreads();                 // the headers are empty
   } else {
-    scan_blocks<NC>(p, prefix, warp_sums);
-    const Line line(prefix[p.batch], gridDim.x * WARPS);
+    pre = scan_blocks<NC>(p, prefix, warp_sums);
+    const Line line(pre.total, gridDim.x * WARPS);
     const int w = blockIdx.x * WARPS + warp;
     u = line.begin(w);
     left = line.begin(w + 1) - u;
-    if (left > 0) x = locate<NC>(p, prefix, u);
+    if (left > 0) x = locate<NC>(p, pre, u);
+    if (left > 0) {                  // the same for all warps: an item that goes on behind the CTA leaves none without a block
+      const int c0 = line.begin(blockIdx.x * WARPS), c1 = line.begin((blockIdx.x + 1) * WARPS), first = u - x.blk;
+      inside = first < c0 && first + x.s.n > c1;
+    }
   }
   // rows of sequences without a position: zeros
   for (int b = blockIdx.x; b < p.batch; b += gridDim.x) {
@@ -261,15 +282,32 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
           p.out[(int64_t)(s.row0 + r) * p.ldo + e] = __float2bfloat16_rn(0.f);
   }
 
-  uint8_t* const ring = smem + warp * C::WARP_BYTES;
+  uint8_t* const ring = smem + warp * C::RING;
   const uint32_t ring_addr = (uint32_t)__cvta_generic_to_shared(ring);
-  uint4* const q_sm = reinterpret_cast<uint4*>(ring + C::RING + C::SLOT * 4);      // CG > 1: [CG][KC][code][lane]
   const int ps = p.c.page_size;
 
+  int stored = 0;                      // a piece of this warp is in shared memory
   while (left > 0) {
     const int n_blk = min(x.s.n - x.blk, left);
     const int col0 = x.chunk * NC, cols = min(NC, x.s.rows * p.G - col0), h0 = x.kvh * p.G;
     const int32_t* bt = p.c.table + (int64_t)x.b * p.c.max_pages;
+
+    // the query rows' loads go out first: of column group cg a lane takes column g at dims 64 c + 16 t .. + 15
+    uint4 raw[CG][KC][2];
+    int row_of_col[CG];
+#pragma unroll
+    for (int cg = 0; cg < CG; ++cg) {
+      const int col = col0 + cg * 8 + g;
+      const bool live = cg * 8 + g < cols;
+      const int i = live ? col / p.G : 0, h = live ? col - i * p.G : 0;
+      row_of_col[cg] = i;
+      const bf16* qrow = p.q + (int64_t)(x.s.row0 + i) * p.ldq + (int64_t)(h0 + h) * HD + 16 * t;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        raw[cg][c][0] = *reinterpret_cast<const uint4*>(qrow + 64 * c);
+        raw[cg][c][1] = *reinterpret_cast<const uint4*>(qrow + 64 * c + 8);
+      }
+    }
 
     // Places and scales of 32 blocks at a time, one per lane: block number in the pool (-1, read as zeros, for a table
     // entry that is no page of it) and both scale bytes
@@ -289,51 +327,46 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
     int base = 0, id_c, sc_c, id_n = -1, sc_n = 0;     // the 32 blocks from `base` on, and the 32 behind them
     fetch(0, id_c, sc_c);
     if (n_blk > 32) fetch(32, id_n, sc_n);
-    auto issue = [&](int i, int stage) {
-      const int k = i - base, id = __shfl_sync(FULL, k < 32 ? id_c : id_n, k & 31);
-      const int64_t off = id < 0 ? 0 : (int64_t)id * C::TILE;
-      const int bytes = id < 0 ? 0 : 16;
-      const uint32_t dst = ring_addr + stage * 2 * C::TILE;
+    auto issue = [&](int i, int stage) {               // blocks i .. i + BPI - 1; one that is not there reads as zeros
 #pragma unroll
-      for (int c = 0; c < C::TILE / 512; ++c) {
-        const int e = c * 32 + lane;
-        const uint32_t at = dst + swz<HD>(e / CH, e % CH);
-        cp_async16(at, p.c.k + off + e * 16, bytes);
-        cp_async16(at + C::TILE, p.c.v + off + e * 16, bytes);
+      for (int u2 = 0; u2 < BPI; ++u2) {
+        const int k = i + u2 - base, id = __shfl_sync(FULL, k < 32 ? id_c : id_n, k & 31);
+        const int64_t off = id < 0 ? 0 : (int64_t)id * C::TILE;
+        const int bytes = id < 0 ? 0 : 16;
+        const uint32_t dst = ring_addr + stage * C::STAGE + u2 * 2 * C::TILE;
+        const uint8_t *ks = p.c.k + off + lane * 16, *vs = p.c.v + off + lane * 16;
+#pragma unroll
+        for (int c = 0; c < C::TILE / 512; ++c) {
+          const int e = c * 32 + lane;
+          const uint32_t at = dst + swz<HD>(e / CH, e % CH);
+          cp_async16(at, ks + c * 512, bytes);
+          cp_async16(at + C::TILE, vs + c * 512, bytes);
+        }
       }
     };
 #pragma unroll
     for (int i = 0; i < NST; ++i) {
-      if (i < n_blk) issue(i, i);
+      if (i * BPI < n_blk) issue(i * BPI, i);
       cp_async_commit();
     }
 
     // q^T as the B operand: of column group cg a lane holds column g at dims 64 c + 16 t + 4 w .. + 3, scaled so that the
     // column's largest element is in [2^7, 2^8), as two codes: the nearest one and the nearest one of what is left.
     // Per column of this lane's scores (2t and 2t + 1 of each group): factor and position.
-    uint32_t qh[CG == 1 ? KC : 1][4], ql[CG == 1 ? KC : 1][4];
+    uint32_t qh[CG][KC][4], ql[CG][KC][4];
     float c0[CG], c1[CG];
     int pos0[CG], pos1[CG];
 #pragma unroll
     for (int cg = 0; cg < CG; ++cg) {
-      const int col = col0 + cg * 8 + g;
       const bool live = cg * 8 + g < cols;
-      const int i = live ? col / p.G : 0, h = live ? col - i * p.G : 0;
-      const bf16* qrow = p.q + (int64_t)(x.s.row0 + i) * p.ldq + (int64_t)(h0 + h) * HD + 16 * t;
-      uint4 raw[KC][2];
       float am = 0.f;
-#pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        raw[c][0] = *reinterpret_cast<const uint4*>(qrow + 64 * c);
-        raw[c][1] = *reinterpret_cast<const uint4*>(qrow + 64 * c + 8);
-      }
       auto lo_f = [](uint32_t w) { return __uint_as_float(w << 16); };
       auto hi_f = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
 #pragma unroll
       for (int c = 0; c < KC; ++c)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const uint32_t w[4] = {raw[c][k].x, raw[c][k].y, raw[c][k].z, raw[c][k].w};
+          const uint32_t w[4] = {raw[cg][c][k].x, raw[cg][c][k].y, raw[cg][c][k].z, raw[cg][c][k].w};
 #pragma unroll
           for (int m = 0; m < 4; ++m) am = fmaxf(am, fmaxf(fabsf(lo_f(w[m])), fabsf(hi_f(w[m]))));
         }
@@ -343,32 +376,21 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
       const float mul = live ? c8_pow2(134 - eb) : 0.f, inv = c8_pow2(eb - 134) * p.scale_log2;
 #pragma unroll
       for (int c = 0; c < KC; ++c) {
-        uint32_t hi4[4], lo4[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-          const uint4& r = raw[c][k >> 1];
+          const uint4& r = raw[cg][c][k >> 1];
           const uint32_t w0 = (k & 1) ? r.z : r.x, w1 = (k & 1) ? r.w : r.y;
           const float e0 = lo_f(w0) * mul, e1 = hi_f(w0) * mul, e2 = lo_f(w1) * mul, e3 = hi_f(w1) * mul;
           const uint32_t hi = c8_codes4(e0, e1, e2, e3), f0 = c8_half2_lo(hi), f1 = c8_half2_hi(hi);
           const float2 r0 = __half22float2(*reinterpret_cast<const __half2*>(&f0));
           const float2 r1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
-          hi4[k] = hi;
-          lo4[k] = c8_codes4(e0 - r0.x, e1 - r0.y, e2 - r1.x, e3 - r1.y);
-        }
-        if constexpr (CG == 1) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            qh[c][k] = hi4[k];
-            ql[c][k] = lo4[k];
-          }
-        } else {                       // read back by the lane that wrote it
-          q_sm[((cg * KC + c) * 2 + 0) * 32 + lane] = make_uint4(hi4[0], hi4[1], hi4[2], hi4[3]);
-          q_sm[((cg * KC + c) * 2 + 1) * 32 + lane] = make_uint4(lo4[0], lo4[1], lo4[2], lo4[3]);
+          qh[cg][c][k] = hi;
+          ql[cg][c][k] = c8_codes4(e0 - r0.x, e1 - r0.y, e2 - r1.x, e3 - r1.y);
         }
       }
       c0[cg] = __shfl_sync(FULL, inv, t * 8);
       c1[cg] = __shfl_sync(FULL, inv, t * 8 + 4);
-      const int pos = x.s.len - x.s.rows + i;
+      const int pos = x.s.len - x.s.rows + row_of_col[cg];
       pos0[cg] = __shfl_sync(FULL, pos, t * 8);
       pos1[cg] = __shfl_sync(FULL, pos, t * 8 + 4);
     }
@@ -387,8 +409,8 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
     }
 
     int stage = 0;
-    for (int i = 0; i < n_blk; ++i) {
-      const int at = (x.s.first + x.blk + i) * C8_BLOCK;       // first position of the block
+    for (int i = 0; i < n_blk; i += BPI) {
+      const int at = (x.s.first + x.blk + i) * C8_BLOCK;       // first position of the first block
       cp_async_wait<NST - 1>();
       __syncwarp();
       if (i - base == 32) {
@@ -397,73 +419,65 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
         sc_c = sc_n;
         if (i + 32 < n_blk) fetch(i + 32, id_n, sc_n);
       }
-      const int sc = __shfl_sync(FULL, sc_c, i - base), ke = sc & 255, ve = sc >> 8;
-      const uint8_t* st = ring + stage * 2 * C::TILE;
-      float s[CG][4], sb[CG][4];       // of the two codes of q
+      const uint8_t* st = ring + stage * C::STAGE;
+      float s[BPI][CG][4];
 #pragma unroll
-      for (int cg = 0; cg < CG; ++cg)
+      for (int u2 = 0; u2 < BPI; ++u2) {
+        float sb[CG][4];               // s and sb: of the two codes of q
 #pragma unroll
-        for (int k = 0; k < 4; ++k) s[cg][k] = sb[cg][k] = 0.f;
+        for (int cg = 0; cg < CG; ++cg)
 #pragma unroll
-      for (int c = 0; c < KC; ++c) {                           // keys g and g + 8 at bytes 64 c + 16 t .. + 15
-        const uint4 ka = *reinterpret_cast<const uint4*>(st + swz<HD>(g, 4 * c + t));
-        const uint4 kb = *reinterpret_cast<const uint4*>(st + swz<HD>(g + 8, 4 * c + t));
+          for (int k = 0; k < 4; ++k) s[u2][cg][k] = sb[cg][k] = 0.f;
 #pragma unroll
-        for (int cg = 0; cg < CG; ++cg) {
-          uint32_t qa[4], qz[4];
-          if constexpr (CG == 1) {
+        for (int c = 0; c < KC; ++c) {                         // keys g and g + 8 at bytes 64 c + 16 t .. + 15
+          const uint4 ka = *reinterpret_cast<const uint4*>(st + u2 * 2 * C::TILE + swz<HD>(g, 4 * c + t));
+          const uint4 kb = *reinterpret_cast<const uint4*>(st + u2 * 2 * C::TILE + swz<HD>(g + 8, 4 * c + t));
 #pragma unroll
-            for (int k = 0; k < 4; ++k) { qa[k] = qh[c][k]; qz[k] = ql[c][k]; }
-          } else {
-            const uint4 a = q_sm[((cg * KC + c) * 2 + 0) * 32 + lane], z = q_sm[((cg * KC + c) * 2 + 1) * 32 + lane];
-            qa[0] = a.x; qa[1] = a.y; qa[2] = a.z; qa[3] = a.w;
-            qz[0] = z.x; qz[1] = z.y; qz[2] = z.z; qz[3] = z.w;
-          }
-          mma_e4m3(s[cg], ka.x, kb.x, ka.y, kb.y, qa[0], qa[1]);
-          mma_e4m3(sb[cg], ka.x, kb.x, ka.y, kb.y, qz[0], qz[1]);
-          mma_e4m3(s[cg], ka.z, kb.z, ka.w, kb.w, qa[2], qa[3]);
-          mma_e4m3(sb[cg], ka.z, kb.z, ka.w, kb.w, qz[2], qz[3]);
-        }
-      }
-      uint32_t vr[4][VW];              // values of keys 2t, 2t + 1, 2t + 8, 2t + 9
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int r = 2 * t + (k & 1) + (k >> 1) * 8;
-        if constexpr (HD == 64) {
-          const uint2 v = *reinterpret_cast<const uint2*>(st + C::TILE + swz<HD>(r, g >> 1) + (g & 1) * 8);
-          vr[k][0] = v.x; vr[k][1] = v.y;
-        } else {
-#pragma unroll
-          for (int c = 0; c < VW / 4; ++c) {
-            const uint4 v = *reinterpret_cast<const uint4*>(st + C::TILE + swz<HD>(r, 8 * c + g));
-            vr[k][4 * c] = v.x; vr[k][4 * c + 1] = v.y; vr[k][4 * c + 2] = v.z; vr[k][4 * c + 3] = v.w;
+          for (int cg = 0; cg < CG; ++cg) {
+            mma_e4m3(s[u2][cg], ka.x, kb.x, ka.y, kb.y, qh[cg][c][0], qh[cg][c][1]);
+            mma_e4m3(sb[cg], ka.x, kb.x, ka.y, kb.y, ql[cg][c][0], ql[cg][c][1]);
+            mma_e4m3(s[u2][cg], ka.z, kb.z, ka.w, kb.w, qh[cg][c][2], qh[cg][c][3]);
+            mma_e4m3(sb[cg], ka.z, kb.z, ka.w, kb.w, ql[cg][c][2], ql[cg][c][3]);
           }
         }
-      }
-      if (at + C8_BLOCK > x.s.len) {   // behind the sequence: no value whatever is there
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          if (at + 2 * t + (k & 1) + (k >> 1) * 8 >= x.s.len) {
+        for (int cg = 0; cg < CG; ++cg)
 #pragma unroll
-            for (int w = 0; w < VW; ++w) vr[k][w] = 0;
-          }
+          for (int k = 0; k < 4; ++k) s[u2][cg][k] += sb[cg][k];
       }
-      const float kf = c8_pow2(ke - 127), lv = (float)(ve - 127), inv_v = c8_pow2(127 - ve);
-      const bool edge = at + C8_BLOCK - 1 > full_hi || at < full_lo;
-      uint32_t pb0[CG], pb1[CG];
+      float kf[BPI], lv[BPI], inv_v[BPI];
+#pragma unroll
+      for (int u2 = 0; u2 < BPI; ++u2) {
+        const int sc = __shfl_sync(FULL, sc_c, i + u2 - base), ke = sc & 255, ve = sc >> 8;
+        kf[u2] = c8_pow2(ke - 127);
+        lv[u2] = (float)(ve - 127);
+        inv_v[u2] = c8_pow2(127 - ve);
+      }
+      const bool edge = at + BPI * C8_BLOCK - 1 > full_hi || at < full_lo || i + BPI > n_blk;
+      const int end = (x.s.first + x.blk + n_blk) * C8_BLOCK;  // of this stretch: the blocks behind it are not its own
+      uint32_t pb[CG][BPI][2];
 #pragma unroll
       for (int cg = 0; cg < CG; ++cg) {
-        const float k0 = c0[cg] * kf, k1 = c1[cg] * kf;
-        float s0 = fmaf(s[cg][0] + sb[cg][0], k0, lv), s1 = fmaf(s[cg][1] + sb[cg][1], k1, lv);
-        float s2 = fmaf(s[cg][2] + sb[cg][2], k0, lv), s3 = fmaf(s[cg][3] + sb[cg][3], k1, lv);
-        if (edge) {                    // keys that a column does not see: no weight whatever is there
-          const int a = at + g, w0 = p.window > 0 ? pos0[cg] - p.window : -1, w1 = p.window > 0 ? pos1[cg] - p.window : -1;
-          if (a > pos0[cg] || a <= w0) s0 = -INFINITY;
-          if (a > pos1[cg] || a <= w1) s1 = -INFINITY;
-          if (a + 8 > pos0[cg] || a + 8 <= w0) s2 = -INFINITY;
-          if (a + 8 > pos1[cg] || a + 8 <= w1) s3 = -INFINITY;
+        float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+        for (int u2 = 0; u2 < BPI; ++u2) {
+          float* v = s[u2][cg];
+          const float k0 = c0[cg] * kf[u2], k1 = c1[cg] * kf[u2];
+          v[0] = fmaf(v[0], k0, lv[u2]);
+          v[1] = fmaf(v[1], k1, lv[u2]);
+          v[2] = fmaf(v[2], k0, lv[u2]);
+          v[3] = fmaf(v[3], k1, lv[u2]);
+          if (edge) {                  // keys that a column does not see: no weight whatever is there
+            const int a = at + u2 * C8_BLOCK + g, h0c = min(pos0[cg], end - 1), h1c = min(pos1[cg], end - 1);
+            const int w0 = p.window > 0 ? pos0[cg] - p.window : -1, w1 = p.window > 0 ? pos1[cg] - p.window : -1;
+            if (a > h0c || a <= w0) v[0] = -INFINITY;
+            if (a > h1c || a <= w1) v[1] = -INFINITY;
+            if (a + 8 > h0c || a + 8 <= w0) v[2] = -INFINITY;
+            if (a + 8 > h1c || a + 8 <= w1) v[3] = -INFINITY;
+          }
+          x0 = fmaxf(x0, fmaxf(v[0], v[2]));
+          x1 = fmaxf(x1, fmaxf(v[1], v[3]));
         }
-        float x0 = fmaxf(s0, s2), x1 = fmaxf(s1, s3);
 #pragma unroll
         for (int w = 4; w < 32; w <<= 1) {
           x0 = fmaxf(x0, __shfl_xor_sync(FULL, x0, w));
@@ -474,34 +488,67 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
         const float b0 = n0 == -INFINITY ? 0.f : n0, b1 = n1 == -INFINITY ? 0.f : n1;
         const float f0 = ex2(m0[cg] - b0), f1 = ex2(m1[cg] - b1);
         const float e0 = b0 - W_SHIFT, e1 = b1 - W_SHIFT;
-        const float p0 = ex2(s0 - e0), p1 = ex2(s1 - e1), p2 = ex2(s2 - e0), p3 = ex2(s3 - e1);
-        l0[cg] = fmaf(p0 + p2, inv_v, l0[cg] * f0);
-        l1[cg] = fmaf(p1 + p3, inv_v, l1[cg] * f1);
+        l0[cg] *= f0;
+        l1[cg] *= f1;
         m0[cg] = n0;
         m1[cg] = n1;
+#pragma unroll
+        for (int u2 = 0; u2 < BPI; ++u2) {
+          const float* v = s[u2][cg];
+          const float p0 = ex2(v[0] - e0), p1 = ex2(v[1] - e1), p2 = ex2(v[2] - e0), p3 = ex2(v[3] - e1);
+          l0[cg] = fmaf(p0 + p2, inv_v[u2], l0[cg]);
+          l1[cg] = fmaf(p1 + p3, inv_v[u2], l1[cg]);
+          pb[cg][u2][0] = movm_t(pack_half2(p0, p1));          // keys 0-7 of the block
+          pb[cg][u2][1] = movm_t(pack_half2(p2, p3));          // keys 8-15
+        }
         if (__any_sync(FULL, f0 != 1.f || f1 != 1.f)) {
 #pragma unroll
           for (int j = 0; j < NT; ++j) {
             o[cg][j][0] *= f0; o[cg][j][1] *= f1; o[cg][j][2] *= f0; o[cg][j][3] *= f1;
           }
         }
-        pb0[cg] = movm_t(pack_half2(p0, p1));        // keys 0-7 of the block
-        pb1[cg] = movm_t(pack_half2(p2, p3));        // keys 8-15
       }
 #pragma unroll
-      for (int w = 0; w < VW; ++w) {
-        const uint32_t a = __byte_perm(vr[0][w], vr[1][w], 0x5140), b = __byte_perm(vr[0][w], vr[1][w], 0x7362);
-        const uint32_t c = __byte_perm(vr[2][w], vr[3][w], 0x5140), d = __byte_perm(vr[2][w], vr[3][w], 0x7362);
-        const uint32_t a0 = c8_half2_lo(a), a1 = c8_half2_hi(a), a2 = c8_half2_lo(c), a3 = c8_half2_hi(c);
-        const uint32_t b0 = c8_half2_lo(b), b1 = c8_half2_hi(b), b2 = c8_half2_lo(d), b3 = c8_half2_hi(d);
+      for (int u2 = 0; u2 < BPI; ++u2) {
+        const uint8_t* sv = st + (u2 * 2 + 1) * C::TILE;
+        uint32_t vr[4][VW];            // values of keys 2t, 2t + 1, 2t + 8, 2t + 9
 #pragma unroll
-        for (int cg = 0; cg < CG; ++cg) {
-          mma_f16(o[cg][2 * w], a0, a1, a2, a3, pb0[cg], pb1[cg]);
-          mma_f16(o[cg][2 * w + 1], b0, b1, b2, b3, pb0[cg], pb1[cg]);
+        for (int k = 0; k < 4; ++k) {
+          const int r = 2 * t + (k & 1) + (k >> 1) * 8;
+          if constexpr (HD == 64) {
+            const uint2 v = *reinterpret_cast<const uint2*>(sv + swz<HD>(r, g >> 1) + (g & 1) * 8);
+            vr[k][0] = v.x; vr[k][1] = v.y;
+          } else {
+#pragma unroll
+            for (int c = 0; c < VW / 4; ++c) {
+              const uint4 v = *reinterpret_cast<const uint4*>(sv + swz<HD>(r, 8 * c + g));
+              vr[k][4 * c] = v.x; vr[k][4 * c + 1] = v.y; vr[k][4 * c + 2] = v.z; vr[k][4 * c + 3] = v.w;
+            }
+          }
+        }
+        if (at + (u2 + 1) * C8_BLOCK > x.s.len) {              // behind the sequence: no value whatever is there
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (at + u2 * C8_BLOCK + 2 * t + (k & 1) + (k >> 1) * 8 >= x.s.len) {
+#pragma unroll
+              for (int w = 0; w < VW; ++w) vr[k][w] = 0;
+            }
+        }
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+          const uint32_t a = __byte_perm(vr[0][w], vr[1][w], 0x5140), b = __byte_perm(vr[0][w], vr[1][w], 0x7362);
+          const uint32_t c = __byte_perm(vr[2][w], vr[3][w], 0x5140), d = __byte_perm(vr[2][w], vr[3][w], 0x7362);
+          const uint32_t a0 = c8_half2_lo(a), a1 = c8_half2_hi(a), a2 = c8_half2_lo(c), a3 = c8_half2_hi(c);
+          const uint32_t b0 = c8_half2_lo(b), b1 = c8_half2_hi(b), b2 = c8_half2_lo(d), b3 = c8_half2_hi(d);
+#pragma unroll
+          for (int cg = 0; cg < CG; ++cg) {
+            mma_f16(o[cg][2 * w], a0, a1, a2, a3, pb[cg][u2][0], pb[cg][u2][1]);
+            mma_f16(o[cg][2 * w + 1], b0, b1, b2, b3, pb[cg][u2][0], pb[cg][u2][1]);
+          }
         }
       }
       __syncwarp();                    // every lane is done with the stage
-      if (i + NST < n_blk) issue(i + NST, stage);
+      if (i + NST * BPI < n_blk) issue(i + NST * BPI, stage);
       cp_async_commit();
       stage = stage + 1 == NST ? 0 : stage + 1;
     }
@@ -515,7 +562,7 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
       }
     // lane (g, t) holds columns 2t ([0], [2]) and 2t + 1 ([1], [3]) at dims dim_of(j, g) and the one behind it
     const bool starts = x.blk == 0, ends = x.blk + n_blk == x.s.n;
-    if (starts && ends && p.cluster <= 1) {
+    if (starts && ends && !p.cluster) {
 #pragma unroll
       for (int cg = 0; cg < CG; ++cg)
 #pragma unroll
@@ -531,95 +578,75 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
                 __floats2bfloat162_rn(o[cg][j][hh] * inv, o[cg][j][2 + hh] * inv);
         }
     } else {
-      const int si = 2 * warp + (starts ? 1 : 0);
-      float* sl = slot_of(si);
-      __syncwarp();                    // slot 2 w + 1 goes over the ring, which every lane has left
-      if (lane == 0) {
-        hdr_item[si] = x.kvh * p.chunks + x.chunk;             // with the sequence: which item
-        hdr_b[si] = x.b;
-        hdr_flags[si] = (starts ? 1 : 0) | (ends ? 2 : 0);
-      }
+      // for the CTA's merge over the ring, which every lane has left; else to the workspace
+      const bool local = p.cluster || inside;
+      const int cs = local ? HS : HD;                          // floats per column
+      float* sl = local ? slot_of(warp)
+                        : p.partial + (((int64_t)blockIdx.x * WARPS + warp) * 2 + (starts ? 1 : 0)) * C::PSLOT;
+      stored = local;
+      __syncwarp();
 #pragma unroll
       for (int cg = 0; cg < CG; ++cg) {
         if (g == 0) {
           sl[cg * 8 + 2 * t] = m0[cg]; sl[cg * 8 + 2 * t + 1] = m1[cg];
           sl[NC + cg * 8 + 2 * t] = l0[cg]; sl[NC + cg * 8 + 2 * t + 1] = l1[cg];
         }
-        float* so = sl + 2 * NC + (cg * 8 + 2 * t) * HS + 2 * g;
+        float* so = sl + 2 * NC + (cg * 8 + 2 * t) * cs + 2 * g;
 #pragma unroll
         for (int j = 0; j < NT; ++j) {
           *reinterpret_cast<float2*>(so + 16 * j) = make_float2(o[cg][j][0], o[cg][j][2]);
-          *reinterpret_cast<float2*>(so + HS + 16 * j) = make_float2(o[cg][j][1], o[cg][j][3]);
+          *reinterpret_cast<float2*>(so + cs + 16 * j) = make_float2(o[cg][j][1], o[cg][j][3]);
         }
       }
     }
     left -= n_blk;
     if (left > 0) {                    // the line goes on with the next item
       u += n_blk;
-      x = locate<NC>(p, prefix, u);
+      x = locate<NC>(p, pre, u);
     }
   }
-  __syncthreads();
-
-  // Pieces in the order of the line: slots 2 w and 2 w + 1 of warp w; lane k < 16 knows slot k. Those of one item are merged
-  // by tasks of one column and 32 pairs of dims.
-  const int my_item = lane < 2 * WARPS ? hdr_item[lane] : -1, my_b = my_item >= 0 ? hdr_b[lane] : -1;
-  unsigned todo = __ballot_sync(FULL, my_item >= 0);
-  if (p.cluster > 1) {
-    if (todo == 0)                     // fewer blocks than CTAs: an empty piece
-      for (int e = threadIdx.x; e < NC; e += blockDim.x) {
-        xchg[e] = -INFINITY;
-        xchg[NC + e] = 0.f;
-      }
+  if (!p.cluster && !inside) return;
+  // The CTA's pieces of its one item, by tasks of one column and 32 pairs of dims; lane k < 8 knows the piece of warp k. A
+  // warp without a block leaves an empty piece.
+  if (!stored) {
+    float* sl = slot_of(warp);
+    for (int e = lane; e < C::SLOT; e += 32) sl[e] = e < NC ? -INFINITY : 0.f;
   }
-  while (todo) {
-    const int first = __ffs(todo) - 1, it = __shfl_sync(FULL, my_item, first), b = __shfl_sync(FULL, my_b, first);
-    const unsigned mine = __ballot_sync(FULL, my_item == it && my_b == b);
-    todo &= ~mine;
-    const int last = 31 - __clz(mine);
-    const bool starts = hdr_flags[first] & 1, ends = hdr_flags[last] & 2;
-    const Seq s = seq_of<NC>(p, b);
-    const int kvh = it / p.chunks, col0 = (it - kvh * p.chunks) * NC, cols = min(NC, s.rows * p.G - col0);
-    constexpr int PARTS = HD / 64;     // tasks per column
-    for (int task = warp; task < cols * PARTS; task += WARPS) {
-      const int k = task / PARTS, pr = (task - k * PARTS) * 32 + lane;     // pair pr: dims dim_of(pr / 8, pr % 8) and the next
-      const bool has = (mine >> lane) & 1;
-      const float mk = has ? slot_of(lane)[k] : -INFINITY;
-      float m = mk;
+  __syncthreads();
+  const bool has = lane < WARPS;
+  const int col0 = x.chunk * NC, cols = x.s.len == 0 ? 0 : min(NC, x.s.rows * p.G - col0);
+  constexpr int PARTS = HD / 64;       // tasks per column
+  for (int task = warp; task < cols * PARTS; task += WARPS) {
+    const int k = task / PARTS, pr = (task - k * PARTS) * 32 + lane;       // pair pr: dims dim_of(pr / 8, pr % 8) and the next
+    const float mk = has ? slot_of(lane)[k] : -INFINITY;
+    float m = mk;
 #pragma unroll
-      for (int w = 8; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, w));
-      m = __shfl_sync(FULL, m, 0);     // lanes 16 .. 31 hold no slot
-      const float f = mk == -INFINITY ? 0.f : ex2(mk - m);
-      float l = has ? slot_of(lane)[NC + k] * f : 0.f;
+    for (int w = 4; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(FULL, m, w));
+    m = __shfl_sync(FULL, m, 0);       // lanes 8 .. 31 hold no piece
+    const float f = mk == -INFINITY ? 0.f : ex2(mk - m);
+    float l = has ? slot_of(lane)[NC + k] * f : 0.f;
 #pragma unroll
-      for (int w = 8; w > 0; w >>= 1) l += __shfl_xor_sync(FULL, l, w);
-      l = __shfl_sync(FULL, l, 0);
-      float2 v = make_float2(0.f, 0.f);
-      for (unsigned rem = mine; rem; rem &= rem - 1) {
-        const int sl = __ffs(rem) - 1;
-        const float fk = __shfl_sync(FULL, f, sl);
-        const float2 ov = *reinterpret_cast<const float2*>(slot_of(sl) + 2 * NC + k * HS + 2 * pr);
-        v.x = fmaf(ov.x, fk, v.x);
-        v.y = fmaf(ov.y, fk, v.y);
-      }
-      if (p.cluster > 1) {
-        *reinterpret_cast<float2*>(xchg + 2 * NC + k * HS + 2 * pr) = v;
-        if (pr == 0) {
-          xchg[k] = m;
-          xchg[NC + k] = l;
-        }
-      } else if (starts && ends) {
-        const int i = (col0 + k) / p.G, h = col0 + k - i * p.G;
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        bf16* dst = p.out + (int64_t)(s.row0 + i) * p.ldo + (int64_t)(kvh * p.G + h) * HD + dim_of<HD>(pr >> 3, pr & 7);
-        *reinterpret_cast<__nv_bfloat162*>(dst) = __floats2bfloat162_rn(v.x * inv, v.y * inv);
-      } else {                         // 1: the item starts in this CTA and goes on; 0: it came from an earlier one
-        float* dst = p.partial + ((int64_t)blockIdx.x * 2 + (starts ? 1 : 0)) * C::PSLOT;
-        *reinterpret_cast<float2*>(dst + 2 * NC + k * HD + 2 * pr) = v;
-        if (pr == 0) {
-          dst[k] = m;
-          dst[NC + k] = l;
-        }
+    for (int w = 4; w > 0; w >>= 1) l += __shfl_xor_sync(FULL, l, w);
+    l = __shfl_sync(FULL, l, 0);
+    float2 v = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+      const float fk = __shfl_sync(FULL, f, w);
+      const float2 ov = *reinterpret_cast<const float2*>(slot_of(w) + 2 * NC + k * HS + 2 * pr);
+      v.x = fmaf(ov.x, fk, v.x);
+      v.y = fmaf(ov.y, fk, v.y);
+    }
+    if (p.cluster == 1) {
+      const int i = (col0 + k) / p.G, h = col0 + k - i * p.G;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      bf16* dst = p.out + (int64_t)(x.s.row0 + i) * p.ldo + (int64_t)(x.kvh * p.G + h) * HD + dim_of<HD>(pr >> 3, pr & 7);
+      *reinterpret_cast<__nv_bfloat162*>(dst) = __floats2bfloat162_rn(v.x * inv, v.y * inv);
+    } else {                           // for the cluster; or as the piece of the CTA's first warp
+      float* dst = p.cluster ? xchg : p.partial + (int64_t)blockIdx.x * WARPS * 2 * C::PSLOT;
+      *reinterpret_cast<float2*>(dst + 2 * NC + k * (p.cluster ? HS : HD) + 2 * pr) = v;
+      if (pr == 0) {
+        dst[k] = m;
+        dst[NC + k] = l;
       }
     }
   }
@@ -628,10 +655,6 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
     cluster_arrive();
     cluster_wait();
     const int rank = (int)cluster_ctarank();
-    const int item = blockIdx.x / p.cluster, per_seq = p.n_kv * p.chunks;
-    const int b = item / per_seq, in = item - b * per_seq, kvh = in / p.chunks;
-    const Seq s = seq_of<NC>(p, b);
-    const int col0 = (in - kvh * p.chunks) * NC, cols = s.len == 0 ? 0 : min(NC, s.rows * p.G - col0);
     const uint32_t xa = smem_u32(xchg);
     for (int e = rank * WARPS * 32 + threadIdx.x; e < cols * (HD / 2); e += p.cluster * WARPS * 32) {
       const int k = e / (HD / 2), pr = e - k * (HD / 2);
@@ -653,15 +676,15 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
       for (int r = 0; r < 8; ++r) m = fmaxf(m, mr[r]);
 #pragma unroll
       for (int r = 0; r < 8; ++r)
-        if (mr[r] != -INFINITY) {                    // an empty piece's sums may not be written
-          const float f = ex2(mr[r] - m);
+        {
+          const float f = mr[r] == -INFINITY ? 0.f : ex2(mr[r] - m);
           l = fmaf(lr[r], f, l);
           ox = fmaf(vx[r], f, ox);
           oy = fmaf(vy[r], f, oy);
         }
       const int i = (col0 + k) / p.G, h = col0 + k - i * p.G;
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      bf16* dst = p.out + (int64_t)(s.row0 + i) * p.ldo + (int64_t)(kvh * p.G + h) * HD + dim_of<HD>(pr >> 3, pr & 7);
+      bf16* dst = p.out + (int64_t)(x.s.row0 + i) * p.ldo + (int64_t)(x.kvh * p.G + h) * HD + dim_of<HD>(pr >> 3, pr & 7);
       *reinterpret_cast<__nv_bfloat162*>(dst) = __floats2bfloat162_rn(ox * inv, oy * inv);
     }
     // nobody leaves while a neighbour may still read its shared memory
@@ -670,72 +693,85 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
   }
 }
 
-// Items that cross CTAs. The blocks of this grid are the CTAs of the attention kernel: those that hold pieces of an item
-// share its elements out among them, so that few long items are merged by many CTAs. Reads the same lengths, so it finds
-// the same places. Four neighbouring pairs of dims (a 32-byte sector) to four lanes, eight pieces at a time.
+// Items that several warps have pieces of. Block w of this grid is for the border between warps w - 1 and w: if it lies
+// inside an item, the blocks of all the borders inside it share its elements out. Reads the same lengths as the attention
+// kernel, so it finds the same places. With few pieces every lane takes a pair of dims; with many, four neighbouring pairs (a
+// 32-byte sector) go to four lanes, eight pieces at a time.
+constexpr int MERGE_WARPS = 4;
 template <int HD, int CG>
-__device__ __forceinline__ void merge_item(const Dec8Dev& p, const Line& line, const Place& x, int first) {
+__global__ void __launch_bounds__(MERGE_WARPS * 32) dec8_merge_kernel(const __grid_constant__ Dec8Dev p) {
   using C = D8<HD, CG>;
   constexpr int NC = C::NC;
-  const int c0 = line.owner(first) / WARPS, c1 = line.owner(first + x.s.n - 1) / WARPS;
-  const int col0 = x.chunk * NC, cols = min(NC, x.s.rows * p.G - col0);
-  const int lane = threadIdx.x & 31, pk = lane >> 2, pe = lane & 3;
-  const int workers = (c1 - c0 + 1) * WARPS;
-  for (int quad = (blockIdx.x - c0) * WARPS + (threadIdx.x >> 5); quad < cols * (HD / 8); quad += workers) {
-    const int k = quad / (HD / 8), pr = (quad - k * (HD / 8)) * 4 + pe;
-    float m = -INFINITY, l = 0.f;
-    float2 v = make_float2(0.f, 0.f);
-#pragma unroll 4
-    for (int c = c0 + pk; c <= c1; c += 8) {
-      const float* sl = p.partial + (2 * (int64_t)c + (c == c0 ? 1 : 0)) * C::PSLOT;
-      const float mk = __ldcg(sl + k), lk = __ldcg(sl + NC + k);
-      const float2 ov = __ldcg(reinterpret_cast<const float2*>(sl + 2 * NC + k * HD + 2 * pr));
-      if (mk == -INFINITY) continue;
-      const float n = fmaxf(m, mk), fa = ex2(m - n), fb = ex2(mk - n);
-      l = l * fa + lk * fb;
-      v.x = v.x * fa + ov.x * fb;
-      v.y = v.y * fa + ov.y * fb;
-      m = n;
-    }
-#pragma unroll
-    for (int w = 4; w < 32; w <<= 1) {
-      const float mk = __shfl_xor_sync(FULL, m, w), lk = __shfl_xor_sync(FULL, l, w);
-      const float ox = __shfl_xor_sync(FULL, v.x, w), oy = __shfl_xor_sync(FULL, v.y, w);
-      const float n = fmaxf(m, mk), fa = m == n ? 1.f : ex2(m - n), fb = mk == n ? 1.f : ex2(mk - n);   // both may be empty
-      l = l * fa + lk * fb;
-      v.x = v.x * fa + ox * fb;
-      v.y = v.y * fa + oy * fb;
-      m = n;
-    }
-    if (pk == 0) {
-      const int i = (col0 + k) / p.G, h = col0 + k - i * p.G;
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      bf16* dst = p.out + (int64_t)(x.s.row0 + i) * p.ldo + (int64_t)(x.kvh * p.G + h) * HD + dim_of<HD>(pr >> 3, pr & 7);
-      *reinterpret_cast<__nv_bfloat162*>(dst) = __floats2bfloat162_rn(v.x * inv, v.y * inv);
-    }
-  }
-}
-template <int HD, int CG>
-__global__ void __launch_bounds__(WARPS * 32) dec8_merge_kernel(const __grid_constant__ Dec8Dev p) {
-  constexpr int NC = D8<HD, CG>::NC;
   extern __shared__ __align__(16) int prefix[];
   __shared__ int warp_sums[WARPS];
   chain_trigger();
   // this kernel starts behind the attention kernel's wait, so the lengths are there; only the pieces have to be waited for
-  scan_blocks<NC>(p, prefix, warp_sums);
-  const Line line(prefix[p.batch], gridDim.x * WARPS);
-  const int u0 = line.begin(blockIdx.x * WARPS), u1 = line.begin((blockIdx.x + 1) * WARPS);
-  Place a{}, z{};
-  if (u0 < u1) {
-    a = locate<NC>(p, prefix, u0);
-    z = locate<NC>(p, prefix, u1 - 1);
-  }
+  const Prefix pre = scan_blocks<NC>(p, prefix, warp_sums);
+  const Line line(pre.total, gridDim.x);
+  const int w = blockIdx.x, u = line.begin(w);
+  Place x{};
+  if (u < line.T) x = locate<NC>(p, pre, u);
   chain_wait();
-  if (u0 >= u1) return;
-  // the item that came from an earlier CTA, and the one that goes on in the next (they may be the same)
-  if (a.blk > 0) merge_item<HD, CG>(p, line, a, u0 - a.blk);
-  const int first = u1 - 1 - z.blk;
-  if (z.blk + 1 < z.s.n && first >= u0) merge_item<HD, CG>(p, line, z, first);
+  if (u >= line.T || x.blk == 0) return;       // behind the line's end, or the border is one between items
+  const int first = u - x.blk, w0 = line.owner(first), w1 = line.owner(first + x.s.n - 1);
+  // pieces: of the warps of the first CTA, of the CTAs inside the item (one each), of the warps of the last CTA
+  const int q0 = w0 / WARPS, q1 = w1 / WARPS;
+  const int n0 = min(w1, q0 * WARPS + WARPS - 1) - w0 + 1, n1 = max(0, q1 - q0 - 1), n = n0 + n1 + (q1 > q0 ? w1 - q1 * WARPS + 1 : 0);
+  auto piece = [&](int i) {
+    const int pw = i < n0 ? w0 + i : i < n0 + n1 ? (q0 + 1 + i - n0) * WARPS : q1 * WARPS + i - n0 - n1;
+    return p.partial + ((int64_t)pw * 2 + (pw == w0 ? 1 : 0)) * C::PSLOT;
+  };
+  const int col0 = x.chunk * NC, cols = min(NC, x.s.rows * p.G - col0);
+  const int lane = threadIdx.x & 31;
+  const int rank = (w - w0 - 1) * MERGE_WARPS + (threadIdx.x >> 5), workers = (w1 - w0) * MERGE_WARPS;
+  float m = -INFINITY, l = 0.f;
+  float2 v = make_float2(0.f, 0.f);
+  auto add = [&](int i, int k, int pr) {
+    const float* sl = piece(i);
+    const float mk = __ldcg(sl + k), lk = __ldcg(sl + NC + k);
+    const float2 ov = __ldcg(reinterpret_cast<const float2*>(sl + 2 * NC + k * HD + 2 * pr));
+    const float mx = fmaxf(m, mk), z = mx == -INFINITY ? 0.f : mx, fa = ex2(m - z), fb = ex2(mk - z);
+    l = l * fa + lk * fb;
+    v.x = v.x * fa + ov.x * fb;
+    v.y = v.y * fa + ov.y * fb;
+    m = mx;
+  };
+  auto finish = [&](int k, int pr) {
+    const int i = (col0 + k) / p.G, h = col0 + k - i * p.G;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    bf16* dst = p.out + (int64_t)(x.s.row0 + i) * p.ldo + (int64_t)(x.kvh * p.G + h) * HD + dim_of<HD>(pr >> 3, pr & 7);
+    *reinterpret_cast<__nv_bfloat162*>(dst) = __floats2bfloat162_rn(v.x * inv, v.y * inv);
+  };
+  if (n <= 24) {
+    for (int task = rank; task < cols * (HD / 64); task += workers) {
+      const int k = task / (HD / 64), pr = (task - k * (HD / 64)) * 32 + lane;
+      m = -INFINITY;
+      l = v.x = v.y = 0.f;
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) add(i, k, pr);
+      finish(k, pr);
+    }
+    return;
+  }
+  const int pk = lane >> 2, pe = lane & 3;
+  for (int quad = rank; quad < cols * (HD / 8); quad += workers) {
+    const int k = quad / (HD / 8), pr = (quad - k * (HD / 8)) * 4 + pe;
+    m = -INFINITY;
+    l = v.x = v.y = 0.f;
+#pragma unroll 4
+    for (int i = pk; i < n; i += 8) add(i, k, pr);
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) {
+      const float mk = __shfl_xor_sync(FULL, m, d), lk = __shfl_xor_sync(FULL, l, d);
+      const float ox = __shfl_xor_sync(FULL, v.x, d), oy = __shfl_xor_sync(FULL, v.y, d);
+      const float mx = fmaxf(m, mk), z = mx == -INFINITY ? 0.f : mx, fa = ex2(m - z), fb = ex2(mk - z);
+      l = l * fa + lk * fb;
+      v.x = v.x * fa + ox * fb;
+      v.y = v.y * fa + oy * fb;
+      m = mx;
+    }
+    if (pk == 0) finish(k, pr);
+  }
 }
 
 template <int HD, int CG>
@@ -760,7 +796,7 @@ int launch_t(const Attn8Args& a, Dec8Dev& p, cudaStream_t s) {
     grid = ctas;
     const int64_t most = (blocks * items + WARPS - 1) / WARPS;    // no fewer than one block per warp
     if (grid > most) grid = most;
-    if ((size_t)grid * 2 * C::PSLOT * 4 > a.workspace_bytes) return POP_E_NOSPACE;
+    if ((size_t)grid * WARPS * 2 * C::PSLOT * 4 > a.workspace_bytes) return POP_E_NOSPACE;
   }
   p.status = status_word();
   if (!p.status) return POP_E_CUDA;
@@ -781,7 +817,7 @@ int launch_t(const Attn8Args& a, Dec8Dev& p, cudaStream_t s) {
   if (rc != cudaSuccess) return POP_E_CUDA;
   count_launch();
   if (!p.cluster) {
-    if (launch_chained(dec8_merge_kernel<HD, CG>, dim3((unsigned)grid), dim3(WARPS * 32), (size_t)scan_bytes, s, p) !=
+    if (launch_chained(dec8_merge_kernel<HD, CG>, dim3((unsigned)grid * WARPS), dim3(MERGE_WARPS * 32), (size_t)scan_bytes, s, p) !=
         cudaSuccess)
       return POP_E_CUDA;
     count_launch();
