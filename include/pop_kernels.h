@@ -220,7 +220,7 @@ int pop_k_quant_cache_e4m3(const void* k_pool, const void* v_pool, int64_t src_l
  * v to the cache.
  *   Rotation: pair (j, j + hd/2) turns by rope_table[p][j] = (cos, sin), float2 [table_rows][hd/2]. p is the cache position
  * if positions is NULL, else positions[axis * ld_pos + row] (device int32 [n_axes][ld_pos], row = packed row) with axis =
- * pair_axis[j] (device uint8 [hd/2], values < n_axes; NULL: axis 0): time, height and width of image and video tokens,
+ * pair_axis[j] (device uint8 [hd/2], 4-byte aligned, values < n_axes; NULL: axis 0): time, height and width of image and video tokens,
  * in sections or interleaved as the model has it.
  *   Scales: a block whose 16 positions all come from this call, or whose earlier positions are all new, gets the scale of its
  * rows. A block that holds earlier positions (start not a multiple of 16) keeps the larger of its scale and the one the new

@@ -50,7 +50,7 @@ struct Quant8Dev {
 };
 
 template <int HD>
-__global__ void __launch_bounds__(256) quant_cache8_kernel(const __grid_constant__ Quant8Dev p) {
+__global__ void __launch_bounds__(256, HD == 256 ? 2 : 4) quant_cache8_kernel(const __grid_constant__ Quant8Dev p) {
   constexpr int LPR = HD / 8, RPW = 32 / LPR, NP = C8_BLOCK / RPW;
   const Quant8Args& a = p.a;
   chain_trigger();
@@ -122,6 +122,7 @@ __global__ void __launch_bounds__(256) quant_cache8_kernel(const __grid_constant
 // rotary rows come from L1 after the first.
 struct Append8Dev {
   Append8Args a;
+  int head_groups;              // CTAs per block of positions: eight heads each
   int* status;
 };
 
@@ -130,25 +131,33 @@ __global__ void __launch_bounds__(256) append8_kernel(const __grid_constant__ Ap
   constexpr int LPR = HD / 8, RPW = 32 / LPR, NP = C8_BLOCK / RPW, HALF = HD / 2;
   const Append8Args& a = p.a;
   chain_trigger();
-  chain_wait();
   const int lane = threadIdx.x & 31, sub = lane / LPR, j0 = (lane % LPR) * 4;
   const int heads = a.n_q + 2 * a.n_kv;
-  const int head_groups = (heads + 7) / 8;
-  const int h = (int)(blockIdx.x % head_groups) * 8 + (threadIdx.x >> 5);
+  const int h = (int)(blockIdx.x % p.head_groups) * 8 + (threadIdx.x >> 5), blk = blockIdx.x / p.head_groups;
   const int b = blockIdx.y;
   if (h >= heads) return;
-  const int row0 = a.cu ? a.cu[b] : b * a.rows;
-  const int start = a.start ? a.start[b] : a.pos0;
-  int n = a.cu ? a.cu[b + 1] - row0 : a.rows;
-  const bool over = n > a.rows || start < 0 || start > 0x7ffffff0 - a.rows;
-  if (over && lane == 0) atomicMin(p.status, (int)POP_E_INVALID);
-  if (over || n <= 0) return;
-  const int first = start / C8_BLOCK * C8_BLOCK + (int)(blockIdx.x / head_groups) * C8_BLOCK;   // of this block
+  const bool is_q = h < a.n_q, is_v = h >= a.n_q + a.n_kv;
+  chain_wait();
+  const int row0 = a.cu ? __ldg(a.cu + b) : b * a.rows;
+  const int n = a.cu ? __ldg(a.cu + b + 1) - row0 : a.rows;
+  const int start = a.start ? __ldg(a.start + b) : a.pos0;
+  bool bad = n > a.rows || start < 0 || start > 0x7ffffff0 - a.rows;
+  if (bad || n <= 0) {
+    if (bad && lane == 0) atomicMin(p.status, (int)POP_E_INVALID);
+    return;
+  }
+  const int first = (start / C8_BLOCK + blk) * C8_BLOCK;                          // position of the block's slot 0
   if (first >= start + n) return;
   const int lo = max(start - first, 0), hi = min(start + n - first, C8_BLOCK);    // live slots of the block
-  const bool is_q = h < a.n_q, is_v = h >= a.n_q + a.n_kv;
   const int64_t r_base = (int64_t)row0 + first - start;                           // packed row of slot 0
 
+  // Everything that is read is asked for before anything is computed: the page, the rows, the positions, the old scale. What
+  // the checks find is raised once, at the end: a status write between loads would put them in order.
+  int page = -1;
+  if (!is_q) {
+    const int pi = first / a.dst.page_size;
+    if (pi < a.dst.max_pages) page = __ldg(a.dst.table + (int64_t)b * a.dst.max_pages + pi);
+  }
   float x[NP][8];               // [.. 0..3] elements j0 + i, [.. 4..7] their partners j0 + i + hd/2
 #pragma unroll
   for (int i = 0; i < NP; ++i) {
@@ -158,46 +167,48 @@ __global__ void __launch_bounds__(256) append8_kernel(const __grid_constant__ Ap
     if (s < lo || s >= hi) continue;
     const int64_t off = (r_base + s) * a.ld_in + (int64_t)h * HD + j0;
     if constexpr (IN_BF16) {
-      const uint2 l = *reinterpret_cast<const uint2*>(static_cast<const bf16*>(a.in) + off);
-      const uint2 m = *reinterpret_cast<const uint2*>(static_cast<const bf16*>(a.in) + off + HALF);
+      const uint2 l = __ldg(reinterpret_cast<const uint2*>(static_cast<const bf16*>(a.in) + off));
+      const uint2 m = __ldg(reinterpret_cast<const uint2*>(static_cast<const bf16*>(a.in) + off + HALF));
       unpack_bf16x2(l.x, x[i][0], x[i][1]);
       unpack_bf16x2(l.y, x[i][2], x[i][3]);
       unpack_bf16x2(m.x, x[i][4], x[i][5]);
       unpack_bf16x2(m.y, x[i][6], x[i][7]);
     } else {
-      const float4 l = *reinterpret_cast<const float4*>(static_cast<const float*>(a.in) + off);
-      const float4 m = *reinterpret_cast<const float4*>(static_cast<const float*>(a.in) + off + HALF);
+      const float4 l = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(a.in) + off));
+      const float4 m = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(a.in) + off + HALF));
       x[i][0] = l.x; x[i][1] = l.y; x[i][2] = l.z; x[i][3] = l.w;
       x[i][4] = m.x; x[i][5] = m.y; x[i][6] = m.z; x[i][7] = m.w;
     }
   }
-  float am = 0.f;
   if (!is_v) {
-    const float* gain = is_q ? a.q_gain : a.k_gain;
-    float g[8];
-    if (gain != nullptr) {
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        g[u] = gain[j0 + u];
-        g[u + 4] = gain[j0 + u + HALF];
-      }
-    }
     int axis[4] = {0, 0, 0, 0};
     if (a.pair_axis != nullptr) {
+      const uchar4 v = __ldg(reinterpret_cast<const uchar4*>(a.pair_axis + j0));
+      axis[0] = v.x; axis[1] = v.y; axis[2] = v.z; axis[3] = v.w;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        axis[u] = a.pair_axis[j0 + u];
-        if (axis[u] >= a.n_axes) {           // never turned into an address
-          atomicMin(p.status, (int)POP_E_INVALID);
+      for (int u = 0; u < 4; ++u)
+        if (axis[u] >= a.n_axes) {             // never turned into an address
+          bad = true;
           axis[u] = 0;
         }
-      }
     }
     const bool one_axis = axis[0] == axis[1] && axis[1] == axis[2] && axis[2] == axis[3];
-    auto angle_row = [&](int ax, int64_t r, int pos) {
-      int t = a.positions ? a.positions[(int64_t)ax * a.ld_pos + r] : pos;
+    int tp[NP];                                // table row of the lane's first pair
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int s = i * RPW + sub;
+      tp[i] = first + s;
+      if (a.positions != nullptr) tp[i] = s >= lo && s < hi ? __ldg(a.positions + axis[0] * a.ld_pos + r_base + s) : 0;
+    }
+    const float* gain = is_q ? a.q_gain : a.k_gain;
+    float4 g0 = make_float4(1.f, 1.f, 1.f, 1.f), g1 = g0;
+    if (gain != nullptr) {
+      g0 = make_float4(__ldg(gain + j0), __ldg(gain + j0 + 1), __ldg(gain + j0 + 2), __ldg(gain + j0 + 3));
+      g1 = make_float4(__ldg(gain + j0 + HALF), __ldg(gain + j0 + HALF + 1), __ldg(gain + j0 + HALF + 2), __ldg(gain + j0 + HALF + 3));
+    }
+    auto row_of = [&](int t) {
       if ((unsigned)t >= (unsigned)a.table_rows) {      // never turned into an address
-        atomicMin(p.status, (int)POP_E_INVALID);
+        bad = true;
         t = 0;
       }
       return a.table + (int64_t)t * HALF + j0;
@@ -206,6 +217,21 @@ __global__ void __launch_bounds__(256) append8_kernel(const __grid_constant__ Ap
     for (int i = 0; i < NP; ++i) {
       const int s = i * RPW + sub;
       const bool live = s >= lo && s < hi;
+      float2 cs[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) cs[u] = make_float2(1.f, 0.f);
+      if (live) {
+        if (one_axis) {
+          const float4* t = reinterpret_cast<const float4*>(row_of(tp[i]));
+          const float4 t0 = __ldg(t), t1 = __ldg(t + 1);
+          cs[0] = make_float2(t0.x, t0.y); cs[1] = make_float2(t0.z, t0.w);
+          cs[2] = make_float2(t1.x, t1.y); cs[3] = make_float2(t1.z, t1.w);
+        } else {
+          cs[0] = __ldg(row_of(tp[i]));
+#pragma unroll
+          for (int u = 1; u < 4; ++u) cs[u] = __ldg(row_of(__ldg(a.positions + axis[u] * a.ld_pos + r_base + s)) + u);
+        }
+      }
       if (gain != nullptr) {
         float ss = 0.f;
 #pragma unroll
@@ -213,27 +239,17 @@ __global__ void __launch_bounds__(256) append8_kernel(const __grid_constant__ Ap
 #pragma unroll
         for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(FULL, ss, o);
         const float rstd = rsqrtf(ss / (float)HD + a.eps);
-#pragma unroll
-        for (int u = 0; u < 8; ++u) x[i][u] = x[i][u] * rstd * g[u];
+        x[i][0] = x[i][0] * rstd * g0.x; x[i][1] = x[i][1] * rstd * g0.y;
+        x[i][2] = x[i][2] * rstd * g0.z; x[i][3] = x[i][3] * rstd * g0.w;
+        x[i][4] = x[i][4] * rstd * g1.x; x[i][5] = x[i][5] * rstd * g1.y;
+        x[i][6] = x[i][6] * rstd * g1.z; x[i][7] = x[i][7] * rstd * g1.w;
       }
-      if (live) {
-        float2 cs[4];
-        if (one_axis) {
-          const float4* t = reinterpret_cast<const float4*>(angle_row(axis[0], r_base + s, first + s));
-          const float4 t0 = t[0], t1 = t[1];
-          cs[0] = make_float2(t0.x, t0.y); cs[1] = make_float2(t0.z, t0.w);
-          cs[2] = make_float2(t1.x, t1.y); cs[3] = make_float2(t1.z, t1.w);
-        } else {
 #pragma unroll
-          for (int u = 0; u < 4; ++u) cs[u] = angle_row(axis[u], r_base + s, first + s)[u];
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const float c = x[i][u] * cs[u].x - x[i][u + 4] * cs[u].y;
-          const float d = x[i][u + 4] * cs[u].x + x[i][u] * cs[u].y;
-          x[i][u] = c;
-          x[i][u + 4] = d;
-        }
+      for (int u = 0; u < 4; ++u) {
+        const float c = x[i][u] * cs[u].x - x[i][u + 4] * cs[u].y;
+        const float d = x[i][u + 4] * cs[u].x + x[i][u] * cs[u].y;
+        x[i][u] = c;
+        x[i][u + 4] = d;
       }
       if (is_q && live) {
         bf16* dst = a.q_out + (r_base + s) * a.ldq + (int64_t)h * HD + j0;
@@ -246,52 +262,54 @@ __global__ void __launch_bounds__(256) append8_kernel(const __grid_constant__ Ap
         *reinterpret_cast<uint2*>(dst + HALF) = o;
       }
     }
-    if (is_q) return;
   }
+  if (!is_q) {
+    if ((unsigned)page >= (unsigned)a.dst.num_pages) {   // never turned into an address: nothing is stored
+      bad = true;
+    } else {
+      const int slot = first % a.dst.page_size;
+      const int64_t tile = (int64_t)page * a.n_kv + (h - a.n_q - (is_v ? a.n_kv : 0));
+      uint8_t* dst = (is_v ? a.dst.v : a.dst.k) + (tile * a.dst.page_size + slot) * HD + j0;
+      uint8_t* scale = (is_v ? a.dst.vs : a.dst.ks) + tile * (a.dst.page_size / C8_BLOCK) + slot / C8_BLOCK;
+      const int was = lo > 0 ? *scale : 0;               // the block holds earlier positions
+      float am = 0.f;
 #pragma unroll
-  for (int i = 0; i < NP; ++i)
+      for (int i = 0; i < NP; ++i)
 #pragma unroll
-    for (int u = 0; u < 8; ++u) am = fmaxf(am, fabsf(x[i][u]));      // dead slots are zeros
-  const int page = page_of(a.dst.table, b, a.dst.max_pages, a.dst.num_pages, first / a.dst.page_size, p.status, lane);
-  if (page < 0) return;
-  const int slot = first % a.dst.page_size;
-  const int64_t tile = (int64_t)page * a.n_kv + (h - a.n_q - (is_v ? a.n_kv : 0));
-  uint8_t* dst = (is_v ? a.dst.v : a.dst.k) + (tile * a.dst.page_size + slot) * HD + j0;
-  uint8_t* scale = (is_v ? a.dst.vs : a.dst.ks) + tile * (a.dst.page_size / C8_BLOCK) + slot / C8_BLOCK;
-  int e = c8_scale_exp(warp_amax(am));
-  if (lo > 0) {                 // the block holds earlier positions: their scale stays unless the new rows need a larger
-    const int was = *scale;
-    if (e > was) {              // bring their codes to it: exponents shift, small codes round again
-      const float f = c8_pow2(was - e);
+        for (int u = 0; u < 8; ++u) am = fmaxf(am, fabsf(x[i][u]));      // dead slots are zeros
+      int e = c8_scale_exp(warp_amax(am));
+      if (e > was && lo > 0) {  // bring the earlier codes to the larger scale: exponents shift, small codes round again
+        const float f = c8_pow2(was - e);
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+          const int s = i * RPW + sub;
+          if (s >= lo) continue;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD + half * HALF);
+            const uint32_t l = c8_half2_lo(*w), m = c8_half2_hi(*w);
+            const float2 v0 = __half22float2(*reinterpret_cast<const __half2*>(&l));
+            const float2 v1 = __half22float2(*reinterpret_cast<const __half2*>(&m));
+            *w = c8_codes4(v0.x * f, v0.y * f, v1.x * f, v1.y * f);
+          }
+        }
+      }
+      e = max(e, was);
+      __syncwarp();             // every lane has read the old scale
+      if (lane == 0) *scale = (uint8_t)e;
+      const float inv = c8_pow2(127 - e);
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         const int s = i * RPW + sub;
-        if (s >= lo) continue;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint32_t* w = reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD + half * HALF);
-          const uint32_t l = c8_half2_lo(*w), m = c8_half2_hi(*w);
-          const float2 v0 = __half22float2(*reinterpret_cast<const __half2*>(&l));
-          const float2 v1 = __half22float2(*reinterpret_cast<const __half2*>(&m));
-          *w = c8_codes4(v0.x * f, v0.y * f, v1.x * f, v1.y * f);
-        }
+        if (s < lo || s >= hi) continue;
+        *reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD) =
+            c8_codes4(x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv);
+        *reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD + HALF) =
+            c8_codes4(x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv);
       }
-    } else {
-      e = was;
     }
   }
-  __syncwarp();                 // every lane has read the old scale
-  if (lane == 0) *scale = (uint8_t)e;
-  const float inv = c8_pow2(127 - e);
-#pragma unroll
-  for (int i = 0; i < NP; ++i) {
-    const int s = i * RPW + sub;
-    if (s < lo || s >= hi) continue;
-    *reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD) =
-        c8_codes4(x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv);
-    *reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD + HALF) =
-        c8_codes4(x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv);
-  }
+  if (bad) atomicMin(p.status, (int)POP_E_INVALID);
 }
 
 bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
@@ -335,20 +353,21 @@ int launch_append8(const Append8Args& a, cudaStream_t s) {
     return POP_E_INVALID;
   if (a.head_dim != 64 && a.head_dim != 128 && a.head_dim != 256) return POP_E_INVALID;
   if (a.positions != nullptr && a.n_axes < 1) return POP_E_INVALID;
-  if (a.pair_axis != nullptr && (a.positions == nullptr || a.n_axes > 255)) return POP_E_INVALID;
+  if (a.pair_axis != nullptr && (a.positions == nullptr || a.n_axes > 255 || !aligned(a.pair_axis, 4))) return POP_E_INVALID;
   if (!aligned(a.in, 16) || !aligned(a.table, 16) || a.ld_in % 4 || (a.n_q > 0 && (!aligned(a.q_out, 8) || a.ldq % 4)))
     return POP_E_INVALID;
   if ((int64_t)a.batch * a.rows > 0x7fffffff) return POP_E_INVALID;
   if (a.start == nullptr && (int64_t)a.pos0 + a.rows > (int64_t)a.dst.max_pages * a.dst.page_size) return POP_E_NOSPACE;
   if (a.rows == 0) return POP_OK;
-  Append8Dev p;
+  Append8Dev p{};
   p.a = a;
   p.status = status_word();
   if (!p.status) return POP_E_CUDA;
   const int heads = a.n_q + 2 * a.n_kv;
+  p.head_groups = ceil_div(heads, 8);
   // rows that start anywhere in a block touch at most this many blocks
   const int64_t blocks = ((int64_t)a.rows + 2 * C8_BLOCK - 2) / C8_BLOCK;
-  const int64_t gx = blocks * ceil_div(heads, 8);
+  const int64_t gx = blocks * p.head_groups;
   if (gx > 0x7fffffff) return POP_E_INVALID;
   const dim3 grid((unsigned)gx, a.batch);
   ProfScope prof(PROF_ELEMENTWISE,

@@ -68,7 +68,7 @@ REFUSED = {
                       dict(src_layer_stride=4), dict(code_layer_stride=8)],
     "append": CACHE + [dict(x=None), dict(q_out=None), dict(rope_table=None), dict(x=A + 4), dict(ld_in=193),
                        dict(q_out=A + 2), dict(ldq=66), dict(table_rows=0), dict(pos0=-1), dict(max_rows=-1),
-                       dict(positions=A), dict(pair_axis=A), dict(positions=A, pair_axis=A, n_axes=300), dict(n_q=-1),
+                       dict(positions=A), dict(pair_axis=A), dict(positions=A, pair_axis=A, n_axes=300), dict(positions=A, pair_axis=A + 2, n_axes=3), dict(n_q=-1),
                        dict(batch=70000), dict(batch=60000, max_rows=60000)],
     "decode": CACHE + [dict(q=None), dict(out=None), dict(q=A + 8), dict(out=A + 2), dict(ldq=65), dict(ldo=68),
                        dict(n_q=3, n_kv=2), dict(n_q=0), dict(kv_len=-1), dict(window=-1), dict(batch=4097),
