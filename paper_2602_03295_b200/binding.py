@@ -414,18 +414,32 @@ class PopLibrary:
         """pop_k_quant_cache_e4m3: pools bf16 [layers, pages, page_size, n_kv, hd] -> codes uint8 [layers, pages, n_kv,
         page_size, hd] and scales uint8 [layers, pages, n_kv, page_size / 16]; seq_lens int32 [batch] or None (max_len)."""
         layers, src_pages, src_page, n_kv, hd = k_pool.shape
-        if k8.dim() != 5 or not (k8.shape[0] == v8.shape[0] == ks.shape[0] == vs.shape[0] == layers) or \
-                k_pool.dtype != torch.bfloat16 or v_pool.dtype != torch.bfloat16 or v_pool.shape != k_pool.shape:
-            raise PopError(POP_E_INVALID, "quant_cache_e4m3: pools, codes and scales of the same layers are wanted")
-        page, pages, max_pages, batch, here = self._cache8(k8[0], v8[0], ks[0], vs[0], block_table, n_kv, hd,
-                                                           (k_pool, v_pool, src_table, seq_lens))
-        if src_table.shape[0] != batch or src_table.dtype != torch.int32 or not src_table.is_contiguous() or \
-                not (k_pool[0].is_contiguous() and v_pool[0].is_contiguous()) or \
-                k_pool.stride(0) != v_pool.stride(0) or k8.stride(0) != v8.stride(0) or ks.stride(0) != vs.stride(0):
-            raise PopError(POP_E_INVALID, "quant_cache_e4m3: layers contiguous and alike for K and V, tables of one batch")
+        at = k8.get_device()
+        if at < 0 or at != torch._C._cuda_getDevice():
+            raise PopError(POP_E_INVALID, "8-bit cache: tensors on the current CUDA device are wanted")
+        for t in (k_pool, v_pool, src_table, v8, ks, vs, block_table, seq_lens):
+            if t is not None and t.get_device() != at:
+                raise PopError(POP_E_INVALID, "8-bit cache: all tensors have to be on the current CUDA device")
+        shape = k8.shape
+        if len(shape) != 5 or shape[0] != layers or shape[2] != n_kv or shape[4] != hd or v8.shape != shape or \
+                ks.shape != shape[:3] + (shape[3] // 16,) or vs.shape != ks.shape or v_pool.shape != k_pool.shape or \
+                k_pool.dtype != torch.bfloat16 or v_pool.dtype != torch.bfloat16 or \
+                not (k8.dtype == v8.dtype == ks.dtype == vs.dtype == torch.uint8):
+            raise PopError(POP_E_INVALID, "quant_cache_e4m3: bf16 pools, uint8 codes and scales of the same layers are wanted")
+        pages, page = shape[1], shape[3]
+        src_ls, code_ls, scale_ls = k_pool.stride(), k8.stride(), ks.stride()
+        if src_ls[1:] != (src_page * n_kv * hd, n_kv * hd, hd, 1) or code_ls[1:] != (n_kv * page * hd, page * hd, hd, 1) or \
+                scale_ls[1:] != (n_kv * (page // 16), page // 16, 1) or v_pool.stride() != src_ls or v8.stride() != code_ls \
+                or vs.stride() != scale_ls:
+            raise PopError(POP_E_INVALID, "quant_cache_e4m3: layers have to be contiguous, and alike for K and V")
+        batch, max_pages = block_table.shape
+        if src_table.shape[0] != batch or src_table.dtype != torch.int32 or block_table.dtype != torch.int32 or \
+                not (src_table.is_contiguous() and block_table.is_contiguous()):
+            raise PopError(POP_E_INVALID, "quant_cache_e4m3: contiguous int32 tables of one batch are wanted")
+        here = torch._C._cuda_getCurrentRawStream(at)
         code = self.dll.pop_k_quant_cache_e4m3(
-            k_pool.data_ptr(), v_pool.data_ptr(), k_pool.stride(0), src_table.data_ptr(), src_page, src_pages,
-            src_table.shape[1], k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), k8.stride(0), ks.stride(0),
+            k_pool.data_ptr(), v_pool.data_ptr(), src_ls[0], src_table.data_ptr(), src_page, src_pages,
+            src_table.shape[1], k8.data_ptr(), v8.data_ptr(), ks.data_ptr(), vs.data_ptr(), code_ls[0], scale_ls[0],
             block_table.data_ptr(), page, pages, max_pages, self._ints(seq_lens, batch, "seq_lens"), max_len, layers,
             batch, n_kv, hd, here if stream is None else stream.cuda_stream)
         if code:

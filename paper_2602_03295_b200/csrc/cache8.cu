@@ -116,26 +116,30 @@ __global__ void __launch_bounds__(256, HD == 256 ? 2 : 4) quant_cache8_kernel(co
 }
 
 // ------------------------------------------------------------------------------ norm + rotation + append
-// One warp per (sequence, block of 16 cache positions that the new rows touch, head). hd / 8 lanes take one row, each
-// four rotation pairs (j, j + hd/2): two 16-byte loads of fp32 (8-byte of bf16). A k or v head's rows all stay in
-// registers until the block's maximum is known; the eight warps of a CTA are eight heads of the same rows, so the
-// rotary rows come from L1 after the first.
+// Two warps per (sequence, block of 16 cache positions that the new rows touch, head), eight slots each. hd / 8 lanes take
+// one row, each four rotation pairs (j, j + hd/2): two 16-byte loads of fp32 (8-byte of bf16). The rows stay in registers
+// until the block's maximum is known, which the two warps exchange (one warp for all 16 rows: 128 registers, 72 us for 6656
+// rows of 32 + 16 heads; two warps at four CTAs per SM 57; the bytes take 35). A CTA is four heads of the same rows, so the rotary rows come from L1 after the
+// first.
 struct Append8Dev {
   Append8Args a;
-  int head_groups;              // CTAs per block of positions: eight heads each
+  int head_groups;              // CTAs per block of positions: four heads each
   int* status;
 };
 
 template <int HD, bool IN_BF16>
-__global__ void __launch_bounds__(256) append8_kernel(const __grid_constant__ Append8Dev p) {
-  constexpr int LPR = HD / 8, RPW = 32 / LPR, NP = C8_BLOCK / RPW, HALF = HD / 2;
+__global__ void __launch_bounds__(256, HD == 256 ? 2 : 4) append8_kernel(const __grid_constant__ Append8Dev p) {
+  constexpr int LPR = HD / 8, RPW = 32 / LPR, NP = C8_BLOCK / 2 / RPW, HALF = HD / 2;
+  __shared__ float half_max[8];
   const Append8Args& a = p.a;
   chain_trigger();
-  const int lane = threadIdx.x & 31, sub = lane / LPR, j0 = (lane % LPR) * 4;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, j0 = (lane % LPR) * 4;
+  const int sub = (warp & 1) * (C8_BLOCK / 2) + lane / LPR;                       // slot of the lane's first row
   const int heads = a.n_q + 2 * a.n_kv;
-  const int h = (int)(blockIdx.x % p.head_groups) * 8 + (threadIdx.x >> 5), blk = blockIdx.x / p.head_groups;
-  const int b = blockIdx.y;
-  if (h >= heads) return;
+  const int blk = blockIdx.x / p.head_groups, b = blockIdx.y;
+  int h = (int)(blockIdx.x - blk * p.head_groups) * 4 + (warp >> 1);
+  const bool idle = h >= heads;                                                   // works on the last head, stores nothing
+  if (idle) h = heads - 1;
   const bool is_q = h < a.n_q, is_v = h >= a.n_q + a.n_kv;
   chain_wait();
   const int row0 = a.cu ? __ldg(a.cu + b) : b * a.rows;
@@ -148,7 +152,7 @@ __global__ void __launch_bounds__(256) append8_kernel(const __grid_constant__ Ap
   }
   const int first = (start / C8_BLOCK + blk) * C8_BLOCK;                          // position of the block's slot 0
   if (first >= start + n) return;
-  const int lo = max(start - first, 0), hi = min(start + n - first, C8_BLOCK);    // live slots of the block
+  const int lo = max(start - first, 0), hi = idle ? 0 : min(start + n - first, C8_BLOCK);    // live slots of the block
   const int64_t r_base = (int64_t)row0 + first - start;                           // packed row of slot 0
 
   // Everything that is read is asked for before anything is computed: the page, the rows, the positions, the old scale. What
@@ -263,50 +267,54 @@ __global__ void __launch_bounds__(256) append8_kernel(const __grid_constant__ Ap
       }
     }
   }
-  if (!is_q) {
-    if ((unsigned)page >= (unsigned)a.dst.num_pages) {   // never turned into an address: nothing is stored
-      bad = true;
-    } else {
-      const int slot = first % a.dst.page_size;
-      const int64_t tile = (int64_t)page * a.n_kv + (h - a.n_q - (is_v ? a.n_kv : 0));
-      uint8_t* dst = (is_v ? a.dst.v : a.dst.k) + (tile * a.dst.page_size + slot) * HD + j0;
-      uint8_t* scale = (is_v ? a.dst.vs : a.dst.ks) + tile * (a.dst.page_size / C8_BLOCK) + slot / C8_BLOCK;
-      const int was = lo > 0 ? *scale : 0;               // the block holds earlier positions
-      float am = 0.f;
+  // the other half of the block's rows is in the neighbouring warp
+  const bool stores = !is_q && !idle && (unsigned)page < (unsigned)a.dst.num_pages;       // else never turned into an address
+  bad |= !is_q && !idle && !stores;
+  const int slot = first % a.dst.page_size;
+  const int64_t tile = (int64_t)(stores ? page : 0) * a.n_kv + (stores ? h - a.n_q - (is_v ? a.n_kv : 0) : 0);
+  uint8_t* dst = (is_v ? a.dst.v : a.dst.k) + (tile * a.dst.page_size + slot) * HD + j0;
+  uint8_t* scale = (is_v ? a.dst.vs : a.dst.ks) + tile * (a.dst.page_size / C8_BLOCK) + slot / C8_BLOCK;
+  int was = 0;                                           // the scale of earlier positions in the block
+  if (stores) {
+    if (lo > 0) was = *scale;
+    float am = 0.f;
 #pragma unroll
-      for (int i = 0; i < NP; ++i)
+    for (int i = 0; i < NP; ++i)
 #pragma unroll
-        for (int u = 0; u < 8; ++u) am = fmaxf(am, fabsf(x[i][u]));      // dead slots are zeros
-      int e = c8_scale_exp(warp_amax(am));
-      if (e > was && lo > 0) {  // bring the earlier codes to the larger scale: exponents shift, small codes round again
-        const float f = c8_pow2(was - e);
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const int s = i * RPW + sub;
-          if (s >= lo) continue;
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t* w = reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD + half * HALF);
-            const uint32_t l = c8_half2_lo(*w), m = c8_half2_hi(*w);
-            const float2 v0 = __half22float2(*reinterpret_cast<const __half2*>(&l));
-            const float2 v1 = __half22float2(*reinterpret_cast<const __half2*>(&m));
-            *w = c8_codes4(v0.x * f, v0.y * f, v1.x * f, v1.y * f);
-          }
-        }
-      }
-      e = max(e, was);
-      __syncwarp();             // every lane has read the old scale
-      if (lane == 0) *scale = (uint8_t)e;
-      const float inv = c8_pow2(127 - e);
+      for (int u = 0; u < 8; ++u) am = fmaxf(am, fabsf(x[i][u]));      // dead slots are zeros
+    am = warp_amax(am);
+    if (lane == 0) half_max[warp] = am;
+  }
+  __syncthreads();                                       // also: both warps have read the old scale
+  if (stores) {
+    int e = c8_scale_exp(fmaxf(half_max[warp], half_max[warp ^ 1]));
+    if (e > was && lo > 0) {    // bring the earlier codes to the larger scale: exponents shift, small codes round again
+      const float f = c8_pow2(was - e);
 #pragma unroll
       for (int i = 0; i < NP; ++i) {
         const int s = i * RPW + sub;
-        if (s < lo || s >= hi) continue;
-        *reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD) =
-            c8_codes4(x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv);
-        *reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD + HALF) =
-            c8_codes4(x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv);
+        if (s >= lo) continue;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD + half * HALF);
+          const uint32_t l = c8_half2_lo(*w), m = c8_half2_hi(*w);
+          const float2 v0 = __half22float2(*reinterpret_cast<const __half2*>(&l));
+          const float2 v1 = __half22float2(*reinterpret_cast<const __half2*>(&m));
+          *w = c8_codes4(v0.x * f, v0.y * f, v1.x * f, v1.y * f);
+        }
       }
+    }
+    e = max(e, was);
+    if (lane == 0 && (warp & 1) == 0) *scale = (uint8_t)e;
+    const float inv = c8_pow2(127 - e);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+      const int s = i * RPW + sub;
+      if (s < lo || s >= hi) continue;
+      *reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD) =
+          c8_codes4(x[i][0] * inv, x[i][1] * inv, x[i][2] * inv, x[i][3] * inv);
+      *reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD + HALF) =
+          c8_codes4(x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv);
     }
   }
   if (bad) atomicMin(p.status, (int)POP_E_INVALID);
@@ -364,7 +372,7 @@ int launch_append8(const Append8Args& a, cudaStream_t s) {
   p.status = status_word();
   if (!p.status) return POP_E_CUDA;
   const int heads = a.n_q + 2 * a.n_kv;
-  p.head_groups = ceil_div(heads, 8);
+  p.head_groups = ceil_div(heads, 4);
   // rows that start anywhere in a block touch at most this many blocks
   const int64_t blocks = ((int64_t)a.rows + 2 * C8_BLOCK - 2) / C8_BLOCK;
   const int64_t gx = blocks * p.head_groups;
