@@ -21,8 +21,10 @@
 //   an MMA warp: scores of 128 keys with one set of instructions, O += P V per 64 keys with P from TMEM. Two score
 //       buffers: one for each of two tiles, or two for one tile, so that the tensor pipe works while the softmax does;
 //   a scale warp: the scales of 32 blocks at a time, converted, in a small ring.
-// With fewer CTAs than SMs (few rows) the keys are split over several CTAs, which leave unnormalised rows in the
-// workspace for a second, chained launch to merge.
+// Where few CTAs would leave SMs idle or wait for the longest sequence, the keys are split over several CTAs, which leave
+// unnormalised rows in the workspace for a second, chained launch to merge (512 rows each of three sequences of up to
+// 16384, which are 192 CTAs of unequal length: 290 us in one piece, 237 us in two).
+#include "../../include/pop_kernels.h"
 #include "cache8.cuh"
 #include "ptx.cuh"
 
@@ -89,7 +91,7 @@ struct A8Dev {
   int per;                      // positions per tile (one head group)
   uint32_t inv;                 // 2^16 / G, rounded up
   int q_tiles;                  // CTAs along the rows of the longest sequence
-  int splits;
+  int splits, chunk;            // pieces of a tile's keys, each of at most chunk 64-key tiles
   float* partial;               // [CTA][NQT * 128][hd + 4]: m, l, two unused, accumulator
   float scale_log2;
 };
@@ -140,6 +142,8 @@ __device__ __forceinline__ Job job_of(const A8Dev& p, int bx, int by, int b, int
   x.n_tiles = last < 0 || tile < 0 ? 0 : last / 64 - x.j_lo + 1;
   return x;
 }
+// Pieces that the CTA's keys are cut into, at least one
+__device__ __forceinline__ int pieces_of(const A8Dev& p, const Job& x) { return max(1, (x.n_tiles + p.chunk - 1) / p.chunk); }
 __device__ __forceinline__ int row_pos(const Job& x, int r) { return (int)(r * x.inv >> 16); }     // r / heads
 
 __device__ __forceinline__ float ex2(float x) {
@@ -229,20 +233,19 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
   int t_lo = 0, n_tiles = x.n_tiles;                     // 64 keys each
   float* part = nullptr;
   if (p.splits > 1) {
-    t_lo = (int)((int64_t)x.n_tiles * split / p.splits);
-    n_tiles = (int)((int64_t)x.n_tiles * (split + 1) / p.splits) - t_lo;
-    part = p.partial + (((int64_t)(blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x) * (NQT * 128)) * (HD + 4);
+    const int pieces = pieces_of(p, x);
+    if (split >= pieces) return;                         // fewer keys than the longest sequence's
+    const int each = x.n_tiles / pieces, more = x.n_tiles - each * pieces;      // the first `more` have one tile more
+    t_lo = split * each + min(split, more);
+    n_tiles = each + (split < more ? 1 : 0);
+    if (pieces > 1)                                      // a tile of one piece is written at once
+      part = p.partial + (((int64_t)(blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x) * (NQT * 128)) * (HD + 4);
   }
   const int n_pairs = (n_tiles + 1) >> 1;
   const int key0 = (x.j_lo + t_lo) * BKV;                // first key of tile 0
 
-  if (n_tiles <= 0) {                                    // rows that see nothing (here): zeros, or an empty piece
+  if (n_tiles <= 0) {                                    // rows that see nothing: zeros
     for (int r = threadIdx.x; r < NQT * 128; r += blockDim.x) {
-      if (part != nullptr) {
-        part[(int64_t)r * (HD + 4)] = -INFINITY;
-        part[(int64_t)r * (HD + 4) + 1] = 0.f;
-        continue;
-      }
       const int in_tile = r & 127, ip = row_pos(x, in_tile), i = x.q0 + (r >> 7) * x.per + ip;
       if (in_tile >= x.per * x.heads || i >= x.n) continue;
       uint4* dst = reinterpret_cast<uint4*>(p.out + ((int64_t)x.row0 + i) * p.ldo +
@@ -713,29 +716,49 @@ __global__ void __launch_bounds__(256) attn8_merge_kernel(const __grid_constant_
   const int groups = NQT * 128 / 8;
   const int by = blockIdx.y / groups, r = (blockIdx.y % groups) * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const Job x = job_of<NQT>(p, blockIdx.x, by, blockIdx.z, status);
-  if (x.q0 < 0) return;
+  const int pieces = pieces_of(p, x);
+  if (x.q0 < 0 || pieces == 1) return;
   const int in_tile = r & 127, ip = row_pos(x, in_tile), i = x.q0 + (r >> 7) * x.per + ip;
   if (in_tile >= x.per * x.heads || i >= x.n) return;
   constexpr int PER = HD / 32;
   float m = -INFINITY, l = 0.f, o[PER];
 #pragma unroll
   for (int k = 0; k < PER; ++k) o[k] = 0.f;
-  for (int sp = 0; sp < p.splits; ++sp) {
-    const int64_t cta = ((int64_t)(blockIdx.z * p.splits + sp) * p.q_tiles + by) * gridDim.x + blockIdx.x;
-    const float* src = p.partial + (cta * (NQT * 128) + r) * (HD + 4);
-    const float ms = __ldcg(src), ls = __ldcg(src + 1);
-    if (ms == -INFINITY) continue;                       // nothing seen there, its accumulator may not be written
-    const float n = fmaxf(m, ms), fa = ex2(m - n), fb = ex2(ms - n);
-    l = l * fa + ls * fb;
-#pragma unroll
-    for (int k = 0; k < PER; k += 2) {
-      const float2 v = __ldcg(reinterpret_cast<const float2*>(src + 4 + lane * 2 + k * 32));
-      o[k] = o[k] * fa + v.x * fb;
-      o[k + 1] = o[k + 1] * fa + v.y * fb;
+  const int64_t stride = (int64_t)p.q_tiles * gridDim.x * (NQT * 128) * (HD + 4);           // from piece to piece
+  const float* src = p.partial + (((int64_t)blockIdx.z * p.splits * p.q_tiles + by) * gridDim.x + blockIdx.x) *
+                                     (int64_t)(NQT * 128) * (HD + 4) + (int64_t)r * (HD + 4);
+  for (int s0 = 0; s0 < pieces; s0 += 32, src += 32 * stride) {
+    // a lane per piece: its share in the sum; every piece has written its row, zeros where it saw nothing
+    const int live = min(32, pieces - s0);
+    float ms = -INFINITY, ls = 0.f;
+    if (lane < live) {
+      ms = __ldcg(src + lane * stride);
+      ls = __ldcg(src + lane * stride + 1);
     }
+    float n = fmaxf(m, ms);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) n = fmaxf(n, __shfl_xor_sync(0xffffffffu, n, d));
+    if (n == -INFINITY) continue;
+    const float f = ex2(m - n), w = ex2(ms - n);
+    float sum = w * ls;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    l = l * f + sum;
     m = n;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) o[k] *= f;
+#pragma unroll 4
+    for (int q = 0; q < live; ++q) {
+      const float wq = __shfl_sync(0xffffffffu, w, q);
+#pragma unroll
+      for (int k = 0; k < PER; k += 2) {
+        const float2 v = __ldcg(reinterpret_cast<const float2*>(src + q * stride + 4 + lane * 2 + k * 32));
+        o[k] = fmaf(v.x, wq, o[k]);
+        o[k + 1] = fmaf(v.y, wq, o[k + 1]);
+      }
+    }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;      // l 0: no piece was read, the sums are zeros
+  const float inv = l == 0.f ? 0.f : 1.f / l;      // l 0: no piece saw a key, the sums are zeros
   bf16* dst = p.out + ((int64_t)x.row0 + i) * p.ldo + (int64_t)(x.h0 + in_tile - ip * x.heads) * HD + lane * 2;
 #pragma unroll
   for (int k = 0; k < PER; k += 2)
@@ -752,14 +775,26 @@ int launch_t(const Attn8Args& a, A8Dev& p, cudaStream_t s) {
   if (q_tiles > 65535) return POP_E_INVALID;
   p.q_tiles = (int)q_tiles;
   const int64_t base = (int64_t)a.n_kv * p.hg * q_tiles * a.batch;
-  // fewer CTAs than SMs: split the keys, four 64-key tiles or more to a piece
-  const int span = a.window > 0 && (int64_t)a.window + NQT * per < a.kv_len ? a.window + NQT * per : a.kv_len;
-  int64_t splits = device_sms() / (base > 0 ? base : 1);
-  const int64_t most = (span + 255) / 256;
-  if (splits > most) splits = most;
-  if (splits < 1) splits = 1;
+  // Pieces per tile: what takes the fewest turns of all SMs at the longest sequence's keys. The unit is a tile of 64 keys
+  // (1.1 us at hd 128); beginning and ending a CTA costs eight, the merge four and its reads one per 96 pieces. Never more
+  // than what POP_E4M3_WORKSPACE_BYTES holds, so that a workspace of that size covers every call.
+  const int64_t span = a.window > 0 && (int64_t)a.window + NQT * per < a.kv_len ? a.window + NQT * per : a.kv_len;
+  const int64_t sms = device_sms(), piece = (int64_t)NQT * 128 * (HD + 4) * 4;
+  const int64_t tiles = span < 64 ? 1 : (span + 63) / 64 + (a.window > 0 ? 1 : 0);
+  int64_t splits = 1, chunk = tiles, best = INT64_MAX;
+  for (int64_t n = 1; n == 1 || (n <= sms && base * n <= 4 * sms && base * n * piece <= POP_E4M3_WORKSPACE_BYTES); ++n) {
+    const int64_t c = n > 1 && tiles < 4 * n ? 4 : (tiles + n - 1) / n;         // four tiles or more to a piece
+    const int64_t turns = (base * n + sms - 1) / sms, cost = turns * (c + 8) + (n > 1 ? 4 + base * n / 96 : 0);
+    if (cost < best) {
+      best = cost;
+      chunk = c;
+      splits = (tiles + c - 1) / c;
+    }
+    if (c <= 4) break;
+  }
   p.splits = (int)splits;
-  if (splits > 1 && (size_t)(base * splits) * NQT * 128 * (HD + 4) * 4 > a.workspace_bytes) return POP_E_NOSPACE;
+  p.chunk = (int)chunk;
+  if (splits > 1 && (size_t)(base * splits * piece) > a.workspace_bytes) return POP_E_NOSPACE;
   if (a.batch * splits > 65535) return POP_E_INVALID;
   static bool configured = false;
   if (!configured) {
