@@ -199,7 +199,7 @@ int pop_k_decode_attention_static(const void* q, int64_t ldq, const void* k_pool
  * make it 2^120), a code is value / s rounded to nearest even, saturating at 448 (NaN stays NaN). hd is 64, 128 or 256.
  * Device-side checks in every call: a block-table entry outside [0, num_pages), a length above the stated maximum, a
  * rotation row outside the table are never turned into addresses; the status word is raised to POP_E_INVALID and what
- * depends on them is not written or reads as zeros. The codes behind a sequence's last position are left as they are.
+ * depends on them is not written or reads as zeros. Lengths (kv_len) go up to 2^31 - 2^16. The codes behind a sequence's last position are left as they are.
  *
  * pop_k_quant_cache_e4m3: the bf16 cache that a prefill left, for `layers` consecutive layers (src_layer_stride elements,
  *   code_layer_stride and scale_layer_stride bytes apart), positions 0 .. n-1 of every sequence, n = seq_lens[b] (device
@@ -256,7 +256,8 @@ int pop_k_decode_attention_e4m3(const void* q, int64_t ldq, const void* k_codes,
  * max_rows), or max_rows rows each if cu_rows is NULL, and len cached positions (seq_lens / kv_len as above) which include
  * the rows' own: row i sits at position len - n + i and sees positions j <= its own, and j > its own - window if window > 0.
  * A row that sees nothing (a length below its sequence's rows) becomes zeros. Rows of no sequence are left as they are.
- * NaN codes inside a sequence may reach rows that do not see them. */
+ * Pages in front of the window of every query are not read: their table entries may be anything (decode: the same). NaN
+ * codes inside the part of a sequence that some row of the call sees may reach rows that do not see them. */
 int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int32_t max_rows, const void* k_codes,
                          const void* v_codes, const void* k_scales, const void* v_scales, const int32_t* block_table,
                          int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, const int32_t* seq_lens,

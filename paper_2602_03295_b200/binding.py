@@ -492,7 +492,7 @@ class PopLibrary:
         return q_out
 
     @staticmethod
-    def _attn8_rows(q, out, width, workspace):
+    def _attn8_rows(q, out, width, workspace, stream):
         """Checks queries and outputs; returns (rows, strides of both, workspace, its bytes)."""
         rows, w = q.shape
         ldq, q_inner = q.stride()
@@ -502,6 +502,8 @@ class PopLibrary:
             raise PopError(POP_E_INVALID, "q and out are bf16 [rows, n_q hd]")
         if workspace is None:
             workspace = torch.empty(POP_E4M3_WORKSPACE_BYTES, dtype=torch.uint8, device=q.device)
+            if stream is not None:             # its memory goes back when the call returns: not before that stream is past it
+                workspace.record_stream(stream)
         elif not workspace.is_contiguous():
             raise PopError(POP_E_INVALID, "workspace has to be contiguous")
         return rows, ldq, ldo, workspace, workspace.numel() * workspace.element_size()
@@ -511,7 +513,7 @@ class PopLibrary:
         """pop_k_decode_attention_e4m3: q, out bf16 [batch, n_q hd]; seq_lens int32 [batch] (each <= kv_len) or kv_len for
         all. `workspace` (POP_E4M3_WORKSPACE_BYTES of any dtype) is allocated if not given."""
         page, pages, max_pages, batch, here = self._cache8(k8, v8, ks, vs, block_table, n_kv, hd, (q, out, workspace, seq_lens))
-        rows, ldq, ldo, ws, nbytes = self._attn8_rows(q, out, n_q * hd, workspace)
+        rows, ldq, ldo, ws, nbytes = self._attn8_rows(q, out, n_q * hd, workspace, stream)
         if rows != batch:
             raise PopError(POP_E_INVALID, "decode_attention_e4m3: one query row and one block-table row per sequence")
         code = self.dll.pop_k_decode_attention_e4m3(
@@ -528,7 +530,7 @@ class PopLibrary:
         max_rows rows each); seq_lens int32 [batch] cached positions, the rows' own included, or kv_len for all."""
         page, pages, max_pages, batch, here = self._cache8(k8, v8, ks, vs, block_table, n_kv, hd,
                                                            (q, out, workspace, seq_lens, cu_rows))
-        rows, ldq, ldo, ws, nbytes = self._attn8_rows(q, out, n_q * hd, workspace)
+        rows, ldq, ldo, ws, nbytes = self._attn8_rows(q, out, n_q * hd, workspace, stream)
         if cu_rows is None and rows != batch * max_rows:
             raise PopError(POP_E_INVALID, "attention_e4m3: max_rows rows of every sequence, or cu_rows, are wanted")
         if rows == 0:

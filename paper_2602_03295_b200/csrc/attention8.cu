@@ -16,7 +16,7 @@
 //   NQT softmax warpgroups, one row per thread: place both codes of Q in shared memory, then read S = Q K^T from TMEM 64
 //       keys at a time, write the weights over it, rescale the TMEM accumulator when the maximum grew by more than 2^8;
 //   a converter warpgroup: 64 keys of V at a time from the staged codes to f16 in the 128-byte-swizzled operand layout;
-//       positions past the end become zeros;
+//       positions past the end, or in front of every row's window, become zeros;
 //   a TMA warp: codes of K (128 keys) and V (64 keys) from the paged pools, a row being one position of one head;
 //   an MMA warp: scores of 128 keys with one set of instructions, O += P V per 64 keys with P from TMEM. Two score
 //       buffers: one for each of two tiles, or two for one tile, so that the tensor pipe works while the softmax does;
@@ -102,7 +102,7 @@ struct Job {
   uint32_t inv;                 // 2^16 / heads, rounded up: r / heads = r * inv >> 16 for r < 256
   int row0, n, q0;              // first packed row of the sequence, its rows, first row of the CTA (< 0: none)
   int len, pos0;                // cached positions; position of row q0
-  int j_lo, n_tiles;            // 64-key tiles that its rows see
+  int lo, j_lo, n_tiles;        // first key that its rows see; 64-key tiles that they see
 };
 template <int NQT>
 __device__ __forceinline__ Job job_of(const A8Dev& p, int bx, int by, int b, int* status) {
@@ -138,7 +138,8 @@ __device__ __forceinline__ Job job_of(const A8Dev& p, int bx, int by, int b, int
   x.q0 = tile * step;
   x.pos0 = x.len - x.n + x.q0;
   const int last = min(x.pos0 + step - 1, x.len - 1);
-  x.j_lo = p.window > 0 ? max(0, x.pos0 - p.window + 1) / 64 : 0;
+  x.lo = p.window > 0 ? max(0, max(0, x.pos0) - p.window + 1) : 0;
+  x.j_lo = x.lo / 64;
   x.n_tiles = last < 0 || tile < 0 ? 0 : last / 64 - x.j_lo + 1;
   return x;
 }
@@ -267,12 +268,13 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
   };
 
 
-  // TMA: lane l holds the pool row of copy l of a pair (128 keys), fetched a pair ahead. A copy that starts past the end
-  // is left out; one of a bad page goes past the pool's end and is filled with zeros.
+  // TMA: lane l holds the pool row of copy l of a pair (128 keys), fetched a pair ahead. A copy that starts past the end, or
+  // ends in front of the window (its page may belong to another sequence by now), is left out; one of a bad page goes past the
+  // pool's end and is filled with zeros.
   const int boxes = PKV / p.box, half_boxes = boxes >> 1;
   auto row_of = [&](int J) {
     const int pos = key0 + J * PKV + lane * p.box;
-    if (lane >= boxes || J >= n_pairs || pos >= x.len) return -2;
+    if (lane >= boxes || J >= n_pairs || pos >= x.len || pos + p.box <= x.lo) return -2;
     const int r = pool_row(pos);
     return r < 0 ? p.pool_rows : r;
   };
@@ -465,7 +467,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       auto fetch = [&](int grp, int& ke, int& ve) {
         ke = ve = 127;
         const int pos = key0 + (grp * 32 + lane) * C8_BLOCK;
-        if (pos < x.len && grp * 8 + (lane >> 2) < n_tiles) {
+        if (pos < x.len && pos + C8_BLOCK > x.lo && grp * 8 + (lane >> 2) < n_tiles) {
           const int r = pool_row(pos);
           if (r >= 0) {
             ke = p.c.ks[r / C8_BLOCK];
@@ -504,7 +506,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         const int ci = i * 128 + tid, row = ci / CPR, c = ci % CPR;
         cur[i] = *reinterpret_cast<const uint4*>(s.vr[vs] + (c / (INNER / 16)) * (BKV * INNER) +
                                                  code_at<INNER>(row, c % (INNER / 16)));
-        if (kv0 + row >= x.len) cur[i] = make_uint4(0, 0, 0, 0);
+        if (kv0 + row >= x.len || kv0 + row < x.lo) cur[i] = make_uint4(0, 0, 0, 0);
       }
 #pragma unroll
       for (int i = 0; i < C::LOADS; ++i) {
@@ -778,9 +780,9 @@ int launch_t(const Attn8Args& a, A8Dev& p, cudaStream_t s) {
   // Pieces per tile: what takes the fewest turns of all SMs at the longest sequence's keys. The unit is a tile of 64 keys
   // (1.1 us at hd 128); beginning and ending a CTA costs eight, the merge four and its reads one per 96 pieces. Never more
   // than what POP_E4M3_WORKSPACE_BYTES holds, so that a workspace of that size covers every call.
-  const int64_t span = a.window > 0 && (int64_t)a.window + NQT * per < a.kv_len ? a.window + NQT * per : a.kv_len;
+  const int64_t span = p.window > 0 && (int64_t)p.window + NQT * per < a.kv_len ? p.window + NQT * per : a.kv_len;
   const int64_t sms = device_sms(), piece = (int64_t)NQT * 128 * (HD + 4) * 4;
-  const int64_t tiles = span < 64 ? 1 : (span + 63) / 64 + (a.window > 0 ? 1 : 0);
+  const int64_t tiles = span < 64 ? 1 : (span + 63) / 64 + (p.window > 0 ? 1 : 0);
   int64_t splits = 1, chunk = tiles, best = INT64_MAX;
   for (int64_t n = 1; n == 1 || (n <= sms && base * n <= 4 * sms && base * n * piece <= POP_E4M3_WORKSPACE_BYTES); ++n) {
     const int64_t c = n > 1 && tiles < 4 * n ? 4 : (tiles + n - 1) / n;         // four tiles or more to a piece
@@ -796,19 +798,15 @@ int launch_t(const Attn8Args& a, A8Dev& p, cudaStream_t s) {
   p.chunk = (int)chunk;
   if (splits > 1 && (size_t)(base * splits * piece) > a.workspace_bytes) return POP_E_NOSPACE;
   if (a.batch * splits > 65535) return POP_E_INVALID;
-  static bool configured = false;
-  if (!configured) {
-    if (cudaFuncSetAttribute(attn8_kernel<HD, NQT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
-      return POP_E_CUDA;
-    configured = true;
-  }
+  static std::atomic<uint64_t> configured{0};
+  if (!c8_allow_smem(configured, reinterpret_cast<const void*>(attn8_kernel<HD, NQT>), (int)smem)) return POP_E_CUDA;
   int* status = status_word();
   if (!status) return POP_E_CUDA;
   CUtensorMap tk, tv;
   if (make_tmap_u8_rows(&tk, a.c.k, HD, p.pool_rows, C::INNER, p.box) != POP_OK ||
       make_tmap_u8_rows(&tv, a.c.v, HD, p.pool_rows, C::INNER, p.box) != POP_OK)
     return POP_E_CUDA;
-  ProfScope prof(PROF_ATTENTION, 4.0 * HD * a.n_q * a.batch * (double)a.rows * (span - (a.window > 0 ? 0.0 : 0.5 * a.rows)), s);
+  ProfScope prof(PROF_ATTENTION, 4.0 * HD * a.n_q * a.batch * (double)a.rows * (span - (p.window > 0 ? 0.0 : 0.5 * a.rows)), s);
   if (launch_chained(attn8_kernel<HD, NQT>, dim3(a.n_kv * p.hg, (unsigned)q_tiles, (unsigned)(a.batch * splits)),
                      dim3(C::THREADS), smem, s, tk, tv, p, status) != cudaSuccess)
     return POP_E_CUDA;
@@ -827,7 +825,7 @@ int launch_t(const Attn8Args& a, A8Dev& p, cudaStream_t s) {
 int launch_attention8(const Attn8Args& a, cudaStream_t s) {
   if (!a.q || !a.out || !c8_cache_ok(a.c)) return POP_E_INVALID;
   if (a.batch < 1 || a.batch > 65535 || a.n_kv < 1 || a.n_q < 1 || a.n_q % a.n_kv || a.n_q > 65536 || a.rows < 0 ||
-      a.kv_len < 0 || a.kv_len > 0x7ffffff0 || a.window < 0 || a.window > 0x7ffffff0)
+      a.kv_len < 0 || a.kv_len > 0x7fff0000 || a.window < 0 || a.window > 0x7ffffff0)
     return POP_E_INVALID;
   if (a.head_dim != 64 && a.head_dim != 128 && a.head_dim != 256) return POP_E_INVALID;
   if (reinterpret_cast<uintptr_t>(a.q) % 16 || reinterpret_cast<uintptr_t>(a.out) % 16 || a.ldq % 8 || a.ldo % 8)
@@ -851,7 +849,7 @@ int launch_attention8(const Attn8Args& a, cudaStream_t s) {
   p.n_q = a.n_q; p.n_kv = a.n_kv; p.G = a.n_q / a.n_kv; p.hg = (p.G + 127) / 128;
   p.per = 128 / (p.G < 128 ? p.G : 128);
   p.inv = (65536 + p.G - 1) / p.G;
-  p.window = a.window;
+  p.window = a.window < a.kv_len ? a.window : 0;         // a longer one hides nothing
   p.partial = static_cast<float*>(a.workspace);
   p.scale_log2 = 1.4426950408889634f / sqrtf((float)a.head_dim);
   // one tile of 128 rows where no sequence has more

@@ -11,6 +11,8 @@
 
 #include <cuda_fp16.h>
 
+#include <atomic>
+
 namespace pop {
 
 constexpr int C8_BLOCK = 16;          // positions per scale
@@ -91,6 +93,16 @@ struct Attn8Args {
 int launch_decode_attention8(const Attn8Args& a, cudaStream_t s);
 int launch_attention8(const Attn8Args& a, cudaStream_t s);
 int launch_few8(const Attn8Args& a, cudaStream_t s);           // few rows; arguments checked by the two above
+// Lets a kernel have `bytes` of dynamic shared memory on the current device; done: a bit per device that has been asked
+inline bool c8_allow_smem(std::atomic<uint64_t>& done, const void* kernel, int bytes) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const uint64_t bit = uint64_t(1) << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return true;
+}
 int device_sms();                                              // SMs of the device that was current at the first call
 
 }  // namespace pop

@@ -24,6 +24,7 @@
 //   - else all items form one line of blocks and every warp of a full GPU takes an equal stretch of it, whatever the
 //     lengths are. An item that a warp has whole is finished by it; the pieces of the others go through the workspace to a
 //     second, chained launch (a CTA that lies inside one item merges its eight in shared memory first).
+#include "../../include/pop_kernels.h"
 #include "cache8.cuh"
 #include "ptx.cuh"
 
@@ -56,6 +57,8 @@ struct D8 {
   static constexpr int RING = NST * STAGE;              // of a warp; a piece for the CTA's merge goes over the idle ring
   static constexpr int SMEM = WARPS * RING + SLOT * 4;  // and the CTA's merged piece, for its cluster
   static_assert(SLOT * 4 <= RING, "a piece goes over the ring");
+  // two pieces of every warp: the stated workspace covers a GPU of up to 160 SMs
+  static_assert(160 * PER_SM * WARPS * 2 * PSLOT * 4 <= POP_E4M3_WORKSPACE_BYTES, "workspace");
 };
 
 // Where 16-byte piece ch of row r of a block lies in its stage: permuted so that the eight lanes that read together (two
@@ -778,7 +781,7 @@ template <int HD, int CG>
 int launch_t(const Attn8Args& a, Dec8Dev& p, cudaStream_t s) {
   using C = D8<HD, CG>;
   p.chunks = (int)(((int64_t)a.rows * p.G + C::NC - 1) / C::NC);
-  const int span = a.window > 0 && (int64_t)a.window + a.rows + C8_BLOCK < a.kv_len ? a.window + a.rows + C8_BLOCK : a.kv_len;
+  const int span = p.window > 0 && (int64_t)p.window + a.rows + C8_BLOCK < a.kv_len ? p.window + a.rows + C8_BLOCK : a.kv_len;
   const int64_t blocks = ((int64_t)span + C8_BLOCK - 1) / C8_BLOCK, items = (int64_t)a.batch * a.n_kv * p.chunks;
   // block numbers, of the call and of the pool, are 32-bit
   if (blocks > 0x7fffffff / (items + 1) ||
@@ -801,13 +804,9 @@ int launch_t(const Attn8Args& a, Dec8Dev& p, cudaStream_t s) {
   p.status = status_word();
   if (!p.status) return POP_E_CUDA;
   const int scan_bytes = p.cluster ? 0 : (a.batch + 1) * 4;
-  static bool configured = false;
-  if (!configured) {
-    if (cudaFuncSetAttribute(dec8_kernel<HD, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                             C::SMEM + (MAX_BATCH + 1) * 4) != cudaSuccess)
-      return POP_E_CUDA;
-    configured = true;
-  }
+  static std::atomic<uint64_t> configured{0};
+  if (!c8_allow_smem(configured, reinterpret_cast<const void*>(dec8_kernel<HD, CG>), C::SMEM + (MAX_BATCH + 1) * 4))
+    return POP_E_CUDA;
   ProfScope prof(PROF_DECODE_ATTN, (double)a.batch * span * a.n_kv * (2.0 * HD + 0.125), s);
   const size_t smem = (size_t)(C::SMEM + scan_bytes);
   const cudaError_t rc = p.cluster > 1
@@ -832,7 +831,8 @@ int launch_few8(const Attn8Args& a, cudaStream_t s) {
   p.q = a.q; p.ldq = a.ldq;
   p.c = a.c;
   p.cu = a.cu; p.rows = a.rows;
-  p.seq_lens = a.seq_lens; p.kv_len = a.kv_len; p.window = a.window;
+  p.seq_lens = a.seq_lens; p.kv_len = a.kv_len;
+  p.window = a.window < a.kv_len ? a.window : 0;         // a longer one hides nothing
   p.out = a.out; p.ldo = a.ldo;
   p.batch = a.batch; p.n_q = a.n_q; p.n_kv = a.n_kv; p.G = a.n_q / a.n_kv;
   p.partial = static_cast<float*>(a.workspace);
@@ -850,7 +850,7 @@ int launch_few8(const Attn8Args& a, cudaStream_t s) {
 int launch_decode_attention8(const Attn8Args& a, cudaStream_t s) {
   if (!a.q || !a.out || !c8_cache_ok(a.c)) return POP_E_INVALID;
   if (a.batch < 1 || a.batch > MAX_BATCH || a.n_kv < 1 || a.n_q < 1 || a.n_q % a.n_kv || a.n_q > 65536 || a.kv_len < 0 ||
-      a.kv_len > 0x7ffffff0 || a.window < 0 || a.window > 0x7ffffff0)
+      a.kv_len > 0x7fff0000 || a.window < 0 || a.window > 0x7ffffff0)
     return POP_E_INVALID;
   if (a.head_dim != 64 && a.head_dim != 128 && a.head_dim != 256) return POP_E_INVALID;
   if (reinterpret_cast<uintptr_t>(a.q) % 16 || reinterpret_cast<uintptr_t>(a.out) % 16 || a.ldq % 8 || a.ldo % 8 ||

@@ -123,3 +123,11 @@ def test_binding_refuses_tensors_that_are_not_on_the_device(library):
     with pytest.raises(PopError) as e:
         library.decode_attention_e4m3(q, c, c, s, s, bt, q.clone(), 1, 1, 64, 16)
     assert e.value.code == POP_E_INVALID
+
+
+@pytest.mark.parametrize("op", ["decode", "prompt"])
+def test_lengths_and_windows_behind_the_largest_are_refused(library, op):
+    from paper_2602_03295_b200 import POP_E_INVALID
+    name, args = CALLS[op]
+    for change in (dict(kv_len=0x7fff0001), dict(window=0x7ffffff1)):
+        assert getattr(library.dll, name)(*{**args, "max_pages": 1 << 28, **change}.values()) == POP_E_INVALID

@@ -592,3 +592,144 @@ def test_offsets_behind_32_bits(L):
     check_attention(q.cpu(), out.cpu(), local, [1], [n + 1], 8, n_kv, hd, 0, decode=True)
     L.attention_e4m3(q, k8, v8, ks, vs, ids.to(DEV), out, 8, n_kv, hd, 1, n + 1)
     check_attention(q.cpu(), out.cpu(), local, [1], [n + 1], 8, n_kv, hd, 0)
+
+
+# ---------------------------------------------------------------------------------------------- ways to split the work
+def run_rows(L, cache, rows, lens, n_q, n_kv, hd, window, seed, decode=False, top=None, **over):
+    """One attention call over the first layer of the cache; returns (queries, outputs), the outputs poisoned before it."""
+    q = queries(seed, sum(rows), n_q, hd)
+    out = torch.full(q.shape, math.nan, dtype=torch.bfloat16, device=DEV)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    ln = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    top = max(lens) if top is None else top
+    if decode:
+        L.decode_attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, top, seq_lens=ln, window=window, **over)
+    else:
+        cu = torch.tensor([sum(rows[:i]) for i in range(len(rows) + 1)], dtype=torch.int32, device=DEV)
+        L.attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, max(rows), top, cu_rows=cu, seq_lens=ln, window=window, **over)
+    return q, out
+
+
+def spread(n, low, high):
+    return [low + (high - low) * ((i * 37) % n) // max(n - 1, 1) for i in range(n)]
+
+
+FEW = [  # rows, lens, n_q, n_kv, hd, page, window: few query rows, from one block per warp to many warps per sequence
+    ([1] * 40, spread(40, 0, 500), 4, 2, 128, 16, 0), ([2] * 40, spread(40, 2, 500), 8, 2, 64, 64, 0),
+    ([1] * 20, spread(20, 1, 960), 16, 2, 128, 32, 0), ([3] * 10, spread(10, 3, 1100), 6, 2, 256, 16, 0),
+    ([2], [4800], 18, 2, 128, 128, 0), ([1, 1], [4800, 5], 8, 2, 64, 16, 0), ([1], [20000], 8, 2, 128, 128, 0),
+    ([4, 1], [19000, 7], 16, 2, 64, 64, 0), ([1, 2], [18000, 18001], 8, 2, 256, 128, 0), ([1] * 70, spread(70, 0, 1500), 4, 2, 128, 16, 0),
+    ([3, 0, 2, 1] * 18, [x + 3 for x in spread(72, 0, 1400)], 8, 2, 64, 32, 0), ([1] * 80, spread(80, 0, 1300), 4, 2, 256, 16, 300),
+    ([2] * 75, spread(75, 1, 1300), 10, 2, 128, 64, 100), ([8], [900], 1, 1, 128, 16, 0), ([9], [900], 1, 1, 128, 16, 7),
+    ([16, 5], [900, 40], 1, 1, 64, 16, 0), ([17, 3], [100, 2000], 2, 2, 128, 16, 0), ([8, 8, 7], [300, 9, 3000], 3, 1, 64, 32, 20),
+    ([32, 31, 1], [700, 40, 2], 2, 2, 128, 64, 0), ([33, 31, 1], [700, 40, 2], 2, 2, 128, 64, 0), ([4, 3], [9000, 100], 16, 2, 256, 128, 500),
+]
+
+
+@pytest.mark.parametrize("rows,lens,n_q,n_kv,hd,page,window", FEW, ids=lambda v: str(v)[:24])
+def test_few_rows_however_the_blocks_are_dealt(L, rows, lens, n_q, n_kv, hd, page, window):
+    cache = random_cache(100, 1, len(lens), max(lens), n_kv, hd, page)
+    poison_behind(cache, lens)
+    decode = set(rows) == {1}
+    q, out = run_rows(L, cache, rows, lens, n_q, n_kv, hd, window, 101, decode)
+    assert L.status() == 0
+    check_attention(q, out.cpu(), cache, rows, lens, n_q, n_kv, hd, window, decode=decode)
+
+
+PIECES = [  # rows, lens, n_q, n_kv, hd, page, window: tiles whose keys are cut into several pieces, and tiles that are not
+    ([40, 33, 100], [5000, 64, 700], 2, 1, 128, 128, 0), ([200, 90], [3000, 91], 2, 1, 64, 64, 500),
+    ([40] * 80, spread(80, 30, 2300), 4, 2, 128, 16, 0), ([50, 70] * 40, spread(80, 60, 1500), 2, 2, 256, 64, 0),
+    ([70, 0, 64], [9000, 0, 50], 4, 1, 256, 384, 0), ([150] * 20, spread(20, 100, 1800), 16, 4, 64, 32, 600),
+    ([513], [4000], 2, 1, 128, 64, 0), ([3], [2000], 300, 1, 64, 16, 0),
+]
+
+
+@pytest.mark.parametrize("rows,lens,n_q,n_kv,hd,page,window", PIECES, ids=lambda v: str(v)[:24])
+def test_prompt_rows_whose_keys_are_cut(L, rows, lens, n_q, n_kv, hd, page, window):
+    cache = random_cache(110, 1, len(lens), max(lens), n_kv, hd, page)
+    poison_behind(cache, lens)
+    q, out = run_rows(L, cache, rows, lens, n_q, n_kv, hd, window, 111)
+    assert L.status() == 0
+    check_attention(q, out.cpu(), cache, rows, lens, n_q, n_kv, hd, window, pick=1)
+
+
+@pytest.mark.parametrize("hd,page,rows,window", [(128, 16, 1, 100), (256, 64, 1, 300), (64, 16, 5, 40), (128, 16, 60, 77),
+                                                (64, 32, 200, 500), (256, 16, 30, 130), (128, 128, 90, 1)])
+def test_pages_in_front_of_the_window_are_gone(L, hd, page, rows, window):
+    """Their table entries are no pages any more, and pages with other contents (NaN codes) are reached by none."""
+    n_q, n_kv, lens = 4, 2, [1500, 1111, 900]
+    cache = random_cache(120, 1, len(lens), max(lens), n_kv, hd, page)
+    poison_behind(cache, lens)
+    whole = tuple(t.clone() for t in cache)
+    for b, n in enumerate(lens):
+        gone = max(0, n - rows - window + 1) // page
+        for c in cache[:2]:
+            c[0, cache[4][b, :gone].long()] = 0x7f
+        cache[4][b, :gone] = -1 if b else 2 ** 30
+    q, out = run_rows(L, cache, [rows] * 3, lens, n_q, n_kv, hd, window, 121, rows == 1)
+    assert L.status() == 0
+    check_attention(q, out.cpu(), whole, [rows] * 3, lens, n_q, n_kv, hd, window, decode=rows == 1)
+
+
+@pytest.mark.parametrize("rows", [1, 3, 200])
+def test_a_window_longer_than_the_cache_hides_nothing(L, rows):
+    n_q, n_kv, hd, lens = 4, 2, 64, [150, 90]
+    cache = random_cache(130, 1, 2, 150, n_kv, hd, 16)
+    base = run_rows(L, cache, [rows] * 2, lens, n_q, n_kv, hd, 0, 131)
+    for window in (150, 151, 2 ** 31 - 17):
+        assert torch.equal(run_rows(L, cache, [rows] * 2, lens, n_q, n_kv, hd, window, 131)[1], base[1])
+    assert L.status() == 0
+    check_attention(base[0], base[1].cpu(), cache, [rows] * 2, lens, n_q, n_kv, hd, 0)
+
+
+def test_stream_argument_without_a_workspace(L):
+    """The workspace that such a call makes for itself stays its own until that stream is past it."""
+    n_q, n_kv, hd, lens = 8, 2, 128, [20000, 19000]
+    cache = random_cache(140, 1, 2, 20000, n_kv, hd, 128)
+    side = torch.cuda.Stream()
+    want = {rows: run_rows(L, cache, [rows] * 2, lens, n_q, n_kv, hd, 0, 141 + rows)[1] for rows in (1, 60)}
+    torch.cuda.synchronize()
+    for rows in (1, 60):
+        for _ in range(4):
+            q = queries(141 + rows, 2 * rows, n_q, hd).to(DEV)
+            dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+            ln, out = torch.tensor(lens, dtype=torch.int32, device=DEV), torch.empty_like(q)
+            cu = torch.tensor([0, rows, 2 * rows], dtype=torch.int32, device=DEV)
+            torch.cuda.synchronize()
+            L.attention_e4m3(q, *dev, out, n_q, n_kv, hd, rows, 20000, cu_rows=cu, seq_lens=ln, stream=side)
+            torch.full((64 << 18,), math.nan, device=DEV)              # as large as the workspace, on the current stream
+            torch.cuda.synchronize()
+            assert torch.equal(out, want[rows])
+    assert L.status() == 0
+
+
+def test_calls_from_two_threads(L):
+    """Each with its stream and workspace."""
+    import threading
+    n_q, n_kv, hd, lens = 8, 2, 64, [3000, 700]
+    cache = random_cache(150, 1, 2, 3000, n_kv, hd, 64)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    ln = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    jobs = []
+    for rows in (1, 70):
+        q = queries(151 + rows, 2 * rows, n_q, hd).to(DEV)
+        jobs.append((rows, q, run_rows(L, cache, [rows] * 2, lens, n_q, n_kv, hd, 0, 151 + rows)[1],
+                     torch.cuda.Stream(), torch.empty(64 << 20, dtype=torch.uint8, device=DEV)))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(rows, q, want, stream, ws):
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                out = torch.full_like(q, math.nan)
+                L.attention_e4m3(q, *dev, out, n_q, n_kv, hd, rows, 3000, seq_lens=ln, workspace=ws)
+                stream.synchronize()
+                if not torch.equal(out, want):
+                    wrong.append(rows)
+
+    threads = [threading.Thread(target=work, args=j) for j in jobs]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong and L.status() == 0
