@@ -18,8 +18,11 @@
 //   a converter warpgroup: 64 keys of V at a time from the staged codes to f16 in the 128-byte-swizzled operand layout;
 //       positions past the end, or in front of every row's window, become zeros;
 //   a TMA warp: codes of K (128 keys) and V (64 keys) from the paged pools, a row being one position of one head;
-//   an MMA warp: scores of 128 keys with one set of instructions, O += P V per 64 keys with P from TMEM. Two score
-//       buffers: one for each of two tiles, or two for one tile, so that the tensor pipe works while the softmax does;
+//   an MMA warp per tile: scores, then O += P V per 64 keys with P from TMEM. Two score buffers per tile, so that the next
+//       scores are there before the softmax is done with the last: 64 keys each for two tiles, 128 for one (a set of 128
+//       keys shares the reads of Q, 64 against 48 clocks an instruction, but with two tiles TMEM has room for one such set
+//       per tile: 573 us for an 8192-token prompt, 556 with two of 64). One warp for both tiles spent 2190 clocks per 64
+//       keys, 1560 of them issuing (54 per instruction), and made the softmax wait for scores;
 //   a scale warp: the scales of 32 blocks at a time, converted, in a small ring.
 // Where few CTAs would leave SMs idle or wait for the longest sequence, the keys are split over several CTAs, which leave
 // unnormalised rows in the workspace for a second, chained launch to merge (512 rows each of three sequences of up to
@@ -48,7 +51,8 @@ struct A8 {
   static constexpr int NK = HD == 256 ? 2 : 3;
   static constexpr int NVR = HD == 256 ? 2 : 4;
   static constexpr int NVF = HD == 256 ? 2 : 4;
-  static constexpr int NB = NQT == 1 ? 2 : 1;                  // score buffers per tile
+  static constexpr int SK = NQT == 1 ? 128 : 64;               // keys of a set of scores: two buffers of them per tile
+  static constexpr int HPS = SK / BKV, SPP = PKV / SK;         // 64-key tiles per set, sets per pair of tiles
   static constexpr int SM_WARPS = NQT * 4;
   static constexpr int THREADS = (SM_WARPS + 8) * 32;
   static constexpr int LOADS = BKV * HD / (16 * 128);          // 16-byte pieces of a V stage per converter thread
@@ -70,9 +74,9 @@ struct __align__(1024) A8Smem {
   uint64_t vr_full[C::NVR], vr_empty[C::NVR];
   uint64_t vf_full[C::NVF], vf_empty[C::NVF];
   uint64_t sc_full[2], sc_empty[2];
-  uint64_t s_full[2];           // scores of a pair of key tiles complete; index: tile or buffer
-  uint64_t p_ready[2][2];       // P of half h written over its scores (one arrival per softmax warp)
-  uint64_t pv_done[2][2];       // O += P V of half h complete
+  uint64_t s_full[NQT][2];      // a set of scores complete; index: tile, buffer
+  uint64_t p_ready[NQT][2][C::HPS];  // P of 64 keys written over their scores (one arrival per softmax warp)
+  uint64_t pv_done[NQT][2][C::HPS];  // O += P V of 64 keys complete
   uint32_t tmem_base;
   uint32_t raised;
   volatile uint32_t abort;
@@ -199,22 +203,24 @@ __global__ void __launch_bounds__(A8<HD, NQT>::THREADS, 1)
 attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
              const __grid_constant__ A8Dev p, int* __restrict__ status) {
   using C = A8<HD, NQT>;
-  constexpr int BKV = C::BKV, PKV = C::PKV, INNER = C::INNER, SLICES = C::SLICES, NB = C::NB;
+  constexpr int BKV = C::BKV, PKV = C::PKV, INNER = C::INNER, SLICES = C::SLICES;
+  constexpr int SK = C::SK, HPS = C::HPS, SPP = C::SPP;
   extern __shared__ uint8_t smem_raw[];
   A8Smem<HD, NQT>& s =
       *reinterpret_cast<A8Smem<HD, NQT>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   chain_trigger();
-  const int warp = threadIdx.x >> 5;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);      // known to be the same in the warp: uniform registers
   const int lane = threadIdx.x & 31;
   if (threadIdx.x == (C::SM_WARPS + 4) * 32) {           // the TMA warp's first lane: it uses them before the others do
-    for (int i = 0; i < C::NK; ++i) { mbar_init(&s.k_full[i], 1); mbar_init(&s.k_empty[i], 1); }
+    for (int i = 0; i < C::NK; ++i) { mbar_init(&s.k_full[i], 1); mbar_init(&s.k_empty[i], NQT); }
     for (int i = 0; i < C::NVR; ++i) { mbar_init(&s.vr_full[i], 1); mbar_init(&s.vr_empty[i], 4); }
-    for (int i = 0; i < C::NVF; ++i) { mbar_init(&s.vf_full[i], 4); mbar_init(&s.vf_empty[i], 1); }
+    for (int i = 0; i < C::NVF; ++i) { mbar_init(&s.vf_full[i], 4); mbar_init(&s.vf_empty[i], NQT); }
     for (int i = 0; i < 2; ++i) { mbar_init(&s.sc_full[i], 1); mbar_init(&s.sc_empty[i], C::SM_WARPS); }
-    for (int t = 0; t < 2; ++t) {
-      mbar_init(&s.s_full[t], 1);
-      for (int i = 0; i < 2; ++i) { mbar_init(&s.p_ready[t][i], 4); mbar_init(&s.pv_done[t][i], 1); }
-    }
+    for (int t = 0; t < NQT; ++t)
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&s.s_full[t][i], 1);
+        for (int h = 0; h < C::HPS; ++h) { mbar_init(&s.p_ready[t][i][h], 4); mbar_init(&s.pv_done[t][i][h], 1); }
+      }
     s.abort = 0;
     fence_barrier_init();
     prefetch_tmap(&tmK);
@@ -388,18 +394,25 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         tma_row = next;
       }
       if (!ok) A8_ABORT(s, status);
-    } else if (role == 1) {
-      // ---------------------------------------------------------------- MMA (whole warp, elected lane)
+    } else if (role == 1 || (NQT == 2 && role == 3)) {
+      // ---------------------------------------------------------------- MMA of tile t (whole warp, elected lane)
       const uint32_t leader = elect_one();
-      constexpr uint32_t idesc_s = umma_idesc_e4m3(128, PKV);
+      // everything that the instructions are made of is the same in the warp, in a way that the compiler sees: descriptors are
+      // computed in uniform registers (an 8192-token prompt: 603 -> 577 us)
+      const uint32_t tmem_u = __shfl_sync(0xffffffffu, tmem_base, 0);
+      const int n_tiles_u = __shfl_sync(0xffffffffu, n_tiles, 0);
+      auto wait_all = [&](uint64_t* bar, uint32_t parity) {
+        return (bool)__all_sync(0xffffffffu, mbar_wait_relaxed(bar, parity));
+      };
+      constexpr uint32_t idesc_s = umma_idesc_e4m3(128, SK);
       constexpr uint32_t idesc_o = umma_idesc_f16(128, HD, 1);
       const uint64_t q_desc = code_desc<INNER>(smem_u32(s.q[0][0]));
       const uint64_t k_desc = code_desc<INNER>(smem_u32(s.k[0]));
       const uint64_t v_desc = umma_smem_desc(smem_u32(s.vf[0]), C::VF_SUB, 1024);    // MN-major
-      auto issue_s = [&](int t, int J) {                   // 128 keys, both codes of q
-        const int sb = NQT == 1 ? (J & 1) : t;
-        const uint64_t kd = k_desc + uint64_t((J % C::NK) * (C::K_STAGE >> 4));
-        const uint32_t d = tmem_base + sb * 128;
+      const int t = role >> 1;
+      auto issue_s = [&](int i) {                          // set i, both codes of q
+        const uint64_t kd = k_desc + uint64_t((i / SPP % C::NK * C::K_STAGE + i % SPP * SK * INNER) >> 4);
+        const uint32_t d = tmem_u + t * 128 + (i & 1) * SK;
 #pragma unroll
         for (int part_i = 0; part_i < 2; ++part_i) {
           const uint64_t qd = q_desc + uint64_t((t * 2 + part_i) * (C::Q_PART >> 4));
@@ -410,56 +423,52 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
                            kd + uint64_t((sl * PKV * INNER + in * 32) >> 4), idesc_s, (part_i | kk) ? 1u : 0u);
           }
         }
-        umma_commit_w(leader, &s.s_full[sb]);
+        umma_commit_w(leader, &s.s_full[t][i & 1]);
       };
-      auto issue_pv = [&](int t, int jj) {                 // 64 keys: A = P in TMEM (8 packed columns per 16 keys), B = V
-        const int sb = NQT == 1 ? ((jj >> 1) & 1) : t, h = jj & 1;
-        const uint32_t pa = tmem_base + sb * 128 + h * BKV;
+      auto issue_pv = [&](int jj) {                        // 64 keys: A = P in TMEM (8 packed columns per 16 keys), B = V
+        const int i = jj / HPS, h = jj % HPS;
+        const uint32_t pa = tmem_u + t * 128 + (i & 1) * SK + h * BKV;
         const uint64_t vd = v_desc + uint64_t((jj % C::NVF) * (C::VF_STAGE >> 4));
-        const uint32_t d = tmem_base + C::O_COL + t * HD;
+        const uint32_t d = tmem_u + C::O_COL + t * HD;
 #pragma unroll
         for (int kk = 0; kk < BKV / 16; ++kk)
           umma_bf16_ts_w(leader, d, pa + kk * 8, vd + uint64_t((kk * 2048) >> 4), idesc_o, (jj > 0 || kk > 0) ? 1u : 0u);
-        umma_commit_w(leader, &s.pv_done[sb][h]);
+        umma_commit_w(leader, &s.pv_done[t][i & 1][h]);
+      };
+      const int n_sets = (n_tiles_u + HPS - 1) / HPS;
+      // before set i: its keys are there; behind it: they are free once the pair's last set is done
+      auto keys_of = [&](int i) {
+        if (i % SPP != 0) return true;
+        const bool there = wait_all(&s.k_full[i / SPP % C::NK], (i / SPP / C::NK) & 1);
+        tc_fence_after();
+        return there;
+      };
+      auto keys_done = [&](int i) {
+        if (i % SPP == SPP - 1 || i == n_sets - 1) umma_commit_w(leader, &s.k_empty[i / SPP % C::NK]);
       };
       bool ok = true;
-      // scores of the first pair (of two pairs where one tile has both buffers)
-      for (int J = 0; J < NB && J < n_pairs && ok; ++J) {
-        ok = mbar_wait_relaxed(&s.k_full[J % C::NK], (J / C::NK) & 1);
+      for (int i = 0; i < 2 && i < n_sets && ok; ++i) {    // all buffers' first scores
+        ok = keys_of(i);
+        if (ok) {
+          issue_s(i);
+          keys_done(i);
+        }
+      }
+      for (int jj = 0; jj < n_tiles_u && ok && !__any_sync(0xffffffffu, s.abort); ++jj) {
+        const int i = jj / HPS, h = jj % HPS, in = i + 2;  // in: the set whose scores go where this one's are
+        const bool more = in < n_sets && h == HPS - 1;
+        ok = wait_all(&s.vf_full[jj % C::NVF], (jj / C::NVF) & 1);
+        ok = ok && wait_all(&s.p_ready[t][i & 1][h], (i >> 1) & 1);
         if (!ok) break;
         tc_fence_after();
-        for (int t = 0; t < NQT; ++t) issue_s(t, J);
-        umma_commit_w(leader, &s.k_empty[J % C::NK]);
-      }
-      for (int J = 0; J < n_pairs && ok && !s.abort; ++J) {
-        const int Jn = J + NB;                             // the pair whose scores go where this one's are
-        const bool more = Jn < n_pairs;
-        bool k_ready = false;
-        for (int h = 0; h < 2 && ok; ++h) {
-          const int jj = 2 * J + h;
-          if (jj >= n_tiles) break;
-          const bool last_half = h == 1 || jj + 1 >= n_tiles;
-          ok = mbar_wait_relaxed(&s.vf_full[jj % C::NVF], (jj / C::NVF) & 1);
-          for (int t = 0; t < NQT && ok; ++t) {
-            const int sb = NQT == 1 ? (J & 1) : t;
-            ok = mbar_wait_relaxed(&s.p_ready[sb][h], (J / NB) & 1);
-            if (!ok) break;
-            tc_fence_after();
-            issue_pv(t, jj);
-            if (last_half && more) {
-              // both halves of the buffer are consumed: the pipe runs its instructions in order
-              if (!k_ready) {
-                ok = mbar_wait_relaxed(&s.k_full[Jn % C::NK], (Jn / C::NK) & 1);
-                if (!ok) break;
-                tc_fence_after();
-                k_ready = true;
-              }
-              issue_s(t, Jn);
-            }
-          }
-          if (ok) umma_commit_w(leader, &s.vf_empty[jj % C::NVF]);
+        issue_pv(jj);
+        umma_commit_w(leader, &s.vf_empty[jj % C::NVF]);
+        if (more) {                                        // the buffer is consumed: the pipe runs its instructions in order
+          ok = keys_of(in);
+          if (!ok) break;
+          issue_s(in);
+          keys_done(in);
         }
-        if (ok && more) umma_commit_w(leader, &s.k_empty[Jn % C::NK]);
       }
       if (!ok) A8_ABORT(s, status);
     } else if (role == 2) {
@@ -547,12 +556,11 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     float m_run = -INFINITY;      // running (possibly stale) maximum of the exponent, ev included
     float l_run = 0.f;
     bool ok = true;
-    auto buf_of = [&](int jj) { return NQT == 1 ? ((jj >> 1) & 1) : t; };
-    auto wait_pv = [&](int jj) { return mbar_wait(&s.pv_done[buf_of(jj)][jj & 1], ((jj >> 1) / NB) & 1); };
+    auto wait_pv = [&](int jj) { return mbar_wait(&s.pv_done[t][jj / HPS & 1][jj % HPS], (jj / HPS >> 1) & 1); };
 
     for (int jj = 0; jj < n_tiles; ++jj) {
-      const int kv0 = key0 + jj * BKV, J = jj >> 1, h = jj & 1, sb = buf_of(jj), grp = jj >> 3;
-      const uint32_t sp_addr = tmem_base + lane_addr + sb * 128 + h * BKV;
+      const int kv0 = key0 + jj * BKV, set = jj / HPS, h = jj % HPS, grp = jj >> 3;
+      const uint32_t sp_addr = tmem_base + lane_addr + t * 128 + (set & 1) * SK + h * BKV;
       if ((jj & 7) == 0 && !mbar_wait(&s.sc_full[grp & 1], (grp >> 1) & 1)) { ok = false; break; }
       float kf[4], lv[4], iv[4];
 #pragma unroll
@@ -563,7 +571,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
         iv[k] = f.z;
       }
       if (h == 0) {
-        if (!mbar_wait(&s.s_full[sb], (J / NB) & 1)) { ok = false; break; }
+        if (!mbar_wait(&s.s_full[t][set & 1], (set >> 1) & 1)) { ok = false; break; }
         tc_fence_after();
       }
       float sv[BKV];
@@ -652,7 +660,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {
-        mbar_arrive(&s.p_ready[sb][h]);
+        mbar_arrive(&s.p_ready[t][set & 1][h]);
         if ((jj & 7) == 7) mbar_arrive(&s.sc_empty[grp & 1]);
       }
     }
