@@ -90,6 +90,7 @@ struct A8Dev {
   const int32_t* cu; int rows;
   const int32_t* seq_lens; int kv_len;
   bf16* out; int64_t ldo;
+  bool out32;                   // output rows on 32-byte boundaries
   int n_q, n_kv, G, hg;         // query heads per kv head; head groups of at most 128 per kv head
   int window;
   int per;                      // positions per tile (one head group)
@@ -163,6 +164,10 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 }
 __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ uint32_t sub_h2(uint32_t a, uint32_t b) {
+  const __half2 v = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 __device__ __forceinline__ uint32_t pack_b2(float lo, float hi) {
@@ -325,52 +330,61 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     tmem_alloc(&s.tmem_base, C::TMEM_COLS);
     tmem_relinquish();
   } else if (warp < C::SM_WARPS + 4) {
-    constexpr int LPR = HD / 8, RPI = 32 / LPR, WARPS = C::SM_WARPS + 4;      // lanes per row, rows per load
+    constexpr int LPR = HD / 32, RPI = 32 / LPR, WARPS = C::SM_WARPS + 4;     // lanes per row, rows at a time
     constexpr int GROUPS = NQT * 128 / RPI;
     static_assert(NQT * 128 * HD * 2 <= sizeof(s.vf), "the rows pass through the memory of V's stages");
-    const int c = lane % LPR;
     // asynchronous copies and small loops instead of registers and unrolled code: this runs once per CTA, from a cold
-    // instruction cache (unrolled it took 9900 cycles, most of them fetching instructions)
+    // instruction cache. A lane takes 32 elements of a row (with 8 each, shuffles and addresses were most of the work).
+    const int c = lane % LPR;
     uint8_t* raw = s.vf[0] + lane * 16;
 #pragma unroll 1
     for (int g = warp; g < GROUPS; g += WARPS) {
       const int r = g * RPI + lane / LPR, tr = r & 127, ip = row_pos(x, tr), iq = x.q0 + (r >> 7) * x.per + ip;
       const bool live = tr < x.per * x.heads && iq < x.n;
       const bf16* src = p.q;
-      if (live) src += ((int64_t)x.row0 + iq) * p.ldq + (int64_t)(x.h0 + tr - ip * x.heads) * HD + c * 8;
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(raw + g * 512)), "l"(src),
-                   "r"(live ? 16 : 0) : "memory");
+      if (live) src += ((int64_t)x.row0 + iq) * p.ldq + (int64_t)(x.h0 + tr - ip * x.heads) * HD + c * 16;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)                          // two neighbouring pieces of 16 bytes, and two LPR pairs behind them
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(raw + g * 2048 + k * 512)),
+                     "l"(src + (k >> 1) * (LPR * 16) + (k & 1) * 8), "r"(live ? 16 : 0) : "memory");
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-#pragma unroll 2
+#pragma unroll 1
     for (int g = warp; g < GROUPS; g += WARPS) {
       const int r = g * RPI + lane / LPR;
-      const uint4 v = *reinterpret_cast<const uint4*>(raw + g * 512);       // this thread's own copy
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+      uint4 v[4];                                          // this thread's own copies
       float am = 0.f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        am = max3(am, fabsf(__uint_as_float(w[k] << 16)), fabsf(__uint_as_float(w[k] & 0xffff0000u)));
+      for (int k = 0; k < 4; ++k) {
+        v[k] = *reinterpret_cast<const uint4*>(raw + g * 2048 + k * 512);
+        const uint32_t w[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          am = max3(am, fabsf(__uint_as_float(w[u] << 16)), fabsf(__uint_as_float(w[u] & 0xffff0000u)));
+      }
 #pragma unroll
       for (int o = LPR / 2; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(0xffffffffu, am, o));
       const int eb = max((int)(__float_as_uint(am) >> 23), 20);
       const float mul = c8_pow2(134 - eb);
       if (c == 0) s.crow[r] = c8_pow2(eb - 134) * p.scale_log2;
-      uint32_t hi[2], lo[2];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const float e0 = __uint_as_float(w[2 * k] << 16) * mul, e1 = __uint_as_float(w[2 * k] & 0xffff0000u) * mul;
-        const float e2 = __uint_as_float(w[2 * k + 1] << 16) * mul, e3 = __uint_as_float(w[2 * k + 1] & 0xffff0000u) * mul;
-        const uint32_t h4 = c8_codes4(e0, e1, e2, e3), f0 = c8_half2_lo(h4), f1 = c8_half2_hi(h4);
-        const float2 r0 = __half22float2(*reinterpret_cast<const __half2*>(&f0));
-        const float2 r1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
-        hi[k] = h4;
-        lo[k] = c8_codes4(e0 - r0.x, e1 - r0.y, e2 - r1.x, e3 - r1.y);
+      for (int k = 0; k < 4; k += 2) {
+        uint32_t hi[4], lo[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint4& y = v[k + (u >> 1)];
+          const uint32_t w0 = (u & 1) ? y.z : y.x, w1 = (u & 1) ? y.w : y.y;
+          // scaled, a bf16 element is an f16 one exactly (to 2^-25), and so is what its nearest code leaves
+          const uint32_t a = pack_h2(__uint_as_float(w0 << 16) * mul, __uint_as_float(w0 & 0xffff0000u) * mul);
+          const uint32_t b = pack_h2(__uint_as_float(w1 << 16) * mul, __uint_as_float(w1 & 0xffff0000u) * mul);
+          hi[u] = c8_codes4_h2(a, b);
+          lo[u] = c8_codes4_h2(sub_h2(a, c8_half2_lo(hi[u])), sub_h2(b, c8_half2_hi(hi[u])));
+        }
+        const int c16 = (k >> 1) * LPR + c;
+        const int at = (c16 / (INNER / 16)) * (128 * INNER) + code_at<INNER>(r & 127, c16 % (INNER / 16));
+        *reinterpret_cast<uint4*>(s.q[r >> 7][0] + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        *reinterpret_cast<uint4*>(s.q[r >> 7][1] + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
       }
-      const int c16 = c >> 1;
-      const int at = (c16 / (INNER / 16)) * (128 * INNER) + code_at<INNER>(r & 127, c16 % (INNER / 16)) + (c & 1) * 8;
-      *reinterpret_cast<uint2*>(s.q[r >> 7][0] + at) = make_uint2(hi[0], hi[1]);
-      *reinterpret_cast<uint2*>(s.q[r >> 7][1] + at) = make_uint2(lo[0], lo[1]);
     }
     fence_proxy_async_smem();
   }
@@ -688,14 +702,20 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
             for (int v = 0; v < 8; ++v)
               *reinterpret_cast<uint4*>(pr + 4 + c * 32 + v * 4) = make_uint4(o[v * 4], o[v * 4 + 1], o[v * 4 + 2], o[v * 4 + 3]);
           } else if (used) {
+            uint32_t w[16];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-              uint4 w;
-              w.x = pack_b2(__uint_as_float(o[v * 8 + 0]) * inv, __uint_as_float(o[v * 8 + 1]) * inv);
-              w.y = pack_b2(__uint_as_float(o[v * 8 + 2]) * inv, __uint_as_float(o[v * 8 + 3]) * inv);
-              w.z = pack_b2(__uint_as_float(o[v * 8 + 4]) * inv, __uint_as_float(o[v * 8 + 5]) * inv);
-              w.w = pack_b2(__uint_as_float(o[v * 8 + 6]) * inv, __uint_as_float(o[v * 8 + 7]) * inv);
-              *reinterpret_cast<uint4*>(out + c * 32 + v * 8) = w;
+            for (int v = 0; v < 16; ++v)
+              w[v] = pack_b2(__uint_as_float(o[v * 2]) * inv, __uint_as_float(o[v * 2 + 1]) * inv);
+#pragma unroll
+            for (int v = 0; v < 16; v += 8) {
+              bf16* dst = out + c * 32 + v * 2;
+              if (p.out32) {                             // a sector at once: half the stores, each of 32 different lines
+                asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(w[v]), "r"(w[v + 1]),
+                             "r"(w[v + 2]), "r"(w[v + 3]), "r"(w[v + 4]), "r"(w[v + 5]), "r"(w[v + 6]), "r"(w[v + 7]) : "memory");
+              } else {
+                *reinterpret_cast<uint4*>(dst) = make_uint4(w[v], w[v + 1], w[v + 2], w[v + 3]);
+                *reinterpret_cast<uint4*>(dst + 8) = make_uint4(w[v + 4], w[v + 5], w[v + 6], w[v + 7]);
+              }
             }
           }
         }
@@ -854,6 +874,7 @@ int launch_attention8(const Attn8Args& a, cudaStream_t s) {
   p.cu = a.cu; p.rows = a.rows;
   p.seq_lens = a.seq_lens; p.kv_len = a.kv_len;
   p.out = a.out; p.ldo = a.ldo;
+  p.out32 = reinterpret_cast<uintptr_t>(a.out) % 32 == 0 && a.ldo % 16 == 0;
   p.n_q = a.n_q; p.n_kv = a.n_kv; p.G = a.n_q / a.n_kv; p.hg = (p.G + 127) / 128;
   p.per = 128 / (p.G < 128 ? p.G : 128);
   p.inv = (65536 + p.G - 1) / p.G;

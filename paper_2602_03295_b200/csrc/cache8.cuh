@@ -35,6 +35,13 @@ __device__ __forceinline__ uint32_t c8_codes4(float a, float b, float c, float d
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
   return (uint32_t)lo | ((uint32_t)hi << 16);
 }
+// the same of two packed f16 pairs
+__device__ __forceinline__ uint32_t c8_codes4_h2(uint32_t ab, uint32_t cd) {
+  uint16_t lo, hi;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(lo) : "r"(ab));
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(hi) : "r"(cd));
+  return (uint32_t)lo | ((uint32_t)hi << 16);
+}
 // two codes (low and high byte of h) -> packed f16, exact
 __device__ __forceinline__ uint32_t c8_half2(uint16_t h) {
   uint32_t r;

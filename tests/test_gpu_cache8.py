@@ -733,3 +733,18 @@ def test_calls_from_two_threads(L):
     for t in threads:
         t.join()
     assert not wrong and L.status() == 0
+
+
+@pytest.mark.parametrize("hd,rows", [(64, 5), (64, 90), (128, 90), (256, 40)])
+@pytest.mark.parametrize("lead,pad", [(8, 0), (0, 8), (16, 0)])
+def test_outputs_on_boundaries_of_16_bytes(L, hd, rows, lead, pad):
+    n_q, n_kv, length = 4, 2, 200
+    cache = random_cache(160, 1, 1, length, n_kv, hd, 64)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    q = queries(161, rows, n_q, hd, pad=lead + pad)
+    whole = torch.full((rows, lead + n_q * hd + pad), 5.0, dtype=torch.bfloat16, device=DEV)
+    out = whole[:, lead:lead + n_q * hd]
+    L.attention_e4m3(q.to(DEV)[:, lead:lead + n_q * hd], *dev, out, n_q, n_kv, hd, rows, length)
+    assert L.status() == 0
+    assert (whole[:, :lead] == 5.0).all() and (whole[:, lead + n_q * hd:] == 5.0).all()
+    check_attention(q[:, lead:lead + n_q * hd], out.cpu(), cache, [rows], [length], n_q, n_kv, hd, 0, pick=1)
