@@ -5,8 +5,8 @@
 // j > it - window). With codes k_j, v_j, block exponents ek, ev and c = log2(e) / sqrt(hd):
 //   w_j = exp2(c q.k_j 2^(ek) + ev - m),  out = sum_j w_j v_j / sum_j w_j 2^(-ev)
 // (m the running maximum of the exponent without -m): the block scales never touch the tensor cores' operands, which are
-// the codes themselves as f16 (exact), the query as f16 after a power-of-two scale per row (exact down to 2^-36 of the
-// row's largest element) and the weights as f16. Scores, statistics, sums and the accumulator are fp32.
+// the K codes as they are, the query as two codes an element, the V codes as f16 (exact) and the weights as f16 (half a
+// step: 2^-11 relative). Scores, statistics, sums and the accumulator are fp32.
 //
 // A CTA owns NQT tiles of 128 rows of one kv head; a row is a (position, query head) pair of that kv head, so that the
 // keys are read once for all heads that share them, however few the positions are. K codes are E4M3 operands as they
@@ -27,6 +27,15 @@
 // Where few CTAs would leave SMs idle or wait for the longest sequence, the keys are split over several CTAs, which leave
 // unnormalised rows in the workspace for a second, chained launch to merge (512 rows each of three sequences of up to
 // 16384, which are 192 CTAs of unequal length: 290 us in one piece, 237 us in two).
+//
+// Measured, causal, 32 heads over 8, hd 128: 8192 rows of 8192 551 us, 998 TFLOP/s (0.60 of a bf16 GEMM's); hd 256, 16 over
+// 8, window 1024: 8192 rows 191 us; 512 rows each of three sequences of up to 16384 239 us. Bound by the softmax warps'
+// dependent steps: 1980 clocks per 64 keys, of which the exponential unit works 1024 (two warps of a scheduler) and the tensor
+// pipe 1280; halving the exponentials (a copy, to see) took 14 % off, leaving out the row maximum 3 %, the V conversion
+// nothing. A CTA's start takes 13000 clocks and its end 4500, of 145000 (hd 256 with the window: of 50000). Tried and slower:
+// one CTA per SM that walks equal shares of all tiles (898 us; the segments' starts and the live state cost more than the
+// balance gave), the next tile's scores or scales asked for before this one's weights are stored (551 to 569 against 556),
+// query rows by bulk copies (570).
 #include "../../include/pop_kernels.h"
 #include "cache8.cuh"
 #include "ptx.cuh"
@@ -35,7 +44,11 @@ namespace pop {
 namespace {
 
 constexpr int kSmemLimit = 227 * 1024;
-constexpr int FEW_COLUMNS = 32;       // up to this many (row, head) pairs of a kv head go to decode8.cu
+// Up to this many (row, head) pairs of a kv head go to decode8.cu, which reads the keys once per eight of them; here they are
+// rows of a tile of 128. Both measured, hd 128, 32 heads over 8: 12 sequences of up to 8000 positions 16 pairs 34 against 94
+// us, 32 44 / 94, 64 68 / 95, 96 97 / 95; one of 8192 16 16.4 / 25, 32 16.5 / 25, 48 26 / 25, 64 30 / 25; 40 of up to 500 16
+// 21 / 31, 32 36 / 31, 64 65 / 31.
+constexpr int FEW_COLUMNS = 32;
 constexpr float W_SHIFT = 7.f;        // weights are stored times 2^7; the lazy maximum lets them reach 2^15
 
 template <int HD, int NQT>

@@ -9,7 +9,7 @@
 // the weights that meet the tensor cores are at most 1 whatever the scales of the blocks are.
 //
 // Bound by the cache's bytes: 2 hd + 1/8 per kv head and position. A warp takes blocks of 16 positions of one item - a
-// (sequence, kv head, group of at most 8 CG columns) - through its own small ring in shared memory (16-byte asynchronous
+// (sequence, kv head, group of at most 8 columns) - through its own small ring in shared memory (16-byte asynchronous
 // copies; a block is one contiguous piece) and works on them with the warp-level MMA, the KEYS on the M side
 // (S^T = K q^T, O^T = V^T P^T): a dot product does not see the order of its terms, so a lane's 16 consecutive bytes of a
 // key feed the MMAs as they are. K codes meet the query as E4M3 operands: after a power-of-two scale per column an element
@@ -24,6 +24,14 @@
 //   - else all items form one line of blocks and every warp of a full GPU takes an equal stretch of it, whatever the
 //     lengths are. An item that a warp has whole is finished by it; the pieces of the others go through the workspace to a
 //     second, chained launch (a CTA that lies inside one item merges its eight in shared memory first).
+// More than eight columns are several items, which read the same keys one after another from L2. (Two groups of columns
+// per item, for one reading and conversion of the values, had one warp's registers full and were slower: five rows each of
+// twelve sequences of up to 8000, 20 columns, 48.6 against 38.7 us.)
+//
+// Measured, hd 128, 32 heads over 8: 48 sequences of up to 16001 positions 142 us, 5.8 TB/s of the cache's bytes (0.88 of a
+// copy's rate); one of 8192 11.0 us, where starting, one round through memory and merging are nearly all; hd 256, 20 windows
+// of 1024 28.8 us: the blocks are read at the memory's rate in 11 us, the rest is the start (5.5 us: lengths, table, first
+// blocks) and the second launch.
 #include "../../include/pop_kernels.h"
 #include "cache8.cuh"
 #include "ptx.cuh"
@@ -37,9 +45,9 @@ constexpr int MAX_BATCH = 4096;      // the block counts' prefix sums sit in sha
 constexpr float W_SHIFT = 14.f;      // weights are stored times 2^14
 constexpr int CLUSTER_BLOCKS = 16;   // cluster form: blocks per warp at most
 
-template <int HD, int CG>
+template <int HD>
 struct D8 {
-  static constexpr int NC = 8 * CG;            // columns of an item: the N extent of CG MMAs
+  static constexpr int NC = 8;                 // columns of an item: the N extent of an MMA
   static constexpr int NT = HD / 16;           // MMAs along the head
   static constexpr int KC = HD / 64;           // 16-byte pieces of a key row per lane
   static constexpr int VW = HD / 32;           // words of a value row per lane
@@ -234,9 +242,9 @@ __device__ __forceinline__ Place locate(const Dec8Dev& p, const Prefix& pre, int
   return x;
 }
 
-template <int HD, int CG>
-__global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(const __grid_constant__ Dec8Dev p) {
-  using C = D8<HD, CG>;
+template <int HD>
+__global__ void __launch_bounds__(WARPS * 32, D8<HD>::PER_SM) dec8_kernel(const __grid_constant__ Dec8Dev p) {
+  using C = D8<HD>;
   constexpr int NC = C::NC, NT = C::NT, KC = C::KC, VW = C::VW, CH = C::CH, HS = C::HS, NST = C::NST, BPI = C::BPI;
   extern __shared__ __align__(128) uint8_t smem[];            // RING bytes of every warp, SLOT floats, the prefix sums
   __shared__ int warp_sums[WARPS];
@@ -295,21 +303,16 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
     const int col0 = x.chunk * NC, cols = min(NC, x.s.rows * p.G - col0), h0 = x.kvh * p.G;
     const int32_t* bt = p.c.table + (int64_t)x.b * p.c.max_pages;
 
-    // the query rows' loads go out first: of column group cg a lane takes column g at dims 64 c + 16 t .. + 15
-    uint4 raw[CG][KC][2];
-    int row_of_col[CG];
+    // the query rows' loads go out first: a lane takes column g at dims 64 c + 16 t .. + 15
+    uint4 raw[KC][2];
+    const int col = col0 + g;
+    const bool live = g < cols;
+    const int row_of_col = live ? col / p.G : 0, h = live ? col - row_of_col * p.G : 0;
+    const bf16* qrow = p.q + (int64_t)(x.s.row0 + row_of_col) * p.ldq + (int64_t)(h0 + h) * HD + 16 * t;
 #pragma unroll
-    for (int cg = 0; cg < CG; ++cg) {
-      const int col = col0 + cg * 8 + g;
-      const bool live = cg * 8 + g < cols;
-      const int i = live ? col / p.G : 0, h = live ? col - i * p.G : 0;
-      row_of_col[cg] = i;
-      const bf16* qrow = p.q + (int64_t)(x.s.row0 + i) * p.ldq + (int64_t)(h0 + h) * HD + 16 * t;
-#pragma unroll
-      for (int c = 0; c < KC; ++c) {
-        raw[cg][c][0] = *reinterpret_cast<const uint4*>(qrow + 64 * c);
-        raw[cg][c][1] = *reinterpret_cast<const uint4*>(qrow + 64 * c + 8);
-      }
+    for (int c = 0; c < KC; ++c) {
+      raw[c][0] = *reinterpret_cast<const uint4*>(qrow + 64 * c);
+      raw[c][1] = *reinterpret_cast<const uint4*>(qrow + 64 * c + 8);
     }
 
     // Places and scales of 32 blocks at a time, one per lane: block number in the pool (-1, read as zeros, for a table
@@ -353,63 +356,50 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
       cp_async_commit();
     }
 
-    // q^T as the B operand: of column group cg a lane holds column g at dims 64 c + 16 t + 4 w .. + 3, scaled so that the
+    // q^T as the B operand: a lane holds column g at dims 64 c + 16 t + 4 w .. + 3, scaled so that the
     // column's largest element is in [2^7, 2^8), as two codes: the nearest one and the nearest one of what is left.
-    // Per column of this lane's scores (2t and 2t + 1 of each group): factor and position.
-    uint32_t qh[CG][KC][4], ql[CG][KC][4];
-    float c0[CG], c1[CG];
-    int pos0[CG], pos1[CG];
+    // Per column of this lane's scores (2t and 2t + 1): factor and position.
+    uint32_t qh[KC][4], ql[KC][4];
+    float am = 0.f;
+    auto lo_f = [](uint32_t w) { return __uint_as_float(w << 16); };
+    auto hi_f = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
 #pragma unroll
-    for (int cg = 0; cg < CG; ++cg) {
-      const bool live = cg * 8 + g < cols;
-      float am = 0.f;
-      auto lo_f = [](uint32_t w) { return __uint_as_float(w << 16); };
-      auto hi_f = [](uint32_t w) { return __uint_as_float(w & 0xffff0000u); };
+    for (int c = 0; c < KC; ++c)
 #pragma unroll
-      for (int c = 0; c < KC; ++c)
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t w[4] = {raw[c][k].x, raw[c][k].y, raw[c][k].z, raw[c][k].w};
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const uint32_t w[4] = {raw[cg][c][k].x, raw[cg][c][k].y, raw[cg][c][k].z, raw[cg][c][k].w};
-#pragma unroll
-          for (int m = 0; m < 4; ++m) am = fmaxf(am, fmaxf(fabsf(lo_f(w[m])), fabsf(hi_f(w[m]))));
-        }
-      am = fmaxf(am, __shfl_xor_sync(FULL, am, 1));
-      am = fmaxf(am, __shfl_xor_sync(FULL, am, 2));
-      const int eb = max((int)(__float_as_uint(am) >> 23), 20);
-      const float mul = live ? c8_pow2(134 - eb) : 0.f, inv = c8_pow2(eb - 134) * p.scale_log2;
-#pragma unroll
-      for (int c = 0; c < KC; ++c) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint4& r = raw[cg][c][k >> 1];
-          const uint32_t w0 = (k & 1) ? r.z : r.x, w1 = (k & 1) ? r.w : r.y;
-          const float e0 = lo_f(w0) * mul, e1 = hi_f(w0) * mul, e2 = lo_f(w1) * mul, e3 = hi_f(w1) * mul;
-          const uint32_t hi = c8_codes4(e0, e1, e2, e3), f0 = c8_half2_lo(hi), f1 = c8_half2_hi(hi);
-          const float2 r0 = __half22float2(*reinterpret_cast<const __half2*>(&f0));
-          const float2 r1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
-          qh[cg][c][k] = hi;
-          ql[cg][c][k] = c8_codes4(e0 - r0.x, e1 - r0.y, e2 - r1.x, e3 - r1.y);
-        }
+        for (int m = 0; m < 4; ++m) am = fmaxf(am, fmaxf(fabsf(lo_f(w[m])), fabsf(hi_f(w[m]))));
       }
-      c0[cg] = __shfl_sync(FULL, inv, t * 8);
-      c1[cg] = __shfl_sync(FULL, inv, t * 8 + 4);
-      const int pos = x.s.len - x.s.rows + row_of_col[cg];
-      pos0[cg] = __shfl_sync(FULL, pos, t * 8);
-      pos1[cg] = __shfl_sync(FULL, pos, t * 8 + 4);
+    am = fmaxf(am, __shfl_xor_sync(FULL, am, 1));
+    am = fmaxf(am, __shfl_xor_sync(FULL, am, 2));
+    const int eb = max((int)(__float_as_uint(am) >> 23), 20);
+    const float mul = live ? c8_pow2(134 - eb) : 0.f, inv = c8_pow2(eb - 134) * p.scale_log2;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint4& r = raw[c][k >> 1];
+        const uint32_t w0 = (k & 1) ? r.z : r.x, w1 = (k & 1) ? r.w : r.y;
+        const float e0 = lo_f(w0) * mul, e1 = hi_f(w0) * mul, e2 = lo_f(w1) * mul, e3 = hi_f(w1) * mul;
+        const uint32_t hi = c8_codes4(e0, e1, e2, e3), f0 = c8_half2_lo(hi), f1 = c8_half2_hi(hi);
+        const float2 r0 = __half22float2(*reinterpret_cast<const __half2*>(&f0));
+        const float2 r1 = __half22float2(*reinterpret_cast<const __half2*>(&f1));
+        qh[c][k] = hi;
+        ql[c][k] = c8_codes4(e0 - r0.x, e1 - r0.y, e2 - r1.x, e3 - r1.y);
+      }
     }
+    const float c0 = __shfl_sync(FULL, inv, t * 8), c1 = __shfl_sync(FULL, inv, t * 8 + 4);
+    const int pos = x.s.len - x.s.rows + row_of_col;
+    const int pos0 = __shfl_sync(FULL, pos, t * 8), pos1 = __shfl_sync(FULL, pos, t * 8 + 4);
     // blocks up to key full_hi need no causal mask, from key full_lo on no window mask
     const int first_row = col0 / p.G, last_row = (col0 + cols - 1) / p.G;
     const int full_hi = x.s.len - x.s.rows + first_row;
     const int full_lo = p.window > 0 ? x.s.len - x.s.rows + last_row - p.window + 1 : 0;
 
-    float m0[CG], m1[CG], l0[CG], l1[CG], o[CG][NT][4];
+    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f, o[NT][4];
 #pragma unroll
-    for (int cg = 0; cg < CG; ++cg) {
-      m0[cg] = m1[cg] = -INFINITY;
-      l0[cg] = l1[cg] = 0.f;
-#pragma unroll
-      for (int j = 0; j < NT; ++j) o[cg][j][0] = o[cg][j][1] = o[cg][j][2] = o[cg][j][3] = 0.f;
-    }
+    for (int j = 0; j < NT; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
 
     int stage = 0;
     for (int i = 0; i < n_blk; i += BPI) {
@@ -423,30 +413,23 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
         if (i + 32 < n_blk) fetch(i + 32, id_n, sc_n);
       }
       const uint8_t* st = ring + stage * C::STAGE;
-      float s[BPI][CG][4];
+      float s[BPI][4];
 #pragma unroll
       for (int u2 = 0; u2 < BPI; ++u2) {
-        float sb[CG][4];               // s and sb: of the two codes of q
+        float sb[4];                   // s and sb: of the two codes of q
 #pragma unroll
-        for (int cg = 0; cg < CG; ++cg)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) s[u2][cg][k] = sb[cg][k] = 0.f;
+        for (int k = 0; k < 4; ++k) s[u2][k] = sb[k] = 0.f;
 #pragma unroll
         for (int c = 0; c < KC; ++c) {                         // keys g and g + 8 at bytes 64 c + 16 t .. + 15
           const uint4 ka = *reinterpret_cast<const uint4*>(st + u2 * 2 * C::TILE + swz<HD>(g, 4 * c + t));
           const uint4 kb = *reinterpret_cast<const uint4*>(st + u2 * 2 * C::TILE + swz<HD>(g + 8, 4 * c + t));
-#pragma unroll
-          for (int cg = 0; cg < CG; ++cg) {
-            mma_e4m3(s[u2][cg], ka.x, kb.x, ka.y, kb.y, qh[cg][c][0], qh[cg][c][1]);
-            mma_e4m3(sb[cg], ka.x, kb.x, ka.y, kb.y, ql[cg][c][0], ql[cg][c][1]);
-            mma_e4m3(s[u2][cg], ka.z, kb.z, ka.w, kb.w, qh[cg][c][2], qh[cg][c][3]);
-            mma_e4m3(sb[cg], ka.z, kb.z, ka.w, kb.w, ql[cg][c][2], ql[cg][c][3]);
-          }
+          mma_e4m3(s[u2], ka.x, kb.x, ka.y, kb.y, qh[c][0], qh[c][1]);
+          mma_e4m3(sb, ka.x, kb.x, ka.y, kb.y, ql[c][0], ql[c][1]);
+          mma_e4m3(s[u2], ka.z, kb.z, ka.w, kb.w, qh[c][2], qh[c][3]);
+          mma_e4m3(sb, ka.z, kb.z, ka.w, kb.w, ql[c][2], ql[c][3]);
         }
 #pragma unroll
-        for (int cg = 0; cg < CG; ++cg)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) s[u2][cg][k] += sb[cg][k];
+        for (int k = 0; k < 4; ++k) s[u2][k] += sb[k];
       }
       float kf[BPI], lv[BPI], inv_v[BPI];
 #pragma unroll
@@ -458,57 +441,54 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
       }
       const bool edge = at + BPI * C8_BLOCK - 1 > full_hi || at < full_lo || i + BPI > n_blk;
       const int end = (x.s.first + x.blk + n_blk) * C8_BLOCK;  // of this stretch: the blocks behind it are not its own
-      uint32_t pb[CG][BPI][2];
+      uint32_t pb[BPI][2];
+      float x0 = -INFINITY, x1 = -INFINITY;
 #pragma unroll
-      for (int cg = 0; cg < CG; ++cg) {
-        float x0 = -INFINITY, x1 = -INFINITY;
-#pragma unroll
-        for (int u2 = 0; u2 < BPI; ++u2) {
-          float* v = s[u2][cg];
-          const float k0 = c0[cg] * kf[u2], k1 = c1[cg] * kf[u2];
-          v[0] = fmaf(v[0], k0, lv[u2]);
-          v[1] = fmaf(v[1], k1, lv[u2]);
-          v[2] = fmaf(v[2], k0, lv[u2]);
-          v[3] = fmaf(v[3], k1, lv[u2]);
-          if (edge) {                  // keys that a column does not see: no weight whatever is there
-            const int a = at + u2 * C8_BLOCK + g, h0c = min(pos0[cg], end - 1), h1c = min(pos1[cg], end - 1);
-            const int w0 = p.window > 0 ? pos0[cg] - p.window : -1, w1 = p.window > 0 ? pos1[cg] - p.window : -1;
-            if (a > h0c || a <= w0) v[0] = -INFINITY;
-            if (a > h1c || a <= w1) v[1] = -INFINITY;
-            if (a + 8 > h0c || a + 8 <= w0) v[2] = -INFINITY;
-            if (a + 8 > h1c || a + 8 <= w1) v[3] = -INFINITY;
-          }
-          x0 = fmaxf(x0, fmaxf(v[0], v[2]));
-          x1 = fmaxf(x1, fmaxf(v[1], v[3]));
+      for (int u2 = 0; u2 < BPI; ++u2) {
+        float* v = s[u2];
+        const float k0 = c0 * kf[u2], k1 = c1 * kf[u2];
+        v[0] = fmaf(v[0], k0, lv[u2]);
+        v[1] = fmaf(v[1], k1, lv[u2]);
+        v[2] = fmaf(v[2], k0, lv[u2]);
+        v[3] = fmaf(v[3], k1, lv[u2]);
+        if (edge) {                    // keys that a column does not see: no weight whatever is there
+          const int a = at + u2 * C8_BLOCK + g, h0c = min(pos0, end - 1), h1c = min(pos1, end - 1);
+          const int w0 = p.window > 0 ? pos0 - p.window : -1, w1 = p.window > 0 ? pos1 - p.window : -1;
+          if (a > h0c || a <= w0) v[0] = -INFINITY;
+          if (a > h1c || a <= w1) v[1] = -INFINITY;
+          if (a + 8 > h0c || a + 8 <= w0) v[2] = -INFINITY;
+          if (a + 8 > h1c || a + 8 <= w1) v[3] = -INFINITY;
         }
+        x0 = fmaxf(x0, fmaxf(v[0], v[2]));
+        x1 = fmaxf(x1, fmaxf(v[1], v[3]));
+      }
 #pragma unroll
-        for (int w = 4; w < 32; w <<= 1) {
-          x0 = fmaxf(x0, __shfl_xor_sync(FULL, x0, w));
-          x1 = fmaxf(x1, __shfl_xor_sync(FULL, x1, w));
-        }
-        const float n0 = fmaxf(m0[cg], x0), n1 = fmaxf(m1[cg], x1);
-        // a column that has seen nothing yet keeps its maximum of -inf and weights of 0
-        const float b0 = n0 == -INFINITY ? 0.f : n0, b1 = n1 == -INFINITY ? 0.f : n1;
-        const float f0 = ex2(m0[cg] - b0), f1 = ex2(m1[cg] - b1);
-        const float e0 = b0 - W_SHIFT, e1 = b1 - W_SHIFT;
-        l0[cg] *= f0;
-        l1[cg] *= f1;
-        m0[cg] = n0;
-        m1[cg] = n1;
+      for (int w = 4; w < 32; w <<= 1) {
+        x0 = fmaxf(x0, __shfl_xor_sync(FULL, x0, w));
+        x1 = fmaxf(x1, __shfl_xor_sync(FULL, x1, w));
+      }
+      const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
+      // a column that has seen nothing yet keeps its maximum of -inf and weights of 0
+      const float b0 = n0 == -INFINITY ? 0.f : n0, b1 = n1 == -INFINITY ? 0.f : n1;
+      const float f0 = ex2(m0 - b0), f1 = ex2(m1 - b1);
+      const float e0 = b0 - W_SHIFT, e1 = b1 - W_SHIFT;
+      l0 *= f0;
+      l1 *= f1;
+      m0 = n0;
+      m1 = n1;
 #pragma unroll
-        for (int u2 = 0; u2 < BPI; ++u2) {
-          const float* v = s[u2][cg];
-          const float p0 = ex2(v[0] - e0), p1 = ex2(v[1] - e1), p2 = ex2(v[2] - e0), p3 = ex2(v[3] - e1);
-          l0[cg] = fmaf(p0 + p2, inv_v[u2], l0[cg]);
-          l1[cg] = fmaf(p1 + p3, inv_v[u2], l1[cg]);
-          pb[cg][u2][0] = movm_t(pack_half2(p0, p1));          // keys 0-7 of the block
-          pb[cg][u2][1] = movm_t(pack_half2(p2, p3));          // keys 8-15
-        }
-        if (__any_sync(FULL, f0 != 1.f || f1 != 1.f)) {
+      for (int u2 = 0; u2 < BPI; ++u2) {
+        const float* v = s[u2];
+        const float p0 = ex2(v[0] - e0), p1 = ex2(v[1] - e1), p2 = ex2(v[2] - e0), p3 = ex2(v[3] - e1);
+        l0 = fmaf(p0 + p2, inv_v[u2], l0);
+        l1 = fmaf(p1 + p3, inv_v[u2], l1);
+        pb[u2][0] = movm_t(pack_half2(p0, p1));          // keys 0-7 of the block
+        pb[u2][1] = movm_t(pack_half2(p2, p3));          // keys 8-15
+      }
+      if (__any_sync(FULL, f0 != 1.f || f1 != 1.f)) {
 #pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            o[cg][j][0] *= f0; o[cg][j][1] *= f1; o[cg][j][2] *= f0; o[cg][j][3] *= f1;
-          }
+        for (int j = 0; j < NT; ++j) {
+          o[j][0] *= f0; o[j][1] *= f1; o[j][2] *= f0; o[j][3] *= f1;
         }
       }
 #pragma unroll
@@ -543,11 +523,8 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
           const uint32_t c = __byte_perm(vr[2][w], vr[3][w], 0x5140), d = __byte_perm(vr[2][w], vr[3][w], 0x7362);
           const uint32_t a0 = c8_half2_lo(a), a1 = c8_half2_hi(a), a2 = c8_half2_lo(c), a3 = c8_half2_hi(c);
           const uint32_t b0 = c8_half2_lo(b), b1 = c8_half2_hi(b), b2 = c8_half2_lo(d), b3 = c8_half2_hi(d);
-#pragma unroll
-          for (int cg = 0; cg < CG; ++cg) {
-            mma_f16(o[cg][2 * w], a0, a1, a2, a3, pb[cg][u2][0], pb[cg][u2][1]);
-            mma_f16(o[cg][2 * w + 1], b0, b1, b2, b3, pb[cg][u2][0], pb[cg][u2][1]);
-          }
+          mma_f16(o[2 * w], a0, a1, a2, a3, pb[u2][0], pb[u2][1]);
+          mma_f16(o[2 * w + 1], b0, b1, b2, b3, pb[u2][0], pb[u2][1]);
         }
       }
       __syncwarp();                    // every lane is done with the stage
@@ -557,29 +534,25 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
     }
     cp_async_wait<0>();
 #pragma unroll
-    for (int cg = 0; cg < CG; ++cg)
-#pragma unroll
-      for (int w = 4; w < 32; w <<= 1) {
-        l0[cg] += __shfl_xor_sync(FULL, l0[cg], w);
-        l1[cg] += __shfl_xor_sync(FULL, l1[cg], w);
-      }
+    for (int w = 4; w < 32; w <<= 1) {
+      l0 += __shfl_xor_sync(FULL, l0, w);
+      l1 += __shfl_xor_sync(FULL, l1, w);
+    }
     // lane (g, t) holds columns 2t ([0], [2]) and 2t + 1 ([1], [3]) at dims dim_of(j, g) and the one behind it
     const bool starts = x.blk == 0, ends = x.blk + n_blk == x.s.n;
     if (starts && ends && !p.cluster) {
 #pragma unroll
-      for (int cg = 0; cg < CG; ++cg)
+      for (int hh = 0; hh < 2; ++hh) {
+        const int k = 2 * t + hh;
+        if (k >= cols) continue;
+        const int i = (col0 + k) / p.G, h = col0 + k - i * p.G;
+        const float l = hh ? l1 : l0, inv = l == 0.f ? 0.f : 1.f / l;
+        bf16* dst = p.out + (int64_t)(x.s.row0 + i) * p.ldo + (int64_t)(h0 + h) * HD;
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          const int k = cg * 8 + 2 * t + hh;
-          if (k >= cols) continue;
-          const int i = (col0 + k) / p.G, h = col0 + k - i * p.G;
-          const float l = hh ? l1[cg] : l0[cg], inv = l == 0.f ? 0.f : 1.f / l;
-          bf16* dst = p.out + (int64_t)(x.s.row0 + i) * p.ldo + (int64_t)(h0 + h) * HD;
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-            *reinterpret_cast<__nv_bfloat162*>(dst + dim_of<HD>(j, g)) =
-                __floats2bfloat162_rn(o[cg][j][hh] * inv, o[cg][j][2 + hh] * inv);
-        }
+        for (int j = 0; j < NT; ++j)
+          *reinterpret_cast<__nv_bfloat162*>(dst + dim_of<HD>(j, g)) =
+              __floats2bfloat162_rn(o[j][hh] * inv, o[j][2 + hh] * inv);
+      }
     } else {
       // for the CTA's merge over the ring, which every lane has left; else to the workspace
       const bool local = p.cluster || inside;
@@ -588,18 +561,15 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
                         : p.partial + (((int64_t)blockIdx.x * WARPS + warp) * 2 + (starts ? 1 : 0)) * C::PSLOT;
       stored = local;
       __syncwarp();
+      if (g == 0) {
+        sl[2 * t] = m0; sl[2 * t + 1] = m1;
+        sl[NC + 2 * t] = l0; sl[NC + 2 * t + 1] = l1;
+      }
+      float* so = sl + 2 * NC + 2 * t * cs + 2 * g;
 #pragma unroll
-      for (int cg = 0; cg < CG; ++cg) {
-        if (g == 0) {
-          sl[cg * 8 + 2 * t] = m0[cg]; sl[cg * 8 + 2 * t + 1] = m1[cg];
-          sl[NC + cg * 8 + 2 * t] = l0[cg]; sl[NC + cg * 8 + 2 * t + 1] = l1[cg];
-        }
-        float* so = sl + 2 * NC + (cg * 8 + 2 * t) * cs + 2 * g;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          *reinterpret_cast<float2*>(so + 16 * j) = make_float2(o[cg][j][0], o[cg][j][2]);
-          *reinterpret_cast<float2*>(so + cs + 16 * j) = make_float2(o[cg][j][1], o[cg][j][3]);
-        }
+      for (int j = 0; j < NT; ++j) {
+        *reinterpret_cast<float2*>(so + 16 * j) = make_float2(o[j][0], o[j][2]);
+        *reinterpret_cast<float2*>(so + cs + 16 * j) = make_float2(o[j][1], o[j][3]);
       }
     }
     left -= n_blk;
@@ -701,9 +671,9 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD, CG>::PER_SM) dec8_kernel(co
 // kernel, so it finds the same places. With few pieces every lane takes a pair of dims; with many, four neighbouring pairs (a
 // 32-byte sector) go to four lanes, eight pieces at a time.
 constexpr int MERGE_WARPS = 4;
-template <int HD, int CG>
+template <int HD>
 __global__ void __launch_bounds__(MERGE_WARPS * 32) dec8_merge_kernel(const __grid_constant__ Dec8Dev p) {
-  using C = D8<HD, CG>;
+  using C = D8<HD>;
   constexpr int NC = C::NC;
   extern __shared__ __align__(16) int prefix[];
   __shared__ int warp_sums[WARPS];
@@ -777,9 +747,35 @@ __global__ void __launch_bounds__(MERGE_WARPS * 32) dec8_merge_kernel(const __gr
   }
 }
 
-template <int HD, int CG>
+// Clusters of n CTAs that the GPU holds at once (of the device that was current at the first call): fewer than its SMs
+// would give, since a cluster lies within one group of SMs
+template <int HD>
+int max_clusters(int n) {
+  using C = D8<HD>;
+  static std::atomic<int> known[9];
+  int most = known[n].load(std::memory_order_relaxed);
+  if (most > 0) return most - 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(n);
+  cfg.blockDim = dim3(WARPS * 32);
+  cfg.dynamicSmemBytes = C::SMEM;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeClusterDimension;
+  attr.val.clusterDim.x = n;
+  attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&most, dec8_kernel<HD>, &cfg) != cudaSuccess) {
+    cudaGetLastError();                          // no GPU: no clusters
+    return 0;
+  }
+  known[n].store(most + 1, std::memory_order_relaxed);
+  return most;
+}
+
+template <int HD>
 int launch_t(const Attn8Args& a, Dec8Dev& p, cudaStream_t s) {
-  using C = D8<HD, CG>;
+  using C = D8<HD>;
   p.chunks = (int)(((int64_t)a.rows * p.G + C::NC - 1) / C::NC);
   const int span = p.window > 0 && (int64_t)p.window + a.rows + C8_BLOCK < a.kv_len ? p.window + a.rows + C8_BLOCK : a.kv_len;
   const int64_t blocks = ((int64_t)span + C8_BLOCK - 1) / C8_BLOCK, items = (int64_t)a.batch * a.n_kv * p.chunks;
@@ -788,10 +784,15 @@ int launch_t(const Attn8Args& a, Dec8Dev& p, cudaStream_t s) {
       (int64_t)a.c.num_pages * a.n_kv > 0x7fffffff / (a.c.page_size / C8_BLOCK))
     return POP_E_INVALID;
   const int ctas = device_sms() * C::PER_SM;
+  static std::atomic<uint64_t> configured{0};
+  const bool ready =                             // asked before the clusters are; counts when the kernel is launched
+      c8_allow_smem(configured, reinterpret_cast<const void*>(dec8_kernel<HD>), C::SMEM + (MAX_BATCH + 1) * 4);
   // Clusters (one launch): one CTA per item while its warps have few blocks each; more per item while all of them are
-  // resident at once and no warp gets more than CLUSTER_BLOCKS blocks.
+  // resident at once and no warp gets more than CLUSTER_BLOCKS blocks. Against the line, hd 128: 1 x 8192 positions 11.0
+  // against 14.5 us, 1 x 2000 7.0 / 14.2, 9 x 2000 13.0 / 21.2, 18 x 400 7.4 / 14.6; and 2 x 8192 with clusters of 8, which are
+  // not all resident, 21.2 against 16.5 with those of 4.
   int cs = 1;
-  while (cs < 8 && blocks > (int64_t)cs * WARPS * 2 && items * cs * 2 <= ctas) cs *= 2;
+  while (cs < 8 && blocks > (int64_t)cs * WARPS * 2 && items <= max_clusters<HD>(cs * 2)) cs *= 2;
   p.cluster = blocks <= (int64_t)cs * WARPS * CLUSTER_BLOCKS && (cs > 1 || blocks <= WARPS * 4) ? cs : 0;
   int64_t grid = items * cs;
   if (!p.cluster) {
@@ -803,20 +804,18 @@ int launch_t(const Attn8Args& a, Dec8Dev& p, cudaStream_t s) {
   }
   p.status = status_word();
   if (!p.status) return POP_E_CUDA;
+  if (!ready) return POP_E_CUDA;
   const int scan_bytes = p.cluster ? 0 : (a.batch + 1) * 4;
-  static std::atomic<uint64_t> configured{0};
-  if (!c8_allow_smem(configured, reinterpret_cast<const void*>(dec8_kernel<HD, CG>), C::SMEM + (MAX_BATCH + 1) * 4))
-    return POP_E_CUDA;
   ProfScope prof(PROF_DECODE_ATTN, (double)a.batch * span * a.n_kv * (2.0 * HD + 0.125), s);
   const size_t smem = (size_t)(C::SMEM + scan_bytes);
   const cudaError_t rc = p.cluster > 1
-                             ? launch_chained_cluster_x(dec8_kernel<HD, CG>, dim3((unsigned)grid), dim3(WARPS * 32), smem, s,
+                             ? launch_chained_cluster_x(dec8_kernel<HD>, dim3((unsigned)grid), dim3(WARPS * 32), smem, s,
                                                         (unsigned)p.cluster, p)
-                             : launch_chained(dec8_kernel<HD, CG>, dim3((unsigned)grid), dim3(WARPS * 32), smem, s, p);
+                             : launch_chained(dec8_kernel<HD>, dim3((unsigned)grid), dim3(WARPS * 32), smem, s, p);
   if (rc != cudaSuccess) return POP_E_CUDA;
   count_launch();
   if (!p.cluster) {
-    if (launch_chained(dec8_merge_kernel<HD, CG>, dim3((unsigned)grid * WARPS), dim3(MERGE_WARPS * 32), (size_t)scan_bytes, s, p) !=
+    if (launch_chained(dec8_merge_kernel<HD>, dim3((unsigned)grid * WARPS), dim3(MERGE_WARPS * 32), (size_t)scan_bytes, s, p) !=
         cudaSuccess)
       return POP_E_CUDA;
     count_launch();
@@ -837,13 +836,10 @@ int launch_few8(const Attn8Args& a, cudaStream_t s) {
   p.batch = a.batch; p.n_q = a.n_q; p.n_kv = a.n_kv; p.G = a.n_q / a.n_kv;
   p.partial = static_cast<float*>(a.workspace);
   p.scale_log2 = 1.4426950408889634f / sqrtf((float)a.head_dim);
-  // two column groups per item where there are more than eight columns: the keys are read from memory once for both. Not
-  // for hd 256, whose accumulators alone would fill the registers.
-  const bool wide = (int64_t)a.rows * p.G > 8;
   switch (a.head_dim) {
-    case 64: return wide ? launch_t<64, 2>(a, p, s) : launch_t<64, 1>(a, p, s);
-    case 128: return wide ? launch_t<128, 2>(a, p, s) : launch_t<128, 1>(a, p, s);
-    default: return launch_t<256, 1>(a, p, s);
+    case 64: return launch_t<64>(a, p, s);
+    case 128: return launch_t<128>(a, p, s);
+    default: return launch_t<256>(a, p, s);
   }
 }
 
