@@ -19,7 +19,7 @@
 // fp32. The 8-bit MMA runs at 3.5 times the f16 one's rate and needs no conversion.
 //
 // Who takes what:
-//   - few items (a small batch): a thread-block cluster of 1, 2, 4 or 8 CTAs per item, its blocks dealt to the warps in
+//   - few items or short ones: a thread-block cluster of 1, 2, 4 or 8 CTAs per item, its blocks dealt to the warps in
 //     equal stretches, the pieces merged in shared memory and over the cluster's. One launch.
 //   - else all items form one line of blocks and every warp of a full GPU takes an equal stretch of it, whatever the
 //     lengths are. An item that a warp has whole is finished by it; the pieces of the others go through the workspace to a
@@ -43,7 +43,7 @@ constexpr uint32_t FULL = 0xffffffffu;
 constexpr int WARPS = 8;
 constexpr int MAX_BATCH = 4096;      // the block counts' prefix sums sit in shared memory
 constexpr float W_SHIFT = 14.f;      // weights are stored times 2^14
-constexpr int CLUSTER_BLOCKS = 16;   // cluster form: blocks per warp at most
+constexpr int CLUSTER_BLOCKS = 16;   // one-launch form: blocks per warp at most
 
 template <int HD>
 struct D8 {
@@ -787,13 +787,15 @@ int launch_t(const Attn8Args& a, Dec8Dev& p, cudaStream_t s) {
   static std::atomic<uint64_t> configured{0};
   const bool ready =                             // asked before the clusters are; counts when the kernel is launched
       c8_allow_smem(configured, reinterpret_cast<const void*>(dec8_kernel<HD>), C::SMEM + (MAX_BATCH + 1) * 4);
-  // Clusters (one launch): one CTA per item while its warps have few blocks each; more per item while all of them are
-  // resident at once and no warp gets more than CLUSTER_BLOCKS blocks. Against the line, hd 128: 1 x 8192 positions 11.0
-  // against 14.5 us, 1 x 2000 7.0 / 14.2, 9 x 2000 13.0 / 21.2, 18 x 400 7.4 / 14.6; and 2 x 8192 with clusters of 8, which are
-  // not all resident, 21.2 against 16.5 with those of 4.
+  // One launch, a CTA or a cluster per item, where no warp gets more than CLUSTER_BLOCKS blocks and the CTAs are resident
+  // at once; two rounds of CTAs pay up to eight blocks per warp, any number up to four. Against the line and its second
+  // launch, hd 128, 8 kv heads (us): 1 x 8192 positions 11.0 / 14.5, 1 x 2000 7.0 / 14.2, 9 x 2000 13.0 / 21.2, 18 x 1000 12.2
+  // / 19.9, 18 x 2000 17.8 / 26.1; two rounds 20 x 1000 19.7 / 20.0 (unequal lengths 13.0 / 16.4), 30 x 1000 21.6 / 23.3, but 20 x
+  // 2000 29.7 / 27.2. And 2 x 8192 in clusters of 8, which are not all resident, 21.2 against 16.5 in those of 4.
   int cs = 1;
   while (cs < 8 && blocks > (int64_t)cs * WARPS * 2 && items <= max_clusters<HD>(cs * 2)) cs *= 2;
-  p.cluster = blocks <= (int64_t)cs * WARPS * CLUSTER_BLOCKS && (cs > 1 || blocks <= WARPS * 4) ? cs : 0;
+  const bool one_launch = cs > 1 || items <= ctas || blocks <= WARPS * 4 || (items <= 2 * ctas && blocks <= WARPS * 8);
+  p.cluster = one_launch && blocks <= (int64_t)cs * WARPS * CLUSTER_BLOCKS ? cs : 0;
   int64_t grid = items * cs;
   if (!p.cluster) {
     if (a.batch > MAX_BATCH) return POP_E_INVALID;

@@ -748,3 +748,22 @@ def test_outputs_on_boundaries_of_16_bytes(L, hd, rows, lead, pad):
     assert L.status() == 0
     assert (whole[:, :lead] == 5.0).all() and (whole[:, lead + n_q * hd:] == 5.0).all()
     check_attention(q[:, lead:lead + n_q * hd], out.cpu(), cache, [rows], [length], n_q, n_kv, hd, 0, pick=1)
+
+
+LINE = [  # rows, lens, n_q, n_kv, hd, page, window: more items than the GPU takes at once, cut into equal stretches
+    ([1] * 90, spread(90, 0, 1400), 4, 2, 128, 16, 0), ([2] * 80, [x + 1 for x in spread(80, 0, 1500)], 16, 4, 64, 32, 0),
+    ([3, 0, 2, 1] * 12, [x + 3 for x in spread(48, 0, 1400)], 16, 2, 128, 128, 0), ([1] * 44, spread(44, 0, 1300), 8, 4, 256, 64, 0),
+    ([4, 0, 1] * 15, [x + 2 for x in spread(45, 0, 2500)], 8, 2, 256, 16, 1200), ([1] * 30, spread(30, 1, 2600), 7, 7, 128, 64, 0),
+]
+
+
+@pytest.mark.parametrize("rows,lens,n_q,n_kv,hd,page,window", LINE, ids=lambda v: str(v)[:24])
+def test_few_rows_of_many_sequences(L, rows, lens, n_q, n_kv, hd, page, window):
+    cache = random_cache(170, 1, len(lens), max(lens), n_kv, hd, page)
+    poison_behind(cache, lens)
+    decode = set(rows) == {1}
+    q, out = run_rows(L, cache, rows, lens, n_q, n_kv, hd, window, 171, decode)
+    assert L.status() == 0
+    check_attention(q, out.cpu(), cache, rows, lens, n_q, n_kv, hd, window, decode=decode)
+    again = run_rows(L, cache, rows, lens, n_q, n_kv, hd, window, 171, decode)[1]
+    assert torch.equal(out, again)
