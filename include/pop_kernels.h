@@ -199,7 +199,8 @@ int pop_k_decode_attention_static(const void* q, int64_t ldq, const void* k_pool
  * make it 2^120), a code is value / s rounded to nearest even, saturating at 448 (NaN stays NaN). hd is 64, 128 or 256.
  * Device-side checks in every call: a block-table entry outside [0, num_pages), a length above the stated maximum, a
  * rotation row outside the table are never turned into addresses; the status word is raised to POP_E_INVALID and what
- * depends on them is not written or reads as zeros. Lengths (kv_len) go up to 2^31 - 2^16. The codes behind a sequence's last position are left as they are.
+ * depends on them is not written or reads as zeros. Lengths (kv_len) go up to 2^31 - 2^16. The codes behind a sequence's
+ * last position are left as they are.
  *
  * pop_k_quant_cache_e4m3: the bf16 cache that a prefill left, for `layers` consecutive layers (src_layer_stride elements,
  *   code_layer_stride and scale_layer_stride bytes apart), positions 0 .. n-1 of every sequence, n = seq_lens[b] (device
@@ -220,8 +221,8 @@ int pop_k_quant_cache_e4m3(const void* k_pool, const void* v_pool, int64_t src_l
  * v to the cache.
  *   Rotation: pair (j, j + hd/2) turns by rope_table[p][j] = (cos, sin), float2 [table_rows][hd/2]. p is the cache position
  * if positions is NULL, else positions[axis * ld_pos + row] (device int32 [n_axes][ld_pos], row = packed row) with axis =
- * pair_axis[j] (device uint8 [hd/2], 4-byte aligned, values < n_axes; NULL: axis 0): time, height and width of image and video tokens,
- * in sections or interleaved as the model has it.
+ * pair_axis[j] (device uint8 [hd/2], 4-byte aligned, values < n_axes; NULL: axis 0): time, height and width of image and
+ * video tokens, in sections or interleaved as the model has it.
  *   Scales: a block whose 16 positions all come from this call, or whose earlier positions are all new, gets the scale of its
  * rows. A block that holds earlier positions (start not a multiple of 16) keeps the larger of its scale and the one the new
  * rows need, and its codes are brought to it. Positions at or behind `start` count as empty, whatever is there: a sequence

@@ -120,8 +120,9 @@ __global__ void __launch_bounds__(256, HD == 256 ? 2 : 4) quant_cache8_kernel(co
 // Two warps per (sequence, block of 16 cache positions that the new rows touch, head), eight slots each. hd / 8 lanes take
 // one row, each four rotation pairs (j, j + hd/2): two 16-byte loads of fp32 (8-byte of bf16). The rows stay in registers
 // until the block's maximum is known, which the two warps exchange (one warp for all 16 rows: 128 registers, 72 us for 6656
-// rows of 32 + 16 heads; two warps at four CTAs per SM 57; the bytes take 35). A CTA is four heads of the same rows, so the rotary rows come from L1 after the
-// first.
+// rows of 32 + 16 heads; two warps at four CTAs per SM 57 us, 4.0 TB/s; the bytes take 35). Bound by the loads that the
+// resident warps keep in flight; one token alone takes 2.8 us, launch and dependent loads. A CTA is four heads of the same
+// rows, so the rotary rows come from L1 after the first.
 struct Append8Dev {
   Append8Args a;
   int head_groups;              // CTAs per block of positions: four heads each
