@@ -378,7 +378,7 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
 #pragma unroll
       for (int o = LPR / 2; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(0xffffffffu, am, o));
       const int eb = max((int)(__float_as_uint(am) >> 23), 20);
-      const float mul = c8_pow2(134 - eb);
+      const float mul = eb == 255 ? NAN : c8_pow2(134 - eb);      // an infinite element makes the row NaN, as its softmax is
       if (c == 0) s.crow[r] = c8_pow2(eb - 134) * p.scale_log2;
 #pragma unroll
       for (int k = 0; k < 4; k += 2) {
@@ -873,6 +873,7 @@ int launch_attention8(const Attn8Args& a, cudaStream_t s) {
     return POP_E_INVALID;
   if (reinterpret_cast<uintptr_t>(a.workspace) % 16 || (int64_t)a.batch * a.rows > 0x7fffffff) return POP_E_INVALID;
   if (!a.seq_lens && a.rows > a.kv_len) return POP_E_INVALID;
+  if ((int64_t)a.batch * a.rows > 1 && a.ldo < (int64_t)a.n_q * a.head_dim) return POP_E_INVALID;     // rows over each other
   // rows of the pool are 32-bit coordinates
   if (a.c.num_pages * (int64_t)a.n_kv > 0x7ffffff0 / a.c.page_size) return POP_E_INVALID;
   if ((int64_t)a.kv_len > (int64_t)a.c.max_pages * a.c.page_size) return POP_E_NOSPACE;

@@ -367,6 +367,7 @@ int launch_append8(const Append8Args& a, cudaStream_t s) {
   if (!aligned(a.in, 16) || !aligned(a.table, 16) || a.ld_in % 4 || (a.n_q > 0 && (!aligned(a.q_out, 8) || a.ldq % 4)))
     return POP_E_INVALID;
   if ((int64_t)a.batch * a.rows > 0x7fffffff) return POP_E_INVALID;
+  if (a.n_q > 0 && (int64_t)a.batch * a.rows > 1 && a.ldq < (int64_t)a.n_q * a.head_dim) return POP_E_INVALID;
   if (a.start == nullptr && (int64_t)a.pos0 + a.rows > (int64_t)a.dst.max_pages * a.dst.page_size) return POP_E_NOSPACE;
   if (a.rows == 0) return POP_OK;
   Append8Dev p{};

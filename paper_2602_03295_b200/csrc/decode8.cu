@@ -374,7 +374,8 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD>::PER_SM) dec8_kernel(const 
     am = fmaxf(am, __shfl_xor_sync(FULL, am, 1));
     am = fmaxf(am, __shfl_xor_sync(FULL, am, 2));
     const int eb = max((int)(__float_as_uint(am) >> 23), 20);
-    const float mul = live ? c8_pow2(134 - eb) : 0.f, inv = c8_pow2(eb - 134) * p.scale_log2;
+    // an infinite element makes the column NaN, as its softmax is
+    const float mul = !live ? 0.f : eb == 255 ? NAN : c8_pow2(134 - eb), inv = c8_pow2(eb - 134) * p.scale_log2;
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
 #pragma unroll
@@ -854,6 +855,7 @@ int launch_decode_attention8(const Attn8Args& a, cudaStream_t s) {
   if (reinterpret_cast<uintptr_t>(a.q) % 16 || reinterpret_cast<uintptr_t>(a.out) % 16 || a.ldq % 8 || a.ldo % 8 ||
       reinterpret_cast<uintptr_t>(a.workspace) % 16)
     return POP_E_INVALID;
+  if (a.batch > 1 && a.ldo < (int64_t)a.n_q * a.head_dim) return POP_E_INVALID;       // rows over each other
   if ((int64_t)a.kv_len > (int64_t)a.c.max_pages * a.c.page_size) return POP_E_NOSPACE;
   return launch_few8(a, s);
 }

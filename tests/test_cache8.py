@@ -131,3 +131,11 @@ def test_lengths_and_windows_behind_the_largest_are_refused(library, op):
     name, args = CALLS[op]
     for change in (dict(kv_len=0x7fff0001), dict(window=0x7ffffff1)):
         assert getattr(library.dll, name)(*{**args, "max_pages": 1 << 28, **change}.values()) == POP_E_INVALID
+
+
+def test_output_rows_over_each_other_are_refused(library):
+    from paper_2602_03295_b200 import POP_E_INVALID
+    dll = library.dll
+    assert dll.pop_k_decode_attention_e4m3(*{**DECODE, "batch": 2, "ldo": 56}.values()) == POP_E_INVALID
+    assert dll.pop_k_attention_e4m3(*{**PROMPT, "max_rows": 2, "ldo": 0}.values()) == POP_E_INVALID
+    assert dll.pop_k_rope_cache_e4m3(*{**APPEND, "max_rows": 2, "ldq": 60}.values()) == POP_E_INVALID

@@ -767,3 +767,48 @@ def test_few_rows_of_many_sequences(L, rows, lens, n_q, n_kv, hd, page, window):
     check_attention(q, out.cpu(), cache, rows, lens, n_q, n_kv, hd, window, decode=decode)
     again = run_rows(L, cache, rows, lens, n_q, n_kv, hd, window, 171, decode)[1]
     assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("hd,rows", [(64, 1), (128, 1), (256, 1), (128, 40), (256, 70)])
+def test_infinite_and_nan_queries_stay_in_their_rows(L, hd, rows):
+    """A query with an infinity or a NaN has no softmax: its output is NaN, as that of a row that sees nothing is zeros."""
+    n_q, n_kv, length = 4, 2, 300
+    cache = random_cache(180, 1, 1, length, n_kv, hd, 64)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    q = queries(181, rows, n_q, hd)
+    ln = torch.tensor([length], dtype=torch.int32, device=DEV)
+    clean, out = torch.empty_like(q, device=DEV), torch.empty_like(q, device=DEV)
+    L.attention_e4m3(q.to(DEV), *dev, clean, n_q, n_kv, hd, rows, length, seq_lens=ln)
+    bad = q.clone().view(rows, n_q, hd)
+    bad[0, 0, 3], bad[0, 2, hd - 1], bad[rows - 1, 3, 0] = math.inf, -math.inf, math.nan
+    L.attention_e4m3(bad.view(rows, -1).to(DEV), *dev, out, n_q, n_kv, hd, rows, length, seq_lens=ln)
+    assert L.status() == 0
+    hit = ~torch.isfinite(bad).all(-1).to(DEV)
+    got, want = out.view(rows, n_q, hd), clean.view(rows, n_q, hd)
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], want[~hit])
+
+
+def test_first_call_of_a_process_may_be_captured():
+    import subprocess
+    import sys
+    code = """
+import torch, paper_2602_03295_b200 as pk
+L, dev = pk.lib(), "cuda"
+k8 = torch.zeros(4, 2, 64, 128, dtype=torch.uint8, device=dev); v8 = torch.full_like(k8, 0x38)
+ks = torch.full((4, 2, 4), 127, dtype=torch.uint8, device=dev); vs = ks.clone()
+table = torch.arange(4, dtype=torch.int32, device=dev)[None]
+q, outs = torch.ones(1, 512, dtype=torch.bfloat16, device=dev), []
+big = torch.ones(100, 512, dtype=torch.bfloat16, device=dev)
+ws = torch.empty(pk.binding.POP_E4M3_WORKSPACE_BYTES, dtype=torch.uint8, device=dev)
+o1, o2 = torch.zeros_like(q), torch.zeros_like(big)
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    L.decode_attention_e4m3(q, k8, v8, ks, vs, table, o1, 4, 2, 128, 256, workspace=ws)
+    L.attention_e4m3(big, k8, v8, ks, vs, table, o2, 4, 2, 128, 100, 256, workspace=ws)
+g.replay(); torch.cuda.synchronize()
+assert L.status() == 0 and (o1 == 1).all() and (o2 == 1).all()
+print("captured")
+"""
+    got = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert "captured" in got.stdout, got.stderr[-2000:]
