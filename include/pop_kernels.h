@@ -243,8 +243,8 @@ int pop_k_rope_cache_e4m3(const void* in, int32_t in_bf16, int64_t ld_in, const 
 /* pop_k_decode_attention over the 8-bit cache, with a length per sequence: one query per sequence at position
  * len - 1, len = seq_lens[b] (device int32 [batch], each <= kv_len) or kv_len for all if seq_lens is NULL, over the last
  * `window` positions (0: all). q bf16 [batch][ldq], out bf16 [batch][ldo] (strides multiples of 8, ldo >= n_q hd, 16-byte aligned), any
- * n_q that is a multiple of n_kv. A sequence of length 0 gets a row of zeros. batch <= 4096. Work is split evenly over the
- * GPU whatever the lengths are; results do not depend on scheduling. */
+ * n_q that is a multiple of n_kv. A sequence of length 0 gets a row of zeros. batch <= 4096. Unequal
+ * lengths are shared out over the whole GPU; results do not depend on scheduling. */
 int pop_k_decode_attention_e4m3(const void* q, int64_t ldq, const void* k_codes, const void* v_codes,
                                 const void* k_scales, const void* v_scales, const int32_t* block_table,
                                 int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq,
