@@ -117,11 +117,69 @@ __global__ void __launch_bounds__(256, HD == 256 ? 2 : 4) quant_cache8_kernel(co
 }
 
 // ------------------------------------------------------------------------------ norm + rotation + append
+// Elements j0 .. j0 + 3 of a head's row into x[0..3], their rotation partners j0 + hd/2 .. into x[4..7]
+template <int HD, bool IN_BF16>
+__device__ __forceinline__ void load_row8(const void* in, int64_t off, float (&x)[8]) {
+  if constexpr (IN_BF16) {
+    const uint2 l = __ldg(reinterpret_cast<const uint2*>(static_cast<const bf16*>(in) + off));
+    const uint2 m = __ldg(reinterpret_cast<const uint2*>(static_cast<const bf16*>(in) + off + HD / 2));
+    unpack_bf16x2(l.x, x[0], x[1]);
+    unpack_bf16x2(l.y, x[2], x[3]);
+    unpack_bf16x2(m.x, x[4], x[5]);
+    unpack_bf16x2(m.y, x[6], x[7]);
+  } else {
+    const float4 l = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(in) + off));
+    const float4 m = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(in) + off + HD / 2));
+    x[0] = l.x; x[1] = l.y; x[2] = l.z; x[3] = l.w;
+    x[4] = m.x; x[5] = m.y; x[6] = m.z; x[7] = m.w;
+  }
+}
+// RMSNorm over the row that hd / 8 lanes hold, by all lanes of the warp
+template <int HD>
+__device__ __forceinline__ void norm_row8(float (&x)[8], float4 g0, float4 g1, float eps) {
+  float ss = 0.f;
+#pragma unroll
+  for (int u = 0; u < 8; ++u) ss = fmaf(x[u], x[u], ss);
+#pragma unroll
+  for (int o = HD / 16; o > 0; o >>= 1) ss += __shfl_xor_sync(FULL, ss, o);
+  const float rstd = rsqrtf(ss / (float)HD + eps);
+  x[0] = x[0] * rstd * g0.x; x[1] = x[1] * rstd * g0.y;
+  x[2] = x[2] * rstd * g0.z; x[3] = x[3] * rstd * g0.w;
+  x[4] = x[4] * rstd * g1.x; x[5] = x[5] * rstd * g1.y;
+  x[6] = x[6] * rstd * g1.z; x[7] = x[7] * rstd * g1.w;
+}
+__device__ __forceinline__ void turn_row8(float (&x)[8], const float2 (&cs)[4]) {
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const float c = x[u] * cs[u].x - x[u + 4] * cs[u].y;
+    const float d = x[u + 4] * cs[u].x + x[u] * cs[u].y;
+    x[u] = c;
+    x[u + 4] = d;
+  }
+}
+template <int HD>
+__device__ __forceinline__ void store_q8(bf16* dst, const float (&x)[8]) {
+  __nv_bfloat162 w0 = __floats2bfloat162_rn(x[0], x[1]), w1 = __floats2bfloat162_rn(x[2], x[3]);
+  __nv_bfloat162 w2 = __floats2bfloat162_rn(x[4], x[5]), w3 = __floats2bfloat162_rn(x[6], x[7]);
+  uint2 o;
+  o.x = *reinterpret_cast<uint32_t*>(&w0); o.y = *reinterpret_cast<uint32_t*>(&w1);
+  *reinterpret_cast<uint2*>(dst) = o;
+  o.x = *reinterpret_cast<uint32_t*>(&w2); o.y = *reinterpret_cast<uint32_t*>(&w3);
+  *reinterpret_cast<uint2*>(dst + HD / 2) = o;
+}
+// four codes times a power of two, rounded again
+__device__ __forceinline__ uint32_t rescaled4(uint32_t w, float f) {
+  const uint32_t l = c8_half2_lo(w), m = c8_half2_hi(w);
+  const float2 v0 = __half22float2(*reinterpret_cast<const __half2*>(&l));
+  const float2 v1 = __half22float2(*reinterpret_cast<const __half2*>(&m));
+  return c8_codes4(v0.x * f, v0.y * f, v1.x * f, v1.y * f);
+}
+
 // Two warps per (sequence, block of 16 cache positions that the new rows touch, head), eight slots each. hd / 8 lanes take
 // one row, each four rotation pairs (j, j + hd/2): two 16-byte loads of fp32 (8-byte of bf16). The rows stay in registers
 // until the block's maximum is known, which the two warps exchange (one warp for all 16 rows: 128 registers, 72 us for 6656
 // rows of 32 + 16 heads; two warps at four CTAs per SM 57 us, 4.0 TB/s; the bytes take 35). Bound by the loads that the
-// resident warps keep in flight; one token alone takes 2.8 us, launch and dependent loads. A CTA is four heads of the same
+// resident warps keep in flight. A CTA is four heads of the same
 // rows, so the rotary rows come from L1 after the first.
 struct Append8Dev {
   Append8Args a;
@@ -172,19 +230,7 @@ __global__ void __launch_bounds__(256, HD == 256 ? 2 : 4) append8_kernel(const _
     for (int u = 0; u < 8; ++u) x[i][u] = 0.f;
     if (s < lo || s >= hi) continue;
     const int64_t off = (r_base + s) * a.ld_in + (int64_t)h * HD + j0;
-    if constexpr (IN_BF16) {
-      const uint2 l = __ldg(reinterpret_cast<const uint2*>(static_cast<const bf16*>(a.in) + off));
-      const uint2 m = __ldg(reinterpret_cast<const uint2*>(static_cast<const bf16*>(a.in) + off + HALF));
-      unpack_bf16x2(l.x, x[i][0], x[i][1]);
-      unpack_bf16x2(l.y, x[i][2], x[i][3]);
-      unpack_bf16x2(m.x, x[i][4], x[i][5]);
-      unpack_bf16x2(m.y, x[i][6], x[i][7]);
-    } else {
-      const float4 l = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(a.in) + off));
-      const float4 m = __ldg(reinterpret_cast<const float4*>(static_cast<const float*>(a.in) + off + HALF));
-      x[i][0] = l.x; x[i][1] = l.y; x[i][2] = l.z; x[i][3] = l.w;
-      x[i][4] = m.x; x[i][5] = m.y; x[i][6] = m.z; x[i][7] = m.w;
-    }
+    load_row8<HD, IN_BF16>(a.in, off, x[i]);
   }
   if (!is_v) {
     int axis[4] = {0, 0, 0, 0};
@@ -238,35 +284,9 @@ __global__ void __launch_bounds__(256, HD == 256 ? 2 : 4) append8_kernel(const _
           for (int u = 1; u < 4; ++u) cs[u] = __ldg(row_of(__ldg(a.positions + axis[u] * a.ld_pos + r_base + s)) + u);
         }
       }
-      if (gain != nullptr) {
-        float ss = 0.f;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) ss = fmaf(x[i][u], x[i][u], ss);
-#pragma unroll
-        for (int o = LPR / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(FULL, ss, o);
-        const float rstd = rsqrtf(ss / (float)HD + a.eps);
-        x[i][0] = x[i][0] * rstd * g0.x; x[i][1] = x[i][1] * rstd * g0.y;
-        x[i][2] = x[i][2] * rstd * g0.z; x[i][3] = x[i][3] * rstd * g0.w;
-        x[i][4] = x[i][4] * rstd * g1.x; x[i][5] = x[i][5] * rstd * g1.y;
-        x[i][6] = x[i][6] * rstd * g1.z; x[i][7] = x[i][7] * rstd * g1.w;
-      }
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const float c = x[i][u] * cs[u].x - x[i][u + 4] * cs[u].y;
-        const float d = x[i][u + 4] * cs[u].x + x[i][u] * cs[u].y;
-        x[i][u] = c;
-        x[i][u + 4] = d;
-      }
-      if (is_q && live) {
-        bf16* dst = a.q_out + (r_base + s) * a.ldq + (int64_t)h * HD + j0;
-        __nv_bfloat162 w0 = __floats2bfloat162_rn(x[i][0], x[i][1]), w1 = __floats2bfloat162_rn(x[i][2], x[i][3]);
-        __nv_bfloat162 w2 = __floats2bfloat162_rn(x[i][4], x[i][5]), w3 = __floats2bfloat162_rn(x[i][6], x[i][7]);
-        uint2 o;
-        o.x = *reinterpret_cast<uint32_t*>(&w0); o.y = *reinterpret_cast<uint32_t*>(&w1);
-        *reinterpret_cast<uint2*>(dst) = o;
-        o.x = *reinterpret_cast<uint32_t*>(&w2); o.y = *reinterpret_cast<uint32_t*>(&w3);
-        *reinterpret_cast<uint2*>(dst + HALF) = o;
-      }
+      if (gain != nullptr) norm_row8<HD>(x[i], g0, g1, a.eps);
+      turn_row8(x[i], cs);
+      if (is_q && live) store_q8<HD>(a.q_out + (r_base + s) * a.ldq + (int64_t)h * HD + j0, x[i]);
     }
   }
   // the other half of the block's rows is in the neighbouring warp
@@ -299,10 +319,7 @@ __global__ void __launch_bounds__(256, HD == 256 ? 2 : 4) append8_kernel(const _
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           uint32_t* w = reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD + half * HALF);
-          const uint32_t l = c8_half2_lo(*w), m = c8_half2_hi(*w);
-          const float2 v0 = __half22float2(*reinterpret_cast<const __half2*>(&l));
-          const float2 v1 = __half22float2(*reinterpret_cast<const __half2*>(&m));
-          *w = c8_codes4(v0.x * f, v0.y * f, v1.x * f, v1.y * f);
+          *w = rescaled4(*w, f);
         }
       }
     }
@@ -318,6 +335,112 @@ __global__ void __launch_bounds__(256, HD == 256 ? 2 : 4) append8_kernel(const _
       *reinterpret_cast<uint32_t*>(dst + (int64_t)s * HD + HALF) =
           c8_codes4(x[i][4] * inv, x[i][5] * inv, x[i][6] * inv, x[i][7] * inv);
     }
+  }
+  if (bad) atomicMin(p.status, (int)POP_E_INVALID);
+}
+
+// The form of one row per sequence, a decode step: hd / 8 lanes per (sequence, head), one CTA for 256 / (hd / 8) heads. The
+// same arithmetic; the codes that a larger scale brings along are the only thing beyond one row. Bound by its chain of
+// loads (start, page, old scale); the kernel above, whose lanes would be empty in 15 of 16 slots, took 9.3 us for 96
+// sequences of 32 + 16 heads (two rounds of CTAs), this one 3.3; one sequence 2.8 and 1.9.
+template <int HD, bool IN_BF16>
+__global__ void __launch_bounds__(256) append8_row_kernel(const __grid_constant__ Append8Dev p) {
+  constexpr int LPR = HD / 8, HALF = HD / 2;
+  const Append8Args& a = p.a;
+  chain_trigger();
+  const int lane = threadIdx.x & 31, j0 = (lane % LPR) * 4, b = blockIdx.y;
+  const int heads = a.n_q + 2 * a.n_kv;
+  int h = (int)(blockIdx.x * (256 / LPR) + threadIdx.x / LPR);
+  const bool idle = h >= heads;                                                   // works on the last head, stores nothing
+  if (idle) h = heads - 1;
+  const bool is_q = h < a.n_q, is_v = h >= a.n_q + a.n_kv;
+  chain_wait();
+  const int row = a.cu ? __ldg(a.cu + b) : b;
+  const int n = a.cu ? __ldg(a.cu + b + 1) - row : 1;
+  const int at = a.start ? __ldg(a.start + b) : a.pos0;                           // the row's cache position
+  bool bad = n > 1 || at < 0 || at > 0x7ffffff0 - 1;
+  if (bad || n <= 0) {
+    if (bad && threadIdx.x == 0) atomicMin(p.status, (int)POP_E_INVALID);
+    return;
+  }
+  const int lo = at % C8_BLOCK, first = at - lo;                                  // earlier positions of its block
+  int page = -1;
+  if (!is_q) {
+    const int pi = first / a.dst.page_size;
+    if (pi < a.dst.max_pages) page = __ldg(a.dst.table + (int64_t)b * a.dst.max_pages + pi);
+  }
+  float x[8];
+  load_row8<HD, IN_BF16>(a.in, (int64_t)row * a.ld_in + (int64_t)h * HD + j0, x);
+  float2 cs[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) cs[u] = make_float2(1.f, 0.f);
+  if (!is_v) {
+    uchar4 axis = make_uchar4(0, 0, 0, 0);
+    if (a.pair_axis != nullptr) axis = __ldg(reinterpret_cast<const uchar4*>(a.pair_axis + j0));
+    const int ax[4] = {axis.x, axis.y, axis.z, axis.w};
+    const float2* from[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const bool known = a.pair_axis == nullptr || ax[u] < a.n_axes;              // else never turned into an address
+      int t = a.positions != nullptr && known ? __ldg(a.positions + ax[u] * a.ld_pos + row) : at;
+      if (!known || (unsigned)t >= (unsigned)a.table_rows) {
+        bad = true;
+        t = 0;
+      }
+      from[u] = a.table + (int64_t)t * HALF + j0 + u;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) cs[u] = __ldg(from[u]);
+  }
+  const float* gain = is_q ? a.q_gain : is_v ? nullptr : a.k_gain;
+  if (a.q_gain != nullptr || a.k_gain != nullptr) {                               // by all lanes: heads of a warp may differ
+    float4 g0 = make_float4(1.f, 1.f, 1.f, 1.f), g1 = g0;
+    if (gain != nullptr) {
+      g0 = make_float4(__ldg(gain + j0), __ldg(gain + j0 + 1), __ldg(gain + j0 + 2), __ldg(gain + j0 + 3));
+      g1 = make_float4(__ldg(gain + j0 + HALF), __ldg(gain + j0 + HALF + 1), __ldg(gain + j0 + HALF + 2), __ldg(gain + j0 + HALF + 3));
+    }
+    float y[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) y[u] = x[u];
+    norm_row8<HD>(y, g0, g1, a.eps);
+    if (gain != nullptr) {
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = y[u];
+    }
+  }
+  if (!is_v) turn_row8(x, cs);
+  if (is_q && !idle) store_q8<HD>(a.q_out + (int64_t)row * a.ldq + (int64_t)h * HD + j0, x);
+  const bool stores = !is_q && !idle && (unsigned)page < (unsigned)a.dst.num_pages;       // else never turned into an address
+  bad |= !is_q && !idle && !stores;
+  const int slot = first % a.dst.page_size;
+  const int64_t tile = (int64_t)(stores ? page : 0) * a.n_kv + (stores ? h - a.n_q - (is_v ? a.n_kv : 0) : 0);
+  uint8_t* dst = (is_v ? a.dst.v : a.dst.k) + (tile * a.dst.page_size + slot) * HD + j0;
+  uint8_t* scale = (is_v ? a.dst.vs : a.dst.ks) + tile * (a.dst.page_size / C8_BLOCK) + slot / C8_BLOCK;
+  const int was = stores && lo > 0 ? *scale : 0;                                  // the scale of earlier positions in the block
+  float am = 0.f;
+#pragma unroll
+  for (int u = 0; u < 8; ++u) am = fmaxf(am, fabsf(x[u]));
+#pragma unroll
+  for (int o = LPR / 2; o > 0; o >>= 1) am = fmaxf(am, __shfl_xor_sync(FULL, am, o));
+  __syncwarp();                                          // every lane has the old scale
+  if (stores) {
+    int e = c8_scale_exp(am);
+    if (e > was && lo > 0) {    // bring the earlier codes to the larger scale: exponents shift, small codes round again
+      const float f = c8_pow2(was - e);
+#pragma unroll 5
+      for (int i = 0; i < lo; ++i)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(dst + (int64_t)i * HD + half * HALF);
+          *w = rescaled4(*w, f);
+        }
+    }
+    e = max(e, was);
+    if (j0 == 0) *scale = (uint8_t)e;
+    const float inv = c8_pow2(127 - e);
+    uint32_t* to = reinterpret_cast<uint32_t*>(dst + (int64_t)lo * HD);
+    to[0] = c8_codes4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+    to[HALF / 4] = c8_codes4(x[4] * inv, x[5] * inv, x[6] * inv, x[7] * inv);
   }
   if (bad) atomicMin(p.status, (int)POP_E_INVALID);
 }
@@ -383,20 +506,23 @@ int launch_append8(const Append8Args& a, cudaStream_t s) {
   const dim3 grid((unsigned)gx, a.batch);
   ProfScope prof(PROF_ELEMENTWISE,
                  (double)a.batch * a.rows * a.head_dim * (heads * (a.in_bf16 ? 2.0 : 4.0) + a.n_q * 2.0 + a.n_kv * 2.0), s);
-  cudaError_t rc;
-  if (a.in_bf16) {
+  void (*kernel)(Append8Dev);
+  dim3 g = grid;
+  if (a.rows == 1) {
+    g.x = ceil_div(heads, 2048 / a.head_dim);
     switch (a.head_dim) {
-      case 64: rc = launch_chained(append8_kernel<64, true>, grid, dim3(256), 0, s, p); break;
-      case 128: rc = launch_chained(append8_kernel<128, true>, grid, dim3(256), 0, s, p); break;
-      default: rc = launch_chained(append8_kernel<256, true>, grid, dim3(256), 0, s, p); break;
+      case 64: kernel = a.in_bf16 ? append8_row_kernel<64, true> : append8_row_kernel<64, false>; break;
+      case 128: kernel = a.in_bf16 ? append8_row_kernel<128, true> : append8_row_kernel<128, false>; break;
+      default: kernel = a.in_bf16 ? append8_row_kernel<256, true> : append8_row_kernel<256, false>; break;
     }
   } else {
     switch (a.head_dim) {
-      case 64: rc = launch_chained(append8_kernel<64, false>, grid, dim3(256), 0, s, p); break;
-      case 128: rc = launch_chained(append8_kernel<128, false>, grid, dim3(256), 0, s, p); break;
-      default: rc = launch_chained(append8_kernel<256, false>, grid, dim3(256), 0, s, p); break;
+      case 64: kernel = a.in_bf16 ? append8_kernel<64, true> : append8_kernel<64, false>; break;
+      case 128: kernel = a.in_bf16 ? append8_kernel<128, true> : append8_kernel<128, false>; break;
+      default: kernel = a.in_bf16 ? append8_kernel<256, true> : append8_kernel<256, false>; break;
     }
   }
+  const cudaError_t rc = launch_chained(kernel, g, dim3(256), 0, s, p);
   if (rc != cudaSuccess) return POP_E_CUDA;
   count_launch();
   return POP_OK;

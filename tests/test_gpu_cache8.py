@@ -812,3 +812,49 @@ print("captured")
 """
     got = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
     assert "captured" in got.stdout, got.stderr[-2000:]
+
+
+ONE_ROW = [  # starts, rows of each, n_q, n_kv, hd, page, bf16 input, norm, axes: a decode step
+    ([0, 1, 15, 16, 17, 47], [1] * 6, 5, 3, 64, 16, False, True, 3), ([33, 2, 95], [1, 0, 1], 17, 2, 128, 32, True, False, 1),
+    ([7, 126, 127, 128], [1] * 4, 3, 2, 256, 128, False, True, 1), ([40, 9], [1, 1], 0, 5, 128, 64, False, True, 3),
+    ([11] * 3, [1, 1, 0], 8, 4, 256, 16, True, True, 3), ([383, 384], [1, 1], 1, 1, 64, 384, True, True, 1),
+]
+
+
+@pytest.mark.parametrize("case", ONE_ROW, ids=str)
+@pytest.mark.parametrize("strided,scale", [(False, 1.0), (True, 30.0), (False, 1e-3)])
+def test_append_of_one_row_each(L, case, strided, scale):
+    a = append_inputs(case, 190, scale)
+    cache = random_cache(191, 1, len(case[0]), a.top + 20, case[3], case[4], case[5])
+    check_append(case, a, cache, *run_append(L, case, a, cache, strided))
+
+
+def test_append_of_one_row_raises_the_status_for_bad_places(L):
+    from paper_2602_03295_b200 import POP_E_INVALID
+    case = ([5, 9], [1, 1], 2, 1, 64, 16, False, True, 3)
+    up = lambda t: None if t is None else t.to(DEV)  # noqa: E731
+    for what in ("page", "rotation", "axis", "rows", "start", "end"):
+        a = append_inputs(case, 192)
+        cache = list(random_cache(193, 1, 2, 16, 1, 64, 16))
+        if what == "page":
+            cache[4][1, 0] = -5
+        elif what == "rotation":
+            a.positions[1, 1] = -1
+        elif what == "axis":
+            a.pair_axis[7] = 200
+        elif what == "rows":
+            a.cu = torch.tensor([0, 2, 2], dtype=torch.int32)
+        elif what == "start":
+            a.starts[1] = -1
+        else:
+            a.starts[1] = 16 * cache[4].shape[1]
+        dev = [t[0].to(DEV).contiguous() for t in cache[:4]]
+        q = torch.empty(2, 128, dtype=torch.bfloat16, device=DEV)
+        L.rope_cache_e4m3(up(a.x), q, *dev, up(cache[4]), up(a.rope), 2, 1, 64, 1, start=up(a.starts), cu_rows=up(a.cu),
+                          q_gain=up(a.gains[0]), k_gain=up(a.gains[1]), eps=a.eps, positions=up(a.positions),
+                          pair_axis=up(a.pair_axis))
+        assert L.status() == POP_E_INVALID and L.status() == 0
+        if what in ("page", "start", "end"):     # the other sequence is stored, nothing else changes
+            keep = torch.ones(cache[0].shape[1], dtype=torch.bool)
+            keep[int(cache[4][0, 0])] = False
+            assert torch.equal(dev[0].cpu()[keep], cache[0][0][keep]) and torch.equal(dev[1].cpu()[keep], cache[1][0][keep])
