@@ -161,8 +161,10 @@ __device__ __forceinline__ Job job_of(const A8Dev& p, int bx, int by, int b, int
   x.n_tiles = last < 0 || tile < 0 ? 0 : last / 64 - x.j_lo + 1;
   return x;
 }
-// Pieces that the CTA's keys are cut into, at least one
-__device__ __forceinline__ int pieces_of(const A8Dev& p, const Job& x) { return max(1, (x.n_tiles + p.chunk - 1) / p.chunk); }
+// Pieces that the CTA's keys are cut into: at least one, and no more than there are CTAs and rows of the workspace for
+__device__ __forceinline__ int pieces_of(const A8Dev& p, const Job& x) {
+  return min(max(1, (x.n_tiles + p.chunk - 1) / p.chunk), p.splits);
+}
 __device__ __forceinline__ int row_pos(const Job& x, int r) { return (int)(r * x.inv >> 16); }     // r / heads
 
 __device__ __forceinline__ float ex2(float x) {
@@ -818,10 +820,12 @@ int launch_t(const Attn8Args& a, A8Dev& p, cudaStream_t s) {
   if (q_tiles > 65535) return POP_E_INVALID;
   p.q_tiles = (int)q_tiles;
   const int64_t base = (int64_t)a.n_kv * p.hg * q_tiles * a.batch;
+  // Positions of a CTA at most: the last of several head groups may have fewer heads than the others, so more of them
+  const int most = NQT * (128 / (p.G - (p.hg - 1) * 128)), reach = most < a.rows ? most : a.rows;
   // Pieces per tile: what takes the fewest turns of all SMs at the longest sequence's keys. The unit is a tile of 64 keys
   // (1.1 us at hd 128); beginning and ending a CTA costs eight, the merge four and its reads one per 96 pieces. Never more
   // than what POP_E4M3_WORKSPACE_BYTES holds, so that a workspace of that size covers every call.
-  const int64_t span = p.window > 0 && (int64_t)p.window + NQT * per < a.kv_len ? p.window + NQT * per : a.kv_len;
+  const int64_t span = p.window > 0 && (int64_t)p.window + reach < a.kv_len ? p.window + reach : a.kv_len;
   const int64_t sms = device_sms(), piece = (int64_t)NQT * 128 * (HD + 4) * 4;
   const int64_t tiles = span < 64 ? 1 : (span + 63) / 64 + (p.window > 0 ? 1 : 0);
   int64_t splits = 1, chunk = tiles, best = INT64_MAX;

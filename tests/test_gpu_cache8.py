@@ -858,3 +858,18 @@ def test_append_of_one_row_raises_the_status_for_bad_places(L):
             keep = torch.ones(cache[0].shape[1], dtype=torch.bool)
             keep[int(cache[4][0, 0])] = False
             assert torch.equal(dev[0].cpu()[keep], cache[0][0][keep]) and torch.equal(dev[1].cpu()[keep], cache[1][0][keep])
+
+
+UNEVEN_GROUPS = [  # heads over one kv head, hd, rows, length, window: the last of several head groups has tiles of many positions
+    (130, 64, 49, 849, 692), (129, 64, 59, 932, 689), (129, 128, 44, 1155, 680), (130, 128, 51, 1034, 675),
+    (136, 256, 36, 1176, 703), (129, 256, 90, 2177, 2064), (257, 64, 60, 1500, 900),
+]
+
+
+@pytest.mark.parametrize("n_q,hd,rows,length,window", UNEVEN_GROUPS)
+def test_head_groups_of_unequal_size_lose_no_keys(L, n_q, hd, rows, length, window):
+    cache = random_cache(200, 1, 1, length, 1, hd, 64)
+    poison_behind(cache, [length])
+    q, out = run_rows(L, cache, [rows], [length], n_q, 1, hd, window, 201)
+    assert L.status() == 0
+    check_attention(q, out.cpu(), cache, [rows], [length], n_q, 1, hd, window, pick=1)
