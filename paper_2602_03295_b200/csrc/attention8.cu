@@ -194,6 +194,9 @@ __host__ __device__ constexpr uint32_t umma_idesc_f16(int m, int n, int b_mn_maj
   return (1u << 4) | (uint32_t(b_mn_major) << 16) | (uint32_t(n >> 3) << 17) | (uint32_t(m >> 4) << 24);
 }
 
+// the lowest status wins, so a wait that ran out stays to be seen beside wrong arguments
+__device__ __forceinline__ bool gave_up(int status) { return status <= (int)POP_E_DEVICE_TIMEOUT; }
+
 #define A8_ABORT(S, status)                           \
   do {                                                \
     (S).abort = 1;                                    \
@@ -247,7 +250,8 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
     prefetch_tmap(&tmV);
   }
   chain_wait();
-  // the status word is on its way while the lengths are (read by the TMA warp alone)
+  // the status word is on its way while the lengths are (read by the TMA warp alone). Only a kernel that gave up on a wait
+  // stops this one: a wrong place of another call, or of another sequence of this one, does not touch these rows
   int raised = 0;
   if (warp == C::SM_WARPS + 4) raised = *reinterpret_cast<const volatile int*>(status);
   int split = 0, b = blockIdx.z;
@@ -335,7 +339,8 @@ attn8_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CU
   int tma_row = -2;
   if (warp == C::SM_WARPS + 4) {
     raised = __shfl_sync(0xffffffffu, raised, 0);
-    if (lane == 0) s.raised = raised != 0 ? 1u : 0u;
+    raised = gave_up(raised) ? 1 : 0;
+    if (lane == 0) s.raised = (uint32_t)raised;
     if (raised == 0) {
       tma_row = row_of(0);
       load_pair(0, tma_row);                               // the ring is empty: nothing is waited for
@@ -758,6 +763,7 @@ template <int HD, int NQT>
 __global__ void __launch_bounds__(256) attn8_merge_kernel(const __grid_constant__ A8Dev p, int* __restrict__ status) {
   chain_trigger();
   chain_wait();
+  if (gave_up(*reinterpret_cast<const volatile int*>(status))) return;      // there are pieces that nobody wrote
   const int groups = NQT * 128 / 8;
   const int by = blockIdx.y / groups, r = (blockIdx.y % groups) * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const Job x = job_of<NQT>(p, blockIdx.x, by, blockIdx.z, status);

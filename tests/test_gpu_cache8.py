@@ -873,3 +873,86 @@ def test_head_groups_of_unequal_size_lose_no_keys(L, n_q, hd, rows, length, wind
     q, out = run_rows(L, cache, [rows], [length], n_q, 1, hd, window, 201)
     assert L.status() == 0
     check_attention(q, out.cpu(), cache, [rows], [length], n_q, 1, hd, window, pick=1)
+
+
+def clean_and_harmed(L, case, harm, before=False):
+    """Outputs of a prompt call as it should be and of one with something wrong in sequence 1, both over poisoned rows, and
+    the status after each. harm(cache, lens, cu) changes its arguments; before: an earlier call has raised the status."""
+    rows, lens, n_q, n_kv, hd, page = case
+    outs, codes = [], []
+    for wrong in (False, True):
+        cache = random_cache(220, 1, len(lens), max(lens), n_kv, hd, page)
+        ln = torch.tensor(lens, dtype=torch.int32)
+        cu = torch.tensor([sum(rows[:i]) for i in range(len(rows) + 1)], dtype=torch.int32)
+        if wrong:
+            harm(cache, ln, cu)
+        dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+        q = queries(221, sum(rows), n_q, hd).to(DEV)
+        out = torch.full_like(q, 5.0)
+        if wrong and before:
+            one = torch.zeros(1, n_q * hd, dtype=torch.bfloat16, device=DEV)
+            L.decode_attention_e4m3(one, *dev[:4], torch.full((1, 1), -3, dtype=torch.int32, device=DEV),
+                                    torch.empty_like(one), n_q, n_kv, hd, 16)
+        L.attention_e4m3(q, *dev, out, n_q, n_kv, hd, max(rows), max(lens), cu_rows=cu.to(DEV), seq_lens=ln.to(DEV),
+                         workspace=torch.full((64 << 18,), math.nan, device=DEV))
+        outs.append(out)
+        codes.append(L.status())
+    return outs, codes
+
+
+SOME_WRONG = [  # rows, lens, n_q, n_kv, hd, page: keys in one piece, keys in several, more CTAs than the GPU takes at once
+    ([40, 50, 30], [300, 200, 64], 4, 2, 128, 64), ([40, 50, 30], [9000, 8000, 7000], 4, 2, 128, 64),
+    ([40, 50, 30], [9000, 8000, 7000], 4, 2, 256, 128), ([40, 50, 30], [300, 9000, 64], 8, 1, 64, 16),
+    ([700, 600, 300], [900, 800, 300], 32, 8, 64, 32),
+]
+
+
+@pytest.mark.parametrize("case", SOME_WRONG, ids=str)
+@pytest.mark.parametrize("what", ["page", "length", "rows", "earlier call"])
+def test_prompt_rows_of_the_other_sequences_are_whole(L, case, what):
+    """What is wrong with one sequence, or was with another call, changes nothing of the others' rows."""
+    from paper_2602_03295_b200 import POP_E_INVALID
+    rows, lens, page = case[0], case[1], case[5]
+    first, last = rows[0], rows[0] + rows[1]
+
+    def harm(cache, ln, cu):
+        if what == "page":
+            cache[4][1, 1] = 2 ** 30
+        elif what == "length":
+            ln[1] = max(lens) + 1
+        elif what == "rows":                       # sequence 1 says that it has more rows than any has
+            cu[2] = cu[1] + max(rows) + 1
+            cu[3] = cu[2]
+    (clean, out), codes = clean_and_harmed(L, case, harm, what == "earlier call")
+    assert codes == [0, POP_E_INVALID]
+    assert torch.equal(out[:first], clean[:first])
+    if what != "rows":
+        assert torch.equal(out[last:], clean[last:])
+    if what == "earlier call":
+        assert torch.equal(out, clean)
+    if what == "page":                             # a page that is none reads as zeros, with a scale of 1
+        def zero(cache, ln, cu):
+            pg = cache[4][1, 1].long()
+            for i in range(4):
+                cache[i][0, pg] = 0 if i < 2 else 127
+        (_, zeros), codes = clean_and_harmed(L, case, zero)
+        assert codes == [0, 0] and torch.equal(out, zeros)
+
+
+@pytest.mark.parametrize("case", SOME_WRONG[:3], ids=str)
+def test_prompt_after_a_kernel_gave_up_writes_nothing(L, case):
+    from paper_2602_03295_b200 import POP_E_DEVICE_TIMEOUT
+    rows, lens, n_q, n_kv, hd, page = case
+    cache = random_cache(222, 1, len(lens), max(lens), n_kv, hd, page)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    q = queries(223, sum(rows), n_q, hd).to(DEV)
+    out = torch.full_like(q, 5.0)
+    cu = torch.tensor([sum(rows[:i]) for i in range(len(rows) + 1)], dtype=torch.int32, device=DEV)
+    ln = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    ws = torch.full((64 << 18,), math.nan, device=DEV)
+    L.wait_selftest()
+    L.attention_e4m3(q, *dev, out, n_q, n_kv, hd, max(rows), max(lens), cu_rows=cu, seq_lens=ln, workspace=ws)
+    assert L.status() == POP_E_DEVICE_TIMEOUT and L.status() == 0
+    assert (out == 5.0).all()
+    L.attention_e4m3(q, *dev, out, n_q, n_kv, hd, max(rows), max(lens), cu_rows=cu, seq_lens=ln, workspace=ws)
+    assert L.status() == 0 and not (out == 5.0).all(1).any()
