@@ -789,8 +789,9 @@ __global__ void __launch_bounds__(256) attn8_merge_kernel(const __grid_constant_
     float n = fmaxf(m, ms);
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) n = fmaxf(n, __shfl_xor_sync(0xffffffffu, n, d));
-    if (n == -INFINITY) continue;
-    const float f = ex2(m - n), w = ex2(ms - n);
+    // no maximum so far: the pieces saw nothing (zeros), or scores that are all NaN, whose sums stay NaN
+    const float z = n == -INFINITY ? 0.f : n;
+    const float f = ex2(m - z), w = ex2(ms - z);
     float sum = w * ls;
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);

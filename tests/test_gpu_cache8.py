@@ -956,3 +956,36 @@ def test_prompt_after_a_kernel_gave_up_writes_nothing(L, case):
     assert (out == 5.0).all()
     L.attention_e4m3(q, *dev, out, n_q, n_kv, hd, max(rows), max(lens), cu_rows=cu, seq_lens=ln, workspace=ws)
     assert L.status() == 0 and not (out == 5.0).all(1).any()
+
+
+@pytest.mark.parametrize("hd,rows", [(64, 40), (128, 40), (256, 40), (128, 1), (128, 16)])
+def test_infinite_and_nan_queries_stay_nan_where_the_keys_are_cut(L, hd, rows):
+    """The same row whether its keys are attended to in one piece or in several."""
+    from paper_2602_03295_b200 import POP_E_NOSPACE, PopError
+    n_q, n_kv, length = 4, 2, 9000 if rows > 16 else 40000
+    cache = random_cache(210, 1, 1, length, n_kv, hd, 64)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    q = queries(211, rows, n_q, hd)
+    clean, out = torch.empty_like(q, device=DEV), torch.empty_like(q, device=DEV)
+    L.attention_e4m3(q.to(DEV), *dev, clean, n_q, n_kv, hd, rows, length)
+    with pytest.raises(PopError) as e:                     # pieces are what the workspace is for
+        L.attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, rows, length, workspace=torch.empty(16, device=DEV))
+    assert e.value.code == POP_E_NOSPACE
+    bad = q.clone().view(rows, n_q, hd)
+    bad[0, 0, 3], bad[0, 2, hd - 1], bad[rows - 1, 3, 0] = math.inf, -math.inf, math.nan
+    L.attention_e4m3(bad.view(rows, -1).to(DEV), *dev, out, n_q, n_kv, hd, rows, length)
+    assert L.status() == 0
+    hit = ~torch.isfinite(bad).all(-1).to(DEV)
+    got, want = out.view(rows, n_q, hd), clean.view(rows, n_q, hd)
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], want[~hit])
+
+
+@pytest.mark.parametrize("at", [0, 4000, 8959])
+def test_a_nan_key_reaches_the_rows_that_see_it_where_the_keys_are_cut(L, at):
+    n_q, n_kv, hd, rows, length = 4, 2, 128, 40, 9000
+    k8, v8, ks, vs, table = random_cache(212, 1, 1, length, n_kv, hd, 64)
+    k8[0, table[0, at // 64].long(), 1, at % 64, 5] = 0x7f
+    q, out = run_rows(L, (k8, v8, ks, vs, table), [rows], [length], n_q, n_kv, hd, 0, 213)
+    assert L.status() == 0
+    nan = torch.isnan(out.view(rows, n_kv, 2 * hd))
+    assert nan[:, 1].all() and not nan[:, 0].any()
