@@ -501,9 +501,10 @@ class PopLibrary:
                 q_inner != 1 or o_inner != 1:
             raise PopError(POP_E_INVALID, "q and out are bf16 [rows, n_q hd]")
         if workspace is None:
-            workspace = torch.empty(POP_E4M3_WORKSPACE_BYTES, dtype=torch.uint8, device=q.device)
-            if stream is not None:             # its memory goes back when the call returns: not before that stream is past it
-                workspace.record_stream(stream)
+            # from the pool of the stream that runs the call: its memory has no work of another stream in front of it, and
+            # goes back, when the call returns, to that stream's later work
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(POP_E4M3_WORKSPACE_BYTES, dtype=torch.uint8, device=q.device)
         elif not workspace.is_contiguous():
             raise PopError(POP_E_INVALID, "workspace has to be contiguous")
         return rows, ldq, ldo, workspace, workspace.numel() * workspace.element_size()

@@ -989,3 +989,31 @@ def test_a_nan_key_reaches_the_rows_that_see_it_where_the_keys_are_cut(L, at):
     assert L.status() == 0
     nan = torch.isnan(out.view(rows, n_kv, 2 * hd))
     assert nan[:, 1].all() and not nan[:, 0].any()
+
+
+@pytest.mark.parametrize("op", ["decode", "prompt"])
+def test_stream_argument_without_a_workspace_takes_no_memory_with_work_behind_it(L, op):
+    """Memory that was given back while work of the current stream on it is still to come is not what the call on another
+    stream writes its pieces to."""
+    n_q, n_kv, hd, lens = 8, 2, 128, [20000, 19000]
+    rows = 1 if op == "decode" else 60
+    cache = random_cache(240, 1, 2, 20000, n_kv, hd, 128)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    q, want = run_rows(L, cache, [rows] * 2, lens, n_q, n_kv, hd, 0, 241, op == "decode")
+    q, out, ln = q.to(DEV), torch.empty_like(want), torch.tensor(lens, dtype=torch.int32, device=DEV)
+    side = torch.cuda.Stream()
+    kept = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    given_back = torch.full((64 << 20,), 9, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(400000000)                   # the copy below is still to come when the call runs
+    kept.copy_(given_back)
+    del given_back
+    if op == "decode":
+        L.decode_attention_e4m3(q, *dev, out, n_q, n_kv, hd, 20000, seq_lens=ln, stream=side)
+    else:
+        L.attention_e4m3(q, *dev, out, n_q, n_kv, hd, rows, 20000, seq_lens=ln, stream=side)
+    torch.cuda.synchronize()
+    assert L.status() == 0
+    assert (kept == 9).all() and torch.equal(out, want)
