@@ -510,13 +510,16 @@ __global__ void __launch_bounds__(WARPS * 32, D8<HD>::PER_SM) dec8_kernel(const 
             }
           }
         }
-        if (at + (u2 + 1) * C8_BLOCK > x.s.len) {              // behind the sequence: no value whatever is there
+        // behind the sequence, or in front of every row's window: no value whatever is there
+        if (at + (u2 + 1) * C8_BLOCK > x.s.len || at + u2 * C8_BLOCK < x.s.lo) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (at + u2 * C8_BLOCK + 2 * t + (k & 1) + (k >> 1) * 8 >= x.s.len) {
+          for (int k = 0; k < 4; ++k) {
+            const int a = at + u2 * C8_BLOCK + 2 * t + (k & 1) + (k >> 1) * 8;
+            if (a >= x.s.len || a < x.s.lo) {
 #pragma unroll
               for (int w = 0; w < VW; ++w) vr[k][w] = 0;
             }
+          }
         }
 #pragma unroll
         for (int w = 0; w < VW; ++w) {

@@ -1017,3 +1017,27 @@ def test_stream_argument_without_a_workspace_takes_no_memory_with_work_behind_it
     torch.cuda.synchronize()
     assert L.status() == 0
     assert (kept == 9).all() and torch.equal(out, want)
+
+
+@pytest.mark.parametrize("hd,page,rows,window", [(128, 16, 1, 100), (256, 64, 1, 300), (64, 16, 5, 40), (128, 128, 4, 1),
+                                                (64, 64, 1, 1), (128, 64, 1, 1100), (128, 16, 60, 77), (256, 16, 30, 130), (64, 32, 200, 500)])
+def test_positions_just_in_front_of_the_window_reach_no_row(L, hd, page, rows, window):
+    """NaN codes up to the first position that a row of the sequence sees, in that position's own block too."""
+    n_q, n_kv, lens = 4, 2, [1500, 1111, 900, 1007, 3]
+    n = [min(rows, x) for x in lens]
+    cache = random_cache(230, 1, len(lens), max(lens), n_kv, hd, page)
+    poison_behind(cache, lens)
+    whole = tuple(t.clone() for t in cache)
+    for b, x in enumerate(lens):
+        pos = torch.arange(max(0, x - n[b] - window + 1))
+        for c in cache[:2]:
+            c[0, cache[4][b].long()[pos // page], :, pos % page] = 0x7f
+    q, out = run_rows(L, cache, n, lens, n_q, n_kv, hd, window, 231, rows == 1)
+    assert L.status() == 0
+    check_attention(q, out.cpu(), whole, n, lens, n_q, n_kv, hd, window, decode=rows == 1, pick=None if rows < 60 else 1)
+    if rows == 1:                                  # the other entry point, and with the long window the work dealt in stretches
+        many = 30
+        big = tuple(t for t in cache[:4]) + (cache[4].repeat(many, 1),)
+        qs, outs = run_rows(L, big, [1] * (5 * many), lens * many, n_q, n_kv, hd, window, 232, False, top=1500)
+        assert L.status() == 0
+        check_attention(qs, outs.cpu(), whole[:4] + (whole[4].repeat(many, 1),), [1] * (5 * many), lens * many, n_q, n_kv, hd, window)
