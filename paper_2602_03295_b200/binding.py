@@ -627,14 +627,14 @@ class KVCacheE4M3:
     def fill_from(self, cache: KVCache, max_len: Optional[int] = None, seq_lens=None, library: Optional[PopLibrary] = None,
                   stream=None):
         """pop_k_quant_cache_e4m3: all layers of a bf16 cache, positions 0 .. n-1 (max_len, or seq_lens int32 [batch])."""
+        n = min(cache.seq_len, self.seq_len) if max_len is None else max_len
         (library or lib()).quant_cache_e4m3(cache.k, cache.v, cache.block_table, self.k, self.v, self.k_scale, self.v_scale,
-                                            self.block_table, max_len or min(cache.seq_len, self.seq_len),
-                                            seq_lens=seq_lens, stream=stream)
+                                            self.block_table, n, seq_lens=seq_lens, stream=stream)
 
     def gather(self, layer: int, seq_len: Optional[int] = None):
         """(K, V) of 0-based `layer` as dense bf16 [batch, seq_len, n_kv, hd]: code times scale is exact in bf16 (a
         host-side view for checks)."""
-        n = seq_len or self.seq_len
+        n = self.seq_len if seq_len is None else seq_len
         pos = torch.arange(n, device=self.k.device)
         pages = self.block_table[:, pos // self.page_size].long()          # [batch, n]
         slots = (pos % self.page_size)[None, :].expand_as(pages)

@@ -139,3 +139,15 @@ def test_output_rows_over_each_other_are_refused(library):
     assert dll.pop_k_decode_attention_e4m3(*{**DECODE, "batch": 2, "ldo": 56}.values()) == POP_E_INVALID
     assert dll.pop_k_attention_e4m3(*{**PROMPT, "max_rows": 2, "ldo": 0}.values()) == POP_E_INVALID
     assert dll.pop_k_rope_cache_e4m3(*{**APPEND, "max_rows": 2, "ldq": 60}.values()) == POP_E_INVALID
+
+
+def test_fill_from_takes_a_length_of_zero_for_what_it_is():
+    from types import SimpleNamespace
+    from paper_2602_03295_b200.binding import KVCache, KVCacheE4M3
+    cfg = SimpleNamespace(n_layers=1, n_kv_heads=1, head_dim=64)
+    a, c, asked = KVCache(cfg, 1, 40, 16, device="cpu"), KVCacheE4M3(cfg, 1, 32, 16, device="cpu"), []
+    fake = SimpleNamespace(quant_cache_e4m3=lambda *args, **kw: asked.append(args[8]))
+    for n in (0, 7, None):
+        c.fill_from(a, n, library=fake)
+    assert asked == [0, 7, 32]
+    assert [t.shape[1] for t in c.gather(0, 0)] == [0, 0] and [t.shape[1] for t in c.gather(0)] == [32, 32]
