@@ -200,8 +200,8 @@ int pop_k_decode_attention_static(const void* q, int64_t ldq, const void* k_pool
  * Device-side checks in every call: a block-table entry outside [0, num_pages), a length above the stated maximum, a
  * rotation row outside the table are never turned into addresses; the status word is raised to POP_E_INVALID and what
  * depends on them is not written or reads as zeros; the other sequences, and calls made while the word holds POP_E_INVALID,
- * are not touched by it (behind POP_E_DEVICE_TIMEOUT pop_k_attention_e4m3 may leave rows as they are). Lengths (kv_len) go up to 2^31 - 2^16. The codes behind a sequence's
- * last position are left as they are.
+ * are not touched by it (behind POP_E_DEVICE_TIMEOUT pop_k_attention_e4m3 may leave rows as they are). Lengths (kv_len,
+ * max_len) go up to 2^31 - 2^16. The codes behind a sequence's last position are left as they are.
  *
  * pop_k_quant_cache_e4m3: the bf16 cache that a prefill left, for `layers` consecutive layers (src_layer_stride elements,
  *   code_layer_stride and scale_layer_stride bytes apart), positions 0 .. n-1 of every sequence, n = seq_lens[b] (device

@@ -452,7 +452,7 @@ bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % 
 int launch_quant_cache8(const Quant8Args& a, cudaStream_t s) {
   if (!a.k || !a.v || !a.table || !c8_cache_ok(a.dst)) return POP_E_INVALID;
   if (a.layers < 1 || a.layers > 32767 || a.batch < 1 || a.batch > 65535 || a.n_kv < 1 || a.n_kv > 1024 ||
-      a.max_len < 0 || !page_size_ok(a.page_size) || a.num_pages < 1 || a.max_pages < 1)
+      a.max_len < 0 || a.max_len > 0x7fff0000 || !page_size_ok(a.page_size) || a.num_pages < 1 || a.max_pages < 1)
     return POP_E_INVALID;
   if (a.head_dim != 64 && a.head_dim != 128 && a.head_dim != 256) return POP_E_INVALID;
   if (!aligned(a.k, 16) || !aligned(a.v, 16) || a.layer_stride % 8 || a.code_layer_stride % 16) return POP_E_INVALID;

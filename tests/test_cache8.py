@@ -151,3 +151,11 @@ def test_fill_from_takes_a_length_of_zero_for_what_it_is():
         c.fill_from(a, n, library=fake)
     assert asked == [0, 7, 32]
     assert [t.shape[1] for t in c.gather(0, 0)] == [0, 0] and [t.shape[1] for t in c.gather(0)] == [32, 32]
+
+
+def test_conversion_of_lengths_behind_the_largest_is_refused(library):
+    """As those of the attention calls: a block number times 16 has to stay a 32-bit position in every thread of the grid."""
+    from paper_2602_03295_b200 import POP_E_INVALID
+    big = {**QUANT, "max_pages": 1 << 28, "src_max_pages": 1 << 28}
+    for n in (0x7fff0001, 0x7fffff81, 0x7fffffff):
+        assert library.dll.pop_k_quant_cache_e4m3(*{**big, "max_len": n}.values()) == POP_E_INVALID
