@@ -5,14 +5,12 @@
 namespace pop {
 
 int device_sms() {
-  static int sms = 0;
-  if (sms == 0) {
+  static const int sms = [] {          // asked once, however many threads call at the same time
     int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1)
-      n = 148;
-    sms = n;
-  }
+    const bool known = cudaGetDevice(&dev) == cudaSuccess &&
+                       cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess && n > 0;
+    return known ? n : 148;
+  }();
   return sms;
 }
 

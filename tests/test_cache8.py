@@ -159,3 +159,25 @@ def test_conversion_of_lengths_behind_the_largest_is_refused(library):
     big = {**QUANT, "max_pages": 1 << 28, "src_max_pages": 1 << 28}
     for n in (0x7fff0001, 0x7fffff81, 0x7fffffff):
         assert library.dll.pop_k_quant_cache_e4m3(*{**big, "max_len": n}.values()) == POP_E_INVALID
+
+
+def test_the_count_of_sms_is_asked_for_once_by_all_threads(tmp_path):
+    """The host code under ThreadSanitizer: two threads whose first calls come at the same time."""
+    import subprocess
+    from paper_2602_03295_b200 import _build
+    (tmp_path / "main.cu").write_text("""
+#include <thread>
+namespace pop { int device_sms(); }
+int main() {
+  int a = 0, b = 0;
+  std::thread x([&] { a = pop::device_sms(); }), y([&] { b = pop::device_sms(); });
+  x.join();
+  y.join();
+  return a == b && a > 0 ? 0 : 1;
+}
+""")
+    flags = ["/usr/local/cuda/bin/nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-O1", "-std=c++17", "-Xcompiler", "-fsanitize=thread"]
+    files = [tmp_path / "main.cu"] + [_build.CSRC + "/" + n for n in ("cache8.cu", "runtime.cu")]
+    subprocess.run(flags + ["-o", str(tmp_path / "race")] + [str(f) for f in files], check=True, capture_output=True, text=True)
+    got = subprocess.run([str(tmp_path / "race")], capture_output=True, text=True, timeout=120)
+    assert got.returncode == 0, got.stderr[-3000:]
