@@ -201,7 +201,10 @@ int pop_k_decode_attention_static(const void* q, int64_t ldq, const void* k_pool
  * rotation row outside the table are never turned into addresses; the status word is raised to POP_E_INVALID and what
  * depends on them is not written or reads as zeros; the other sequences, and calls made while the word holds POP_E_INVALID,
  * are not touched by it (behind POP_E_DEVICE_TIMEOUT pop_k_attention_e4m3 may leave rows as they are). Lengths (kv_len,
- * max_len) go up to 2^31 - 2^16. The codes behind a sequence's last position are left as they are.
+ * max_len) go up to 2^31 - 2^16. The codes behind a sequence's last position are left as they are. cu_rows is taken at its
+ * word: the calls do not know how many rows in, q and out have.
+ * Scale bytes are 63 to 247, as these calls write them. The V scales of the positions that a row sees may lie up to 2^100
+ * apart (beside blocks of zeros: values up to 2^44); beyond that the small blocks' share of the softmax sum may be lost.
  *
  * pop_k_quant_cache_e4m3: the bf16 cache that a prefill left, for `layers` consecutive layers (src_layer_stride elements,
  *   code_layer_stride and scale_layer_stride bytes apart), positions 0 .. n-1 of every sequence, n = seq_lens[b] (device
@@ -243,9 +246,11 @@ int pop_k_rope_cache_e4m3(const void* in, int32_t in_bf16, int64_t ld_in, const 
 
 /* pop_k_decode_attention over the 8-bit cache, with a length per sequence: one query per sequence at position
  * len - 1, len = seq_lens[b] (device int32 [batch], each <= kv_len) or kv_len for all if seq_lens is NULL, over the last
- * `window` positions (0: all). q bf16 [batch][ldq], out bf16 [batch][ldo] (strides multiples of 8, ldo >= n_q hd, 16-byte aligned), any
- * n_q that is a multiple of n_kv. A sequence of length 0 gets a row of zeros. batch <= 4096. Unequal
- * lengths are shared out over the whole GPU; results do not depend on scheduling. */
+ * `window` positions (0: all). q bf16 [batch][ldq], out bf16 [batch][ldo] (strides multiples of 8, ldo >= n_q hd, 16-byte
+ * aligned), any n_q that is a multiple of n_kv. A sequence of length 0 gets a row of zeros. batch <= 4096. Unequal lengths are
+ * shared out over the whole GPU; results do not depend on scheduling. Blocks of 16 positions have 32-bit numbers, in the pool
+ * (num_pages n_kv page_size / 16 < 2^31) and in the call (batch n_kv ceil(n_q / n_kv / 8) + 1 times the blocks of kv_len, or
+ * of the window, < 2^31); a larger call is refused with POP_E_INVALID. */
 int pop_k_decode_attention_e4m3(const void* q, int64_t ldq, const void* k_codes, const void* v_codes,
                                 const void* k_scales, const void* v_scales, const int32_t* block_table,
                                 int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq,
@@ -259,7 +264,10 @@ int pop_k_decode_attention_e4m3(const void* q, int64_t ldq, const void* k_codes,
  * the rows' own: row i sits at position len - n + i and sees positions j <= its own, and j > its own - window if window > 0.
  * A row that sees nothing (a length below its sequence's rows) becomes zeros. Rows of no sequence are left as they are.
  * Pages in front of the window of every query are not read: their table entries may be anything (decode: the same). NaN
- * codes inside the part of a sequence that some row of the call sees may reach rows that do not see them. */
+ * codes inside the part of a sequence that some row of the call sees may reach rows that do not see them. A row that sees a
+ * position and has an infinite or NaN query element is NaN. Refused with POP_E_INVALID: num_pages n_kv page_size above
+ * 2^31 - 16; max_rows above 131070 (hd 256: 65535) times floor(128 / min(128, n_q / n_kv)); where max_rows n_q / n_kv is 32 or
+ * less, the decode call's limit on the blocks of the call with that product in place of n_q / n_kv. */
 int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int32_t max_rows, const void* k_codes,
                          const void* v_codes, const void* k_scales, const void* v_scales, const int32_t* block_table,
                          int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, const int32_t* seq_lens,

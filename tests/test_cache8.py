@@ -181,3 +181,19 @@ int main() {
     subprocess.run(flags + ["-o", str(tmp_path / "race")] + [str(f) for f in files], check=True, capture_output=True, text=True)
     got = subprocess.run([str(tmp_path / "race")], capture_output=True, text=True, timeout=120)
     assert got.returncode == 0, got.stderr[-3000:]
+
+
+def test_limits_that_the_header_states(library):
+    """Refused one behind the limit; at the limit the call is taken, as far as a machine without a GPU takes it."""
+    from paper_2602_03295_b200 import POP_E_INVALID
+    call = lambda op, **change: getattr(library.dll, CALLS[op][0])(*{**CALLS[op][1], "max_pages": 1 << 20, **change}.values())  # noqa: E731
+    for hd, n_q, most in ((64, 128, 131070), (128, 200, 131070), (256, 128, 65535), (64, 60, 262140), (256, 1, 8388480)):
+        for n in (most, most + 1):
+            got = call("prompt", head_dim=hd, n_q=n_q, ldq=n_q * hd, ldo=n_q * hd, max_rows=n, kv_len=n)
+            assert (got == POP_E_INVALID) == (n > most), (hd, n_q, n, got)
+    for op in ("decode", "prompt"):
+        for batch, refused in ((15, False), (16, True), (17, True)):          # times 2^27 blocks
+            got = call(op, batch=batch, kv_len=0x7fff0000, max_pages=1 << 28)
+            assert (got == POP_E_INVALID) == refused, (op, batch, got)
+    for pages in ((1 << 27) - 1, 1 << 27):                                    # of 16 positions
+        assert (call("prompt", num_pages=pages, max_rows=40) == POP_E_INVALID) == (pages >= 1 << 27)

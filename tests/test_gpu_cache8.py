@@ -1041,3 +1041,132 @@ def test_positions_just_in_front_of_the_window_reach_no_row(L, hd, page, rows, w
         qs, outs = run_rows(L, big, [1] * (5 * many), lens * many, n_q, n_kv, hd, window, 232, False, top=1500)
         assert L.status() == 0
         check_attention(qs, outs.cpu(), whole[:4] + (whole[4].repeat(many, 1),), [1] * (5 * many), lens * many, n_q, n_kv, hd, window)
+
+
+def test_captured_prompt_graphs_on_two_streams(L):
+    """Append of several rows and the prompt kernel, with the keys in one piece and cut, captured into two graphs with a workspace
+    each and replayed on two streams at once, equal the eager calls bit for bit."""
+    n_q, n_kv, hd, page, batch, rows, length = 8, 2, 128, 64, 3, 24, 9000
+    cache = random_cache(250, 1, batch, length, n_kv, hd, page)
+    ang = torch.arange(length)[:, None].double() * 1e4 ** (-torch.arange(0, hd, 2).double() / hd)
+    rope = torch.stack([ang.cos(), ang.sin()], -1).float().to(DEV)
+    lens = torch.tensor([9000, 24, 6400], dtype=torch.int32, device=DEV)
+    short = torch.tensor([700, 24, 640], dtype=torch.int32, device=DEV)
+    start = lens - rows
+
+    def make(seed):
+        s = SimpleNamespace()
+        s.dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+        s.x = torch.randn(batch * rows, (n_q + 2 * n_kv) * hd, generator=gen(seed)).to(DEV)
+        s.q = torch.empty(batch * rows, n_q * hd, dtype=torch.bfloat16, device=DEV)
+        s.o1, s.o2 = torch.empty_like(s.q), torch.empty_like(s.q)
+        s.ws = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+        return s
+
+    def chain(s):
+        L.rope_cache_e4m3(s.x, s.q, *s.dev, rope, n_q, n_kv, hd, rows, start=start)
+        L.attention_e4m3(s.q, *s.dev, s.o1, n_q, n_kv, hd, rows, length, seq_lens=lens, workspace=s.ws)
+        L.attention_e4m3(s.q, *s.dev, s.o2, n_q, n_kv, hd, rows, 700, seq_lens=short, window=300, workspace=s.ws)
+
+    states, graphs = [make(251), make(252)], []
+    chain(make(253))
+    torch.cuda.synchronize()
+    side = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in states:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            chain(s)
+        graphs.append(g)
+    for seed in (254, 256):
+        for i, s in enumerate(states):
+            s.x.copy_(torch.randn(s.x.shape, generator=gen(seed + i)))
+            for t, u in zip(s.dev, cache[:4]):
+                t.copy_(u[0])
+        torch.cuda.synchronize()
+        for g, st in zip(graphs, side):
+            with torch.cuda.stream(st):
+                g.replay()
+        torch.cuda.synchronize()
+        assert L.status() == 0
+        for i, s in enumerate(states):
+            e = make(seed + i)
+            chain(e)
+            torch.cuda.synchronize()
+            assert torch.equal(e.o1, s.o1) and torch.equal(e.o2, s.o2) and torch.equal(e.q, s.q)
+            assert all(torch.equal(t, u) for t, u in zip(e.dev, s.dev))
+
+
+def test_prompt_offsets_behind_32_bits(L):
+    """The prompt kernel over the last pages of a pool of more than 2^32 code bytes, after an append of its rows."""
+    n_kv, hd, page, pages, rows = 8, 256, 256, 8300, 40             # 8300 * 524288 bytes = 4.35 GB
+    k8 = torch.zeros(pages, n_kv, page, hd, dtype=torch.uint8, device=DEV)
+    v8 = torch.zeros_like(k8)
+    ks = torch.full((pages, n_kv, page // BLOCK), 120, dtype=torch.uint8, device=DEV)
+    vs = ks.clone()
+    small = random_cache(260, 1, 1, 3 * page, n_kv, hd, page)
+    ids = torch.tensor([[pages - 1, 3, pages - 40]], dtype=torch.int32)
+    at = ids[0].long().to(DEV)
+    for t, u in zip((k8, v8, ks, vs), small[:4]):
+        t[at] = u[0][small[4][0].long()].to(DEV)
+    n = 2 * page + 100
+    case = ([n - rows], [rows], 8, n_kv, hd, page, False, False, 1)
+    a = append_inputs(case, 261)
+    q = torch.empty(rows, 8 * hd, dtype=torch.bfloat16, device=DEV)
+    out = torch.empty_like(q)
+    L.rope_cache_e4m3(a.x.to(DEV), q, k8, v8, ks, vs, ids.to(DEV), a.rope.to(DEV), 8, n_kv, hd, rows, pos0=n - rows)
+    L.attention_e4m3(q, k8, v8, ks, vs, ids.to(DEV), out, 8, n_kv, hd, rows, n)
+    assert L.status() == 0
+    local = tuple(t[at].cpu()[None] for t in (k8, v8, ks, vs)) + (torch.tensor([[0, 1, 2]], dtype=torch.int32),)
+    before = tuple(u[:, small[4][0].long()] for u in small[:4]) + (local[4],)
+    check_append(case, a, before, q.cpu(), [t[0] for t in local[:4]])
+    check_attention(q.cpu(), out.cpu(), local, [rows], [n], 8, n_kv, hd, 0, pick=1)
+
+
+@pytest.mark.parametrize("hd,length", [(64, 300), (128, 300), (256, 300), (128, 9000)])
+def test_prompt_rows_with_tiny_and_zero_queries(L, hd, length):
+    n_q, n_kv, page, rows = 4, 2, 32, 30
+    cache = random_cache(270, 1, 1, length, n_kv, hd, page)
+    q = queries(271, rows, n_q, hd)
+    q[0] = 0
+    q[1] *= 1e-30
+    q[2, :hd] = 0
+    q[3] *= 1e-38
+    q[rows - 1, hd:2 * hd] = 0
+    out = torch.full(q.shape, math.nan, dtype=torch.bfloat16, device=DEV)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [cache[4].to(DEV)]
+    L.attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, rows, length)
+    assert L.status() == 0
+    check_attention(q, out.cpu(), cache, [rows], [length], n_q, n_kv, hd, 0, pick=None if length < 1000 else 1)
+
+
+@pytest.mark.parametrize("hd", [64, 128, 256])
+@pytest.mark.parametrize("rows", [1, 30])
+def test_blocks_of_zeros_that_have_the_weight(L, hd, rows):
+    """The positions that a row attends to have values of 0 (the smallest scale, 2^-64), the others, with scores that are
+    lower by 20, values of up to 448 * 2^36: the sum that divides has to keep the zeros' share."""
+    n, n_q, n_kv, page = 500, 4, 2, 64
+    k8, v8, ks, vs, table = random_cache(280, 1, 1, n, n_kv, hd, page)
+    k8[:], ks[:], vs[:] = 0, 117, 127 + 36
+    for p0 in range(0, 480, 48):                                   # every third block
+        pg, slot = int(table[0, p0 // page]), p0 % page
+        v8[0, pg, :, slot:slot + BLOCK], vs[0, pg, :, slot // BLOCK] = 0, 63
+        k8[0, pg, :, slot:slot + BLOCK] = 0x48                     # 4.0: a score of hd q 2^-8 / sqrt(hd)
+    q = torch.full((rows, n_q * hd), 5120 / math.sqrt(hd)).bfloat16()
+    cache = (k8, v8, ks, vs, table)
+    dev = [t[0].to(DEV).contiguous() for t in cache[:4]] + [table.to(DEV)]
+    out = torch.empty_like(q, device=DEV)
+    L.attention_e4m3(q.to(DEV), *dev, out, n_q, n_kv, hd, rows, n)
+    assert L.status() == 0
+    check_attention(q, out.cpu(), cache, [rows], [n], n_q, n_kv, hd, 0)
+
+
+def test_few_rows_of_more_sequences_than_the_few_row_kernel_takes(L):
+    n_q, n_kv, hd, page, batch = 2, 1, 64, 16, 4500
+    lens = spread(batch, 0, 40)
+    cache = random_cache(290, 1, batch, 40, n_kv, hd, page)
+    poison_behind(cache, lens)
+    q, out = run_rows(L, cache, [1] * batch, lens, n_q, n_kv, hd, 0, 291)
+    assert L.status() == 0
+    k8, v8, ks, vs, table = cache
+    check_attention(q[:300], out[:300].cpu(), (k8, v8, ks, vs, table[:300]), [1] * 300, lens[:300], n_q, n_kv, hd, 0)
+    check_attention(q[-300:], out[-300:].cpu(), (k8, v8, ks, vs, table[-300:]), [1] * 300, lens[-300:], n_q, n_kv, hd, 0)
