@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(256, HD == 256 ? 2 : 4) append8_kernel(const _
   const int row0 = a.cu ? __ldg(a.cu + b) : b * a.rows;
   const int n = a.cu ? __ldg(a.cu + b + 1) - row0 : a.rows;
   const int start = a.start ? __ldg(a.start + b) : a.pos0;
-  bool bad = n > a.rows || start < 0 || start > 0x7ffffff0 - a.rows;
+  bool bad = (n > 0) & ((n > a.rows) | (start < 0) | (start > 0x7ffffff0 - a.rows));      // no rows: whatever the start is
   if (bad || n <= 0) {
     if (bad && lane == 0) atomicMin(p.status, (int)POP_E_INVALID);
     return;
@@ -356,7 +356,7 @@ __global__ void __launch_bounds__(256) append8_row_kernel(const __grid_constant_
   const int row = a.cu ? __ldg(a.cu + b) : b;
   const int n = a.cu ? __ldg(a.cu + b + 1) - row : 1;
   const int at = a.start ? __ldg(a.start + b) : a.pos0;                           // the row's cache position
-  bool bad = n > 1 || at < 0 || at > 0x7ffffff0 - 1;
+  bool bad = (n > 0) & ((n > 1) | (at < 0) | (at > 0x7ffffff0 - 1));              // no row: whatever the start is
   if (bad || n <= 0) {
     if (bad && threadIdx.x == 0) atomicMin(p.status, (int)POP_E_INVALID);
     return;

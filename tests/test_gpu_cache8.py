@@ -1170,3 +1170,14 @@ def test_few_rows_of_more_sequences_than_the_few_row_kernel_takes(L):
     k8, v8, ks, vs, table = cache
     check_attention(q[:300], out[:300].cpu(), (k8, v8, ks, vs, table[:300]), [1] * 300, lens[:300], n_q, n_kv, hd, 0)
     check_attention(q[-300:], out[-300:].cpu(), (k8, v8, ks, vs, table[-300:]), [1] * 300, lens[-300:], n_q, n_kv, hd, 0)
+
+
+@pytest.mark.parametrize("rows", [[1, 0, 1], [3, 0, 40]])
+@pytest.mark.parametrize("start", [-1, 2 ** 31 - 1])
+def test_append_to_no_rows_takes_any_start(L, rows, start):
+    """A slot without a sequence: there is no first row whose position could be wrong."""
+    case = ([20, 5, 33], rows, 2, 1, 64, 16, False, False, 1)
+    a = append_inputs(case, 300)
+    cache = random_cache(301, 1, 3, 100, 1, 64, 16)
+    a.starts[1] = start
+    check_append(case, a, cache, *run_append(L, case, a, cache))
