@@ -763,12 +763,13 @@ template <int HD, int NQT>
 __global__ void __launch_bounds__(256) attn8_merge_kernel(const __grid_constant__ A8Dev p, int* __restrict__ status) {
   chain_trigger();
   chain_wait();
-  if (gave_up(*reinterpret_cast<const volatile int*>(status))) return;      // there are pieces that nobody wrote
+  // read once per CTA, while the lengths are on their way: 3 x 512 rows 239 us, with every warp's read of the one word 243
+  const int word = threadIdx.x == 0 ? *reinterpret_cast<const volatile int*>(status) : 0;
   const int groups = NQT * 128 / 8;
   const int by = blockIdx.y / groups, r = (blockIdx.y % groups) * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
   const Job x = job_of<NQT>(p, blockIdx.x, by, blockIdx.z, status);
   const int pieces = pieces_of(p, x);
-  if (x.q0 < 0 || pieces == 1) return;
+  if (__syncthreads_or(gave_up(word)) || x.q0 < 0 || pieces == 1) return;   // gave up: there are pieces that nobody wrote
   const int in_tile = r & 127, ip = row_pos(x, in_tile), i = x.q0 + (r >> 7) * x.per + ip;
   if (in_tile >= x.per * x.heads || i >= x.n) return;
   constexpr int PER = HD / 32;
