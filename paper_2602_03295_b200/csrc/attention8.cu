@@ -26,10 +26,11 @@
 //   a scale warp: the scales of 32 blocks at a time, converted, in a small ring.
 // Where few CTAs would leave SMs idle or wait for the longest sequence, the keys are split over several CTAs, which leave
 // unnormalised rows in the workspace for a second, chained launch to merge (512 rows each of three sequences of up to
-// 16384, which are 192 CTAs of unequal length: 290 us in one piece, 237 us in two).
+// 16384, which are 192 CTAs of unequal length: 290 us in one piece, 242 us in two).
 //
-// Measured, causal, 32 heads over 8, hd 128: 8192 rows of 8192 551 us, 998 TFLOP/s (0.60 of a bf16 GEMM's); hd 256, 16 over
-// 8, window 1024: 8192 rows 191 us; 512 rows each of three sequences of up to 16384 239 us. Bound by the softmax warps'
+// Measured in captured graphs, causal, 32 heads over 8, hd 128: 8192 rows of 8192 550 us, 1000 TFLOP/s (0.60 of a bf16 GEMM's;
+// 603 us after a second of calls, when the power cap has brought the clock from 1965 to 1777 MHz; hd 64 509 us); hd 256,
+// 16 over 8, window 1024: 8192 rows 190 us; 512 rows each of three sequences of up to 16384 242 us (hd 64 224). Bound by the softmax warps'
 // dependent steps: 1980 clocks per 64 keys, of which the exponential unit works 1024 (two warps of a scheduler) and the tensor
 // pipe 1280; halving the exponentials (a copy, to see) took 14 % off, leaving out the row maximum 3 %, the V conversion
 // nothing. A CTA's start takes 13000 clocks and its end 4500, of 145000 (hd 256 with the window: of 50000). Tried and slower:
@@ -763,7 +764,7 @@ template <int HD, int NQT>
 __global__ void __launch_bounds__(256) attn8_merge_kernel(const __grid_constant__ A8Dev p, int* __restrict__ status) {
   chain_trigger();
   chain_wait();
-  // read once per CTA, while the lengths are on their way: 3 x 512 rows 239 us, with every warp's read of the one word 243
+  // read once per CTA, while the lengths are on their way: 3 x 512 rows 238.8 us, with every warp's read of the one word 242.5
   const int word = threadIdx.x == 0 ? *reinterpret_cast<const volatile int*>(status) : 0;
   const int groups = NQT * 128 / 8;
   const int by = blockIdx.y / groups, r = (blockIdx.y % groups) * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;

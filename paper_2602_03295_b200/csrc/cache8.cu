@@ -177,8 +177,8 @@ __device__ __forceinline__ uint32_t rescaled4(uint32_t w, float f) {
 // one row, each four rotation pairs (j, j + hd/2): two 16-byte loads of fp32 (8-byte of bf16). The rows stay in registers
 // until the block's maximum is known, which the two warps exchange (one warp for all 16 rows: 128 registers, 72 us for 6656
 // rows of 32 + 16 heads; two warps at four CTAs per SM 57 us, 4.0 TB/s; the bytes take 35). Bound by the loads that the
-// resident warps keep in flight. A CTA is four heads of the same
-// rows, so the rotary rows come from L1 after the first.
+// resident warps keep in flight: bf16 rows, with half the bytes in each, take 63 us where the bytes take 23. A CTA is four
+// heads of the same rows, so the rotary rows come from L1 after the first.
 struct Append8Dev {
   Append8Args a;
   int head_groups;              // CTAs per block of positions: four heads each
@@ -340,7 +340,8 @@ __global__ void __launch_bounds__(256, HD == 256 ? 2 : 4) append8_kernel(const _
 // The form of one row per sequence, a decode step: hd / 8 lanes per (sequence, head), one CTA for 256 / (hd / 8) heads. The
 // same arithmetic; the codes that a larger scale brings along are the only thing beyond one row. Bound by its chain of
 // loads (start, page, old scale); the kernel above, whose lanes would be empty in 15 of 16 slots, took 9.3 us for 96
-// sequences of 32 + 16 heads (two rounds of CTAs), this one 3.3; one sequence 2.8 and 1.9.
+// sequences of 32 + 16 heads (two rounds of CTAs), this one 3.3; one sequence 2.8 and 1.8 (in a captured
+// graph; an eager call's host time is 15 or more).
 template <int HD, bool IN_BF16>
 __global__ void __launch_bounds__(256) append8_row_kernel(const __grid_constant__ Append8Dev p) {
   constexpr int LPR = HD / 8, HALF = HD / 2;

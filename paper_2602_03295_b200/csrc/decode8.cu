@@ -26,11 +26,11 @@
 //     second, chained launch (a CTA that lies inside one item merges its eight in shared memory first).
 // More than eight columns are several items, which read the same keys one after another from L2. (Two groups of columns
 // per item, for one reading and conversion of the values, had one warp's registers full and were slower: five rows each of
-// twelve sequences of up to 8000, 20 columns, 48.6 against 38.7 us.)
+// twelve sequences of up to 8000, 20 columns, 48.6 against 39.0 us.)
 //
 // Measured, hd 128, 32 heads over 8: 48 sequences of up to 16001 positions 142 us, 5.8 TB/s of the cache's bytes (0.88 of a
-// copy's rate); one of 8192 11.0 us, where starting, one round through memory and merging are nearly all; hd 256, 20 windows
-// of 1024 28.8 us: the blocks are read at the memory's rate in 11 us, the rest is the start (5.5 us: lengths, table, first
+// copy's rate); one of 8192 11.1 us, where starting, one round through memory and merging are nearly all; hd 256, 20 windows
+// of 1024 29.1 us: the blocks are read at the memory's rate in 11 us, the rest is the start (5.5 us: lengths, table, first
 // blocks) and the second launch.
 #include "../../include/pop_kernels.h"
 #include "cache8.cuh"
@@ -793,7 +793,7 @@ int launch_t(const Attn8Args& a, Dec8Dev& p, cudaStream_t s) {
       c8_allow_smem(configured, reinterpret_cast<const void*>(dec8_kernel<HD>), C::SMEM + (MAX_BATCH + 1) * 4);
   // One launch, a CTA or a cluster per item, where no warp gets more than CLUSTER_BLOCKS blocks and the CTAs are resident
   // at once; two rounds of CTAs pay up to eight blocks per warp, any number up to four. Against the line and its second
-  // launch, hd 128, 8 kv heads (us): 1 x 8192 positions 11.0 / 14.5, 1 x 2000 7.0 / 14.2, 9 x 2000 13.0 / 21.2, 18 x 1000 12.2
+  // launch, hd 128, 8 kv heads (us): 1 x 8192 positions 11.1 / 14.5, 1 x 2000 7.0 / 14.2, 9 x 2000 13.0 / 21.2, 18 x 1000 12.2
   // / 19.9, 18 x 2000 17.8 / 26.1; two rounds 20 x 1000 19.7 / 20.0 (unequal lengths 13.0 / 16.4), 30 x 1000 21.6 / 23.3, but 20 x
   // 2000 29.7 / 27.2. And 2 x 8192 in clusters of 8, which are not all resident, 21.2 against 16.5 in those of 4.
   int cs = 1;
