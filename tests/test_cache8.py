@@ -163,6 +163,7 @@ def test_conversion_of_lengths_behind_the_largest_is_refused(library):
 
 def test_the_count_of_sms_is_asked_for_once_by_all_threads(tmp_path):
     """The host code under ThreadSanitizer: two threads whose first calls come at the same time."""
+    import os
     import subprocess
     from paper_2602_03295_b200 import _build
     (tmp_path / "main.cu").write_text("""
@@ -176,10 +177,13 @@ int main() {
   return a == b && a > 0 ? 0 : 1;
 }
 """)
-    flags = ["/usr/local/cuda/bin/nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-O1", "-std=c++17", "-Xcompiler", "-fsanitize=thread"]
+    flags = [os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"), "-gencode", "arch=compute_100a,code=sm_100a", "-O1", "-std=c++17",
+             "-Xcompiler", "-fsanitize=thread"]
     files = [tmp_path / "main.cu"] + [_build.CSRC + "/" + n for n in ("cache8.cu", "runtime.cu")]
     subprocess.run(flags + ["-o", str(tmp_path / "race")] + [str(f) for f in files], check=True, capture_output=True, text=True)
     got = subprocess.run([str(tmp_path / "race")], capture_output=True, text=True, timeout=120)
+    if "unexpected memory mapping" in got.stderr:
+        pytest.skip("ThreadSanitizer cannot place its memory under this kernel's address randomisation")
     assert got.returncode == 0, got.stderr[-3000:]
 
 
