@@ -30,10 +30,10 @@
 //
 // Measured in captured graphs, causal, 32 heads over 8, hd 128: 8192 rows of 8192 550 us, 1000 TFLOP/s (0.60 of a bf16 GEMM's;
 // 603 us after a second of calls, when the power cap has brought the clock from 1965 to 1777 MHz; hd 64 509 us); hd 256,
-// 16 over 8, window 1024: 8192 rows 190 us; 512 rows each of three sequences of up to 16384 242 us (hd 64 224). Bound by the softmax warps'
-// dependent steps: 1980 clocks per 64 keys, of which the exponential unit works 1024 (two warps of a scheduler) and the tensor
-// pipe 1280; halving the exponentials (a copy, to see) took 14 % off, leaving out the row maximum 3 %, the V conversion
-// nothing. A CTA's start takes 13000 clocks and its end 4500, of 145000 (hd 256 with the window: of 50000). Tried and slower:
+// 16 over 8, window 1024: 8192 rows 190 us; 512 rows each of three sequences of up to 16384 242 us (hd 64 224). Bound by
+// the softmax warps' dependent steps: 1980 clocks per 64 keys, of which the exponential unit works 1024 (two warps of a
+// scheduler) and the tensor pipe 1280; halving the exponentials (a copy, to see) took 14 % off, leaving out the row maximum
+// 3 %, the V conversion nothing. A CTA's start takes 13000 clocks and its end 4500, of 145000 (hd 256 with the window: of 50000). Tried and slower:
 // one CTA per SM that walks equal shares of all tiles (898 us; the segments' starts and the live state cost more than the
 // balance gave), the next tile's scores or scales asked for before this one's weights are stored (551 to 569 against 556),
 // query rows by bulk copies (570).
