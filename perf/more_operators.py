@@ -14,7 +14,8 @@ row i of a sequence follows another row of it, or the last cached token. One ste
 
 4-bit weights lie as the kernels read them: tiles of 16 rows and 128 inputs, codes uint8 [rows / 16][inputs / 128][16][64].
 The 64 bytes of a row are 16 words of 8 codes, word 4 t + j for inputs 32 j + 8 t .. + 7; nibble p of a word is the code of its
-input 2 p, or 2 (p - 4) + 1 from p = 4 on. Scales bf16 and zeros uint8 [rows / 16][groups][16].
+input 2 p, or 2 (p - 4) + 1 from p = 4 on. Scales bf16 and zeros uint8 [rows / 16][inputs / 128][16][128 / group], row r of a
+tile at 2 (r % 8) + r / 8.
 
 `own` false: elementary torch operations in fp32, for whole batches; `own` true: the library's calls.
 """
@@ -165,8 +166,8 @@ def _weights(s):
     at = torch.tensor([0, 16, 4, 20, 8, 24, 12, 28], dtype=torch.int32, device=codes.device)
     c = (word[..., None] >> at) & 15                                                   # [.., row, t, j, input of the word]
     c = c.permute(0, 2, 1, 4, 3, 5).reshape(nt * 16, kt * 128)[:s["n"], :s["k"]]
-    group_of = torch.arange(s["k"], device=codes.device) // s["group"]
-    per_group = lambda v: v.permute(0, 2, 1).reshape(nt * 16, -1)[:s["n"]][:, group_of]  # noqa: E731
+    per_group = lambda v: (v.view(nt, kt, 8, 2, -1).permute(0, 3, 2, 1, 4).reshape(nt * 16, -1)[:s["n"]]  # noqa: E731
+                           .repeat_interleave(s["group"], 1)[:, :s["k"]])
     zero = 8 if s["zeros"] is None else per_group(s["zeros"]).int()
     return (c - zero).float() * per_group(s["scales"]).float()
 
@@ -301,12 +302,12 @@ def _rope_rows(n, hd, theta=1e6):
 
 def _prepare_gemv(c, g):
     n, k, rows, group = c["n"], c["k"], c["rows"], c["group"]
-    nt, kt, groups = -(-n // 16), -(-k // 128), -(-k // group)
+    nt, kt, shape = -(-n // 16), -(-k // 128), (-(-n // 16), -(-k // 128), 16, 128 // group)
     s = {"op": "gemv", "mode": c["mode"], "n": n, "k": k, "group": group}
     s["codes"] = torch.randint(0, 256, (nt, kt, 16, 64), generator=g, device=DEV, dtype=torch.uint8)
     # weights of a size of 1 / sqrt(k) with unequal groups
-    s["scales"] = ((0.5 + torch.rand(nt, groups, 16, generator=g, device=DEV)) * 0.25 / math.sqrt(k)).to(torch.bfloat16)
-    s["zeros"] = torch.randint(5, 12, (nt, groups, 16), generator=g, device=DEV, dtype=torch.uint8) if c["zeros"] else None
+    s["scales"] = ((0.5 + torch.rand(shape, generator=g, device=DEV)) * 0.25 / math.sqrt(k)).to(torch.bfloat16)
+    s["zeros"] = torch.randint(5, 12, shape, generator=g, device=DEV, dtype=torch.uint8) if c["zeros"] else None
     s["x"] = torch.randn(rows, k, generator=g, device=DEV).to(torch.bfloat16)
     if c["mode"] == "gated":
         s["out"] = torch.empty(rows, n // 2, dtype=torch.bfloat16, device=DEV)
@@ -403,8 +404,9 @@ def _exact_gemv(s):
         r = torch.arange(r0, min(n, r0 + 4096), device=DEV)[:, None]
         b = s["codes"][r // 16, (i // 128)[None], r % 16, byte[None]].long()
         code = torch.where(high[None] == 1, b // 16, b % 16).double()
-        scale = s["scales"][r // 16, (i // group)[None], r % 16].double()
-        zero = 8.0 if s["zeros"] is None else s["zeros"][r // 16, (i // group)[None], r % 16].double()
+        where = r // 16, (i // 128)[None], r % 8 * 2 + r % 16 // 8, (i % 128 // group)[None]
+        scale = s["scales"][where].double()
+        zero = 8.0 if s["zeros"] is None else s["zeros"][where].double()
         y[:, r0:r0 + r.shape[0]] = x @ ((code - zero) * scale).t()
     if s["mode"] == "add":
         return [s["out"].double() + y]
