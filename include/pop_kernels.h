@@ -274,6 +274,80 @@ int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int
                          int32_t kv_len, void* workspace, size_t workspace_bytes, void* out, int64_t ldo,
                          int32_t batch, int32_t n_q, int32_t n_kv, int32_t head_dim, int32_t window, void* stream);
 
+/* ---------------------------------------------------------------------------------------------------
+ * A step that checks drafted tokens: several tokens of each sequence go through the full model at once (the decode stage of
+ * paper Sec. 3.2 for more than one position), in the form of a tree whose rows each follow another row or the last cached
+ * token. Projections of few rows with 4-bit weights, the append of the rows, their attention, and keeping of the path that was
+ * accepted. Device-side checks as for the 8-bit cache: what the host cannot see (block-table entries, lengths, lists) is
+ * never turned into an address where it is wrong; the status word is raised to POP_E_INVALID, and other sequences, and calls
+ * made while the word holds POP_E_INVALID, are not touched by it.
+ *
+ * 4-bit weights W [N][K]: weight = (code - zero) * scale with codes 0 .. 15, and for every `group` (32, 64 or 128) consecutive
+ * inputs of a row one scale (bf16) and one zero (uint8, 0 .. 15; zeros NULL: 8). They lie in tiles of 16 rows and 128 inputs:
+ *   codes  uint8 [ceil(N / 16)][ceil(K / 128)][16][64]: the 64 bytes of a row are 16 32-bit words of 8 codes, word 4 t + j for
+ *          inputs 32 j + 8 t .. + 7 of the 128; bits 4 p .. 4 p + 3 of a word are the code of its input 2 p (p < 4) or
+ *          2 (p - 4) + 1;
+ *   scales bf16, zeros uint8 [ceil(N / 16)][ceil(K / 128)][16][128 / group]: row r of the tile at index 2 (r % 8) + r / 8.
+ * What lies behind row N or input K is read and has no effect, whatever it is. codes and scales 16-byte aligned, zeros 8-byte.
+ *
+ * pop_k_gemv_w4: pop_k_gemv with such weights: out[b][n] = sum_k x[b][k] W[n][k], x bf16 [B][ldx] (16-byte aligned, ldx and K
+ * multiples of 8), any B (made for 1 to some dozens of rows). Modes as pop_k_gemv: 0 fp32 store, 2 fp32 +=, 3 gated -> bf16
+ * (N a multiple of 256: 128 gate rows, then the 128 matching up rows; act 0 SiLU, 1 tanh-GELU). A group's products are summed
+ * exactly formed and in fp32, then scaled and summed in fp32 in an order that depends on the sizes alone. */
+int pop_k_gemv_w4(const void* x, int64_t ldx, const void* codes, const void* scales, const void* zeros, int32_t group,
+                  void* out, int64_t ldo, int32_t B, int32_t N, int32_t K, int32_t mode, int32_t act, int32_t n_valid,
+                  void* stream);
+
+/* pop_k_rope_cache for drafted rows. in: projections [q heads | k heads | v heads] * hd of `rows` packed rows, fp32 or
+ * (in_bf16) bf16, row stride ld_in (a multiple of 4; 16-byte aligned). Sequence b owns rows cu_rows[b] .. cu_rows[b + 1] - 1
+ * (device int32 [batch + 1], at most max_rows each), or rows b * max_rows .. if cu_rows is NULL; in front of them it has
+ * start[b] cached positions (device int32 [batch]), or pos0 for all if start is NULL. Row i of the sequence goes to cache slot
+ * start + i and has the rotary position start + depth[row] (device int32 [rows], row = packed row: 0 for rows that follow the
+ * last cached token, one more than the row that it follows for the others; NULL: i, a chain). Per row: optional per-head
+ * RMSNorm of q and k (q_gain / k_gain fp32 [hd] or NULL; eps), rotation of q and k by rope_table[position] (float2
+ * [table_rows][hd/2], 16-byte aligned), q to q_out (bf16, row stride ldq, a multiple of 4; n_q may be 0), k and v to the
+ * cache (one layer, pop_kv_cache_t's layout). A row whose position is outside the table is rotated by its row 0 (status word). */
+int pop_k_rope_cache_tree(const void* in, int32_t in_bf16, int64_t ld_in, int32_t rows, const int32_t* cu_rows,
+                          int32_t max_rows, const int32_t* start, int32_t pos0, const int32_t* depth, int32_t batch,
+                          void* q_out, int64_t ldq, void* k_pool, void* v_pool, const int32_t* block_table,
+                          int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, const float* q_gain,
+                          const float* k_gain, float eps, const void* rope_table, int32_t table_rows, int32_t n_q,
+                          int32_t n_kv, int32_t head_dim, void* stream);
+
+/* Workspace of the call below: device memory, 16-byte aligned, contents irrelevant before and after. This size covers every
+ * call; a smaller one is refused with POP_E_NOSPACE where the call needs more. Calls that may overlap on the GPU (other
+ * streams, concurrently replayed graphs) need one each. */
+#define POP_TREE_WORKSPACE_BYTES (64 * 1024 * 1024)
+
+/* Attention of drafted rows over the paged cache (one layer) that has them already: packed rows, cu_rows, max_rows and start
+ * as above (start[b] <= max_start; max_start for all if start is NULL). Row i sees the start positions in front of the draft,
+ * and of the sequence's drafted slots those whose bit is set in its mask: mask device uint32 [rows][mask_words], slot j is bit
+ * j % 32 of word j / 32 (mask_words * 32 >= max_rows; the row's own slot is a bit like the others; bits behind the sequence's
+ * rows have no effect; NULL: slots 0 .. i, a chain). window > 0: only of positions within the last `window` of the row's, its
+ * own included; a drafted slot's position is start + its depth (as above; NULL: a chain).
+ * q bf16 [rows][ldq], out bf16 [rows][ldo] (strides multiples of 8, at least n_q hd; 16-byte aligned), n_q / n_kv <= 128,
+ * batch <= 4096, hd 64, 128 or 256. A row that sees nothing becomes zeros; rows of no sequence are left as they are. Positions
+ * behind a sequence's rows and in front of every row's window may hold anything, their block-table entries too where a whole
+ * page does. An infinite or NaN value in a drafted slot may reach rows of the sequence that do not see the slot. Unequal
+ * lengths are shared out over the whole GPU; results do not depend on scheduling. The key tiles of 64 positions of the call,
+ * batch n_kv ceil(max_rows / rows per tile) ceil((max_start + max_rows) / 64), are at most 2^30 (POP_E_INVALID otherwise). */
+int pop_k_tree_attention(const void* q, int64_t ldq, int32_t rows, const int32_t* cu_rows, int32_t max_rows,
+                         const int32_t* start, int32_t max_start, const void* mask, int32_t mask_words,
+                         const int32_t* depth, const void* k_pool, const void* v_pool, const int32_t* block_table,
+                         int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, void* workspace,
+                         size_t workspace_bytes, void* out, int64_t ldo, int32_t batch, int32_t n_q, int32_t n_kv,
+                         int32_t head_dim, int32_t window, void* stream);
+
+/* Keeps the accepted path of every sequence: the entries of drafted slots kept[b][0] < kept[b][1] < ... move to slots 0, 1,
+ * ... of the draft (cache positions start + i), in `layers` consecutive layers (layer_stride elements apart) of K and V.
+ * kept: device int32 [batch][ld_kept], the first n_kept[b] (device int32 [batch], at most max_kept; NULL: max_kept) of a
+ * row; max_kept <= 1024. start / pos0 as above. The other entries stay as they are. A sequence whose list does not rise or
+ * leaves its block table or the pool is left as it is (status word). */
+int pop_k_cache_keep(void* k_pool, void* v_pool, int64_t layer_stride, int32_t layers, const int32_t* block_table,
+                     int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, const int32_t* kept,
+                     int64_t ld_kept, const int32_t* n_kept, int32_t max_kept, const int32_t* start, int32_t pos0,
+                     int32_t batch, int32_t n_kv, int32_t head_dim, void* stream);
+
 /* Synchronise the stream, then read and clear the library's device status word. */
 int pop_k_status(void* stream);
 

@@ -21,6 +21,7 @@ POP_E_CUDA = -3
 POP_E_DEVICE_TIMEOUT = -4
 POP_E_MISSING = -5
 POP_E4M3_WORKSPACE_BYTES = 64 << 20     # workspace that covers every attention call over the 8-bit cache
+POP_TREE_WORKSPACE_BYTES = 64 << 20     # workspace that covers every attention call of drafted rows
 
 
 class PopError(RuntimeError):
@@ -113,6 +114,13 @@ SIGNATURES = {
                                        _P, _I64] + [_I32] * 5 + [_P]),
     "pop_k_profile": (None, [_I32]),
     "pop_k_profile_summary": (C.c_int, [_I32, C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(_I64)]),
+    "pop_k_gemv_w4": (C.c_int, [_P, _I64, _P, _P, _P, _I32, _P, _I64] + [_I32] * 6 + [_P]),
+    "pop_k_rope_cache_tree": (C.c_int, [_P, _I32, _I64, _I32, _P, _I32, _P, _I32, _P, _I32, _P, _I64, _P, _P, _P, _I32, _I32,
+                                        _I32, _P, _P, _F, _P] + [_I32] * 4 + [_P]),
+    "pop_k_tree_attention": (C.c_int, [_P, _I64, _I32, _P, _I32, _P, _I32, _P, _I32, _P, _P, _P, _P, _I32, _I32, _I32, _P,
+                                       C.c_size_t, _P, _I64] + [_I32] * 5 + [_P]),
+    "pop_k_cache_keep": (C.c_int, [_P, _P, _I64, _I32, _P, _I32, _I32, _I32, _P, _I64, _P, _I32, _P, _I32, _I32, _I32, _I32,
+                                   _P]),
     "pop_k_status": (C.c_int, [_P]),
     "pop_k_wait_selftest": (C.c_int, [_I64, _P]),
     "pop_k_launch_count": (_I64, []),
@@ -492,7 +500,7 @@ class PopLibrary:
         return q_out
 
     @staticmethod
-    def _attn8_rows(q, out, width, workspace, stream):
+    def _attn8_rows(q, out, width, workspace, stream, workspace_bytes=POP_E4M3_WORKSPACE_BYTES):
         """Checks queries and outputs; returns (rows, strides of both, workspace, its bytes)."""
         rows, w = q.shape
         ldq, q_inner = q.stride()
@@ -504,7 +512,7 @@ class PopLibrary:
             # from the pool of the stream that runs the call: its memory has no work of another stream in front of it, and
             # goes back, when the call returns, to that stream's later work
             with torch.cuda.stream(stream):
-                workspace = torch.empty(POP_E4M3_WORKSPACE_BYTES, dtype=torch.uint8, device=q.device)
+                workspace = torch.empty(workspace_bytes, dtype=torch.uint8, device=q.device)
         elif not workspace.is_contiguous():
             raise PopError(POP_E_INVALID, "workspace has to be contiguous")
         return rows, ldq, ldo, workspace, workspace.numel() * workspace.element_size()
@@ -545,6 +553,137 @@ class PopLibrary:
             self.check(code, "pop_k_attention_e4m3")
         return out
 
+    # -------------------------------------------------------------- a step that checks drafted tokens
+    @staticmethod
+    def _here(t, others, what):
+        """The current stream, where t and all of `others` (None left out) are on the current CUDA device."""
+        at = t.get_device()
+        if at < 0 or at != torch._C._cuda_getDevice():
+            raise PopError(POP_E_INVALID, f"{what}: tensors on the current CUDA device are wanted")
+        for o in others:
+            if o is not None and o.get_device() != at:
+                raise PopError(POP_E_INVALID, f"{what}: all tensors have to be on the current CUDA device")
+        return torch._C._cuda_getCurrentRawStream(at)
+
+    def gemv_w4(self, x, codes, scales, zeros, out, n, group, mode=0, act=0, n_valid=None, stream=None):
+        """pop_k_gemv_w4: x bf16 [B, K]; codes uint8 [ceil(n / 16), ceil(K / 128), 16, 64], scales bf16 and zeros uint8 (or
+        None) [.., .., 16, 128 / group] as `pack_w4` lays them out; out fp32 [B, n], or bf16 [B, n_valid] (n / 2 if not given)
+        for mode 3."""
+        here = self._here(x, (codes, scales, zeros, out), "gemv_w4")
+        B, K = x.shape
+        ldx, inner = x.stride()
+        shape = (-(-n // 16), -(-K // 128), 16, 128 // group if group else 0)
+        if x.dtype != torch.bfloat16 or inner != 1 or codes.dtype != torch.uint8 or codes.shape != shape[:3] + (64,) or \
+                not codes.is_contiguous():
+            raise PopError(POP_E_INVALID, "gemv_w4: x is bf16 [B, K], codes contiguous uint8 tiles of n rows and K inputs")
+        if scales.dtype != torch.bfloat16 or scales.shape != shape or not scales.is_contiguous() or \
+                (zeros is not None and (zeros.dtype != torch.uint8 or zeros.shape != shape or not zeros.is_contiguous())):
+            raise PopError(POP_E_INVALID, "gemv_w4: contiguous bf16 scales and uint8 zeros of the tiles' groups are wanted")
+        width = n if mode != 3 else n // 2 if n_valid is None else n_valid
+        ldo, inner = out.stride()
+        if out.dtype != (torch.bfloat16 if mode == 3 else torch.float32) or out.shape[0] != B or out.shape[1] < width or inner != 1:
+            raise PopError(POP_E_INVALID, "gemv_w4: out is fp32 [B, n], or bf16 [B, n_valid] for the gated form")
+        if B == 0:
+            return out
+        code = self.dll.pop_k_gemv_w4(
+            x.data_ptr(), ldx, codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), group,
+            out.data_ptr(), ldo, B, n, K, mode, act, width, here if stream is None else stream.cuda_stream)
+        if code:
+            self.check(code, "pop_k_gemv_w4")
+        return out
+
+    @staticmethod
+    def _layer16(k_pool, v_pool, block_table, n_kv, hd, what):
+        """(page_size, num_pages, max_pages, batch) of one layer of the bf16 cache."""
+        shape = k_pool.shape
+        if len(shape) != 4 or shape[2] != n_kv or shape[3] != hd or v_pool.shape != shape or \
+                k_pool.dtype != torch.bfloat16 or v_pool.dtype != torch.bfloat16 or block_table.dtype != torch.int32 or \
+                not (k_pool.is_contiguous() and v_pool.is_contiguous() and block_table.is_contiguous()):
+            raise PopError(POP_E_INVALID, f"{what}: contiguous bf16 pools [pages, page_size, n_kv, hd] and an int32 block table are wanted")
+        batch, max_pages = block_table.shape
+        return shape[1], shape[0], max_pages, batch
+
+    def rope_cache_tree(self, x, q_out, k_pool, v_pool, block_table, rope_table, n_q, n_kv, hd, max_rows, start=None, pos0=0,
+                        cu_rows=None, depth=None, q_gain=None, k_gain=None, eps=0.0, stream=None):
+        """pop_k_rope_cache_tree: x fp32 or bf16 [rows, (n_q + 2 n_kv) hd]; q_out bf16 [rows, n_q hd] (None if n_q is 0); one
+        layer's pools bf16 [pages, page_size, n_kv, hd]; rope_table fp32 [positions, hd / 2, 2]; start int32 [batch] or pos0
+        for all; cu_rows int32 [batch + 1] or max_rows rows each; depth int32 [rows] or None (a chain)."""
+        what = "rope_cache_tree"
+        here = self._here(x, (q_out, k_pool, v_pool, block_table, rope_table, start, cu_rows, depth, q_gain, k_gain), what)
+        page, pages, max_pages, batch = self._layer16(k_pool, v_pool, block_table, n_kv, hd, what)
+        rows, width = x.shape
+        bf16 = x.dtype == torch.bfloat16
+        ld_in, inner = x.stride()
+        if not (bf16 or x.dtype == torch.float32) or width != (n_q + 2 * n_kv) * hd or inner != 1:
+            raise PopError(POP_E_INVALID, f"{what}: x is fp32 or bf16 [rows, (n_q + 2 n_kv) hd]")
+        q_ptr, ldq = None, 0
+        if n_q:
+            ldq, inner = q_out.stride()
+            q_ptr = q_out.data_ptr()
+            if q_out.dtype != torch.bfloat16 or q_out.shape != (rows, n_q * hd) or inner != 1:
+                raise PopError(POP_E_INVALID, f"{what}: q_out is bf16 [rows, n_q hd]")
+        table_rows = rope_table.numel() // hd
+        if rope_table.dtype != torch.float32 or table_rows * hd != rope_table.numel() or not rope_table.is_contiguous():
+            raise PopError(POP_E_INVALID, f"{what}: rope_table is fp32 [positions, hd / 2, 2]")
+        for g in (q_gain, k_gain):
+            if g is not None and (g.dtype != torch.float32 or g.numel() != hd or not g.is_contiguous()):
+                raise PopError(POP_E_INVALID, f"{what}: gains are fp32 [hd]")
+        if rows == 0:
+            return q_out
+        code = self.dll.pop_k_rope_cache_tree(
+            x.data_ptr(), 1 if bf16 else 0, ld_in, rows, self._ints(cu_rows, batch + 1, "cu_rows"), max_rows,
+            self._ints(start, batch, "start"), pos0, self._ints(depth, rows, "depth"), batch, q_ptr, ldq, k_pool.data_ptr(),
+            v_pool.data_ptr(), block_table.data_ptr(), page, pages, max_pages, _ptr(q_gain), _ptr(k_gain), eps,
+            rope_table.data_ptr(), table_rows, n_q, n_kv, hd, here if stream is None else stream.cuda_stream)
+        if code:
+            self.check(code, "pop_k_rope_cache_tree")
+        return q_out
+
+    def tree_attention(self, q, k_pool, v_pool, block_table, out, n_q, n_kv, hd, max_rows, max_start, start=None, cu_rows=None,
+                       mask=None, depth=None, window=0, workspace=None, stream=None):
+        """pop_k_tree_attention: q, out bf16 [rows, n_q hd]; one layer's pools; start int32 [batch] (each <= max_start) or
+        max_start for all; mask int32 [rows, words] of `tree_mask`, or None (a chain); depth int32 [rows] or None (a chain),
+        used with a window only. `workspace` (POP_TREE_WORKSPACE_BYTES of any dtype) is allocated if not given."""
+        what = "tree_attention"
+        here = self._here(q, (k_pool, v_pool, block_table, out, start, cu_rows, mask, depth, workspace), what)
+        page, pages, max_pages, batch = self._layer16(k_pool, v_pool, block_table, n_kv, hd, what)
+        rows, ldq, ldo, ws, nbytes = self._attn8_rows(q, out, n_q * hd, workspace, stream, POP_TREE_WORKSPACE_BYTES)
+        words = 0
+        if mask is not None:
+            words = mask.shape[-1]
+            if mask.dtype != torch.int32 or mask.shape != (rows, words) or not mask.is_contiguous():
+                raise PopError(POP_E_INVALID, f"{what}: mask is contiguous int32 [rows, words]")
+        if rows == 0:
+            return out
+        code = self.dll.pop_k_tree_attention(
+            q.data_ptr(), ldq, rows, self._ints(cu_rows, batch + 1, "cu_rows"), max_rows, self._ints(start, batch, "start"),
+            max_start, None if mask is None else mask.data_ptr(), words, self._ints(depth, rows, "depth"), k_pool.data_ptr(),
+            v_pool.data_ptr(), block_table.data_ptr(), page, pages, max_pages, ws.data_ptr(), nbytes, out.data_ptr(), ldo,
+            batch, n_q, n_kv, hd, window, here if stream is None else stream.cuda_stream)
+        if code:
+            self.check(code, "pop_k_tree_attention")
+        return out
+
+    def cache_keep(self, k_pool, v_pool, block_table, kept, start=None, pos0=0, n_kept=None, stream=None):
+        """pop_k_cache_keep: pools bf16 [layers, pages, page_size, n_kv, hd], changed where they lie; kept int32 [batch, m]
+        rising slots of the draft, the first n_kept (int32 [batch]; all m if None) of each row; start int32 [batch] or pos0."""
+        here = self._here(k_pool, (v_pool, block_table, kept, start, n_kept), "cache_keep")
+        layers, pages, page, n_kv, hd = k_pool.shape
+        strides = k_pool.stride()
+        batch, max_pages = block_table.shape
+        if k_pool.dtype != torch.bfloat16 or v_pool.dtype != torch.bfloat16 or v_pool.shape != k_pool.shape or \
+                v_pool.stride() != strides or strides[1:] != (page * n_kv * hd, n_kv * hd, hd, 1):
+            raise PopError(POP_E_INVALID, "cache_keep: bf16 pools with contiguous layers, alike for K and V, are wanted")
+        if block_table.dtype != torch.int32 or not block_table.is_contiguous() or kept.dtype != torch.int32 or \
+                kept.shape[0] != batch or kept.stride(1) != 1:
+            raise PopError(POP_E_INVALID, "cache_keep: an int32 block table and int32 kept [batch, m] are wanted")
+        code = self.dll.pop_k_cache_keep(
+            k_pool.data_ptr(), v_pool.data_ptr(), strides[0], layers, block_table.data_ptr(), page, pages, max_pages,
+            kept.data_ptr(), kept.stride(0), self._ints(n_kept, batch, "n_kept"), kept.shape[1],
+            self._ints(start, batch, "start"), pos0, batch, n_kv, hd, here if stream is None else stream.cuda_stream)
+        if code:
+            self.check(code, "pop_k_cache_keep")
+
 
 _LIB: Optional[PopLibrary] = None
 
@@ -555,6 +694,80 @@ def lib() -> PopLibrary:
     if _LIB is None:
         _LIB = PopLibrary()
     return _LIB
+
+
+def pack_w4(codes, scales, zeros=None, group=128):
+    """4-bit weights as pop_k_gemv_w4 reads them, from codes uint8 [N, K] (0 .. 15), scales [N, ceil(K / group)] and zeros uint8
+    of the scales' shape or None (8), group 32, 64 or 128: (codes, scales, zeros) in tiles. Done once, when weights are loaded,
+    on the device that they are on."""
+    n, k = codes.shape
+    if group not in (32, 64, 128) or scales.shape != (n, -(-k // group)) or (zeros is not None and zeros.shape != scales.shape):
+        raise PopError(POP_E_INVALID, "pack_w4: scales and zeros are [N, ceil(K / group)] for a group of 32, 64 or 128")
+    nt, kt, per = -(-n // 16), -(-k // 128), 128 // group
+    c = torch.nn.functional.pad(codes, (0, kt * 128 - k, 0, nt * 16 - n))
+    c = c.view(nt, 16, kt, 4, 4, 8).permute(0, 2, 1, 4, 3, 5).to(torch.int64)             # [.., row, t, j, input of the word]
+    shift = torch.tensor([0, 16, 4, 20, 8, 24, 12, 28], device=codes.device)
+    word = ((c & 15) << shift).sum(-1)
+    tiles = torch.where(word >= 2 ** 31, word - 2 ** 32, word).to(torch.int32).contiguous().view(torch.uint8)
+
+    def grouped(v, dtype):
+        v = torch.nn.functional.pad(v.to(dtype), (0, kt * per - v.shape[1], 0, nt * 16 - n))
+        return v.view(nt, 2, 8, kt, per).permute(0, 3, 2, 1, 4).reshape(nt, kt, 16, per).contiguous()
+
+    return (tiles.view(nt, kt, 16, 64), grouped(scales, torch.bfloat16),
+            None if zeros is None else grouped(zeros, torch.uint8))
+
+
+def quantize_w4(w, group=128, symmetric=True):
+    """Round-to-nearest 4-bit weights of w [N, K], laid out by `pack_w4`. Symmetric: scale = bf16(max|w| / 7) of a group, code
+    = w / scale rounded, + 8. Else scale = bf16((max - min) / 15) with 0 between min and max, zero = -min / scale rounded."""
+    n, k = w.shape
+    groups = -(-k // group)
+    x = torch.nn.functional.pad(w.float(), (0, groups * group - k)).view(n, groups, group)
+    if symmetric:
+        scale, zero = x.abs().amax(-1) / 7, torch.full((n, groups), 8.0, device=w.device)
+    else:
+        lo, hi = x.amin(-1).clamp_max(0), x.amax(-1).clamp_min(0)
+        scale = (hi - lo) / 15
+    scale = torch.where(scale > 0, scale, 1.0).to(torch.bfloat16)
+    if not symmetric:
+        zero = (-lo / scale.float()).round().clamp(0, 15)
+    codes = ((x / scale.float()[..., None]).round() + zero[..., None]).clamp(0, 15).to(torch.uint8)
+    return pack_w4(codes.view(n, -1)[:, :k], scale, None if symmetric else zero.to(torch.uint8), group)
+
+
+def unpack_w4(codes, scales, zeros, n, k):
+    """The fp32 weights [n, k] that `pack_w4`'s tiles stand for (a host-side view for checks, and for prompts in bf16)."""
+    nt, kt = codes.shape[:2]
+    shift = torch.tensor([0, 16, 4, 20, 8, 24, 12, 28], dtype=torch.int32, device=codes.device)
+    c = (codes.view(torch.int32).view(nt, kt, 16, 4, 4, 1) >> shift) & 15
+    c = c.permute(0, 2, 1, 4, 3, 5).reshape(nt * 16, kt, -1, 128 // scales.shape[3])      # [row, chunk, group, input]
+
+    def of_rows(v):
+        return v.view(nt, kt, 8, 2, -1).permute(0, 3, 2, 1, 4).reshape(nt * 16, kt, -1, 1)
+
+    w = (c - (8 if zeros is None else of_rows(zeros).int())).float() * of_rows(scales).float()
+    return w.view(nt * 16, kt * 128)[:n, :k]
+
+
+def tree_mask(parents, cu_rows=None):
+    """(mask int32 [rows, words], depth int32 [rows]) of drafted trees, on the CPU. parents: for each packed row the row of its
+    sequence that it follows (smaller than its own), or -1 for the last cached token; cu_rows: the sequences' first rows and
+    the end (one sequence if not given). A row sees itself and the rows on its way up."""
+    parents = [int(v) for v in parents]
+    cu = [0, len(parents)] if cu_rows is None else [int(v) for v in cu_rows]
+    words = max([1] + [-(-(b - a) // 32) for a, b in zip(cu, cu[1:])])
+    mask, depth = torch.zeros(len(parents), words, dtype=torch.int64), torch.zeros(len(parents), dtype=torch.int32)
+    for a, b in zip(cu, cu[1:]):
+        for i in range(b - a):
+            up = parents[a + i]
+            if not -1 <= up < i:
+                raise PopError(POP_E_INVALID, f"tree_mask: row {i} of a sequence cannot follow row {up}")
+            if up >= 0:
+                mask[a + i] = mask[a + up]
+                depth[a + i] = depth[a + up] + 1
+            mask[a + i, i // 32] |= 1 << (i % 32)
+    return torch.where(mask >= 2 ** 31, mask - 2 ** 32, mask).to(torch.int32), depth
 
 
 def make_config(cfg) -> pop_config_t:

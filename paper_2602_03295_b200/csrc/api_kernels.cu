@@ -1,5 +1,7 @@
 // C-ABI wrappers for the kernel-level entry points declared in pop_kernels.h.
 #include "cache8.cuh"
+#include "tree.cuh"
+#include "w4.cuh"
 #include "../../include/pop_kernels.h"
 
 using namespace pop;
@@ -274,6 +276,72 @@ int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int
   a.batch = batch; a.n_q = n_q; a.n_kv = n_kv; a.head_dim = head_dim; a.window = window;
   a.workspace = workspace; a.workspace_bytes = workspace ? workspace_bytes : 0;
   return launch_attention8(a, static_cast<cudaStream_t>(stream));
+}
+
+int pop_k_gemv_w4(const void* x, int64_t ldx, const void* codes, const void* scales, const void* zeros, int32_t group,
+                  void* out, int64_t ldo, int32_t B, int32_t N, int32_t K, int32_t mode, int32_t act, int32_t n_valid,
+                  void* stream) {
+  Gemv4Args a{};
+  a.x = static_cast<const bf16*>(x); a.ldx = ldx;
+  a.codes = static_cast<const uint8_t*>(codes); a.scales = static_cast<const bf16*>(scales);
+  a.zeros = static_cast<const uint8_t*>(zeros); a.group = group;
+  a.out = out; a.ldo = ldo; a.B = B; a.N = N; a.K = K; a.mode = mode; a.act = act; a.n_valid = n_valid;
+  return launch_gemv4(a, static_cast<cudaStream_t>(stream));
+}
+
+static Pages pages(const void* k, const void* v, const int32_t* table, int32_t page_size, int32_t num_pages,
+                   int32_t max_pages) {
+  Pages c;
+  c.k = static_cast<bf16*>(const_cast<void*>(k)); c.v = static_cast<bf16*>(const_cast<void*>(v));
+  c.table = table; c.page_size = page_size; c.num_pages = num_pages; c.max_pages = max_pages;
+  return c;
+}
+
+int pop_k_rope_cache_tree(const void* in, int32_t in_bf16, int64_t ld_in, int32_t rows, const int32_t* cu_rows,
+                          int32_t max_rows, const int32_t* start, int32_t pos0, const int32_t* depth, int32_t batch,
+                          void* q_out, int64_t ldq, void* k_pool, void* v_pool, const int32_t* block_table,
+                          int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, const float* q_gain,
+                          const float* k_gain, float eps, const void* rope_table, int32_t table_rows, int32_t n_q,
+                          int32_t n_kv, int32_t head_dim, void* stream) {
+  TreeAppendArgs a{};
+  a.in = in; a.in_bf16 = in_bf16 != 0; a.ld_in = ld_in;
+  a.d = Drafts{cu_rows, max_rows, rows, start, pos0, depth, batch};
+  a.q_out = static_cast<bf16*>(q_out); a.ldq = ldq;
+  a.dst = pages(k_pool, v_pool, block_table, page_size, num_pages, max_pages_per_seq);
+  a.q_gain = q_gain; a.k_gain = k_gain; a.eps = eps;
+  a.table = static_cast<const float2*>(rope_table); a.table_rows = table_rows;
+  a.n_q = n_q; a.n_kv = n_kv; a.head_dim = head_dim;
+  return launch_tree_append(a, static_cast<cudaStream_t>(stream));
+}
+
+int pop_k_tree_attention(const void* q, int64_t ldq, int32_t rows, const int32_t* cu_rows, int32_t max_rows,
+                         const int32_t* start, int32_t max_start, const void* mask, int32_t mask_words,
+                         const int32_t* depth, const void* k_pool, const void* v_pool, const int32_t* block_table,
+                         int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, void* workspace,
+                         size_t workspace_bytes, void* out, int64_t ldo, int32_t batch, int32_t n_q, int32_t n_kv,
+                         int32_t head_dim, int32_t window, void* stream) {
+  TreeAttnArgs a{};
+  a.q = static_cast<const bf16*>(q); a.ldq = ldq;
+  a.d = Drafts{cu_rows, max_rows, rows, start, max_start, depth, batch};
+  a.mask = static_cast<const uint32_t*>(mask); a.mask_words = mask_words;
+  a.c = pages(k_pool, v_pool, block_table, page_size, num_pages, max_pages_per_seq);
+  a.out = static_cast<bf16*>(out); a.ldo = ldo;
+  a.n_q = n_q; a.n_kv = n_kv; a.head_dim = head_dim; a.window = window;
+  a.workspace = workspace; a.workspace_bytes = workspace ? workspace_bytes : 0;
+  return launch_tree_attention(a, static_cast<cudaStream_t>(stream));
+}
+
+int pop_k_cache_keep(void* k_pool, void* v_pool, int64_t layer_stride, int32_t layers, const int32_t* block_table,
+                     int32_t page_size, int32_t num_pages, int32_t max_pages_per_seq, const int32_t* kept,
+                     int64_t ld_kept, const int32_t* n_kept, int32_t max_kept, const int32_t* start, int32_t pos0,
+                     int32_t batch, int32_t n_kv, int32_t head_dim, void* stream) {
+  KeepArgs a{};
+  a.c = pages(k_pool, v_pool, block_table, page_size, num_pages, max_pages_per_seq);
+  a.layer_stride = layer_stride; a.layers = layers;
+  a.kept = kept; a.ld_kept = ld_kept; a.n_kept = n_kept; a.max_kept = max_kept;
+  a.start = start; a.pos0 = pos0;
+  a.batch = batch; a.n_kv = n_kv; a.head_dim = head_dim;
+  return launch_cache_keep(a, static_cast<cudaStream_t>(stream));
 }
 
 int pop_k_status(void* stream) { return read_and_clear_status(static_cast<cudaStream_t>(stream)); }

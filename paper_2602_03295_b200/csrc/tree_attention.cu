@@ -1,0 +1,763 @@
+// Attention of drafted tokens over the bf16 paged cache (Attn of paper Eq. 1 for several rows of a sequence that form a tree):
+// row i of a sequence sees the cached positions in front of the draft, and of the drafted slots those whose bit its mask has.
+//
+// A tile is 128 (row, head) pairs of one kv head: K and V are read once for all of them. Few rows over a long cache are bound
+// by the cache's bytes, so what counts is that every SM reads all the time, whatever the sequences' lengths: the key tiles of
+// all (sequence, kv head, row tile) items form one line, and each CTA takes an equal stretch of it. An item that lies in one
+// stretch is finished there; the others leave (maximum, sum, output) of their part, and a second launch joins the parts.
+// Warps of a CTA:
+//   NQT softmax warpgroups, one (row, head) per thread: scores of 64 keys from TMEM, mask, exponentials against the running
+//       maximum, P in bf16 back over the scores it came from;
+//   1 TMA warp: Q of an item, K and V tiles of 64 positions through a ring, in the order in which they are used;
+//   1 MMA warp: scores two tiles ahead of the softmax, across the ends of items too, and O += P V with P from TMEM.
+#include "ptx.cuh"
+#include "tree.cuh"
+
+namespace pop {
+namespace {
+
+constexpr int BKV = 64;
+
+template <int HD, int NQT>
+struct TC {
+  static constexpr int KV_TILE_BYTES = BKV * HD * 2;
+  static constexpr int KV_SUB_BYTES = BKV * 128;       // one 64-wide slice of head_dim
+  static constexpr int Q_TILE_BYTES = 128 * HD * 2;
+  static constexpr int O_COL = NQT * 2 * BKV;          // S_t[b] at (t * 2 + b) * 64, O_t at O_COL + t * HD
+  static constexpr int COLS_USED = O_COL + NQT * HD;
+  static constexpr uint32_t TMEM_COLS = COLS_USED <= 256 ? 256 : 512;
+  static constexpr int PER_SM = TMEM_COLS == 256 ? 2 : 1;        // one CTA's beginnings and ends beside the other's keys
+  static constexpr int RING_BYTES = (PER_SM == 2 ? 113 : 227) * 1024 - 2 * 1024 - NQT * Q_TILE_BYTES;
+  static constexpr int STAGES = RING_BYTES / KV_TILE_BYTES < 12 ? RING_BYTES / KV_TILE_BYTES : 12;
+  static constexpr int THREADS = NQT * 128 + 64;
+  static_assert(COLS_USED <= 512, "TMEM budget");
+  static_assert(STAGES >= 4, "ring too shallow");
+};
+
+template <int HD, int NQT>
+struct __align__(1024) TreeSmem {
+  using C = TC<HD, NQT>;
+  uint8_t q[NQT][C::Q_TILE_BYTES];
+  uint8_t kv[C::STAGES][C::KV_TILE_BYTES];
+  uint64_t q_full, q_empty;
+  uint64_t kv_full[C::STAGES];
+  uint64_t kv_empty[C::STAGES];
+  uint64_t s_full[NQT][2];      // scores of tile f in buffer f & 1, phase f >> 1; the same for the two below
+  uint64_t p_ready[NQT][2];     // P over the scores (one arrival per softmax warp)
+  uint64_t pv_done[NQT][2];     // O += P V complete
+  uint32_t tmem_base;
+  uint32_t raised;
+  volatile uint32_t abort;
+};
+
+struct TreeDev {
+  TreeAttnArgs a;
+  int G, per;                   // query heads per kv head, rows per tile of 128
+  int nqt;                      // tiles of an item
+  int rows_per_load;            // positions of a TMA load: min(page_size, 64)
+  int room;                     // positions that a row of the block table has pages for
+  int ctas;
+  float scale_log2;             // log2(e) / sqrt(hd)
+  float* partial;               // [2 per CTA][nqt * 128][hd + 4]
+  int* status;
+};
+
+// Fewest tiles of a stretch: below, beginning and ending it costs more than its keys
+constexpr int MIN_SHARE = 2;
+
+// One sequence of the line
+struct Seq {
+  int row0, n, start;           // packed rows, positions in front of them
+  int j_lo, tiles, qts;         // first key tile, key tiles of an item, items per kv head
+};
+
+__device__ __forceinline__ Seq seq_of(const TreeDev& p, int b, bool report) {
+  const Drafts& d = p.a.d;
+  Seq x;
+  x.row0 = d.cu ? __ldg(d.cu + b) : b * d.max_rows;
+  x.n = d.cu ? __ldg(d.cu + b + 1) - x.row0 : d.max_rows;
+  x.start = d.start ? __ldg(d.start + b) : d.pos0;
+  x.j_lo = x.tiles = x.qts = 0;
+  if (x.n <= 0) return x;                                      // no rows: whatever the rest is
+  if (x.n > d.max_rows || x.row0 < 0 || x.row0 > d.rows - x.n || x.start < 0 || x.start > d.pos0 ||
+      x.start > p.room - x.n) {
+    if (report) atomicMin(p.status, (int)POP_E_INVALID);
+    x.n = 0;
+    return x;
+  }
+  x.j_lo = p.a.window > 0 ? max(0, x.start - p.a.window + 1) / BKV : 0;
+  x.tiles = (x.start + x.n - 1) / BKV - x.j_lo + 1;
+  x.qts = (x.n + p.nqt * p.per - 1) / (p.nqt * p.per);
+  return x;
+}
+__device__ __forceinline__ int line_of(const TreeDev& p, const Seq& x) { return x.tiles * x.qts * p.a.n_kv; }
+
+__device__ __forceinline__ int warp_add(int v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+// Tiles of a CTA's stretch, by a whole warp
+__device__ __forceinline__ int share_of(const TreeDev& p, int* total, bool report) {
+  int sum = 0;
+  for (int b = threadIdx.x & 31; b < p.a.d.batch; b += 32) sum += line_of(p, seq_of(p, b, report));
+  *total = warp_add(sum);
+  const int share = (*total + p.ctas - 1) / p.ctas;
+  return share > MIN_SHARE ? share : MIN_SHARE;
+}
+// Tiles in front of sequence `b`, by a whole warp
+__device__ __forceinline__ int line_before(const TreeDev& p, int b) {
+  int sum = 0;
+  for (int i = threadIdx.x & 31; i < b; i += 32) sum += line_of(p, seq_of(p, i, false));
+  return warp_add(sum);
+}
+
+// A walk over a stretch of the line, tile by tile, the same for all lanes
+struct Walk {
+  Seq x;
+  int b, left;                  // sequence; its tiles from here on
+  int pos, hi;                  // place in the line, end of the stretch
+  int kvh, q0;                  // the item: kv head, first row
+  int j, j_end;                 // key tile (absolute), end of the segment
+  int j_item_end;
+  __device__ __forceinline__ void item(const TreeDev& p, int off) {
+    const int it = off / x.tiles, r = off - it * x.tiles;
+    kvh = it / x.qts;
+    q0 = (it - kvh * x.qts) * p.nqt * p.per;
+    j = x.j_lo + r;
+    j_item_end = x.j_lo + x.tiles;
+    j_end = min(j_item_end, j + hi - pos);
+    left = line_of(p, x) - off;
+  }
+  // begins at line place `lo` (by a whole warp, all lanes with the same arguments)
+  __device__ __forceinline__ void begin(const TreeDev& p, int lo, int hi_) {
+    const int lane = threadIdx.x & 31;
+    pos = lo;
+    hi = hi_;
+    int base = 0;
+    for (int b0 = 0;; b0 += 32) {
+      const int mine = b0 + lane < p.a.d.batch ? line_of(p, seq_of(p, b0 + lane, false)) : 0;
+      int incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      const uint32_t past = __ballot_sync(0xffffffffu, base + incl > lo);
+      if (past != 0) {                                         // lo lies in front of the line's end, so one is found
+        const int at = __ffs(past) - 1;
+        b = b0 + at;
+        base += __shfl_sync(0xffffffffu, incl - mine, at);
+        break;
+      }
+      base += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    x = seq_of(p, b, false);
+    item(p, lo - base);
+  }
+  // to the next tile; true where another segment begins there
+  __device__ __forceinline__ bool next(const TreeDev& p) {
+    ++pos;
+    --left;
+    if (++j < j_end) return false;
+    if (pos >= hi) return true;
+    if (left == 0) {
+      do {
+        x = seq_of(p, ++b, false);
+      } while (x.tiles == 0);                                  // pos lies in front of the line's end, so one follows
+      item(p, 0);
+    } else {
+      item(p, line_of(p, x) - left);
+    }
+    return true;
+  }
+};
+
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<uint32_t*>(&v);
+}
+__device__ __forceinline__ uint64_t ones(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
+__device__ __forceinline__ bool gave_up(int status) { return status <= (int)POP_E_DEVICE_TIMEOUT; }
+
+// Which of the 64 positions from kv0 on row i (packed row `row`) of the sequence sees
+__device__ __forceinline__ uint64_t seen_of(const TreeDev& p, const Seq& x, int i, int64_t row, int depth, int kv0) {
+  const int ctx = x.start - kv0;                               // positions of the tile in front of the draft
+  const int window = p.a.window;
+  uint64_t vis = ~0ull;
+  if (ctx < 64) {
+    if (p.a.mask == nullptr) {
+      vis = ones(ctx + i + 1);
+    } else {
+      const uint32_t* m = p.a.mask + row * p.a.mask_words;
+      const int slot0 = ctx < 0 ? -ctx : 0, w = slot0 >> 5, sh = slot0 & 31;
+      auto word = [&](int k) { return k < p.a.mask_words ? (uint64_t)__ldg(m + k) : 0ull; };
+      const uint64_t lo = word(w) | (word(w + 1) << 32);
+      const uint64_t drafted = sh == 0 ? lo : (lo >> sh) | (word(w + 2) << (64 - sh));
+      vis = ctx > 0 ? (drafted << ctx) | ones(ctx) : drafted;
+    }
+    vis &= ones(ctx + x.n);
+  }
+  if (window > 0) {
+    const int hidden = x.start + depth - window + 1 - kv0;     // positions in front of the window
+    if (hidden > 0) vis &= ~ones(min(hidden, ctx));
+    if (ctx < 64 && depth >= window) {                         // drafted slots that lie so far up the tree
+      for (uint64_t m = vis & ~ones(ctx); m != 0; m &= m - 1) {
+        const int k = __ffsll((long long)m) - 1, slot = k - ctx;
+        const int d = p.a.d.depth ? __ldg(p.a.d.depth + x.row0 + slot) : slot;
+        if (d <= depth - window) vis &= ~(1ull << k);
+      }
+    }
+  }
+  return vis;
+}
+
+#define TREE_ABORT(S, status)                         \
+  do {                                                \
+    (S).abort = 1;                                    \
+    atomicMin((status), (int)POP_E_DEVICE_TIMEOUT);   \
+  } while (0)
+
+template <int HD, int NQT>
+__global__ void __launch_bounds__(TC<HD, NQT>::THREADS, TC<HD, NQT>::PER_SM)
+tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                 const __grid_constant__ CUtensorMap tmV, const __grid_constant__ TreeDev p) {
+  using C = TC<HD, NQT>;
+  constexpr int STAGES = C::STAGES;
+  extern __shared__ uint8_t smem_raw[];
+  TreeSmem<HD, NQT>& s =
+      *reinterpret_cast<TreeSmem<HD, NQT>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  chain_trigger();
+  if (threadIdx.x == 0) {
+    mbar_init(&s.q_full, 1);
+    mbar_init(&s.q_empty, 1);
+    for (int i = 0; i < STAGES; ++i) {
+      mbar_init(&s.kv_full[i], 1);
+      mbar_init(&s.kv_empty[i], 1);
+    }
+    for (int t = 0; t < NQT; ++t)
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&s.s_full[t][i], 1);
+        mbar_init(&s.p_ready[t][i], 4);
+        mbar_init(&s.pv_done[t][i], 1);
+      }
+    s.abort = 0;
+    fence_barrier_init();
+    prefetch_tmap(&tmQ);
+    prefetch_tmap(&tmK);
+    prefetch_tmap(&tmV);
+  }
+  chain_wait();
+  if (threadIdx.x == 0) s.raised = gave_up(*reinterpret_cast<const volatile int*>(p.status)) ? 1u : 0u;
+  int total;
+  const int share = share_of(p, &total, blockIdx.x == 0 && warp == 0);
+  const int lo = min((int64_t)blockIdx.x * share, (int64_t)total), hi = min(lo + share, total);
+  __syncthreads();
+  if (lo >= hi || s.raised != 0) return;
+  if (warp == NQT * 4 + 1) {
+    tmem_alloc(&s.tmem_base, C::TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = s.tmem_base;
+  const int n_tiles = hi - lo;
+
+  if (warp == NQT * 4) {
+    // ------------------------------------------------------------------ TMA: K_0, K_1, then V_f, K_{f+2}
+    Walk kw, vw;
+    kw.begin(p, lo, hi);
+    vw = kw;
+    const int loads = BKV / p.rows_per_load, log_loads = loads == 1 ? 0 : loads == 2 ? 1 : 2;
+    int ring = 0, items = 0;
+    bool ok = true;
+    // Pages of the next 32 loads of a sequence, an entry per lane, and of the 32 behind them
+    struct Ahead {
+      int b = -1, first = 0, pg0 = 0, pg1 = 0;
+    } k_ahead, v_ahead;
+    auto entry = [&](const Walk& w, int load) {
+      const int at = load * p.rows_per_load;
+      return at < w.x.start + w.x.n ? __ldg(p.a.c.table + (int64_t)w.b * p.a.c.max_pages + at / p.a.c.page_size) : 0;
+    };
+    auto load_tile = [&](const Walk& w, Ahead& ahead, const CUtensorMap* tm) {
+      const int stage = ring % STAGES;
+      const uint32_t phase = (ring / STAGES) & 1;
+      ++ring;
+      const int l0 = w.j << log_loads;
+      if (ahead.b != w.b || l0 < ahead.first || l0 >= ahead.first + 64) {
+        ahead.b = w.b;
+        ahead.first = l0;
+        ahead.pg0 = entry(w, l0 + lane);
+        ahead.pg1 = entry(w, l0 + 32 + lane);
+      } else if (l0 >= ahead.first + 32) {
+        ahead.first += 32;
+        ahead.pg0 = ahead.pg1;
+        ahead.pg1 = entry(w, ahead.first + 32 + lane);
+      }
+      const int kv0 = w.j * BKV, live = min(loads, (w.x.start + w.x.n - kv0 + p.rows_per_load - 1) / p.rows_per_load);
+      if (!mbar_wait_relaxed(&s.kv_empty[stage], phase ^ 1)) {
+        ok = false;
+        return;
+      }
+      if (lane == 0) mbar_expect_tx(&s.kv_full[stage], live * p.rows_per_load * HD * 2);
+      for (int r = 0; r < live; ++r) {
+        const int k = l0 + r - ahead.first;
+        const int page = k < 32 ? __shfl_sync(0xffffffffu, ahead.pg0, k) : __shfl_sync(0xffffffffu, ahead.pg1, k - 32);
+        if (lane == 0) {
+          // an entry outside the pool is clipped by the tensor map (it reads as zeros), but it is an error
+          if ((unsigned)page >= (unsigned)p.a.c.num_pages) atomicMin(p.status, (int)POP_E_INVALID);
+          for (int c = 0; c < HD / 64; ++c)
+            tma_load_4d(s.kv[stage] + c * C::KV_SUB_BYTES + r * p.rows_per_load * 128, tm, &s.kv_full[stage], c * 64,
+                        w.kvh, (kv0 + r * p.rows_per_load) % p.a.c.page_size, page);
+        }
+      }
+    };
+    auto load_q = [&](const Walk& w) {
+      if (items > 0 && !mbar_wait_relaxed(&s.q_empty, (items - 1) & 1)) {
+        ok = false;
+        return;
+      }
+      ++items;
+      if (lane == 0) {
+        mbar_expect_tx(&s.q_full, NQT * p.per * p.G * HD * 2);
+        for (int t = 0; t < NQT; ++t)
+          for (int c = 0; c < HD / 64; ++c)
+            tma_load_3d(s.q[t] + c * 16384, &tmQ, &s.q_full, c * 64, w.kvh * p.G, w.x.row0 + w.q0 + t * p.per);
+      }
+    };
+    bool fresh = true;
+    int kf = 0;
+    auto load_k = [&] {
+      if (fresh) load_q(kw);
+      if (ok) load_tile(kw, k_ahead, &tmK);
+      ++kf;
+      fresh = kw.next(p);
+    };
+    load_k();
+    if (ok && kf < n_tiles) load_k();
+    for (int f = 0; f < n_tiles && ok && !s.abort; ++f) {
+      load_tile(vw, v_ahead, &tmV);
+      vw.next(p);
+      if (ok && kf < n_tiles) load_k();
+    }
+    if (!ok) TREE_ABORT(s, p.status);
+  } else if (warp == NQT * 4 + 1) {
+    // ------------------------------------------------------------------ MMA issuer (whole warp, elected lane)
+    Walk sw, pw;
+    sw.begin(p, lo, hi);
+    pw = sw;
+    const uint32_t leader = elect_one();
+    constexpr uint32_t idesc_s = umma_idesc_bf16(128, BKV, 0, 0);
+    constexpr uint32_t idesc_o = umma_idesc_bf16(128, HD, 0, 1);
+    uint64_t q_desc[NQT];
+    for (int t = 0; t < NQT; ++t) q_desc[t] = umma_smem_desc(smem_u32(s.q[t]), 16, 1024);
+    const uint64_t k_desc0 = umma_smem_desc(smem_u32(s.kv[0]), 16, 1024);                 // K-major
+    const uint64_t v_desc0 = umma_smem_desc(smem_u32(s.kv[0]), C::KV_SUB_BYTES, 1024);    // MN-major
+    auto issue_s = [&](int t, int f, int stage) {
+      const uint64_t kd = k_desc0 + uint64_t(stage * (C::KV_TILE_BYTES >> 4));
+      const uint32_t d = tmem_base + (t * 2 + (f & 1)) * BKV;
+#pragma unroll
+      for (int kk = 0; kk < HD / 16; ++kk)
+        umma_bf16_ss_w(leader, d, q_desc[t] + uint64_t(((kk >> 2) * 16384 + (kk & 3) * 32) >> 4),
+                       kd + uint64_t(((kk >> 2) * C::KV_SUB_BYTES + (kk & 3) * 32) >> 4), idesc_s, kk > 0 ? 1u : 0u);
+      umma_commit_w(leader, &s.s_full[t][f & 1]);
+    };
+    auto issue_pv = [&](int t, int f, int stage, bool begins) {
+      const uint32_t pa = tmem_base + (t * 2 + (f & 1)) * BKV;
+      const uint64_t vd = v_desc0 + uint64_t(stage * (C::KV_TILE_BYTES >> 4));
+      const uint32_t d = tmem_base + C::O_COL + t * HD;
+#pragma unroll
+      for (int kk = 0; kk < BKV / 16; ++kk)
+        umma_bf16_ts_w(leader, d, pa + kk * 8, vd + uint64_t((kk * 2048) >> 4), idesc_o, (!begins || kk > 0) ? 1u : 0u);
+      umma_commit_w(leader, &s.pv_done[t][f & 1]);
+    };
+    int ring = 0, sf = 0, items = 0;
+    bool ok = true, s_fresh = true, p_fresh = true;
+    auto wait_tile = [&](int& stage) {
+      stage = ring % STAGES;
+      const uint32_t phase = (ring / STAGES) & 1;
+      ++ring;
+      return mbar_wait_relaxed(&s.kv_full[stage], phase);
+    };
+    // Scores of the next tile into the buffer that the tile two in front of it has left: its product is issued, and the
+    // tensor pipe runs in order. The first wait of an item is for its queries.
+    auto scores = [&] {
+      if (s_fresh) ok = mbar_wait_relaxed(&s.q_full, items++ & 1);
+      int stage = 0;
+      if (ok) ok = wait_tile(stage);
+      if (!ok) return;
+      tc_fence_after();
+      for (int t = 0; t < NQT; ++t) issue_s(t, sf, stage);
+      umma_commit_w(leader, &s.kv_empty[stage]);
+      ++sf;
+      s_fresh = sw.next(p);
+      if (s_fresh) umma_commit_w(leader, &s.q_empty);
+    };
+    scores();
+    if (ok && sf < n_tiles) scores();
+    for (int f = 0; f < n_tiles && ok && !s.abort; ++f) {
+      int stage = 0;
+      ok = wait_tile(stage);
+      for (int t = 0; t < NQT && ok; ++t) {
+        ok = mbar_wait_relaxed(&s.p_ready[t][f & 1], (f >> 1) & 1);
+        if (!ok) break;
+        tc_fence_after();
+        issue_pv(t, f, stage, p_fresh);
+      }
+      if (!ok) break;
+      umma_commit_w(leader, &s.kv_empty[stage]);
+      p_fresh = pw.next(p);
+      if (sf < n_tiles) scores();
+    }
+    if (!ok) TREE_ABORT(s, p.status);
+  } else {
+    // ------------------------------------------------------------------ softmax warpgroups
+    Walk w;
+    w.begin(p, lo, hi);
+    const int t = warp >> 2, quarter = warp & 3;
+    const int row = quarter * 32 + lane;                  // pair of the tile == TMEM lane
+    const int ip = row / p.G, h = row - ip * p.G;         // row of the tile, head of the kv head
+    const uint32_t lane_addr = uint32_t(quarter * 32) << 16;
+    const uint32_t s_addr = tmem_base + lane_addr + t * 2 * BKV;
+    const uint32_t o_addr = tmem_base + lane_addr + C::O_COL + t * HD;
+    bool ok = true;
+    auto wait_pv = [&](int f) { return mbar_wait(&s.pv_done[t][f & 1], (f >> 1) & 1); };
+    int f = 0;
+    while (f < n_tiles && ok && !s.abort) {
+      // ---- a segment: the tiles of one item that lie in this stretch
+      const Seq x = w.x;
+      const int kvh = w.kvh, j0 = w.j, nt = w.j_end - w.j, i = w.q0 + t * p.per + ip;
+      const bool whole = j0 == x.j_lo && w.j_end == w.j_item_end;
+      const int slot = 2 * (int)blockIdx.x + (f > 0 ? 1 : 0);
+      const bool used = ip < p.per && i < x.n;
+      const bool idle = !__any_sync(0xffffffffu, used);   // a warp without rows only keeps the barriers going
+      const int64_t prow = (int64_t)x.row0 + i;
+      const int depth = !used || p.a.window == 0 ? 0 : p.a.d.depth ? min(max(__ldg(p.a.d.depth + prow), 0), 0xffff) : i;
+      const int win_lo = p.a.window > 0 ? x.start - p.a.window + 1 : 0;      // in front of every row's window
+      const int len = x.start + x.n;
+      float m_run = -INFINITY, l_run = 0.f;
+      for (int jj = 0; jj < nt && !s.abort; ++jj, ++f) {
+        const int kv0 = (j0 + jj) * BKV;
+        const uint32_t sp_addr = s_addr + (f & 1) * BKV;
+        if (!mbar_wait(&s.s_full[t][f & 1], (f >> 1) & 1)) { ok = false; break; }
+        if (!idle) {
+          tc_fence_after();
+          float sv[BKV];
+#pragma unroll
+          for (int c = 0; c < BKV / 32; ++c)
+            tmem_ld_32x32b_x32(sp_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[c * 32]));
+          const uint64_t vis = used ? seen_of(p, x, i, prow, depth, kv0) : 0ull;
+          tmem_wait_ld();
+          if (vis != ~0ull) {
+            const uint32_t v0 = (uint32_t)vis, v1 = (uint32_t)(vis >> 32);
+#pragma unroll
+            for (int k = 0; k < BKV; ++k)
+              if (!(((k < 32 ? v0 : v1) >> (k & 31)) & 1u)) sv[k] = -INFINITY;
+          }
+          // P = exp2(S * scale - m) against the maximum the row already has; this tile's own is reduced alongside and
+          // looked at afterwards. P enters the product as bf16, its sum is taken in fp32 before that rounding.
+          float2 acc0, acc1;
+          uint32_t pk[BKV / 2];
+          float mx0, mx1, mx2, mx3;
+          auto exps = [&](float m_use) {
+            const float2 sc2 = make_float2(p.scale_log2, p.scale_log2);
+            const float2 nm2 = make_float2(-m_use, -m_use);
+            acc0 = make_float2(0.f, 0.f);
+            acc1 = make_float2(0.f, 0.f);
+            mx0 = sv[0]; mx1 = sv[2]; mx2 = sv[4]; mx3 = sv[6];
+#pragma unroll
+            for (int c = 0; c < BKV / 8; ++c) {
+              float2 x0 = __ffma2_rn(make_float2(sv[c * 8 + 0], sv[c * 8 + 1]), sc2, nm2);
+              float2 x1 = __ffma2_rn(make_float2(sv[c * 8 + 2], sv[c * 8 + 3]), sc2, nm2);
+              float2 x2 = __ffma2_rn(make_float2(sv[c * 8 + 4], sv[c * 8 + 5]), sc2, nm2);
+              float2 x3 = __ffma2_rn(make_float2(sv[c * 8 + 6], sv[c * 8 + 7]), sc2, nm2);
+              mx0 = max3(mx0, sv[c * 8 + 0], sv[c * 8 + 1]);
+              mx1 = max3(mx1, sv[c * 8 + 2], sv[c * 8 + 3]);
+              mx2 = max3(mx2, sv[c * 8 + 4], sv[c * 8 + 5]);
+              mx3 = max3(mx3, sv[c * 8 + 6], sv[c * 8 + 7]);
+              x0.x = ex2(x0.x); x0.y = ex2(x0.y);
+              x1.x = ex2(x1.x); x1.y = ex2(x1.y);
+              x2.x = ex2(x2.x); x2.y = ex2(x2.y);
+              x3.x = ex2(x3.x); x3.y = ex2(x3.y);
+              acc0 = __fadd2_rn(acc0, x0);
+              acc1 = __fadd2_rn(acc1, x1);
+              acc0 = __fadd2_rn(acc0, x2);
+              acc1 = __fadd2_rn(acc1, x3);
+              pk[c * 4 + 0] = pack2(x0.x, x0.y);
+              pk[c * 4 + 1] = pack2(x1.x, x1.y);
+              pk[c * 4 + 2] = pack2(x2.x, x2.y);
+              pk[c * 4 + 3] = pack2(x3.x, x3.y);
+            }
+          };
+          exps(m_run == -INFINITY ? 0.f : m_run);
+          const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * p.scale_log2;
+          const float m_new = fmaxf(m_run, mx);
+          const bool need = (m_new - m_run > 8.0f) || (m_run == -INFINITY && m_new > -INFINITY);
+          if (__any_sync(0xffffffffu, need)) {
+            // the maximum grew by more than 2^8 somewhere in this warp: bring the accumulator to the new one
+            const float factor = (m_new == -INFINITY) ? 1.0f : ex2(m_run - m_new);   // ex2(-inf) = 0
+            if (jj > 0) {
+              if (!wait_pv(f - 1)) { ok = false; break; }
+              tc_fence_after();
+#pragma unroll 1
+              for (int c = 0; c < HD / 32; ++c) {
+                uint32_t o[32];
+                tmem_ld_32x32b_x32(o_addr + c * 32, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * factor);
+                tmem_st_32x32b_x32(o_addr + c * 32, o);
+              }
+              tmem_wait_st();
+            }
+            l_run *= factor;
+            m_run = m_new;
+            exps(m_run == -INFINITY ? 0.f : m_run);
+          }
+          l_run += (acc0.x + acc0.y) + (acc1.x + acc1.y);
+          tmem_st_32x32b_x32(sp_addr, pk);
+          tmem_wait_st();
+        }
+        // positions behind the sequence's end or in front of every window may hold anything: zeros in the staged V tile, so
+        // that 0 * garbage cannot reach the accumulator. V_f is entry min(f + 2, n_tiles) + f of the ring.
+        if (t == 0 && warp < 2 && (kv0 + BKV > len || kv0 < win_lo)) {
+          const int rv = min(f + 2, n_tiles) + f;
+          if (!mbar_wait(&s.kv_full[rv % STAGES], (rv / STAGES) & 1)) { ok = false; break; }
+          if (kv0 + row >= len || kv0 + row < win_lo) {
+            for (int c = 0; c < HD / 64; ++c) {
+              uint4* dst = reinterpret_cast<uint4*>(s.kv[rv % STAGES] + c * C::KV_SUB_BYTES + row * 128);
+#pragma unroll
+              for (int q = 0; q < 8; ++q) dst[q] = make_uint4(0, 0, 0, 0);
+            }
+          }
+          fence_proxy_async_smem();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&s.p_ready[t][f & 1]);
+        w.next(p);
+      }
+      if (!ok || s.abort) break;
+      if (!wait_pv(f - 1)) { ok = false; break; }
+      if (!idle) {
+        tc_fence_after();
+        const bool none = l_run == 0.f;                   // a row that sees nothing is a row of zeros
+        const float inv = none ? 0.f : 1.0f / l_run;
+        bf16* out = p.a.out + prow * p.a.ldo + (int64_t)(kvh * p.G + h) * HD;
+        float* part = p.partial + ((int64_t)slot * (NQT * 128) + t * 128 + row) * (HD + 4);
+        if (used && !whole) *reinterpret_cast<float4*>(part) = make_float4(m_run, l_run, 0.f, 0.f);
+#pragma unroll 1
+        for (int c = 0; c < HD / 32; ++c) {
+          uint32_t o[32];
+          tmem_ld_32x32b_x32(o_addr + c * 32, o);
+          tmem_wait_ld();
+          if (none) {
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = 0;
+          }
+          if (!used) continue;
+          if (whole) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              uint4 o4;
+              o4.x = pack2(__uint_as_float(o[v * 8 + 0]) * inv, __uint_as_float(o[v * 8 + 1]) * inv);
+              o4.y = pack2(__uint_as_float(o[v * 8 + 2]) * inv, __uint_as_float(o[v * 8 + 3]) * inv);
+              o4.z = pack2(__uint_as_float(o[v * 8 + 4]) * inv, __uint_as_float(o[v * 8 + 5]) * inv);
+              o4.w = pack2(__uint_as_float(o[v * 8 + 6]) * inv, __uint_as_float(o[v * 8 + 7]) * inv);
+              *reinterpret_cast<uint4*>(out + c * 32 + v * 8) = o4;
+            }
+          } else {
+#pragma unroll
+            for (int v = 0; v < 8; ++v)
+              *reinterpret_cast<uint4*>(part + 4 + c * 32 + v * 4) = make_uint4(o[v * 4], o[v * 4 + 1], o[v * 4 + 2], o[v * 4 + 3]);
+          }
+        }
+      }
+      // the next item's first product overwrites O: it waits for P of all warps, which they write after this
+    }
+    if (!ok) TREE_ABORT(s, p.status);
+  }
+
+  // ------------------------------------------------------------------ teardown
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (s.abort && threadIdx.x == 0) {
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // let in-flight bulk copies land
+  }
+  __syncthreads();
+  if (warp == NQT * 4 + 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, C::TMEM_COLS);
+  }
+}
+
+// Joins the parts of the items that lie in several stretches: a warp per (row, head), out = sum_c w_c o_c / sum_c w_c l_c with
+// w_c = exp2(m_c - max m), the stretches in their order.
+template <int HD>
+__global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeDev p) {
+  chain_trigger();
+  chain_wait();
+  const int lane = threadIdx.x & 31, b = blockIdx.z;
+  const int word = threadIdx.x == 0 ? *reinterpret_cast<const volatile int*>(p.status) : 0;
+  int total;
+  const int share = share_of(p, &total, false);
+  const Seq x = seq_of(p, b, false);
+  const int kvh = blockIdx.x % p.a.n_kv, qt = blockIdx.x / p.a.n_kv;
+  const int u = blockIdx.y * 8 + (threadIdx.x >> 5), pairs = p.per * p.G;       // pair of the item
+  const int a = qt < x.qts ? line_before(p, b) + (kvh * x.qts + qt) * x.tiles : 0;
+  if (__syncthreads_or(gave_up(word)) || qt >= x.qts) return;                   // gave up: there are parts that nobody wrote
+  const int c0 = a / share, c1 = (a + x.tiles - 1) / share, pieces = c1 - c0 + 1;
+  const int t = u / pairs, in_tile = u - t * pairs, ip = in_tile / p.G, i = qt * p.nqt * p.per + t * p.per + ip;
+  if (pieces == 1 || t >= p.nqt || i >= x.n) return;
+  constexpr int PER = HD / 32;
+  float m = -INFINITY, l = 0.f, o[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) o[k] = 0.f;
+  const int64_t stride = (int64_t)(p.nqt * 128) * (HD + 4);                     // from slot to slot
+  const float* rows = p.partial + (int64_t)(t * 128 + in_tile) * (HD + 4);
+  // a stretch's first segment is in its first slot; the item's own beginning may lie behind another item in its stretch
+  auto part_of = [&](int c) { return rows + (2 * (int64_t)c + (a > (int64_t)c * share ? 1 : 0)) * stride; };
+  for (int s0 = c0; s0 <= c1; s0 += 32) {
+    const int live = min(32, c1 - s0 + 1);
+    float ms = -INFINITY, ls = 0.f;
+    if (lane < live) {
+      const float* src = part_of(s0 + lane);
+      ms = __ldcg(src);
+      ls = __ldcg(src + 1);
+    }
+    float n = fmaxf(m, ms);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) n = fmaxf(n, __shfl_xor_sync(0xffffffffu, n, d));
+    // no maximum so far: the parts saw nothing (zeros), or scores that are all NaN, whose sums stay NaN
+    const float z = n == -INFINITY ? 0.f : n;
+    const float f = ex2(m - z), wt = ex2(ms - z);
+    float sum = wt * ls;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+    l = l * f + sum;
+    m = n;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) o[k] *= f;
+#pragma unroll 4
+    for (int q = 0; q < live; ++q) {
+      const float wq = __shfl_sync(0xffffffffu, wt, q);
+      const float* src = part_of(s0 + q) + 4 + lane * 2;
+#pragma unroll
+      for (int k = 0; k < PER; k += 2) {
+        const float2 v = __ldcg(reinterpret_cast<const float2*>(src + k * 32));
+        o[k] = fmaf(v.x, wq, o[k]);
+        o[k + 1] = fmaf(v.y, wq, o[k + 1]);
+      }
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  bf16* dst = p.a.out + ((int64_t)x.row0 + i) * p.a.ldo + (int64_t)(kvh * p.G + in_tile - ip * p.G) * HD + lane * 2;
+#pragma unroll
+  for (int k = 0; k < PER; k += 2)
+    *reinterpret_cast<__nv_bfloat162*>(dst + k * 32) = __floats2bfloat162_rn(o[k] * inv, o[k + 1] * inv);
+}
+
+bool allow_smem(std::atomic<uint64_t>& done, const void* kernel, int bytes) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const uint64_t bit = uint64_t(1) << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_relaxed) & bit)) return true;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  done.fetch_or(bit, std::memory_order_relaxed);
+  return true;
+}
+
+template <int HD, int NQT>
+int launch_t(const TreeAttnArgs& a, TreeDev& p, cudaStream_t s) {
+  using C = TC<HD, NQT>;
+  const size_t smem = sizeof(TreeSmem<HD, NQT>) + 1024;
+  static_assert(sizeof(TreeSmem<HD, NQT>) + 1024 <= (C::PER_SM == 2 ? 113 : 227) * 1024, "shared memory budget");
+  p.nqt = NQT;
+  p.ctas = device_sms() * C::PER_SM;
+  const int64_t qts = ceil_div(a.d.max_rows, NQT * p.per);
+  const int64_t line = (int64_t)a.d.batch * a.n_kv * qts * (((int64_t)a.d.pos0 + a.d.max_rows + BKV - 1) / BKV);
+  if (line > 0x3fffffff || a.n_kv * qts > 0x7fffffff) return POP_E_INVALID;          // places in the line are 32-bit numbers
+  // two parts per CTA at most: of the item that it begins with and of the one that it ends with
+  const size_t need = (size_t)2 * p.ctas * NQT * 128 * (HD + 4) * 4;
+  if (a.workspace_bytes < need) return POP_E_NOSPACE;
+  p.status = status_word();
+  if (!p.status) return POP_E_CUDA;
+  static std::atomic<uint64_t> configured{0};
+  if (!allow_smem(configured, reinterpret_cast<const void*>(tree_attn_kernel<HD, NQT>), (int)smem)) return POP_E_CUDA;
+  CUtensorMap tq, tk, tv;
+  {
+    // Q [rows][heads][hd]: a box is `per` rows of the G heads of a kv head; rows behind the last are zeros
+    const uint64_t dims[5] = {(uint64_t)HD, (uint64_t)a.n_q, (uint64_t)a.d.rows, 1, 1};
+    const uint64_t str[4] = {(uint64_t)HD, (uint64_t)a.ldq, (uint64_t)a.ldq * a.d.rows, (uint64_t)a.ldq * a.d.rows};
+    const uint32_t box[5] = {64, (uint32_t)p.G, (uint32_t)p.per, 1, 1};
+    if (make_tmap_bf16_nd(&tq, a.q, 3, dims, str, box) != POP_OK) return POP_E_CUDA;
+  }
+  {
+    const uint64_t row = (uint64_t)HD * a.n_kv;
+    const uint64_t dims[5] = {(uint64_t)HD, (uint64_t)a.n_kv, (uint64_t)a.c.page_size, (uint64_t)a.c.num_pages, 1};
+    const uint64_t str[4] = {(uint64_t)HD, row, row * a.c.page_size, row * a.c.page_size * a.c.num_pages};
+    const uint32_t box[5] = {64, 1, (uint32_t)p.rows_per_load, 1, 1};
+    if (make_tmap_bf16_nd(&tk, a.c.k, 4, dims, str, box) != POP_OK || make_tmap_bf16_nd(&tv, a.c.v, 4, dims, str, box) != POP_OK)
+      return POP_E_CUDA;
+  }
+  ProfScope prof(PROF_ATTENTION, 4.0 * HD * a.n_q * a.d.rows * ((double)a.d.pos0 + a.d.max_rows), s);
+  if (launch_chained(tree_attn_kernel<HD, NQT>, dim3(p.ctas), dim3(C::THREADS), smem, s, tq, tk, tv, p) != cudaSuccess)
+    return POP_E_CUDA;
+  count_launch();
+  const int pairs = NQT == 1 && a.d.max_rows < p.per ? a.d.max_rows * p.G : NQT * p.per * p.G;
+  if (launch_chained(tree_merge_kernel<HD>, dim3((unsigned)(a.n_kv * qts), ceil_div(pairs, 8), a.d.batch), dim3(256), 0, s, p) !=
+      cudaSuccess)
+    return POP_E_CUDA;
+  count_launch();
+  return POP_OK;
+}
+
+}  // namespace
+
+int launch_tree_attention(const TreeAttnArgs& a, cudaStream_t s) {
+  if (!a.q || !a.out || !pages_ok(a.c)) return POP_E_INVALID;
+  if (a.d.batch < 1 || a.d.batch > 4096 || a.n_kv < 1 || a.n_q < 1 || a.n_q % a.n_kv || a.n_q > 65536 || a.n_q / a.n_kv > 128 ||
+      a.d.max_rows < 0 || a.d.max_rows > 65536 || a.d.rows < 0 || a.d.pos0 < 0 || a.d.pos0 > 0x7fff0000 - 65536 || a.window < 0 ||
+      a.window > 0x7ffffff0)
+    return POP_E_INVALID;
+  if (a.head_dim != 64 && a.head_dim != 128 && a.head_dim != 256) return POP_E_INVALID;
+  if (reinterpret_cast<uintptr_t>(a.q) % 16 || reinterpret_cast<uintptr_t>(a.out) % 16 || a.ldq % 8 || a.ldo % 8 ||
+      reinterpret_cast<uintptr_t>(a.workspace) % 16)
+    return POP_E_INVALID;
+  if (!a.d.cu && (int64_t)a.d.batch * a.d.max_rows > a.d.rows) return POP_E_INVALID;
+  if (a.mask && (int64_t)a.mask_words * 32 < a.d.max_rows) return POP_E_INVALID;
+  if (a.ldq < (int64_t)a.n_q * a.head_dim || (a.d.rows > 1 && a.ldo < (int64_t)a.n_q * a.head_dim)) return POP_E_INVALID;
+  const int64_t room = (int64_t)a.c.max_pages * a.c.page_size;
+  if (a.d.pos0 > room || (!a.d.start && !a.d.cu && (int64_t)a.d.pos0 + a.d.max_rows > room)) return POP_E_NOSPACE;
+  if (a.d.max_rows == 0 || a.d.rows == 0) return POP_OK;
+  TreeDev p{};
+  p.a = a;
+  p.G = a.n_q / a.n_kv;
+  p.per = 128 / p.G;
+  p.room = room < 0x7fff0000 ? (int)room : 0x7fff0000;
+  p.rows_per_load = a.c.page_size < BKV ? a.c.page_size : BKV;
+  p.scale_log2 = 1.4426950408889634f / sqrtf((float)a.head_dim);
+  p.partial = static_cast<float*>(a.workspace);
+  // two tiles share the keys where no tile of 128 pairs holds all rows of a sequence
+  const bool one = a.d.max_rows <= p.per;
+  switch (a.head_dim) {
+    case 64: return one ? launch_t<64, 1>(a, p, s) : launch_t<64, 2>(a, p, s);
+    case 128: return one ? launch_t<128, 1>(a, p, s) : launch_t<128, 2>(a, p, s);
+    default: return launch_t<256, 1>(a, p, s);
+  }
+}
+
+}  // namespace pop
