@@ -288,12 +288,14 @@ int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int
  *          inputs 32 j + 8 t .. + 7 of the 128; bits 4 p .. 4 p + 3 of a word are the code of its input 2 p (p < 4) or
  *          2 (p - 4) + 1;
  *   scales bf16, zeros uint8 [ceil(N / 16)][ceil(K / 128)][16][128 / group]: row r of the tile at index 2 (r % 8) + r / 8.
- * What lies behind row N or input K is read and has no effect, whatever it is. codes and scales 16-byte aligned, zeros 8-byte.
+ * What lies behind row N or input K is read and has no effect, whatever it is. codes, scales and zeros 16-byte aligned.
  *
  * pop_k_gemv_w4: pop_k_gemv with such weights: out[b][n] = sum_k x[b][k] W[n][k], x bf16 [B][ldx] (16-byte aligned, ldx and K
  * multiples of 8), any B (made for 1 to some dozens of rows). Modes as pop_k_gemv: 0 fp32 store, 2 fp32 +=, 3 gated -> bf16
- * (N a multiple of 256: 128 gate rows, then the 128 matching up rows; act 0 SiLU, 1 tanh-GELU). A group's products are summed
- * exactly formed and in fp32, then scaled and summed in fp32 in an order that depends on the sizes alone. */
+ * (N a multiple of 256: 128 gate rows, then the 128 matching up rows; act 0 SiLU, 1 tanh-GELU). The products of
+ * codes and activations are exact (of activations within 2^-27 of the largest of their 128 inputs; smaller ones are off by at
+ * most 2^-36 of it); sums are fp32, in an order that depends on the sizes alone. An activation row with an infinite or NaN
+ * input gives a row of NaN. */
 int pop_k_gemv_w4(const void* x, int64_t ldx, const void* codes, const void* scales, const void* zeros, int32_t group,
                   void* out, int64_t ldo, int32_t B, int32_t N, int32_t K, int32_t mode, int32_t act, int32_t n_valid,
                   void* stream);
