@@ -12,18 +12,9 @@
 namespace pop {
 namespace {
 
-constexpr int WARPS = 16;       // of a CTA, one CTA per SM
-constexpr int SLOT = 2;         // chunks of 128 inputs in a slot of a warp's ring
-constexpr int RING = 4;
-constexpr int SMEM_LIMIT = 227 * 1024;
-
-template <int GRP>
-struct G4 {
-  static constexpr int GPC = 128 / GRP;             // groups of a chunk
-  static constexpr int SC = 32 * GPC, ZR = 16 * GPC;
-  static constexpr int SLOT_BYTES = SLOT * (1024 + SC + ZR);      // codes, then scales, then zeros
-  static constexpr int RING_BYTES = WARPS * RING * SLOT_BYTES;
-};
+constexpr int WARPS = 8;        // of a CTA. Two CTAs per SM, so that one's beginning and end (and the next launch's) lie beside
+                                // the other's work
+constexpr int SMEM_LIMIT = 112 * 1024;
 
 struct Gemv4Dev {
   const bf16* x; int64_t ldx;
@@ -35,7 +26,6 @@ struct Gemv4Dev {
   int clusters, cs;             // cs CTAs of a cluster share tiles and split their chunks
   int sc, passes;               // chunks of a CTA in a pass over x; passes
   int tpr, rounds;              // tiles of a warp between two exchanges of sums; such rounds
-  int* status;
 };
 
 __device__ __forceinline__ uint4 lds128(uint32_t a) {
@@ -48,16 +38,25 @@ __device__ __forceinline__ float2 lds_f2(uint32_t a) {
   asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a));
   return v;
 }
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-               "r"(bytes), "r"(bar)
-               : "memory");
+__device__ __forceinline__ uint4 ld_codes(const uint8_t* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
 }
-__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+// D = A B + (first ? 0 : D), m16n8k16
+__device__ __forceinline__ void mma_f16(float (&d)[4], bool first, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                        uint32_t b0, uint32_t b1) {
+  if (first)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
+        "{%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+  else
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
   const __half2 h = __floats2half2_rn(a, b);
@@ -78,21 +77,20 @@ __device__ __forceinline__ float act_of(float g, int act) {
 //
 // The weight rows are the M side of the warp-level MMA, up to 8 NT activation rows its N side: a tile of 16 rows x 128 inputs
 // is 1 KB in one piece, 16 bytes of row g and 16 of row g + 8 to lane (g = lane / 4, t = lane % 4), word j inputs 32 j + 8 t ..
-// + 7. A warp streams whole tiles through a ring of its own with bulk copies, so nothing is exchanged between warps. The CTAs
-// of a cluster have the same tiles and a part of the inputs each: their activations are converted once, into shared memory,
-// and the sums of some tiles per warp are exchanged at a time, added in the order of the ranks.
+// + 7. A warp streams whole tiles into registers, so nothing is exchanged between warps. The CTAs of a cluster have the same
+// tiles and a part of the inputs each: their activations are converted once, into shared memory, and the sums of some tiles
+// per warp are exchanged at a time, added in the order of the ranks.
 template <int GRP, int NT, bool ZEROS>
-__global__ void __launch_bounds__(WARPS * 32, 1) gemv4_kernel(const __grid_constant__ Gemv4Dev p) {
-  using C = G4<GRP>;
-  constexpr int GPC = C::GPC, COLS = NT * 8;
+__global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_constant__ Gemv4Dev p) {
+  constexpr int GPC = 128 / GRP, COLS = NT * 8, SC = 32 * GPC, ZR = 16 * GPC;
+  constexpr int U = GPC == 1 && NT == 1 ? 4 : 2;    // chunks of a batch of loads; two batches are in flight
   extern __shared__ __align__(128) uint8_t smem[];
   const int xs = p.sc * 256 + 64;                   // bytes of an activation row: 64 off a multiple of 128, so that the
                                                     // rows of a quarter-warp's loads lie in other banks
-  uint8_t* s_x = smem + C::RING_BYTES;
-  uint8_t* s_zero = s_x + COLS * xs;                // 256 zeros: what lanes without an activation row read
-  float* s_acc = reinterpret_cast<float*>(s_zero + 256);          // [tpr][WARPS][COLS][16]
+  uint8_t* s_zero = smem;                           // 256 zeros: what lanes without an activation row read
+  uint8_t* s_x = smem + 256;
+  float* s_acc = reinterpret_cast<float*>(s_x + COLS * xs);       // [tpr][WARPS][NT][32 lanes][4]
   float* s_sum = s_acc + p.tpr * WARPS * COLS * 16;               // [sc][1 + GPC][COLS]: 2^-shift; sums of the groups
-  uint64_t* bars = reinterpret_cast<uint64_t*>(s_sum + p.sc * (1 + GPC) * COLS);      // [WARPS][RING]
   const int tid = threadIdx.x, lane = tid & 31, wic = tid >> 5, g = lane >> 2, t = lane & 3;
   const int rank = blockIdx.x % p.cs, cluster = blockIdx.x / p.cs;
   const int row0 = blockIdx.y * COLS, rows = min(p.B - row0, COLS);
@@ -100,56 +98,74 @@ __global__ void __launch_bounds__(WARPS * 32, 1) gemv4_kernel(const __grid_const
   const int mine = p.tiles > me ? (p.tiles - me + warps - 1) / warps : 0;         // tiles me, me + warps, ..
   const bool gated = p.mode == 3;
   chain_trigger();
-
-  // gated: gate tile and up tile follow each other, so that both are in one cluster
-  auto tile_of = [&](int i) {
-    const int u = me + i * warps;
-    return gated ? (u >> 4) * 16 + ((u >> 1) & 7) + 8 * (u & 1) : u;
-  };
   auto chunks_of = [&](int pass, int& c0) {
     c0 = min((pass * p.cs + rank) * p.sc, p.kt);
     return min(p.sc, p.kt - c0);
   };
-  uint64_t* bar = bars + wic * RING;
-  if (lane < RING) mbar_init(&bar[lane], 1);
-  fence_barrier_init();
-  for (int i = tid; i < 64; i += WARPS * 32) reinterpret_cast<uint32_t*>(s_zero)[i] = 0;
-  __syncwarp();
 
-  // ---- the order of slots: round, pass over x, tile, chunks
-  const uint32_t ring = smem_u32(smem + wic * (RING * C::SLOT_BYTES)), bar0 = smem_u32(bar);
-  int l_round = 0, l_pass = 0, l_i = -1, l_left = 0, l_slot = 0;
-  int64_t l_chunk = 0;
-  auto issue = [&] {
-    while (l_left <= 0) {                           // to the next tile that there is
-      if (l_round >= p.rounds) return;
-      if (++l_i >= min(mine, (l_round + 1) * p.tpr)) {
-        if (++l_pass >= p.passes) {
-          l_pass = 0;
-          ++l_round;
+  // ---- loads: the batches of a round and pass in their order
+  struct Batch {
+    uint4 lo[U], hi[U];
+    uint32_t sc[U][GPC];                            // scales of row g, then of row g + 8
+    uint32_t zr[U][GPC == 4 ? 2 : 1];               // their zeros, a byte each
+  };
+  Batch b0, b1;
+  int l_i = 0, l_end = 0, l_s = 0, l_nc = 0, l_c0 = 0;
+  const uint8_t *l_codes = nullptr, *l_scales = nullptr, *l_zeros = nullptr;
+  auto set_tile = [&] {
+    // gated: gate tile and up tile follow each other, so that both are in one cluster
+    const int u = me + l_i * warps, tile = gated ? (u >> 4) * 16 + ((u >> 1) & 7) + 8 * (u & 1) : u;
+    const int64_t chunk = (int64_t)tile * p.kt + l_c0;
+    l_codes = p.codes + chunk * 1024 + lane * 16;
+    l_scales = p.scales + chunk * SC + g * (4 * GPC);
+    if (ZEROS) l_zeros = p.zeros + chunk * ZR + g * (2 * GPC);
+    l_s = 0;
+  };
+  auto load_next = [&](Batch& q) {
+    if (l_i >= l_end) return;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (l_s + u < l_nc) {
+        q.lo[u] = ld_codes(l_codes + u * 1024);
+        q.hi[u] = ld_codes(l_codes + u * 1024 + 512);
+        if constexpr (GPC == 1) {
+          q.sc[u][0] = __ldg(reinterpret_cast<const uint32_t*>(l_scales + u * SC));
+        } else if constexpr (GPC == 2) {
+          const uint2 v = __ldg(reinterpret_cast<const uint2*>(l_scales + u * SC));
+          q.sc[u][0] = v.x; q.sc[u][1] = v.y;
+        } else {
+          const uint4 v = __ldg(reinterpret_cast<const uint4*>(l_scales + u * SC));
+          q.sc[u][0] = v.x; q.sc[u][1] = v.y; q.sc[u][2] = v.z; q.sc[u][3] = v.w;
         }
-        l_i = l_round * p.tpr - 1;
-        continue;
+        if constexpr (ZEROS) {
+          if constexpr (GPC == 1) {
+            q.zr[u][0] = __ldg(reinterpret_cast<const uint16_t*>(l_zeros + u * ZR));
+          } else if constexpr (GPC == 2) {
+            q.zr[u][0] = __ldg(reinterpret_cast<const uint32_t*>(l_zeros + u * ZR));
+          } else {
+            const uint2 v = __ldg(reinterpret_cast<const uint2*>(l_zeros + u * ZR));
+            q.zr[u][0] = v.x; q.zr[u][1] = v.y;
+          }
+        }
       }
-      int c0;
-      l_left = chunks_of(l_pass, c0);
-      l_chunk = (int64_t)tile_of(l_i) * p.kt + c0;
     }
-    const int cnt = min(SLOT, l_left);
-    if (lane == 0) {
-      const uint32_t dst = ring + l_slot * C::SLOT_BYTES, b = bar0 + l_slot * 8;
-      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(cnt * (1024 + C::SC + (ZEROS ? C::ZR : 0))) : "memory");
-      bulk_load(dst, p.codes + l_chunk * 1024, cnt * 1024, b);
-      bulk_load(dst + SLOT * 1024, p.scales + l_chunk * C::SC, cnt * C::SC, b);
-      if (ZEROS) bulk_load(dst + SLOT * (1024 + C::SC), p.zeros + l_chunk * C::ZR, cnt * C::ZR, b);
-    }
-    l_slot = l_slot == RING - 1 ? 0 : l_slot + 1;
-    l_chunk += cnt;
-    l_left -= cnt;
+    l_s += U;
+    l_codes += U * 1024;
+    l_scales += U * SC;
+    if (ZEROS) l_zeros += U * ZR;
+    if (l_s >= l_nc && ++l_i < l_end) set_tile();
+  };
+  auto begin = [&](int round, int pass) {
+    l_nc = chunks_of(pass, l_c0);
+    l_i = round * p.tpr;
+    l_end = l_nc > 0 ? min(mine, l_i + p.tpr) : 0;
+    if (l_i < l_end) set_tile();
+    load_next(b0);
+    load_next(b1);
   };
   // the first weights go out before the wait on the preceding kernel: no kernel of the library writes them
-#pragma unroll 1
-  for (int i = 0; i < RING; ++i) issue();
+  begin(0, 0);
+  if (tid < 64) reinterpret_cast<uint32_t*>(s_zero)[tid] = 0;
   chain_wait();
 
   uint32_t xp[NT], xstep[NT];
@@ -159,9 +175,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) gemv4_kernel(const __grid_const
     xp[n] = smem_u32(has ? s_x + (n * 8 + g) * xs : s_zero) + t * 16;
     xstep[n] = has ? 256 : 0;
   }
-  int slot = 0;
-  uint32_t phase = 0;
-  bool ok = true, pending = false;                  // pending: peers may still be reading this CTA's sums
+  bool pending = false;                             // peers may still be reading this CTA's sums
   auto settle = [&] {
     if (pending) cluster_wait();
     pending = false;
@@ -208,109 +222,102 @@ __global__ void __launch_bounds__(WARPS * 32, 1) gemv4_kernel(const __grid_const
         }
         __syncthreads();
       }
-      const int end = min(mine, (round + 1) * p.tpr);
-      for (int i = round * p.tpr; i < end && ok; ++i) {
-        float tot[NT][4];
+      // ---- products
+      const int tiles = nc > 0 ? max(0, min(mine - round * p.tpr, p.tpr)) : 0, ppt = (nc + U - 1) / U;
+      float4* acc = reinterpret_cast<float4*>(s_acc) + wic * (NT * 32) + lane;
+      float tot[NT][4];
+      uint32_t x_at[NT], sum_at = 0;
+      int s = 0;
+      auto reset = [&] {
+        s = 0;
+        sum_at = smem_u32(s_sum) + t * 8;
 #pragma unroll
-        for (int n = 0; n < NT; ++n) tot[n][0] = tot[n][1] = tot[n][2] = tot[n][3] = 0.f;
-        uint32_t x_at[NT], sum_at = smem_u32(s_sum) + t * 8;
+        for (int n = 0; n < NT; ++n) {
+          x_at[n] = xp[n];
+          tot[n][0] = tot[n][1] = tot[n][2] = tot[n][3] = 0.f;
+        }
+      };
+      auto store = [&] {
+        settle();
 #pragma unroll
-        for (int n = 0; n < NT; ++n) x_at[n] = xp[n];
-        for (int s = 0; s < nc; s += SLOT) {
-          if (!mbar_wait(&bar[slot], phase)) {
-            ok = false;
-            break;
+        for (int n = 0; n < NT; ++n) {
+          float4 v = make_float4(tot[n][0], tot[n][1], tot[n][2], tot[n][3]);
+          if (pass > 0) {
+            const float4 o = acc[n * 32];
+            v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
           }
-          const uint32_t base = ring + slot * C::SLOT_BYTES;
+          acc[n * 32] = v;
+        }
+        acc += WARPS * (NT * 32);
+      };
+      reset();
+      auto step = [&](Batch& q) {
 #pragma unroll
-          for (int q = 0; q < SLOT; ++q) {
-            if (s + q < nc) {
-              const uint32_t cb = base + q * 1024 + lane * 16;
-              const uint4 lo = lds128(cb), hi = lds128(cb + 512);
-              const uint32_t sb = base + SLOT * 1024 + q * C::SC + g * (4 * GPC);
-              const uint32_t zb = base + SLOT * (1024 + C::SC) + q * C::ZR + g * (2 * GPC);
-              uint32_t sw[GPC], zw[2] = {0, 0};
-              if constexpr (GPC == 1) {
-                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sw[0]) : "r"(sb));
-              } else if constexpr (GPC == 2) {
-                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(sw[0]), "=r"(sw[1]) : "r"(sb));
-              } else {
-                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(sw[0]), "=r"(sw[1]), "=r"(sw[2]), "=r"(sw[3]) : "r"(sb));
-              }
-              if constexpr (ZEROS) {
-                if constexpr (GPC == 1) {
-                  uint16_t z;
-                  asm volatile("ld.shared.u16 %0, [%1];" : "=h"(z) : "r"(zb));
-                  zw[0] = z;
-                } else if constexpr (GPC == 2) {
-                  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(zw[0]) : "r"(zb));
-                } else {
-                  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(zw[0]), "=r"(zw[1]) : "r"(zb));
-                }
-              }
-              float2 fx[NT];
+        for (int u = 0; u < U; ++u) {
+          if (s + u < nc) {
+            const uint4 lo = q.lo[u], hi = q.hi[u];
+            float2 fx[NT];
 #pragma unroll
-              for (int n = 0; n < NT; ++n) fx[n] = lds_f2(sum_at + n * 32);
-              constexpr int JPG = 4 / GPC;          // words of a group
+            for (int n = 0; n < NT; ++n) fx[n] = lds_f2(sum_at + u * ((1 + GPC) * COLS * 4) + n * 32);
+            constexpr int JPG = 4 / GPC;            // words of a group
 #pragma unroll
-              for (int grp = 0; grp < GPC; ++grp) {
-                float d[NT][4];
+            for (int grp = 0; grp < GPC; ++grp) {
+              float d[NT][4];
 #pragma unroll
-                for (int n = 0; n < NT; ++n) d[n][0] = d[n][1] = d[n][2] = d[n][3] = 0.f;
-#pragma unroll
-                for (int jj = 0; jj < JPG; ++jj) {
-                  const int j = grp * JPG + jj;
-                  const uint32_t wl = j == 0 ? lo.x : j == 1 ? lo.y : j == 2 ? lo.z : lo.w;
-                  const uint32_t wh = j == 0 ? hi.x : j == 1 ? hi.y : j == 2 ? hi.z : hi.w;
-                  const uint32_t ul = wl >> 8, uh = wh >> 8;
-#pragma unroll
-                  for (int n = 0; n < NT; ++n) {
-                    const uint4 xv = lds128(x_at[n] + j * 64);
-                    mma_f16(d[n], wl & 0x000f000fu, wh & 0x000f000fu, wl & 0x00f000f0u, wh & 0x00f000f0u, xv.x, xv.y);
-                    mma_f16(d[n], ul & 0x000f000fu, uh & 0x000f000fu, ul & 0x00f000f0u, uh & 0x00f000f0u, xv.z, xv.w);
-                  }
-                }
-                // scales lie as [row half][group], halves of words; zeros as bytes. What lies behind K is never used.
-                const uint32_t w0 = sw[grp / 2], w1 = sw[(GPC + grp) / 2];
-                float f0 = __uint_as_float(grp & 1 ? w0 & 0xffff0000u : w0 << 16);
-                float f1 = __uint_as_float((GPC + grp) & 1 ? w1 & 0xffff0000u : w1 << 16);
-                if (GPC > 1 && grp > 0 && (c0 + s + q) * 128 + grp * GRP >= p.K) f0 = f1 = 0.f;
-                float z0 = 1.f, z1 = 1.f;
-                if constexpr (ZEROS) {              // 2^23 + zero, minus 2^23
-                  const uint32_t b0 = zw[0] >> (8 * grp), b1 = GPC == 4 ? zw[1] >> (8 * grp) : zw[0] >> (8 * (GPC + grp));
-                  z0 = __uint_as_float((b0 & 15u) | 0x4b000000u) - 8388608.f;
-                  z1 = __uint_as_float((b1 & 15u) | 0x4b000000u) - 8388608.f;
-                }
+              for (int jj = 0; jj < JPG; ++jj) {
+                const int j = grp * JPG + jj;
+                const uint32_t wl = j == 0 ? lo.x : j == 1 ? lo.y : j == 2 ? lo.z : lo.w;
+                const uint32_t wh = j == 0 ? hi.x : j == 1 ? hi.y : j == 2 ? hi.z : hi.w;
+                const uint32_t ul = wl >> 8, uh = wh >> 8;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                  const float2 sx = lds_f2(sum_at + (1 + grp) * (COLS * 4) + n * 32);
-                  tot[n][0] = fmaf(fmaf(d[n][0], fx[n].x, -z0 * sx.x), f0, tot[n][0]);
-                  tot[n][1] = fmaf(fmaf(d[n][1], fx[n].y, -z0 * sx.y), f0, tot[n][1]);
-                  tot[n][2] = fmaf(fmaf(d[n][2], fx[n].x, -z1 * sx.x), f1, tot[n][2]);
-                  tot[n][3] = fmaf(fmaf(d[n][3], fx[n].y, -z1 * sx.y), f1, tot[n][3]);
+                  const uint4 xv = lds128(x_at[n] + j * 64);
+                  mma_f16(d[n], jj == 0, wl & 0x000f000fu, wh & 0x000f000fu, wl & 0x00f000f0u, wh & 0x00f000f0u, xv.x, xv.y);
+                  mma_f16(d[n], false, ul & 0x000f000fu, uh & 0x000f000fu, ul & 0x00f000f0u, uh & 0x00f000f0u, xv.z, xv.w);
                 }
               }
+              // scales lie as [row half][group], halves of words; zeros as bytes. What lies behind K is never used.
+              const uint32_t w0 = q.sc[u][grp / 2], w1 = q.sc[u][(GPC + grp) / 2];
+              float f0 = __uint_as_float(grp & 1 ? w0 & 0xffff0000u : w0 << 16);
+              float f1 = __uint_as_float((GPC + grp) & 1 ? w1 & 0xffff0000u : w1 << 16);
+              if (GPC > 1 && grp > 0 && (c0 + s + u) * 128 + grp * GRP >= p.K) f0 = f1 = 0.f;
+              float z0 = 1.f, z1 = 1.f;
+              if constexpr (ZEROS) {                // 2^23 + zero, minus 2^23
+                const uint32_t y0 = q.zr[u][0] >> (8 * grp), y1 = GPC == 4 ? q.zr[u][GPC == 4 ? 1 : 0] >> (8 * grp) : q.zr[u][0] >> (8 * (GPC + grp));
+                z0 = __uint_as_float((y0 & 15u) | 0x4b000000u) - 8388608.f;
+                z1 = __uint_as_float((y1 & 15u) | 0x4b000000u) - 8388608.f;
+              }
 #pragma unroll
-              for (int n = 0; n < NT; ++n) x_at[n] += xstep[n];
-              sum_at += (1 + GPC) * (COLS * 4);
+              for (int n = 0; n < NT; ++n) {
+                const float2 sx = lds_f2(sum_at + (u * (1 + GPC) + 1 + grp) * (COLS * 4) + n * 32);
+                tot[n][0] = fmaf(fmaf(d[n][0], fx[n].x, -z0 * sx.x), f0, tot[n][0]);
+                tot[n][1] = fmaf(fmaf(d[n][1], fx[n].y, -z0 * sx.y), f0, tot[n][1]);
+                tot[n][2] = fmaf(fmaf(d[n][2], fx[n].x, -z1 * sx.x), f1, tot[n][2]);
+                tot[n][3] = fmaf(fmaf(d[n][3], fx[n].y, -z1 * sx.y), f1, tot[n][3]);
+              }
             }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) x_at[n] += xstep[n];
           }
-          __syncwarp();
-          issue();                                  // into the slot that is free now
-          slot = slot == RING - 1 ? 0 : slot + 1;
-          phase ^= slot == 0 ? 1u : 0u;
         }
-        settle();
-        // sum i of n-tile n: row g + 8 (i / 2) of the tile, activation row 2 t + i % 2
-        float* acc = s_acc + ((i - round * p.tpr) * WARPS + wic) * (COLS * 16);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float* dst = acc + (n * 8 + 2 * t + (r & 1)) * 16 + g + 8 * (r >> 1);
-            *dst = pass == 0 ? tot[n][r] : *dst + tot[n][r];
-          }
+        load_next(q);
+        s += U;
+        sum_at += U * ((1 + GPC) * COLS * 4);
+        if (s >= nc) {
+          store();
+          reset();
+        }
+      };
+      const int pieces = tiles * ppt;
+      for (int f = 0; f < pieces; f += 2) {
+        step(b0);
+        if (f + 1 < pieces) step(b1);
       }
+      if (nc == 0 && pass == 0) {                   // more CTAs than chunks: sums of nothing
+        for (int i = round * p.tpr; i < min(mine, (round + 1) * p.tpr); ++i) store();
+      }
+      if (pass + 1 < p.passes) begin(round, pass + 1);
+      else if (round + 1 < p.rounds) begin(round + 1, 0);
     }
     // ---- exchange: every rank finishes its share of the tiles
     settle();
@@ -320,13 +327,14 @@ __global__ void __launch_bounds__(WARPS * 32, 1) gemv4_kernel(const __grid_const
     } else {
       __syncthreads();
     }
-    const int step = gated ? 2 : 1;
-    for (int e = tid + WARPS * 32 * rank; e < p.tpr * WARPS / step * (COLS * 16); e += WARPS * 32 * p.cs) {
-      const int row = e & 15, b = (e >> 4) % COLS, sl = (e >> 4) / COLS * step;
+    const int each = gated ? 2 : 1;
+    for (int e = tid + WARPS * 32 * rank; e < p.tpr * WARPS / each * (COLS * 16); e += WARPS * 32 * p.cs) {
+      const int row = e & 15, b = (e >> 4) % COLS, sl = (e >> 4) / COLS * each;
       const int u = cluster * WARPS + (sl % WARPS) + (round * p.tpr + sl / WARPS) * warps;
       if (u >= p.tiles || b >= rows) continue;
       auto sum_of = [&](int sl_) {
-        const uint32_t a = smem_u32(s_acc + sl_ * (COLS * 16) + b * 16 + row);
+        // row g + 8 i of the tile and activation row 2 t + j: value 2 i + j of lane 4 g + t
+        const uint32_t a = smem_u32(s_acc + ((sl_ * NT + (b >> 3)) * 32 + (row & 7) * 4 + ((b & 7) >> 1)) * 4 + (row >> 3) * 2 + (b & 1));
         float v = 0.f;
         for (int r = 0; r < p.cs; ++r) {
           float w;
@@ -354,10 +362,6 @@ __global__ void __launch_bounds__(WARPS * 32, 1) gemv4_kernel(const __grid_const
     pending = p.cs > 1;
   }
   settle();
-  if (!ok) {
-    if (lane == 0) atomicMin(p.status, (int)POP_E_DEVICE_TIMEOUT);
-    for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // let in-flight bulk copies land
-  }
 }
 
 // Clusters of cs CTAs that the GPU holds at once (of the device that was current at the first call)
@@ -378,7 +382,7 @@ int max_clusters(int cs) {
   cfg.numAttrs = 1;
   if (cudaOccupancyMaxActiveClusters(&most, gemv4_kernel<GRP, NT, ZEROS>, &cfg) != cudaSuccess || most < 1) {
     cudaGetLastError();
-    return device_sms() / cs;
+    return 2 * device_sms() / cs;
   }
   known[cs].store(most, std::memory_order_relaxed);
   return most;
@@ -386,7 +390,6 @@ int max_clusters(int cs) {
 
 template <int GRP, int NT, bool ZEROS>
 int launch_t(Gemv4Dev& p, cudaStream_t s) {
-  using C = G4<GRP>;
   static std::atomic<uint64_t> configured{0};
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return POP_E_CUDA;
@@ -397,10 +400,10 @@ int launch_t(Gemv4Dev& p, cudaStream_t s) {
     configured.fetch_or(bit, std::memory_order_relaxed);
   }
   constexpr int COLS = NT * 8;
-  // shared memory beside the ring: activations with their sums, and sums of products
-  constexpr int ROOM = SMEM_LIMIT - C::RING_BYTES - 256 - COLS * 64 - WARPS * RING * 8 - 128;
-  constexpr int TPR_BYTES = WARPS * COLS * 64, SC_BYTES = COLS * (256 + 4 + 4 * C::GPC);
-  static_assert(ROOM >= TPR_BYTES + 8 * SC_BYTES, "shared memory budget");
+  // shared memory: activations with their sums, and sums of products
+  constexpr int ROOM = SMEM_LIMIT - 256 - COLS * 64;
+  constexpr int TPR_BYTES = WARPS * COLS * 64, SC_BYTES = COLS * (256 + 4 + 4 * (128 / GRP));
+  static_assert(ROOM >= TPR_BYTES + 4 * SC_BYTES, "shared memory budget");
   // Warps take tiles in turn: the cluster size whose busiest warp has the fewest chunks. A tile's beginning and end cost
   // about one chunk, the exchange within a cluster two.
   int64_t best = INT64_MAX;
@@ -424,9 +427,7 @@ int launch_t(Gemv4Dev& p, cudaStream_t s) {
   p.tpr = ceil_div(n_i, p.rounds);
   const int slabs = ceil_div(p.B, COLS);
   if (slabs > 65535) return POP_E_INVALID;
-  p.status = status_word();
-  if (!p.status) return POP_E_CUDA;
-  const size_t smem = C::RING_BYTES + (size_t)p.sc * SC_BYTES + COLS * 64 + 256 + (size_t)p.tpr * TPR_BYTES + WARPS * RING * 8;
+  const size_t smem = 256 + (size_t)p.sc * SC_BYTES + COLS * 64 + (size_t)p.tpr * TPR_BYTES;
   ProfScope prof(PROF_GEMV, (double)p.N * p.K * (0.5 + (p.zeros ? 3.0 : 2.0) / GRP) * slabs, s);
   if (launch_chained_cluster_x(gemv4_kernel<GRP, NT, ZEROS>, dim3(p.clusters * p.cs, slabs), dim3(WARPS * 32), smem, s,
                                (unsigned)p.cs, p) != cudaSuccess)
