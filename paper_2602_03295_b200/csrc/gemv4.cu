@@ -14,6 +14,8 @@ namespace {
 
 constexpr int WARPS = 8;        // of a CTA. Two CTAs per SM, so that one's beginning and end (and the next launch's) lie beside
                                 // the other's work
+constexpr int SLOT = 4;         // chunks of 128 inputs in a slot of a warp's ring
+constexpr int RING = 2;
 constexpr int SMEM_LIMIT = 112 * 1024;
 
 struct Gemv4Dev {
@@ -25,35 +27,30 @@ struct Gemv4Dev {
   int tiles;                    // tiles of 16 rows
   int clusters, cs;             // cs CTAs of a cluster share tiles and split their chunks
   int sc, passes;               // chunks of a CTA in a pass over x; passes
-  int tpr, rounds;              // tiles of a warp between two exchanges of sums; such rounds
+  int tpr, rounds;              // tiles of a cluster between two exchanges of sums; such rounds
+  int grain;                    // a warp's stretch begins at a multiple of it
+  int deal, deal_rest;          // tiles (gated: pairs) of each cluster; how many clusters have one more
+  uint32_t sc_inv, per_inv;     // ceil(2^32 / sc), ceil(2^32 / (16 rows)): products with them replace divisions
+  int rows;                     // activation rows that shared memory has room for
+  int* status;
 };
 
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ float2 lds_f2(uint32_t a) {
-  float2 v;
-  asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ uint4 ld_codes(const uint8_t* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
 }
 // D = A B + (first ? 0 : D), m16n8k16
 __device__ __forceinline__ void mma_f16(float (&d)[4], bool first, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                         uint32_t b0, uint32_t b1) {
   if (first)
-    asm volatile(
+    asm(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, "
         "{%10, %10, %10, %10};"
         : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
   else
-    asm volatile(
+    asm(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -77,105 +74,109 @@ __device__ __forceinline__ float act_of(float g, int act) {
 //
 // The weight rows are the M side of the warp-level MMA, up to 8 NT activation rows its N side: a tile of 16 rows x 128 inputs
 // is 1 KB in one piece, 16 bytes of row g and 16 of row g + 8 to lane (g = lane / 4, t = lane % 4), word j inputs 32 j + 8 t ..
-// + 7. A warp streams whole tiles into registers, so nothing is exchanged between warps. The CTAs of a cluster have the same
-// tiles and a part of the inputs each: their activations are converted once, into shared memory, and the sums of some tiles
-// per warp are exchanged at a time, added in the order of the ranks.
+// + 7. The chunks of a CTA's tiles are one line, of which each warp streams an equal stretch through a ring of its own; bulk
+// copies keep more bytes in flight than loads to registers (1 x 4096 -> 128256: 46 us, 5.8 TB/s, against 55). Where there are
+// fewer tiles than CTAs, or many rows to convert, the CTAs of a cluster have the same tiles and a part of the inputs each. The
+// loop over the chunks stays rolled: each launch meets its instructions cold (unrolled four times: 0.5 to 1 us more a call).
+// What a call costs beside its bytes, 1 x 4096 -> 4096 (4.9 us; the bytes take 1.3): launch, 0.5 us to the first copy, 0.9
+// until the activations are converted, 0.8 for exchange and stores.
 template <int GRP, int NT, bool ZEROS>
 __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_constant__ Gemv4Dev p) {
   constexpr int GPC = 128 / GRP, COLS = NT * 8, SC = 32 * GPC, ZR = 16 * GPC;
-  constexpr int U = GPC == 1 && NT == 1 ? 4 : 2;    // chunks of a batch of loads; two batches are in flight
+  constexpr int SLOT_BYTES = SLOT * (1024 + SC + (ZEROS ? ZR : 0));     // codes, then scales, then zeros
   extern __shared__ __align__(128) uint8_t smem[];
   const int xs = p.sc * 256 + 64;                   // bytes of an activation row: 64 off a multiple of 128, so that the
                                                     // rows of a quarter-warp's loads lie in other banks
-  uint8_t* s_zero = smem;                           // 256 zeros: what lanes without an activation row read
-  uint8_t* s_x = smem + 256;
-  float* s_acc = reinterpret_cast<float*>(s_x + COLS * xs);       // [tpr][WARPS][NT][32 lanes][4]
-  float* s_sum = s_acc + p.tpr * WARPS * COLS * 16;               // [sc][1 + GPC][COLS]: 2^-shift; sums of the groups
   const int tid = threadIdx.x, lane = tid & 31, wic = tid >> 5, g = lane >> 2, t = lane & 3;
-  const int rank = blockIdx.x % p.cs, cluster = blockIdx.x / p.cs;
   const int row0 = blockIdx.y * COLS, rows = min(p.B - row0, COLS);
-  const int warps = p.clusters * WARPS, me = cluster * WARPS + wic;
-  const int mine = p.tiles > me ? (p.tiles - me + warps - 1) / warps : 0;         // tiles me, me + warps, ..
+  const uint8_t* s_ring = smem + wic * (RING * SLOT_BYTES);
+  uint8_t* s_zero = smem + WARPS * RING * SLOT_BYTES;             // 256 zeros: what lanes without an activation row read
+  uint64_t* s_bar = reinterpret_cast<uint64_t*>(s_zero + 256);    // [WARPS][RING]
+  float* s_sum = reinterpret_cast<float*>(s_bar + WARPS * RING);  // [sc][1 + GPC][COLS]: 2^-shift; sums of the groups
+  uint8_t* s_x = reinterpret_cast<uint8_t*>(s_sum + p.sc * (1 + GPC) * COLS);
+  float* s_acc = reinterpret_cast<float*>(s_x + p.rows * xs);     // [tpr + WARPS][rows][16]
+  const int rank = cluster_ctarank();
+  int cluster;
+  asm("mov.u32 %0, %%clusterid.x;" : "=r"(cluster));
   const bool gated = p.mode == 3;
+  // Tiles are dealt to the clusters in turn (gated: a gate tile with its up tile, tiles 2 n and 2 n + 1 of the count)
+  const int each = gated ? 2 : 1, dealt = (p.deal + (cluster < p.deal_rest ? 1 : 0)) * each;
+  auto tile_of = [&](int n) {
+    if (!gated) return n * p.clusters + cluster;
+    const int pair = (n >> 1) * p.clusters + cluster;
+    return (pair >> 3) * 16 + (pair & 7) + 8 * (n & 1);
+  };
+  // The chunks of a round's tiles, p.sc each, are one line, and each warp has an equal stretch of it; the sums of tile n in
+  // warp w's stretch go to place n + w, which no other part has
+  auto stretch = [&](int round, int w) {
+    const int tiles = max(0, min(p.tpr, dealt - round * p.tpr)), line = tiles * p.sc;
+    return min(((line * w >> 3) + p.grain - 1) & -p.grain, line);
+  };
   chain_trigger();
   auto chunks_of = [&](int pass, int& c0) {
     c0 = min((pass * p.cs + rank) * p.sc, p.kt);
     return min(p.sc, p.kt - c0);
   };
+  const uint32_t ring = smem_u32(s_ring), bar = smem_u32(s_bar + wic * RING);
+  if (lane < RING) mbar_init(s_bar + wic * RING + lane, 1);
+  fence_barrier_init();
+  __syncwarp();
 
-  // ---- loads: the batches of a round and pass in their order
-  struct Batch {
-    uint4 lo[U], hi[U];
-    uint32_t sc[U][GPC];                            // scales of row g, then of row g + 8
-    uint32_t zr[U][GPC == 4 ? 2 : 1];               // their zeros, a byte each
-  };
-  Batch b0, b1;
-  int l_i = 0, l_end = 0, l_s = 0, l_nc = 0, l_c0 = 0;
+  // ---- copies, in the order in which they are used: round, pass over x, tile, chunks
+  int l_round = 0, l_pass = 0, l_left = 0, l_slot = 0, l_at = stretch(0, wic), l_end = stretch(0, wic + 1);
   const uint8_t *l_codes = nullptr, *l_scales = nullptr, *l_zeros = nullptr;
-  auto set_tile = [&] {
-    // gated: gate tile and up tile follow each other, so that both are in one cluster
-    const int u = me + l_i * warps, tile = gated ? (u >> 4) * 16 + ((u >> 1) & 7) + 8 * (u & 1) : u;
-    const int64_t chunk = (int64_t)tile * p.kt + l_c0;
-    l_codes = p.codes + chunk * 1024 + lane * 16;
-    l_scales = p.scales + chunk * SC + g * (4 * GPC);
-    if (ZEROS) l_zeros = p.zeros + chunk * ZR + g * (2 * GPC);
-    l_s = 0;
-  };
-  auto load_next = [&](Batch& q) {
-    if (l_i >= l_end) return;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (l_s + u < l_nc) {
-        q.lo[u] = ld_codes(l_codes + u * 1024);
-        q.hi[u] = ld_codes(l_codes + u * 1024 + 512);
-        if constexpr (GPC == 1) {
-          q.sc[u][0] = __ldg(reinterpret_cast<const uint32_t*>(l_scales + u * SC));
-        } else if constexpr (GPC == 2) {
-          const uint2 v = __ldg(reinterpret_cast<const uint2*>(l_scales + u * SC));
-          q.sc[u][0] = v.x; q.sc[u][1] = v.y;
-        } else {
-          const uint4 v = __ldg(reinterpret_cast<const uint4*>(l_scales + u * SC));
-          q.sc[u][0] = v.x; q.sc[u][1] = v.y; q.sc[u][2] = v.z; q.sc[u][3] = v.w;
+  auto issue = [&] {
+    while (l_left <= 0) {                           // to the next part of a tile that there is
+      if (l_round >= p.rounds) return;
+      if (l_at >= l_end) {
+        if (++l_pass >= p.passes) {
+          l_pass = 0;
+          if (++l_round >= p.rounds) return;
         }
-        if constexpr (ZEROS) {
-          if constexpr (GPC == 1) {
-            q.zr[u][0] = __ldg(reinterpret_cast<const uint16_t*>(l_zeros + u * ZR));
-          } else if constexpr (GPC == 2) {
-            q.zr[u][0] = __ldg(reinterpret_cast<const uint32_t*>(l_zeros + u * ZR));
-          } else {
-            const uint2 v = __ldg(reinterpret_cast<const uint2*>(l_zeros + u * ZR));
-            q.zr[u][0] = v.x; q.zr[u][1] = v.y;
-          }
-        }
+        l_at = stretch(l_round, wic);
+        l_end = stretch(l_round, wic + 1);
+        continue;
       }
+      int c0;
+      const int nc = chunks_of(l_pass, c0), n = p.sc == 1 ? l_at : (int)__umulhi(l_at, p.sc_inv), s = l_at - n * p.sc, e = min(l_end - n * p.sc, p.sc);
+      l_left = min(e, nc) - s;
+      l_at += e - s;
+      const int64_t chunk = (int64_t)tile_of(l_round * p.tpr + n) * p.kt + c0 + s;
+      l_codes = p.codes + chunk * 1024;
+      l_scales = p.scales + chunk * SC;
+      if (ZEROS) l_zeros = p.zeros + chunk * ZR;
     }
-    l_s += U;
-    l_codes += U * 1024;
-    l_scales += U * SC;
-    if (ZEROS) l_zeros += U * ZR;
-    if (l_s >= l_nc && ++l_i < l_end) set_tile();
-  };
-  auto begin = [&](int round, int pass) {
-    l_nc = chunks_of(pass, l_c0);
-    l_i = round * p.tpr;
-    l_end = l_nc > 0 ? min(mine, l_i + p.tpr) : 0;
-    if (l_i < l_end) set_tile();
-    load_next(b0);
-    load_next(b1);
+    const int cnt = min(SLOT, l_left);
+    if (lane == 0) {
+      const uint32_t dst = ring + l_slot * SLOT_BYTES, b = bar + l_slot * 8;
+      asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(cnt * (1024 + SC + (ZEROS ? ZR : 0))) : "memory");
+      bulk_load(dst, l_codes, cnt * 1024, b);
+      bulk_load(dst + SLOT * 1024, l_scales, cnt * SC, b);
+      if (ZEROS) bulk_load(dst + SLOT * (1024 + SC), l_zeros, cnt * ZR, b);
+    }
+    l_slot = l_slot == RING - 1 ? 0 : l_slot + 1;
+    l_left -= cnt;
+    l_codes += SLOT * 1024;
+    l_scales += SLOT * SC;
+    if (ZEROS) l_zeros += SLOT * ZR;
   };
   // the first weights go out before the wait on the preceding kernel: no kernel of the library writes them
-  begin(0, 0);
+#pragma unroll 1
+  for (int i = 0; i < RING; ++i) issue();
   if (tid < 64) reinterpret_cast<uint32_t*>(s_zero)[tid] = 0;
   chain_wait();
 
-  uint32_t xp[NT], xstep[NT];
+  const uint8_t* xp[NT];
+  int xstep[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const bool has = n * 8 + g < rows;
-    xp[n] = smem_u32(has ? s_x + (n * 8 + g) * xs : s_zero) + t * 16;
+    xp[n] = (has ? s_x + (n * 8 + g) * xs : s_zero) + t * 16;
     xstep[n] = has ? 256 : 0;
   }
-  bool pending = false;                             // peers may still be reading this CTA's sums
+  int slot = 0;
+  uint32_t phase = 0;
+  bool ok = true, pending = false;                  // pending: peers may still be reading this CTA's sums
   auto settle = [&] {
     if (pending) cluster_wait();
     pending = false;
@@ -188,77 +189,106 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
         // ---- activations of the CTA's chunks to f16, a half-warp per row and chunk, with the sums of its groups
         if (p.passes > 1) __syncthreads();
         const int h = lane & 15;
-#pragma unroll 2
-        for (int item = wic * 2 + (lane >> 4); (item & ~1) < rows * nc; item += WARPS * 2) {
-          const int r = item / nc, c = item - r * nc, k = (c0 + c) * 128 + h * 8;
-          const bool in = r < rows;
-          const uint4 v = in && k < p.K ? *reinterpret_cast<const uint4*>(p.x + (row0 + r) * p.ldx + k) : make_uint4(0, 0, 0, 0);
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-          uint32_t m = 0;
-          float x[8], sum = 0.f;
+        int r = 0, c = wic * 2 + (lane >> 4);       // of the item; r * nc + c runs in steps of two per warp
+        auto wrap = [&] {
+          while (c >= nc && r < rows) {
+            c -= nc;
+            ++r;
+          }
+        };
+        wrap();
+        for (int left = rows * nc - wic * 2; left > 0; left -= 4 * (WARPS * 2)) {
+          uint4 v[4];                               // four items' loads are in flight
+          int ri[4], ci[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const uint32_t lo = w[i] & 0x7fffu, hi = (w[i] >> 16) & 0x7fffu;
-            m = max(m, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));      // infinities and NaN stay what they are
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-            sum += x[2 * i] + x[2 * i + 1];
+            ri[i] = r;
+            ci[i] = c;
+            const int k = (c0 + c) * 128 + h * 8;
+            v[i] = r < rows && k < p.K ? *reinterpret_cast<const uint4*>(p.x + (row0 + r) * p.ldx + k) : make_uint4(0, 0, 0, 0);
+            c += WARPS * 2;
+            wrap();
           }
 #pragma unroll
-          for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+          for (int i = 0; i < 4; ++i) {
+            if (left <= i * (WARPS * 2)) break;     // the same for the warp
+            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+            uint32_t m = 0;
+            float x[8], sum = 0.f;
 #pragma unroll
-          for (int o = 1; o < GRP / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-          // a power of two that brings the largest to 2^14 .. 2^15, as far as fp32 has it
-          const int sh = m == 0 ? 0 : min(14 + 127 - (int)(m >> 7), 126);
-          const float f = __uint_as_float((uint32_t)(127 + sh) << 23), f16th = f * 0.0625f;
-          if (in) {
-            *reinterpret_cast<uint4*>(s_x + r * xs + c * 256 + h * 16) =
-                make_uint4(pack_f16(x[0] * f, x[1] * f), pack_f16(x[2] * f16th, x[3] * f16th), pack_f16(x[4] * f, x[5] * f),
-                           pack_f16(x[6] * f16th, x[7] * f16th));
-            float* to = s_sum + c * (1 + GPC) * COLS + r;
-            if (h == 0) to[0] = __uint_as_float((uint32_t)(127 - sh) << 23);
-            if (h % (GRP / 8) == 0) to[(1 + h / (GRP / 8)) * COLS] = sum * ((ZEROS ? 1.f : 8.f) * 0x1p-24f);
+            for (int j = 0; j < 4; ++j) {
+              m = max(m, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
+              x[2 * j] = __uint_as_float(w[j] << 16);
+              x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+              sum += x[2 * j] + x[2 * j + 1];
+            }
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll
+            for (int o = 1; o < GRP / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            // a power of two that brings the largest to 2^14 .. 2^15, as far as fp32 has it (an infinity or NaN stays what it
+            // is, beside values that no longer matter)
+            const int sh = m == 0 ? 0 : min(14 + 127 - (int)(m >> 7), 126);
+            const float f = __uint_as_float((uint32_t)(127 + sh) << 23), f16th = f * 0.0625f;
+            if (ri[i] < rows) {
+              *reinterpret_cast<uint4*>(s_x + ri[i] * xs + ci[i] * 256 + h * 16) =
+                  make_uint4(pack_f16(x[0] * f, x[1] * f), pack_f16(x[2] * f16th, x[3] * f16th), pack_f16(x[4] * f, x[5] * f),
+                             pack_f16(x[6] * f16th, x[7] * f16th));
+              float* to = s_sum + ci[i] * (1 + GPC) * COLS + ri[i];
+              if (h == 0) to[0] = __uint_as_float((uint32_t)(127 - sh) << 23);
+              if (h % (GRP / 8) == 0) to[(1 + h / (GRP / 8)) * COLS] = sum * ((ZEROS ? 1.f : 8.f) * 0x1p-24f);
+            }
           }
         }
         __syncthreads();
       }
       // ---- products
-      const int tiles = nc > 0 ? max(0, min(mine - round * p.tpr, p.tpr)) : 0, ppt = (nc + U - 1) / U;
-      float4* acc = reinterpret_cast<float4*>(s_acc) + wic * (NT * 32) + lane;
-      float tot[NT][4];
-      uint32_t x_at[NT], sum_at = 0;
-      int s = 0;
-      auto reset = [&] {
-        s = 0;
-        sum_at = smem_u32(s_sum) + t * 8;
+      const int end = stretch(round, wic + 1);
+      for (int at = stretch(round, wic); at < end && ok;) {
+        const int n_tile = p.sc == 1 ? at : (int)__umulhi(at, p.sc_inv), s0 = at - n_tile * p.sc, s1 = min(end - n_tile * p.sc, p.sc), se = min(s1, nc);
+        at += s1 - s0;
+        float tot[NT][4];
+        const uint8_t* x_at[NT];
+        const float* sum_at = s_sum + t * 2 + s0 * ((1 + GPC) * COLS);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-          x_at[n] = xp[n];
+          x_at[n] = xp[n] + s0 * xstep[n];
           tot[n][0] = tot[n][1] = tot[n][2] = tot[n][3] = 0.f;
         }
-      };
-      auto store = [&] {
-        settle();
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          float4 v = make_float4(tot[n][0], tot[n][1], tot[n][2], tot[n][3]);
-          if (pass > 0) {
-            const float4 o = acc[n * 32];
-            v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+        for (int s = s0; s < se; s += SLOT) {
+          if (!mbar_try_wait(s_bar + wic * RING + slot, phase) && !mbar_wait(s_bar + wic * RING + slot, phase)) {
+            ok = false;
+            break;
           }
-          acc[n * 32] = v;
-        }
-        acc += WARPS * (NT * 32);
-      };
-      reset();
-      auto step = [&](Batch& q) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (s + u < nc) {
-            const uint4 lo = q.lo[u], hi = q.hi[u];
+          const uint8_t* base = s_ring + slot * SLOT_BYTES;
+          const uint8_t* cb = base + lane * 16;
+          const uint8_t* sb = base + SLOT * 1024 + g * (4 * GPC);
+          const uint8_t* zb = base + SLOT * (1024 + SC) + g * (2 * GPC);
+          auto chunk = [&](const int c) {
+            const uint4 lo = *reinterpret_cast<const uint4*>(cb), hi = *reinterpret_cast<const uint4*>(cb + 512);
+            uint32_t sw[GPC], zw[2] = {0, 0};
+            if constexpr (GPC == 1) {
+              sw[0] = *reinterpret_cast<const uint32_t*>(sb);
+            } else if constexpr (GPC == 2) {
+              const uint2 v = *reinterpret_cast<const uint2*>(sb);
+              sw[0] = v.x; sw[1] = v.y;
+            } else {
+              const uint4 v = *reinterpret_cast<const uint4*>(sb);
+              sw[0] = v.x; sw[1] = v.y; sw[2] = v.z; sw[3] = v.w;
+            }
+            if constexpr (ZEROS) {
+              if constexpr (GPC == 1) {
+                zw[0] = *reinterpret_cast<const uint16_t*>(zb);
+              } else if constexpr (GPC == 2) {
+                zw[0] = *reinterpret_cast<const uint32_t*>(zb);
+              } else {
+                const uint2 v = *reinterpret_cast<const uint2*>(zb);
+                zw[0] = v.x; zw[1] = v.y;
+              }
+            }
             float2 fx[NT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) fx[n] = lds_f2(sum_at + u * ((1 + GPC) * COLS * 4) + n * 32);
+            for (int n = 0; n < NT; ++n) fx[n] = *reinterpret_cast<const float2*>(sum_at + n * 8);
             constexpr int JPG = 4 / GPC;            // words of a group
 #pragma unroll
             for (int grp = 0; grp < GPC; ++grp) {
@@ -271,25 +301,25 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
                 const uint32_t ul = wl >> 8, uh = wh >> 8;
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
-                  const uint4 xv = lds128(x_at[n] + j * 64);
+                  const uint4 xv = *reinterpret_cast<const uint4*>(x_at[n] + j * 64);
                   mma_f16(d[n], jj == 0, wl & 0x000f000fu, wh & 0x000f000fu, wl & 0x00f000f0u, wh & 0x00f000f0u, xv.x, xv.y);
                   mma_f16(d[n], false, ul & 0x000f000fu, uh & 0x000f000fu, ul & 0x00f000f0u, uh & 0x00f000f0u, xv.z, xv.w);
                 }
               }
               // scales lie as [row half][group], halves of words; zeros as bytes. What lies behind K is never used.
-              const uint32_t w0 = q.sc[u][grp / 2], w1 = q.sc[u][(GPC + grp) / 2];
+              const uint32_t w0 = sw[grp / 2], w1 = sw[(GPC + grp) / 2];
               float f0 = __uint_as_float(grp & 1 ? w0 & 0xffff0000u : w0 << 16);
               float f1 = __uint_as_float((GPC + grp) & 1 ? w1 & 0xffff0000u : w1 << 16);
-              if (GPC > 1 && grp > 0 && (c0 + s + u) * 128 + grp * GRP >= p.K) f0 = f1 = 0.f;
+              if (GPC > 1 && grp > 0 && (c0 + c) * 128 + grp * GRP >= p.K) f0 = f1 = 0.f;
               float z0 = 1.f, z1 = 1.f;
               if constexpr (ZEROS) {                // 2^23 + zero, minus 2^23
-                const uint32_t y0 = q.zr[u][0] >> (8 * grp), y1 = GPC == 4 ? q.zr[u][GPC == 4 ? 1 : 0] >> (8 * grp) : q.zr[u][0] >> (8 * (GPC + grp));
+                const uint32_t y0 = zw[0] >> (8 * grp), y1 = GPC == 4 ? zw[1] >> (8 * grp) : zw[0] >> (8 * (GPC + grp));
                 z0 = __uint_as_float((y0 & 15u) | 0x4b000000u) - 8388608.f;
                 z1 = __uint_as_float((y1 & 15u) | 0x4b000000u) - 8388608.f;
               }
 #pragma unroll
               for (int n = 0; n < NT; ++n) {
-                const float2 sx = lds_f2(sum_at + (u * (1 + GPC) + 1 + grp) * (COLS * 4) + n * 32);
+                const float2 sx = *reinterpret_cast<const float2*>(sum_at + (1 + grp) * COLS + n * 8);
                 tot[n][0] = fmaf(fmaf(d[n][0], fx[n].x, -z0 * sx.x), f0, tot[n][0]);
                 tot[n][1] = fmaf(fmaf(d[n][1], fx[n].y, -z0 * sx.y), f0, tot[n][1]);
                 tot[n][2] = fmaf(fmaf(d[n][2], fx[n].x, -z1 * sx.x), f1, tot[n][2]);
@@ -298,26 +328,32 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) x_at[n] += xstep[n];
+          };
+          const int cnt = min(SLOT, se - s);
+#pragma unroll 1
+          for (int q = 0; q < cnt; ++q) {
+            chunk(s + q);
+            cb += 1024;
+            sb += SC;
+            zb += ZR;
+            sum_at += (1 + GPC) * COLS;
           }
+          __syncwarp();
+          issue();                                  // into the slot that is free now
+          slot = slot == RING - 1 ? 0 : slot + 1;
+          phase ^= slot == 0 ? 1u : 0u;
         }
-        load_next(q);
-        s += U;
-        sum_at += U * ((1 + GPC) * COLS * 4);
-        if (s >= nc) {
-          store();
-          reset();
-        }
-      };
-      const int pieces = tiles * ppt;
-      for (int f = 0; f < pieces; f += 2) {
-        step(b0);
-        if (f + 1 < pieces) step(b1);
+        settle();
+        // sum i of n-tile n: row g + 8 (i / 2) of the tile, activation row 2 t + i % 2
+        float* acc = s_acc + (n_tile + wic) * (p.rows * 16) + 2 * t * 16 + g;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float* dst = acc + (n * 8 + (r & 1)) * 16 + 8 * (r >> 1);
+            if (n * 8 + 2 * t + (r & 1) < rows) *dst = pass == 0 ? tot[n][r] : *dst + tot[n][r];
+          }
       }
-      if (nc == 0 && pass == 0) {                   // more CTAs than chunks: sums of nothing
-        for (int i = round * p.tpr; i < min(mine, (round + 1) * p.tpr); ++i) store();
-      }
-      if (pass + 1 < p.passes) begin(round, pass + 1);
-      else if (round + 1 < p.rounds) begin(round + 1, 0);
     }
     // ---- exchange: every rank finishes its share of the tiles
     settle();
@@ -327,34 +363,45 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
     } else {
       __syncthreads();
     }
-    const int each = gated ? 2 : 1;
-    for (int e = tid + WARPS * 32 * rank; e < p.tpr * WARPS / each * (COLS * 16); e += WARPS * 32 * p.cs) {
-      const int row = e & 15, b = (e >> 4) % COLS, sl = (e >> 4) / COLS * each;
-      const int u = cluster * WARPS + (sl % WARPS) + (round * p.tpr + sl / WARPS) * warps;
-      if (u >= p.tiles || b >= rows) continue;
-      auto sum_of = [&](int sl_) {
-        // row g + 8 i of the tile and activation row 2 t + j: value 2 i + j of lane 4 g + t
-        const uint32_t a = smem_u32(s_acc + ((sl_ * NT + (b >> 3)) * 32 + (row & 7) * 4 + ((b & 7) >> 1)) * 4 + (row >> 3) * 2 + (b & 1));
-        float v = 0.f;
-        for (int r = 0; r < p.cs; ++r) {
-          float w;
-          asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(mapa_u32(a, r)));
-          v += w;
+    const int tiles = max(0, min(p.tpr, dealt - round * p.tpr)), per = p.rows * 16, all = tiles / each * per;
+    for (int e = rank * (WARPS * 32) + tid; e < all; e += p.cs * (WARPS * 32)) {
+      const int n = __umulhi(e, p.per_inv) * each, at = e - n / each * per, tile = tile_of(round * p.tpr + n);
+      if (at >= rows * 16) continue;
+      auto sum_of = [&](int m) {
+        // the parts of tile m, in the order of the warps; the same places in all ranks
+        float v = 0.f, w[WARPS];
+        const float* part = s_acc + m * (p.rows * 16) + at;
+        auto parts = [&](auto&& load) {
+#pragma unroll
+          for (int i = 0; i < WARPS; ++i) {
+            const int lo = max(stretch(round, i), m * p.sc), hi = min(stretch(round, i + 1), (m + 1) * p.sc);
+            w[i] = 0.f;
+            if (lo < hi) w[i] = load(part + i * (p.rows * 16));
+          }
+#pragma unroll
+          for (int i = 0; i < WARPS; ++i) v += w[i];
+        };
+        if (p.cs == 1) {
+          parts([](const float* a) { return *a; });
+        } else {
+          for (int r = 0; r < p.cs; ++r)
+            parts([&](const float* a) {
+              float x;
+              asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(mapa_u32(smem_u32(a), r)));
+              return x;
+            });
         }
         return v * 0x1p24f;
       };
+      const int b = row0 + (at >> 4), row = at & 15;
+      const float v = sum_of(n);
       if (gated) {
-        const float gate = sum_of(sl), up = sum_of(sl + 1);
-        const int o = (u >> 4) * 128 + ((u >> 1) & 7) * 16 + row;
-        if (o < p.n_valid)
-          static_cast<bf16*>(p.out)[(int64_t)(row0 + b) * p.ldo + o] = __float2bfloat16_rn(act_of(gate, p.act) * up);
-      } else {
-        const int o = u * 16 + row;
-        if (o < p.N) {
-          float* dst = static_cast<float*>(p.out) + (int64_t)(row0 + b) * p.ldo + o;
-          const float v = sum_of(sl);
-          *dst = p.mode == 0 ? v : *dst + v;
-        }
+        const float up = sum_of(n + 1);
+        const int o = (tile >> 4) * 128 + (tile & 7) * 16 + row;
+        if (o < p.n_valid) static_cast<bf16*>(p.out)[(int64_t)b * p.ldo + o] = __float2bfloat16_rn(act_of(v, p.act) * up);
+      } else if (tile * 16 + row < p.N) {
+        float* dst = static_cast<float*>(p.out) + (int64_t)b * p.ldo + tile * 16 + row;
+        *dst = p.mode == 0 ? v : *dst + v;
       }
     }
     if (p.cs > 1) cluster_arrive();                 // this CTA has read its peers' sums
@@ -362,6 +409,10 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
     pending = p.cs > 1;
   }
   settle();
+  if (!ok) {
+    if (lane == 0) atomicMin(p.status, (int)POP_E_DEVICE_TIMEOUT);
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // let in-flight bulk copies land
+  }
 }
 
 // Clusters of cs CTAs that the GPU holds at once (of the device that was current at the first call)
@@ -401,33 +452,44 @@ int launch_t(Gemv4Dev& p, cudaStream_t s) {
   }
   constexpr int COLS = NT * 8;
   // shared memory: activations with their sums, and sums of products
-  constexpr int ROOM = SMEM_LIMIT - 256 - COLS * 64;
-  constexpr int TPR_BYTES = WARPS * COLS * 64, SC_BYTES = COLS * (256 + 4 + 4 * (128 / GRP));
-  static_assert(ROOM >= TPR_BYTES + 4 * SC_BYTES, "shared memory budget");
-  // Warps take tiles in turn: the cluster size whose busiest warp has the fewest chunks. A tile's beginning and end cost
-  // about one chunk, the exchange within a cluster two.
+  constexpr int GPC = 128 / GRP, RING_BYTES = WARPS * RING * SLOT * (1024 + 32 * GPC + (ZEROS ? 16 * GPC : 0));
+  constexpr int FIXED = RING_BYTES + 256 + WARPS * RING * 8 + COLS * 64;
+  static_assert(SMEM_LIMIT - FIXED >= (WARPS + 2) * COLS * 64 + 4 * COLS * (256 + 4 + 4 * GPC), "shared memory budget");
+  p.rows = p.B < COLS ? p.B : COLS;
+  const int room = SMEM_LIMIT - FIXED, acc_bytes = p.rows * 64, sc_bytes = p.rows * 256 + COLS * (4 + 4 * GPC);
+  // Work of an SM with two CTAs, in clocks as measured: 30 to convert a row's chunk, 47 (two n-tiles: 75) for a tile's chunk, the
+  // exchange within a cluster. us in clusters of 1 / 2 / 8: 1 x 4096 -> 28672 gated 14.8 / 16.0 / 21.2, 1 x 14336 -> 4096 11.4 /
+  // 11.4 / 15.0, 12 x 14336 -> 4096 62 / 38 / 24, 16 x 4096 -> 6144 22 / 26 / 14.
+  const int each = p.mode == 3 ? 2 : 1;
   int64_t best = INT64_MAX;
   for (int cs = 1; cs <= 8 && cs <= p.kt; cs *= 2) {
-    const int most = max_clusters<GRP, NT, ZEROS>(cs);
-    const int64_t warps = (int64_t)most * WARPS, per = (p.tiles + warps - 1) / warps;
-    const int64_t cost = per * ((p.kt + cs - 1) / cs + 1) + (cs > 1 ? 2 : 0) + (p.kt + cs - 1) / cs;
+    const int most = max_clusters<GRP, NT, ZEROS>(cs), want = p.tiles / each, clusters = want < most ? want : most;
+    const int64_t nc = ceil_div(p.kt, cs);
+    const int64_t cost = 2 * nc * (p.rows * 30 + (int64_t)p.tiles * (NT == 1 ? 47 : 75) / clusters) + (cs > 1 ? 4000 + 1000 * cs : 0);
     if (cost < best) {
       best = cost;
       p.cs = cs;
-      const int want = ceil_div(p.tiles, WARPS);
-      p.clusters = want < most ? want : most;
+      p.clusters = clusters;
     }
   }
-  // all chunks of a CTA at once if they fit beside the sums of one tile per warp, then as many tiles as fit
-  const int n_i = ceil_div(p.tiles, p.clusters * WARPS), all = ceil_div(p.kt, p.cs), most_sc = (ROOM - TPR_BYTES) / SC_BYTES;
+  // all chunks of a CTA at once if they fit beside the sums of two tiles, then as many tiles as fit
+  const int dealt = ceil_div(p.tiles / each, p.clusters) * each, all = ceil_div(p.kt, p.cs);
+  const int most_sc = (room - (WARPS + 2) * acc_bytes) / sc_bytes;
   p.passes = ceil_div(all, most_sc);
   p.sc = ceil_div(p.kt, p.passes * p.cs);
-  const int most_tpr = (ROOM - p.sc * SC_BYTES) / TPR_BYTES;
-  p.rounds = ceil_div(n_i, most_tpr);
-  p.tpr = ceil_div(n_i, p.rounds);
+  const int most_tpr = ((room - p.sc * sc_bytes) / acc_bytes - WARPS) / 2 * 2;
+  p.rounds = ceil_div(dealt, most_tpr);
+  p.tpr = ceil_div(dealt / each, p.rounds) * each;
+  p.grain = p.sc % SLOT == 0 ? SLOT : 1;
+  p.deal = p.tiles / each / p.clusters;
+  p.deal_rest = p.tiles / each % p.clusters;
+  p.sc_inv = (uint32_t)(((1ull << 32) + p.sc - 1) / p.sc);
+  p.per_inv = (uint32_t)(((1ull << 32) + p.rows * 16 - 1) / (p.rows * 16));
   const int slabs = ceil_div(p.B, COLS);
   if (slabs > 65535) return POP_E_INVALID;
-  const size_t smem = 256 + (size_t)p.sc * SC_BYTES + COLS * 64 + (size_t)p.tpr * TPR_BYTES;
+  const size_t smem = FIXED + (size_t)p.sc * sc_bytes + (size_t)(p.tpr + WARPS) * acc_bytes;
+  p.status = status_word();
+  if (!p.status) return POP_E_CUDA;
   ProfScope prof(PROF_GEMV, (double)p.N * p.K * (0.5 + (p.zeros ? 3.0 : 2.0) / GRP) * slabs, s);
   if (launch_chained_cluster_x(gemv4_kernel<GRP, NT, ZEROS>, dim3(p.clusters * p.cs, slabs), dim3(WARPS * 32), smem, s,
                                (unsigned)p.cs, p) != cudaSuccess)
