@@ -297,8 +297,11 @@ int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int
  * most 2^-36 of it); sums are fp32, in an order that depends on the sizes alone. An activation row with an infinite or NaN
  * input gives a row of NaN. */
 int pop_k_gemv_w4(const void* x, int64_t ldx, const void* codes, const void* scales, const void* zeros, int32_t group,
-                  void* out, int64_t ldo, int32_t B, int32_t N, int32_t K, int32_t mode, int32_t act, int32_t n_valid,
-                  void* stream);
+                  void* workspace, size_t workspace_bytes, void* out, int64_t ldo, int32_t B, int32_t N, int32_t K,
+                  int32_t mode, int32_t act, int32_t n_valid, void* stream);
+/* Bytes of device workspace (16-byte aligned, contents irrelevant before and after; one for each of calls that may overlap)
+ * that the call needs for its activations; 0 for one or two rows, where workspace may be NULL. A smaller one is POP_E_NOSPACE. */
+size_t pop_k_gemv_w4_workspace_bytes(int32_t B, int32_t K, int32_t group);
 
 /* pop_k_rope_cache for drafted rows. in: projections [q heads | k heads | v heads] * hd of `rows` packed rows, fp32 or
  * (in_bf16) bf16, row stride ld_in (a multiple of 4; 16-byte aligned). Sequence b owns rows cu_rows[b] .. cu_rows[b + 1] - 1

@@ -114,7 +114,8 @@ SIGNATURES = {
                                        _P, _I64] + [_I32] * 5 + [_P]),
     "pop_k_profile": (None, [_I32]),
     "pop_k_profile_summary": (C.c_int, [_I32, C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(_I64)]),
-    "pop_k_gemv_w4": (C.c_int, [_P, _I64, _P, _P, _P, _I32, _P, _I64] + [_I32] * 6 + [_P]),
+    "pop_k_gemv_w4": (C.c_int, [_P, _I64, _P, _P, _P, _I32, _P, C.c_size_t, _P, _I64] + [_I32] * 6 + [_P]),
+    "pop_k_gemv_w4_workspace_bytes": (C.c_size_t, [_I32, _I32, _I32]),
     "pop_k_rope_cache_tree": (C.c_int, [_P, _I32, _I64, _I32, _P, _I32, _P, _I32, _P, _I32, _P, _I64, _P, _P, _P, _I32, _I32,
                                         _I32, _P, _P, _F, _P] + [_I32] * 4 + [_P]),
     "pop_k_tree_attention": (C.c_int, [_P, _I64, _I32, _P, _I32, _P, _I32, _P, _I32, _P, _P, _P, _P, _I32, _I32, _I32, _P,
@@ -500,6 +501,13 @@ class PopLibrary:
         return q_out
 
     @staticmethod
+    def _scratch(nbytes, device, stream):
+        """A call's own workspace, from the pool of the stream that runs the call: its memory has no work of another stream in
+        front of it, and goes back, when the call returns, to that stream's later work."""
+        with torch.cuda.stream(stream):
+            return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+    @staticmethod
     def _attn8_rows(q, out, width, workspace, stream, workspace_bytes=POP_E4M3_WORKSPACE_BYTES):
         """Checks queries and outputs; returns (rows, strides of both, workspace, its bytes)."""
         rows, w = q.shape
@@ -509,10 +517,7 @@ class PopLibrary:
                 q_inner != 1 or o_inner != 1:
             raise PopError(POP_E_INVALID, "q and out are bf16 [rows, n_q hd]")
         if workspace is None:
-            # from the pool of the stream that runs the call: its memory has no work of another stream in front of it, and
-            # goes back, when the call returns, to that stream's later work
-            with torch.cuda.stream(stream):
-                workspace = torch.empty(workspace_bytes, dtype=torch.uint8, device=q.device)
+            workspace = PopLibrary._scratch(workspace_bytes, q.device, stream)
         elif not workspace.is_contiguous():
             raise PopError(POP_E_INVALID, "workspace has to be contiguous")
         return rows, ldq, ldo, workspace, workspace.numel() * workspace.element_size()
@@ -565,11 +570,11 @@ class PopLibrary:
                 raise PopError(POP_E_INVALID, f"{what}: all tensors have to be on the current CUDA device")
         return torch._C._cuda_getCurrentRawStream(at)
 
-    def gemv_w4(self, x, codes, scales, zeros, out, n, group, mode=0, act=0, n_valid=None, stream=None):
+    def gemv_w4(self, x, codes, scales, zeros, out, n, group, mode=0, act=0, n_valid=None, workspace=None, stream=None):
         """pop_k_gemv_w4: x bf16 [B, K]; codes uint8 [ceil(n / 16), ceil(K / 128), 16, 64], scales bf16 and zeros uint8 (or
         None) [.., .., 16, 128 / group] as `pack_w4` lays them out; out fp32 [B, n], or bf16 [B, n_valid] (n / 2 if not given)
-        for mode 3."""
-        here = self._here(x, (codes, scales, zeros, out), "gemv_w4")
+        for mode 3. `workspace` (pop_k_gemv_w4_workspace_bytes of any dtype) is allocated if it is needed and not given."""
+        here = self._here(x, (codes, scales, zeros, out, workspace), "gemv_w4")
         B, K = x.shape
         ldx, inner = x.stride()
         shape = (-(-n // 16), -(-K // 128), 16, 128 // group if group else 0)
@@ -585,9 +590,13 @@ class PopLibrary:
             raise PopError(POP_E_INVALID, "gemv_w4: out is fp32 [B, n], or bf16 [B, n_valid] for the gated form")
         if B == 0:
             return out
+        need = self.dll.pop_k_gemv_w4_workspace_bytes(B, K, group) if B > 2 else 0
+        if need and workspace is None:
+            workspace = self._scratch(need, x.device, stream)
         code = self.dll.pop_k_gemv_w4(
             x.data_ptr(), ldx, codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), group,
-            out.data_ptr(), ldo, B, n, K, mode, act, width, here if stream is None else stream.cuda_stream)
+            None if workspace is None else workspace.data_ptr(),
+            0 if workspace is None else workspace.numel() * workspace.element_size(), out.data_ptr(), ldo, B, n, K, mode, act, width, here if stream is None else stream.cuda_stream)
         if code:
             self.check(code, "pop_k_gemv_w4")
         return out

@@ -278,10 +278,13 @@ int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int
   return launch_attention8(a, static_cast<cudaStream_t>(stream));
 }
 
+size_t pop_k_gemv_w4_workspace_bytes(int32_t B, int32_t K, int32_t group) { return gemv4_workspace_bytes(B, K, group); }
+
 int pop_k_gemv_w4(const void* x, int64_t ldx, const void* codes, const void* scales, const void* zeros, int32_t group,
-                  void* out, int64_t ldo, int32_t B, int32_t N, int32_t K, int32_t mode, int32_t act, int32_t n_valid,
-                  void* stream) {
+                  void* workspace, size_t workspace_bytes, void* out, int64_t ldo, int32_t B, int32_t N, int32_t K,
+                  int32_t mode, int32_t act, int32_t n_valid, void* stream) {
   Gemv4Args a{};
+  a.workspace = workspace; a.workspace_bytes = workspace ? workspace_bytes : 0;
   a.x = static_cast<const bf16*>(x); a.ldx = ldx;
   a.codes = static_cast<const uint8_t*>(codes); a.scales = static_cast<const bf16*>(scales);
   a.zeros = static_cast<const uint8_t*>(zeros); a.group = group;

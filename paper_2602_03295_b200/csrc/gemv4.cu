@@ -14,12 +14,15 @@ namespace {
 
 constexpr int WARPS = 8;        // of a CTA. Two CTAs per SM, so that one's beginning and end (and the next launch's) lie beside
                                 // the other's work
-constexpr int SLOT = 4;         // chunks of 128 inputs in a slot of a warp's ring
-constexpr int RING = 2;
+constexpr int RING = 2;         // slots of a warp's ring
 constexpr int SMEM_LIMIT = 112 * 1024;
+
+// Chunks of 128 inputs in a slot. Several n-tiles leave less shared memory, and more work behind each chunk
+__host__ __device__ constexpr int slot_chunks(int nt) { return nt == 1 ? 4 : 2; }
 
 struct Gemv4Dev {
   const bf16* x; int64_t ldx;
+  const uint8_t* xq;            // activations converted by gemv4_convert_kernel, or null: each CTA converts what it needs
   const uint8_t* codes; const uint8_t* scales; const uint8_t* zeros;
   void* out; int64_t ldo;
   int B, N, K, mode, act, n_valid;
@@ -64,6 +67,56 @@ __device__ __forceinline__ float act_of(float g, int act) {
   return 0.5f * g * (1.0f + tanhf(0.7978845608028654f * (g + 0.044715f * g * g * g)));
 }
 
+// What a lane of a half-warp makes of its 8 of a chunk's 128 activations: f16 values times a common power of two, those that
+// meet codes of bits 4 .. 7 divided by 16; `unit` takes them back, `sum` is that of the lane's group.
+template <int GRP>
+__device__ __forceinline__ uint4 convert8(const uint4& v, float& sum, float& unit) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t m = 0;
+  float x[8];
+  sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    m = max(m, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
+    x[2 * j] = __uint_as_float(w[j] << 16);
+    x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    sum += x[2 * j] + x[2 * j + 1];
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll
+  for (int o = 1; o < GRP / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  // a power of two that brings the largest to 2^14 .. 2^15, as far as fp32 has it (an infinity or NaN stays what it is, beside
+  // values that no longer matter)
+  const int sh = m == 0 ? 0 : min(14 + 127 - (int)(m >> 7), 126);
+  const float f = __uint_as_float((uint32_t)(127 + sh) << 23), f16th = f * 0.0625f;
+  unit = __uint_as_float((uint32_t)(127 - sh) << 23);
+  return make_uint4(pack_f16(x[0] * f, x[1] * f), pack_f16(x[2] * f16th, x[3] * f16th), pack_f16(x[4] * f, x[5] * f),
+                    pack_f16(x[6] * f16th, x[7] * f16th));
+}
+// Sums of groups in the unit of code products (2^-24), without zeros times the 8 that stands for them
+__host__ __device__ constexpr float sum_scale(bool zeros) { return (zeros ? 1.f : 8.f) * 0x1p-24f; }
+
+// Converted activations for many CTAs: per slab of COLS rows [COLS][kt][128] f16, then [kt][1 + GPC][COLS] units and sums. A
+// half-warp per row and chunk; bound by launch and one round through memory.
+__host__ __device__ constexpr int64_t slab_bytes(int cols, int gpc, int64_t kt) { return kt * cols * (256 + 4 * (1 + gpc)); }
+template <int GRP>
+__global__ void __launch_bounds__(256) gemv4_convert_kernel(const bf16* __restrict__ x, int64_t ldx, uint8_t* __restrict__ out,
+                                                            int B, int K, int kt, int cols, int zeros) {
+  constexpr int GPC = 128 / GRP;
+  chain_trigger();
+  chain_wait();
+  const int h = threadIdx.x & 15, c = blockIdx.x * 16 + (threadIdx.x >> 4), r = blockIdx.y, k = c * 128 + h * 8;
+  float sum, unit;
+  const uint4 q = convert8<GRP>(c < kt && k < K ? *reinterpret_cast<const uint4*>(x + r * ldx + k) : make_uint4(0, 0, 0, 0), sum, unit);
+  if (c >= kt) return;
+  uint8_t* slab = out + r / cols * slab_bytes(cols, GPC, kt);
+  *reinterpret_cast<uint4*>(slab + ((int64_t)(r % cols) * kt + c) * 256 + h * 16) = q;
+  float* to = reinterpret_cast<float*>(slab + (int64_t)cols * kt * 256) + (int64_t)c * (1 + GPC) * cols + r % cols;
+  if (h == 0) to[0] = unit;
+  if (h % (GRP / 8) == 0) to[(1 + h / (GRP / 8)) * cols] = sum * sum_scale(zeros != 0);
+}
+
 // A code in the low bits of an f16 is code * 2^-24, in bits 4 .. 7 code * 2^-20: subnormals are linear, so that a mask alone
 // makes a tensor-core operand of two codes of a word, and one shift the other half of them. The activations go in as f16 too,
 // those of a chunk of 128 inputs times a power of two that brings their largest near 2^15 (bf16 values stay exact down to
@@ -82,7 +135,7 @@ __device__ __forceinline__ float act_of(float g, int act) {
 // until the activations are converted, 0.8 for exchange and stores.
 template <int GRP, int NT, bool ZEROS>
 __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_constant__ Gemv4Dev p) {
-  constexpr int GPC = 128 / GRP, COLS = NT * 8, SC = 32 * GPC, ZR = 16 * GPC;
+  constexpr int GPC = 128 / GRP, COLS = NT * 8, SC = 32 * GPC, ZR = 16 * GPC, SLOT = slot_chunks(NT);
   constexpr int SLOT_BYTES = SLOT * (1024 + SC + (ZEROS ? ZR : 0));     // codes, then scales, then zeros
   extern __shared__ __align__(128) uint8_t smem[];
   const int xs = p.sc * 256 + 64;                   // bytes of an activation row: 64 off a multiple of 128, so that the
@@ -91,8 +144,8 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
   const int row0 = blockIdx.y * COLS, rows = min(p.B - row0, COLS);
   const uint8_t* s_ring = smem + wic * (RING * SLOT_BYTES);
   uint8_t* s_zero = smem + WARPS * RING * SLOT_BYTES;             // 256 zeros: what lanes without an activation row read
-  uint64_t* s_bar = reinterpret_cast<uint64_t*>(s_zero + 256);    // [WARPS][RING]
-  float* s_sum = reinterpret_cast<float*>(s_bar + WARPS * RING);  // [sc][1 + GPC][COLS]: 2^-shift; sums of the groups
+  uint64_t* s_bar = reinterpret_cast<uint64_t*>(s_zero + 256);    // [WARPS][RING], and one of the activations
+  float* s_sum = reinterpret_cast<float*>(s_bar + WARPS * RING + 2);  // [sc][1 + GPC][COLS]: 2^-shift; sums of the groups
   uint8_t* s_x = reinterpret_cast<uint8_t*>(s_sum + p.sc * (1 + GPC) * COLS);
   float* s_acc = reinterpret_cast<float*>(s_x + p.rows * xs);     // [tpr + WARPS][rows][16]
   const int rank = cluster_ctarank();
@@ -119,6 +172,7 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
   };
   const uint32_t ring = smem_u32(s_ring), bar = smem_u32(s_bar + wic * RING);
   if (lane < RING) mbar_init(s_bar + wic * RING + lane, 1);
+  if (tid == RING) mbar_init(s_bar + WARPS * RING, 1);
   fence_barrier_init();
   __syncwarp();
 
@@ -164,6 +218,7 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
 #pragma unroll 1
   for (int i = 0; i < RING; ++i) issue();
   if (tid < 64) reinterpret_cast<uint32_t*>(s_zero)[tid] = 0;
+  __syncthreads();
   chain_wait();
 
   const uint8_t* xp[NT];
@@ -175,7 +230,7 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
     xstep[n] = has ? 256 : 0;
   }
   int slot = 0;
-  uint32_t phase = 0;
+  uint32_t phase = 0, x_phase = 0;
   bool ok = true, pending = false;                  // pending: peers may still be reading this CTA's sums
   auto settle = [&] {
     if (pending) cluster_wait();
@@ -188,6 +243,22 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
       if (p.passes > 1 || round == 0) {
         // ---- activations of the CTA's chunks to f16, a half-warp per row and chunk, with the sums of its groups
         if (p.passes > 1) __syncthreads();
+        if (p.xq != nullptr) {
+          // converted already: a copy per row, one of the sums
+          if (wic == 0) {
+            const uint8_t* slab = p.xq + blockIdx.y * slab_bytes(COLS, GPC, p.kt);
+            const uint32_t b = smem_u32(s_bar + WARPS * RING), sums = max(nc, 0) * (1 + GPC) * COLS * 4;
+            if (lane == 0)
+              asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(rows * nc * 256 + sums) : "memory");
+            __syncwarp();
+            for (int r = lane; r < rows && nc > 0; r += 32)
+              bulk_load(smem_u32(s_x + r * xs), slab + ((int64_t)r * p.kt + c0) * 256, nc * 256, b);
+            if (lane == 0 && nc > 0)
+              bulk_load(smem_u32(s_sum), slab + (int64_t)COLS * p.kt * 256 + (int64_t)c0 * (1 + GPC) * COLS * 4, sums, b);
+          }
+          if (!mbar_wait(s_bar + WARPS * RING, x_phase)) ok = false;
+          x_phase ^= 1;
+        } else {
         const int h = lane & 15;
         int r = 0, c = wic * 2 + (lane >> 4);       // of the item; r * nc + c runs in steps of two per warp
         auto wrap = [&] {
@@ -212,35 +283,18 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             if (left <= i * (WARPS * 2)) break;     // the same for the warp
-            const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-            uint32_t m = 0;
-            float x[8], sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              m = max(m, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
-              x[2 * j] = __uint_as_float(w[j] << 16);
-              x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-              sum += x[2 * j] + x[2 * j + 1];
-            }
-#pragma unroll
-            for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-#pragma unroll
-            for (int o = 1; o < GRP / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            // a power of two that brings the largest to 2^14 .. 2^15, as far as fp32 has it (an infinity or NaN stays what it
-            // is, beside values that no longer matter)
-            const int sh = m == 0 ? 0 : min(14 + 127 - (int)(m >> 7), 126);
-            const float f = __uint_as_float((uint32_t)(127 + sh) << 23), f16th = f * 0.0625f;
+            float sum, unit;
+            const uint4 q = convert8<GRP>(v[i], sum, unit);
             if (ri[i] < rows) {
-              *reinterpret_cast<uint4*>(s_x + ri[i] * xs + ci[i] * 256 + h * 16) =
-                  make_uint4(pack_f16(x[0] * f, x[1] * f), pack_f16(x[2] * f16th, x[3] * f16th), pack_f16(x[4] * f, x[5] * f),
-                             pack_f16(x[6] * f16th, x[7] * f16th));
+              *reinterpret_cast<uint4*>(s_x + ri[i] * xs + ci[i] * 256 + h * 16) = q;
               float* to = s_sum + ci[i] * (1 + GPC) * COLS + ri[i];
-              if (h == 0) to[0] = __uint_as_float((uint32_t)(127 - sh) << 23);
-              if (h % (GRP / 8) == 0) to[(1 + h / (GRP / 8)) * COLS] = sum * ((ZEROS ? 1.f : 8.f) * 0x1p-24f);
+              if (h == 0) to[0] = unit;
+              if (h % (GRP / 8) == 0) to[(1 + h / (GRP / 8)) * COLS] = sum * sum_scale(ZEROS);
             }
           }
         }
         __syncthreads();
+        }
       }
       // ---- products
       const int end = stretch(round, wic + 1);
@@ -368,28 +422,28 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
       const int n = __umulhi(e, p.per_inv) * each, at = e - n / each * per, tile = tile_of(round * p.tpr + n);
       if (at >= rows * 16) continue;
       auto sum_of = [&](int m) {
-        // the parts of tile m, in the order of the warps; the same places in all ranks
+        // the parts of tile m in the order of the warps and ranks; they lie in the same places in all ranks
         float v = 0.f, w[WARPS];
         const float* part = s_acc + m * (p.rows * 16) + at;
-        auto parts = [&](auto&& load) {
+        auto has = [&](int i) { return max(stretch(round, i), m * p.sc) < min(stretch(round, i + 1), (m + 1) * p.sc); };
+        if (p.cs == 1) {
 #pragma unroll
-          for (int i = 0; i < WARPS; ++i) {
-            const int lo = max(stretch(round, i), m * p.sc), hi = min(stretch(round, i + 1), (m + 1) * p.sc);
-            w[i] = 0.f;
-            if (lo < hi) w[i] = load(part + i * (p.rows * 16));
-          }
+          for (int i = 0; i < WARPS; ++i) w[i] = has(i) ? part[i * (p.rows * 16)] : 0.f;
 #pragma unroll
           for (int i = 0; i < WARPS; ++i) v += w[i];
-        };
-        if (p.cs == 1) {
-          parts([](const float* a) { return *a; });
         } else {
-          for (int r = 0; r < p.cs; ++r)
-            parts([&](const float* a) {
-              float x;
-              asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(mapa_u32(smem_u32(a), r)));
-              return x;
-            });
+#pragma unroll 1
+          for (int i = 0; i < WARPS; ++i) {
+            if (!has(i)) continue;
+            const uint32_t a = smem_u32(part + i * (p.rows * 16));
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+              w[r] = 0.f;
+              if (r < p.cs) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w[r]) : "r"(mapa_u32(a, r)));
+            }
+#pragma unroll
+            for (int r = 0; r < 8; ++r) v += w[r];
+          }
         }
         return v * 0x1p24f;
       };
@@ -452,35 +506,36 @@ int launch_t(Gemv4Dev& p, cudaStream_t s) {
   }
   constexpr int COLS = NT * 8;
   // shared memory: activations with their sums, and sums of products
-  constexpr int GPC = 128 / GRP, RING_BYTES = WARPS * RING * SLOT * (1024 + 32 * GPC + (ZEROS ? 16 * GPC : 0));
-  constexpr int FIXED = RING_BYTES + 256 + WARPS * RING * 8 + COLS * 64;
+  constexpr int GPC = 128 / GRP, RING_BYTES = WARPS * RING * slot_chunks(NT) * (1024 + 32 * GPC + (ZEROS ? 16 * GPC : 0));
+  constexpr int FIXED = RING_BYTES + 256 + (WARPS * RING + 2) * 8 + COLS * 64;
   static_assert(SMEM_LIMIT - FIXED >= (WARPS + 2) * COLS * 64 + 4 * COLS * (256 + 4 + 4 * GPC), "shared memory budget");
   p.rows = p.B < COLS ? p.B : COLS;
   const int room = SMEM_LIMIT - FIXED, acc_bytes = p.rows * 64, sc_bytes = p.rows * 256 + COLS * (4 + 4 * GPC);
   // Work of an SM with two CTAs, in clocks as measured: 30 to convert a row's chunk, 47 (two n-tiles: 75) for a tile's chunk, the
   // exchange within a cluster. us in clusters of 1 / 2 / 8: 1 x 4096 -> 28672 gated 14.8 / 16.0 / 21.2, 1 x 14336 -> 4096 11.4 /
   // 11.4 / 15.0, 12 x 14336 -> 4096 62 / 38 / 24, 16 x 4096 -> 6144 22 / 26 / 14.
-  const int each = p.mode == 3 ? 2 : 1;
+  // A pass over part of the inputs, or a round over part of the tiles, costs 6000 more.
+  const int each = p.mode == 3 ? 2 : 1, want = p.tiles / each;
   int64_t best = INT64_MAX;
   for (int cs = 1; cs <= 8 && cs <= p.kt; cs *= 2) {
-    const int most = max_clusters<GRP, NT, ZEROS>(cs), want = p.tiles / each, clusters = want < most ? want : most;
-    const int64_t nc = ceil_div(p.kt, cs);
-    const int64_t cost = 2 * nc * (p.rows * 30 + (int64_t)p.tiles * (NT == 1 ? 47 : 75) / clusters) + (cs > 1 ? 4000 + 1000 * cs : 0);
+    const int most = max_clusters<GRP, NT, ZEROS>(cs), clusters = want < most ? want : most;
+    // all chunks of a CTA at once if they fit beside the sums of two tiles, then as many tiles as fit
+    const int dealt = ceil_div(want, clusters) * each, nc = ceil_div(p.kt, cs);
+    const int passes = ceil_div(nc, (room - (WARPS + 2) * acc_bytes) / sc_bytes), sc = ceil_div(p.kt, passes * cs);
+    const int rounds = ceil_div(dealt, ((room - sc * sc_bytes) / acc_bytes - WARPS) / 2 * 2);
+    const int64_t cost = (int64_t)2 * nc * (p.rows * (p.xq ? 2 : 30) + (int64_t)p.tiles * (NT == 1 ? 47 : NT == 2 ? 60 : 90) / clusters) +
+                         (cs > 1 ? 4000 + 1000 * cs : 0) + (passes * rounds - 1) * 6000;
     if (cost < best) {
       best = cost;
       p.cs = cs;
       p.clusters = clusters;
+      p.passes = passes;
+      p.sc = sc;
+      p.rounds = rounds;
+      p.tpr = ceil_div(dealt / each, rounds) * each;
     }
   }
-  // all chunks of a CTA at once if they fit beside the sums of two tiles, then as many tiles as fit
-  const int dealt = ceil_div(p.tiles / each, p.clusters) * each, all = ceil_div(p.kt, p.cs);
-  const int most_sc = (room - (WARPS + 2) * acc_bytes) / sc_bytes;
-  p.passes = ceil_div(all, most_sc);
-  p.sc = ceil_div(p.kt, p.passes * p.cs);
-  const int most_tpr = ((room - p.sc * sc_bytes) / acc_bytes - WARPS) / 2 * 2;
-  p.rounds = ceil_div(dealt, most_tpr);
-  p.tpr = ceil_div(dealt / each, p.rounds) * each;
-  p.grain = p.sc % SLOT == 0 ? SLOT : 1;
+  p.grain = p.sc % slot_chunks(NT) == 0 ? slot_chunks(NT) : 1;
   p.deal = p.tiles / each / p.clusters;
   p.deal_rest = p.tiles / each % p.clusters;
   p.sc_inv = (uint32_t)(((1ull << 32) + p.sc - 1) / p.sc);
@@ -498,13 +553,33 @@ int launch_t(Gemv4Dev& p, cudaStream_t s) {
   return POP_OK;
 }
 
+// Rows from which a launch of its own converts the activations
+constexpr int CONVERT_ROWS = 3;
+constexpr int cols_of(int B) { return B <= 8 ? 8 : B <= 16 ? 16 : 32; }
+
 template <int GRP>
-int launch_grp(Gemv4Dev& p, cudaStream_t s) {
-  if (p.zeros) return p.B <= 8 ? launch_t<GRP, 1, true>(p, s) : launch_t<GRP, 2, true>(p, s);
-  return p.B <= 8 ? launch_t<GRP, 1, false>(p, s) : launch_t<GRP, 2, false>(p, s);
+int launch_grp(Gemv4Dev& p, void* workspace, size_t bytes, cudaStream_t s) {
+  if (p.B >= CONVERT_ROWS) {
+    const int cols = cols_of(p.B), slabs = ceil_div(p.B, cols);
+    if (!workspace || (int64_t)bytes < slabs * slab_bytes(cols, 128 / GRP, p.kt)) return POP_E_NOSPACE;
+    if (p.B > 65535) return POP_E_INVALID;
+    p.xq = static_cast<uint8_t*>(workspace);
+    ProfScope prof(PROF_ELEMENTWISE, (double)p.B * p.K * 4, s);
+    if (launch_chained(gemv4_convert_kernel<GRP>, dim3(ceil_div(p.kt, 16), p.B), dim3(256), 0, s, p.x, p.ldx,
+                       static_cast<uint8_t*>(workspace), p.B, p.K, p.kt, cols, p.zeros ? 1 : 0) != cudaSuccess)
+      return POP_E_CUDA;
+    count_launch();
+  }
+  if (p.zeros) return p.B <= 8 ? launch_t<GRP, 1, true>(p, s) : p.B <= 16 ? launch_t<GRP, 2, true>(p, s) : launch_t<GRP, 4, true>(p, s);
+  return p.B <= 8 ? launch_t<GRP, 1, false>(p, s) : p.B <= 16 ? launch_t<GRP, 2, false>(p, s) : launch_t<GRP, 4, false>(p, s);
 }
 
 }  // namespace
+
+size_t gemv4_workspace_bytes(int B, int K, int group) {
+  if (B < CONVERT_ROWS || K < 1 || (group != 32 && group != 64 && group != 128)) return 0;
+  return (size_t)(ceil_div(B, cols_of(B)) * slab_bytes(cols_of(B), 128 / group, ceil_div(K, 128)));
+}
 
 int launch_gemv4(const Gemv4Args& a, cudaStream_t s) {
   if (!a.x || !a.codes || !a.scales || !a.out || a.B < 1 || a.N < 1 || a.K < 8 || a.K % 8) return POP_E_INVALID;
@@ -512,7 +587,7 @@ int launch_gemv4(const Gemv4Args& a, cudaStream_t s) {
   if (a.group != 32 && a.group != 64 && a.group != 128) return POP_E_INVALID;
   if (a.mode == 3 && (a.N % 256 || a.n_valid < 0 || a.n_valid > a.N / 2 || (a.act != 0 && a.act != 1))) return POP_E_INVALID;
   if (reinterpret_cast<uintptr_t>(a.x) % 16 || a.ldx % 8 || reinterpret_cast<uintptr_t>(a.codes) % 16 ||
-      reinterpret_cast<uintptr_t>(a.scales) % 16 || reinterpret_cast<uintptr_t>(a.zeros) % 16 ||
+      reinterpret_cast<uintptr_t>(a.scales) % 16 || reinterpret_cast<uintptr_t>(a.workspace) % 16 || reinterpret_cast<uintptr_t>(a.zeros) % 16 ||
       reinterpret_cast<uintptr_t>(a.out) % (a.mode == 3 ? 2 : 4))
     return POP_E_INVALID;
   if (a.N > (1 << 30) || a.K > (1 << 30)) return POP_E_INVALID;
@@ -525,9 +600,9 @@ int launch_gemv4(const Gemv4Args& a, cudaStream_t s) {
   p.kt = ceil_div(a.K, 128);
   p.tiles = ceil_div(a.N, 16);
   switch (a.group) {
-    case 32: return launch_grp<32>(p, s);
-    case 64: return launch_grp<64>(p, s);
-    default: return launch_grp<128>(p, s);
+    case 32: return launch_grp<32>(p, a.workspace, a.workspace_bytes, s);
+    case 64: return launch_grp<64>(p, a.workspace, a.workspace_bytes, s);
+    default: return launch_grp<128>(p, a.workspace, a.workspace_bytes, s);
   }
 }
 

@@ -69,8 +69,8 @@ def test_masks_of_trees():
 # ---------------------------------------------------------------------------------------- the C calls' refusals
 A = 1 << 20          # an aligned address that nothing dereferences
 CALLS = {
-    "pop_k_gemv_w4": dict(x=A, ldx=128, codes=A, scales=A, zeros=None, group=128, out=A, ldo=16, B=2, N=16, K=128, mode=0, act=0,
-                          n_valid=0, stream=None),
+    "pop_k_gemv_w4": dict(x=A, ldx=128, codes=A, scales=A, zeros=None, group=128, workspace=None, workspace_bytes=0, out=A, ldo=16,
+                          B=2, N=16, K=128, mode=0, act=0, n_valid=0, stream=None),
     "pop_k_rope_cache_tree": dict(x=A, in_bf16=0, ld_in=192, rows=2, cu_rows=None, max_rows=2, start=None, pos0=0, depth=None,
                                   batch=1, q_out=A, ldq=64, k_pool=A, v_pool=A, block_table=A, page_size=16, num_pages=4,
                                   max_pages=4, q_gain=None, k_gain=None, eps=0.0, rope_table=A, table_rows=64, n_q=1, n_kv=1,
@@ -88,7 +88,7 @@ CACHE = [dict(k_pool=None), dict(v_pool=None), dict(block_table=None), dict(page
 REFUSED = {
     "pop_k_gemv_w4": [dict(x=None), dict(codes=None), dict(scales=None), dict(out=None), dict(B=0), dict(N=0), dict(K=0), dict(K=12),
                       dict(mode=1), dict(mode=4), dict(group=16), dict(group=96), dict(group=0), dict(x=A + 8), dict(ldx=132),
-                      dict(ldx=120), dict(codes=A + 8), dict(scales=A + 4), dict(zeros=A + 4), dict(out=A + 2), dict(ldo=8),
+                      dict(ldx=120), dict(workspace=A + 8), dict(codes=A + 8), dict(scales=A + 4), dict(zeros=A + 4), dict(out=A + 2), dict(ldo=8),
                       dict(mode=3), dict(mode=3, N=256, ldo=128, n_valid=129), dict(mode=3, N=256, ldo=128, n_valid=-1),
                       dict(mode=3, N=256, ldo=128, n_valid=128, act=2)],
     "pop_k_rope_cache_tree": CACHE + [dict(x=None), dict(q_out=None), dict(rope_table=None), dict(x=A + 4), dict(ld_in=193),
@@ -107,7 +107,8 @@ REFUSED = {
 }
 NOSPACE = [("pop_k_rope_cache_tree", dict(pos0=63)), ("pop_k_tree_attention", dict(max_start=63)),
            ("pop_k_tree_attention", dict(max_start=65, start=A)), ("pop_k_tree_attention", dict(workspace_bytes=1 << 20)),
-           ("pop_k_tree_attention", dict(workspace=None)), ("pop_k_cache_keep", dict(pos0=61))]
+           ("pop_k_tree_attention", dict(workspace=None)), ("pop_k_gemv_w4", dict(B=9)),
+           ("pop_k_gemv_w4", dict(B=9, workspace=A, workspace_bytes=4000)), ("pop_k_cache_keep", dict(pos0=61))]
 NOTHING = [("pop_k_rope_cache_tree", dict(max_rows=0)), ("pop_k_rope_cache_tree", dict(rows=0, cu_rows=A)),
            ("pop_k_tree_attention", dict(max_rows=0)), ("pop_k_tree_attention", dict(rows=0, cu_rows=A)),
            ("pop_k_cache_keep", dict(max_kept=0))]
