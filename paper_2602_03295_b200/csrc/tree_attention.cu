@@ -6,9 +6,12 @@
 // all (sequence, kv head, row tile) items form one line, and each CTA takes an equal stretch of it. An item that lies in one
 // stretch is finished there; the others leave (maximum, sum, output) of their part, and a second launch joins the parts.
 // Warps of a CTA:
-//   NQT softmax warpgroups, one (row, head) per thread: scores of 64 keys from TMEM, mask, exponentials against the running
-//       maximum, P in bf16 back over the scores it came from;
-//   1 TMA warp: Q of an item, K and V tiles of 64 positions through a ring, in the order in which they are used;
+//   4 softmax warps, a thread per (row, head): scores of 64 keys from TMEM, mask, maximum, exponentials, P in bf16 back over
+//       the scores. These dependent steps (1700 clocks) are what a CTA waits for; where a second CTA shares the SM that is
+//       hidden, else (hd 256) 8 warps take half of the keys each, and join their maxima through shared memory (16 x 12 rows,
+//       window 1024: 45 us against 49; with two CTAs on the SM it costs: 24 x 27 rows of up to 12001 147 against 135);
+//   1 TMA warp: the CTA's place in the line, then Q of an item and K and V tiles of 64 positions through a ring, in the order in
+//       which they are used;
 //   1 MMA warp: scores two tiles ahead of the softmax, across the ends of items too, and O += P V with P from TMEM.
 #include "ptx.cuh"
 #include "tree.cuh"
@@ -18,33 +21,49 @@ namespace {
 
 constexpr int BKV = 64;
 
-template <int HD, int NQT>
+template <int HD>
 struct TC {
   static constexpr int KV_TILE_BYTES = BKV * HD * 2;
   static constexpr int KV_SUB_BYTES = BKV * 128;       // one 64-wide slice of head_dim
   static constexpr int Q_TILE_BYTES = 128 * HD * 2;
-  static constexpr int O_COL = NQT * 2 * BKV;          // S_t[b] at (t * 2 + b) * 64, O_t at O_COL + t * HD
-  static constexpr int COLS_USED = O_COL + NQT * HD;
-  static constexpr uint32_t TMEM_COLS = COLS_USED <= 256 ? 256 : 512;
+  static constexpr int O_COL = 2 * BKV;                // scores of tile f at (f & 1) * 64, O behind them
+  static constexpr uint32_t TMEM_COLS = O_COL + HD <= 256 ? 256 : 512;
   static constexpr int PER_SM = TMEM_COLS == 256 ? 2 : 1;        // one CTA's beginnings and ends beside the other's keys
-  static constexpr int RING_BYTES = (PER_SM == 2 ? 113 : 227) * 1024 - 2 * 1024 - NQT * Q_TILE_BYTES;
+  static constexpr int RING_BYTES = (PER_SM == 2 ? 113 : 227) * 1024 - 4 * 1024 - Q_TILE_BYTES;
   static constexpr int STAGES = RING_BYTES / KV_TILE_BYTES < 12 ? RING_BYTES / KV_TILE_BYTES : 12;
-  static constexpr int THREADS = NQT * 128 + 64;
-  static_assert(COLS_USED <= 512, "TMEM budget");
+  static constexpr int HALVES = PER_SM == 2 ? 1 : 2;   // threads that share a row's keys of a tile
+  static constexpr int KEYS = BKV / HALVES;
+  static constexpr int THREADS = HALVES * 128 + 64;
   static_assert(STAGES >= 4, "ring too shallow");
 };
 
-template <int HD, int NQT>
+// One sequence of the line
+struct Seq {
+  int row0, n, start;           // packed rows, positions in front of them
+  int j_lo, tiles, qts;         // first key tile, key tiles of an item, items per kv head
+};
+
+// Where a CTA's stretch of the line begins
+struct Plan {
+  int lo, hi;                   // its places in the line; nothing to do where they are equal
+  int b, base;                  // the sequence at lo, and where that one begins
+  Seq x;
+};
+
+template <int HD>
 struct __align__(1024) TreeSmem {
-  using C = TC<HD, NQT>;
-  uint8_t q[NQT][C::Q_TILE_BYTES];
+  using C = TC<HD>;
+  uint8_t q[C::Q_TILE_BYTES];
   uint8_t kv[C::STAGES][C::KV_TILE_BYTES];
   uint64_t q_full, q_empty;
   uint64_t kv_full[C::STAGES];
   uint64_t kv_empty[C::STAGES];
-  uint64_t s_full[NQT][2];      // scores of tile f in buffer f & 1, phase f >> 1; the same for the two below
-  uint64_t p_ready[NQT][2];     // P over the scores (one arrival per softmax warp)
-  uint64_t pv_done[NQT][2];     // O += P V complete
+  uint64_t s_full[2];           // scores of tile f in buffer f & 1, phase f >> 1; the same for the two below
+  uint64_t p_ready[2];          // P over the scores (one arrival per softmax warp)
+  uint64_t pv_done[2];          // O += P V complete
+  float half_max[2][2][128];    // [tile & 1][half of its keys][row]
+  float half_sum[128];
+  Plan plan;
   uint32_t tmem_base;
   uint32_t raised;
   volatile uint32_t abort;
@@ -52,24 +71,22 @@ struct __align__(1024) TreeSmem {
 
 struct TreeDev {
   TreeAttnArgs a;
-  int G, per;                   // query heads per kv head, rows per tile of 128
-  int nqt;                      // tiles of an item
+  int G, per;                   // query heads per kv head, rows of an item: a tile of 128 pairs
   int rows_per_load;            // positions of a TMA load: min(page_size, 64)
   int room;                     // positions that a row of the block table has pages for
   int ctas;
   float scale_log2;             // log2(e) / sqrt(hd)
-  float* partial;               // [2 per CTA][nqt * 128][hd + 4]
+  float* partial;               // [2 per CTA] parts
+  int* starts;                  // [batch + 1]: see plan_of
   int* status;
 };
 
+// Floats of a part: [hd / 4][128 rows][4] of the output, then maximum and sum as [128][4], two of them used. Neighbouring lanes
+// have neighbouring rows, so that what they write and read together lies together.
+__host__ __device__ constexpr int part_floats(int hd) { return (hd + 4) * 128; }
+
 // Fewest tiles of a stretch: below, beginning and ending it costs more than its keys
 constexpr int MIN_SHARE = 2;
-
-// One sequence of the line
-struct Seq {
-  int row0, n, start;           // packed rows, positions in front of them
-  int j_lo, tiles, qts;         // first key tile, key tiles of an item, items per kv head
-};
 
 __device__ __forceinline__ Seq seq_of(const TreeDev& p, int b, bool report) {
   const Drafts& d = p.a.d;
@@ -87,7 +104,7 @@ __device__ __forceinline__ Seq seq_of(const TreeDev& p, int b, bool report) {
   }
   x.j_lo = p.a.window > 0 ? max(0, x.start - p.a.window + 1) / BKV : 0;
   x.tiles = (x.start + x.n - 1) / BKV - x.j_lo + 1;
-  x.qts = (x.n + p.nqt * p.per - 1) / (p.nqt * p.per);
+  x.qts = (x.n + p.per - 1) / p.per;
   return x;
 }
 __device__ __forceinline__ int line_of(const TreeDev& p, const Seq& x) { return x.tiles * x.qts * p.a.n_kv; }
@@ -97,19 +114,59 @@ __device__ __forceinline__ int warp_add(int v) {
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-// Tiles of a CTA's stretch, by a whole warp
-__device__ __forceinline__ int share_of(const TreeDev& p, int* total, bool report) {
-  int sum = 0;
-  for (int b = threadIdx.x & 31; b < p.a.d.batch; b += 32) sum += line_of(p, seq_of(p, b, report));
-  *total = warp_add(sum);
-  const int share = (*total + p.ctas - 1) / p.ctas;
-  return share > MIN_SHARE ? share : MIN_SHARE;
-}
-// Tiles in front of sequence `b`, by a whole warp
-__device__ __forceinline__ int line_before(const TreeDev& p, int b) {
-  int sum = 0;
-  for (int i = threadIdx.x & 31; i < b; i += 32) sum += line_of(p, seq_of(p, i, false));
-  return warp_add(sum);
+// Finds the stretch of CTA `cta`, by a whole warp. `starts`, if given, gets the place where each sequence begins and, behind them,
+// the tiles of a stretch: what the second launch asks for.
+__device__ __forceinline__ Plan plan_of(const TreeDev& p, int cta, int* starts) {
+  const int lane = threadIdx.x & 31, batch = p.a.d.batch;
+  Seq x;
+  int mine = 0, total = 0;
+  for (int b0 = 0; b0 < batch; b0 += 32) {
+    mine = 0;
+    if (b0 + lane < batch) {
+      x = seq_of(p, b0 + lane, cta == 0);
+      mine = line_of(p, x);
+    }
+    total += warp_add(mine);
+  }
+  int share = (total + p.ctas - 1) / p.ctas;
+  if (share < MIN_SHARE) share = MIN_SHARE;
+  Plan r;
+  r.lo = (int)min((int64_t)cta * share, (int64_t)total);
+  r.hi = min(r.lo + share, total);
+  r.b = -1;
+  int base = 0;
+  for (int b0 = 0; b0 < batch; b0 += 32) {
+    if (batch > 32) {                                          // else the first loop's are still there
+      mine = 0;
+      if (b0 + lane < batch) {
+        x = seq_of(p, b0 + lane, false);
+        mine = line_of(p, x);
+      }
+    }
+    int incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    if (starts != nullptr && b0 + lane < batch) starts[b0 + lane] = base + incl - mine;
+    const uint32_t past = __ballot_sync(0xffffffffu, base + incl > r.lo);
+    if (past != 0 && r.b < 0) {
+      const int at = __ffs(past) - 1;
+      r.b = b0 + at;
+      r.base = base + __shfl_sync(0xffffffffu, incl - mine, at);
+      r.x.row0 = __shfl_sync(0xffffffffu, x.row0, at);
+      r.x.n = __shfl_sync(0xffffffffu, x.n, at);
+      r.x.start = __shfl_sync(0xffffffffu, x.start, at);
+      r.x.j_lo = __shfl_sync(0xffffffffu, x.j_lo, at);
+      r.x.tiles = __shfl_sync(0xffffffffu, x.tiles, at);
+      r.x.qts = __shfl_sync(0xffffffffu, x.qts, at);
+      if (starts == nullptr) break;
+    }
+    base += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (starts != nullptr && lane == 0) starts[batch] = share;
+  return r;
 }
 
 // A walk over a stretch of the line, tile by tile, the same for all lanes
@@ -123,37 +180,18 @@ struct Walk {
   __device__ __forceinline__ void item(const TreeDev& p, int off) {
     const int it = off / x.tiles, r = off - it * x.tiles;
     kvh = it / x.qts;
-    q0 = (it - kvh * x.qts) * p.nqt * p.per;
+    q0 = (it - kvh * x.qts) * p.per;
     j = x.j_lo + r;
     j_item_end = x.j_lo + x.tiles;
     j_end = min(j_item_end, j + hi - pos);
     left = line_of(p, x) - off;
   }
-  // begins at line place `lo` (by a whole warp, all lanes with the same arguments)
-  __device__ __forceinline__ void begin(const TreeDev& p, int lo, int hi_) {
-    const int lane = threadIdx.x & 31;
-    pos = lo;
-    hi = hi_;
-    int base = 0;
-    for (int b0 = 0;; b0 += 32) {
-      const int mine = b0 + lane < p.a.d.batch ? line_of(p, seq_of(p, b0 + lane, false)) : 0;
-      int incl = mine;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += v;
-      }
-      const uint32_t past = __ballot_sync(0xffffffffu, base + incl > lo);
-      if (past != 0) {                                         // lo lies in front of the line's end, so one is found
-        const int at = __ffs(past) - 1;
-        b = b0 + at;
-        base += __shfl_sync(0xffffffffu, incl - mine, at);
-        break;
-      }
-      base += __shfl_sync(0xffffffffu, incl, 31);
-    }
-    x = seq_of(p, b, false);
-    item(p, lo - base);
+  __device__ __forceinline__ void begin(const TreeDev& p, const Plan& at) {
+    x = at.x;
+    b = at.b;
+    pos = at.lo;
+    hi = at.hi;
+    item(p, at.lo - at.base);
   }
   // to the next tile; true where another segment begins there
   __device__ __forceinline__ bool next(const TreeDev& p) {
@@ -187,23 +225,22 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
 }
-__device__ __forceinline__ uint64_t ones(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
+__device__ __forceinline__ uint32_t ones(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
 __device__ __forceinline__ bool gave_up(int status) { return status <= (int)POP_E_DEVICE_TIMEOUT; }
 
-// Which of the 64 positions from kv0 on row i (packed row `row`) of the sequence sees
-__device__ __forceinline__ uint64_t seen_of(const TreeDev& p, const Seq& x, int i, int64_t row, int depth, int kv0) {
-  const int ctx = x.start - kv0;                               // positions of the tile in front of the draft
+// Which of the 32 positions from kv0 on row i (packed row `row`) of the sequence sees
+__device__ __forceinline__ uint32_t seen_of(const TreeDev& p, const Seq& x, int i, int64_t row, int depth, int kv0) {
+  const int ctx = x.start - kv0;                               // positions of these in front of the draft
   const int window = p.a.window;
-  uint64_t vis = ~0ull;
-  if (ctx < 64) {
+  uint32_t vis = ~0u;
+  if (ctx < 32) {
     if (p.a.mask == nullptr) {
       vis = ones(ctx + i + 1);
     } else {
       const uint32_t* m = p.a.mask + row * p.a.mask_words;
-      const int slot0 = ctx < 0 ? -ctx : 0, w = slot0 >> 5, sh = slot0 & 31;
-      auto word = [&](int k) { return k < p.a.mask_words ? (uint64_t)__ldg(m + k) : 0ull; };
-      const uint64_t lo = word(w) | (word(w + 1) << 32);
-      const uint64_t drafted = sh == 0 ? lo : (lo >> sh) | (word(w + 2) << (64 - sh));
+      const int slot0 = ctx < 0 ? -ctx : 0, w = slot0 >> 5;
+      auto word = [&](int k) { return k < p.a.mask_words ? __ldg(m + k) : 0u; };
+      const uint32_t drafted = __funnelshift_r(word(w), word(w + 1), slot0 & 31);
       vis = ctx > 0 ? (drafted << ctx) | ones(ctx) : drafted;
     }
     vis &= ones(ctx + x.n);
@@ -211,11 +248,11 @@ __device__ __forceinline__ uint64_t seen_of(const TreeDev& p, const Seq& x, int 
   if (window > 0) {
     const int hidden = x.start + depth - window + 1 - kv0;     // positions in front of the window
     if (hidden > 0) vis &= ~ones(min(hidden, ctx));
-    if (ctx < 64 && depth >= window) {                         // drafted slots that lie so far up the tree
-      for (uint64_t m = vis & ~ones(ctx); m != 0; m &= m - 1) {
-        const int k = __ffsll((long long)m) - 1, slot = k - ctx;
+    if (ctx < 32 && depth >= window) {                         // drafted slots that lie so far up the tree
+      for (uint32_t m = vis & ~ones(ctx); m != 0; m &= m - 1) {
+        const int k = __ffs((int)m) - 1, slot = k - ctx;
         const int d = p.a.d.depth ? __ldg(p.a.d.depth + x.row0 + slot) : slot;
-        if (d <= depth - window) vis &= ~(1ull << k);
+        if (d <= depth - window) vis &= ~(1u << k);
       }
     }
   }
@@ -228,57 +265,70 @@ __device__ __forceinline__ uint64_t seen_of(const TreeDev& p, const Seq& x, int 
     atomicMin((status), (int)POP_E_DEVICE_TIMEOUT);   \
   } while (0)
 
-template <int HD, int NQT>
-__global__ void __launch_bounds__(TC<HD, NQT>::THREADS, TC<HD, NQT>::PER_SM)
+// waits for, or only counts towards, a barrier of `n` threads
+__device__ __forceinline__ void named_sync(int id, int n) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+__device__ __forceinline__ void named_arrive(int id, int n) { asm volatile("bar.arrive %0, %1;" ::"r"(id), "r"(n) : "memory"); }
+
+template <int HD>
+__global__ void __launch_bounds__(TC<HD>::THREADS, TC<HD>::PER_SM)
 tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV, const __grid_constant__ TreeDev p) {
-  using C = TC<HD, NQT>;
-  constexpr int STAGES = C::STAGES;
+  using C = TC<HD>;
+  constexpr int STAGES = C::STAGES, HALVES = C::HALVES, KEYS = C::KEYS, TMA_WARP = 4 * HALVES, MMA_WARP = TMA_WARP + 1, PLAN_BAR = 1, PAIR_BAR = 2;     // PAIR_BAR + quarter
   extern __shared__ uint8_t smem_raw[];
-  TreeSmem<HD, NQT>& s =
-      *reinterpret_cast<TreeSmem<HD, NQT>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  TreeSmem<HD>& s = *reinterpret_cast<TreeSmem<HD>*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   chain_trigger();
-  if (threadIdx.x == 0) {
-    mbar_init(&s.q_full, 1);
-    mbar_init(&s.q_empty, 1);
-    for (int i = 0; i < STAGES; ++i) {
-      mbar_init(&s.kv_full[i], 1);
-      mbar_init(&s.kv_empty[i], 1);
-    }
-    for (int t = 0; t < NQT; ++t)
-      for (int i = 0; i < 2; ++i) {
-        mbar_init(&s.s_full[t][i], 1);
-        mbar_init(&s.p_ready[t][i], 4);
-        mbar_init(&s.pv_done[t][i], 1);
+  Plan plan;
+  plan.lo = plan.hi = 0;
+  if (warp == TMA_WARP) {
+    if (lane == 0) {
+      mbar_init(&s.q_full, 1);
+      mbar_init(&s.q_empty, 1);
+      for (int i = 0; i < STAGES; ++i) {
+        mbar_init(&s.kv_full[i], 1);
+        mbar_init(&s.kv_empty[i], 1);
       }
-    s.abort = 0;
-    fence_barrier_init();
-    prefetch_tmap(&tmQ);
-    prefetch_tmap(&tmK);
-    prefetch_tmap(&tmV);
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(&s.s_full[i], 1);
+        mbar_init(&s.p_ready[i], 4 * HALVES);
+        mbar_init(&s.pv_done[i], 1);
+      }
+      s.abort = 0;
+      fence_barrier_init();
+      prefetch_tmap(&tmQ);
+      prefetch_tmap(&tmK);
+      prefetch_tmap(&tmV);
+    }
+    __syncwarp();
+    chain_wait();
+    const int raised = lane == 0 ? *reinterpret_cast<const volatile int*>(p.status) : 0;
+    plan = plan_of(p, blockIdx.x, blockIdx.x == 0 ? p.starts : nullptr);
+    if (__shfl_sync(0xffffffffu, gave_up(raised) ? 1 : 0, 0)) plan.hi = plan.lo;     // a call that is not to run
+    if (lane == 0) s.plan = plan;
+    __syncwarp();
+    named_arrive(PLAN_BAR, C::THREADS);
+  } else {
+    chain_wait();
+    if (warp == MMA_WARP) {
+      // columns that a CTA of another call has not given back yet are waited for: that CTA waits for nobody
+      tmem_alloc(&s.tmem_base, C::TMEM_COLS);
+      tmem_relinquish();
+    }
+    tc_fence_before();
+    named_sync(PLAN_BAR, C::THREADS);
+    tc_fence_after();
   }
-  chain_wait();
-  if (threadIdx.x == 0) s.raised = gave_up(*reinterpret_cast<const volatile int*>(p.status)) ? 1u : 0u;
-  int total;
-  const int share = share_of(p, &total, blockIdx.x == 0 && warp == 0);
-  const int lo = min((int64_t)blockIdx.x * share, (int64_t)total), hi = min(lo + share, total);
-  __syncthreads();
-  if (lo >= hi || s.raised != 0) return;
-  if (warp == NQT * 4 + 1) {
-    tmem_alloc(&s.tmem_base, C::TMEM_COLS);
-    tmem_relinquish();
-  }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
   const uint32_t tmem_base = s.tmem_base;
-  const int n_tiles = hi - lo;
+  const int lo = warp == TMA_WARP ? plan.lo : s.plan.lo, hi = warp == TMA_WARP ? plan.hi : s.plan.hi, n_tiles = hi - lo;
+  const bool nothing = n_tiles <= 0;
 
-  if (warp == NQT * 4) {
+  if (nothing) {
+    // beyond the line's end
+  } else if (warp == TMA_WARP) {
     // ------------------------------------------------------------------ TMA: K_0, K_1, then V_f, K_{f+2}
     Walk kw, vw;
-    kw.begin(p, lo, hi);
+    kw.begin(p, plan);
     vw = kw;
     const int loads = BKV / p.rows_per_load, log_loads = loads == 1 ? 0 : loads == 2 ? 1 : 2;
     int ring = 0, items = 0;
@@ -331,10 +381,9 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       }
       ++items;
       if (lane == 0) {
-        mbar_expect_tx(&s.q_full, NQT * p.per * p.G * HD * 2);
-        for (int t = 0; t < NQT; ++t)
-          for (int c = 0; c < HD / 64; ++c)
-            tma_load_3d(s.q[t] + c * 16384, &tmQ, &s.q_full, c * 64, w.kvh * p.G, w.x.row0 + w.q0 + t * p.per);
+        mbar_expect_tx(&s.q_full, p.per * p.G * HD * 2);
+        for (int c = 0; c < HD / 64; ++c)
+          tma_load_3d(s.q + c * 16384, &tmQ, &s.q_full, c * 64, w.kvh * p.G, w.x.row0 + w.q0);
       }
     };
     bool fresh = true;
@@ -353,35 +402,33 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       if (ok && kf < n_tiles) load_k();
     }
     if (!ok) TREE_ABORT(s, p.status);
-  } else if (warp == NQT * 4 + 1) {
+  } else if (warp == MMA_WARP) {
     // ------------------------------------------------------------------ MMA issuer (whole warp, elected lane)
     Walk sw, pw;
-    sw.begin(p, lo, hi);
+    sw.begin(p, s.plan);
     pw = sw;
     const uint32_t leader = elect_one();
     constexpr uint32_t idesc_s = umma_idesc_bf16(128, BKV, 0, 0);
     constexpr uint32_t idesc_o = umma_idesc_bf16(128, HD, 0, 1);
-    uint64_t q_desc[NQT];
-    for (int t = 0; t < NQT; ++t) q_desc[t] = umma_smem_desc(smem_u32(s.q[t]), 16, 1024);
+    const uint64_t q_desc = umma_smem_desc(smem_u32(s.q), 16, 1024);
     const uint64_t k_desc0 = umma_smem_desc(smem_u32(s.kv[0]), 16, 1024);                 // K-major
     const uint64_t v_desc0 = umma_smem_desc(smem_u32(s.kv[0]), C::KV_SUB_BYTES, 1024);    // MN-major
-    auto issue_s = [&](int t, int f, int stage) {
+    auto issue_s = [&](int f, int stage) {
       const uint64_t kd = k_desc0 + uint64_t(stage * (C::KV_TILE_BYTES >> 4));
-      const uint32_t d = tmem_base + (t * 2 + (f & 1)) * BKV;
+      const uint32_t d = tmem_base + (f & 1) * BKV;
 #pragma unroll
       for (int kk = 0; kk < HD / 16; ++kk)
-        umma_bf16_ss_w(leader, d, q_desc[t] + uint64_t(((kk >> 2) * 16384 + (kk & 3) * 32) >> 4),
+        umma_bf16_ss_w(leader, d, q_desc + uint64_t(((kk >> 2) * 16384 + (kk & 3) * 32) >> 4),
                        kd + uint64_t(((kk >> 2) * C::KV_SUB_BYTES + (kk & 3) * 32) >> 4), idesc_s, kk > 0 ? 1u : 0u);
-      umma_commit_w(leader, &s.s_full[t][f & 1]);
+      umma_commit_w(leader, &s.s_full[f & 1]);
     };
-    auto issue_pv = [&](int t, int f, int stage, bool begins) {
-      const uint32_t pa = tmem_base + (t * 2 + (f & 1)) * BKV;
+    auto issue_pv = [&](int f, int stage, bool begins) {
+      const uint32_t pa = tmem_base + (f & 1) * BKV;
       const uint64_t vd = v_desc0 + uint64_t(stage * (C::KV_TILE_BYTES >> 4));
-      const uint32_t d = tmem_base + C::O_COL + t * HD;
 #pragma unroll
       for (int kk = 0; kk < BKV / 16; ++kk)
-        umma_bf16_ts_w(leader, d, pa + kk * 8, vd + uint64_t((kk * 2048) >> 4), idesc_o, (!begins || kk > 0) ? 1u : 0u);
-      umma_commit_w(leader, &s.pv_done[t][f & 1]);
+        umma_bf16_ts_w(leader, tmem_base + C::O_COL, pa + kk * 8, vd + uint64_t((kk * 2048) >> 4), idesc_o, (!begins || kk > 0) ? 1u : 0u);
+      umma_commit_w(leader, &s.pv_done[f & 1]);
     };
     int ring = 0, sf = 0, items = 0;
     bool ok = true, s_fresh = true, p_fresh = true;
@@ -399,7 +446,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       if (ok) ok = wait_tile(stage);
       if (!ok) return;
       tc_fence_after();
-      for (int t = 0; t < NQT; ++t) issue_s(t, sf, stage);
+      issue_s(sf, stage);
       umma_commit_w(leader, &s.kv_empty[stage]);
       ++sf;
       s_fresh = sw.next(p);
@@ -410,35 +457,32 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     for (int f = 0; f < n_tiles && ok && !s.abort; ++f) {
       int stage = 0;
       ok = wait_tile(stage);
-      for (int t = 0; t < NQT && ok; ++t) {
-        ok = mbar_wait_relaxed(&s.p_ready[t][f & 1], (f >> 1) & 1);
-        if (!ok) break;
-        tc_fence_after();
-        issue_pv(t, f, stage, p_fresh);
-      }
+      if (ok) ok = mbar_wait_relaxed(&s.p_ready[f & 1], (f >> 1) & 1);
       if (!ok) break;
+      tc_fence_after();
+      issue_pv(f, stage, p_fresh);
       umma_commit_w(leader, &s.kv_empty[stage]);
       p_fresh = pw.next(p);
       if (sf < n_tiles) scores();
     }
     if (!ok) TREE_ABORT(s, p.status);
   } else {
-    // ------------------------------------------------------------------ softmax warpgroups
+    // ------------------------------------------------------------------ softmax
     Walk w;
-    w.begin(p, lo, hi);
-    const int t = warp >> 2, quarter = warp & 3;
+    w.begin(p, s.plan);
+    const int half = warp >> 2, quarter = warp & 3;       // half of a tile's keys
     const int row = quarter * 32 + lane;                  // pair of the tile == TMEM lane
     const int ip = row / p.G, h = row - ip * p.G;         // row of the tile, head of the kv head
     const uint32_t lane_addr = uint32_t(quarter * 32) << 16;
-    const uint32_t s_addr = tmem_base + lane_addr + t * 2 * BKV;
-    const uint32_t o_addr = tmem_base + lane_addr + C::O_COL + t * HD;
+    const uint32_t s_addr = tmem_base + lane_addr;
+    const uint32_t o_addr = tmem_base + lane_addr + C::O_COL + half * (HD / HALVES);
     bool ok = true;
-    auto wait_pv = [&](int f) { return mbar_wait(&s.pv_done[t][f & 1], (f >> 1) & 1); };
+    auto wait_pv = [&](int f) { return mbar_wait(&s.pv_done[f & 1], (f >> 1) & 1); };
     int f = 0;
     while (f < n_tiles && ok && !s.abort) {
       // ---- a segment: the tiles of one item that lie in this stretch
       const Seq x = w.x;
-      const int kvh = w.kvh, j0 = w.j, nt = w.j_end - w.j, i = w.q0 + t * p.per + ip;
+      const int kvh = w.kvh, j0 = w.j, nt = w.j_end - w.j, i = w.q0 + ip;
       const bool whole = j0 == x.j_lo && w.j_end == w.j_item_end;
       const int slot = 2 * (int)blockIdx.x + (f > 0 ? 1 : 0);
       const bool used = ip < p.per && i < x.n;
@@ -451,68 +495,53 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       for (int jj = 0; jj < nt && !s.abort; ++jj, ++f) {
         const int kv0 = (j0 + jj) * BKV;
         const uint32_t sp_addr = s_addr + (f & 1) * BKV;
-        if (!mbar_wait(&s.s_full[t][f & 1], (f >> 1) & 1)) { ok = false; break; }
+        if (!mbar_wait(&s.s_full[f & 1], (f >> 1) & 1)) { ok = false; break; }
         if (!idle) {
           tc_fence_after();
-          float sv[BKV];
+          float sv[KEYS];
 #pragma unroll
-          for (int c = 0; c < BKV / 32; ++c)
-            tmem_ld_32x32b_x32(sp_addr + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[c * 32]));
-          const uint64_t vis = used ? seen_of(p, x, i, prow, depth, kv0) : 0ull;
-          tmem_wait_ld();
-          if (vis != ~0ull) {
-            const uint32_t v0 = (uint32_t)vis, v1 = (uint32_t)(vis >> 32);
+          for (int c = 0; c < KEYS / 32; ++c)
+            tmem_ld_32x32b_x32(sp_addr + half * KEYS + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[c * 32]));
+          uint32_t vis[KEYS / 32];
 #pragma unroll
-            for (int k = 0; k < BKV; ++k)
-              if (!(((k < 32 ? v0 : v1) >> (k & 31)) & 1u)) sv[k] = -INFINITY;
+          for (int c = 0; c < KEYS / 32; ++c) vis[c] = used ? ~0u : 0u;
+          if (kv0 + BKV > x.start || (p.a.window > 0 && kv0 + p.a.window <= x.start + depth)) {
+#pragma unroll
+            for (int c = 0; c < KEYS / 32; ++c) vis[c] = used ? seen_of(p, x, i, prow, depth, kv0 + half * KEYS + c * 32) : 0u;
           }
-          // P = exp2(S * scale - m) against the maximum the row already has; this tile's own is reduced alongside and
-          // looked at afterwards. P enters the product as bf16, its sum is taken in fp32 before that rounding.
-          float2 acc0, acc1;
-          uint32_t pk[BKV / 2];
-          float mx0, mx1, mx2, mx3;
-          auto exps = [&](float m_use) {
-            const float2 sc2 = make_float2(p.scale_log2, p.scale_log2);
-            const float2 nm2 = make_float2(-m_use, -m_use);
-            acc0 = make_float2(0.f, 0.f);
-            acc1 = make_float2(0.f, 0.f);
-            mx0 = sv[0]; mx1 = sv[2]; mx2 = sv[4]; mx3 = sv[6];
+          tmem_wait_ld();
+          if ((vis[0] & vis[KEYS / 32 - 1]) != ~0u) {
 #pragma unroll
-            for (int c = 0; c < BKV / 8; ++c) {
-              float2 x0 = __ffma2_rn(make_float2(sv[c * 8 + 0], sv[c * 8 + 1]), sc2, nm2);
-              float2 x1 = __ffma2_rn(make_float2(sv[c * 8 + 2], sv[c * 8 + 3]), sc2, nm2);
-              float2 x2 = __ffma2_rn(make_float2(sv[c * 8 + 4], sv[c * 8 + 5]), sc2, nm2);
-              float2 x3 = __ffma2_rn(make_float2(sv[c * 8 + 6], sv[c * 8 + 7]), sc2, nm2);
-              mx0 = max3(mx0, sv[c * 8 + 0], sv[c * 8 + 1]);
-              mx1 = max3(mx1, sv[c * 8 + 2], sv[c * 8 + 3]);
-              mx2 = max3(mx2, sv[c * 8 + 4], sv[c * 8 + 5]);
-              mx3 = max3(mx3, sv[c * 8 + 6], sv[c * 8 + 7]);
-              x0.x = ex2(x0.x); x0.y = ex2(x0.y);
-              x1.x = ex2(x1.x); x1.y = ex2(x1.y);
-              x2.x = ex2(x2.x); x2.y = ex2(x2.y);
-              x3.x = ex2(x3.x); x3.y = ex2(x3.y);
-              acc0 = __fadd2_rn(acc0, x0);
-              acc1 = __fadd2_rn(acc1, x1);
-              acc0 = __fadd2_rn(acc0, x2);
-              acc1 = __fadd2_rn(acc1, x3);
-              pk[c * 4 + 0] = pack2(x0.x, x0.y);
-              pk[c * 4 + 1] = pack2(x1.x, x1.y);
-              pk[c * 4 + 2] = pack2(x2.x, x2.y);
-              pk[c * 4 + 3] = pack2(x3.x, x3.y);
-            }
-          };
-          exps(m_run == -INFINITY ? 0.f : m_run);
-          const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * p.scale_log2;
-          const float m_new = fmaxf(m_run, mx);
+            for (int k = 0; k < KEYS; ++k)
+              if (!((vis[k / 32] >> (k & 31)) & 1u)) sv[k] = -INFINITY;
+          }
+          float mx0 = sv[0], mx1 = sv[2], mx2 = sv[4], mx3 = sv[6];
+#pragma unroll
+          for (int c = 0; c < KEYS / 8; ++c) {
+            mx0 = max3(mx0, sv[c * 8 + 0], sv[c * 8 + 1]);
+            mx1 = max3(mx1, sv[c * 8 + 2], sv[c * 8 + 3]);
+            mx2 = max3(mx2, sv[c * 8 + 4], sv[c * 8 + 5]);
+            mx3 = max3(mx3, sv[c * 8 + 6], sv[c * 8 + 7]);
+          }
+          float mine = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
+          if constexpr (HALVES == 2) {
+            // the other half's maximum; behind this barrier both halves have their scores, and P may overwrite them
+            s.half_max[f & 1][half][row] = mine;
+            tc_fence_before();
+            named_sync(PAIR_BAR + quarter, 64);
+            tc_fence_after();
+            mine = fmaxf(mine, s.half_max[f & 1][half ^ 1][row]);
+          }
+          const float m_new = fmaxf(m_run, mine * p.scale_log2);
           const bool need = (m_new - m_run > 8.0f) || (m_run == -INFINITY && m_new > -INFINITY);
           if (__any_sync(0xffffffffu, need)) {
-            // the maximum grew by more than 2^8 somewhere in this warp: bring the accumulator to the new one
+            // the maximum grew by more than 2^8 somewhere in these rows: bring the accumulator to the new one
             const float factor = (m_new == -INFINITY) ? 1.0f : ex2(m_run - m_new);   // ex2(-inf) = 0
             if (jj > 0) {
               if (!wait_pv(f - 1)) { ok = false; break; }
               tc_fence_after();
 #pragma unroll 1
-              for (int c = 0; c < HD / 32; ++c) {
+              for (int c = 0; c < HD / HALVES / 32; ++c) {
                 uint32_t o[32];
                 tmem_ld_32x32b_x32(o_addr + c * 32, o);
                 tmem_wait_ld();
@@ -524,15 +553,31 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             }
             l_run *= factor;
             m_run = m_new;
-            exps(m_run == -INFINITY ? 0.f : m_run);
+          }
+          // P = exp2(S * scale - m): enters the product as bf16, its sum is taken in fp32 before that rounding
+          const float m_use = m_run == -INFINITY ? 0.f : m_run;
+          const float2 sc2 = make_float2(p.scale_log2, p.scale_log2), nm2 = make_float2(-m_use, -m_use);
+          float2 acc0 = make_float2(0.f, 0.f), acc1 = make_float2(0.f, 0.f);
+          uint32_t pk[KEYS / 2];
+#pragma unroll
+          for (int c = 0; c < KEYS / 4; ++c) {
+            float2 x0 = __ffma2_rn(make_float2(sv[c * 4 + 0], sv[c * 4 + 1]), sc2, nm2);
+            float2 x1 = __ffma2_rn(make_float2(sv[c * 4 + 2], sv[c * 4 + 3]), sc2, nm2);
+            x0.x = ex2(x0.x); x0.y = ex2(x0.y);
+            x1.x = ex2(x1.x); x1.y = ex2(x1.y);
+            acc0 = __fadd2_rn(acc0, x0);
+            acc1 = __fadd2_rn(acc1, x1);
+            pk[c * 2 + 0] = pack2(x0.x, x0.y);
+            pk[c * 2 + 1] = pack2(x1.x, x1.y);
           }
           l_run += (acc0.x + acc0.y) + (acc1.x + acc1.y);
-          tmem_st_32x32b_x32(sp_addr, pk);
+          if constexpr (HALVES == 2) tmem_st_32x32b_x16(sp_addr + half * 16, pk);
+          else tmem_st_32x32b_x32(sp_addr, pk);
           tmem_wait_st();
         }
         // positions behind the sequence's end or in front of every window may hold anything: zeros in the staged V tile, so
         // that 0 * garbage cannot reach the accumulator. V_f is entry min(f + 2, n_tiles) + f of the ring.
-        if (t == 0 && warp < 2 && (kv0 + BKV > len || kv0 < win_lo)) {
+        if (warp < 2 && (kv0 + BKV > len || kv0 < win_lo)) {
           const int rv = min(f + 2, n_tiles) + f;
           if (!mbar_wait(&s.kv_full[rv % STAGES], (rv / STAGES) & 1)) { ok = false; break; }
           if (kv0 + row >= len || kv0 + row < win_lo) {
@@ -546,20 +591,31 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&s.p_ready[t][f & 1]);
+        if (lane == 0) mbar_arrive(&s.p_ready[f & 1]);
         w.next(p);
       }
       if (!ok || s.abort) break;
       if (!wait_pv(f - 1)) { ok = false; break; }
       if (!idle) {
         tc_fence_after();
+        if constexpr (HALVES == 2) {                      // the sum of both halves, the first half's first
+          if (half == 1) s.half_sum[row] = l_run;
+          named_sync(PAIR_BAR + quarter, 64);
+          if (half == 0) {
+            l_run += s.half_sum[row];
+            s.half_sum[row] = l_run;
+          }
+          named_sync(PAIR_BAR + quarter, 64);
+          l_run = s.half_sum[row];
+        }
         const bool none = l_run == 0.f;                   // a row that sees nothing is a row of zeros
         const float inv = none ? 0.f : 1.0f / l_run;
-        bf16* out = p.a.out + prow * p.a.ldo + (int64_t)(kvh * p.G + h) * HD;
-        float* part = p.partial + ((int64_t)slot * (NQT * 128) + t * 128 + row) * (HD + 4);
-        if (used && !whole) *reinterpret_cast<float4*>(part) = make_float4(m_run, l_run, 0.f, 0.f);
+        bf16* out = p.a.out + prow * p.a.ldo + (int64_t)(kvh * p.G + h) * HD + half * (HD / HALVES);
+        float* part = p.partial + (int64_t)slot * part_floats(HD) + row * 4;     // four columns of all rows, then the next
+        if (used && !whole && half == 0) *reinterpret_cast<float2*>(part + HD * 128) = make_float2(m_run, l_run);
+        part += half * (HD / HALVES / 4) * 512;
 #pragma unroll 1
-        for (int c = 0; c < HD / 32; ++c) {
+        for (int c = 0; c < HD / HALVES / 32; ++c) {
           uint32_t o[32];
           tmem_ld_32x32b_x32(o_addr + c * 32, o);
           tmem_wait_ld();
@@ -581,93 +637,92 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           } else {
 #pragma unroll
             for (int v = 0; v < 8; ++v)
-              *reinterpret_cast<uint4*>(part + 4 + c * 32 + v * 4) = make_uint4(o[v * 4], o[v * 4 + 1], o[v * 4 + 2], o[v * 4 + 3]);
+              *reinterpret_cast<uint4*>(part + (c * 8 + v) * 512) = make_uint4(o[v * 4], o[v * 4 + 1], o[v * 4 + 2], o[v * 4 + 3]);
           }
         }
       }
       // the next item's first product overwrites O: it waits for P of all warps, which they write after this
     }
     if (!ok) TREE_ABORT(s, p.status);
+    // the other half may be waiting for this one; it looks at abort next
+    if (HALVES == 2 && __any_sync(0xffffffffu, s.abort != 0)) named_arrive(PAIR_BAR + quarter, 64);
   }
 
   // ------------------------------------------------------------------ teardown
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (s.abort && threadIdx.x == 0) {
+  if (!nothing && s.abort && threadIdx.x == 0) {
     for (int i = 0; i < 2000; ++i) __nanosleep(1000);   // let in-flight bulk copies land
   }
   __syncthreads();
-  if (warp == NQT * 4 + 1) {
+  if (warp == MMA_WARP) {
     tc_fence_after();
     tmem_dealloc(tmem_base, C::TMEM_COLS);
   }
 }
 
-// Joins the parts of the items that lie in several stretches: a warp per (row, head), out = sum_c w_c o_c / sum_c w_c l_c with
-// w_c = exp2(m_c - max m), the stretches in their order.
+// Joins the parts of the items that lie in several stretches: a thread per (row, head) and 8 columns, out = sum_c w_c o_c /
+// sum_c w_c l_c with w_c = exp2(m_c - max m), the stretches in their order.
+constexpr int MERGE_COLS = 8;
 template <int HD>
-__global__ void __launch_bounds__(256) tree_merge_kernel(const __grid_constant__ TreeDev p) {
+__global__ void __launch_bounds__(128) tree_merge_kernel(const __grid_constant__ TreeDev p) {
   chain_trigger();
   chain_wait();
-  const int lane = threadIdx.x & 31, b = blockIdx.z;
-  const int word = threadIdx.x == 0 ? *reinterpret_cast<const volatile int*>(p.status) : 0;
-  int total;
-  const int share = share_of(p, &total, false);
+  const int b = blockIdx.z, kvh = blockIdx.x % p.a.n_kv, qt = blockIdx.x / p.a.n_kv, col = blockIdx.y * MERGE_COLS, row = threadIdx.x;
+  const int word = *reinterpret_cast<const volatile int*>(p.status), share = p.starts[p.a.d.batch], first = p.starts[b];
   const Seq x = seq_of(p, b, false);
-  const int kvh = blockIdx.x % p.a.n_kv, qt = blockIdx.x / p.a.n_kv;
-  const int u = blockIdx.y * 8 + (threadIdx.x >> 5), pairs = p.per * p.G;       // pair of the item
-  const int a = qt < x.qts ? line_before(p, b) + (kvh * x.qts + qt) * x.tiles : 0;
-  if (__syncthreads_or(gave_up(word)) || qt >= x.qts) return;                   // gave up: there are parts that nobody wrote
-  const int c0 = a / share, c1 = (a + x.tiles - 1) / share, pieces = c1 - c0 + 1;
-  const int t = u / pairs, in_tile = u - t * pairs, ip = in_tile / p.G, i = qt * p.nqt * p.per + t * p.per + ip;
-  if (pieces == 1 || t >= p.nqt || i >= x.n) return;
-  constexpr int PER = HD / 32;
-  float m = -INFINITY, l = 0.f, o[PER];
-#pragma unroll
-  for (int k = 0; k < PER; ++k) o[k] = 0.f;
-  const int64_t stride = (int64_t)(p.nqt * 128) * (HD + 4);                     // from slot to slot
-  const float* rows = p.partial + (int64_t)(t * 128 + in_tile) * (HD + 4);
+  if (qt >= x.qts || gave_up(word)) return;                                     // gave up: there are parts that nobody wrote
+  const int a = first + (kvh * x.qts + qt) * x.tiles, c0 = a / share, c1 = (a + x.tiles - 1) / share;
+  const int ip = row / p.G, i = qt * p.per + ip;
+  if (c0 == c1 || ip >= p.per || i >= x.n) return;
   // a stretch's first segment is in its first slot; the item's own beginning may lie behind another item in its stretch
-  auto part_of = [&](int c) { return rows + (2 * (int64_t)c + (a > (int64_t)c * share ? 1 : 0)) * stride; };
-  for (int s0 = c0; s0 <= c1; s0 += 32) {
-    const int live = min(32, c1 - s0 + 1);
-    float ms = -INFINITY, ls = 0.f;
-    if (lane < live) {
-      const float* src = part_of(s0 + lane);
-      ms = __ldcg(src);
-      ls = __ldcg(src + 1);
+  constexpr int64_t step = 2 * part_floats(HD);
+  const float* at = p.partial + row * 4 + c0 * step;
+  const float* head = at + (a > c0 * share ? part_floats(HD) : 0);
+  constexpr int N = MERGE_COLS / 4;
+  float m = -INFINITY, l = 0.f, o[MERGE_COLS];
+#pragma unroll
+  for (int k = 0; k < MERGE_COLS; ++k) o[k] = 0.f;
+  // eight parts at a time: their loads are in flight together
+  for (int c = c0; c <= c1; c += 8) {
+    float2 ml[8];
+    float4 v[8][N];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float* src = c + u == c0 ? head : at + (c + u - c0) * step;
+      const bool in = c + u <= c1;
+      ml[u] = in ? __ldcg(reinterpret_cast<const float2*>(src + HD * 128)) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        v[u][k] = in ? __ldcg(reinterpret_cast<const float4*>(src + (col / 4 + k) * 512)) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    float n = fmaxf(m, ms);
+    float n = m;
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) n = fmaxf(n, __shfl_xor_sync(0xffffffffu, n, d));
+    for (int u = 0; u < 8; ++u) n = fmaxf(n, ml[u].x);
     // no maximum so far: the parts saw nothing (zeros), or scores that are all NaN, whose sums stay NaN
-    const float z = n == -INFINITY ? 0.f : n;
-    const float f = ex2(m - z), wt = ex2(ms - z);
-    float sum = wt * ls;
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    l = l * f + sum;
+    const float z = n == -INFINITY ? 0.f : n, f = ex2(m - z);
     m = n;
+    l *= f;
 #pragma unroll
-    for (int k = 0; k < PER; ++k) o[k] *= f;
-#pragma unroll 4
-    for (int q = 0; q < live; ++q) {
-      const float wq = __shfl_sync(0xffffffffu, wt, q);
-      const float* src = part_of(s0 + q) + 4 + lane * 2;
+    for (int k = 0; k < MERGE_COLS; ++k) o[k] *= f;
 #pragma unroll
-      for (int k = 0; k < PER; k += 2) {
-        const float2 v = __ldcg(reinterpret_cast<const float2*>(src + k * 32));
-        o[k] = fmaf(v.x, wq, o[k]);
-        o[k + 1] = fmaf(v.y, wq, o[k + 1]);
+    for (int u = 0; u < 8; ++u) {
+      const float w = ex2(ml[u].x - z);
+      l = fmaf(w, ml[u].y, l);
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        o[k * 4 + 0] = fmaf(v[u][k].x, w, o[k * 4 + 0]);
+        o[k * 4 + 1] = fmaf(v[u][k].y, w, o[k * 4 + 1]);
+        o[k * 4 + 2] = fmaf(v[u][k].z, w, o[k * 4 + 2]);
+        o[k * 4 + 3] = fmaf(v[u][k].w, w, o[k * 4 + 3]);
       }
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  bf16* dst = p.a.out + ((int64_t)x.row0 + i) * p.a.ldo + (int64_t)(kvh * p.G + in_tile - ip * p.G) * HD + lane * 2;
-#pragma unroll
-  for (int k = 0; k < PER; k += 2)
-    *reinterpret_cast<__nv_bfloat162*>(dst + k * 32) = __floats2bfloat162_rn(o[k] * inv, o[k + 1] * inv);
+  bf16* dst = p.a.out + ((int64_t)x.row0 + i) * p.a.ldo + (int64_t)(kvh * p.G + row - ip * p.G) * HD + col;
+  *reinterpret_cast<uint4*>(dst) = make_uint4(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv), pack2(o[4] * inv, o[5] * inv),
+                                              pack2(o[6] * inv, o[7] * inv));
 }
 
 bool allow_smem(std::atomic<uint64_t>& done, const void* kernel, int bytes) {
@@ -680,23 +735,23 @@ bool allow_smem(std::atomic<uint64_t>& done, const void* kernel, int bytes) {
   return true;
 }
 
-template <int HD, int NQT>
+template <int HD>
 int launch_t(const TreeAttnArgs& a, TreeDev& p, cudaStream_t s) {
-  using C = TC<HD, NQT>;
-  const size_t smem = sizeof(TreeSmem<HD, NQT>) + 1024;
-  static_assert(sizeof(TreeSmem<HD, NQT>) + 1024 <= (C::PER_SM == 2 ? 113 : 227) * 1024, "shared memory budget");
-  p.nqt = NQT;
+  using C = TC<HD>;
+  const size_t smem = sizeof(TreeSmem<HD>) + 1024;
+  static_assert(sizeof(TreeSmem<HD>) + 1024 <= (C::PER_SM == 2 ? 113 : 227) * 1024, "shared memory budget");
   p.ctas = device_sms() * C::PER_SM;
-  const int64_t qts = ceil_div(a.d.max_rows, NQT * p.per);
+  const int64_t qts = ceil_div(a.d.max_rows, p.per);
   const int64_t line = (int64_t)a.d.batch * a.n_kv * qts * (((int64_t)a.d.pos0 + a.d.max_rows + BKV - 1) / BKV);
   if (line > 0x3fffffff || a.n_kv * qts > 0x7fffffff) return POP_E_INVALID;          // places in the line are 32-bit numbers
   // two parts per CTA at most: of the item that it begins with and of the one that it ends with
-  const size_t need = (size_t)2 * p.ctas * NQT * 128 * (HD + 4) * 4;
+  const size_t parts = (size_t)2 * p.ctas * part_floats(HD), need = (parts + a.d.batch + 1) * 4;
+  p.starts = reinterpret_cast<int*>(p.partial + parts);
   if (a.workspace_bytes < need) return POP_E_NOSPACE;
   p.status = status_word();
   if (!p.status) return POP_E_CUDA;
   static std::atomic<uint64_t> configured{0};
-  if (!allow_smem(configured, reinterpret_cast<const void*>(tree_attn_kernel<HD, NQT>), (int)smem)) return POP_E_CUDA;
+  if (!allow_smem(configured, reinterpret_cast<const void*>(tree_attn_kernel<HD>), (int)smem)) return POP_E_CUDA;
   CUtensorMap tq, tk, tv;
   {
     // Q [rows][heads][hd]: a box is `per` rows of the G heads of a kv head; rows behind the last are zeros
@@ -714,12 +769,12 @@ int launch_t(const TreeAttnArgs& a, TreeDev& p, cudaStream_t s) {
       return POP_E_CUDA;
   }
   ProfScope prof(PROF_ATTENTION, 4.0 * HD * a.n_q * a.d.rows * ((double)a.d.pos0 + a.d.max_rows), s);
-  if (launch_chained(tree_attn_kernel<HD, NQT>, dim3(p.ctas), dim3(C::THREADS), smem, s, tq, tk, tv, p) != cudaSuccess)
+  if (launch_chained(tree_attn_kernel<HD>, dim3(p.ctas), dim3(C::THREADS), smem, s, tq, tk, tv, p) != cudaSuccess)
     return POP_E_CUDA;
   count_launch();
-  const int pairs = NQT == 1 && a.d.max_rows < p.per ? a.d.max_rows * p.G : NQT * p.per * p.G;
-  if (launch_chained(tree_merge_kernel<HD>, dim3((unsigned)(a.n_kv * qts), ceil_div(pairs, 8), a.d.batch), dim3(256), 0, s, p) !=
-      cudaSuccess)
+  const int pairs = a.d.max_rows < p.per ? a.d.max_rows * p.G : p.per * p.G;
+  if (launch_chained(tree_merge_kernel<HD>, dim3((unsigned)(a.n_kv * qts), HD / MERGE_COLS, a.d.batch), dim3((pairs + 31) & ~31), 0, s,
+                     p) != cudaSuccess)
     return POP_E_CUDA;
   count_launch();
   return POP_OK;
@@ -751,12 +806,10 @@ int launch_tree_attention(const TreeAttnArgs& a, cudaStream_t s) {
   p.rows_per_load = a.c.page_size < BKV ? a.c.page_size : BKV;
   p.scale_log2 = 1.4426950408889634f / sqrtf((float)a.head_dim);
   p.partial = static_cast<float*>(a.workspace);
-  // two tiles share the keys where no tile of 128 pairs holds all rows of a sequence
-  const bool one = a.d.max_rows <= p.per;
   switch (a.head_dim) {
-    case 64: return one ? launch_t<64, 1>(a, p, s) : launch_t<64, 2>(a, p, s);
-    case 128: return one ? launch_t<128, 1>(a, p, s) : launch_t<128, 2>(a, p, s);
-    default: return launch_t<256, 1>(a, p, s);
+    case 64: return launch_t<64>(a, p, s);
+    case 128: return launch_t<128>(a, p, s);
+    default: return launch_t<256>(a, p, s);
   }
 }
 
