@@ -121,6 +121,9 @@ int make_tmap_u8_rows(CUtensorMap* out, const void* base, uint64_t row_bytes, ui
                       uint32_t box_rows);
 int make_tmap_f32_3d(CUtensorMap* out, const void* base, uint64_t dim0, uint64_t dim1, uint64_t dim2,
                      uint64_t stride1_elems, uint64_t stride2_elems, uint32_t box1);
+// contiguous words [dim2][dim1][words], words <= 256, no swizzle, box = [box2][box1][words]: tiles of 4-bit weights
+int make_tmap_u32_tiles(CUtensorMap* out, const void* base, uint32_t words, uint64_t dim1, uint64_t dim2, uint32_t box1,
+                        uint32_t box2);
 // rank-`rank` (3..5) bf16 tensor, dims/strides/box given innermost first (strides in elements, for
 // dims 1..rank-1), 128-byte swizzle. Used for Q and for the paged KV pools [page][slot][head][hd].
 int make_tmap_bf16_nd(CUtensorMap* out, const void* base, int rank, const uint64_t dims[5],

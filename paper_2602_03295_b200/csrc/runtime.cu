@@ -167,6 +167,20 @@ int make_tmap_f32_3d(CUtensorMap* out, const void* base, uint64_t dim0, uint64_t
   return r == CUDA_SUCCESS ? POP_OK : POP_E_CUDA;
 }
 
+int make_tmap_u32_tiles(CUtensorMap* out, const void* base, uint32_t words, uint64_t dim1, uint64_t dim2, uint32_t box1,
+                        uint32_t box2) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return POP_E_CUDA;
+  cuuint64_t dims[3] = {words, dim1, dim2};
+  cuuint64_t strides[2] = {(cuuint64_t)words * 4, (cuuint64_t)words * 4 * dim1};
+  cuuint32_t box[3] = {words, box1, box2};
+  cuuint32_t estr[3] = {1, 1, 1};
+  CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, const_cast<void*>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? POP_OK : POP_E_CUDA;
+}
+
 int make_tmap_bf16_nd(CUtensorMap* out, const void* base, int rank, const uint64_t dims[5],
                       const uint64_t strides_elems[4], const uint32_t box[5]) {
   EncodeTiledFn fn = encode_fn();

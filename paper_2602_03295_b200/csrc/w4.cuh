@@ -2,6 +2,8 @@
 #pragma once
 #include "common.cuh"
 
+#include <cuda_fp16.h>
+
 namespace pop {
 
 struct Gemv4Args {
@@ -16,6 +18,58 @@ struct Gemv4Args {
 };
 size_t gemv4_workspace_bytes(int B, int K, int group);
 int launch_gemv4(const Gemv4Args& a, cudaStream_t s);
+// Slabs of rows in which the activations are converted
+constexpr int cols_of(int B) { return B <= 8 ? 8 : B <= 16 ? 16 : B <= 32 ? 32 : 64; }
+__host__ __device__ constexpr int64_t slab_bytes(int cols, int gpc, int64_t kt) { return kt * cols * (256 + 4 * (1 + gpc)); }
+// chunks of 128 inputs that a slab has room for: with more than 8 rows they come in pairs
+constexpr int64_t slab_chunks(int cols, int64_t kt) { return cols == 8 ? kt : (kt + 1) / 2 * 2; }
+// the products from 9 rows on, with the activations converted
+int launch_gemm4(const Gemv4Args& a, const uint8_t* xq, cudaStream_t s);
 int device_sms();                                      // SMs of the device that was current at the first call
+
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+               "r"(bytes), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 h = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ float act_of(float g, int act) {
+  if (act == 0) return g / (1.0f + expf(-g));
+  return 0.5f * g * (1.0f + tanhf(0.7978845608028654f * (g + 0.044715f * g * g * g)));
+}
+
+// What a lane of a half-warp makes of its 8 of a chunk's 128 activations: f16 values times a common power of two, those that
+// meet codes of bits 4 .. 7 divided by 16; `unit` takes them back, `sum` is that of the lane's group.
+template <int GRP>
+__device__ __forceinline__ uint4 convert8(const uint4& v, float& sum, float& unit) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t m = 0;
+  float x[8];
+  sum = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    m = max(m, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
+    x[2 * j] = __uint_as_float(w[j] << 16);
+    x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    sum += x[2 * j] + x[2 * j + 1];
+  }
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll
+  for (int o = 1; o < GRP / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  // a power of two that brings the largest to 2^14 .. 2^15, as far as fp32 has it (an infinity or NaN stays what it is, beside
+  // values that no longer matter)
+  const int sh = m == 0 ? 0 : min(14 + 127 - (int)(m >> 7), 126);
+  const float f = __uint_as_float((uint32_t)(127 + sh) << 23), f16th = f * 0.0625f;
+  unit = __uint_as_float((uint32_t)(127 - sh) << 23);
+  return make_uint4(pack_f16(x[0] * f, x[1] * f), pack_f16(x[2] * f16th, x[3] * f16th), pack_f16(x[4] * f, x[5] * f),
+                    pack_f16(x[6] * f16th, x[7] * f16th));
+}
+// Sums of groups in the unit of code products (2^-24), without zeros times the 8 that stands for them
+__host__ __device__ constexpr float sum_scale(bool zeros) { return (zeros ? 1.f : 8.f) * 0x1p-24f; }
+
 
 }  // namespace pop
