@@ -195,9 +195,18 @@ struct Walk {
   }
   // to the next tile; true where another segment begins there
   __device__ __forceinline__ bool next(const TreeDev& p) {
-    ++pos;
-    --left;
-    if (++j < j_end) return false;
+    if (j + 1 < j_end) {
+      ++pos;
+      --left;
+      ++j;
+      return false;
+    }
+    return segment(p);
+  }
+  // to the next segment
+  __device__ __forceinline__ bool segment(const TreeDev& p) {
+    pos += j_end - j;
+    left -= j_end - j;
     if (pos >= hi) return true;
     if (left == 0) {
       do {
@@ -225,34 +234,50 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
 }
-__device__ __forceinline__ uint32_t ones(int n) { return n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1; }
+__device__ __forceinline__ uint64_t ones(int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1; }
 __device__ __forceinline__ bool gave_up(int status) { return status <= (int)POP_E_DEVICE_TIMEOUT; }
 
-// Which of the 32 positions from kv0 on row i (packed row `row`) of the sequence sees
-__device__ __forceinline__ uint32_t seen_of(const TreeDev& p, const Seq& x, int i, int64_t row, int depth, int kv0) {
+// The first words of a row's mask, asked for where its segment begins: a tile of the draft comes long after
+struct Words {
+  uint32_t w[4];
+};
+
+// Which of the 64 positions from kv0 on row i (packed row `row`) of the sequence sees. One body, not unrolled by halves: its
+// instructions are met cold, and a launch waits for the CTAs that have the drafts.
+__device__ __forceinline__ uint64_t seen_of(const TreeDev& p, const Seq& x, int i, int64_t row, const Words& first, int depth, int kv0) {
   const int ctx = x.start - kv0;                               // positions of these in front of the draft
   const int window = p.a.window;
-  uint32_t vis = ~0u;
-  if (ctx < 32) {
+  uint64_t vis = ~0ull;
+  if (ctx < 64) {
     if (p.a.mask == nullptr) {
       vis = ones(ctx + i + 1);
     } else {
-      const uint32_t* m = p.a.mask + row * p.a.mask_words;
       const int slot0 = ctx < 0 ? -ctx : 0, w = slot0 >> 5;
-      auto word = [&](int k) { return k < p.a.mask_words ? __ldg(m + k) : 0u; };
-      const uint32_t drafted = __funnelshift_r(word(w), word(w + 1), slot0 & 31);
-      vis = ctx > 0 ? (drafted << ctx) | ones(ctx) : drafted;
+      uint32_t a = first.w[0], b = first.w[1], c = first.w[2];
+      if (w == 1) {
+        a = b;
+        b = c;
+        c = first.w[3];
+      } else if (w > 1) {
+        const uint32_t* m = p.a.mask + row * p.a.mask_words;
+        auto word = [&](int k) { return k < p.a.mask_words ? __ldg(m + k) : 0u; };
+        a = word(w);
+        b = word(w + 1);
+        c = word(w + 2);
+      }
+      vis = ((uint64_t)__funnelshift_r(b, c, slot0 & 31) << 32) | __funnelshift_r(a, b, slot0 & 31);
+      if (ctx > 0) vis = (vis << ctx) | ones(ctx);
     }
     vis &= ones(ctx + x.n);
   }
   if (window > 0) {
     const int hidden = x.start + depth - window + 1 - kv0;     // positions in front of the window
     if (hidden > 0) vis &= ~ones(min(hidden, ctx));
-    if (ctx < 32 && depth >= window) {                         // drafted slots that lie so far up the tree
-      for (uint32_t m = vis & ~ones(ctx); m != 0; m &= m - 1) {
-        const int k = __ffs((int)m) - 1, slot = k - ctx;
+    if (ctx < 64 && depth >= window) {                         // drafted slots that lie so far up the tree
+      for (uint64_t m = vis & ~ones(ctx); m != 0; m &= m - 1) {
+        const int k = __ffsll((long long)m) - 1, slot = k - ctx;
         const int d = p.a.d.depth ? __ldg(p.a.d.depth + x.row0 + slot) : slot;
-        if (d <= depth - window) vis &= ~(1u << k);
+        if (d <= depth - window) vis &= ~(1ull << k);
       }
     }
   }
@@ -491,10 +516,28 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       const int depth = !used || p.a.window == 0 ? 0 : p.a.d.depth ? min(max(__ldg(p.a.d.depth + prow), 0), 0xffff) : i;
       const int win_lo = p.a.window > 0 ? x.start - p.a.window + 1 : 0;      // in front of every row's window
       const int len = x.start + x.n;
+      Words first = {{0, 0, 0, 0}};
+      if (used && p.a.mask != nullptr && w.j_end * BKV > x.start) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (k < p.a.mask_words) first.w[k] = __ldg(p.a.mask + prow * p.a.mask_words + k);
+      }
       float m_run = -INFINITY, l_run = 0.f;
-      for (int jj = 0; jj < nt && !s.abort; ++jj, ++f) {
+      for (int jj = 0; jj < nt; ++jj, ++f) {
         const int kv0 = (j0 + jj) * BKV;
         const uint32_t sp_addr = s_addr + (f & 1) * BKV;
+        uint32_t vis[KEYS / 32];
+#pragma unroll
+        for (int c = 0; c < KEYS / 32; ++c) vis[c] = used ? ~0u : 0u;
+        if (used && (kv0 + BKV > x.start || (p.a.window > 0 && kv0 + p.a.window <= x.start + depth))) {
+          const uint64_t v = seen_of(p, x, i, prow, first, depth, kv0);
+          if constexpr (HALVES == 2) {
+            vis[0] = half ? (uint32_t)(v >> 32) : (uint32_t)v;
+          } else {
+            vis[0] = (uint32_t)v;
+            vis[KEYS / 32 - 1] = (uint32_t)(v >> 32);
+          }
+        }
         if (!mbar_wait(&s.s_full[f & 1], (f >> 1) & 1)) { ok = false; break; }
         if (!idle) {
           tc_fence_after();
@@ -502,13 +545,6 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 #pragma unroll
           for (int c = 0; c < KEYS / 32; ++c)
             tmem_ld_32x32b_x32(sp_addr + half * KEYS + c * 32, *reinterpret_cast<uint32_t(*)[32]>(&sv[c * 32]));
-          uint32_t vis[KEYS / 32];
-#pragma unroll
-          for (int c = 0; c < KEYS / 32; ++c) vis[c] = used ? ~0u : 0u;
-          if (kv0 + BKV > x.start || (p.a.window > 0 && kv0 + p.a.window <= x.start + depth)) {
-#pragma unroll
-            for (int c = 0; c < KEYS / 32; ++c) vis[c] = used ? seen_of(p, x, i, prow, depth, kv0 + half * KEYS + c * 32) : 0u;
-          }
           tmem_wait_ld();
           if ((vis[0] & vis[KEYS / 32 - 1]) != ~0u) {
 #pragma unroll
@@ -581,10 +617,11 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           const int rv = min(f + 2, n_tiles) + f;
           if (!mbar_wait(&s.kv_full[rv % STAGES], (rv / STAGES) & 1)) { ok = false; break; }
           if (kv0 + row >= len || kv0 + row < win_lo) {
+#pragma unroll 1
             for (int c = 0; c < HD / 64; ++c) {
               uint4* dst = reinterpret_cast<uint4*>(s.kv[rv % STAGES] + c * C::KV_SUB_BYTES + row * 128);
 #pragma unroll
-              for (int q = 0; q < 8; ++q) dst[q] = make_uint4(0, 0, 0, 0);
+              for (int q = 0; q < 8; ++q) dst[q ^ (row & 7)] = make_uint4(0, 0, 0, 0);       // neighbours in other banks
             }
           }
           fence_proxy_async_smem();
@@ -592,7 +629,6 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.p_ready[f & 1]);
-        w.next(p);
       }
       if (!ok || s.abort) break;
       if (!wait_pv(f - 1)) { ok = false; break; }
@@ -641,6 +677,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           }
         }
       }
+      w.segment(p);
       // the next item's first product overwrites O: it waits for P of all warps, which they write after this
     }
     if (!ok) TREE_ABORT(s, p.status);
