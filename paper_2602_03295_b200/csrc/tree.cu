@@ -7,23 +7,24 @@ namespace pop {
 namespace {
 
 // ------------------------------------------------------------------------------ norm + rotation + append
-// hd / 8 lanes per (row, head), each with four rotation pairs; a CTA has consecutive heads of a row, so that the row's
-// rotary entries come from L1 after the first. Every value is read and written once: bound by the bytes, and for few rows by
-// the chain of loads (prefix sums and start, then page, depth and row, then the rotary entries).
+// hd / 8 lanes per row and HPG consecutive heads, each with four rotation pairs: place, position, page and rotary entries are
+// found once for the heads, whose rows are all asked for before the first is used. Every value is read and written once: bound
+// by the bytes, and for few rows by the chain of loads (prefix sums and start, then page, depth and rows, then the rotary
+// entries).
 struct TreeAppendDev {
   TreeAppendArgs a;
   int* status;
 };
 
-template <int HD, bool IN_BF16>
+template <int HD, bool IN_BF16, int HPG>
 __global__ void __launch_bounds__(256) tree_append_kernel(const __grid_constant__ TreeAppendDev p) {
   constexpr int LPR = HD / 8, HALF = HD / 2;
   const TreeAppendArgs& a = p.a;
   chain_trigger();
   const int lane = threadIdx.x & 31, j0 = (lane % LPR) * 4, b = blockIdx.y;
-  const int heads = a.n_q + 2 * a.n_kv;
-  const int64_t item = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
-  const int i = (int)(item / heads), h = (int)(item - (int64_t)i * heads);
+  const uint32_t heads = a.n_q + 2 * a.n_kv, groups = (heads + HPG - 1) / HPG;
+  const uint32_t item = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;             // below 2^29
+  const int i = item / groups, h0 = (item - i * groups) * HPG;
   chain_wait();
   const int row0 = a.d.cu ? __ldg(a.d.cu + b) : b * a.d.max_rows;
   const int n = a.d.cu ? __ldg(a.d.cu + b + 1) - row0 : a.d.max_rows;
@@ -33,23 +34,20 @@ __global__ void __launch_bounds__(256) tree_append_kernel(const __grid_constant_
     if (threadIdx.x == 0) atomicMin(p.status, (int)POP_E_INVALID);
     return;
   }
-  if ((int64_t)blockIdx.x * (256 / LPR) >= (int64_t)n * heads) return;
-  // The lanes behind the last item work on the last one and store nothing: the warp stays whole for the norm's shuffles
+  if (blockIdx.x * (256 / LPR) >= n * groups) return;
+  // The lanes behind the last item work on the last row and store nothing: the warp stays whole for the norm's shuffles
   const bool idle = i >= n;
-  const int ii = idle ? n - 1 : i, hh = idle ? heads - 1 : h;
-  const bool is_q = hh < a.n_q, is_v = hh >= a.n_q + a.n_kv;
+  const int ii = idle ? n - 1 : i;
   const int64_t row = row0 + ii;
-  const int slot = start + ii;
+  const uint32_t slot = start + ii, page_at = slot / (uint32_t)a.dst.page_size, in_page = slot - page_at * a.dst.page_size;
   bool bad = false;
   int page = -1;
-  if (!is_q && slot / a.dst.page_size < a.dst.max_pages)
-    page = __ldg(a.dst.table + (int64_t)b * a.dst.max_pages + slot / a.dst.page_size);
-  float x[8];
-  load_row8<HD, IN_BF16>(a.in, row * a.ld_in + (int64_t)hh * HD + j0, x);
-  float2 cs[4];
+  if (h0 + HPG > a.n_q && page_at < (uint32_t)a.dst.max_pages) page = __ldg(a.dst.table + (int64_t)b * a.dst.max_pages + page_at);
+  float x[HPG][8];
 #pragma unroll
-  for (int u = 0; u < 4; ++u) cs[u] = make_float2(1.f, 0.f);
-  if (!is_v) {
+  for (int u = 0; u < HPG; ++u) load_row8<HD, IN_BF16>(a.in, row * a.ld_in + (int64_t)min(h0 + u, (int)heads - 1) * HD + j0, x[u]);
+  float2 cs[4];
+  if (h0 < a.n_q + a.n_kv) {
     int64_t at = (int64_t)start + (a.d.depth ? __ldg(a.d.depth + row) : ii);
     if (at < 0 || at >= a.table_rows) {                                           // never turned into an address
       bad = true;
@@ -61,33 +59,49 @@ __global__ void __launch_bounds__(256) tree_append_kernel(const __grid_constant_
     cs[2] = make_float2(t1.x, t1.y); cs[3] = make_float2(t1.z, t1.w);
   }
   if (a.q_gain != nullptr || a.k_gain != nullptr) {                               // by all lanes: heads of a warp may differ
-    const float* gain = is_q ? a.q_gain : is_v ? nullptr : a.k_gain;
-    float4 g0 = make_float4(1.f, 1.f, 1.f, 1.f), g1 = g0;
-    if (gain != nullptr) {
-      g0 = make_float4(__ldg(gain + j0), __ldg(gain + j0 + 1), __ldg(gain + j0 + 2), __ldg(gain + j0 + 3));
-      g1 = make_float4(__ldg(gain + j0 + HALF), __ldg(gain + j0 + HALF + 1), __ldg(gain + j0 + HALF + 2), __ldg(gain + j0 + HALF + 3));
-    }
-    float y[8];
+    const float* have = nullptr;
+    float4 g0, g1;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) y[u] = x[u];
-    norm_row8<HD>(y, g0, g1, a.eps);
-    if (gain != nullptr) {
+    for (int u = 0; u < HPG; ++u) {
+      const int h = h0 + u;
+      const float* gain = h < a.n_q ? a.q_gain : h < a.n_q + a.n_kv ? a.k_gain : nullptr;
+      if (gain != nullptr && gain != have) {
+        if (reinterpret_cast<uintptr_t>(gain) % 16 == 0) {
+          g0 = __ldg(reinterpret_cast<const float4*>(gain + j0));
+          g1 = __ldg(reinterpret_cast<const float4*>(gain + j0 + HALF));
+        } else {
+          g0 = make_float4(__ldg(gain + j0), __ldg(gain + j0 + 1), __ldg(gain + j0 + 2), __ldg(gain + j0 + 3));
+          g1 = make_float4(__ldg(gain + j0 + HALF), __ldg(gain + j0 + HALF + 1), __ldg(gain + j0 + HALF + 2), __ldg(gain + j0 + HALF + 3));
+        }
+        have = gain;
+      }
+      float y[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = y[u];
+      for (int v = 0; v < 8; ++v) y[v] = x[u][v];
+      norm_row8<HD>(y, g0, g1, a.eps);
+      if (gain != nullptr) {
+#pragma unroll
+        for (int v = 0; v < 8; ++v) x[u][v] = y[v];
+      }
     }
   }
-  if (!is_v) turn_row8(x, cs);
-  if (!idle) {
-    if (is_q) {
-      store_q8<HD>(a.q_out + row * a.ldq + (int64_t)hh * HD + j0, x);
+  if (idle) return;
+#pragma unroll
+  for (int u = 0; u < HPG; ++u) {
+    const int h = h0 + u;
+    if (h >= (int)heads) break;
+    if (h < a.n_q + a.n_kv) turn_row8(x[u], cs);
+    if (h < a.n_q) {
+      store_q8<HD>(a.q_out + row * a.ldq + (int64_t)h * HD + j0, x[u]);
     } else if ((unsigned)page < (unsigned)a.dst.num_pages) {                      // else never turned into an address
-      const int head = hh - a.n_q - (is_v ? a.n_kv : 0);
-      store_q8<HD>((is_v ? a.dst.v : a.dst.k) + (((int64_t)page * a.dst.page_size + slot % a.dst.page_size) * a.n_kv + head) * HD + j0, x);
+      const bool is_v = h >= a.n_q + a.n_kv;
+      const int head = h - a.n_q - (is_v ? a.n_kv : 0);
+      store_q8<HD>((is_v ? a.dst.v : a.dst.k) + (((int64_t)page * a.dst.page_size + in_page) * a.n_kv + head) * HD + j0, x[u]);
     } else {
       bad = true;
     }
-    if (bad) atomicMin(p.status, (int)POP_E_INVALID);
   }
+  if (bad) atomicMin(p.status, (int)POP_E_INVALID);
 }
 
 // ------------------------------------------------------------------------------ the accepted path
@@ -154,6 +168,12 @@ __global__ void __launch_bounds__(KEEP_THREADS) cache_keep_kernel(const __grid_c
   }
 }
 
+template <int HD>
+auto kernel_of(bool in_bf16, bool four) {
+  return in_bf16 ? (four ? tree_append_kernel<HD, true, 4> : tree_append_kernel<HD, true, 1>)
+                 : (four ? tree_append_kernel<HD, false, 4> : tree_append_kernel<HD, false, 1>);
+}
+
 }  // namespace
 
 int launch_tree_append(const TreeAppendArgs& a, cudaStream_t s) {
@@ -173,14 +193,19 @@ int launch_tree_append(const TreeAppendArgs& a, cudaStream_t s) {
   p.a = a;
   p.status = status_word();
   if (!p.status) return POP_E_CUDA;
+  // Four heads at a time where there are more blocks of one than the SMs hold, else one. us for one / four: 48 x up to 33 rows of
+  // 48 heads, normalised 10.3 / 8.8, 16 x up to 64 rows of 32 heads of 256 8.7 / 7.1; 24 x up to 20 rows of 48 heads 3.9 / 4.2,
+  // 8 rows of 48 heads 1.7 / 2.2
   const int heads = a.n_q + 2 * a.n_kv, per = 2048 / a.head_dim;
-  const dim3 grid((unsigned)(((int64_t)a.d.max_rows * heads + per - 1) / per), a.d.batch);
+  const bool four = (int64_t)a.d.rows * heads >= (int64_t)device_sms() * 8 * per;
+  const int groups = four ? ceil_div(heads, 4) : heads;
+  const dim3 grid(ceil_div(a.d.max_rows * groups, per), a.d.batch);
   ProfScope prof(PROF_ELEMENTWISE, (double)a.d.rows * a.head_dim * heads * ((a.in_bf16 ? 2.0 : 4.0) + 2.0), s);
   void (*kernel)(TreeAppendDev);
   switch (a.head_dim) {
-    case 64: kernel = a.in_bf16 ? tree_append_kernel<64, true> : tree_append_kernel<64, false>; break;
-    case 128: kernel = a.in_bf16 ? tree_append_kernel<128, true> : tree_append_kernel<128, false>; break;
-    default: kernel = a.in_bf16 ? tree_append_kernel<256, true> : tree_append_kernel<256, false>; break;
+    case 64: kernel = kernel_of<64>(a.in_bf16, four); break;
+    case 128: kernel = kernel_of<128>(a.in_bf16, four); break;
+    default: kernel = kernel_of<256>(a.in_bf16, four); break;
   }
   if (launch_chained(kernel, grid, dim3(256), 0, s, p) != cudaSuccess) return POP_E_CUDA;
   count_launch();
