@@ -295,7 +295,8 @@ int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int
  * (N a multiple of 256: 128 gate rows, then the 128 matching up rows; act 0 SiLU, 1 tanh-GELU). The products of
  * codes and activations are exact (of activations within 2^-27 of the largest of their 128 inputs; smaller ones are off by at
  * most 2^-36 of it); sums are fp32, in an order that depends on the sizes alone. An activation row with an infinite or NaN
- * input gives a row of NaN. */
+ * input gives a row of NaN. Weights are read ahead, before the kernel in front of the call on the stream has ended (as
+ * pop_k_gemv reads its own): whoever writes them on the GPU synchronises before the first call that uses them. */
 int pop_k_gemv_w4(const void* x, int64_t ldx, const void* codes, const void* scales, const void* zeros, int32_t group,
                   void* workspace, size_t workspace_bytes, void* out, int64_t ldo, int32_t B, int32_t N, int32_t K,
                   int32_t mode, int32_t act, int32_t n_valid, void* stream);

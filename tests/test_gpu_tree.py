@@ -68,6 +68,9 @@ GEMV = [  # B, N, K, group, zeros
     (64, 272, 768, 32, True), (65, 16, 40, 64, False), (130, 31, 128, 128, False), (1, 4096, 4096, 128, False),
     (5, 4096, 14336, 64, True), (24, 6000, 4096, 128, False), (1, 40, 40000, 128, True), (1, 9000, 96, 32, True),
     (2, 2400, 8192, 64, True), (300, 144, 640, 128, True),
+    # long and wide ones of more rows than a warp-level product takes, and their ends
+    (9, 4000, 14336, 128, True), (12, 16, 40000, 32, True), (48, 20000, 520, 64, False), (20, 129, 8, 32, True), (32, 256, 264, 32, False),
+    (16, 1000, 4096, 32, True), (64, 128, 2176, 128, False),
 ]
 
 
@@ -109,7 +112,8 @@ def test_gemv_w4_is_exact_where_fp32_is(L, B, N, K, group, zeros):
 
 @pytest.mark.parametrize("B,F,K,group,zeros,act,n_valid", [
     (1, 128, 64, 32, True, 0, 128), (1, 688, 256, 64, False, 0, 688), (6, 256, 1032, 128, True, 1, 200), (13, 384, 512, 32, False, 1, 384),
-    (40, 512, 768, 128, True, 0, 500), (1, 14336, 4096, 128, False, 0, 14336), (70, 128, 136, 64, True, 0, 127)])
+    (40, 512, 768, 128, True, 0, 500), (1, 14336, 4096, 128, False, 0, 14336), (70, 128, 136, 64, True, 0, 127),
+    (9, 896, 4096, 32, True, 0, 890), (17, 20000, 256, 128, False, 1, 20000), (64, 300, 1000, 64, False, 0, 300)])
 def test_gemv_w4_gated(L, B, F, K, group, zeros, act, n_valid):
     N = -(-F // 128) * 256
     g = gen(F + K + B)
@@ -122,6 +126,64 @@ def test_gemv_w4_gated(L, B, F, K, group, zeros, act, n_valid):
     L.gemv_w4(x.cuda(), *laid_out(L, codes, scales, z, group), out, N, group, mode=3, act=act, n_valid=n_valid)
     within(out[:, :n_valid], want[:, :n_valid], bound[:, :n_valid])
     assert (out[:, n_valid:] == 7).all()
+
+
+@pytest.mark.parametrize("B", [1, 2, 5, 8, 9, 30, 64])
+def test_gemv_w4_of_all_magnitudes(L, B):
+    """Rows from 2^-90 to 2^90, inputs within a chunk up to 2^20 apart. Those below 2^-27 of a chunk's largest are off by 2^-36 of it."""
+    g = gen(B)
+    N, K, group = 100, 1152, 64
+    plain = weights(N, K, group, True, g)
+    x = torch.randn(B, K, generator=g) * torch.exp2(torch.randint(-20, 1, (B, K), generator=g).float())
+    x = (x * torch.exp2(torch.linspace(-90, 90, B)[:, None].round())).to(torch.bfloat16)
+    want = x.double() @ ref.w4_values(*plain, group).t()
+    # the sums of code x and zero x are rounded apart: magnitudes of 15 + 15 steps for each weight
+    steps = plain[1].double().abs().repeat_interleave(group, 1)[:, :K] * 30
+    out = torch.empty(B, N, device=DEV)
+    L.gemv_w4(x.cuda(), *laid_out(L, *plain, group), out, N, group)
+    within(out, want, ref.gemv(x, steps, group)[1])
+
+
+def test_gemv_w4_of_more_than_2_to_the_32_weights(L):
+    g = gen(1)
+    N, K, last = (1 << 19) + 40, 8448, 200
+    gd = torch.Generator(device=DEV).manual_seed(1)
+    nt, kt = -(-N // 16), K // 128
+    codes = torch.randint(0, 256, (nt, kt, 16, 64), generator=gd, device=DEV, dtype=torch.uint8)
+    scales = (torch.rand(nt, kt, 16, 1, generator=gd, device=DEV) * 0.02 + 0.01).to(torch.bfloat16)
+    assert codes.numel() > 1 << 31
+    from paper_2602_03295_b200 import unpack_w4
+    tail = -(-last // 16)
+    w = unpack_w4(codes[-tail:].contiguous(), scales[-tail:].contiguous(), None, N - (nt - tail) * 16, K).double().cpu()
+    for B in (1, 12):
+        x = torch.randn(B, K, generator=g).to(torch.bfloat16)
+        out = torch.empty(B, N, device=DEV)
+        L.gemv_w4(x.cuda(), codes, scales, None, out, N, 128)
+        want, bound = ref.gemv(x, w, 128)
+        within(out[:, -w.shape[0]:], want, bound)
+
+
+def test_gemv_w4_workspaces_of_two_streams(L):
+    """Calls on two streams at once, each with a workspace of its own, and with those that the binding takes."""
+    g = gen(6)
+    plain = weights(640, 2048, 128, False, g)
+    tiles = laid_out(L, *plain, 128)
+    xs = [torch.randn(24, 2048, generator=g).to(torch.bfloat16).cuda() for _ in range(2)]
+    want = [torch.empty(24, 640, device=DEV) for _ in range(2)]
+    for x, o in zip(xs, want):
+        L.gemv_w4(x, *tiles, o, 640, 128)
+    torch.cuda.synchronize()
+    need = L.dll.pop_k_gemv_w4_workspace_bytes(24, 2048, 128)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for given in (True, False):
+        got = [torch.zeros(24, 640, device=DEV) for _ in range(2)]
+        ws = [torch.full((need,), 255, dtype=torch.uint8, device=DEV) if given else None for _ in range(2)]
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for x, o, w, st in zip(xs, got, ws, streams):
+                L.gemv_w4(x, *tiles, o, 640, 128, workspace=w, stream=st)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 def test_gemv_w4_rows_do_not_meet(L):
@@ -189,7 +251,10 @@ APPEND = [  # rows, starts, n_q, n_kv, hd, page, bf16, norm, tree
     ([1], [0], 1, 1, 64, 16, False, False, True), ([5], [300], 4, 2, 64, 16, False, True, False),
     ([8], [1000], 32, 8, 128, 128, False, False, True), ([3, 0, 33, 1], [17, 5, 0, 126], 6, 3, 128, 32, True, True, True),
     ([12, 40], [63, 500], 8, 8, 256, 64, True, False, True), ([7] * 9, list(range(0, 90, 10)), 5, 1, 64, 256, False, True, True),
-    ([130], [64], 2, 2, 256, 128, False, True, True), ([4, 2], [9, 10], 0, 2, 128, 16, False, True, True)]
+    ([130], [64], 2, 2, 256, 128, False, True, True), ([4, 2], [9, 10], 0, 2, 128, 16, False, True, True),
+    # so many that a group of lanes has four heads of a row, of one kind or of several
+    ([33] * 44 + [0, 20], list(range(46)), 7, 3, 128, 64, True, True, True), ([40] * 60, [5] * 60, 10, 3, 64, 32, False, False, False),
+    ([20] * 50, list(range(50)), 6, 2, 256, 16, False, True, True), ([25] * 100, [1] * 100, 0, 4, 128, 64, True, True, False)]
 
 
 @pytest.mark.parametrize("rows,starts,n_q,n_kv,hd,page,bf16,norm,tree", APPEND)
@@ -227,6 +292,47 @@ def test_append_of_a_tree(L, rows, starts, n_q, n_kv, hd, page, bf16, norm, tree
     if n_q:
         assert (q_out[:, n_q * hd:] == 7).all()
     assert torch.equal(kd.cpu()[~touched], k[~touched]) and torch.equal(vd.cpu()[~touched], v[~touched])
+
+
+def test_append_with_gains_anywhere(L):
+    g = gen(8)
+    n_q, n_kv, hd = 6, 2, 128
+    rope, table = rope_rows(64, hd).cuda(), torch.arange(4, dtype=torch.int32, device=DEV)[None]
+    for rows in (3, 50):
+        x, outs = torch.randn(rows, (n_q + 2 * n_kv) * hd, generator=g).cuda(), []
+        gain = 0.5 + torch.rand(hd, generator=g)
+        for shift in (0, 1, 2, 3):
+            at = torch.zeros(hd + 4, device=DEV)
+            at[shift:shift + hd] = gain.cuda()
+            k, v = (torch.zeros(4, 16, n_kv, hd, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+            q = torch.empty(rows, n_q * hd, dtype=torch.bfloat16, device=DEV)
+            L.rope_cache_tree(x, q, k, v, table, rope, n_q, n_kv, hd, rows, pos0=2, q_gain=at[shift:shift + hd], k_gain=at[shift:shift + hd], eps=1e-5)
+            outs.append((q, k, v))
+        assert all(torch.equal(a, b) for o in outs[1:] for a, b in zip(o, outs[0]))
+
+
+def test_pools_beyond_32_bits(L):
+    """Append, attention and keeping in pages whose bytes and entries lie beyond 2^32 give what they give in the first pages."""
+    n_q, n_kv, hd, page, n, start = 16, 8, 128, 128, 12, 250
+    g = gen(21)
+    pages = (1 << 32) // (page * n_kv * hd) + 8                     # entries, not only bytes
+    big = [torch.empty(1, pages, page, n_kv, hd, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    small = [torch.zeros(1, 8, page, n_kv, hd, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    low = torch.tensor([[2, 0, 5]], dtype=torch.int32, device=DEV)
+    high = torch.tensor([[pages - 1, pages - 4, pages - 7]], dtype=torch.int32, device=DEV)
+    for i in range(2):
+        small[i][0, low[0].long()] = torch.randn(3, page, n_kv, hd, generator=g).to(torch.bfloat16).cuda()
+        for a, b in zip(high[0].tolist(), low[0].tolist()):
+            big[i][0, a] = small[i][0, b]
+    x, rope = torch.randn(n, (n_q + 2 * n_kv) * hd, generator=g).cuda(), rope_rows(400, hd).cuda()
+    res = []
+    for (k, v), table in ((small, low), (big, high)):
+        q, out = (torch.empty(n, n_q * hd, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        L.rope_cache_tree(x, q, k[0], v[0], table, rope, n_q, n_kv, hd, n, pos0=start)
+        L.tree_attention(q, k[0], v[0], table, out, n_q, n_kv, hd, n, start)
+        L.cache_keep(k, v, table, torch.tensor([[1, 3, 4, 10]], dtype=torch.int32, device=DEV), pos0=start)
+        res.append([q, out] + [p[0, t] for p in (k, v) for t in table[0].tolist()])
+    assert all(torch.equal(a, b) for a, b in zip(*res))
 
 
 ATTEND = [  # rows, starts, n_q, n_kv, hd, page, window, kind
