@@ -461,12 +461,12 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       stage = ring % STAGES;
       const uint32_t phase = (ring / STAGES) & 1;
       ++ring;
-      return mbar_wait_relaxed(&s.kv_full[stage], phase);
+      return mbar_wait(&s.kv_full[stage], phase);
     };
     // Scores of the next tile into the buffer that the tile two in front of it has left: its product is issued, and the
     // tensor pipe runs in order. The first wait of an item is for its queries.
     auto scores = [&] {
-      if (s_fresh) ok = mbar_wait_relaxed(&s.q_full, items++ & 1);
+      if (s_fresh) ok = mbar_wait(&s.q_full, items++ & 1);
       int stage = 0;
       if (ok) ok = wait_tile(stage);
       if (!ok) return;
@@ -482,7 +482,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     for (int f = 0; f < n_tiles && ok && !s.abort; ++f) {
       int stage = 0;
       ok = wait_tile(stage);
-      if (ok) ok = mbar_wait_relaxed(&s.p_ready[f & 1], (f >> 1) & 1);
+      if (ok) ok = mbar_wait(&s.p_ready[f & 1], (f >> 1) & 1);
       if (!ok) break;
       tc_fence_after();
       issue_pv(f, stage, p_fresh);
