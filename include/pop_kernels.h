@@ -354,6 +354,11 @@ int pop_k_cache_keep(void* k_pool, void* v_pool, int64_t layer_stride, int32_t l
                      int64_t ld_kept, const int32_t* n_kept, int32_t max_kept, const int32_t* start, int32_t pos0,
                      int32_t batch, int32_t n_kv, int32_t head_dim, void* stream);
 
+/* The four calls above (call 0 pop_k_gemv_w4, 1 pop_k_rope_cache_tree, 2 pop_k_tree_attention, 3 pop_k_cache_keep) with their
+ * arguments as 64-bit words in their order: pointers, integers, and eps as the bits of a double. For callers whose foreign
+ * function interface converts argument by argument, which for these calls can cost as much as the launch. */
+int pop_k_packed(int32_t call, const int64_t* words);
+
 /* Synchronise the stream, then read and clear the library's device status word. */
 int pop_k_status(void* stream);
 

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -122,11 +123,26 @@ SIGNATURES = {
                                        C.c_size_t, _P, _I64] + [_I32] * 5 + [_P]),
     "pop_k_cache_keep": (C.c_int, [_P, _P, _I64, _I32, _P, _I32, _I32, _I32, _P, _I64, _P, _I32, _P, _I32, _I32, _I32, _I32,
                                    _P]),
+    "pop_k_packed": (C.c_int, [_I32, C.c_char_p]),
     "pop_k_status": (C.c_int, [_P]),
     "pop_k_wait_selftest": (C.c_int, [_I64, _P]),
     "pop_k_launch_count": (_I64, []),
     "pop_k_reset_launch_count": (None, []),
 }
+
+
+# pop_k_packed's words for calls 0 .. 3
+_PACK_GEMV, _PACK_APPEND, _PACK_ATTEND, _PACK_KEEP = (struct.Struct(f).pack for f in ("17q", "20qd6q", "26q", "18q"))
+_BF16, _FP32, _INT32, _UINT8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+
+
+def _vector(t, n, what):
+    """Address of an optional int32 device vector of n entries (0: none)."""
+    if t is None:
+        return 0
+    if t.dtype is not _INT32 or t.shape != (n,) or not t.is_contiguous():
+        raise PopError(POP_E_INVALID, f"{what}: contiguous int32 [{n}] is wanted")
+    return t.data_ptr()
 
 
 def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
@@ -577,26 +593,28 @@ class PopLibrary:
         here = self._here(x, (codes, scales, zeros, out, workspace), "gemv_w4")
         B, K = x.shape
         ldx, inner = x.stride()
-        shape = (-(-n // 16), -(-K // 128), 16, 128 // group if group else 0)
-        if x.dtype != torch.bfloat16 or inner != 1 or codes.dtype != torch.uint8 or codes.shape != shape[:3] + (64,) or \
-                not codes.is_contiguous():
+        nt, kt = -(-n // 16), -(-K // 128)
+        if x.dtype is not _BF16 or inner != 1 or codes.dtype is not _UINT8 or codes.shape != (nt, kt, 16, 64) or not codes.is_contiguous():
             raise PopError(POP_E_INVALID, "gemv_w4: x is bf16 [B, K], codes contiguous uint8 tiles of n rows and K inputs")
-        if scales.dtype != torch.bfloat16 or scales.shape != shape or not scales.is_contiguous() or \
-                (zeros is not None and (zeros.dtype != torch.uint8 or zeros.shape != shape or not zeros.is_contiguous())):
+        shape = (nt, kt, 16, 128 // group if group else 0)
+        if scales.dtype is not _BF16 or scales.shape != shape or not scales.is_contiguous() or \
+                (zeros is not None and (zeros.dtype is not _UINT8 or zeros.shape != shape or not zeros.is_contiguous())):
             raise PopError(POP_E_INVALID, "gemv_w4: contiguous bf16 scales and uint8 zeros of the tiles' groups are wanted")
         width = n if mode != 3 else n // 2 if n_valid is None else n_valid
         ldo, inner = out.stride()
-        if out.dtype != (torch.bfloat16 if mode == 3 else torch.float32) or out.shape[0] != B or out.shape[1] < width or inner != 1:
+        rows, cols = out.shape
+        if out.dtype is not (_BF16 if mode == 3 else _FP32) or rows != B or cols < width or inner != 1:
             raise PopError(POP_E_INVALID, "gemv_w4: out is fp32 [B, n], or bf16 [B, n_valid] for the gated form")
         if B == 0:
             return out
         need = self.dll.pop_k_gemv_w4_workspace_bytes(B, K, group) if B > 2 else 0
         if need and workspace is None:
             workspace = self._scratch(need, x.device, stream)
-        code = self.dll.pop_k_gemv_w4(
-            x.data_ptr(), ldx, codes.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), group,
-            None if workspace is None else workspace.data_ptr(),
-            0 if workspace is None else workspace.numel() * workspace.element_size(), out.data_ptr(), ldo, B, n, K, mode, act, width, here if stream is None else stream.cuda_stream)
+        code = self.dll.pop_k_packed(0, _PACK_GEMV(
+            x.data_ptr(), ldx, codes.data_ptr(), scales.data_ptr(), 0 if zeros is None else zeros.data_ptr(), group,
+            0 if workspace is None else workspace.data_ptr(),
+            0 if workspace is None else workspace.numel() * workspace.element_size(), out.data_ptr(), ldo, B, n, K, mode, act, width,
+            here if stream is None else stream.cuda_stream))
         if code:
             self.check(code, "pop_k_gemv_w4")
         return out
@@ -606,7 +624,7 @@ class PopLibrary:
         """(page_size, num_pages, max_pages, batch) of one layer of the bf16 cache."""
         shape = k_pool.shape
         if len(shape) != 4 or shape[2] != n_kv or shape[3] != hd or v_pool.shape != shape or \
-                k_pool.dtype != torch.bfloat16 or v_pool.dtype != torch.bfloat16 or block_table.dtype != torch.int32 or \
+                k_pool.dtype is not _BF16 or v_pool.dtype is not _BF16 or block_table.dtype is not _INT32 or \
                 not (k_pool.is_contiguous() and v_pool.is_contiguous() and block_table.is_contiguous()):
             raise PopError(POP_E_INVALID, f"{what}: contiguous bf16 pools [pages, page_size, n_kv, hd] and an int32 block table are wanted")
         batch, max_pages = block_table.shape
@@ -621,29 +639,32 @@ class PopLibrary:
         here = self._here(x, (q_out, k_pool, v_pool, block_table, rope_table, start, cu_rows, depth, q_gain, k_gain), what)
         page, pages, max_pages, batch = self._layer16(k_pool, v_pool, block_table, n_kv, hd, what)
         rows, width = x.shape
-        bf16 = x.dtype == torch.bfloat16
+        dtype = x.dtype
         ld_in, inner = x.stride()
-        if not (bf16 or x.dtype == torch.float32) or width != (n_q + 2 * n_kv) * hd or inner != 1:
+        if dtype is not _BF16 and dtype is not _FP32 or width != (n_q + 2 * n_kv) * hd or inner != 1:
             raise PopError(POP_E_INVALID, f"{what}: x is fp32 or bf16 [rows, (n_q + 2 n_kv) hd]")
-        q_ptr, ldq = None, 0
+        q_ptr = ldq = 0
         if n_q:
             ldq, inner = q_out.stride()
             q_ptr = q_out.data_ptr()
-            if q_out.dtype != torch.bfloat16 or q_out.shape != (rows, n_q * hd) or inner != 1:
+            if q_out.dtype is not _BF16 or q_out.shape != (rows, n_q * hd) or inner != 1:
                 raise PopError(POP_E_INVALID, f"{what}: q_out is bf16 [rows, n_q hd]")
-        table_rows = rope_table.numel() // hd
-        if rope_table.dtype != torch.float32 or table_rows * hd != rope_table.numel() or not rope_table.is_contiguous():
+        table_rows, rest = divmod(rope_table.numel(), hd)
+        if rope_table.dtype is not _FP32 or rest or not rope_table.is_contiguous():
             raise PopError(POP_E_INVALID, f"{what}: rope_table is fp32 [positions, hd / 2, 2]")
-        for g in (q_gain, k_gain):
-            if g is not None and (g.dtype != torch.float32 or g.numel() != hd or not g.is_contiguous()):
-                raise PopError(POP_E_INVALID, f"{what}: gains are fp32 [hd]")
+        gains = [0, 0]
+        for i, g in enumerate((q_gain, k_gain)):
+            if g is not None:
+                if g.dtype is not _FP32 or g.numel() != hd or not g.is_contiguous():
+                    raise PopError(POP_E_INVALID, f"{what}: gains are fp32 [hd]")
+                gains[i] = g.data_ptr()
         if rows == 0:
             return q_out
-        code = self.dll.pop_k_rope_cache_tree(
-            x.data_ptr(), 1 if bf16 else 0, ld_in, rows, self._ints(cu_rows, batch + 1, "cu_rows"), max_rows,
-            self._ints(start, batch, "start"), pos0, self._ints(depth, rows, "depth"), batch, q_ptr, ldq, k_pool.data_ptr(),
-            v_pool.data_ptr(), block_table.data_ptr(), page, pages, max_pages, _ptr(q_gain), _ptr(k_gain), eps,
-            rope_table.data_ptr(), table_rows, n_q, n_kv, hd, here if stream is None else stream.cuda_stream)
+        code = self.dll.pop_k_packed(1, _PACK_APPEND(
+            x.data_ptr(), dtype is _BF16, ld_in, rows, _vector(cu_rows, batch + 1, "cu_rows"), max_rows,
+            _vector(start, batch, "start"), pos0, _vector(depth, rows, "depth"), batch, q_ptr, ldq, k_pool.data_ptr(),
+            v_pool.data_ptr(), block_table.data_ptr(), page, pages, max_pages, gains[0], gains[1], eps,
+            rope_table.data_ptr(), table_rows, n_q, n_kv, hd, here if stream is None else stream.cuda_stream))
         if code:
             self.check(code, "pop_k_rope_cache_tree")
         return q_out
@@ -660,15 +681,15 @@ class PopLibrary:
         words = 0
         if mask is not None:
             words = mask.shape[-1]
-            if mask.dtype != torch.int32 or mask.shape != (rows, words) or not mask.is_contiguous():
+            if mask.dtype is not _INT32 or mask.shape != (rows, words) or not mask.is_contiguous():
                 raise PopError(POP_E_INVALID, f"{what}: mask is contiguous int32 [rows, words]")
         if rows == 0:
             return out
-        code = self.dll.pop_k_tree_attention(
-            q.data_ptr(), ldq, rows, self._ints(cu_rows, batch + 1, "cu_rows"), max_rows, self._ints(start, batch, "start"),
-            max_start, None if mask is None else mask.data_ptr(), words, self._ints(depth, rows, "depth"), k_pool.data_ptr(),
+        code = self.dll.pop_k_packed(2, _PACK_ATTEND(
+            q.data_ptr(), ldq, rows, _vector(cu_rows, batch + 1, "cu_rows"), max_rows, _vector(start, batch, "start"), max_start,
+            0 if mask is None else mask.data_ptr(), words, _vector(depth, rows, "depth"), k_pool.data_ptr(),
             v_pool.data_ptr(), block_table.data_ptr(), page, pages, max_pages, ws.data_ptr(), nbytes, out.data_ptr(), ldo,
-            batch, n_q, n_kv, hd, window, here if stream is None else stream.cuda_stream)
+            batch, n_q, n_kv, hd, window, here if stream is None else stream.cuda_stream))
         if code:
             self.check(code, "pop_k_tree_attention")
         return out
@@ -677,19 +698,20 @@ class PopLibrary:
         """pop_k_cache_keep: pools bf16 [layers, pages, page_size, n_kv, hd], changed where they lie; kept int32 [batch, m]
         rising slots of the draft, the first n_kept (int32 [batch]; all m if None) of each row; start int32 [batch] or pos0."""
         here = self._here(k_pool, (v_pool, block_table, kept, start, n_kept), "cache_keep")
-        layers, pages, page, n_kv, hd = k_pool.shape
-        strides = k_pool.stride()
+        shape, strides = k_pool.shape, k_pool.stride()
+        layers, pages, page, n_kv, hd = shape
         batch, max_pages = block_table.shape
-        if k_pool.dtype != torch.bfloat16 or v_pool.dtype != torch.bfloat16 or v_pool.shape != k_pool.shape or \
-                v_pool.stride() != strides or strides[1:] != (page * n_kv * hd, n_kv * hd, hd, 1):
+        if k_pool.dtype is not _BF16 or v_pool.dtype is not _BF16 or v_pool.shape != shape or v_pool.stride() != strides or \
+                strides[1:] != (page * n_kv * hd, n_kv * hd, hd, 1):
             raise PopError(POP_E_INVALID, "cache_keep: bf16 pools with contiguous layers, alike for K and V, are wanted")
-        if block_table.dtype != torch.int32 or not block_table.is_contiguous() or kept.dtype != torch.int32 or \
-                kept.shape[0] != batch or kept.stride(1) != 1:
+        rows, most = kept.shape
+        ld_kept, inner = kept.stride()
+        if block_table.dtype is not _INT32 or not block_table.is_contiguous() or kept.dtype is not _INT32 or rows != batch or inner != 1:
             raise PopError(POP_E_INVALID, "cache_keep: an int32 block table and int32 kept [batch, m] are wanted")
-        code = self.dll.pop_k_cache_keep(
+        code = self.dll.pop_k_packed(3, _PACK_KEEP(
             k_pool.data_ptr(), v_pool.data_ptr(), strides[0], layers, block_table.data_ptr(), page, pages, max_pages,
-            kept.data_ptr(), kept.stride(0), self._ints(n_kept, batch, "n_kept"), kept.shape[1],
-            self._ints(start, batch, "start"), pos0, batch, n_kv, hd, here if stream is None else stream.cuda_stream)
+            kept.data_ptr(), ld_kept, _vector(n_kept, batch, "n_kept"), most, _vector(start, batch, "start"), pos0, batch, n_kv, hd,
+            here if stream is None else stream.cuda_stream))
         if code:
             self.check(code, "pop_k_cache_keep")
 

@@ -4,6 +4,8 @@
 #include "w4.cuh"
 #include "../../include/pop_kernels.h"
 
+#include <cstring>
+
 using namespace pop;
 
 extern "C" {
@@ -345,6 +347,34 @@ int pop_k_cache_keep(void* k_pool, void* v_pool, int64_t layer_stride, int32_t l
   a.start = start; a.pos0 = pos0;
   a.batch = batch; a.n_kv = n_kv; a.head_dim = head_dim;
   return launch_cache_keep(a, static_cast<cudaStream_t>(stream));
+}
+
+int pop_k_packed(int32_t call, const int64_t* w) {
+  if (!w) return POP_E_INVALID;
+  const auto ptr = [w](int i) { return reinterpret_cast<void*>(static_cast<uintptr_t>(w[i])); };
+  const auto ints = [&](int i) { return static_cast<const int32_t*>(ptr(i)); };
+  const auto floats = [&](int i) { return static_cast<const float*>(ptr(i)); };
+  const auto n = [w](int i) { return w[i] == (int32_t)w[i] ? (int32_t)w[i] : INT32_MIN; };      // which the calls refuse
+  switch (call) {
+    case 0:
+      return pop_k_gemv_w4(ptr(0), w[1], ptr(2), ptr(3), ptr(4), n(5), ptr(6), (size_t)w[7], ptr(8), w[9], n(10), n(11), n(12),
+                           n(13), n(14), n(15), ptr(16));
+    case 1: {
+      double eps;
+      memcpy(&eps, w + 20, sizeof eps);
+      return pop_k_rope_cache_tree(ptr(0), n(1), w[2], n(3), ints(4), n(5), ints(6), n(7), ints(8), n(9), ptr(10), w[11],
+                                   ptr(12), ptr(13), ints(14), n(15), n(16), n(17), floats(18), floats(19), (float)eps, ptr(21),
+                                   n(22), n(23), n(24), n(25), ptr(26));
+    }
+    case 2:
+      return pop_k_tree_attention(ptr(0), w[1], n(2), ints(3), n(4), ints(5), n(6), ptr(7), n(8), ints(9), ptr(10), ptr(11),
+                                  ints(12), n(13), n(14), n(15), ptr(16), (size_t)w[17], ptr(18), w[19], n(20), n(21), n(22),
+                                  n(23), n(24), ptr(25));
+    case 3:
+      return pop_k_cache_keep(ptr(0), ptr(1), w[2], n(3), ints(4), n(5), n(6), n(7), ints(8), w[9], ints(10), n(11), ints(12),
+                              n(13), n(14), n(15), n(16), ptr(17));
+    default: return POP_E_INVALID;
+  }
 }
 
 int pop_k_status(void* stream) { return read_and_clear_status(static_cast<cudaStream_t>(stream)); }

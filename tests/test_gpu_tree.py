@@ -585,6 +585,38 @@ def test_captured_and_on_another_stream(L):
         assert torch.equal(a, b) and torch.equal(a, c)
 
 
+def test_calls_argument_by_argument(L):
+    """The four entry points called directly give the bits of the binding, which hands them packed words."""
+    n_q, n_kv, hd, page, rows, start, K = 4, 2, 64, 32, 6, 100, 256
+    g = gen(31)
+    N = (n_q + 2 * n_kv) * hd
+    tiles = laid_out(L, *weights(N, K, 32, True, g), 32)
+    k, v, table = pools(31, 1, start + rows, n_kv, hd, page, layers=1)
+    x, rope, tab, gain = torch.randn(rows, K, generator=g).to(torch.bfloat16).cuda(), rope_rows(200, hd).cuda(), table.cuda(), torch.rand(hd, generator=g).cuda()
+    kept = torch.tensor([[1, 2, 5]], dtype=torch.int32, device=DEV)
+    res = []
+    for direct in (False, True):
+        kd, vd = k.cuda(), v.cuda()
+        qkv, q, out = torch.empty(rows, N, device=DEV), *(torch.empty(rows, n_q * hd, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        ws = torch.empty(64 << 20, dtype=torch.uint8, device=DEV)
+        if direct:
+            s, p = torch.cuda.current_stream().cuda_stream, lambda t: t.data_ptr()  # noqa: E731
+            pages = (kd.shape[1], tab.shape[1])
+            assert L.dll.pop_k_gemv_w4(p(x), K, p(tiles[0]), p(tiles[1]), p(tiles[2]), 32, p(ws), ws.numel(), p(qkv), N, rows, N, K, 0, 0, N, s) == 0
+            assert L.dll.pop_k_rope_cache_tree(p(qkv), 0, N, rows, None, rows, None, start, None, 1, p(q), n_q * hd, p(kd), p(vd), p(tab), page,
+                                               *pages, p(gain), p(gain), 1e-3, p(rope), 200, n_q, n_kv, hd, s) == 0
+            assert L.dll.pop_k_tree_attention(p(q), n_q * hd, rows, None, rows, None, start, None, 0, None, p(kd), p(vd), p(tab), page, *pages,
+                                              p(ws), ws.numel(), p(out), n_q * hd, 1, n_q, n_kv, hd, 0, s) == 0
+            assert L.dll.pop_k_cache_keep(p(kd), p(vd), kd.stride(0), 1, p(tab), page, *pages, p(kept), 3, None, 3, None, start, 1, n_kv, hd, s) == 0
+        else:
+            L.gemv_w4(x, *tiles, qkv, N, 32)
+            L.rope_cache_tree(qkv, q, kd[0], vd[0], tab, rope, n_q, n_kv, hd, rows, pos0=start, q_gain=gain, k_gain=gain, eps=1e-3)
+            L.tree_attention(q, kd[0], vd[0], tab, out, n_q, n_kv, hd, rows, start)
+            L.cache_keep(kd, vd, tab, kept, pos0=start)
+        res.append((qkv, q, out, kd, vd))
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+
+
 def test_a_checked_path_is_what_decoding_gives(L):
     """A tree is projected, appended and attended at once; its accepted path is kept. The same tokens decoded one by one with
     the calls that the library has had (projection by the bf16 GEMV over the same weights, append of one row, single-query

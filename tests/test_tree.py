@@ -132,6 +132,30 @@ def test_nothing_to_do(library, call, change):
     assert getattr(library.dll, call)(*{**CALLS[call], **change}.values()) == 0
 
 
+PACKED = ("pop_k_gemv_w4", "pop_k_rope_cache_tree", "pop_k_tree_attention", "pop_k_cache_keep")
+
+
+@pytest.mark.parametrize("call,change", [(c, ch) for c in REFUSED for ch in REFUSED[c]] + NOSPACE + NOTHING)
+def test_packed_words_are_the_same_call(library, call, change):
+    import struct
+    args = {**CALLS[call], **change}
+    words = struct.pack("=" + "".join("d" if n == "eps" else "q" for n in args), *[0 if v is None else v for v in args.values()])
+    assert library.dll.pop_k_packed(PACKED.index(call), words) == getattr(library.dll, call)(*args.values())
+
+
+def test_packed_words_outside_their_type(library):
+    import struct
+    from paper_2602_03295_b200 import POP_E_INVALID
+    for n, call in enumerate(PACKED):
+        args = CALLS[call]
+        for name in ("rows", "batch", "n_q", "n_kv", "head_dim", "B", "N", "K", "group", "mode", "max_rows", "page_size"):
+            if name in args:
+                big = {**args, name: args[name] + (1 << 32)}            # the right value in its low half
+                words = struct.pack("=" + "".join("d" if k == "eps" else "q" for k in big), *[0 if v is None else v for v in big.values()])
+                assert library.dll.pop_k_packed(n, words) == POP_E_INVALID, (call, name)
+    assert library.dll.pop_k_packed(4, words) == POP_E_INVALID and library.dll.pop_k_packed(0, None) == POP_E_INVALID
+
+
 def test_binding_wants_the_current_device(library):
     from paper_2602_03295_b200 import PopError
     x = torch.zeros(2, 128, dtype=torch.bfloat16)
