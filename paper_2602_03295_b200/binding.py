@@ -520,6 +520,8 @@ class PopLibrary:
     def _scratch(nbytes, device, stream):
         """A call's own workspace, from the pool of the stream that runs the call: its memory has no work of another stream in
         front of it, and goes back, when the call returns, to that stream's later work."""
+        if stream is None:
+            return torch.empty(nbytes, dtype=torch.uint8, device=device)
         with torch.cuda.stream(stream):
             return torch.empty(nbytes, dtype=torch.uint8, device=device)
 

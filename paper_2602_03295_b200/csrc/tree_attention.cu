@@ -118,6 +118,19 @@ __device__ __forceinline__ int warp_add(int v) {
 // the tiles of a stretch: what the second launch asks for.
 __device__ __forceinline__ Plan plan_of(const TreeDev& p, int cta, int* starts) {
   const int lane = threadIdx.x & 31, batch = p.a.d.batch;
+  if (batch == 1) {                                            // nothing to add up (1 x 5 rows of 300: 10.9 us against 11.3)
+    Plan r;
+    r.x = seq_of(p, 0, cta == 0 && lane == 0);
+    const int total = line_of(p, r.x), share = max((total + p.ctas - 1) / p.ctas, MIN_SHARE);
+    r.lo = (int)min((int64_t)cta * share, (int64_t)total);
+    r.hi = min(r.lo + share, total);
+    r.b = r.base = 0;
+    if (starts != nullptr && lane == 0) {
+      starts[0] = 0;
+      starts[1] = share;
+    }
+    return r;
+  }
   Seq x;
   int mine = 0, total = 0;
   for (int b0 = 0; b0 < batch; b0 += 32) {
@@ -699,14 +712,13 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
   }
 }
 
-// Joins the parts of the items that lie in several stretches: a thread per (row, head) and 8 columns, out = sum_c w_c o_c /
-// sum_c w_c l_c with w_c = exp2(m_c - max m), the stretches in their order.
-constexpr int MERGE_COLS = 8;
-template <int HD>
+// Joins the parts of the items that lie in several stretches: a thread per (row, head) and COLS columns, out = sum_c w_c o_c /
+// sum_c w_c l_c with w_c = exp2(m_c - max m), the stretches in their order, the loads of PARTS of them in flight together.
+template <int HD, int COLS, int PARTS>
 __global__ void __launch_bounds__(128) tree_merge_kernel(const __grid_constant__ TreeDev p) {
   chain_trigger();
   chain_wait();
-  const int b = blockIdx.z, kvh = blockIdx.x % p.a.n_kv, qt = blockIdx.x / p.a.n_kv, col = blockIdx.y * MERGE_COLS, row = threadIdx.x;
+  const int b = blockIdx.z, kvh = blockIdx.x % p.a.n_kv, qt = blockIdx.x / p.a.n_kv, col = blockIdx.y * COLS, row = threadIdx.x;
   const int word = *reinterpret_cast<const volatile int*>(p.status), share = p.starts[p.a.d.batch], first = p.starts[b];
   const Seq x = seq_of(p, b, false);
   if (qt >= x.qts || gave_up(word)) return;                                     // gave up: there are parts that nobody wrote
@@ -717,16 +729,15 @@ __global__ void __launch_bounds__(128) tree_merge_kernel(const __grid_constant__
   constexpr int64_t step = 2 * part_floats(HD);
   const float* at = p.partial + row * 4 + c0 * step;
   const float* head = at + (a > c0 * share ? part_floats(HD) : 0);
-  constexpr int N = MERGE_COLS / 4;
-  float m = -INFINITY, l = 0.f, o[MERGE_COLS];
+  constexpr int N = COLS / 4;
+  float m = -INFINITY, l = 0.f, o[COLS];
 #pragma unroll
-  for (int k = 0; k < MERGE_COLS; ++k) o[k] = 0.f;
-  // eight parts at a time: their loads are in flight together
-  for (int c = c0; c <= c1; c += 8) {
-    float2 ml[8];
-    float4 v[8][N];
+  for (int k = 0; k < COLS; ++k) o[k] = 0.f;
+  for (int c = c0; c <= c1; c += PARTS) {
+    float2 ml[PARTS];
+    float4 v[PARTS][N];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
+    for (int u = 0; u < PARTS; ++u) {
       const float* src = c + u == c0 ? head : at + (c + u - c0) * step;
       const bool in = c + u <= c1;
       ml[u] = in ? __ldcg(reinterpret_cast<const float2*>(src + HD * 128)) : make_float2(-INFINITY, 0.f);
@@ -736,15 +747,15 @@ __global__ void __launch_bounds__(128) tree_merge_kernel(const __grid_constant__
     }
     float n = m;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) n = fmaxf(n, ml[u].x);
+    for (int u = 0; u < PARTS; ++u) n = fmaxf(n, ml[u].x);
     // no maximum so far: the parts saw nothing (zeros), or scores that are all NaN, whose sums stay NaN
     const float z = n == -INFINITY ? 0.f : n, f = ex2(m - z);
     m = n;
     l *= f;
 #pragma unroll
-    for (int k = 0; k < MERGE_COLS; ++k) o[k] *= f;
+    for (int k = 0; k < COLS; ++k) o[k] *= f;
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
+    for (int u = 0; u < PARTS; ++u) {
       const float w = ex2(ml[u].x - z);
       l = fmaf(w, ml[u].y, l);
 #pragma unroll
@@ -758,8 +769,11 @@ __global__ void __launch_bounds__(128) tree_merge_kernel(const __grid_constant__
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   bf16* dst = p.a.out + ((int64_t)x.row0 + i) * p.a.ldo + (int64_t)(kvh * p.G + row - ip * p.G) * HD + col;
-  *reinterpret_cast<uint4*>(dst) = make_uint4(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv), pack2(o[4] * inv, o[5] * inv),
-                                              pack2(o[6] * inv, o[7] * inv));
+  if constexpr (COLS == 8)
+    *reinterpret_cast<uint4*>(dst) = make_uint4(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv), pack2(o[4] * inv, o[5] * inv),
+                                                pack2(o[6] * inv, o[7] * inv));
+  else
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack2(o[0] * inv, o[1] * inv), pack2(o[2] * inv, o[3] * inv));
 }
 
 bool allow_smem(std::atomic<uint64_t>& done, const void* kernel, int bytes) {
@@ -810,8 +824,13 @@ int launch_t(const TreeAttnArgs& a, TreeDev& p, cudaStream_t s) {
     return POP_E_CUDA;
   count_launch();
   const int pairs = a.d.max_rows < p.per ? a.d.max_rows * p.G : p.per * p.G;
-  if (launch_chained(tree_merge_kernel<HD>, dim3((unsigned)(a.n_kv * qts), HD / MERGE_COLS, a.d.batch), dim3((pairs + 31) & ~31), 0, s,
-                     p) != cudaSuccess)
+  // Few items of many parts are joined by more threads, which each have more loads in flight: 1 x 64 rows of 8192 27.3 us against
+  // 28.6, 1 x 16 of 2000 13.4 against 14.4. Many items (16 x 12 rows, window 1024: 48.4 against 43.1) or few parts (1 x 5 of 300: 11.3
+  // against 10.9) would lose.
+  const int64_t share = (line + p.ctas - 1) / p.ctas, tiles = ((int64_t)a.d.pos0 + a.d.max_rows + BKV - 1) / BKV;
+  const bool wide = tiles > 8 * (share < MIN_SHARE ? MIN_SHARE : share) && a.n_kv * qts * (HD / 8) * a.d.batch <= 2 * device_sms();
+  if (launch_chained(wide ? tree_merge_kernel<HD, 4, 16> : tree_merge_kernel<HD, 8, 8>,
+                     dim3((unsigned)(a.n_kv * qts), HD / (wide ? 4 : 8), a.d.batch), dim3((pairs + 31) & ~31), 0, s, p) != cudaSuccess)
     return POP_E_CUDA;
   count_launch();
   return POP_OK;
