@@ -28,7 +28,7 @@ namespace pop {
 namespace {
 
 constexpr int SPREAD = 8, FLUSH = 8;      // warps that bring codes to TMEM, and that take the sums
-constexpr int COPY_WARP = SPREAD + FLUSH, MMA_WARP = COPY_WARP + 1, THREADS = (MMA_WARP + 1) * 32;
+constexpr int COPY_WARP = SPREAD + FLUSH, MMA_WARP = COPY_WARP + 1;
 constexpr int SMEM_BYTES = 227 * 1024;
 
 template <int GRP, int NB, bool ZEROS>
@@ -43,6 +43,8 @@ struct G4 {
   static constexpr int STAGE = (STAGE_BYTES + 1023) / 1024 * 1024;
   static constexpr int STAGES = (SMEM_BYTES - 2048) / STAGE < 8 ? (SMEM_BYTES - 2048) / STAGE : 8;
   static constexpr int BATCH = 2 * GPC * NB <= 128 ? 2 * GPC : 128 / NB;        // groups whose sums are taken together
+  // Where a step fills one buffer of sums, two warps issue products, every second step each, with buffers of its own
+  static constexpr int ISSUERS = BATCH == 2 * GPC ? 2 : 1, THREADS = (MMA_WARP + ISSUERS) * 32;
   static constexpr int D_COLS = BATCH * NB, D_BUFS = 256 / D_COLS < 4 ? 256 / D_COLS : 4;
   static constexpr int A_COL = 256;                                     // two steps of codes, 128 columns each
   static_assert(STAGES >= 3 && STAGES * STAGE >= NB * 512, "ring too shallow");
@@ -74,11 +76,11 @@ __device__ __forceinline__ void tmem_ld_cols(uint32_t from, float (&d)[N]) {
 }
 
 template <int GRP, int NB, bool ZEROS>
-__global__ void __launch_bounds__(THREADS, 1)
+__global__ void __launch_bounds__(G4<GRP, NB, ZEROS>::THREADS, 1)
 gemm4_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant__ CUtensorMap tm_scales,
              const __grid_constant__ CUtensorMap tm_zeros, const __grid_constant__ G4Dev p) {
   using C = G4<GRP, NB, ZEROS>;
-  constexpr int GPC = C::GPC, STAGES = C::STAGES;
+  constexpr int GPC = C::GPC, STAGES = C::STAGES, THREADS = C::THREADS;
   extern __shared__ uint8_t smem_raw[];
   G4Smem& s = *reinterpret_cast<G4Smem*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* ring = reinterpret_cast<uint8_t*>(&s) + 1024;
@@ -156,13 +158,13 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant
       copy_weights(f);
       copy_x(f);
     }
-  } else if (warp == MMA_WARP) {
+  } else if (warp >= MMA_WARP) {
     // f16 operands, fp32 sums, 128 x NB
     constexpr uint32_t idesc = umma_idesc_f16(128, NB);
     const uint32_t leader = elect_one();
     const uint64_t x_desc = umma_smem_desc(smem_u32(ring), 16, 1024);
-    int buf = 0, turn = 0;
-    for (int f = 0; f < n_steps && ok && !s.abort; ++f) {
+    int buf = warp - MMA_WARP, turn = 0;
+    for (int f = warp - MMA_WARP; f < n_steps && ok && !s.abort; f += C::ISSUERS) {
       const int stage = f % STAGES;
       const uint64_t xd = x_desc + uint64_t(stage * (C::STAGE >> 4));
       ok = wait(&s.full[stage], (f / STAGES) & 1) && wait(&s.a_ready[f & 1], (f >> 1) & 1);
@@ -178,8 +180,9 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant
                          xd + uint64_t(((k >> 2) * (NB * 128) + (k & 3) * 32) >> 4), idesc, kk % (GRP / 16) > 0 ? 1u : 0u);
         }
         umma_commit_w(leader, &s.d_full[buf]);
-        if (++buf == C::D_BUFS) {
-          buf = 0;
+        buf += C::ISSUERS;
+        if (buf >= C::D_BUFS) {
+          buf -= C::D_BUFS;
           ++turn;
         }
       }
@@ -386,7 +389,7 @@ int max_clusters(int n) {
   if (most > 0) return most;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(n);
-  cfg.blockDim = dim3(THREADS);
+  cfg.blockDim = dim3(G4<GRP, NB, ZEROS>::THREADS);
   cfg.dynamicSmemBytes = SMEM_BYTES;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -440,7 +443,7 @@ int launch_t(const Gemv4Args& a, G4Dev& p, cudaStream_t s) {
     zeros = scales;
   }
   ProfScope prof(PROF_GEMV, (double)p.N * p.K * (0.5 + (ZEROS ? 3.0 : 2.0) / GRP) * slabs, s);
-  if (launch_chained_cluster_x(gemm4_kernel<GRP, NB, ZEROS>, dim3((unsigned)(units * p.cs * each), slabs), dim3(THREADS), SMEM_BYTES,
+  if (launch_chained_cluster_x(gemm4_kernel<GRP, NB, ZEROS>, dim3((unsigned)(units * p.cs * each), slabs), dim3(C::THREADS), SMEM_BYTES,
                                s, (unsigned)(p.cs * each), codes, scales, zeros, p) != cudaSuccess)
     return POP_E_CUDA;
   count_launch();
