@@ -237,16 +237,16 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant
       ok = wait(&s.full[stage], (f / STAGES) & 1);
 #pragma unroll 1
       for (int g0 = 0; g0 < 2 * GPC && ok; g0 += C::BATCH) {
-        float2 sc2[C::BATCH], nz2[C::BATCH];
+        float2 sc2[C::BATCH], z2[C::BATCH];
 #pragma unroll
         for (int b = 0; b < C::BATCH; ++b) {
           const int q = g0 + b, grp = q % GPC, place = at + q / GPC * (16 * GPC) + grp;
           float scale = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(base + C::SCALES + place * 2) << 16);
           // what lies behind K is never used
           if (q > 0 && (first + f) * 256 + q * GRP >= p.K) scale = 0.f;
-          const float nz = ZEROS ? -(float)(base[C::ZEROS_AT + place] & 15) : -1.f;
+          const float z = ZEROS ? (float)(base[C::ZEROS_AT + place] & 15) : 1.f;
           sc2[b] = make_float2(scale, scale);
-          nz2[b] = make_float2(nz, nz);
+          z2[b] = make_float2(z, z);
         }
         ok = wait(&s.d_full[buf], turn & 1);
         if (!ok) break;
@@ -276,10 +276,14 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant
                 const float4 x = *reinterpret_cast<const float4*>(of + i * 4);
                 float2& t0 = acc[c / 2 + i * 2];
                 float2& t1 = acc[c / 2 + i * 2 + 1];
-                t0 = __ffma2_rn(__ffma2_rn(make_float2(d[b][i * 4], d[b][i * 4 + 1]), make_float2(u.x, u.y),
-                                           __fmul2_rn(nz2[b0 + b], make_float2(x.x, x.y))), sc2[b0 + b], t0);
-                t1 = __ffma2_rn(__ffma2_rn(make_float2(d[b][i * 4 + 2], d[b][i * 4 + 3]), make_float2(u.z, u.w),
-                                           __fmul2_rn(nz2[b0 + b], make_float2(x.z, x.w))), sc2[b0 + b], t1);
+                // the sums of activations are negative, and without zeros times the 8 that stands for them
+                float2 x0 = make_float2(x.x, x.y), x1 = make_float2(x.z, x.w);
+                if constexpr (ZEROS) {
+                  x0 = __fmul2_rn(z2[b0 + b], x0);
+                  x1 = __fmul2_rn(z2[b0 + b], x1);
+                }
+                t0 = __ffma2_rn(__ffma2_rn(make_float2(d[b][i * 4], d[b][i * 4 + 1]), make_float2(u.x, u.y), x0), sc2[b0 + b], t0);
+                t1 = __ffma2_rn(__ffma2_rn(make_float2(d[b][i * 4 + 2], d[b][i * 4 + 3]), make_float2(u.z, u.w), x1), sc2[b0 + b], t1);
               }
             }
           }

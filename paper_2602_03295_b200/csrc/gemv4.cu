@@ -54,7 +54,7 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], bool first, uint32_t a0, 
 }
 // Converted activations for many CTAs: per slab of `cols` rows f16 values, then [kt][1 + GPC][cols] units and sums. The values
 // lie as [cols][kt][128]; for slabs of more than 8 rows, chunks come in pairs (K as if filled up with zeros), the values as
-// gemm4.cu's products read them in front of the units and sums. A half-warp per row and chunk; bound by launch
+// gemm4.cu's products read them in front of the units and the (negative) sums. A half-warp per row and chunk; bound by launch
 // and one round through memory.
 template <int GRP>
 __global__ void __launch_bounds__(256) gemv4_convert_kernel(const bf16* __restrict__ x, int64_t ldx, uint8_t* __restrict__ out,
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(256) gemv4_convert_kernel(const bf16* __restri
                                                  : slab + (c >> 1) * slab_bytes(cols, GPC, 2) + cols * 512 + (c & 1) * ((1 + GPC) * cols * 4)) +
               r % cols;
   if (h == 0) to[0] = unit;
-  if (h % (GRP / 8) == 0) to[(1 + h / (GRP / 8)) * cols] = sum * sum_scale(zeros != 0);
+  if (h % (GRP / 8) == 0) to[(1 + h / (GRP / 8)) * cols] = sum * (cols == 8 ? sum_scale(zeros != 0) : -sum_scale(zeros != 0));
 }
 
 // A code in the low bits of an f16 is code * 2^-24, in bits 4 .. 7 code * 2^-20: subnormals are linear, so that a mask alone
