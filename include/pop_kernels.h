@@ -291,7 +291,7 @@ int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int
  * What lies behind row N or input K is read and has no effect, whatever it is. codes, scales and zeros 16-byte aligned.
  *
  * pop_k_gemv_w4: pop_k_gemv with such weights: out[b][n] = sum_k x[b][k] W[n][k], x bf16 [B][ldx] (16-byte aligned, ldx and K
- * multiples of 8), any B (made for 1 to some dozens of rows). Modes as pop_k_gemv: 0 fp32 store, 2 fp32 +=, 3 gated -> bf16
+ * multiples of 8), B up to 65535 (made for 1 to some dozens of rows). Modes as pop_k_gemv: 0 fp32 store, 2 fp32 +=, 3 gated -> bf16
  * (N a multiple of 256: 128 gate rows, then the 128 matching up rows; act 0 SiLU, 1 tanh-GELU). The products of
  * codes and activations are exact (of activations within 2^-27 of the largest of their 128 inputs; smaller ones are off by at
  * most 2^-36 of it); sums are fp32, in an order that depends on the sizes alone. An activation row with an infinite or NaN
@@ -301,8 +301,9 @@ int pop_k_gemv_w4(const void* x, int64_t ldx, const void* codes, const void* sca
                   void* workspace, size_t workspace_bytes, void* out, int64_t ldo, int32_t B, int32_t N, int32_t K,
                   int32_t mode, int32_t act, int32_t n_valid, void* stream);
 /* Bytes of device workspace (16-byte aligned, contents irrelevant before and after; one for each of calls that may overlap)
- * that the call needs for its activations; 0 for one or two rows, where workspace may be NULL. A smaller one is POP_E_NOSPACE. */
-size_t pop_k_gemv_w4_workspace_bytes(int32_t B, int32_t K, int32_t group);
+ * that the call needs for its activations; 0 for one or two rows and for small products, where workspace may be NULL. A smaller
+ * one is POP_E_NOSPACE. */
+size_t pop_k_gemv_w4_workspace_bytes(int32_t B, int32_t N, int32_t K, int32_t group);
 
 /* pop_k_rope_cache for drafted rows. in: projections [q heads | k heads | v heads] * hd of `rows` packed rows, fp32 or
  * (in_bf16) bf16, row stride ld_in (a multiple of 4; 16-byte aligned). Sequence b owns rows cu_rows[b] .. cu_rows[b + 1] - 1

@@ -116,7 +116,7 @@ SIGNATURES = {
     "pop_k_profile": (None, [_I32]),
     "pop_k_profile_summary": (C.c_int, [_I32, C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(_I64)]),
     "pop_k_gemv_w4": (C.c_int, [_P, _I64, _P, _P, _P, _I32, _P, C.c_size_t, _P, _I64] + [_I32] * 6 + [_P]),
-    "pop_k_gemv_w4_workspace_bytes": (C.c_size_t, [_I32, _I32, _I32]),
+    "pop_k_gemv_w4_workspace_bytes": (C.c_size_t, [_I32, _I32, _I32, _I32]),
     "pop_k_rope_cache_tree": (C.c_int, [_P, _I32, _I64, _I32, _P, _I32, _P, _I32, _P, _I32, _P, _I64, _P, _P, _P, _I32, _I32,
                                         _I32, _P, _P, _F, _P] + [_I32] * 4 + [_P]),
     "pop_k_tree_attention": (C.c_int, [_P, _I64, _I32, _P, _I32, _P, _I32, _P, _I32, _P, _P, _P, _P, _I32, _I32, _I32, _P,
@@ -609,7 +609,7 @@ class PopLibrary:
             raise PopError(POP_E_INVALID, "gemv_w4: out is fp32 [B, n], or bf16 [B, n_valid] for the gated form")
         if B == 0:
             return out
-        need = self.dll.pop_k_gemv_w4_workspace_bytes(B, K, group) if B > 2 else 0
+        need = self.dll.pop_k_gemv_w4_workspace_bytes(B, n, K, group) if B > 2 else 0
         if need and workspace is None:
             workspace = self._scratch(need, x.device, stream)
         code = self.dll.pop_k_packed(0, _PACK_GEMV(

@@ -280,7 +280,7 @@ int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int
   return launch_attention8(a, static_cast<cudaStream_t>(stream));
 }
 
-size_t pop_k_gemv_w4_workspace_bytes(int32_t B, int32_t K, int32_t group) { return gemv4_workspace_bytes(B, K, group); }
+size_t pop_k_gemv_w4_workspace_bytes(int32_t B, int32_t N, int32_t K, int32_t group) { return gemv4_workspace_bytes(B, N, K, group); }
 
 int pop_k_gemv_w4(const void* x, int64_t ldx, const void* codes, const void* scales, const void* zeros, int32_t group,
                   void* workspace, size_t workspace_bytes, void* out, int64_t ldo, int32_t B, int32_t N, int32_t K,

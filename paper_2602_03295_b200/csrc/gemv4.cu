@@ -33,6 +33,7 @@ struct Gemv4Dev {
   int tpr, rounds;              // tiles of a cluster between two exchanges of sums; such rounds
   int grain;                    // a warp's stretch begins at a multiple of it
   int deal, deal_rest;          // tiles (gated: pairs) of each cluster; how many clusters have one more
+  int rows;                     // activation rows that shared memory has room for
   uint32_t sc_inv, per_inv;     // ceil(2^32 / sc), ceil(2^32 / (16 rows)): products with them replace divisions
   int* status;
 };
@@ -92,7 +93,7 @@ __global__ void __launch_bounds__(256) gemv4_convert_kernel(const bf16* __restri
 //   scale (2^-shift sum_k code_k x'_k - zero sum_k x_k),   the second sum made once with the conversion.
 // (Subtracting the zero from every pair of codes took 32 more operations per KB of codes; codes as bf16 128 + code, 64.)
 //
-// The weight rows are the M side of the warp-level MMA, up to 8 activation rows its N side (more: gemm4.cu): a tile of 16 rows x 128 inputs
+// The weight rows are the M side of the warp-level MMA, 8 activation rows of a grid row its N side (many: gemm4.cu): a tile of 16 rows x 128 inputs
 // is 1 KB in one piece, 16 bytes of row g and 16 of row g + 8 to lane (g = lane / 4, t = lane % 4), word j inputs 32 j + 8 t ..
 // + 7. The chunks of a CTA's tiles are one line, of which each warp streams an equal stretch through a ring of its own; bulk
 // copies keep more bytes in flight than loads to registers (1 x 4096 -> 128256: 46 us, 5.8 TB/s, against 55). Where there are
@@ -108,13 +109,13 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
   const int xs = p.sc * 256 + 64;                   // bytes of an activation row: 64 off a multiple of 128, so that the
                                                     // rows of a quarter-warp's loads lie in other banks
   const int tid = threadIdx.x, lane = tid & 31, wic = tid >> 5, g = lane >> 2, t = lane & 3;
-  const int rows = p.B;
+  const int row0 = blockIdx.y * COLS, rows = min(p.B - row0, COLS);
   const uint8_t* s_ring = smem + wic * (RING * SLOT_BYTES);
   uint8_t* s_zero = smem + WARPS * RING * SLOT_BYTES;             // 256 zeros: what lanes without an activation row read
   uint64_t* s_bar = reinterpret_cast<uint64_t*>(s_zero + 256);    // [WARPS][RING], and one of the activations
   float* s_sum = reinterpret_cast<float*>(s_bar + WARPS * RING + 2);  // [sc][1 + GPC][COLS]: 2^-shift; sums of the groups
   uint8_t* s_x = reinterpret_cast<uint8_t*>(s_sum + p.sc * (1 + GPC) * COLS);
-  float* s_acc = reinterpret_cast<float*>(s_x + p.B * xs);     // [tpr + WARPS][rows][16]
+  float* s_acc = reinterpret_cast<float*>(s_x + p.rows * xs);     // [tpr + WARPS][rows][16]
   const int rank = cluster_ctarank();
   int cluster;
   asm("mov.u32 %0, %%clusterid.x;" : "=r"(cluster));
@@ -236,7 +237,7 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
             ri[i] = r;
             ci[i] = c;
             const int k = (c0 + c) * 128 + h * 8;
-            v[i] = r < rows && k < p.K ? *reinterpret_cast<const uint4*>(p.x + r * p.ldx + k) : make_uint4(0, 0, 0, 0);
+            v[i] = r < rows && k < p.K ? *reinterpret_cast<const uint4*>(p.x + (row0 + r) * p.ldx + k) : make_uint4(0, 0, 0, 0);
             c += WARPS * 2;
             wrap();
           }
@@ -345,7 +346,7 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
         }
         settle();
         // sum r: row g + 8 (r / 2) of the tile, activation row 2 t + r % 2
-        float* acc = s_acc + (n_tile + wic) * (p.B * 16) + 2 * t * 16 + g;
+        float* acc = s_acc + (n_tile + wic) * (p.rows * 16) + 2 * t * 16 + g;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           float* dst = acc + (r & 1) * 16 + 8 * (r >> 1);
@@ -361,25 +362,25 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
     } else {
       __syncthreads();
     }
-    const int tiles = max(0, min(p.tpr, dealt - round * p.tpr)), per = p.B * 16, all = tiles / each * per;
+    const int tiles = max(0, min(p.tpr, dealt - round * p.tpr)), per = p.rows * 16, all = tiles / each * per;
     for (int e = rank * (WARPS * 32) + tid; e < all; e += p.cs * (WARPS * 32)) {
       const int n = __umulhi(e, p.per_inv) * each, at = e - n / each * per, tile = tile_of(round * p.tpr + n);
       if (at >= rows * 16) continue;
       auto sum_of = [&](int m) {
         // the parts of tile m in the order of the warps and ranks; they lie in the same places in all ranks
         float v = 0.f, w[WARPS];
-        const float* part = s_acc + m * (p.B * 16) + at;
+        const float* part = s_acc + m * (p.rows * 16) + at;
         auto has = [&](int i) { return max(stretch(round, i), m * p.sc) < min(stretch(round, i + 1), (m + 1) * p.sc); };
         if (p.cs == 1) {
 #pragma unroll
-          for (int i = 0; i < WARPS; ++i) w[i] = has(i) ? part[i * (p.B * 16)] : 0.f;
+          for (int i = 0; i < WARPS; ++i) w[i] = has(i) ? part[i * (p.rows * 16)] : 0.f;
 #pragma unroll
           for (int i = 0; i < WARPS; ++i) v += w[i];
         } else {
 #pragma unroll 1
           for (int i = 0; i < WARPS; ++i) {
             if (!has(i)) continue;
-            const uint32_t a = smem_u32(part + i * (p.B * 16));
+            const uint32_t a = smem_u32(part + i * (p.rows * 16));
 #pragma unroll
             for (int r = 0; r < 8; ++r) {
               w[r] = 0.f;
@@ -391,7 +392,7 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
         }
         return v * 0x1p24f;
       };
-      const int b = at >> 4, row = at & 15;
+      const int b = row0 + (at >> 4), row = at & 15;
       const float v = sum_of(n);
       if (gated) {
         const float up = sum_of(n + 1);
@@ -452,19 +453,20 @@ int launch_t(Gemv4Dev& p, cudaStream_t s) {
   constexpr int GPC = 128 / GRP, RING_BYTES = WARPS * RING * SLOT * (1024 + 32 * GPC + (ZEROS ? 16 * GPC : 0));
   constexpr int FIXED = RING_BYTES + 256 + (WARPS * RING + 2) * 8 + COLS * 64;
   static_assert(SMEM_LIMIT - FIXED >= (WARPS + 2) * COLS * 64 + 4 * COLS * (256 + 4 + 4 * GPC), "shared memory budget");
-  const int room = SMEM_LIMIT - FIXED, acc_bytes = p.B * 64, sc_bytes = p.B * 256 + COLS * (4 + 4 * GPC);
+  p.rows = p.B < COLS ? p.B : COLS;
+  const int slabs = ceil_div(p.B, COLS), room = SMEM_LIMIT - FIXED, acc_bytes = p.rows * 64, sc_bytes = p.rows * 256 + COLS * (4 + 4 * GPC);
   // Work of an SM with two CTAs, in clocks as measured: 30 to convert a row's chunk, 47 for a tile's chunk, the exchange within
   // a cluster. us in clusters of 1 / 2 / 8: 1 x 4096 -> 28672 gated 14.8 / 16.0 / 21.2, 1 x 14336 -> 4096 11.4 / 11.4 / 15.0.
   // A pass over part of the inputs, or a round over part of the tiles, costs 6000 more.
   const int each = p.mode == 3 ? 2 : 1, want = p.tiles / each;
   int64_t best = INT64_MAX;
   for (int cs = 1; cs <= 8 && cs <= p.kt; cs *= 2) {
-    const int most = max_clusters<GRP, ZEROS>(cs), clusters = want < most ? want : most;
+    const int most = ceil_div(max_clusters<GRP, ZEROS>(cs), slabs), clusters = want < most ? want : most;
     // all chunks of a CTA at once if they fit beside the sums of two tiles, then as many tiles as fit
     const int dealt = ceil_div(want, clusters) * each, nc = ceil_div(p.kt, cs);
     const int passes = ceil_div(nc, (room - (WARPS + 2) * acc_bytes) / sc_bytes), sc = ceil_div(p.kt, passes * cs);
     const int rounds = ceil_div(dealt, ((room - sc * sc_bytes) / acc_bytes - WARPS) / 2 * 2);
-    const int64_t cost = (int64_t)2 * nc * (p.B * (p.xq ? 2 : 30) + (int64_t)p.tiles * 47 / clusters) +
+    const int64_t cost = (int64_t)2 * nc * (p.rows * (p.xq ? 2 : 30) + (int64_t)p.tiles * 47 / clusters) +
                          (cs > 1 ? 4000 + 1000 * cs : 0) + (passes * rounds - 1) * 6000;
     if (cost < best) {
       best = cost;
@@ -480,29 +482,37 @@ int launch_t(Gemv4Dev& p, cudaStream_t s) {
   p.deal = p.tiles / each / p.clusters;
   p.deal_rest = p.tiles / each % p.clusters;
   p.sc_inv = (uint32_t)(((1ull << 32) + p.sc - 1) / p.sc);
-  p.per_inv = (uint32_t)(((1ull << 32) + p.B * 16 - 1) / (p.B * 16));
+  p.per_inv = (uint32_t)(((1ull << 32) + p.rows * 16 - 1) / (p.rows * 16));
   const size_t smem = FIXED + (size_t)p.sc * sc_bytes + (size_t)(p.tpr + WARPS) * acc_bytes;
   p.status = status_word();
   if (!p.status) return POP_E_CUDA;
-  ProfScope prof(PROF_GEMV, (double)p.N * p.K * (0.5 + (p.zeros ? 3.0 : 2.0) / GRP), s);
-  if (launch_chained_cluster_x(gemv4_kernel<GRP, ZEROS>, dim3(p.clusters * p.cs), dim3(WARPS * 32), smem, s,
+  ProfScope prof(PROF_GEMV, (double)p.N * p.K * (0.5 + (p.zeros ? 3.0 : 2.0) / GRP) * slabs, s);
+  if (launch_chained_cluster_x(gemv4_kernel<GRP, ZEROS>, dim3(p.clusters * p.cs, slabs), dim3(WARPS * 32), smem, s,
                                (unsigned)p.cs, p) != cudaSuccess)
     return POP_E_CUDA;
   count_launch();
   return POP_OK;
 }
 
-// Rows from which a launch of its own converts the activations
-constexpr int CONVERT_ROWS = 3;
+// Whether each CTA converts the activations that it needs, 8 rows at a time, and no launch of its own does it before. us so / by a
+// launch: 3 x 2048 -> 4096 4.7 / 4.9, 8 x 1024 -> 4096 5.1 / 4.8, 8 x 2048 -> 4096 6.9 / 5.3, and beyond 8 rows, where weights are
+// read again for each 8 and the other products begin, 16 x 1024 -> 4096 5.7 / 6.2, 64 x 512 -> 512 3.9 / 8.1, 32 x 1024 -> 4096 6.5 /
+// 7.2, 32 x 2048 -> 4096 9.9 / 8.1, 16 x 2048 -> 4096 7.5 / 6.7. A call of two launches takes 4 us more of the host.
+bool converts_itself(int B, int N, int K) {
+  if (B < 3) return true;
+  if (B <= COLS) return (int64_t)B * ceil_div(K, 128) <= 64;
+  return (int64_t)ceil_div(B, COLS) * N * K < (1 << 24);
+}
 
 template <int GRP>
 int launch_grp(const Gemv4Args& a, Gemv4Dev& p, cudaStream_t s) {
   void* workspace = a.workspace;
   const size_t bytes = a.workspace_bytes;
-  if (p.B >= CONVERT_ROWS) {
+  const bool own = converts_itself(p.B, p.N, p.K);
+  if (p.B > 65535) return POP_E_INVALID;
+  if (!own) {
     const int cols = cols_of(p.B), slabs = ceil_div(p.B, cols), kt = (int)slab_chunks(cols, p.kt);
     if (!workspace || (int64_t)bytes < slabs * slab_bytes(cols, 128 / GRP, kt)) return POP_E_NOSPACE;
-    if (p.B > 65535) return POP_E_INVALID;
     p.xq = static_cast<uint8_t*>(workspace);
     ProfScope prof(PROF_ELEMENTWISE, (double)p.B * p.K * 4, s);
     if (launch_chained(gemv4_convert_kernel<GRP>, dim3(ceil_div(kt, 16), p.B), dim3(256), 0, s, p.x, p.ldx,
@@ -510,14 +520,14 @@ int launch_grp(const Gemv4Args& a, Gemv4Dev& p, cudaStream_t s) {
       return POP_E_CUDA;
     count_launch();
   }
-  if (p.B > COLS) return launch_gemm4(a, p.xq, s);        // at 8 rows the other one is slower: 4096 -> 28672 gated 34 us to 20
+  if (p.B > COLS && !own) return launch_gemm4(a, p.xq, s);        // at 8 rows the other one is slower: 4096 -> 28672 gated 34 us to 20
   return p.zeros ? launch_t<GRP, true>(p, s) : launch_t<GRP, false>(p, s);
 }
 
 }  // namespace
 
-size_t gemv4_workspace_bytes(int B, int K, int group) {
-  if (B < CONVERT_ROWS || K < 1 || (group != 32 && group != 64 && group != 128)) return 0;
+size_t gemv4_workspace_bytes(int B, int N, int K, int group) {
+  if (B < 1 || N < 1 || K < 1 || converts_itself(B, N, K) || (group != 32 && group != 64 && group != 128)) return 0;
   return (size_t)(ceil_div(B, cols_of(B)) * slab_bytes(cols_of(B), 128 / group, slab_chunks(cols_of(B), ceil_div(K, 128))));
 }
 

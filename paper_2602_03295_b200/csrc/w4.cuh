@@ -16,14 +16,14 @@ struct Gemv4Args {
   int B, N, K, mode, act, n_valid;
   void* workspace; size_t workspace_bytes;             // see pop_k_gemv_w4_workspace_bytes
 };
-size_t gemv4_workspace_bytes(int B, int K, int group);
+size_t gemv4_workspace_bytes(int B, int N, int K, int group);
 int launch_gemv4(const Gemv4Args& a, cudaStream_t s);
 // Slabs of rows in which the activations are converted
 constexpr int cols_of(int B) { return B <= 8 ? 8 : B <= 16 ? 16 : B <= 32 ? 32 : 64; }
 __host__ __device__ constexpr int64_t slab_bytes(int cols, int gpc, int64_t kt) { return kt * cols * (256 + 4 * (1 + gpc)); }
 // chunks of 128 inputs that a slab has room for: with more than 8 rows they come in pairs
 constexpr int64_t slab_chunks(int cols, int64_t kt) { return cols == 8 ? kt : (kt + 1) / 2 * 2; }
-// the products from 9 rows on, with the activations converted
+// the products from 9 rows on, unless they are small, with the activations converted
 int launch_gemm4(const Gemv4Args& a, const uint8_t* xq, cudaStream_t s);
 int device_sms();                                      // SMs of the device that was current at the first call
 

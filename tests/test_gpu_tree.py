@@ -71,6 +71,11 @@ GEMV = [  # B, N, K, group, zeros
     # long and wide ones of more rows than a warp-level product takes, and their ends
     (9, 4000, 14336, 128, True), (12, 16, 40000, 32, True), (48, 20000, 520, 64, False), (20, 129, 8, 32, True), (32, 256, 264, 32, False),
     (16, 1000, 4096, 32, True), (64, 128, 2176, 128, False),
+    # large enough for the products on TMEM accumulators: each of their widths, groups and zeros, with ends inside tiles and steps
+    (9, 2051, 4104, 32, True), (10, 2051, 4104, 32, False), (16, 1030, 8200, 64, False), (15, 1030, 8200, 64, True), (13, 4111, 2056, 128, True),
+    (16, 4111, 2056, 128, False), (17, 1400, 4008, 32, True), (32, 2070, 2040, 32, False), (32, 2070, 2040, 64, True), (26, 4200, 1032, 64, False),
+    (25, 4200, 1032, 128, True), (31, 1100, 4104, 128, False), (33, 1700, 2000, 32, True), (130, 1000, 1032, 32, False), (64, 520, 4104, 64, True),
+    (50, 1030, 2600, 64, False), (65, 260, 8072, 128, True), (64, 2111, 1000, 128, False),
 ]
 
 
@@ -97,7 +102,8 @@ def test_gemv_w4(L, B, N, K, group, zeros):
 
 
 @pytest.mark.parametrize("B,N,K,group,zeros", [(1, 40, 264, 32, True), (7, 90, 512, 64, True), (12, 64, 2048, 128, True),
-                                               (40, 300, 640, 32, False), (1, 3000, 1024, 128, False)])
+                                               (40, 300, 640, 32, False), (1, 3000, 1024, 128, False),
+                                               (12, 8200, 1032, 128, True), (40, 6600, 512, 32, False), (20, 6600, 1000, 64, True)])
 def test_gemv_w4_is_exact_where_fp32_is(L, B, N, K, group, zeros):
     """Whole inputs up to 8 and scales that are powers of two: every partial sum is a multiple of 1/8 below 2^21."""
     g = gen(N + K)
@@ -113,7 +119,8 @@ def test_gemv_w4_is_exact_where_fp32_is(L, B, N, K, group, zeros):
 @pytest.mark.parametrize("B,F,K,group,zeros,act,n_valid", [
     (1, 128, 64, 32, True, 0, 128), (1, 688, 256, 64, False, 0, 688), (6, 256, 1032, 128, True, 1, 200), (13, 384, 512, 32, False, 1, 384),
     (40, 512, 768, 128, True, 0, 500), (1, 14336, 4096, 128, False, 0, 14336), (70, 128, 136, 64, True, 0, 127),
-    (9, 896, 4096, 32, True, 0, 890), (17, 20000, 256, 128, False, 1, 20000), (64, 300, 1000, 64, False, 0, 300)])
+    (9, 896, 4096, 32, True, 0, 890), (17, 20000, 256, 128, False, 1, 20000), (64, 300, 1000, 64, False, 0, 300),
+    (12, 2000, 2056, 64, True, 0, 1990), (40, 900, 1640, 128, False, 0, 897), (64, 1000, 1032, 32, True, 1, 1000)])
 def test_gemv_w4_gated(L, B, F, K, group, zeros, act, n_valid):
     N = -(-F // 128) * 256
     g = gen(F + K + B)
@@ -128,11 +135,11 @@ def test_gemv_w4_gated(L, B, F, K, group, zeros, act, n_valid):
     assert (out[:, n_valid:] == 7).all()
 
 
-@pytest.mark.parametrize("B", [1, 2, 5, 8, 9, 30, 64])
+@pytest.mark.parametrize("B", [1, 2, 5, 8, 9, 16, 30, 64])
 def test_gemv_w4_of_all_magnitudes(L, B):
     """Rows from 2^-90 to 2^90, inputs within a chunk up to 2^20 apart. Those below 2^-27 of a chunk's largest are off by 2^-36 of it."""
     g = gen(B)
-    N, K, group = 100, 1152, 64
+    N, K, group = 100 if B in (1, 2, 5, 8, 16) else 7300, 1152, 64
     plain = weights(N, K, group, True, g)
     x = torch.randn(B, K, generator=g) * torch.exp2(torch.randint(-20, 1, (B, K), generator=g).float())
     x = (x * torch.exp2(torch.linspace(-90, 90, B)[:, None].round())).to(torch.bfloat16)
@@ -166,35 +173,57 @@ def test_gemv_w4_of_more_than_2_to_the_32_weights(L):
 def test_gemv_w4_workspaces_of_two_streams(L):
     """Calls on two streams at once, each with a workspace of its own, and with those that the binding takes."""
     g = gen(6)
-    plain = weights(640, 2048, 128, False, g)
+    plain = weights(4200, 2048, 128, False, g)
     tiles = laid_out(L, *plain, 128)
     xs = [torch.randn(24, 2048, generator=g).to(torch.bfloat16).cuda() for _ in range(2)]
-    want = [torch.empty(24, 640, device=DEV) for _ in range(2)]
+    want = [torch.empty(24, 4200, device=DEV) for _ in range(2)]
     for x, o in zip(xs, want):
-        L.gemv_w4(x, *tiles, o, 640, 128)
+        L.gemv_w4(x, *tiles, o, 4200, 128)
     torch.cuda.synchronize()
-    need = L.dll.pop_k_gemv_w4_workspace_bytes(24, 2048, 128)
+    need = L.dll.pop_k_gemv_w4_workspace_bytes(24, 4200, 2048, 128)
     streams = [torch.cuda.Stream() for _ in range(2)]
     for given in (True, False):
-        got = [torch.zeros(24, 640, device=DEV) for _ in range(2)]
+        got = [torch.zeros(24, 4200, device=DEV) for _ in range(2)]
         ws = [torch.full((need,), 255, dtype=torch.uint8, device=DEV) if given else None for _ in range(2)]
         torch.cuda.synchronize()
         for _ in range(20):
             for x, o, w, st in zip(xs, got, ws, streams):
-                L.gemv_w4(x, *tiles, o, 640, 128, workspace=w, stream=st)
+                L.gemv_w4(x, *tiles, o, 4200, 128, workspace=w, stream=st)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_gemv_w4_captured(L):
+    """Calls with and without a launch that converts, captured together and replayed on another stream."""
+    g = gen(16)
+    sizes = [(20, 6000, 1032), (64, 2111, 1000), (12, 300, 512), (8, 500, 2048), (3, 200, 256)]
+    made = []
+    for B, N, K in sizes:
+        made.append((torch.randn(B, K, generator=g).to(torch.bfloat16).cuda(), laid_out(L, *weights(N, K, 64, True, g), 64), N,
+                     torch.empty(B, N, device=DEV), torch.empty(B, N, device=DEV)))
+    for x, tiles, N, a, _ in made:
+        L.gemv_w4(x, *tiles, a, N, 64)
+    torch.cuda.synchronize()
+    graph, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        for x, tiles, N, _, b in made:
+            L.gemv_w4(x, *tiles, b, N, 64)
+    with torch.cuda.stream(s):
+        for _ in range(3):
+            graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for _, _, _, a, b in made)
 
 
 def test_gemv_w4_rows_do_not_meet(L):
     """NaN and infinities of one activation row make that row NaN and reach no other."""
     g = gen(5)
-    for B in (4, 12, 40):
-        plain = weights(96, 512, 64, True, g)
+    for B, N in ((4, 96), (12, 96), (40, 96), (12, 17000), (40, 7000)):
+        plain = weights(N, 512, 64, True, g)
         x = torch.randn(B, 512, generator=g).to(torch.bfloat16)
         x[1, 3], x[2, 100], x[3] = math.nan, math.inf, 0
-        out = torch.empty(B, 96, device=DEV)
-        L.gemv_w4(x.cuda(), *laid_out(L, *plain, 64), out, 96, 64)
+        out = torch.empty(B, N, device=DEV)
+        L.gemv_w4(x.cuda(), *laid_out(L, *plain, 64), out, N, 64)
         w = ref.w4_values(*plain, 64)
         want, bound = ref.gemv(x.nan_to_num(0, 0, 0), w, 64)
         keep = [b for b in range(B) if b not in (1, 2)]

@@ -88,7 +88,7 @@ CACHE = [dict(k_pool=None), dict(v_pool=None), dict(block_table=None), dict(page
 REFUSED = {
     "pop_k_gemv_w4": [dict(x=None), dict(codes=None), dict(scales=None), dict(out=None), dict(B=0), dict(N=0), dict(K=0), dict(K=12),
                       dict(mode=1), dict(mode=4), dict(group=16), dict(group=96), dict(group=0), dict(x=A + 8), dict(ldx=132),
-                      dict(ldx=120), dict(workspace=A + 8), dict(codes=A + 8), dict(scales=A + 4), dict(zeros=A + 4), dict(out=A + 2), dict(ldo=8),
+                      dict(ldx=120), dict(B=65536), dict(workspace=A + 8), dict(codes=A + 8), dict(scales=A + 4), dict(zeros=A + 4), dict(out=A + 2), dict(ldo=8),
                       dict(mode=3), dict(mode=3, N=256, ldo=128, n_valid=129), dict(mode=3, N=256, ldo=128, n_valid=-1),
                       dict(mode=3, N=256, ldo=128, n_valid=128, act=2)],
     "pop_k_rope_cache_tree": CACHE + [dict(x=None), dict(q_out=None), dict(rope_table=None), dict(x=A + 4), dict(ld_in=193),
@@ -107,8 +107,9 @@ REFUSED = {
 }
 NOSPACE = [("pop_k_rope_cache_tree", dict(pos0=63)), ("pop_k_tree_attention", dict(max_start=63)),
            ("pop_k_tree_attention", dict(max_start=65, start=A)), ("pop_k_tree_attention", dict(workspace_bytes=1 << 20)),
-           ("pop_k_tree_attention", dict(workspace=None)), ("pop_k_gemv_w4", dict(B=9)),
-           ("pop_k_gemv_w4", dict(B=9, workspace=A, workspace_bytes=4000)), ("pop_k_cache_keep", dict(pos0=61))]
+           ("pop_k_tree_attention", dict(workspace=None)), ("pop_k_gemv_w4", dict(B=9, N=1 << 16, ldo=1 << 16, K=1024, ldx=1024)),
+           ("pop_k_gemv_w4", dict(B=9, N=1 << 16, ldo=1 << 16, K=1024, ldx=1024, workspace=A, workspace_bytes=9000)),
+           ("pop_k_gemv_w4", dict(B=8, K=4096, ldx=4096)), ("pop_k_cache_keep", dict(pos0=61))]
 NOTHING = [("pop_k_rope_cache_tree", dict(max_rows=0)), ("pop_k_rope_cache_tree", dict(rows=0, cu_rows=A)),
            ("pop_k_tree_attention", dict(max_rows=0)), ("pop_k_tree_attention", dict(rows=0, cu_rows=A)),
            ("pop_k_cache_keep", dict(max_kept=0))]
