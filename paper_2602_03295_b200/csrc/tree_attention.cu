@@ -4,7 +4,8 @@
 // A tile is 128 (row, head) pairs of one kv head: K and V are read once for all of them. Few rows over a long cache are bound
 // by the cache's bytes, so what counts is that every SM reads all the time, whatever the sequences' lengths: the key tiles of
 // all (sequence, kv head, row tile) items form one line, and each CTA takes an equal stretch of it. An item that lies in one
-// stretch is finished there; the others leave (maximum, sum, output) of their part, and a second launch joins the parts.
+// stretch is finished there; the others leave (maximum, sum, output) of their part, and a second launch joins the parts. Short
+// items that fit the CTAs are not cut at all.
 // Warps of a CTA:
 //   4 softmax warps, a thread per (row, head): scores of 64 keys from TMEM, mask, maximum, exponentials, P in bf16 back over
 //       the scores. These dependent steps (1700 clocks) are what a CTA waits for; where a second CTA shares the SM that is
@@ -75,6 +76,7 @@ struct TreeDev {
   int rows_per_load;            // positions of a TMA load: min(page_size, 64)
   int room;                     // positions that a row of the block table has pages for
   int ctas;
+  int whole;                    // CTA c has item c and nothing else: no parts, and no second launch
   float scale_log2;             // log2(e) / sqrt(hd)
   float* partial;               // [2 per CTA] parts
   int* starts;                  // [batch + 1]: see plan_of
@@ -87,6 +89,10 @@ __host__ __device__ constexpr int part_floats(int hd) { return (hd + 4) * 128; }
 
 // Fewest tiles of a stretch: below, beginning and ending it costs more than its keys
 constexpr int MIN_SHARE = 2;
+// Where no item has more tiles than this and there are no more items than CTAs, each CTA has an item, and nothing is to be joined. us
+// so / in stretches: 1 x 5 rows of 50 5.6 / 10.7, 8 x 16 of up to 100 8.0 / 13.1, 1 x 5 of 180 8.3 / 11.1 (pages of 16: 10.6 / 11.0); with
+// four tiles 1 x 5 of 240 9.7 / 9.1 (14.7 / 10.9)
+constexpr int WHOLE_TILES = 3;
 
 __device__ __forceinline__ Seq seq_of(const TreeDev& p, int b, bool report) {
   const Drafts& d = p.a.d;
@@ -108,11 +114,20 @@ __device__ __forceinline__ Seq seq_of(const TreeDev& p, int b, bool report) {
   return x;
 }
 __device__ __forceinline__ int line_of(const TreeDev& p, const Seq& x) { return x.tiles * x.qts * p.a.n_kv; }
+// places of a sequence in what the CTAs share out
+__device__ __forceinline__ int places_of(const TreeDev& p, const Seq& x) { return p.whole ? x.qts * p.a.n_kv : line_of(p, x); }
 
 __device__ __forceinline__ int warp_add(int v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
+}
+// from the item that a CTA has to its tiles
+__device__ __forceinline__ void item_of(Plan& r) {
+  if (r.lo >= r.hi) return;
+  r.lo = (r.lo - r.base) * r.x.tiles;
+  r.hi = r.lo + r.x.tiles;
+  r.base = 0;
 }
 // Finds the stretch of CTA `cta`, by a whole warp. `starts`, if given, gets the place where each sequence begins and, behind them,
 // the tiles of a stretch: what the second launch asks for.
@@ -121,7 +136,7 @@ __device__ __forceinline__ Plan plan_of(const TreeDev& p, int cta, int* starts) 
   if (batch == 1) {                                            // nothing to add up (1 x 5 rows of 300: 10.9 us against 11.3)
     Plan r;
     r.x = seq_of(p, 0, cta == 0 && lane == 0);
-    const int total = line_of(p, r.x), share = max((total + p.ctas - 1) / p.ctas, MIN_SHARE);
+    const int total = places_of(p, r.x), share = p.whole ? 1 : max((total + p.ctas - 1) / p.ctas, MIN_SHARE);
     r.lo = (int)min((int64_t)cta * share, (int64_t)total);
     r.hi = min(r.lo + share, total);
     r.b = r.base = 0;
@@ -129,6 +144,7 @@ __device__ __forceinline__ Plan plan_of(const TreeDev& p, int cta, int* starts) 
       starts[0] = 0;
       starts[1] = share;
     }
+    if (p.whole) item_of(r);
     return r;
   }
   Seq x;
@@ -137,12 +153,11 @@ __device__ __forceinline__ Plan plan_of(const TreeDev& p, int cta, int* starts) 
     mine = 0;
     if (b0 + lane < batch) {
       x = seq_of(p, b0 + lane, cta == 0);
-      mine = line_of(p, x);
+      mine = places_of(p, x);
     }
     total += warp_add(mine);
   }
-  int share = (total + p.ctas - 1) / p.ctas;
-  if (share < MIN_SHARE) share = MIN_SHARE;
+  const int share = p.whole ? 1 : max((total + p.ctas - 1) / p.ctas, MIN_SHARE);
   Plan r;
   r.lo = (int)min((int64_t)cta * share, (int64_t)total);
   r.hi = min(r.lo + share, total);
@@ -153,7 +168,7 @@ __device__ __forceinline__ Plan plan_of(const TreeDev& p, int cta, int* starts) 
       mine = 0;
       if (b0 + lane < batch) {
         x = seq_of(p, b0 + lane, false);
-        mine = line_of(p, x);
+        mine = places_of(p, x);
       }
     }
     int incl = mine;
@@ -179,6 +194,7 @@ __device__ __forceinline__ Plan plan_of(const TreeDev& p, int cta, int* starts) 
     base += __shfl_sync(0xffffffffu, incl, 31);
   }
   if (starts != nullptr && lane == 0) starts[batch] = share;
+  if (p.whole) item_of(r);
   return r;
 }
 
@@ -341,7 +357,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     __syncwarp();
     chain_wait();
     const int raised = lane == 0 ? *reinterpret_cast<const volatile int*>(p.status) : 0;
-    plan = plan_of(p, blockIdx.x, blockIdx.x == 0 ? p.starts : nullptr);
+    plan = plan_of(p, blockIdx.x, blockIdx.x == 0 && !p.whole ? p.starts : nullptr);
     if (__shfl_sync(0xffffffffu, gave_up(raised) ? 1 : 0, 0)) plan.hi = plan.lo;     // a call that is not to run
     if (lane == 0) s.plan = plan;
     __syncwarp();
@@ -798,6 +814,8 @@ int launch_t(const TreeAttnArgs& a, TreeDev& p, cudaStream_t s) {
   // two parts per CTA at most: of the item that it begins with and of the one that it ends with
   const size_t parts = (size_t)2 * p.ctas * part_floats(HD), need = (parts + a.d.batch + 1) * 4;
   p.starts = reinterpret_cast<int*>(p.partial + parts);
+  const int64_t tiles = ((int64_t)a.d.pos0 + a.d.max_rows + BKV - 1) / BKV, items = (int64_t)a.d.batch * a.n_kv * qts;
+  p.whole = tiles <= WHOLE_TILES && items <= p.ctas;
   if (a.workspace_bytes < need) return POP_E_NOSPACE;
   p.status = status_word();
   if (!p.status) return POP_E_CUDA;
@@ -820,14 +838,15 @@ int launch_t(const TreeAttnArgs& a, TreeDev& p, cudaStream_t s) {
       return POP_E_CUDA;
   }
   ProfScope prof(PROF_ATTENTION, 4.0 * HD * a.n_q * a.d.rows * ((double)a.d.pos0 + a.d.max_rows), s);
-  if (launch_chained(tree_attn_kernel<HD>, dim3(p.ctas), dim3(C::THREADS), smem, s, tq, tk, tv, p) != cudaSuccess)
+  if (launch_chained(tree_attn_kernel<HD>, dim3(p.whole ? (int)items : p.ctas), dim3(C::THREADS), smem, s, tq, tk, tv, p) != cudaSuccess)
     return POP_E_CUDA;
   count_launch();
+  if (p.whole) return POP_OK;
   const int pairs = a.d.max_rows < p.per ? a.d.max_rows * p.G : p.per * p.G;
   // Few items of many parts are joined by more threads, which each have more loads in flight: 1 x 64 rows of 8192 27.3 us against
   // 28.6, 1 x 16 of 2000 13.4 against 14.4. Many items (16 x 12 rows, window 1024: 48.4 against 43.1) or few parts (1 x 5 of 300: 11.3
   // against 10.9) would lose.
-  const int64_t share = (line + p.ctas - 1) / p.ctas, tiles = ((int64_t)a.d.pos0 + a.d.max_rows + BKV - 1) / BKV;
+  const int64_t share = (line + p.ctas - 1) / p.ctas;
   const bool wide = tiles > 8 * (share < MIN_SHARE ? MIN_SHARE : share) && a.n_kv * qts * (HD / 8) * a.d.batch <= 2 * device_sms();
   if (launch_chained(wide ? tree_merge_kernel<HD, 4, 16> : tree_merge_kernel<HD, 8, 8>,
                      dim3((unsigned)(a.n_kv * qts), HD / (wide ? 4 : 8), a.d.batch), dim3((pairs + 31) & ~31), 0, s, p) != cudaSuccess)

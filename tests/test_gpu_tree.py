@@ -374,7 +374,11 @@ ATTEND = [  # rows, starts, n_q, n_kv, hd, page, window, kind
     ([9, 8, 40], [5, 0, 200], 7, 1, 128, 128, 0, "bits"), ([2, 2], [64, 128], 128, 1, 64, 64, 0, "tree"),
     ([1] * 70, [(37 * i) % 400 for i in range(70)], 8, 8, 128, 16, 0, "tree"), ([6], [20000], 8, 2, 64, 256, 0, "tree"),
     ([6, 1], [9000, 12], 3, 1, 256, 128, 0, "bits"), ([30, 31], [1100, 0], 24, 1, 128, 128, 0, "tree"),
-    ([4] * 40, [0] * 40, 2, 1, 64, 16, 0, "chain"), ([300], [0], 4, 4, 128, 128, 0, "chain"), ([500], [70], 2, 1, 256, 16, 64, "chain")]
+    ([4] * 40, [0] * 40, 2, 1, 64, 16, 0, "chain"), ([300], [0], 4, 4, 128, 128, 0, "chain"), ([500], [70], 2, 1, 256, 16, 64, "chain"),
+    # short ones, an item to a CTA
+    ([3, 0, 33, 1, 17], [17, 5, 0, 126, 100], 6, 3, 128, 32, 0, "tree"), ([20, 3], [150, 40], 8, 2, 256, 64, 30, "tree"),
+    ([130, 3], [50, 10], 8, 4, 64, 16, 0, "bits"), ([2] * 60, [(7 * i) % 180 for i in range(60)], 4, 2, 128, 64, 0, "tree"),
+    ([60, 70], [120, 100], 16, 1, 64, 128, 0, "tree")]
 
 
 def drafts(rows, kind, g):
