@@ -411,12 +411,15 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         ahead.pg1 = entry(w, ahead.first + 32 + lane);
       }
       const int kv0 = w.j * BKV, live = min(loads, (w.x.start + w.x.n - kv0 + p.rows_per_load - 1) / p.rows_per_load);
+      // Pages in front of every row's window may have been given back: they are not looked at. What the ring has in their
+      // places is masked (K) and cleared (V); the load that has the window's first position is always among the live ones.
+      const int from = p.a.window > 0 ? max(0, max(0, w.x.start - p.a.window + 1) - kv0) / p.rows_per_load : 0;
       if (!mbar_wait_relaxed(&s.kv_empty[stage], phase ^ 1)) {
         ok = false;
         return;
       }
-      if (lane == 0) mbar_expect_tx(&s.kv_full[stage], live * p.rows_per_load * HD * 2);
-      for (int r = 0; r < live; ++r) {
+      if (lane == 0) mbar_expect_tx(&s.kv_full[stage], (live - from) * p.rows_per_load * HD * 2);
+      for (int r = from; r < live; ++r) {
         const int k = l0 + r - ahead.first;
         const int page = k < 32 ? __shfl_sync(0xffffffffu, ahead.pg0, k) : __shfl_sync(0xffffffffu, ahead.pg1, k - 32);
         if (lane == 0) {

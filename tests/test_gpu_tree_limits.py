@@ -1,0 +1,64 @@
+"""The operators of a step that checks drafted tokens at the ends of what their header allows."""
+import pytest
+import torch
+
+from tests import test_gpu_tree as base
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+@pytest.fixture(scope="module")
+def L():
+    import paper_2602_03295_b200 as pk
+    return pk.lib()
+
+
+@pytest.fixture(autouse=True)
+def _clean_status(request):
+    yield
+    if "L" in request.fixturenames:
+        assert request.getfixturevalue("L").dll.pop_k_status(None) == 0
+
+
+def int32(v):
+    return torch.tensor(v, dtype=torch.int32, device=DEV)
+
+
+# ---------------------------------------------------------------------------------------------- windows
+FREED = [  # rows, starts, n_q, n_kv, hd, page, window: cut into stretches, and short ones that go whole to a CTA
+    ([20, 3, 9], [500, 90, 210], 8, 2, 128, 16, 100), ([20, 3, 9], [500, 90, 210], 4, 2, 64, 32, 100),
+    ([9, 5], [3000, 777], 4, 2, 256, 16, 300), ([40], [700], 8, 8, 128, 32, 1), ([33, 20], [1000, 460], 4, 1, 128, 128, 200),
+    ([12, 5], [150, 99], 8, 2, 128, 16, 30), ([6], [120], 4, 2, 256, 32, 40), ([70], [100], 4, 4, 64, 16, 5)]
+
+
+@pytest.mark.parametrize("entry", [-1, 1 << 20])
+@pytest.mark.parametrize("rows,starts,n_q,n_kv,hd,page,window", FREED)
+def test_entries_of_pages_in_front_of_every_window(L, rows, starts, n_q, n_kv, hd, page, window, entry):
+    """Whole pages in front of start - window + 1 may have been given back: any entry, with no effect and no complaint. The
+    first page that a row sees is still looked at."""
+    from paper_2602_03295_b200 import POP_E_INVALID
+    g = base.gen(sum(rows) + page)
+    k, v, table = base.pools(page, len(rows), max(r + s for r, s in zip(rows, starts)), n_kv, hd, page)
+    base.poison(k, v, table, rows, starts, page, window)
+    _, depth, mask = base.drafts(rows, "tree", g)
+    q = torch.randn(sum(rows), n_q * hd, generator=g).to(torch.bfloat16).cuda()
+    kd, vd = k.cuda(), v.cuda()
+
+    def call(entries):
+        out = torch.full_like(q, 7.0)
+        L.tree_attention(q, kd, vd, entries.cuda(), out, n_q, n_kv, hd, max(rows), max(starts), start=int32(starts),
+                         cu_rows=base.prefix(rows).cuda(), mask=mask.cuda(), depth=depth.cuda(), window=window)
+        return out
+
+    want, freed = call(table), table.clone()
+    assert L.dll.pop_k_status(None) == 0
+    for b, s in enumerate(starts):
+        freed[b, :max(0, s - window + 1) // page] = entry
+    assert not torch.equal(freed, table)
+    got = call(freed)
+    assert L.dll.pop_k_status(None) == 0
+    assert torch.equal(got, want)
+    freed[0, max(0, starts[0] - window + 1) // page] = entry
+    call(freed)
+    assert L.dll.pop_k_status(None) == POP_E_INVALID
