@@ -300,7 +300,7 @@ __device__ __forceinline__ uint64_t seen_of(const TreeDev& p, const Seq& x, int 
     vis &= ones(ctx + x.n);
   }
   if (window > 0) {
-    const int hidden = x.start + depth - window + 1 - kv0;     // positions in front of the window
+    const int hidden = ctx > 0 ? ctx + depth - window + 1 : 0; // positions in front of the window
     if (hidden > 0) vis &= ~ones(min(hidden, ctx));
     if (ctx < 64 && depth >= window) {                         // drafted slots that lie so far up the tree
       for (uint64_t m = vis & ~ones(ctx); m != 0; m &= m - 1) {
@@ -561,7 +561,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         uint32_t vis[KEYS / 32];
 #pragma unroll
         for (int c = 0; c < KEYS / 32; ++c) vis[c] = used ? ~0u : 0u;
-        if (used && (kv0 + BKV > x.start || (p.a.window > 0 && kv0 + p.a.window <= x.start + depth))) {
+        if (used && (kv0 + BKV > x.start || (p.a.window > 0 && kv0 <= x.start + depth - p.a.window))) {
           const uint64_t v = seen_of(p, x, i, prow, first, depth, kv0);
           if constexpr (HALVES == 2) {
             vis[0] = half ? (uint32_t)(v >> 32) : (uint32_t)v;
@@ -878,6 +878,7 @@ int launch_tree_attention(const TreeAttnArgs& a, cudaStream_t s) {
   if (a.d.max_rows == 0 || a.d.rows == 0) return POP_OK;
   TreeDev p{};
   p.a = a;
+  if (a.window - 65536 >= a.d.pos0) p.a.window = 0;            // beyond the reach of every row: depths are below 65536
   p.G = a.n_q / a.n_kv;
   p.per = 128 / p.G;
   p.room = room < 0x7fff0000 ? (int)room : 0x7fff0000;

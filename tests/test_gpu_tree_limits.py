@@ -62,3 +62,21 @@ def test_entries_of_pages_in_front_of_every_window(L, rows, starts, n_q, n_kv, h
     freed[0, max(0, starts[0] - window + 1) // page] = entry
     call(freed)
     assert L.dll.pop_k_status(None) == POP_E_INVALID
+
+
+@pytest.mark.parametrize("rows,starts,hd,window", [
+    ([300, 7], [1000, 64], 128, 0x7ffffff0), ([130, 9], [20, 500], 64, 0x7ffffff0), ([40], [3000], 256, 0x7ffffff0),
+    ([300, 7], [1000, 64], 128, 1300), ([70, 60], [100, 90], 128, 0x7fffffe0), ([200], [500], 64, 1 << 30)])
+def test_windows_that_hide_nothing(L, rows, starts, hd, window):
+    """A window that reaches beyond every position is no window, up to the largest that is taken."""
+    n_q, n_kv, page = 4, 2, 64
+    g = base.gen(hd + sum(rows))
+    k, v, table = (t.cuda() for t in base.pools(hd, len(rows), max(r + s for r, s in zip(rows, starts)), n_kv, hd, page))
+    _, depth, mask = base.drafts(rows, "tree", g)
+    q = torch.randn(sum(rows), n_q * hd, generator=g).to(torch.bfloat16).cuda()
+    outs = []
+    for w in (0, window):
+        outs.append(torch.empty_like(q))
+        L.tree_attention(q, k, v, table, outs[-1], n_q, n_kv, hd, max(rows), max(starts), start=int32(starts),
+                         cu_rows=base.prefix(rows).cuda(), mask=mask.cuda(), depth=depth.cuda(), window=w)
+    assert torch.equal(*outs)
