@@ -293,7 +293,7 @@ int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int
  * pop_k_gemv_w4: pop_k_gemv with such weights: out[b][n] = sum_k x[b][k] W[n][k], x bf16 [B][ldx] (16-byte aligned, ldx and K
  * multiples of 8), B up to 65535 (made for 1 to some dozens of rows). Modes as pop_k_gemv: 0 fp32 store, 2 fp32 +=, 3 gated -> bf16
  * (N a multiple of 256: 128 gate rows, then the 128 matching up rows; act 0 SiLU, 1 tanh-GELU). The products of
- * codes and activations are exact (of activations within 2^-27 of the largest of their 128 inputs; smaller ones are off by at
+ * codes and activations are exact (of activations within 2^-28 of the largest of their 128 inputs; smaller ones are off by at
  * most 2^-36 of it); sums are fp32, in an order that depends on the sizes alone. An activation row with an infinite or NaN
  * input gives a row of NaN. Weights are read ahead, before the kernel in front of the call on the stream has ended (as
  * pop_k_gemv reads its own): whoever writes them on the GPU synchronises before the first call that uses them. */

@@ -87,8 +87,8 @@ __global__ void __launch_bounds__(256) gemv4_convert_kernel(const bf16* __restri
 
 // A code in the low bits of an f16 is code * 2^-24, in bits 4 .. 7 code * 2^-20: subnormals are linear, so that a mask alone
 // makes a tensor-core operand of two codes of a word, and one shift the other half of them. The activations go in as f16 too,
-// those of a chunk of 128 inputs times a power of two that brings their largest near 2^15 (bf16 values stay exact down to
-// 2^-27 of it, and within 2^-36 of it below), inputs that meet the codes of bits 4 .. 7 divided by 16. So all products are
+// those of a chunk of 128 inputs times a power of two that brings their largest to 2^15 or more (bf16 values stay exact down to
+// 2^-28 of it, and within 2^-36 of it below), inputs that meet the codes of bits 4 .. 7 divided by 16. So all products are
 // exact; a group's sum is built in the MMA's fp32 accumulator from zero and enters the row's fp32 sum as
 //   scale (2^-shift sum_k code_k x'_k - zero sum_k x_k),   the second sum made once with the conversion.
 // (Subtracting the zero from every pair of codes took 32 more operations per KB of codes; codes as bf16 128 + code, 64.)

@@ -60,9 +60,9 @@ __device__ __forceinline__ uint4 convert8(const uint4& v, float& sum, float& uni
   for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
 #pragma unroll
   for (int o = 1; o < GRP / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  // a power of two that brings the largest to 2^14 .. 2^15, as far as fp32 has it (an infinity or NaN stays what it is, beside
-  // values that no longer matter)
-  const int sh = m == 0 ? 0 : min(14 + 127 - (int)(m >> 7), 126);
+  // a power of two that brings the largest to 2^15 .. 65280, which f16 still has, as far as fp32 has it (an infinity or NaN stays
+  // what it is, beside values that no longer matter). The smallest step of f16, times 16, is then 2^-35 of the largest at most
+  const int sh = m == 0 ? 0 : min(15 + 127 - (int)(m >> 7), 126);
   const float f = __uint_as_float((uint32_t)(127 + sh) << 23), f16th = f * 0.0625f;
   unit = __uint_as_float((uint32_t)(127 - sh) << 23);
   return make_uint4(pack_f16(x[0] * f, x[1] * f), pack_f16(x[2] * f16th, x[3] * f16th), pack_f16(x[4] * f, x[5] * f),

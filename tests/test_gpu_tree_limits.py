@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from tests import test_gpu_tree as base
+from tests import tree_ref as ref
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -80,3 +81,29 @@ def test_windows_that_hide_nothing(L, rows, starts, hd, window):
         L.tree_attention(q, k, v, table, outs[-1], n_q, n_kv, hd, max(rows), max(starts), start=int32(starts),
                          cu_rows=base.prefix(rows).cuda(), mask=mask.cuda(), depth=depth.cuda(), window=w)
     assert torch.equal(*outs)
+
+
+# ---------------------------------------------------------------------------------------------- 4-bit weights
+PLACES = [(1, 512, 512), (2, 256, 256), (8, 2048, 2048), (9, 4096, 2048), (30, 4096, 1024), (64, 4096, 512)]
+
+
+@pytest.mark.parametrize("B,N,K", PLACES)
+def test_gemv_w4_small_inputs_beside_a_large_one(L, B, N, K):
+    """Every chunk of 128 inputs has a largest of 1; each row of weights takes one input alone, with code 15 and zero 0. Inputs
+    down to 2^-28 are exact there, smaller ones off by at most 2^-36 times the code (and one rounding of fp32)."""
+    g = base.gen(B)
+    x = (1 + torch.randint(0, 128, (B, K), generator=g) / 128) * torch.exp2(-torch.randint(20, 40, (B, K), generator=g).float())
+    x *= torch.randint(0, 2, (B, K), generator=g) * 2 - 1
+    x[:, ::128] = 1
+    x = x.to(torch.bfloat16)
+    at = torch.arange(N) % K
+    codes = torch.zeros(N, K, dtype=torch.uint8)
+    codes[torch.arange(N), at] = 15
+    tiles = base.laid_out(L, codes, torch.ones(N, K // 128, dtype=torch.bfloat16), torch.zeros(N, K // 128, dtype=torch.uint8), 128)
+    out = torch.empty(B, N, device=DEV)
+    L.gemv_w4(x.cuda(), *tiles, out, N, 128)
+    want = 15 * x.double()[:, at]
+    exact = want.abs() >= 15 * 2.0 ** -28
+    assert bool(exact.any()) and bool((~exact).any())
+    assert torch.equal(out.cpu().double()[exact], want[exact])
+    base.within(out, want, 15 * 2.0 ** -36 + ref.FP32 * want.abs())
