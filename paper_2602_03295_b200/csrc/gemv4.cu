@@ -65,7 +65,8 @@ __global__ void __launch_bounds__(256) gemv4_convert_kernel(const bf16* __restri
   chain_wait();
   const int h = threadIdx.x & 15, c = blockIdx.x * 16 + (threadIdx.x >> 4), r = blockIdx.y, k = c * 128 + h * 8;
   float sum, unit;
-  const uint4 q = convert8<GRP>(c < kt && k < K ? *reinterpret_cast<const uint4*>(x + r * ldx + k) : make_uint4(0, 0, 0, 0), sum, unit);
+  const uint4 q = convert8<GRP>(c < kt && k < K ? *reinterpret_cast<const uint4*>(x + r * ldx + k) : make_uint4(0, 0, 0, 0),
+                                cols == 8 ? sum_scale(zeros != 0) : -sum_scale(zeros != 0), sum, unit);
   if (c >= kt) return;
   uint8_t* slab = out + r / cols * slab_bytes(cols, GPC, kt);
   if (cols == 8) {
@@ -82,7 +83,7 @@ __global__ void __launch_bounds__(256) gemv4_convert_kernel(const bf16* __restri
                                                  : slab + (c >> 1) * slab_bytes(cols, GPC, 2) + cols * 512 + (c & 1) * ((1 + GPC) * cols * 4)) +
               r % cols;
   if (h == 0) to[0] = unit;
-  if (h % (GRP / 8) == 0) to[(1 + h / (GRP / 8)) * cols] = sum * (cols == 8 ? sum_scale(zeros != 0) : -sum_scale(zeros != 0));
+  if (h % (GRP / 8) == 0) to[(1 + h / (GRP / 8)) * cols] = sum;
 }
 
 // A code in the low bits of an f16 is code * 2^-24, in bits 4 .. 7 code * 2^-20: subnormals are linear, so that a mask alone
@@ -245,12 +246,12 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
           for (int i = 0; i < 4; ++i) {
             if (left <= i * (WARPS * 2)) break;     // the same for the warp
             float sum, unit;
-            const uint4 q = convert8<GRP>(v[i], sum, unit);
+            const uint4 q = convert8<GRP>(v[i], sum_scale(ZEROS), sum, unit);
             if (ri[i] < rows) {
               *reinterpret_cast<uint4*>(s_x + ri[i] * xs + ci[i] * 256 + h * 16) = q;
               float* to = s_sum + ci[i] * (1 + GPC) * COLS + ri[i];
               if (h == 0) to[0] = unit;
-              if (h % (GRP / 8) == 0) to[(1 + h / (GRP / 8)) * COLS] = sum * sum_scale(ZEROS);
+              if (h % (GRP / 8) == 0) to[(1 + h / (GRP / 8)) * COLS] = sum;
             }
           }
         }

@@ -42,9 +42,10 @@ __device__ __forceinline__ float act_of(float g, int act) {
 }
 
 // What a lane of a half-warp makes of its 8 of a chunk's 128 activations: f16 values times a common power of two, those that
-// meet codes of bits 4 .. 7 divided by 16; `unit` takes them back, `sum` is that of the lane's group.
+// meet codes of bits 4 .. 7 divided by 16; `unit` takes them back, `sum` is that of the lane's group times the power of two
+// `of_sum`, which each value is multiplied with before it is added: the plain sum may leave fp32.
 template <int GRP>
-__device__ __forceinline__ uint4 convert8(const uint4& v, float& sum, float& unit) {
+__device__ __forceinline__ uint4 convert8(const uint4& v, float of_sum, float& sum, float& unit) {
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   uint32_t m = 0;
   float x[8];
@@ -54,7 +55,7 @@ __device__ __forceinline__ uint4 convert8(const uint4& v, float& sum, float& uni
     m = max(m, max(w[j] & 0x7fffu, (w[j] >> 16) & 0x7fffu));
     x[2 * j] = __uint_as_float(w[j] << 16);
     x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-    sum += x[2 * j] + x[2 * j + 1];
+    sum += fmaf(x[2 * j], of_sum, x[2 * j + 1] * of_sum);
   }
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -70,6 +71,5 @@ __device__ __forceinline__ uint4 convert8(const uint4& v, float& sum, float& uni
 }
 // Sums of groups in the unit of code products (2^-24), without zeros times the 8 that stands for them
 __host__ __device__ constexpr float sum_scale(bool zeros) { return (zeros ? 1.f : 8.f) * 0x1p-24f; }
-
 
 }  // namespace pop

@@ -107,3 +107,19 @@ def test_gemv_w4_small_inputs_beside_a_large_one(L, B, N, K):
     assert bool(exact.any()) and bool((~exact).any())
     assert torch.equal(out.cpu().double()[exact], want[exact])
     base.within(out, want, 15 * 2.0 ** -36 + ref.FP32 * want.abs())
+
+
+@pytest.mark.parametrize("B,N,K", [(1, 100, 512), (2, 40, 136), (7, 600, 1536), (12, 64, 256), (9, 4200, 2056), (24, 4200, 1032), (50, 2100, 1032)])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_gemv_w4_whose_sums_of_inputs_leave_fp32(L, B, N, K, zeros):
+    """Inputs near the largest bf16, all of one sign: their sums are beyond fp32, the products are not."""
+    g = base.gen(B + K)
+    codes, _, z = base.weights(N, K, 64, zeros, g)
+    scales = torch.full((N, -(-K // 64)), 2.0 ** -30, dtype=torch.bfloat16)
+    x = ((1 + torch.rand(B, K, generator=g)) * 2.0 ** 126).to(torch.bfloat16)
+    assert float(x.double()[:, :64].sum(1).min()) > 2.0 ** 128
+    out = torch.empty(B, N, device=DEV)
+    L.gemv_w4(x.cuda(), *base.laid_out(L, codes, scales, z, 64), out, N, 64)
+    want = x.double() @ ref.w4_values(codes, scales, z, 64).t()
+    # the sums of code x and zero x are rounded apart: magnitudes of 15 + 15 steps for each weight
+    base.within(out, want, ref.gemv(x, torch.full((N, K), 30 * 2.0 ** -30, dtype=torch.float64), 64)[1])
