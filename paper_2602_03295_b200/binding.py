@@ -591,7 +591,9 @@ class PopLibrary:
     def gemv_w4(self, x, codes, scales, zeros, out, n, group, mode=0, act=0, n_valid=None, workspace=None, stream=None):
         """pop_k_gemv_w4: x bf16 [B, K]; codes uint8 [ceil(n / 16), ceil(K / 128), 16, 64], scales bf16 and zeros uint8 (or
         None) [.., .., 16, 128 / group] as `pack_w4` lays them out; out fp32 [B, n], or bf16 [B, n_valid] (n / 2 if not given)
-        for mode 3. `workspace` (pop_k_gemv_w4_workspace_bytes of any dtype) is allocated if it is needed and not given."""
+        for mode 3. `workspace` (pop_k_gemv_w4_workspace_bytes of any dtype) is allocated if it is needed and not given. The
+        weights are read before the kernel in front of the call on the stream has ended: tiles of pack_w4 and quantize_w4 are
+        complete when these return; whoever else writes or copies them on the GPU synchronises before the first call."""
         here = self._here(x, (codes, scales, zeros, out, workspace), "gemv_w4")
         B, K = x.shape
         ldx, inner = x.stride()
@@ -732,7 +734,8 @@ def lib() -> PopLibrary:
 def pack_w4(codes, scales, zeros=None, group=128):
     """4-bit weights as pop_k_gemv_w4 reads them, from codes uint8 [N, K] (0 .. 15), scales [N, ceil(K / group)] and zeros uint8
     of the scales' shape or None (8), group 32, 64 or 128: (codes, scales, zeros) in tiles. Done once, when weights are loaded,
-    on the device that they are on."""
+    on the device that they are on. Waits for the stream: gemv_w4 reads weights ahead of the stream's order, so they have to be
+    there before it is called."""
     n, k = codes.shape
     if group not in (32, 64, 128) or scales.shape != (n, -(-k // group)) or (zeros is not None and zeros.shape != scales.shape):
         raise PopError(POP_E_INVALID, "pack_w4: scales and zeros are [N, ceil(K / group)] for a group of 32, 64 or 128")
@@ -747,13 +750,16 @@ def pack_w4(codes, scales, zeros=None, group=128):
         v = torch.nn.functional.pad(v.to(dtype), (0, kt * per - v.shape[1], 0, nt * 16 - n))
         return v.view(nt, 2, 8, kt, per).permute(0, 3, 2, 1, 4).reshape(nt, kt, 16, per).contiguous()
 
-    return (tiles.view(nt, kt, 16, 64), grouped(scales, torch.bfloat16),
-            None if zeros is None else grouped(zeros, torch.uint8))
+    laid = (tiles.view(nt, kt, 16, 64), grouped(scales, torch.bfloat16), None if zeros is None else grouped(zeros, torch.uint8))
+    if codes.is_cuda:
+        torch.cuda.current_stream(codes.device).synchronize()
+    return laid
 
 
 def quantize_w4(w, group=128, symmetric=True):
     """Round-to-nearest 4-bit weights of w [N, K], laid out by `pack_w4`. Symmetric: scale = bf16(max|w| / 7) of a group, code
-    = w / scale rounded, + 8. Else scale = bf16((max - min) / 15) with 0 between min and max, zero = -min / scale rounded."""
+    = w / scale rounded, + 8. Else scale = bf16((max - min) / 15) with 0 between min and max, zero = -min / scale rounded. Waits
+    for the stream, as `pack_w4` does."""
     n, k = w.shape
     groups = -(-k // group)
     x = torch.nn.functional.pad(w.float(), (0, groups * group - k)).view(n, groups, group)

@@ -123,3 +123,19 @@ def test_gemv_w4_whose_sums_of_inputs_leave_fp32(L, B, N, K, zeros):
     want = x.double() @ ref.w4_values(codes, scales, z, 64).t()
     # the sums of code x and zero x are rounded apart: magnitudes of 15 + 15 steps for each weight
     base.within(out, want, ref.gemv(x, torch.full((N, K), 30 * 2.0 ** -30, dtype=torch.float64), 64)[1])
+
+
+def test_packed_weights_are_there(L):
+    """The products read weights ahead of the stream's order: tiles made on the GPU are complete when their maker returns."""
+    from paper_2602_03295_b200 import pack_w4, quantize_w4
+    w = torch.randn(8192, 4096, device=DEV)
+    codes, scales = torch.zeros(8192, 4096, dtype=torch.uint8, device=DEV), torch.ones(8192, 32, device=DEV)
+    zeros = torch.zeros(8192, 32, dtype=torch.uint8, device=DEV)
+    torch.cuda.synchronize()
+    for make in (lambda: pack_w4(codes, scales), lambda: pack_w4(codes, scales, zeros), lambda: quantize_w4(w), lambda: quantize_w4(w, symmetric=False)):
+        for stream in (torch.cuda.current_stream(), torch.cuda.Stream()):
+            with torch.cuda.stream(stream):
+                make()
+                made = stream.query()
+            torch.cuda.synchronize()
+            assert made
