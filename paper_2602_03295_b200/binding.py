@@ -612,8 +612,10 @@ class PopLibrary:
         if B == 0:
             return out
         need = self.dll.pop_k_gemv_w4_workspace_bytes(B, n, K, group) if B > 2 else 0
-        if need and workspace is None:
-            workspace = self._scratch(need, x.device, stream)
+        if workspace is None:
+            workspace = self._scratch(need, x.device, stream) if need else None
+        elif not workspace.is_contiguous():
+            raise PopError(POP_E_INVALID, "gemv_w4: workspace has to be contiguous")
         code = self.dll.pop_k_packed(0, _PACK_GEMV(
             x.data_ptr(), ldx, codes.data_ptr(), scales.data_ptr(), 0 if zeros is None else zeros.data_ptr(), group,
             0 if workspace is None else workspace.data_ptr(),

@@ -1,0 +1,49 @@
+"""Refusals of the calls that check drafted tokens which need no GPU, beside those of tests/test_tree.py."""
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def library():
+    from paper_2602_03295_b200 import _build, binding
+    _build.build()
+    return binding.PopLibrary()
+
+
+class Recorder:
+    """Stands for the library: takes every call, and does nothing."""
+
+    def __init__(self):
+        self.calls = 0
+
+    def pop_k_gemv_w4_workspace_bytes(self, *args):
+        return 1 << 16
+
+    def pop_k_packed(self, *args):
+        self.calls += 1
+        return 0
+
+
+@pytest.fixture
+def recorded(monkeypatch):
+    """A binding on tensors of the CPU whose calls reach a recorder instead of the library."""
+    from paper_2602_03295_b200 import binding
+    monkeypatch.setattr(binding.PopLibrary, "_here", staticmethod(lambda t, others, what: 0))
+    lib = object.__new__(binding.PopLibrary)
+    lib.dll = Recorder()
+    return lib
+
+
+def test_workspaces_with_gaps_are_refused(recorded):
+    """The products write their workspace as one piece: views with gaps, and one element expanded, are none."""
+    from paper_2602_03295_b200 import PopError
+    x, out = torch.zeros(9, 256, dtype=torch.bfloat16), torch.zeros(9, 16)
+    tiles = torch.zeros(1, 2, 16, 64, dtype=torch.uint8), torch.zeros(1, 2, 16, 1, dtype=torch.bfloat16), None
+    recorded.gemv_w4(x, *tiles, out, 16, 128, workspace=torch.zeros(1 << 16, dtype=torch.uint8))
+    recorded.gemv_w4(x, *tiles, out, 16, 128, workspace=torch.zeros(1 << 8, 1 << 6))
+    assert recorded.dll.calls == 2
+    for bad in (torch.zeros(1, dtype=torch.uint8).expand(1 << 16), torch.zeros(1 << 17, dtype=torch.uint8)[::2],
+                torch.zeros(1 << 8, 1 << 9, dtype=torch.uint8)[:, :1 << 8]):
+        with pytest.raises(PopError):
+            recorded.gemv_w4(x, *tiles, out, 16, 128, workspace=bad)
+    assert recorded.dll.calls == 2
