@@ -346,7 +346,8 @@ int pop_k_tree_attention(const void* q, int64_t ldq, int32_t rows, const int32_t
                          int32_t head_dim, int32_t window, void* stream);
 
 /* Keeps the accepted path of every sequence: the entries of drafted slots kept[b][0] < kept[b][1] < ... move to slots 0, 1,
- * ... of the draft (cache positions start + i), in `layers` consecutive layers (layer_stride elements apart) of K and V.
+ * ... of the draft (cache positions start + i), in `layers` consecutive layers (layer_stride elements apart, a page of one
+ * layer at least) of K and V.
  * kept: device int32 [batch][ld_kept], the first n_kept[b] (device int32 [batch], at most max_kept; NULL: max_kept) of a
  * row; max_kept <= 1024. start / pos0 as above. The other entries stay as they are. A sequence whose list does not rise or
  * leaves its block table or the pool is left as it is (status word). */

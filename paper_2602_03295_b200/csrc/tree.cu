@@ -217,7 +217,8 @@ int launch_cache_keep(const KeepArgs& a, cudaStream_t s) {
       a.n_kv > 1024 || a.max_kept < 0 || a.max_kept > KEEP_LIST || a.pos0 < 0 || (a.batch > 1 && a.ld_kept < a.max_kept))
     return POP_E_INVALID;
   if (a.head_dim != 64 && a.head_dim != 128 && a.head_dim != 256) return POP_E_INVALID;
-  if (a.layers > 1 && a.layer_stride % 8) return POP_E_INVALID;
+  const int64_t page = (int64_t)a.c.page_size * a.n_kv * a.head_dim;
+  if (a.layers > 1 && (a.layer_stride % 8 || (a.layer_stride > -page && a.layer_stride < page))) return POP_E_INVALID;  // layers over each other
   if ((int64_t)a.c.num_pages * a.c.page_size > 0x7fffffff) return POP_E_INVALID;                    // pool rows are 32-bit numbers
   if (!a.start && (int64_t)a.pos0 + a.max_kept > (int64_t)a.c.max_pages * a.c.page_size) return POP_E_NOSPACE;
   if (a.max_kept == 0) return POP_OK;

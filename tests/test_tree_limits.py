@@ -47,3 +47,18 @@ def test_workspaces_with_gaps_are_refused(recorded):
         with pytest.raises(PopError):
             recorded.gemv_w4(x, *tiles, out, 16, 128, workspace=bad)
     assert recorded.dll.calls == 2
+
+
+def test_layers_that_lie_over_each_other_are_refused(library):
+    """Layers are moved at the same time: with less than a page between two of them a page would be moved twice. A page apart is
+    enough, as in pools that interleave the pages of the layers."""
+    from paper_2602_03295_b200 import POP_E_INVALID
+    from tests.test_tree import CALLS
+    name = "pop_k_cache_keep"
+    page = CALLS[name]["page_size"] * CALLS[name]["n_kv"] * CALLS[name]["head_dim"]
+    keep = lambda **change: getattr(library.dll, name)(*{**CALLS[name], **change}.values())  # noqa: E731
+    for stride in (0, 8, page - 8, -8, 8 - page):
+        assert keep(layer_stride=stride) == POP_E_INVALID
+        assert keep(layer_stride=stride, layers=1, max_kept=0) == 0
+    for stride in (page, -page, 1 << 40, -(1 << 63)):
+        assert keep(layer_stride=stride, max_kept=0) == 0
