@@ -185,6 +185,7 @@ int launch_tree_append(const TreeAppendArgs& a, cudaStream_t s) {
   if (reinterpret_cast<uintptr_t>(a.in) % 16 || reinterpret_cast<uintptr_t>(a.table) % 16 || a.ld_in % 4 ||
       (a.n_q > 0 && (reinterpret_cast<uintptr_t>(a.q_out) % 8 || a.ldq % 4)))
     return POP_E_INVALID;
+  if (!words_ok(a.d.cu, a.d.start, a.d.depth, a.q_gain, a.k_gain)) return POP_E_INVALID;
   if (!a.d.cu && (int64_t)a.d.batch * a.d.max_rows > a.d.rows) return POP_E_INVALID;
   if (a.n_q > 0 && a.d.rows > 1 && a.ldq < (int64_t)a.n_q * a.head_dim) return POP_E_INVALID;       // rows over each other
   if (!a.d.start && !a.d.cu && (int64_t)a.d.pos0 + a.d.max_rows > (int64_t)a.dst.max_pages * a.dst.page_size) return POP_E_NOSPACE;
@@ -216,6 +217,7 @@ int launch_cache_keep(const KeepArgs& a, cudaStream_t s) {
   if (!pages_ok(a.c) || !a.kept || a.layers < 1 || a.layers > 32767 || a.batch < 1 || a.batch > 65535 || a.n_kv < 1 ||
       a.n_kv > 1024 || a.max_kept < 0 || a.max_kept > KEEP_LIST || a.pos0 < 0 || (a.batch > 1 && a.ld_kept < a.max_kept))
     return POP_E_INVALID;
+  if (!words_ok(a.kept, a.n_kept, a.start)) return POP_E_INVALID;
   if (a.head_dim != 64 && a.head_dim != 128 && a.head_dim != 256) return POP_E_INVALID;
   const int64_t page = (int64_t)a.c.page_size * a.n_kv * a.head_dim;
   if (a.layers > 1 && (a.layer_stride % 8 || (a.layer_stride > -page && a.layer_stride < page))) return POP_E_INVALID;  // layers over each other

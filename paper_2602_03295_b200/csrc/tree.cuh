@@ -13,8 +13,11 @@ struct Pages {
   const int32_t* table;                // [batch][max_pages]
   int page_size, num_pages, max_pages;
 };
+// arrays of 32-bit words (null ones too) begin at one
+template <typename... T>
+inline bool words_ok(const T*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 3) == 0; }
 inline bool pages_ok(const Pages& c) {
-  return c.k && c.v && c.table && page_size_ok(c.page_size) && c.num_pages >= 1 && c.max_pages >= 1 &&
+  return c.k && c.v && c.table && words_ok(c.table) && page_size_ok(c.page_size) && c.num_pages >= 1 && c.max_pages >= 1 &&
          reinterpret_cast<uintptr_t>(c.k) % 16 == 0 && reinterpret_cast<uintptr_t>(c.v) % 16 == 0;
 }
 

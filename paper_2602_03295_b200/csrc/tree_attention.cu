@@ -868,7 +868,7 @@ int launch_tree_attention(const TreeAttnArgs& a, cudaStream_t s) {
     return POP_E_INVALID;
   if (a.head_dim != 64 && a.head_dim != 128 && a.head_dim != 256) return POP_E_INVALID;
   if (reinterpret_cast<uintptr_t>(a.q) % 16 || reinterpret_cast<uintptr_t>(a.out) % 16 || a.ldq % 8 || a.ldo % 8 ||
-      reinterpret_cast<uintptr_t>(a.workspace) % 16)
+      reinterpret_cast<uintptr_t>(a.workspace) % 16 || !words_ok(a.d.cu, a.d.start, a.d.depth, a.mask))
     return POP_E_INVALID;
   if (!a.d.cu && (int64_t)a.d.batch * a.d.max_rows > a.d.rows) return POP_E_INVALID;
   if (a.mask && (int64_t)a.mask_words * 32 < a.d.max_rows) return POP_E_INVALID;

@@ -62,3 +62,19 @@ def test_layers_that_lie_over_each_other_are_refused(library):
         assert keep(layer_stride=stride, layers=1, max_kept=0) == 0
     for stride in (page, -page, 1 << 40, -(1 << 63)):
         assert keep(layer_stride=stride, max_kept=0) == 0
+
+
+def test_masks_and_vectors_off_their_words_are_refused(library):
+    """Arrays of 32-bit words are read as such: an address between two of them is no address of one."""
+    from paper_2602_03295_b200 import POP_E_INVALID
+    from tests.test_tree import A, CALLS
+    arrays = {"pop_k_rope_cache_tree": ("cu_rows", "start", "depth", "block_table", "q_gain", "k_gain"),
+              "pop_k_tree_attention": ("cu_rows", "start", "depth", "block_table", "mask"),
+              "pop_k_cache_keep": ("kept", "n_kept", "start", "block_table")}
+    for call, names in arrays.items():
+        for name in names:
+            for off in (1, 2, 3):
+                args = {**CALLS[call], name: A + off}
+                if name == "mask":
+                    args["mask_words"] = 1
+                assert getattr(library.dll, call)(*args.values()) == POP_E_INVALID, (call, name, off)
