@@ -384,7 +384,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     Walk kw, vw;
     kw.begin(p, plan);
     vw = kw;
-    const int loads = BKV / p.rows_per_load, log_loads = loads == 1 ? 0 : loads == 2 ? 1 : 2;
+    const int log_rows = p.rows_per_load == 64 ? 6 : p.rows_per_load == 32 ? 5 : 4, log_loads = 6 - log_rows, loads = 1 << log_loads;
     int ring = 0, items = 0;
     bool ok = true;
     // Pages of the next 32 loads of a sequence, an entry per lane, and of the 32 behind them
@@ -392,8 +392,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       int b = -1, first = 0, pg0 = 0, pg1 = 0;
     } k_ahead, v_ahead;
     auto entry = [&](const Walk& w, int load) {
-      const int at = load * p.rows_per_load;
-      return at < w.x.start + w.x.n ? __ldg(p.a.c.table + (int64_t)w.b * p.a.c.max_pages + at / p.a.c.page_size) : 0;
+      const int at = load << log_rows;
+      return at < w.x.start + w.x.n ? __ldg(p.a.c.table + (int64_t)w.b * p.a.c.max_pages + (uint32_t)at / (uint32_t)p.a.c.page_size) : 0;
     };
     auto load_tile = [&](const Walk& w, Ahead& ahead, const CUtensorMap* tm) {
       const int stage = ring % STAGES;
@@ -410,10 +410,10 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         ahead.pg0 = ahead.pg1;
         ahead.pg1 = entry(w, ahead.first + 32 + lane);
       }
-      const int kv0 = w.j * BKV, live = min(loads, (w.x.start + w.x.n - kv0 + p.rows_per_load - 1) / p.rows_per_load);
+      const int kv0 = w.j * BKV, live = min(loads, (w.x.start + w.x.n - kv0 + p.rows_per_load - 1) >> log_rows);
       // Pages in front of every row's window may have been given back: they are not looked at. What the ring has in their
       // places is masked (K) and cleared (V); the load that has the window's first position is always among the live ones.
-      const int from = p.a.window > 0 ? max(0, max(0, w.x.start - p.a.window + 1) - kv0) / p.rows_per_load : 0;
+      const int from = p.a.window > 0 ? max(0, max(0, w.x.start - p.a.window + 1) - kv0) >> log_rows : 0;
       if (!mbar_wait_relaxed(&s.kv_empty[stage], phase ^ 1)) {
         ok = false;
         return;
@@ -427,7 +427,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
           if ((unsigned)page >= (unsigned)p.a.c.num_pages) atomicMin(p.status, (int)POP_E_INVALID);
           for (int c = 0; c < HD / 64; ++c)
             tma_load_4d(s.kv[stage] + c * C::KV_SUB_BYTES + r * p.rows_per_load * 128, tm, &s.kv_full[stage], c * 64,
-                        w.kvh, (kv0 + r * p.rows_per_load) % p.a.c.page_size, page);
+                        w.kvh, (uint32_t)(kv0 + r * p.rows_per_load) % (uint32_t)p.a.c.page_size, page);
         }
       }
     };
