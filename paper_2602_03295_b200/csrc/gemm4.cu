@@ -192,15 +192,15 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant
   } else if (warp < SPREAD) {
     // the codes of a tile of 16 rows, which are in this warp's quarter of TMEM
     const int quarter = warp & 3, half = warp >> 2;
-    for (int f = 0; f < n_steps && ok && !s.abort; ++f) {
+    for (int f = 0; f < n_steps; ++f) {
       const int stage = f % STAGES;
       ok = wait(&s.full[stage], (f / STAGES) & 1);
-      if (!ok) break;
       const uint8_t* src = ring + stage * C::STAGE + C::CODES + (2 * quarter + half) * 2048 + lane * 16;
       uint4 w[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = *reinterpret_cast<const uint4*>(src + i * 512);
-      if (f >= 2) ok = wait(&s.a_free[f & 1], ((f >> 1) - 1) & 1);
+      if (f >= 2 && ok) ok = wait(&s.a_free[f & 1], ((f >> 1) - 1) & 1);
+      ok = warp_agrees(ok);                             // a role whose work has stopped ends at its own limit
       if (!ok) break;
       tc_fence_after();
 #pragma unroll
@@ -231,11 +231,11 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant
 #pragma unroll
     for (int i = 0; i < C::COLS / 2; ++i) acc[i] = make_float2(0.f, 0.f);
     int buf = 0, turn = 0;
-    for (int f = 0; f < n_steps && ok && !s.abort; ++f) {
+    for (int f = 0; f < n_steps && ok; ++f) {
       const int stage = f % STAGES;
       const uint8_t* base = ring + stage * C::STAGE;
       const float* sums = reinterpret_cast<const float*>(base + C::SUMS) + col;
-      ok = wait(&s.full[stage], (f / STAGES) & 1);
+      const bool here = wait(&s.full[stage], (f / STAGES) & 1);
 #pragma unroll 1
       for (int g0 = 0; g0 < 2 * GPC && ok; g0 += C::BATCH) {
         float2 sc2[C::BATCH], z2[C::BATCH];
@@ -249,7 +249,7 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant
           sc2[b] = make_float2(scale, scale);
           z2[b] = make_float2(z, z);
         }
-        ok = wait(&s.d_full[buf], turn & 1);
+        ok = warp_agrees(here && wait(&s.d_full[buf], turn & 1));
         if (!ok) break;
         tc_fence_after();
         // as many sums at once as registers have room for

@@ -218,7 +218,7 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
             if (lane == 0 && nc > 0)
               bulk_load(smem_u32(s_sum), p.xq + (int64_t)COLS * p.kt * 256 + (int64_t)c0 * (1 + GPC) * COLS * 4, sums, b);
           }
-          if (!mbar_wait(s_bar + WARPS * RING, x_phase)) ok = false;
+          if (!warp_agrees(mbar_wait(s_bar + WARPS * RING, x_phase))) ok = false;
           x_phase ^= 1;
         } else {
         const int h = lane & 15;
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(WARPS * 32, 2) gemv4_kernel(const __grid_const
         const uint8_t* x_at = xp + s0 * xstep;
         const float* sum_at = s_sum + t * 2 + s0 * ((1 + GPC) * COLS);
         for (int s = s0; s < se; s += SLOT) {
-          if (!mbar_try_wait(s_bar + wic * RING + slot, phase) && !mbar_wait(s_bar + wic * RING + slot, phase)) {
+          if (!warp_agrees(mbar_try_wait(s_bar + wic * RING + slot, phase) || mbar_wait(s_bar + wic * RING + slot, phase))) {
             ok = false;
             break;
           }

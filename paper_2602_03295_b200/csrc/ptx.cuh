@@ -99,6 +99,10 @@ __device__ __forceinline__ bool mbar_wait_relaxed(uint64_t* bar, uint32_t parity
   }
 }
 
+// For a warp that goes on together into aligned instructions (tcgen05 loads and stores, warp-level products) or shuffles: each
+// lane leaves its polls by itself; the vote joins the lanes again and gives them one answer, where a limit ran out too.
+__device__ __forceinline__ bool warp_agrees(bool came) { return __all_sync(0xffffffffu, came); }
+
 // A kernel of this library does nothing once the status word is raised: after one kernel gave up
 // on a wait, the launches queued behind it return at once instead of each running into its own
 // limit. Thread 0 samples the word, so every thread of the CTA takes the same branch.

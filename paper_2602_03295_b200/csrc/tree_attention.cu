@@ -414,7 +414,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       // Pages in front of every row's window may have been given back: they are not looked at. What the ring has in their
       // places is masked (K) and cleared (V); the load that has the window's first position is always among the live ones.
       const int from = p.a.window > 0 ? max(0, max(0, w.x.start - p.a.window + 1) - kv0) >> log_rows : 0;
-      if (!mbar_wait_relaxed(&s.kv_empty[stage], phase ^ 1)) {
+      if (!warp_agrees(mbar_wait_relaxed(&s.kv_empty[stage], phase ^ 1) && !s.abort)) {
         ok = false;
         return;
       }
@@ -432,7 +432,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       }
     };
     auto load_q = [&](const Walk& w) {
-      if (items > 0 && !mbar_wait_relaxed(&s.q_empty, (items - 1) & 1)) {
+      if (items > 0 && !warp_agrees(mbar_wait_relaxed(&s.q_empty, (items - 1) & 1))) {
         ok = false;
         return;
       }
@@ -453,7 +453,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     };
     load_k();
     if (ok && kf < n_tiles) load_k();
-    for (int f = 0; f < n_tiles && ok && !s.abort; ++f) {
+    for (int f = 0; f < n_tiles && ok; ++f) {
       load_tile(vw, v_ahead, &tmV);
       vw.next(p);
       if (ok && kf < n_tiles) load_k();
@@ -534,9 +534,9 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     const uint32_t s_addr = tmem_base + lane_addr;
     const uint32_t o_addr = tmem_base + lane_addr + C::O_COL + half * (HD / HALVES);
     bool ok = true;
-    auto wait_pv = [&](int f) { return mbar_wait(&s.pv_done[f & 1], (f >> 1) & 1); };
+    auto wait_pv = [&](int f) { return warp_agrees(mbar_wait(&s.pv_done[f & 1], (f >> 1) & 1)); };
     int f = 0;
-    while (f < n_tiles && ok && !s.abort) {
+    while (f < n_tiles && ok) {
       // ---- a segment: the tiles of one item that lie in this stretch
       const Seq x = w.x;
       const int kvh = w.kvh, j0 = w.j, nt = w.j_end - w.j, i = w.q0 + ip;
@@ -570,7 +570,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             vis[KEYS / 32 - 1] = (uint32_t)(v >> 32);
           }
         }
-        if (!mbar_wait(&s.s_full[f & 1], (f >> 1) & 1)) { ok = false; break; }
+        if (!warp_agrees(mbar_wait(&s.s_full[f & 1], (f >> 1) & 1) && !s.abort)) { ok = false; break; }
         if (!idle) {
           tc_fence_after();
           float sv[KEYS];
@@ -647,7 +647,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         // that 0 * garbage cannot reach the accumulator. V_f is entry min(f + 2, n_tiles) + f of the ring.
         if (warp < 2 && (kv0 + BKV > len || kv0 < win_lo)) {
           const int rv = min(f + 2, n_tiles) + f;
-          if (!mbar_wait(&s.kv_full[rv % STAGES], (rv / STAGES) & 1)) { ok = false; break; }
+          if (!warp_agrees(mbar_wait(&s.kv_full[rv % STAGES], (rv / STAGES) & 1))) { ok = false; break; }
           if (kv0 + row >= len || kv0 + row < win_lo) {
 #pragma unroll 1
             for (int c = 0; c < HD / 64; ++c) {
@@ -662,7 +662,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.p_ready[f & 1]);
       }
-      if (!ok || s.abort) break;
+      if (!ok) break;
       if (!wait_pv(f - 1)) { ok = false; break; }
       if (!idle) {
         tc_fence_after();
