@@ -64,6 +64,7 @@ struct __align__(1024) TreeSmem {
   uint64_t pv_done[2];          // O += P V complete
   float half_max[2][2][128];    // [tile & 1][half of its keys][row]
   float half_sum[128];
+  volatile uint32_t half_lost[4][2];      // [quarter][meeting & 1]: a half of the rows has given up
   Plan plan;
   uint32_t tmem_base;
   uint32_t raised;
@@ -349,6 +350,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         mbar_init(&s.pv_done[i], 1);
       }
       s.abort = 0;
+      for (int i = 0; i < 8; ++i) s.half_lost[i >> 1][i & 1] = 0;
       fence_barrier_init();
       prefetch_tmap(&tmQ);
       prefetch_tmap(&tmK);
@@ -534,6 +536,15 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     const uint32_t s_addr = tmem_base + lane_addr;
     const uint32_t o_addr = tmem_base + lane_addr + C::O_COL + half * (HD / HALVES);
     bool ok = true;
+    // Where two warps share rows, they meet at a barrier that knows no limit: neither leaves except behind a meeting, at which each
+    // tells whether it goes on. The word of a meeting is written again two meetings later, when the other half has read it.
+    int meetings = 0;
+    auto meet = [&](bool fine) {
+      volatile uint32_t& lost = s.half_lost[quarter][meetings++ & 1];
+      if (!fine) lost = 1;
+      named_sync(PAIR_BAR + quarter, 64);
+      return lost == 0;
+    };
     auto wait_pv = [&](int f) { return warp_agrees(mbar_wait(&s.pv_done[f & 1], (f >> 1) & 1)); };
     int f = 0;
     while (f < n_tiles && ok) {
@@ -544,6 +555,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       const int slot = 2 * (int)blockIdx.x + (f > 0 ? 1 : 0);
       const bool used = ip < p.per && i < x.n;
       const bool idle = !__any_sync(0xffffffffu, used);   // a warp without rows only keeps the barriers going
+      const bool paired = HALVES == 2 && !idle;
       const int64_t prow = (int64_t)x.row0 + i;
       const int depth = !used || p.a.window == 0 ? 0 : p.a.d.depth ? min(max(__ldg(p.a.d.depth + prow), 0), 0xffff) : i;
       const int win_lo = p.a.window > 0 ? x.start - p.a.window + 1 : 0;      // in front of every row's window
@@ -570,7 +582,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             vis[KEYS / 32 - 1] = (uint32_t)(v >> 32);
           }
         }
-        if (!warp_agrees(mbar_wait(&s.s_full[f & 1], (f >> 1) & 1) && !s.abort)) { ok = false; break; }
+        if (ok) ok = warp_agrees(mbar_wait(&s.s_full[f & 1], (f >> 1) & 1) && !s.abort);
+        if (!ok && !paired) break;
         if (!idle) {
           tc_fence_after();
           float sv[KEYS];
@@ -596,7 +609,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             // the other half's maximum; behind this barrier both halves have their scores, and P may overwrite them
             s.half_max[f & 1][half][row] = mine;
             tc_fence_before();
-            named_sync(PAIR_BAR + quarter, 64);
+            ok = meet(ok);
+            if (!ok) break;
             tc_fence_after();
             mine = fmaxf(mine, s.half_max[f & 1][half ^ 1][row]);
           }
@@ -606,7 +620,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             // the maximum grew by more than 2^8 somewhere in these rows: bring the accumulator to the new one
             const float factor = (m_new == -INFINITY) ? 1.0f : ex2(m_run - m_new);   // ex2(-inf) = 0
             if (jj > 0) {
-              if (!wait_pv(f - 1)) { ok = false; break; }
+              ok = wait_pv(f - 1);
+              if (!ok && !paired) break;
               tc_fence_after();
 #pragma unroll 1
               for (int c = 0; c < HD / HALVES / 32; ++c) {
@@ -647,7 +662,8 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         // that 0 * garbage cannot reach the accumulator. V_f is entry min(f + 2, n_tiles) + f of the ring.
         if (warp < 2 && (kv0 + BKV > len || kv0 < win_lo)) {
           const int rv = min(f + 2, n_tiles) + f;
-          if (!warp_agrees(mbar_wait(&s.kv_full[rv % STAGES], (rv / STAGES) & 1))) { ok = false; break; }
+          if (ok) ok = warp_agrees(mbar_wait(&s.kv_full[rv % STAGES], (rv / STAGES) & 1));
+          if (!ok && !paired) break;
           if (kv0 + row >= len || kv0 + row < win_lo) {
 #pragma unroll 1
             for (int c = 0; c < HD / 64; ++c) {
@@ -662,18 +678,19 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         __syncwarp();
         if (lane == 0) mbar_arrive(&s.p_ready[f & 1]);
       }
-      if (!ok) break;
-      if (!wait_pv(f - 1)) { ok = false; break; }
+      if (ok) ok = wait_pv(f - 1);
+      if (!ok && !paired) break;
       if (!idle) {
         tc_fence_after();
         if constexpr (HALVES == 2) {                      // the sum of both halves, the first half's first
           if (half == 1) s.half_sum[row] = l_run;
-          named_sync(PAIR_BAR + quarter, 64);
+          ok = meet(ok);
+          if (!ok) break;
           if (half == 0) {
             l_run += s.half_sum[row];
             s.half_sum[row] = l_run;
           }
-          named_sync(PAIR_BAR + quarter, 64);
+          meet(true);
           l_run = s.half_sum[row];
         }
         const bool none = l_run == 0.f;                   // a row that sees nothing is a row of zeros
@@ -713,8 +730,6 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       // the next item's first product overwrites O: it waits for P of all warps, which they write after this
     }
     if (!ok) TREE_ABORT(s, p.status);
-    // the other half may be waiting for this one; it looks at abort next
-    if (HALVES == 2 && __any_sync(0xffffffffu, s.abort != 0)) named_arrive(PAIR_BAR + quarter, 64);
   }
 
   // ------------------------------------------------------------------ teardown
