@@ -416,7 +416,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
       // Pages in front of every row's window may have been given back: they are not looked at. What the ring has in their
       // places is masked (K) and cleared (V); the load that has the window's first position is always among the live ones.
       const int from = p.a.window > 0 ? max(0, max(0, w.x.start - p.a.window + 1) - kv0) >> log_rows : 0;
-      if (!warp_agrees(mbar_wait_relaxed(&s.kv_empty[stage], phase ^ 1) && !s.abort)) {
+      if (!warp_agrees(mbar_wait_relaxed(&s.kv_empty[stage], phase ^ 1))) {
         ok = false;
         return;
       }
@@ -582,7 +582,7 @@ tree_attn_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             vis[KEYS / 32 - 1] = (uint32_t)(v >> 32);
           }
         }
-        if (ok) ok = warp_agrees(mbar_wait(&s.s_full[f & 1], (f >> 1) & 1) && !s.abort);
+        if (ok) ok = warp_agrees(mbar_wait(&s.s_full[f & 1], (f >> 1) & 1));
         if (!ok && !paired) break;
         if (!idle) {
           tc_fence_after();
