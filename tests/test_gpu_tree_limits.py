@@ -139,3 +139,23 @@ def test_packed_weights_are_there(L):
                 made = stream.query()
             torch.cuda.synchronize()
             assert made
+
+
+# ---------------------------------------------------------------------------------------------- the accepted path
+def test_lists_of_paths_with_a_row_stride(L):
+    """Lists that are columns of a wider tensor; what lies behind a sequence's list is not looked at."""
+    starts, kept = [100, 31, 64, 7], [[1, 2, 5], [], [0, 1, 7], [4, 6]]
+    k, v, table = base.pools(7, 4, 120, 2, 64, 16, layers=2)
+    wide = torch.full((4, 9), -5, dtype=torch.int32)
+    for b, x in enumerate(kept):
+        wide[b, :len(x)] = torch.tensor(x, dtype=torch.int32)
+    lists = wide.cuda()[:, :3]
+    assert lists.stride() == (9, 1)
+    kd, vd = k.cuda(), v.cuda()
+    L.cache_keep(kd, vd, table.cuda(), lists, start=int32(starts), n_kept=int32([len(x) for x in kept]))
+    for pool, got in ((k, kd), (v, vd)):
+        want = pool.clone()
+        for b, (s, x) in enumerate(zip(starts, kept)):
+            src, dst = base.places(table, b, s + torch.tensor(x).long(), 16), base.places(table, b, s + torch.arange(len(x)), 16)
+            want[:, dst[0], dst[1]] = pool[:, src[0], src[1]]
+        assert torch.equal(got.cpu(), want)
