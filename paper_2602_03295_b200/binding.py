@@ -794,9 +794,11 @@ def unpack_w4(codes, scales, zeros, n, k):
 def tree_mask(parents, cu_rows=None):
     """(mask int32 [rows, words], depth int32 [rows]) of drafted trees, on the CPU. parents: for each packed row the row of its
     sequence that it follows (smaller than its own), or -1 for the last cached token; cu_rows: the sequences' first rows and
-    the end (one sequence if not given). A row sees itself and the rows on its way up."""
+    the end (one sequence if not given). A row sees itself and the rows on its way up; one of no sequence sees nothing."""
     parents = [int(v) for v in parents]
     cu = [0, len(parents)] if cu_rows is None else [int(v) for v in cu_rows]
+    if cu != sorted(cu) or (cu and (cu[0] < 0 or cu[-1] > len(parents))):
+        raise PopError(POP_E_INVALID, f"tree_mask: cu_rows has to rise within the {len(parents)} rows")
     words = max([1] + [-(-(b - a) // 32) for a, b in zip(cu, cu[1:])])
     mask, depth = torch.zeros(len(parents), words, dtype=torch.int64), torch.zeros(len(parents), dtype=torch.int32)
     for a, b in zip(cu, cu[1:]):

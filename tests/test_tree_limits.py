@@ -78,3 +78,13 @@ def test_masks_and_vectors_off_their_words_are_refused(library):
                 if name == "mask":
                     args["mask_words"] = 1
                 assert getattr(library.dll, call)(*args.values()) == POP_E_INVALID, (call, name, off)
+
+
+def test_prefix_sums_of_trees_that_leave_the_rows_are_refused():
+    """Sequences lie one behind the other within the rows; rows of no sequence see nothing."""
+    from paper_2602_03295_b200 import PopError, tree_mask
+    mask, depth = tree_mask([-1, -1, 0, -1], [1, 1, 3])
+    assert mask.tolist() == [[0], [1], [3], [0]] and depth.tolist() == [0, 0, 1, 0]
+    for cu in ([0, 5], [-1, 3], [0, 3, 2], [2, 0], [0, 2, 9]):
+        with pytest.raises(PopError):
+            tree_mask([-1, -1, 0, -1], cu)
