@@ -294,9 +294,10 @@ int pop_k_attention_e4m3(const void* q, int64_t ldq, const int32_t* cu_rows, int
  * multiples of 8), B up to 65535 (made for 1 to some dozens of rows). Modes as pop_k_gemv: 0 fp32 store, 2 fp32 +=, 3 gated -> bf16
  * (N a multiple of 256: 128 gate rows, then the 128 matching up rows; act 0 SiLU, 1 tanh-GELU). The products of
  * codes and activations are exact (of activations within 2^-28 of the largest of their 128 inputs; smaller ones are off by at
- * most 2^-36 of it); sums are fp32, in an order that depends on the sizes alone. An activation row with an infinite or NaN
- * input gives a row of NaN. Weights are read ahead, before the kernel in front of the call on the stream has ended (as
- * pop_k_gemv reads its own): whoever writes them on the GPU synchronises before the first call that uses them. */
+ * most 2^-36 of it); sums are fp32, in an order that depends on the sizes alone, in units of 2^-24 (results below 2^-101 lose
+ * digits, as subnormals do). An activation row with an infinite or NaN input gives a row of NaN. Weights are read ahead, before
+ * the kernel in front of the call on the stream has ended (as pop_k_gemv reads its own): whoever writes them on the GPU
+ * synchronises before the first call that uses them. */
 int pop_k_gemv_w4(const void* x, int64_t ldx, const void* codes, const void* scales, const void* zeros, int32_t group,
                   void* workspace, size_t workspace_bytes, void* out, int64_t ldo, int32_t B, int32_t N, int32_t K,
                   int32_t mode, int32_t act, int32_t n_valid, void* stream);
@@ -322,8 +323,10 @@ int pop_k_rope_cache_tree(const void* in, int32_t in_bf16, int64_t ld_in, int32_
                           int32_t n_kv, int32_t head_dim, void* stream);
 
 /* Workspace of the call below: device memory, 16-byte aligned, contents irrelevant before and after. This size covers every
- * call; a smaller one is refused with POP_E_NOSPACE where the call needs more. Calls that may overlap on the GPU (other
- * streams, concurrently replayed graphs) need one each. */
+ * call. How much a call asks for depends on head_dim, batch and the GPU's SMs and not on lengths, so that a call that is taken
+ * for one length is taken for all; a smaller one, or NULL, is refused with POP_E_NOSPACE (calls of a few short sequences ask
+ * for it too, though they leave it as it is). Calls that may overlap on the GPU (other streams, concurrently replayed graphs)
+ * need one each. */
 #define POP_TREE_WORKSPACE_BYTES (64 * 1024 * 1024)
 
 /* Attention of drafted rows over the paged cache (one layer) that has them already: packed rows, cu_rows, max_rows and start
@@ -335,7 +338,9 @@ int pop_k_rope_cache_tree(const void* in, int32_t in_bf16, int64_t ld_in, int32_
  * q bf16 [rows][ldq], out bf16 [rows][ldo] (strides multiples of 8, at least n_q hd; 16-byte aligned), n_q / n_kv <= 128,
  * batch <= 4096, hd 64, 128 or 256. A row that sees nothing becomes zeros; rows of no sequence are left as they are. Positions
  * behind a sequence's rows and in front of every row's window may hold anything, their block-table entries too where a whole
- * page does. An infinite or NaN value in a drafted slot may reach rows of the sequence that do not see the slot. Unequal
+ * page does. An infinite or NaN value in a drafted slot, or in a position that is in front of some rows' windows, may reach rows
+ * of the sequence that do not see it. Scores, maxima and sums are fp32; the softmax's weights enter the product with V as bf16
+ * (the sum that divides takes them before that rounding), as in the library's other attention calls over bf16. Unequal
  * lengths are shared out over the whole GPU; results do not depend on scheduling. The key tiles of 64 positions of the call,
  * batch n_kv ceil(max_rows / rows per tile) ceil((max_start + max_rows) / 64), are at most 2^30 (POP_E_INVALID otherwise). */
 int pop_k_tree_attention(const void* q, int64_t ldq, int32_t rows, const int32_t* cu_rows, int32_t max_rows,

@@ -9,16 +9,16 @@
 //   scale (2^-shift sum - zero sum_k x_k).
 // The CTAs of a cluster have the same tile (gated: its gate and its up tile) and a part of the inputs each, and join their sums
 // through distributed shared memory, in the order of the parts.
-// Warps of a CTA, which has an SM to itself (two smaller ones per SM, a chunk a step: 12 x 14336 -> 4096 20.9 us against 18.4,
-// 64 x 4096 -> 6144 20.0 against 15.2; what a step costs beside its work is many waits):
+// Warps of a CTA, which has an SM to itself (two smaller ones per SM, a chunk a step, took 14 % more for 12 x 14336 -> 4096 and 32 %
+// more for 64 x 4096 -> 6144; what a step costs beside its work is many waits):
 //   8 warps: the codes of a step of two chunks, a tile of 16 rows each, to TMEM;
 //   8 warps: the sums of the groups from TMEM, 32 rows and half of the columns each;
 //   1 warp: copies of codes, scales, zeros (a tensor map each: a copy per 16 rows made the copying warp the slowest of all, at 72
 //       clocks an instruction) and activations with their sums, through a ring of steps
-//       (activations converted here instead, for 12 x 14336 -> 4096: by the first eight warps 22.6 us, by four more 26.5, against 16.7);
+//       (activations converted here instead: 29 % more for 12 x 14336 -> 4096 by the first eight warps, 51 % more by four others);
 //   1 or 2 warps: the products.
 // A step takes 1250 clocks with 16 columns: the codes are four times their bytes as f16, 64 KB that are written to TMEM and read
-// from it; with 64 columns 2000, the sums' arithmetic.
+// from it; with 64 columns 2000, the sums' arithmetic. us: 12 x 14336 -> 4096 16.8, 64 x 4096 -> 6144 15.0, with groups of 32 31.6.
 #include "common.cuh"
 #include "ptx.cuh"
 #include "w4.cuh"
@@ -145,8 +145,8 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tm_codes, const __grid_constant
   tc_fence_after();
   const uint32_t tmem = s.tmem_base;
   bool ok = true;
-  // A test that does not suspend sees a complete barrier earlier (12 x 14336 -> 4096 17.7 us against 18.4, 32 x 4096 -> 6144 11.4
-  // against 12.1); with 64 columns the longer code costs more than it gives (groups of 32: 35.3 against 32.6)
+  // A test that does not suspend sees a complete barrier earlier (4 % of 12 x 14336 -> 4096, 6 % of 32 x 4096 -> 6144); with 64
+  // columns the longer code costs more than it gives (8 % with groups of 32)
   auto wait = [](uint64_t* bar, uint32_t parity) { return (NB < 64 && mbar_test(bar, parity)) || mbar_wait(bar, parity); };
 
   float2 acc[C::COLS / 2];
@@ -425,7 +425,7 @@ int launch_t(const Gemv4Args& a, G4Dev& p, cudaStream_t s) {
   const int each = p.mode == 3 ? 2 : 1, units = ceil_div(p.N, 128 * each), slabs = ceil_div(p.B, NB);
   if (slabs > 65535 || (int64_t)units * each * 8 > 0x7fffffff) return POP_E_INVALID;
   // parts of the inputs: waves of clusters, each of its chunks and of what a CTA costs beside them, in chunks. us in 1 / 2 / 4 / 5
-  // parts: 12 x 14336 -> 4096 45.7 / 26.4 / 18.4 / 30 (two waves), 16 x 4096 -> 6144 16.0 / 11.1 / 15.5 (two waves) / 16.1
+  // parts: 12 x 14336 -> 4096 40.2 / 23.5 / 16.9 / 27.7 (two waves), 16 x 4096 -> 6144 14.1 / 10.3 / 14.9 (two waves) / 15.7
   int64_t best = INT64_MAX;
   for (int cs = 1; cs * each <= 8 && cs <= p.steps; ++cs) {
     const int most = max_clusters<GRP, NB, ZEROS>(cs * each);

@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(256) gemv4_convert_kernel(const bf16* __restri
 // The weight rows are the M side of the warp-level MMA, 8 activation rows of a grid row its N side (many: gemm4.cu): a tile of 16 rows x 128 inputs
 // is 1 KB in one piece, 16 bytes of row g and 16 of row g + 8 to lane (g = lane / 4, t = lane % 4), word j inputs 32 j + 8 t ..
 // + 7. The chunks of a CTA's tiles are one line, of which each warp streams an equal stretch through a ring of its own; bulk
-// copies keep more bytes in flight than loads to registers (1 x 4096 -> 128256: 46 us, 5.8 TB/s, against 55). Where there are
+// copies keep more bytes in flight than loads to registers (1 x 4096 -> 128256: 47 us, 5.7 TB/s; loads took a fifth more). Where there are
 // fewer tiles than CTAs, or many rows to convert, the CTAs of a cluster have the same tiles and a part of the inputs each. The
 // loop over the chunks stays rolled: each launch meets its instructions cold (unrolled four times: 0.5 to 1 us more a call).
 // What a call costs beside its bytes, 1 x 4096 -> 4096 (4.9 us; the bytes take 1.3): launch, 0.5 us to the first copy, 0.9
@@ -457,7 +457,7 @@ int launch_t(Gemv4Dev& p, cudaStream_t s) {
   p.rows = p.B < COLS ? p.B : COLS;
   const int slabs = ceil_div(p.B, COLS), room = SMEM_LIMIT - FIXED, acc_bytes = p.rows * 64, sc_bytes = p.rows * 256 + COLS * (4 + 4 * GPC);
   // Work of an SM with two CTAs, in clocks as measured: 30 to convert a row's chunk, 47 for a tile's chunk, the exchange within
-  // a cluster. us in clusters of 1 / 2 / 8: 1 x 4096 -> 28672 gated 14.8 / 16.0 / 21.2, 1 x 14336 -> 4096 11.4 / 11.4 / 15.0.
+  // a cluster. us in clusters of 1 / 2 / 8: 1 x 4096 -> 28672 gated 15.1 / 17.1 / 20.0, 1 x 14336 -> 4096 11.2 / 12.3 / 14.0.
   // A pass over part of the inputs, or a round over part of the tiles, costs 6000 more.
   const int each = p.mode == 3 ? 2 : 1, want = p.tiles / each;
   int64_t best = INT64_MAX;
@@ -496,9 +496,9 @@ int launch_t(Gemv4Dev& p, cudaStream_t s) {
 }
 
 // Whether each CTA converts the activations that it needs, 8 rows at a time, and no launch of its own does it before. us so / by a
-// launch: 3 x 2048 -> 4096 4.7 / 4.9, 8 x 1024 -> 4096 5.1 / 4.8, 8 x 2048 -> 4096 6.9 / 5.3, and beyond 8 rows, where weights are
-// read again for each 8 and the other products begin, 16 x 1024 -> 4096 5.7 / 6.2, 64 x 512 -> 512 3.9 / 8.1, 32 x 1024 -> 4096 6.5 /
-// 7.2, 32 x 2048 -> 4096 9.9 / 8.1, 16 x 2048 -> 4096 7.5 / 6.7. A call of two launches takes 4 us more of the host.
+// launch: 3 x 2048 -> 4096 4.5 / 5.1, 8 x 1024 -> 4096 4.6 / 4.6, 8 x 2048 -> 4096 6.3 / 5.5, and beyond 8 rows, where weights are
+// read again for each 8 and the other products begin, 16 x 1024 -> 4096 5.0 / 6.0, 64 x 512 -> 512 3.9 / 6.5, 32 x 1024 -> 4096 5.9 /
+// 6.4, 32 x 2048 -> 4096 9.2 / 7.7, 16 x 2048 -> 4096 7.1 / 6.9. A call of two launches takes 4 us more of the host.
 bool converts_itself(int B, int N, int K) {
   if (B < 3) return true;
   if (B <= COLS) return (int64_t)B * ceil_div(K, 128) <= 64;

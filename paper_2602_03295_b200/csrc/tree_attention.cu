@@ -10,7 +10,7 @@
 //   4 softmax warps, a thread per (row, head): scores of 64 keys from TMEM, mask, maximum, exponentials, P in bf16 back over
 //       the scores. These dependent steps (1700 clocks) are what a CTA waits for; where a second CTA shares the SM that is
 //       hidden, else (hd 256) 8 warps take half of the keys each, and join their maxima through shared memory (16 x 12 rows,
-//       window 1024: 45 us against 49; with two CTAs on the SM it costs: 24 x 27 rows of up to 12001 147 against 135);
+//       window 1024: 8 % less; with two CTAs on the SM it costs: 24 x 27 rows of up to 12001 9 % more);
 //   1 TMA warp: the CTA's place in the line, then Q of an item and K and V tiles of 64 positions through a ring, in the order in
 //       which they are used;
 //   1 MMA warp: scores two tiles ahead of the softmax, across the ends of items too, and O += P V with P from TMEM.
@@ -91,8 +91,8 @@ __host__ __device__ constexpr int part_floats(int hd) { return (hd + 4) * 128; }
 // Fewest tiles of a stretch: below, beginning and ending it costs more than its keys
 constexpr int MIN_SHARE = 2;
 // Where no item has more tiles than this and there are no more items than CTAs, each CTA has an item, and nothing is to be joined. us
-// so / in stretches: 1 x 5 rows of 50 5.6 / 10.7, 8 x 16 of up to 100 8.0 / 13.1, 1 x 5 of 180 8.3 / 11.1 (pages of 16: 10.6 / 11.0); with
-// four tiles 1 x 5 of 240 9.7 / 9.1 (14.7 / 10.9)
+// so / in stretches: 1 x 5 rows of 50 5.7 / 11.0, 8 x 16 of up to 100 8.0 / 12.8, 1 x 5 of 180 7.2 / 9.6 (pages of 16: 10.8 / 11.3); with
+// four tiles 1 x 5 of 240 8.4 / 7.8 (13.3 / 10.2)
 constexpr int WHOLE_TILES = 3;
 
 __device__ __forceinline__ Seq seq_of(const TreeDev& p, int b, bool report) {
@@ -134,7 +134,7 @@ __device__ __forceinline__ void item_of(Plan& r) {
 // the tiles of a stretch: what the second launch asks for.
 __device__ __forceinline__ Plan plan_of(const TreeDev& p, int cta, int* starts) {
   const int lane = threadIdx.x & 31, batch = p.a.d.batch;
-  if (batch == 1) {                                            // nothing to add up (1 x 5 rows of 300: 10.9 us against 11.3)
+  if (batch == 1) {                                            // nothing to add up (4 % of 1 x 5 rows of 300)
     Plan r;
     r.x = seq_of(p, 0, cta == 0 && lane == 0);
     const int total = places_of(p, r.x), share = p.whole ? 1 : max((total + p.ctas - 1) / p.ctas, MIN_SHARE);
@@ -861,9 +861,9 @@ int launch_t(const TreeAttnArgs& a, TreeDev& p, cudaStream_t s) {
   count_launch();
   if (p.whole) return POP_OK;
   const int pairs = a.d.max_rows < p.per ? a.d.max_rows * p.G : p.per * p.G;
-  // Few items of many parts are joined by more threads, which each have more loads in flight: 1 x 64 rows of 8192 27.3 us against
-  // 28.6, 1 x 16 of 2000 13.4 against 14.4. Many items (16 x 12 rows, window 1024: 48.4 against 43.1) or few parts (1 x 5 of 300: 11.3
-  // against 10.9) would lose.
+  // Few items of many parts are joined by more threads, which each have more loads in flight: 1 x 64 rows of 8192 26.8 us against
+  // 27.5, 1 x 16 of 2000 13.3 against 14.1. Many items (16 x 12 rows, window 1024: 48.2 against 43.4) or few parts (1 x 5 of 300: 11.3
+  // against 11.0) would lose.
   const int64_t share = (line + p.ctas - 1) / p.ctas;
   const bool wide = tiles > 8 * (share < MIN_SHARE ? MIN_SHARE : share) && a.n_kv * qts * (HD / 8) * a.d.batch <= 2 * device_sms();
   if (launch_chained(wide ? tree_merge_kernel<HD, 4, 16> : tree_merge_kernel<HD, 8, 8>,
