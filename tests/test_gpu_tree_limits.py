@@ -159,3 +159,35 @@ def test_lists_of_paths_with_a_row_stride(L):
             src, dst = base.places(table, b, s + torch.tensor(x).long(), 16), base.places(table, b, s + torch.arange(len(x)), 16)
             want[:, dst[0], dst[1]] = pool[:, src[0], src[1]]
         assert torch.equal(got.cpu(), want)
+
+
+# ---------------------------------------------------------------------------------------------- calls at once
+def test_calls_of_three_streams_at_once(L):
+    """Attention of two head sizes and products on tensor memory, each on a stream of its own with a workspace of its own, give the
+    bits that they give one after the other."""
+    g = base.gen(41)
+    tiles = base.laid_out(L, *base.weights(4200, 2048, 64, True, g), 64)
+    x = torch.randn(40, 2048, generator=g).to(torch.bfloat16).cuda()
+    calls = [lambda o, w, s: L.gemv_w4(x, *tiles, o, 4200, 64, workspace=w, stream=s)]
+    outs = [torch.zeros(40, 4200, device=DEV)]
+    for hd, rows, starts in ((128, [12, 30, 5], [3000, 70, 900]), (256, [9, 20], [2500, 400])):
+        k, v, table = (t.cuda() for t in base.pools(hd, len(rows), max(r + s for r, s in zip(rows, starts)), 2, hd, 64))
+        _, depth, mask = base.drafts(rows, "tree", g)
+        q = torch.randn(sum(rows), 8 * hd, generator=g).to(torch.bfloat16).cuda()
+        calls.append(lambda o, w, s, q=q, k=k, v=v, t=table, hd=hd, rows=rows, more=dict(
+            start=int32(starts), cu_rows=base.prefix(rows).cuda(), mask=mask.cuda(), depth=depth.cuda(), window=2000), top=max(starts):
+            L.tree_attention(q, k, v, t, o, 8, 2, hd, max(rows), top, workspace=w, stream=s, **more))
+        outs.append(torch.zeros_like(q))
+    spaces = [torch.empty(64 << 20, dtype=torch.uint8, device=DEV) for _ in calls]
+    for call, o, w in zip(calls, outs, spaces):
+        call(o, w, None)
+    torch.cuda.synchronize()
+    want, streams = [o.clone() for o in outs], [torch.cuda.Stream() for _ in calls]
+    for o in outs:
+        o.zero_()
+    torch.cuda.synchronize()
+    for _ in range(100):
+        for call, o, w, s in zip(calls, outs, spaces, streams):
+            call(o, w, s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
